@@ -234,6 +234,122 @@ dendsn_status dendsn_lif_backward(const dendsn_lif_config *cfg, const void *x,
                                   const void *grad_spikes, const float *grad_v,
                                   const void *saved, void *grad_x, void *stream);
 
+/*
+ * Token-sequence operators around a DendSN layer: the embedding that turns token ids into
+ * input currents, a compartment scan whose decay is an input of its own, and the softmax
+ * cross entropy of a linear readout of the spikes. Same conventions as above: device
+ * pointers, dense row-major tensors, asynchronous on `stream`, host-side validation with
+ * nothing enqueued on an error, caller-owned scratch whose contents need no initialisation,
+ * dendsn_last_error(). All sums and states are float32; a bfloat16 output is rounded once.
+ * Every result is the same for the same inputs from run to run (no floating-point atomics).
+ * Tensors are naturally aligned (one element); rows whose addresses and lengths are multiples
+ * of 16 bytes take wider loads.
+ */
+typedef enum { DENDSN_I32 = 0, DENDSN_I64 = 1 } dendsn_index;
+
+/*
+ * Embedding lookup with scaling, and its gradient.
+ *   out[i, :]        = scale * table[ids[i], :]        for 0 <= ids[i] < V
+ *   grad_table[v, :] = scale * sum of grad_out[i, :] over ids[i] = v, i ascending
+ * A token equal to padding_id gives a row of zeros and takes no part in the gradient
+ * (padding_id < 0: there is none). A token outside [0, V) gives a row of NaN and takes no
+ * part in the gradient.
+ *   table, grad_table [V, D], out, grad_out [n, D]   dtype x_dtype
+ *   ids               [n]                            dtype ids_dtype
+ *   grad_table is OVERWRITTEN: rows without tokens become zero. n >= 0, n < 2^31.
+ */
+typedef struct {
+    int64_t n;              /* tokens */
+    int64_t padding_id;     /* token id without a row, or negative: none */
+    int32_t V, D;           /* vocabulary, row length */
+    int32_t x_dtype;        /* dendsn_dtype of table, out, grad_out, grad_table */
+    int32_t ids_dtype;      /* dendsn_index of ids */
+    float scale;
+} dendsn_embed_config;
+
+/* scratch_bytes of the backward (the forward needs none). */
+dendsn_status dendsn_embed_workspace_size(const dendsn_embed_config *cfg, size_t *scratch_bytes);
+dendsn_status dendsn_embed_forward(const dendsn_embed_config *cfg, const void *table,
+                                   const void *ids, void *out, void *stream);
+dendsn_status dendsn_embed_backward(const dendsn_embed_config *cfg, const void *ids,
+                                    const void *grad_out, void *grad_table, void *scratch,
+                                    void *stream);
+
+/*
+ * Gated compartment scan: Eq. methods-compartment with a decay of its own for every channel
+ * and step (channel = one of the B * N compartments).
+ *   a[t] = gate[t] (DECAY) or 1 / (1 + exp(-gate[t])) (LOGIT)
+ *   u[t] = x[t] (PLAIN) or (1 - a[t]) x[t] (COMPLEMENT)
+ *   h[t] = a[t] h[t-1] + u[t],  h[-1] = h0
+ * starts marks the first step of each packed sequence of a sample: where it is nonzero,
+ * h[t] = u[t] whatever came before (also infinities and NaN), and no gradient passes back.
+ *   x, gate, h, grad_h, grad_x, grad_gate   [T, B, N] or [B, T, N] (layout), dtype x_dtype
+ *   starts        [T, B] or [B, T] uint8, or NULL: one sequence for each sample
+ *   h0, grad_h0   [B, N] float32, or NULL (h0 NULL: zeros)
+ *   h_last, grad_last [B, N] float32, or NULL; h_last may be h0 itself (a serving step)
+ *   saved         saved_bytes, 16-byte aligned: the states at the end of every 64 steps, written
+ *                 by the forward when not NULL and read by the backward (needed for T > 64)
+ * The backward recomputes h from x and gate. grad_gate is the gradient of gate itself.
+ * With T = 0, h_last = h0 and grad_h0 = grad_last (zeros where NULL).
+ */
+typedef enum { DENDSN_GATE_DECAY = 0, DENDSN_GATE_LOGIT = 1 } dendsn_gate;
+typedef enum { DENDSN_MIX_PLAIN = 0, DENDSN_MIX_COMPLEMENT = 1 } dendsn_mix;
+typedef enum { DENDSN_TIME_FIRST = 0, DENDSN_BATCH_FIRST = 1 } dendsn_scan_layout;
+
+typedef struct {
+    int32_t T, B, N;        /* steps, samples, channels per sample */
+    int32_t x_dtype;        /* dendsn_dtype of x, gate, h and their gradients */
+    int32_t gate;           /* dendsn_gate */
+    int32_t mix;            /* dendsn_mix */
+    int32_t layout;         /* dendsn_scan_layout */
+} dendsn_scan_config;
+
+dendsn_status dendsn_scan_workspace_size(const dendsn_scan_config *cfg, size_t *saved_bytes);
+dendsn_status dendsn_scan_forward(const dendsn_scan_config *cfg, const void *x, const void *gate,
+                                  const uint8_t *starts, const float *h0, void *h,
+                                  float *h_last, void *saved, void *stream);
+dendsn_status dendsn_scan_backward(const dendsn_scan_config *cfg, const void *x, const void *gate,
+                                   const uint8_t *starts, const float *h0, const void *grad_h,
+                                   const float *grad_last, const void *saved, void *grad_x,
+                                   void *grad_gate, float *grad_h0, void *stream);
+
+/*
+ * Softmax cross entropy of a linear readout, in pieces of the vocabulary: the logits
+ * hidden weight^T are never kept.
+ *   l[r, v] = sum_d hidden[r, d] weight[v, d];  lse[r] = log sum_v exp l[r, v]
+ *   loss[r] = lse[r] - l[r, labels[r]]
+ * and, for an upstream gradient grad_loss of the row losses,
+ *   G[r, v] = grad_loss[r] (exp(l[r, v] - lse[r]) - [v = labels[r]])
+ *   grad_hidden = G weight;  grad_weight = G^T hidden
+ * A row whose label is ignore_index has loss 0, lse 0 and zero gradient, whatever its hidden
+ * values are (also infinities and NaN). A row with any other label outside [0, V) has loss,
+ * lse and grad_hidden NaN and takes no part in grad_weight.
+ * bfloat16 inputs: products are exact and sums float32; G is rounded to bfloat16 before the
+ * two products that take it. float32 inputs: every operand is split into three bfloat16
+ * terms, whose six leading products are summed (a relative error of about 2^-24 of each
+ * product).
+ *   hidden, grad_hidden [M, D], weight, grad_weight [V, D]   dtype x_dtype
+ *   labels [M] dtype labels_dtype;  loss, lse, grad_loss [M] float32
+ *   grad_hidden and grad_weight are OVERWRITTEN. V, D >= 1; M >= 0.
+ *   scratch: 256-byte aligned; forward_bytes for the forward, backward_bytes for the backward.
+ */
+typedef struct {
+    int64_t ignore_index;
+    int32_t M, V, D;        /* rows, vocabulary, row length */
+    int32_t x_dtype;        /* dendsn_dtype of hidden, weight and their gradients */
+    int32_t labels_dtype;   /* dendsn_index of labels */
+} dendsn_xent_config;
+
+dendsn_status dendsn_xent_workspace_size(const dendsn_xent_config *cfg, size_t *forward_bytes,
+                                         size_t *backward_bytes);
+dendsn_status dendsn_xent_forward(const dendsn_xent_config *cfg, const void *hidden,
+                                  const void *weight, const void *labels, float *loss,
+                                  float *lse, void *scratch, void *stream);
+dendsn_status dendsn_xent_backward(const dendsn_xent_config *cfg, const void *hidden,
+                                   const void *weight, const void *labels, const float *lse,
+                                   const float *grad_loss, void *grad_hidden,
+                                   void *grad_weight, void *scratch, void *stream);
+
 /* Static description of a status code. */
 const char *dendsn_status_string(dendsn_status status);
 

@@ -68,6 +68,65 @@ def config_of(w) -> dendsn_config:
                        w.residual, layout=w.layout)
 
 
+I32, I64 = 0, 1
+GATE_DECAY, GATE_LOGIT = 0, 1
+MIX_PLAIN, MIX_COMPLEMENT = 0, 1
+TIME_FIRST, BATCH_FIRST = 0, 1
+
+
+class dendsn_embed_config(ctypes.Structure):
+    """Mirror of the C struct dendsn_embed_config."""
+    _fields_ = [("n", ctypes.c_int64), ("padding_id", ctypes.c_int64), ("V", ctypes.c_int32),
+                ("D", ctypes.c_int32), ("x_dtype", ctypes.c_int32),
+                ("ids_dtype", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class dendsn_scan_config(ctypes.Structure):
+    """Mirror of the C struct dendsn_scan_config (the gated compartment scan)."""
+    _fields_ = [("T", ctypes.c_int32), ("B", ctypes.c_int32), ("N", ctypes.c_int32),
+                ("x_dtype", ctypes.c_int32), ("gate", ctypes.c_int32), ("mix", ctypes.c_int32),
+                ("layout", ctypes.c_int32)]
+
+
+class dendsn_xent_config(ctypes.Structure):
+    """Mirror of the C struct dendsn_xent_config (cross entropy of a linear readout)."""
+    _fields_ = [("ignore_index", ctypes.c_int64), ("M", ctypes.c_int32), ("V", ctypes.c_int32),
+                ("D", ctypes.c_int32), ("x_dtype", ctypes.c_int32),
+                ("labels_dtype", ctypes.c_int32)]
+
+
+def _code(what, value, codes):
+    if value not in codes:
+        raise ValueError(f"{what} must be one of {sorted(codes)}, got {value!r}")
+    return codes[value]
+
+
+_DTYPES = {"f32": F32, "bf16": BF16}
+_INDEX = {"i32": I32, "i64": I64}
+
+
+def make_embed_config(n, V, D, dtype="f32", scale=1.0, padding_id=None,
+                      ids_dtype="i64") -> dendsn_embed_config:
+    """padding_id: the token whose row is zero and has no gradient; None: there is none."""
+    return dendsn_embed_config(n, -1 if padding_id is None else padding_id, V, D,
+                               _code("dtype", dtype, _DTYPES),
+                               _code("ids_dtype", ids_dtype, _INDEX), float(scale))
+
+
+def make_scan_config(T, B, N, dtype="f32", gate="decay", mix="plain",
+                     layout="time") -> dendsn_scan_config:
+    return dendsn_scan_config(T, B, N, _code("dtype", dtype, _DTYPES),
+                              _code("gate", gate, {"decay": GATE_DECAY, "logit": GATE_LOGIT}),
+                              _code("mix", mix, {"plain": MIX_PLAIN, "complement": MIX_COMPLEMENT}),
+                              _code("layout", layout, {"time": TIME_FIRST, "batch": BATCH_FIRST}))
+
+
+def make_xent_config(M, V, D, dtype="f32", ignore_index=-100,
+                     labels_dtype="i64") -> dendsn_xent_config:
+    return dendsn_xent_config(ignore_index, M, V, D, _code("dtype", dtype, _DTYPES),
+                              _code("labels_dtype", labels_dtype, _INDEX))
+
+
 class dendsn_lif_config(ctypes.Structure):
     """Mirror of the C struct dendsn_lif_config (the point-neuron LIF layer)."""
     _fields_ = [("T", ctypes.c_int32), ("B", ctypes.c_int32), ("N", ctypes.c_int32),
@@ -113,6 +172,15 @@ def load() -> ctypes.CDLL:
                        lib.dendsn_lif_workspace_size, lib.dendsn_lif_forward,
                        lib.dendsn_lif_backward):
                 fn.restype = ctypes.c_int
+            for name, cfg_t, sizes, forward, backward in (
+                    ("embed", dendsn_embed_config, 1, 4, 5), ("scan", dendsn_scan_config, 1, 8, 11),
+                    ("xent", dendsn_xent_config, 2, 7, 9)):
+                cp = ctypes.POINTER(cfg_t)
+                for fn, args in (("workspace_size", [ctypes.POINTER(ctypes.c_size_t)] * sizes),
+                                 ("forward", [P] * forward), ("backward", [P] * backward)):
+                    f = getattr(lib, f"dendsn_{name}_{fn}")
+                    f.argtypes = [cp] + args
+                    f.restype = ctypes.c_int
             lib.dendsn_status_string.argtypes = [ctypes.c_int]
             lib.dendsn_status_string.restype = ctypes.c_char_p
             lib.dendsn_last_error.argtypes = []
@@ -304,6 +372,196 @@ def lif_workspace(cfg, device=None):
     return torch.empty(sb, dtype=torch.uint8, device=device or torch.device("cuda")) if sb else None
 
 
+# ------------------------------------------------------------------ token-sequence operators
+def _expect(name, t, shape, dtype, optional=False):
+    """Refuses on the host a tensor of another shape or dtype than the config's."""
+    if t is None:
+        if optional:
+            return
+        raise ValueError(f"{name} is required")
+    if tuple(t.shape) != shape or t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
+
+
+def _idtype(code) -> torch.dtype:
+    return torch.int64 if code == I64 else torch.int32
+
+
+def _bytes(name, t, need):
+    have = 0 if t is None else t.numel() * t.element_size()
+    if have < need:
+        raise ValueError(f"{name}: {have} bytes, the config needs {need}")
+
+
+def _scratch(nbytes, device):
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+
+
+def dendsn_embed_workspace_size(cfg: dendsn_embed_config) -> int:
+    """scratch_bytes of the embedding's backward."""
+    s = ctypes.c_size_t(0)
+    _check("dendsn_embed_workspace_size",
+           load().dendsn_embed_workspace_size(ctypes.byref(cfg), ctypes.byref(s)))
+    return int(s.value)
+
+
+def dendsn_embed_forward(cfg, table, ids, out, stream=None):
+    """out = scale * table[ids]; table [V, D], ids of n tokens (any shape), out n rows of D."""
+    dt = _xdtype(cfg)
+    _expect("table", table, (cfg.V, cfg.D), dt)
+    _expect("ids", ids, tuple(ids.shape) if ids.numel() == cfg.n else (cfg.n,), _idtype(cfg.ids_dtype))
+    _expect("out", out, tuple(ids.shape) + (cfg.D,), dt)
+    _check("dendsn_embed_forward", load().dendsn_embed_forward(
+        ctypes.byref(cfg), _ptr(table), _ptr(ids), _ptr(out), _stream(stream)))
+
+
+def dendsn_embed_backward(cfg, ids, grad_out, grad_table, scratch, stream=None):
+    """grad_table [V, D] (overwritten) from grad_out, n rows of D."""
+    dt = _xdtype(cfg)
+    _expect("ids", ids, tuple(ids.shape) if ids.numel() == cfg.n else (cfg.n,), _idtype(cfg.ids_dtype))
+    _expect("grad_out", grad_out, tuple(ids.shape) + (cfg.D,), dt)
+    _expect("grad_table", grad_table, (cfg.V, cfg.D), dt)
+    _bytes("scratch", scratch, dendsn_embed_workspace_size(cfg))
+    _check("dendsn_embed_backward", load().dendsn_embed_backward(
+        ctypes.byref(cfg), _ptr(ids), _ptr(grad_out), _ptr(grad_table), _ptr(scratch),
+        _stream(stream)))
+
+
+def embed_forward(cfg, table, ids, stream=None):
+    """Allocating embedding: scale * table[ids], of shape [*ids.shape, D]."""
+    out = torch.empty(tuple(ids.shape) + (cfg.D,), dtype=table.dtype, device=table.device)
+    dendsn_embed_forward(cfg, table, ids, out, stream)
+    return out
+
+
+def embed_backward(cfg, ids, grad_out, scratch=None, stream=None):
+    """Allocating gradient of the embedding table, [V, D] in grad_out's dtype."""
+    if scratch is None:
+        scratch = _scratch(dendsn_embed_workspace_size(cfg), ids.device)
+    gtable = torch.empty((cfg.V, cfg.D), dtype=grad_out.dtype, device=grad_out.device)
+    dendsn_embed_backward(cfg, ids, grad_out, gtable, scratch, stream)
+    return gtable
+
+
+def dendsn_scan_workspace_size(cfg: dendsn_scan_config) -> int:
+    """saved_bytes of the gated scan (states every 64 steps; 0 for T <= 64)."""
+    s = ctypes.c_size_t(0)
+    _check("dendsn_scan_workspace_size",
+           load().dendsn_scan_workspace_size(ctypes.byref(cfg), ctypes.byref(s)))
+    return int(s.value)
+
+
+def _scan_expect(cfg, seq, starts, states, saved, needs_saved):
+    batch = cfg.layout == BATCH_FIRST
+    lead = (cfg.B, cfg.T) if batch else (cfg.T, cfg.B)
+    dt = _xdtype(cfg)
+    for name, t in seq.items():
+        _expect(name, t, lead + (cfg.N,), dt)
+    _expect("starts", starts, lead, torch.uint8, optional=True)
+    for name, t in states.items():
+        _expect(name, t, (cfg.B, cfg.N), torch.float32, optional=True)
+    if saved is not None or needs_saved:
+        _bytes("saved", saved, dendsn_scan_workspace_size(cfg))
+
+
+def dendsn_scan_forward(cfg, x, gate, starts, h0, h, h_last=None, saved=None, stream=None):
+    _scan_expect(cfg, dict(x=x, gate=gate, h=h), starts, dict(h0=h0, h_last=h_last), saved, False)
+    _check("dendsn_scan_forward", load().dendsn_scan_forward(
+        ctypes.byref(cfg), _ptr(x), _ptr(gate), _ptr(starts), _ptr(h0), _ptr(h), _ptr(h_last),
+        _ptr(saved), _stream(stream)))
+
+
+def dendsn_scan_backward(cfg, x, gate, starts, h0, grad_h, grad_last, saved, grad_x, grad_gate,
+                         grad_h0=None, stream=None):
+    _scan_expect(cfg, dict(x=x, gate=gate, grad_h=grad_h, grad_x=grad_x, grad_gate=grad_gate),
+                 starts, dict(h0=h0, grad_last=grad_last, grad_h0=grad_h0), saved, True)
+    _check("dendsn_scan_backward", load().dendsn_scan_backward(
+        ctypes.byref(cfg), _ptr(x), _ptr(gate), _ptr(starts), _ptr(h0), _ptr(grad_h),
+        _ptr(grad_last), _ptr(saved), _ptr(grad_x), _ptr(grad_gate), _ptr(grad_h0),
+        _stream(stream)))
+
+
+def scan_workspace(cfg, device=None):
+    """The gated scan's checkpoint buffer, or None when T <= 64."""
+    return _scratch(dendsn_scan_workspace_size(cfg), device or torch.device("cuda"))
+
+
+def scan_forward(cfg, x, gate, starts=None, h0=None, saved=None, want_last=False, stream=None):
+    """Allocating gated scan. Returns (h, h_last or None); h_last [B, N] float32."""
+    h = torch.empty_like(x)
+    last = torch.empty((cfg.B, cfg.N), dtype=torch.float32, device=x.device) if want_last else None
+    dendsn_scan_forward(cfg, x, gate, starts, h0, h, last, saved, stream)
+    return h, last
+
+
+def scan_backward(cfg, x, gate, grad_h, starts=None, h0=None, grad_last=None, saved=None,
+                  stream=None):
+    """Allocating backward of the gated scan. Returns dict gx, ggate, and gh0 where h0 is given."""
+    out = dict(gx=torch.empty_like(x), ggate=torch.empty_like(gate))
+    gh0 = None
+    if h0 is not None:
+        gh0 = out["gh0"] = torch.empty_like(h0)
+    dendsn_scan_backward(cfg, x, gate, starts, h0, grad_h, grad_last, saved, out["gx"],
+                         out["ggate"], gh0, stream)
+    return out
+
+
+def dendsn_xent_workspace_size(cfg: dendsn_xent_config):
+    """(forward_bytes, backward_bytes) of scratch."""
+    f, b = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    _check("dendsn_xent_workspace_size",
+           load().dendsn_xent_workspace_size(ctypes.byref(cfg), ctypes.byref(f), ctypes.byref(b)))
+    return int(f.value), int(b.value)
+
+
+def _xent_expect(cfg, hidden, weight, labels, **rows):
+    dt = _xdtype(cfg)
+    _expect("hidden", hidden, (cfg.M, cfg.D), dt)
+    _expect("weight", weight, (cfg.V, cfg.D), dt)
+    _expect("labels", labels, (cfg.M,), _idtype(cfg.labels_dtype))
+    for name, t in rows.items():
+        _expect(name, t, (cfg.M,), torch.float32)
+
+
+def dendsn_xent_forward(cfg, hidden, weight, labels, loss, lse, scratch, stream=None):
+    _xent_expect(cfg, hidden, weight, labels, loss=loss, lse=lse)
+    _bytes("scratch", scratch, dendsn_xent_workspace_size(cfg)[0])
+    _check("dendsn_xent_forward", load().dendsn_xent_forward(
+        ctypes.byref(cfg), _ptr(hidden), _ptr(weight), _ptr(labels), _ptr(loss), _ptr(lse),
+        _ptr(scratch), _stream(stream)))
+
+
+def dendsn_xent_backward(cfg, hidden, weight, labels, lse, grad_loss, grad_hidden, grad_weight,
+                         scratch, stream=None):
+    _xent_expect(cfg, hidden, weight, labels, lse=lse, grad_loss=grad_loss)
+    _expect("grad_hidden", grad_hidden, (cfg.M, cfg.D), hidden.dtype)
+    _expect("grad_weight", grad_weight, (cfg.V, cfg.D), hidden.dtype)
+    _bytes("scratch", scratch, dendsn_xent_workspace_size(cfg)[1])
+    _check("dendsn_xent_backward", load().dendsn_xent_backward(
+        ctypes.byref(cfg), _ptr(hidden), _ptr(weight), _ptr(labels), _ptr(lse), _ptr(grad_loss),
+        _ptr(grad_hidden), _ptr(grad_weight), _ptr(scratch), _stream(stream)))
+
+
+def xent_forward(cfg, hidden, weight, labels, scratch=None, stream=None):
+    """Allocating cross entropy of hidden [M, D] read out by weight [V, D]: (loss [M], lse [M])."""
+    if scratch is None:
+        scratch = _scratch(dendsn_xent_workspace_size(cfg)[0], hidden.device)
+    loss = torch.empty((cfg.M,), dtype=torch.float32, device=hidden.device)
+    lse = torch.empty_like(loss)
+    dendsn_xent_forward(cfg, hidden, weight, labels, loss, lse, scratch, stream)
+    return loss, lse
+
+
+def xent_backward(cfg, hidden, weight, labels, lse, grad_loss, scratch=None, stream=None):
+    """Allocating backward. Returns dict ghidden [M, D], gweight [V, D] in hidden's dtype."""
+    if scratch is None:
+        scratch = _scratch(dendsn_xent_workspace_size(cfg)[1], hidden.device)
+    out = dict(ghidden=torch.empty_like(hidden), gweight=torch.empty_like(weight))
+    dendsn_xent_backward(cfg, hidden, weight, labels, lse, grad_loss, out["ghidden"],
+                         out["gweight"], scratch, stream)
+    return out
+
+
 # ------------------------------------------------------------------ tensor-level helpers
 def _xdtype(cfg) -> torch.dtype:
     return torch.bfloat16 if cfg.x_dtype == BF16 else torch.float32
@@ -407,3 +665,78 @@ class DendSNFunction(torch.autograd.Function):
         ga = g["galpha"].sum_to_size(ctx.alpha_shape)
         gb = g["gbeta"].sum() if ctx.learn_beta else None
         return g["gx"], ga, g["gxi"], g["gzeta"], g["gkappa"], None, None, gb
+
+
+def _dtype_name(t) -> str:
+    names = {torch.float32: "f32", torch.bfloat16: "bf16"}
+    if t.dtype not in names:
+        raise ValueError(f"dtype must be float32 or bfloat16, got {t.dtype}")
+    return names[t.dtype]
+
+
+def _index_name(t) -> str:
+    names = {torch.int32: "i32", torch.int64: "i64"}
+    if t.dtype not in names:
+        raise ValueError(f"ids and labels must be int32 or int64, got {t.dtype}")
+    return names[t.dtype]
+
+
+class EmbedFunction(torch.autograd.Function):
+    """autograd wrapper: scale * table[ids], with the gradient of the table."""
+
+    @staticmethod
+    def forward(ctx, table, ids, scale=1.0, padding_id=None):
+        ids = ids.contiguous()
+        ctx.cfg = make_embed_config(ids.numel(), *table.shape, _dtype_name(table), scale,
+                                    padding_id, _index_name(ids))
+        ctx.save_for_backward(ids)
+        return embed_forward(ctx.cfg, table.contiguous(), ids)
+
+    @staticmethod
+    def backward(ctx, g):
+        ids, = ctx.saved_tensors
+        return embed_backward(ctx.cfg, ids, g.contiguous()), None, None, None
+
+
+class ScanFunction(torch.autograd.Function):
+    """autograd wrapper of the gated compartment scan: (h, h_last) of x and gate, [T, B, N] or,
+    with layout "batch", [B, T, N]. starts and h0 may be None."""
+
+    @staticmethod
+    def forward(ctx, x, gate, starts=None, h0=None, gate_kind="decay", mix="plain",
+                layout="time"):
+        x, gate = x.contiguous(), gate.contiguous()
+        starts = None if starts is None else starts.contiguous()
+        h0 = None if h0 is None else h0.contiguous()
+        T, B = x.shape[:2] if layout == "time" else (x.shape[1], x.shape[0])
+        ctx.cfg = make_scan_config(T, B, x.shape[2], _dtype_name(x), gate_kind, mix, layout)
+        ctx.saved = scan_workspace(ctx.cfg, x.device)
+        h, last = scan_forward(ctx.cfg, x, gate, starts, h0, ctx.saved, want_last=True)
+        ctx.save_for_backward(x, gate, starts, h0)
+        return h, last
+
+    @staticmethod
+    def backward(ctx, gh, glast):
+        x, gate, starts, h0 = ctx.saved_tensors
+        g = scan_backward(ctx.cfg, x, gate, gh.contiguous(), starts, h0,
+                          None if glast is None else glast.contiguous(), ctx.saved)
+        return g["gx"], g["ggate"], None, g.get("gh0"), None, None, None
+
+
+class XentFunction(torch.autograd.Function):
+    """autograd wrapper: the row losses [M] of hidden [M, D] read out by weight [V, D]."""
+
+    @staticmethod
+    def forward(ctx, hidden, weight, labels, ignore_index=-100):
+        hidden, weight, labels = hidden.contiguous(), weight.contiguous(), labels.contiguous()
+        ctx.cfg = make_xent_config(hidden.shape[0], weight.shape[0], hidden.shape[1],
+                                   _dtype_name(hidden), ignore_index, _index_name(labels))
+        loss, lse = xent_forward(ctx.cfg, hidden, weight, labels)
+        ctx.save_for_backward(hidden, weight, labels, lse)
+        return loss
+
+    @staticmethod
+    def backward(ctx, gloss):
+        hidden, weight, labels, lse = ctx.saved_tensors
+        g = xent_backward(ctx.cfg, hidden, weight, labels, lse, gloss.float().contiguous())
+        return g["ghidden"], g["gweight"], None, None

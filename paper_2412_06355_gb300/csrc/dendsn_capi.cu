@@ -10,6 +10,7 @@
 
 #include "dendsn.h"
 #include "dendsn_types.h"
+#include "seq/seq_common.h"
 
 namespace dendsn {
 
@@ -125,6 +126,20 @@ dendsn_status fail(dendsn_status st, const char *fmt, ...) {
 }
 
 bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+
+}  // namespace
+
+// The token-sequence entry points (seq/) report through the same message and counter.
+dendsn_status dendsn::seq_fail(dendsn_status st, const char *fmt, ...) {
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_last_error, sizeof g_last_error, fmt, ap);
+    va_end(ap);
+    return st;
+}
+void dendsn::seq_count_launches(int n) { g_launches.fetch_add((uint64_t)n, std::memory_order_relaxed); }
+
+namespace {
 
 struct Plan {
     Geometry gf, gb;   // forward and backward tilings (block sizes may differ)
