@@ -1,13 +1,56 @@
 // Softmax cross entropy of a linear readout in pieces of the vocabulary, and its gradient.
+//
+// Four products, all on the fifth-generation tensor cores (tcgen05 on a pair of blocks, a
+// 256 x 256 tile of float32 sums in TMEM, operands by tensor copies into 128-byte-swizzled
+// shared memory):
+//   STATS   l = H W^T of all the vocabulary; the epilogue keeps each row's maximum and sum of
+//           exponentials of 128 columns, and the label's logit; a small kernel joins them
+//   PIECE   l again for one piece of the vocabulary; the epilogue writes
+//           G = c (exp(l - lse) - [label]) in bfloat16
+//   HIDDEN  grad_hidden += G W of the piece, in float32
+//   WEIGHT  grad_weight of the piece = G^T H
+// so 2 M V D operations in the forward and 6 M V D in the backward, a third of those to form
+// the logits again instead of keeping M V of them.
+//
+// Rows that are ignored are left out before the products: the others are copied together
+// (xent_rows, xent_pack), so ignored rows cost nothing and no infinity or NaN in them can
+// reach a product as 0 * inf. That copy also gives rows of any D the 16-byte pitch that
+// tensor copies need, and float32 operands their three bfloat16 terms: x = x0 + x1 + x2 with
+// 8 bits each; the products x_i y_j with i + j <= 2 are summed, the smallest first, and the
+// others are below 2^-26 of x y.
 #include <cuda_bf16.h>
 
 #include <algorithm>
+#include <mutex>
 
 #include "seq_common.h"
+#include "tc.cuh"
 
 namespace dendsn {
 namespace {
 
+enum { STATS = 0, PIECE = 1, HIDDEN = 2, WEIGHT = 3 };
+
+constexpr int kTileM = 256, kTileN = 256, kTileK = 64;    // of a pair of blocks
+constexpr int kStages = 6;
+constexpr int kHalfBytes = 128 * kTileK * 2;              // one block's 128 x 64 operand tile
+constexpr int kStageBytes = 2 * kHalfBytes;
+constexpr int kThreads = 320;                             // copies, products, 8 warps of epilogue
+constexpr size_t kSmem = kStages * kStageBytes + 1024 + 256;
+constexpr int kIgnored = -1, kBadLabel = -2;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct Ctl {                // at the start of the scratch buffer
+    int32_t rows;           // rows that take part
+    int32_t failed;         // a wait ran out: results become NaN
+    int32_t pad[62];
+};
+
+template <typename I>
+__device__ __forceinline__ int label_of(const void *labels, int64_t r, int V, int64_t ignore) {
+    const int64_t y = static_cast<const I *>(labels)[r];
+    return y == ignore ? kIgnored : (y < 0 || y >= V) ? kBadLabel : (int)y;
+}
 template <typename T> __device__ __forceinline__ float to_f(T v);
 template <> __device__ __forceinline__ float to_f<float>(float v) { return v; }
 template <> __device__ __forceinline__ float to_f<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
@@ -15,176 +58,455 @@ template <typename T> __device__ __forceinline__ T from_f(float v);
 template <> __device__ __forceinline__ float from_f<float>(float v) { return v; }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
-constexpr int kTile = 64, kK = 16;
-constexpr int kIgnored = -1, kBadLabel = -2;
+__device__ __forceinline__ float nan_f() { return __int_as_float(0x7fffffff); }
 
-template <typename I>
-__device__ __forceinline__ int label_of(const void *labels, int r, int V, int64_t ignore) {
-    const int64_t y = static_cast<const I *>(labels)[r];
-    return y == ignore ? kIgnored : (y < 0 || y >= V) ? kBadLabel : (int)y;
+__device__ __forceinline__ uint32_t two(__nv_bfloat16 a, __nv_bfloat16 b) {
+    return (uint32_t)__bfloat16_as_ushort(a) | (uint32_t)__bfloat16_as_ushort(b) << 16;
 }
 
-// acc[i][j] += sum_k A(row0 + 4 ty + i, k) B(col0 + 4 tx + j, k) over k in [0, K), with the
-// loaders returning 0 outside their matrices; 256 threads, 64 x 64 tile.
-template <typename LA, typename LB>
-__device__ __forceinline__ void tile_product(float (&acc)[4][4], int64_t K, LA la, LB lb) {
-    __shared__ float As[kK][kTile + 1], Bs[kK][kTile + 1];
-    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    for (int64_t k0 = 0; k0 < K; k0 += kK) {
-        __syncthreads();
-        for (int e = threadIdx.x; e < kTile * kK; e += 256) {
-            As[e % kK][e / kK] = k0 + e % kK < K ? la(e / kK, k0 + e % kK) : 0.f;
-            Bs[e % kK][e / kK] = k0 + e % kK < K ? lb(e / kK, k0 + e % kK) : 0.f;
+// Term `term` of x = x0 + x1 + x2. A finite x whose rounding would overflow is truncated; what
+// is not finite stays in the first term alone.
+__device__ __forceinline__ void split(float x, __nv_bfloat16 (&t)[3]) {
+    t[0] = __float2bfloat16_rn(x);
+    if (!isfinite(__bfloat162float(t[0]))) {
+        if (!isfinite(x)) {
+            t[1] = t[2] = __float2bfloat16_rn(0.f);
+            return;
         }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < kK; ++k)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    acc[i][j] = fmaf(As[k][4 * ty + i], Bs[k][4 * tx + j], acc[i][j]);
+        t[0] = __float2bfloat16_rz(x);
     }
+    const float r = x - __bfloat162float(t[0]);
+    t[1] = __float2bfloat16_rn(r);
+    t[2] = __float2bfloat16_rn(r - __bfloat162float(t[1]));
 }
 
-struct Args {
-    const void *hidden, *weight, *labels;
-    int64_t ignore;
-    int32_t M, V, D;
-    float *loss, *lse;
-    const float *lse_in, *gloss;
-    void *gh, *gw;
-    float *G, *gh32;
-    int32_t v0, vc;
+// ------------------------------------------------------------------ rows that take part
+struct Rows {
+    Ctl *ctl;
+    int32_t *index;         // [Mp] row of the call
+    int32_t *label;         // [Mp]
+    int32_t *where;         // [M] place of a row, or kIgnored, kBadLabel
+    float *lse, *weight;    // [Mp] of the backward: its lse and grad_loss
+    float *picked;          // [Mp] of the forward: the label's logit
 };
 
-template <typename T, typename I>
-__global__ void __launch_bounds__(256) xent_forward_kernel(const Args A) {
-    __shared__ int lab[kTile];
-    __shared__ float picked[kTile];
-    const int64_t r0 = (int64_t)blockIdx.x * kTile;
-    const T *H = static_cast<const T *>(A.hidden), *W = static_cast<const T *>(A.weight);
-    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    if (threadIdx.x < kTile) {
-        lab[threadIdx.x] = r0 + threadIdx.x < A.M ? label_of<I>(A.labels, r0 + threadIdx.x, A.V, A.ignore) : kIgnored;
-        picked[threadIdx.x] = 0.f;
-    }
-    __syncthreads();
-    float top[4], sum[4];
-    for (int i = 0; i < 4; ++i) { top[i] = -INFINITY; sum[i] = 0.f; }
-    for (int v0 = 0; v0 < A.V; v0 += kTile) {
-        float acc[4][4] = {};
-        tile_product(acc, A.D,
-                     [&](int i, int64_t k) { return lab[i] >= 0 ? to_f<T>(H[(r0 + i) * A.D + k]) : 0.f; },
-                     [&](int j, int64_t k) { return v0 + j < A.V ? to_f<T>(W[(int64_t)(v0 + j) * A.D + k]) : 0.f; });
-        for (int i = 0; i < 4; ++i) {
-            float m = top[i];
-            for (int j = 0; j < 4; ++j) {
-                const int v = v0 + 4 * tx + j;
-                if (v < A.V) m = fmaxf(m, acc[i][j]);
-                if (v < A.V && v == lab[4 * ty + i]) picked[4 * ty + i] = acc[i][j];
+// One block: lists the rows with a label in the vocabulary, in order, and fills the places up
+// to the next multiple of 256 with rows of weight zero.
+template <typename I>
+__global__ void __launch_bounds__(1024) xent_rows_kernel(Rows R, const void *labels, int32_t M, int32_t V,
+                                                         int64_t ignore, float *loss, float *lse_out,
+                                                         const float *lse, const float *gloss) {
+    __shared__ int warps[32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int done = 0;
+    for (int64_t r0 = 0; r0 < M; r0 += 1024) {
+        const int64_t r = r0 + threadIdx.x;
+        const int y = r < M ? label_of<I>(labels, r, V, ignore) : kIgnored;
+        const unsigned m = __ballot_sync(0xffffffffu, y >= 0);
+        if (lane == 0) warps[warp] = __popc(m);
+        __syncthreads();
+        int at = done + __popc(m & ((1u << lane) - 1));
+        for (int w = 0; w < 32; ++w) {
+            if (w < warp) at += warps[w];
+            done += warps[w];
+        }
+        __syncthreads();
+        if (r < M) {
+            R.where[r] = y >= 0 ? at : y;
+            if (y >= 0) {
+                R.index[at] = (int32_t)r;
+                R.label[at] = y;
+                if (lse) {
+                    R.lse[at] = lse[r];
+                    R.weight[at] = gloss[r];
+                }
+            } else if (loss) {
+                loss[r] = lse_out[r] = y == kIgnored ? 0.f : nan_f();
             }
-            const float ref = m == -INFINITY ? 0.f : m;
-            float s = sum[i] * expf(top[i] - ref);
-            for (int j = 0; j < 4; ++j)
-                if (v0 + 4 * tx + j < A.V) s += expf(acc[i][j] - ref);
-            top[i] = m;
-            sum[i] = s;
         }
     }
+    const int end = (done + kTileM - 1) / kTileM * kTileM;
+    for (int i = done + threadIdx.x; i < end; i += 1024) {
+        R.index[i] = -1;
+        R.label[i] = -1;
+        if (lse) R.lse[i] = R.weight[i] = 0.f;
+    }
+    if (threadIdx.x == 0) {
+        R.ctl->rows = done;
+        R.ctl->failed = 0;
+    }
+}
+
+// Copies rows of D elements to rows of Dp bfloat16 elements with zeros behind, in `terms` planes.
+// index: the row to copy for each place (negative: zeros), or null: the same row.
+template <typename T>
+__global__ void __launch_bounds__(256) xent_pack_kernel(const T *from, __nv_bfloat16 *to, const int32_t *index,
+                                                        const Ctl *ctl, int64_t rows, int32_t D, int32_t Dp,
+                                                        int64_t plane) {
+    const int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (r >= rows) return;
+    int64_t src = r;
+    if (index) {
+        if (r >= (ctl->rows + kTileM - 1) / kTileM * kTileM) return;
+        src = index[r];
+    }
+    const T *p = from + src * D;
+    for (int32_t d = (threadIdx.x & 31) * 2; d < Dp; d += 64) {
+        const float a = src >= 0 && d < D ? to_f<T>(p[d]) : 0.f;
+        const float b = src >= 0 && d + 1 < D ? to_f<T>(p[d + 1]) : 0.f;
+        uint32_t *q = reinterpret_cast<uint32_t *>(to + r * Dp + d);
+        if constexpr (sizeof(T) == 2) {
+            *q = two(__float2bfloat16_rn(a), __float2bfloat16_rn(b));
+        } else {
+            __nv_bfloat16 u[3], v[3];
+            split(a, u);
+            split(b, v);
+#pragma unroll
+            for (int t = 0; t < 3; ++t) q[t * (plane / 2)] = two(u[t], v[t]);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ the products
+struct Gemm {
+    Ctl *ctl;
+    const int32_t *label;
+    const float *lse, *weight;
+    float *picked;
+    float2 *part;           // [2 * nt][Mp]
+    __nv_bfloat16 *G;       // [terms][Mp][pitch]
+    float *sum;             // [splits][Mp][nt * kTileN]
+    void *gw;               // [V][D]
+    int64_t Mp, gplane;
+    int32_t pitch;
+    int32_t mt, nt, splits; // tiles (mt of the products over rows follows from ctl->rows)
+    int32_t kb, kb_split;   // blocks of kTileK along the sum, in all and for one split
+    int32_t V, D, v0, vc;
+    bool wide;              // rows of gw can be written 16 bytes at a time
+};
+
+// The operand terms of each pass over the sum, smallest products first.
+__device__ __forceinline__ int term_a(int phase) { return 0x201100 >> (20 - 4 * phase) & 0xf; }
+__device__ __forceinline__ int term_b(int phase) { return 0x021010 >> (20 - 4 * phase) & 0xf; }
+
+template <int MODE> __device__ __forceinline__ void tile_of(const Gemm &g, int mt, int64_t item, int &m, int &n, int &s) {
+    s = 0;
+    if (MODE == STATS || MODE == PIECE) {      // the hidden rows stay in L2, the weights pass once
+        m = (int)(item % mt);
+        n = (int)(item / mt);
+    } else {                                   // G passes once
+        n = (int)(item % g.nt);
+        const int64_t rest = item / g.nt;
+        m = (int)(rest % mt);
+        s = (int)(rest / mt);
+    }
+}
+
+template <int MODE, typename T>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+    xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                        const Gemm g) {
+    constexpr bool kF32 = sizeof(T) == 4;
+    constexpr int kPhases = kF32 ? 6 : 1;
+    constexpr bool kRowsA = MODE != WEIGHT;                   // operand rows run along the sum
+    constexpr bool kRowsB = MODE == STATS || MODE == PIECE;
+    extern __shared__ uint8_t raw[];
+    __shared__ uint32_t tmem_base;
+    const uint32_t stage0 = (tc::smem_addr(raw) + 1023) & ~1023u;
+    const uint32_t bars = stage0 + kStages * kStageBytes;
+    const uint32_t full = bars, empty = bars + 8 * kStages, acc_full = bars + 16 * kStages, acc_empty = acc_full + 16;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = tc::cluster_rank();
+    const int rows = g.ctl->rows;
+    const int mt = MODE == WEIGHT ? g.mt : (rows + kTileM - 1) / kTileM;
+    const int kb = MODE == WEIGHT ? (rows + kTileK - 1) / kTileK : g.kb;
+    const int64_t items = (int64_t)mt * g.nt * g.splits;
+    const int64_t first = blockIdx.x / 2, stride = gridDim.x / 2;
+
+    if (warp == 0 && lane == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            tc::bar_init(full + 8 * i, 1);
+            tc::bar_init(empty + 8 * i, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            tc::bar_init(acc_full + 8 * i, 1);
+            tc::bar_init(acc_empty + 8 * i, 16);
+        }
+        tc::bar_init_fence();
+        tc::prefetch_map(&map_a);
+        tc::prefetch_map(&map_b);
+    }
+    if (warp == 1) tc::tmem_alloc(tc::smem_addr(&tmem_base), 512);
+    tc::fence_before_sync();
     __syncthreads();
-    for (int i = 0; i < 4; ++i) {
-        for (int o = 8; o; o >>= 1) {
-            const float m2 = __shfl_xor_sync(0xffffffffu, top[i], o), s2 = __shfl_xor_sync(0xffffffffu, sum[i], o);
-            const float m = fmaxf(top[i], m2), ref = m == -INFINITY ? 0.f : m;
-            sum[i] = sum[i] * expf(top[i] - ref) + s2 * expf(m2 - ref);
-            top[i] = m;
+    tc::cluster_sync();
+    tc::fence_after_sync();
+    const uint32_t tmem = tmem_base;
+    bool ok = true;
+
+    if (warp == 0 && lane == 0) {                             // copies, in both blocks
+        const uint32_t full0 = tc::in_block(full, 0);
+        int stage = 0;
+        uint32_t phase = 1;
+        for (int64_t item = first; ok && item < items; item += stride) {
+            int m, n, s;
+            tile_of<MODE>(g, mt, item, m, n, s);
+            const int am = m * kTileM + (int)rank * 128, bn = n * kTileN + (int)rank * 128;
+            const int k0 = s * g.kb_split, k1 = MODE == WEIGHT ? kb : min(kb, k0 + g.kb_split);
+            for (int ph = 0; ok && ph < kPhases; ++ph) {
+                const int ta = kF32 ? term_a(ph) : 0, tb = kF32 ? term_b(ph) : 0;
+                for (int k = k0; k < k1; ++k) {
+                    if (!(ok = tc::bar_wait(empty + 8 * stage, phase))) break;
+                    if (rank == 0) tc::bar_expect(full + 8 * stage, 2 * kStageBytes);
+                    const uint32_t a = stage0 + stage * kStageBytes, b = a + kHalfBytes, bar = full0 + 8 * stage;
+                    if (kRowsA) {
+                        tc::load_box(a, &map_a, bar, k * kTileK, am, ta);
+                    } else {
+                        tc::load_box(a, &map_a, bar, am, k * kTileK, ta);
+                        tc::load_box(a + kHalfBytes / 2, &map_a, bar, am + 64, k * kTileK, ta);
+                    }
+                    if (kRowsB) {
+                        tc::load_box(b, &map_b, bar, k * kTileK, g.v0 + bn, tb);
+                    } else {
+                        const int row = MODE == HIDDEN ? g.v0 + k * kTileK : k * kTileK;
+                        tc::load_box(b, &map_b, bar, bn, row, tb);
+                        tc::load_box(b + kHalfBytes / 2, &map_b, bar, bn + 64, row, tb);
+                    }
+                    if (++stage == kStages) { stage = 0; phase ^= 1; }
+                }
+            }
         }
-        const int r = 4 * ty + i;
-        if (tx == 0 && r0 + r < A.M) {
-            const float lse = (top[i] == -INFINITY ? 0.f : top[i]) + logf(sum[i]);
-            const float nan = __int_as_float(0x7fffffff);
-            A.lse[r0 + r] = lab[r] >= 0 ? lse : lab[r] == kIgnored ? 0.f : nan;
-            A.loss[r0 + r] = lab[r] >= 0 ? lse - picked[r] : lab[r] == kIgnored ? 0.f : nan;
+    } else if (warp == 1 && lane == 0 && rank == 0) {         // products, in the first block
+        constexpr uint32_t idesc = tc::product_of(kTileM, kTileN, !kRowsA, !kRowsB);
+        int stage = 0, acc = 0;
+        uint32_t phase = 0, acc_phase = 1;
+        for (int64_t item = first; ok && item < items; item += stride) {
+            int m, n, s;
+            tile_of<MODE>(g, mt, item, m, n, s);
+            const int k0 = s * g.kb_split, k1 = MODE == WEIGHT ? kb : min(kb, k0 + g.kb_split);
+            const int steps = (k1 - k0) * kPhases;
+            if (steps <= 0) continue;
+            if (!(ok = tc::bar_wait(acc_empty + 8 * acc, acc_phase))) break;
+            tc::fence_after_sync();
+            for (int i = 0; i < steps; ++i) {
+                if (!(ok = tc::bar_wait(full + 8 * stage, phase))) break;
+                tc::fence_after_sync();
+                const uint32_t a = stage0 + stage * kStageBytes, b = a + kHalfBytes;
+#pragma unroll
+                for (int j = 0; j < kTileK / 16; ++j)
+                    tc::mma(tmem + acc * kTileN, tc::operand(a + j * (kRowsA ? 32 : 2048), kRowsA, kHalfBytes / 2),
+                            tc::operand(b + j * (kRowsB ? 32 : 2048), kRowsB, kHalfBytes / 2), idesc, i + j > 0);
+                tc::commit_both(empty + 8 * stage);
+                if (++stage == kStages) { stage = 0; phase ^= 1; }
+            }
+            if (!ok) break;
+            tc::commit_both(acc_full + 8 * acc);
+            if (++acc == 2) { acc = 0; acc_phase ^= 1; }
+        }
+    } else if (warp >= 2) {                                   // epilogue, in both blocks
+        const int quad = warp % 4, half = (warp - 2) / 4;
+        const uint32_t empty0 = tc::in_block(acc_empty, 0);
+        int acc = 0;
+        uint32_t acc_phase = 0;
+        for (int64_t item = first; item < items; item += stride) {
+            int m, n, s;
+            tile_of<MODE>(g, mt, item, m, n, s);
+            const int k0 = s * g.kb_split, k1 = MODE == WEIGHT ? kb : min(kb, k0 + g.kb_split);
+            const bool any = k1 > k0;
+            const int row = m * kTileM + (int)rank * 128 + quad * 32 + lane;
+            const int col0 = n * kTileN + half * 128;
+            if (any) {
+                ok = tc::bar_wait(acc_full + 8 * acc, acc_phase);
+                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                tc::fence_after_sync();
+            }
+            float top = -INFINITY, total = 0.f;
+            int y = -1;
+            float lse = 0.f, weight = 0.f;
+            if (MODE == STATS || MODE == PIECE) y = g.label[row];
+            if (MODE == PIECE) {
+                lse = g.lse[row];
+                weight = g.weight[row];
+            }
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+                float v[32];
+                const int col = col0 + 32 * c;                // within the piece, or within D
+                if (any) tc::tmem_load(v, tmem + ((uint32_t)quad << 21) + acc * kTileN + half * 128 + 32 * c);
+                else
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] = 0.f;
+                if (MODE == STATS) {
+                    const int left = g.V - col;
+                    if (left < 32)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = i < left ? v[i] : -INFINITY;
+                    if (y >= col && y < col + 32)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (y == col + i) g.picked[row] = v[i];
+                    float t = top;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) t = fmaxf(t, v[i]);
+                    const float ref = t == -INFINITY ? 0.f : t * kLog2e;
+                    // the reference 2^ref is what the sum is relative to, so its rounding cancels
+                    const float old = top == -INFINITY ? 0.f : top * kLog2e;
+                    total = total == 0.f ? 0.f : total * exp2f(old - ref);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) total += exp2f(fmaf(v[i], kLog2e, -ref));
+                    top = t;
+                } else if (MODE == PIECE) {
+                    const int at = y - g.v0 - col;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        const float p = exp2f((v[i] - lse) * kLog2e);
+                        v[i] = weight * (i == at ? p - 1.f : p);
+                    }
+                    uint4 *to = reinterpret_cast<uint4 *>(g.G + (int64_t)row * g.pitch + col);
+                    if constexpr (!kF32) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            uint32_t q[4];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                q[j] = two(__float2bfloat16_rn(v[8 * i + 2 * j]), __float2bfloat16_rn(v[8 * i + 2 * j + 1]));
+                            to[i] = make_uint4(q[0], q[1], q[2], q[3]);
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            uint32_t q[3][4];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                __nv_bfloat16 a[3], b[3];
+                                split(v[8 * i + 2 * j], a);
+                                split(v[8 * i + 2 * j + 1], b);
+#pragma unroll
+                                for (int t = 0; t < 3; ++t) q[t][j] = two(a[t], b[t]);
+                            }
+#pragma unroll
+                            for (int t = 0; t < 3; ++t)
+                                to[i + t * (g.gplane / 8)] = make_uint4(q[t][0], q[t][1], q[t][2], q[t][3]);
+                        }
+                    }
+                } else if (MODE == HIDDEN) {
+                    float4 *to = reinterpret_cast<float4 *>(g.sum + ((int64_t)s * g.Mp + row) * (g.nt * kTileN) + col);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        float4 q = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                        if (g.v0) {
+                            const float4 o = to[i];
+                            q = make_float4(q.x + o.x, q.y + o.y, q.z + o.z, q.w + o.w);
+                        }
+                        to[i] = q;
+                    }
+                } else {
+                    T *to = static_cast<T *>(g.gw) + ((int64_t)g.v0 + row) * g.D + col;
+                    if (row < g.vc) {
+                        if (g.wide && col + 32 <= g.D) {
+                            if constexpr (kF32) {
+#pragma unroll
+                                for (int i = 0; i < 8; ++i)
+                                    reinterpret_cast<float4 *>(to)[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    uint32_t q[4];
+#pragma unroll
+                                    for (int j = 0; j < 4; ++j)
+                                        q[j] = two(__float2bfloat16_rn(v[8 * i + 2 * j]), __float2bfloat16_rn(v[8 * i + 2 * j + 1]));
+                                    reinterpret_cast<uint4 *>(to)[i] = make_uint4(q[0], q[1], q[2], q[3]);
+                                }
+                            }
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (col + i < g.D) to[i] = from_f<T>(v[i]);
+                        }
+                    }
+                }
+            }
+            if (any) {
+                tc::fence_before_sync();
+                __syncwarp();
+                if (lane == 0) tc::bar_arrive_cluster(empty0 + 8 * acc);
+                if (++acc == 2) { acc = 0; acc_phase ^= 1; }
+            }
+            if (MODE == STATS)
+                g.part[(int64_t)(2 * n + half) * g.Mp + row] = make_float2(top == -INFINITY ? 0.f : top * kLog2e, total);
         }
     }
-}
-
-template <typename T, typename I>
-__global__ void __launch_bounds__(256) xent_piece_kernel(const Args A) {
-    __shared__ int lab[kTile];
-    const int64_t r0 = (int64_t)blockIdx.y * kTile, c0 = (int64_t)blockIdx.x * kTile;
-    const T *H = static_cast<const T *>(A.hidden), *W = static_cast<const T *>(A.weight) + (int64_t)A.v0 * A.D;
-    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    if (threadIdx.x < kTile)
-        lab[threadIdx.x] = r0 + threadIdx.x < A.M ? label_of<I>(A.labels, r0 + threadIdx.x, A.V, A.ignore) : kIgnored;
+    if (!ok) g.ctl->failed = 1;
+    __syncwarp();
+    tc::fence_before_sync();
     __syncthreads();
-    float acc[4][4] = {};
-    tile_product(acc, A.D,
-                 [&](int i, int64_t k) { return lab[i] >= 0 ? to_f<T>(H[(r0 + i) * A.D + k]) : 0.f; },
-                 [&](int j, int64_t k) { return c0 + j < A.vc ? to_f<T>(W[(c0 + j) * A.D + k]) : 0.f; });
-    for (int i = 0; i < 4; ++i) {
-        const int64_t r = r0 + 4 * ty + i;
-        const int y = lab[4 * ty + i];
-        if (r >= A.M) continue;
-        for (int j = 0; j < 4; ++j) {
-            const int64_t c = c0 + 4 * tx + j;
-            if (c >= A.vc) continue;
-            float g = 0.f;
-            if (y >= 0) g = A.gloss[r] * (expf(acc[i][j] - A.lse_in[r]) - (y == A.v0 + c ? 1.f : 0.f));
-            A.G[r * A.vc + c] = g;
-        }
+    tc::cluster_sync();
+    tc::fence_after_sync();
+    if (warp == 1) tc::tmem_free(tmem, 512);
+}
+
+// Joins the maxima and sums of a row: 32 rows of a block, its 8 warps take every eighth part.
+__global__ void __launch_bounds__(256) xent_join_kernel(Rows R, const float2 *part, int32_t parts, int64_t Mp,
+                                                        float *loss, float *lse) {
+    __shared__ float2 sh[8][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int r = blockIdx.x * 32 + lane;
+    const int rows = R.ctl->rows;
+    if (blockIdx.x * 32 >= rows) return;
+    float2 a = make_float2(-INFINITY, 0.f);
+    auto add = [](float2 &x, const float2 &y) {
+        if (y.y == 0.f) return;                               // nothing in it
+        const float m = fmaxf(x.x, y.x);
+        x.y = (x.y == 0.f ? 0.f : x.y * exp2f(x.x - m)) + y.y * exp2f(y.x - m);
+        x.x = m;
+    };
+    if (r < rows)
+        for (int p = warp; p < parts; p += 8) add(a, part[(int64_t)p * Mp + r]);
+    sh[warp][lane] = a;
+    __syncthreads();
+    if (warp == 0 && r < rows) {
+        for (int w = 1; w < 8; ++w) add(a, sh[w][lane]);
+        const float v = R.ctl->failed ? nan_f() : kLn2 * (a.x + log2f(a.y));
+        lse[R.index[r]] = v;
+        loss[R.index[r]] = v - R.picked[r];
     }
 }
 
-// gh32 (+)= G W of the piece; the last piece writes grad_hidden.
-template <typename T, typename I>
-__global__ void __launch_bounds__(256) xent_grad_hidden_kernel(const Args A) {
-    const int64_t r0 = (int64_t)blockIdx.y * kTile, d0 = (int64_t)blockIdx.x * kTile;
-    const T *W = static_cast<const T *>(A.weight) + (int64_t)A.v0 * A.D;
-    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    float acc[4][4] = {};
-    tile_product(acc, A.vc, [&](int i, int64_t k) { return r0 + i < A.M ? A.G[(r0 + i) * A.vc + k] : 0.f; },
-                 [&](int j, int64_t k) { return d0 + j < A.D ? to_f<T>(W[k * A.D + d0 + j]) : 0.f; });
-    const bool last = A.v0 + A.vc == A.V;
-    for (int i = 0; i < 4; ++i) {
-        const int64_t r = r0 + 4 * ty + i;
-        if (r >= A.M) continue;
-        const int y = label_of<I>(A.labels, r, A.V, A.ignore);
-        for (int j = 0; j < 4; ++j) {
-            const int64_t d = d0 + 4 * tx + j;
-            if (d >= A.D) continue;
-            float v = acc[i][j] + (A.v0 ? A.gh32[r * A.D + d] : 0.f);
-            A.gh32[r * A.D + d] = v;
-            if (y < 0) v = y == kIgnored ? 0.f : __int_as_float(0x7fffffff);
-            if (last) static_cast<T *>(A.gh)[r * A.D + d] = from_f<T>(v);
-        }
+// grad_hidden of every row of the call from the sums of its place.
+template <typename T>
+__global__ void __launch_bounds__(256) xent_hidden_kernel(Rows R, const float *sum, T *gh, int64_t M, int64_t Mp,
+                                                          int32_t D, int32_t Dq, int32_t splits) {
+    const int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (r >= M) return;
+    const int at = R.where[r];
+    const bool failed = R.ctl->failed;
+    for (int32_t d = threadIdx.x & 31; d < D; d += 32) {
+        float v = 0.f;
+        if (at >= 0)
+            for (int s = 0; s < splits; ++s) v += sum[((int64_t)s * Mp + at) * Dq + d];
+        if (at == kBadLabel || failed) v = nan_f();
+        gh[r * D + d] = from_f<T>(v);
     }
 }
 
-template <typename T, typename I>
-__global__ void __launch_bounds__(256) xent_grad_weight_kernel(const Args A) {
-    const int64_t c0 = (int64_t)blockIdx.y * kTile, d0 = (int64_t)blockIdx.x * kTile;
-    const T *H = static_cast<const T *>(A.hidden);
-    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    float acc[4][4] = {};
-    tile_product(acc, A.M, [&](int i, int64_t k) { return c0 + i < A.vc ? A.G[k * A.vc + c0 + i] : 0.f; },
-                 [&](int j, int64_t k) {
-                     return d0 + j < A.D && label_of<I>(A.labels, k, A.V, A.ignore) >= 0
-                                ? to_f<T>(H[k * A.D + d0 + j]) : 0.f;
-                 });
-    for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) {
-            const int64_t c = c0 + 4 * ty + i, d = d0 + 4 * tx + j;
-            if (c < A.vc && d < A.D) static_cast<T *>(A.gw)[(A.v0 + c) * A.D + d] = from_f<T>(acc[i][j]);
-        }
-}
-
-constexpr int kPiece = 4096;
+// ------------------------------------------------------------------ host
+constexpr size_t kPieceBytes = size_t(256) << 20;   // of G
+constexpr int kClusters = 76;                        // pairs of the card's 152 SMs
 
 struct Plan {
-    size_t fwd = 0, bwd = 0, gh32 = 0;
+    int terms;
+    int64_t Mp;                     // rows, a multiple of the tile
+    int32_t Dp, Dq;                 // packed row, row of the sums
+    int32_t nt, dt, mt;             // tiles along the vocabulary, D and the rows
+    int32_t pitch, pieces;          // columns of a piece
+    int32_t splits, kb_split;       // of the sum over a piece in HIDDEN
+    bool pack_w;
+    // offsets in the scratch buffer
+    size_t index, label, where, lse, weight, picked, part, H, W, G, sum;
+    size_t fwd, bwd;
 };
+
+int32_t up(int64_t v, int64_t to) { return (int32_t)((v + to - 1) / to * to); }
 
 dendsn_status make_plan(const dendsn_xent_config *cfg, Plan *pl) {
     if (!cfg) return seq_fail(DENDSN_ERR_INVALID_ARG, "cfg is NULL");
@@ -194,34 +516,255 @@ dendsn_status make_plan(const dendsn_xent_config *cfg, Plan *pl) {
         return seq_fail(DENDSN_ERR_INVALID_ARG, "bad x_dtype %d", cfg->x_dtype);
     if (cfg->labels_dtype != DENDSN_I32 && cfg->labels_dtype != DENDSN_I64)
         return seq_fail(DENDSN_ERR_INVALID_ARG, "bad labels_dtype %d", cfg->labels_dtype);
-    auto up = [](size_t v) { return (v + 255) / 256 * 256; };
-    pl->gh32 = up((size_t)cfg->M * cfg->D * 4);
-    pl->bwd = pl->gh32 + up((size_t)cfg->M * std::min(cfg->V, kPiece) * 4);
+    if (cfg->M > (1 << 30) || cfg->V > (1 << 30) || cfg->D > (1 << 24))
+        return seq_fail(DENDSN_ERR_UNSUPPORTED, "size out of range (M=%d V=%d D=%d)", cfg->M, cfg->V, cfg->D);
+    Plan &p = *pl;
+    p.terms = cfg->x_dtype == DENDSN_F32 ? 3 : 1;
+    p.Mp = up(cfg->M, kTileM);
+    p.Dp = up(cfg->D, kTileK);
+    p.Dq = up(cfg->D, kTileN);
+    p.mt = (int32_t)(p.Mp / kTileM);
+    p.nt = up(cfg->V, kTileN) / kTileN;
+    p.dt = p.Dq / kTileN;
+    // pieces of equal size, each a multiple of the tile and with G within kPieceBytes
+    const int64_t row = std::max<int64_t>(p.Mp, 1) * p.terms * 2;
+    const int64_t most = std::max<int64_t>(1, (int64_t)kPieceBytes / (row * kTileN));
+    p.pieces = (int32_t)((p.nt + most - 1) / most);
+    p.pitch = (p.nt + p.pieces - 1) / p.pieces * kTileN;
+    // few tiles of grad_hidden: the sum over the piece is split over the card
+    const int32_t kb = p.pitch / kTileK;
+    const int64_t tiles = (int64_t)std::max(p.mt, 1) * p.dt;
+    p.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(kClusters / tiles, kb / 8));
+    p.kb_split = (kb + p.splits - 1) / p.splits;
+    p.splits = (kb + p.kb_split - 1) / p.kb_split;
+    size_t at = sizeof(Ctl);
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += (bytes + 255) / 256 * 256;
+        return here;
+    };
+    p.index = take(p.Mp * 4);
+    p.label = take(p.Mp * 4);
+    p.where = take((size_t)cfg->M * 4);
+    p.H = take((size_t)p.terms * p.Mp * p.Dp * 2);
+    // weights are packed unless their rows can be copied as they are (also asked of their address)
+    p.W = take((size_t)p.terms * cfg->V * p.Dp * 2);
+    const size_t shared = at;
+    p.picked = take(p.Mp * 4);
+    p.part = take((size_t)2 * p.nt * p.Mp * 8);
+    p.fwd = at;
+    at = shared;
+    p.lse = take(p.Mp * 4);
+    p.weight = take(p.Mp * 4);
+    p.G = take((size_t)p.terms * p.Mp * p.pitch * 2);
+    p.sum = take((size_t)p.splits * p.Mp * p.Dq * 4);
+    p.bwd = at;
     return DENDSN_OK;
 }
 
-unsigned tiles(int64_t n) { return (unsigned)((n + kTile - 1) / kTile); }
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                 const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-template <typename T, typename I>
-cudaError_t run_forward(const Args &a, cudaStream_t s) {
-    xent_forward_kernel<T, I><<<tiles(a.M), 256, 0, s>>>(a);
+EncodeTiled encode_tiled() {
+    static std::mutex mutex;
+    static EncodeTiled fn = nullptr;
+    std::lock_guard<std::mutex> lock(mutex);
+    if (!fn) {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult got;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &got) == cudaSuccess &&
+            got == cudaDriverEntryPointSuccess)
+            fn = reinterpret_cast<EncodeTiled>(p);
+    }
+    return fn;
+}
+
+// A [planes][rows][inner] bfloat16 tensor read in boxes of 64 x box_rows, zeros outside.
+bool make_map(CUtensorMap *map, const void *base, int64_t inner, int64_t rows, int64_t pitch, int planes,
+              int64_t plane, int box_rows) {
+    EncodeTiled fn = encode_tiled();
+    if (!fn) return false;
+    const cuuint64_t dims[3] = {(cuuint64_t)inner, (cuuint64_t)rows, (cuuint64_t)planes};
+    const cuuint64_t strides[2] = {(cuuint64_t)pitch * 2, (cuuint64_t)plane * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, ones[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides, box, ones,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int MODE, typename T>
+cudaError_t product(const CUtensorMap &a, const CUtensorMap &b, const Gemm &g, int64_t items, cudaStream_t s) {
+    cudaError_t e = cudaFuncSetAttribute(xent_product_kernel<MODE, T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                         (int)kSmem);
+    if (e != cudaSuccess) return e;
+    const unsigned clusters = (unsigned)std::max<int64_t>(1, std::min<int64_t>(items, kClusters));
+    xent_product_kernel<MODE, T><<<2 * clusters, kThreads, kSmem, s>>>(a, b, g);
     return cudaGetLastError();
 }
 
-template <typename T, typename I>
-cudaError_t run_backward(Args a, cudaStream_t s, int *launches) {
-    for (int v0 = 0; v0 < a.V; v0 += kPiece) {
-        a.v0 = v0;
-        a.vc = std::min(kPiece, a.V - v0);
-        if (a.M > 0) {
-            xent_piece_kernel<T, I><<<dim3(tiles(a.vc), tiles(a.M)), 256, 0, s>>>(a);
-            xent_grad_hidden_kernel<T, I><<<dim3(tiles(a.D), tiles(a.M)), 256, 0, s>>>(a);
-            *launches += 2;
-        }
-        xent_grad_weight_kernel<T, I><<<dim3(tiles(a.D), tiles(a.vc)), 256, 0, s>>>(a);
-        *launches += 1;
+struct Call {
+    const dendsn_xent_config *cfg;
+    Plan pl;
+    char *scratch;
+    cudaStream_t s;
+    int launches;
+    template <typename P> P *at(size_t offset) const { return reinterpret_cast<P *>(scratch + offset); }
+};
+
+Rows rows_of(const Call &c) {
+    Rows r{};
+    r.ctl = c.at<Ctl>(0);
+    r.index = c.at<int32_t>(c.pl.index);
+    r.label = c.at<int32_t>(c.pl.label);
+    r.where = c.at<int32_t>(c.pl.where);
+    r.lse = c.at<float>(c.pl.lse);
+    r.weight = c.at<float>(c.pl.weight);
+    r.picked = c.at<float>(c.pl.picked);
+    return r;
+}
+
+// The operands both passes share: packed rows, and the weights packed or as they are.
+template <typename T>
+cudaError_t operands(Call &c, const void *hidden, const void *weight, const __nv_bfloat16 **w, int32_t *w_pitch,
+                     int64_t *w_inner) {
+    const Plan &p = c.pl;
+    const int D = c.cfg->D;
+    xent_pack_kernel<T><<<(unsigned)((p.Mp + 7) / 8), 256, 0, c.s>>>(
+        static_cast<const T *>(hidden), c.at<__nv_bfloat16>(p.H), c.at<int32_t>(p.index), c.at<Ctl>(0), p.Mp, D, p.Dp,
+        p.Mp * p.Dp);
+    c.launches += 1;
+    if (sizeof(T) == 2 && D % 8 == 0 && seq_aligned(weight, 16)) {
+        *w = static_cast<const __nv_bfloat16 *>(weight);
+        *w_pitch = D;
+        *w_inner = D;
+    } else {
+        xent_pack_kernel<T><<<(unsigned)(((int64_t)c.cfg->V + 7) / 8), 256, 0, c.s>>>(
+            static_cast<const T *>(weight), c.at<__nv_bfloat16>(p.W), nullptr, nullptr, c.cfg->V, D, p.Dp,
+            (int64_t)c.cfg->V * p.Dp);
+        c.launches += 1;
+        *w = c.at<__nv_bfloat16>(p.W);
+        *w_pitch = p.Dp;
+        *w_inner = p.Dp;
     }
     return cudaGetLastError();
+}
+
+template <typename I>
+cudaError_t find_rows(Call &c, const void *labels, float *loss, float *lse_out, const float *lse, const float *gloss) {
+    xent_rows_kernel<I><<<1, 1024, 0, c.s>>>(rows_of(c), labels, c.cfg->M, c.cfg->V, c.cfg->ignore_index, loss, lse_out,
+                                             lse, gloss);
+    c.launches += 1;
+    return cudaGetLastError();
+}
+
+template <typename T>
+dendsn_status run_forward(Call &c, const void *hidden, const void *weight, const void *labels, float *loss, float *lse) {
+    const Plan &p = c.pl;
+    const int V = c.cfg->V;
+    const __nv_bfloat16 *w = nullptr;
+    int32_t w_pitch = 0;
+    int64_t w_inner = 0;
+    cudaError_t e = c.cfg->labels_dtype == DENDSN_I64 ? find_rows<int64_t>(c, labels, loss, lse, nullptr, nullptr)
+                                                      : find_rows<int32_t>(c, labels, loss, lse, nullptr, nullptr);
+    if (e == cudaSuccess) e = operands<T>(c, hidden, weight, &w, &w_pitch, &w_inner);
+    CUtensorMap a, b;
+    if (e == cudaSuccess) {
+        if (!make_map(&a, c.at<void>(p.H), p.Dp, p.Mp, p.Dp, p.terms, p.Mp * p.Dp, 128) ||
+            !make_map(&b, w, w_inner, V, w_pitch, p.terms, (int64_t)V * w_pitch, 128))
+            return seq_fail(DENDSN_ERR_CUDA, "tensor map refused");
+        Gemm g{};
+        g.ctl = c.at<Ctl>(0);
+        g.label = c.at<int32_t>(p.label);
+        g.picked = c.at<float>(p.picked);
+        g.part = c.at<float2>(p.part);
+        g.Mp = p.Mp;
+        g.nt = p.nt;
+        g.splits = 1;
+        g.kb = g.kb_split = p.Dp / kTileK;
+        g.V = V;
+        g.D = c.cfg->D;
+        e = product<STATS, T>(a, b, g, (int64_t)p.mt * p.nt, c.s);
+        c.launches += 1;
+    }
+    if (e == cudaSuccess) {
+        xent_join_kernel<<<(unsigned)((p.Mp + 31) / 32), 256, 0, c.s>>>(rows_of(c), c.at<float2>(p.part), 2 * p.nt, p.Mp,
+                                                                        loss, lse);
+        c.launches += 1;
+        e = cudaGetLastError();
+    }
+    if (e != cudaSuccess) return seq_fail(DENDSN_ERR_CUDA, "xent forward launch failed: %s", cudaGetErrorString(e));
+    return DENDSN_OK;
+}
+
+template <typename T>
+dendsn_status run_backward(Call &c, const void *hidden, const void *weight, const void *labels, const float *lse,
+                           const float *gloss, void *gh, void *gw) {
+    const Plan &p = c.pl;
+    const int V = c.cfg->V, D = c.cfg->D;
+    const __nv_bfloat16 *w = nullptr;
+    int32_t w_pitch = 0;
+    int64_t w_inner = 0;
+    cudaError_t e = c.cfg->labels_dtype == DENDSN_I64 ? find_rows<int64_t>(c, labels, nullptr, nullptr, lse, gloss)
+                                                      : find_rows<int32_t>(c, labels, nullptr, nullptr, lse, gloss);
+    if (e == cudaSuccess) e = operands<T>(c, hidden, weight, &w, &w_pitch, &w_inner);
+    CUtensorMap h_rows, h_cols, w_rows, w_cols;
+    const __nv_bfloat16 *H = c.at<__nv_bfloat16>(p.H);
+    __nv_bfloat16 *G = c.at<__nv_bfloat16>(p.G);
+    const int64_t hplane = p.Mp * p.Dp, wplane = (int64_t)V * w_pitch, gplane = p.Mp * p.pitch;
+    if (e == cudaSuccess &&
+        (!make_map(&h_rows, H, p.Dp, p.Mp, p.Dp, p.terms, hplane, 128) ||
+         !make_map(&h_cols, H, p.Dp, p.Mp, p.Dp, p.terms, hplane, 64) ||
+         !make_map(&w_rows, w, w_inner, V, w_pitch, p.terms, wplane, 128) ||
+         !make_map(&w_cols, w, w_inner, V, w_pitch, p.terms, wplane, 64)))
+        return seq_fail(DENDSN_ERR_CUDA, "tensor map refused");
+    Gemm g{};
+    g.ctl = c.at<Ctl>(0);
+    g.label = c.at<int32_t>(p.label);
+    g.lse = c.at<float>(p.lse);
+    g.weight = c.at<float>(p.weight);
+    g.G = G;
+    g.sum = c.at<float>(p.sum);
+    g.gw = gw;
+    g.Mp = p.Mp;
+    g.gplane = gplane;
+    g.pitch = p.pitch;
+    g.V = V;
+    g.D = D;
+    g.wide = D * sizeof(T) % 16 == 0 && seq_aligned(gw, 16);
+    for (int32_t v0 = 0; e == cudaSuccess && v0 < V; v0 += p.pitch) {
+        g.v0 = v0;
+        g.vc = std::min(p.pitch, V - v0);
+        CUtensorMap g_rows, g_cols;
+        if (!make_map(&g_rows, G, g.vc, p.Mp, p.pitch, p.terms, gplane, 128) ||
+            !make_map(&g_cols, G, g.vc, p.Mp, p.pitch, p.terms, gplane, 64))
+            return seq_fail(DENDSN_ERR_CUDA, "tensor map refused");
+        const int32_t vt = up(g.vc, kTileM) / kTileM;
+        g.nt = vt;
+        g.splits = 1;
+        g.kb = g.kb_split = p.Dp / kTileK;
+        e = product<PIECE, T>(h_rows, w_rows, g, (int64_t)p.mt * vt, c.s);
+        if (e != cudaSuccess) break;
+        g.nt = p.dt;
+        g.splits = p.splits;
+        g.kb = up(g.vc, kTileK) / kTileK;
+        g.kb_split = p.kb_split;
+        e = product<HIDDEN, T>(g_rows, w_cols, g, (int64_t)p.mt * p.dt * p.splits, c.s);
+        if (e != cudaSuccess) break;
+        g.mt = vt;
+        g.nt = p.dt;
+        g.splits = 1;
+        e = product<WEIGHT, T>(g_cols, h_cols, g, (int64_t)vt * p.dt, c.s);
+        c.launches += 3;
+    }
+    if (e == cudaSuccess) {
+        xent_hidden_kernel<T><<<(unsigned)(((int64_t)c.cfg->M + 7) / 8), 256, 0, c.s>>>(
+            rows_of(c), c.at<float>(p.sum), static_cast<T *>(gh), c.cfg->M, p.Mp, D, p.Dq, p.splits);
+        c.launches += 1;
+        e = cudaGetLastError();
+    }
+    if (e != cudaSuccess) return seq_fail(DENDSN_ERR_CUDA, "xent backward launch failed: %s", cudaGetErrorString(e));
+    return DENDSN_OK;
 }
 
 }  // namespace
@@ -244,8 +787,8 @@ dendsn_status dendsn_xent_workspace_size(const dendsn_xent_config *cfg, size_t *
 dendsn_status dendsn_xent_forward(const dendsn_xent_config *cfg, const void *hidden, const void *weight,
                                   const void *labels, float *loss, float *lse, void *scratch,
                                   void *stream) {
-    Plan pl;
-    dendsn_status st = make_plan(cfg, &pl);
+    Call c{};
+    dendsn_status st = make_plan(cfg, &c.pl);
     if (st != DENDSN_OK) return st;
     if (cfg->M == 0) return DENDSN_OK;
     if (!hidden || !weight || !labels || !loss || !lse)
@@ -254,31 +797,22 @@ dendsn_status dendsn_xent_forward(const dendsn_xent_config *cfg, const void *hid
     if (!seq_aligned(hidden, bf ? 2 : 4) || !seq_aligned(weight, bf ? 2 : 4) || !seq_aligned(labels, i64 ? 8 : 4) ||
         !seq_aligned(loss, 4) || !seq_aligned(lse, 4))
         return seq_fail(DENDSN_ERR_MISALIGNED, "a tensor is misaligned");
-    if (pl.fwd && !scratch) return seq_fail(DENDSN_ERR_INVALID_ARG, "scratch is NULL");
+    if (!scratch) return seq_fail(DENDSN_ERR_INVALID_ARG, "scratch is NULL");
     if (!seq_aligned(scratch, 256)) return seq_fail(DENDSN_ERR_MISALIGNED, "scratch must be 256-byte aligned");
-    Args a{};
-    a.hidden = hidden;
-    a.weight = weight;
-    a.labels = labels;
-    a.ignore = cfg->ignore_index;
-    a.M = cfg->M;
-    a.V = cfg->V;
-    a.D = cfg->D;
-    a.loss = loss;
-    a.lse = lse;
-    cudaStream_t s = static_cast<cudaStream_t>(stream);
-    cudaError_t e = bf ? (i64 ? run_forward<__nv_bfloat16, int64_t>(a, s) : run_forward<__nv_bfloat16, int32_t>(a, s))
-                       : (i64 ? run_forward<float, int64_t>(a, s) : run_forward<float, int32_t>(a, s));
-    if (e != cudaSuccess) return seq_fail(DENDSN_ERR_CUDA, "xent forward launch failed: %s", cudaGetErrorString(e));
-    seq_count_launches(1);
-    return DENDSN_OK;
+    c.cfg = cfg;
+    c.scratch = static_cast<char *>(scratch);
+    c.s = static_cast<cudaStream_t>(stream);
+    st = bf ? run_forward<__nv_bfloat16>(c, hidden, weight, labels, loss, lse)
+            : run_forward<float>(c, hidden, weight, labels, loss, lse);
+    seq_count_launches(c.launches);
+    return st;
 }
 
 dendsn_status dendsn_xent_backward(const dendsn_xent_config *cfg, const void *hidden, const void *weight,
                                    const void *labels, const float *lse, const float *grad_loss,
                                    void *grad_hidden, void *grad_weight, void *scratch, void *stream) {
-    Plan pl;
-    dendsn_status st = make_plan(cfg, &pl);
+    Call c{};
+    dendsn_status st = make_plan(cfg, &c.pl);
     if (st != DENDSN_OK) return st;
     if (!grad_weight || !weight) return seq_fail(DENDSN_ERR_INVALID_ARG, "weight or grad_weight is NULL");
     if (cfg->M > 0 && (!hidden || !labels || !lse || !grad_loss || !grad_hidden))
@@ -289,31 +823,20 @@ dendsn_status dendsn_xent_backward(const dendsn_xent_config *cfg, const void *hi
         !seq_aligned(grad_weight, sx) || !seq_aligned(labels, i64 ? 8 : 4) || !seq_aligned(lse, 4) ||
         !seq_aligned(grad_loss, 4))
         return seq_fail(DENDSN_ERR_MISALIGNED, "a tensor is misaligned");
-    if (pl.bwd && !scratch) return seq_fail(DENDSN_ERR_INVALID_ARG, "scratch is NULL");
+    if (!scratch) return seq_fail(DENDSN_ERR_INVALID_ARG, "scratch is NULL");
     if (!seq_aligned(scratch, 256)) return seq_fail(DENDSN_ERR_MISALIGNED, "scratch must be 256-byte aligned");
-    Args a{};
-    a.hidden = hidden;
-    a.weight = weight;
-    a.labels = labels;
-    a.ignore = cfg->ignore_index;
-    a.M = cfg->M;
-    a.V = cfg->V;
-    a.D = cfg->D;
-    a.lse_in = lse;
-    a.gloss = grad_loss;
-    a.gh = grad_hidden;
-    a.gw = grad_weight;
-    a.gh32 = static_cast<float *>(scratch);
-    a.G = reinterpret_cast<float *>(static_cast<char *>(scratch) + pl.gh32);
-    cudaStream_t s = static_cast<cudaStream_t>(stream);
-    int launches = 0;
-    cudaError_t e = bf ? (i64 ? run_backward<__nv_bfloat16, int64_t>(a, s, &launches)
-                              : run_backward<__nv_bfloat16, int32_t>(a, s, &launches))
-                       : (i64 ? run_backward<float, int64_t>(a, s, &launches)
-                              : run_backward<float, int32_t>(a, s, &launches));
-    if (e != cudaSuccess) return seq_fail(DENDSN_ERR_CUDA, "xent backward launch failed: %s", cudaGetErrorString(e));
-    seq_count_launches(launches);
-    return DENDSN_OK;
+    c.cfg = cfg;
+    c.scratch = static_cast<char *>(scratch);
+    c.s = static_cast<cudaStream_t>(stream);
+    if (cfg->M == 0) {
+        cudaError_t e = cudaMemsetAsync(grad_weight, 0, (size_t)cfg->V * cfg->D * sx, c.s);
+        if (e != cudaSuccess) return seq_fail(DENDSN_ERR_CUDA, "memset failed: %s", cudaGetErrorString(e));
+        return DENDSN_OK;
+    }
+    st = bf ? run_backward<__nv_bfloat16>(c, hidden, weight, labels, lse, grad_loss, grad_hidden, grad_weight)
+            : run_backward<float>(c, hidden, weight, labels, lse, grad_loss, grad_hidden, grad_weight);
+    seq_count_launches(c.launches);
+    return st;
 }
 
 }  // extern "C"
