@@ -1,14 +1,15 @@
 // Gated compartment scan: h[t] = a[t] h[t-1] + u[t] with an input-dependent decay a, and its
 // backward. State in float32.
 //
-// Split. A thread owns VEC neighbouring channels and a segment of S steps; the eight warps of
-// a block stand side by side in time (WT of them) and in channels, and the blocks of a cluster
-// follow one another in time. A segment of the recurrence is the map h -> A h + B with
+// Split. A thread owns a pair of neighbouring channels and a segment of S steps; the 256
+// threads of a block are Q segments one after the other of 256 / Q pairs, and the blocks of a
+// cluster follow one another in time. A segment of the recurrence is the map h -> A h + B with
 // A = prod a, B = its end from a zero state, so a pass is: load the segment into registers,
 // form (A, B), fold the maps of the earlier segments over the state (shared memory within the
 // block, distributed shared memory between the blocks of the cluster), then run the segment
-// from its true state and write. Every element is read and written once; the loads of the next
-// pass are issued before the fold, so that its barriers overlap with memory.
+// from its true state and write. Every element is read and written once; the rows of the
+// passes to come are copied to shared memory meanwhile (cp.async, 16 bytes a thread where rows
+// are aligned), each warp its own segments, so that registers hold one segment only.
 // A start makes its segment's map constant; that is kept as a flag and selected, not
 // multiplied by zero, so that what came before it cannot leak as NaN.
 //
@@ -16,6 +17,9 @@
 // mu -> A mu + L of mu[t] = a[t] (grad_h[t] + mu[t+1]), and recomputes h from x, gate and the
 // state kept every 64 steps: three arrays read and two written, against four read if h were
 // kept, and no rounding of h to the output's type enters the gradient.
+//
+// Bound: 6 (forward) and 10 bytes (backward) of a bfloat16 element against the instructions on
+// it; the arithmetic runs on pairs (f32x2), which halves it.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 
@@ -27,6 +31,10 @@ namespace dendsn {
 namespace {
 
 constexpr int kInterval = 64;     // steps between checkpoints
+// Passes in shared memory at once. Two blocks of an SM have to fit (a cluster of 8 that finds one
+// block an SM waits for a second round: scan_long forward 51 -> 150 us with a third float32 stage).
+template <typename XT> constexpr int kForwardStages = sizeof(XT) == 2 ? 4 : 2;
+template <typename XT> constexpr int kBackwardStages = sizeof(XT) == 2 ? 3 : 2;
 
 struct ScanArgs {
     int64_t M;                    // channels B * N
@@ -38,392 +46,671 @@ struct ScanArgs {
     const float *h0, *glast;
     void *h, *gx, *gg;
     float *last, *saved, *gh0;
-    int32_t WT, WC, CT;           // warps along time and channels, blocks of a cluster
+    int32_t Q, CT;                // segments of a block, blocks of a cluster
+    int32_t PN;                   // pairs of a sample
+    int64_t pairs;                // in all
 };
 
-// VEC elements of a row, loaded and stored at once, held as they are until they are used.
-template <typename XT, int VEC> struct Row;
-template <int VEC> struct Row<float, VEC> {
-    using Raw = typename std::conditional<VEC == 4, float4,
-                typename std::conditional<VEC == 2, float2, float>::type>::type;
-    static __device__ __forceinline__ void unpack(const Raw &r, float (&v)[VEC]) {
-        if constexpr (VEC == 4) { v[0] = r.x; v[1] = r.y; v[2] = r.z; v[3] = r.w; }
-        else if constexpr (VEC == 2) { v[0] = r.x; v[1] = r.y; }
-        else v[0] = r;
-    }
-    static __device__ __forceinline__ Raw pack(const float (&v)[VEC]) {
-        if constexpr (VEC == 4) return make_float4(v[0], v[1], v[2], v[3]);
-        else if constexpr (VEC == 2) return make_float2(v[0], v[1]);
-        else return v[0];
-    }
+// ------------------------------------------------------------------ pairs
+// Two float32 values in one 64-bit register, as the paired instructions take them.
+struct F2 {
+    uint64_t v;
+    F2() = default;
+    __device__ __forceinline__ explicit F2(uint64_t raw) : v(raw) {}
+    __device__ __forceinline__ F2(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
+    __device__ __forceinline__ float x() const { return __uint_as_float((uint32_t)v); }
+    __device__ __forceinline__ float y() const { return __uint_as_float((uint32_t)(v >> 32)); }
 };
-template <int VEC> struct Row<__nv_bfloat16, VEC> {
-    using Raw = typename std::conditional<VEC == 4, uint2,
-                typename std::conditional<VEC == 2, uint32_t, uint16_t>::type>::type;
-    static __device__ __forceinline__ float lo(uint32_t q) { return __uint_as_float(q << 16); }
-    static __device__ __forceinline__ float hi(uint32_t q) { return __uint_as_float(q & 0xffff0000u); }
-    static __device__ __forceinline__ uint32_t two(float a, float b) {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+__device__ __forceinline__ F2 both(float v) { return F2(v, v); }
+__device__ __forceinline__ F2 mul(F2 a, F2 b) {
+    F2 d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v));
+    return d;
+}
+__device__ __forceinline__ F2 add(F2 a, F2 b) {
+    F2 d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v));
+    return d;
+}
+__device__ __forceinline__ F2 fma(F2 a, F2 b, F2 c) {
+    F2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return d;
+}
+__device__ __forceinline__ float exp2_fast(float v) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float rcp_fast(float v) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+
+// One element and a pair of elements as they lie in memory.
+template <typename XT> struct Elem;
+template <> struct Elem<float> {
+    using One = float;
+    using Pair = float2;
+    static __device__ __forceinline__ Pair pair(One a, One b) { return make_float2(a, b); }
+    static __device__ __forceinline__ One first(Pair p) { return p.x; }
+    static __device__ __forceinline__ One second(Pair p) { return p.y; }
+    static __device__ __forceinline__ F2 unpack(Pair p) { return F2(p.x, p.y); }
+    static __device__ __forceinline__ Pair pack(F2 v) { return make_float2(v.x(), v.y()); }
+};
+template <> struct Elem<__nv_bfloat16> {
+    using One = uint16_t;
+    using Pair = uint32_t;
+    static __device__ __forceinline__ Pair pair(One a, One b) { return (uint32_t)a | (uint32_t)b << 16; }
+    static __device__ __forceinline__ One first(Pair p) { return (One)p; }
+    static __device__ __forceinline__ One second(Pair p) { return (One)(p >> 16); }
+    static __device__ __forceinline__ F2 unpack(Pair p) {
+        return F2(__uint_as_float(p << 16), __uint_as_float(p & 0xffff0000u));
+    }
+    static __device__ __forceinline__ Pair pack(F2 v) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(v.x(), v.y());
         return *reinterpret_cast<const uint32_t *>(&h);
     }
-    static __device__ __forceinline__ void unpack(const Raw &r, float (&v)[VEC]) {
-        if constexpr (VEC == 4) { v[0] = lo(r.x); v[1] = hi(r.x); v[2] = lo(r.y); v[3] = hi(r.y); }
-        else if constexpr (VEC == 2) { v[0] = lo(r); v[1] = hi(r); }
-        else v[0] = lo(r);
-    }
-    static __device__ __forceinline__ Raw pack(const float (&v)[VEC]) {
-        if constexpr (VEC == 4) return make_uint2(two(v[0], v[1]), two(v[2], v[3]));
-        else if constexpr (VEC == 2) return two(v[0], v[1]);
-        else {
-            const __nv_bfloat16 h = __float2bfloat16_rn(v[0]);
-            return *reinterpret_cast<const uint16_t *>(&h);
-        }
-    }
 };
 
-template <typename XT, int VEC>
-__device__ __forceinline__ typename Row<XT, VEC>::Raw load_row(const void *p, int64_t at) {
-    return __ldcs(reinterpret_cast<const typename Row<XT, VEC>::Raw *>(static_cast<const XT *>(p) + at));
-}
-template <typename XT, int VEC>
-__device__ __forceinline__ void store_row(void *p, int64_t at, const float (&v)[VEC]) {
-    __stcs(reinterpret_cast<typename Row<XT, VEC>::Raw *>(static_cast<XT *>(p) + at), Row<XT, VEC>::pack(v));
-}
-
-// a and 1 - a. Of a logistic decay both come from e = exp(-|g|), each with its own relative
+// a and 1 - a. Of a logistic decay both come from e = exp(-g), each with its own relative
 // precision: 1 / (1 + e) and e / (1 + e). bfloat16 gates take the hardware's exponential and
-// reciprocal (about 2^-21 relative), float32 gates the correctly rounded forms.
-template <typename XT, bool LOGIT> __device__ __forceinline__ void decay_of(float g, float &a, float &na) {
+// reciprocal (about 2^-21 relative) and are kept above -80, where a is below 2e-35 and e still
+// finite. float32 gates correct the exponent's rounding and take a Newton step (about 2^-22);
+// beyond 88.5 of 0 the smaller of the two is flushed to 0.
+template <bool LOGIT> __device__ __forceinline__ void decay_of(uint32_t raw, F2 &a, F2 &na) {
     if constexpr (LOGIT) {
-        constexpr bool fast = sizeof(XT) == 2;
-        const float e = fast ? __expf(-fabsf(g)) : expf(-fabsf(g));
-        const float r = fast ? __fdividef(1.f, 1.f + e) : 1.f / (1.f + e);
-        const float q = e * r;
-        a = g >= 0.f ? r : q;
-        na = g >= 0.f ? q : r;
-        if (g != g) a = na = g;
+        uint32_t g;
+        asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(g) : "r"(raw), "r"(0xC2A0C2A0u));
+        const F2 t = mul(Elem<__nv_bfloat16>::unpack(g), both(-1.4426950408889634f));
+        const F2 e(exp2_fast(t.x()), exp2_fast(t.y())), d = add(e, both(1.f));
+        a = F2(rcp_fast(d.x()), rcp_fast(d.y()));
+        na = mul(e, a);
     } else {
-        a = g;
-        na = 1.f - g;
+        a = Elem<__nv_bfloat16>::unpack(raw);
+        na = fma(a, both(-1.f), both(1.f));
+    }
+}
+template <bool LOGIT> __device__ __forceinline__ void decay_of(float2 raw, F2 &a, F2 &na) {
+    if constexpr (LOGIT) {
+        float g0, g1;
+        asm("max.NaN.f32 %0, %1, %2;\n\tmin.NaN.f32 %0, %0, %3;" : "=&f"(g0) : "f"(raw.x), "f"(-88.5f), "f"(88.5f));
+        asm("max.NaN.f32 %0, %1, %2;\n\tmin.NaN.f32 %0, %0, %3;" : "=&f"(g1) : "f"(raw.y), "f"(-88.5f), "f"(88.5f));
+        const F2 g(g0, g1), c = both(-1.4426950408889634f), t = mul(g, c), off = fma(g, c, mul(t, both(-1.f)));
+        F2 e(exp2_fast(t.x()), exp2_fast(t.y()));
+        e = fma(mul(e, off), both(0.6931471805599453f), e);
+        const F2 d = add(e, both(1.f)), r(rcp_fast(d.x()), rcp_fast(d.y()));
+        a = mul(r, fma(mul(d, both(-1.f)), r, both(2.f)));
+        const F2 up = mul(e, a), down = fma(a, both(-1.f), both(1.f));
+        na = F2(g0 < 0.f ? down.x() : up.x(), g1 < 0.f ? down.y() : up.y());
+    } else {
+        a = F2(raw.x, raw.y);
+        na = fma(a, both(-1.f), both(1.f));
     }
 }
 
-// A h + B of a segment's map over a state, B alone where the segment has a start; a state of
-// zero stays zero under a product of decays that overflowed.
-__device__ __forceinline__ float map_over(float A, float B, int cut, float h) {
-    return cut || h == 0.f ? B : fmaf(A, h, B);
+// A h + B of a segment's map over a state, B alone where the segment has a start.
+__device__ __forceinline__ F2 map_over(F2 A, F2 B, bool cut, F2 h) {
+    const F2 r = fma(A, h, B);
+    return cut ? B : r;
 }
+// A product of decays, kept finite: a state of zero stays zero under decays above 1 whose
+// product overflows. (Where a decay is NaN, so is the segment's end.)
+template <bool LOGIT> __device__ __forceinline__ F2 finite(F2 A) {
+    constexpr float top = 3.402823466e38f;
+    if constexpr (LOGIT) return A;
+    else return F2(fminf(fmaxf(A.x(), -top), top), fminf(fmaxf(A.y(), -top), top));
+}
+struct alignas(16) Map {
+    F2 A, B;
+};
+__device__ __forceinline__ F2 over(const Map &m, bool cut, F2 h) { return map_over(m.A, m.B, cut, h); }
 
-// The maps of the block's warps, of the block as a whole (two buffers, read by the cluster's
-// other blocks) and of the cluster's blocks.
-template <int VEC> struct ScanShared {
-    float A[8][32][VEC], B[8][32][VEC];
-    float tA[2][32][VEC], tB[2][32][VEC];
-    float rA[2][8][32][VEC], rB[2][8][32][VEC];
-    int cut[8][32], tcut[2][32], rcut[2][8][32];
+// Maps of the segments, in two buffers of alternating passes.
+template <bool CL> struct ScanShared {
+    Map map[2][256];                             // [segment in the order of the fold][pair]
+    F2 carry[2][256];                            // the state at the end of a pass
+    Map block[2][CL ? 8 : 1][CL ? 32 : 1];       // maps of the cluster's blocks
+    int32_t block_cut[2][CL ? 8 : 1][CL ? 32 : 1];
+    uint64_t arrived[2];                         // barriers that count their bytes
+    bool cut[2][256];
 };
 
-// Folds the segment maps over `carry`, the state at the pass's first step (the last one, when
-// REVERSE). Returns in `in` the state before this warp's segment; advances carry by the pass.
-template <int VEC, bool CL, bool REVERSE>
-__device__ __forceinline__ void fold(ScanShared<VEC> &sh, const ScanArgs &P, int wt, int wc, int lane,
-                                     int rank, int pass, const float (&A)[VEC], const float (&B)[VEC],
-                                     int cut, float (&carry)[VEC], float (&in)[VEC]) {
-    const int w0 = wc * P.WT;
-    if (!CL || pass) __syncthreads();         // the maps of the pass before are read
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-        sh.A[w0 + wt][lane][e] = A[e];
-        sh.B[w0 + wt][lane][e] = B[e];
+// Blocks of a cluster hand one another their maps by asynchronous stores, which count
+// themselves in on the receiver's barrier: a cluster-wide barrier would also wait for every
+// write of h on its way to memory (measured: scan_long forward 71 us with it).
+// Buffers need no other guard: a block sends pass k + 2 after it has every map of pass k + 1,
+// and a block sends those after its threads have read pass k.
+template <bool CL> struct Exchange {
+    ScanShared<CL> &sh;
+    const ScanArgs &P;
+    int width;
+    __device__ __forceinline__ static uint32_t addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+    __device__ __forceinline__ void expect(int buf) const {
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(addr(&sh.arrived[buf])),
+                     "r"(P.CT * width * 20) : "memory");
     }
-    sh.cut[w0 + wt][lane] = cut;
-    __syncthreads();
-    if constexpr (CL) {
-        namespace cg = cooperative_groups;
-        cg::cluster_group cluster = cg::this_cluster();
-        const int buf = pass & 1;
-        if (wt == 0) {                        // the block's own map
-            float tA[VEC], tB[VEC];
-            int tc = 0;
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) { tA[e] = 1.f; tB[e] = 0.f; }
-            for (int i = 0; i < P.WT; ++i) {
-                const int w = w0 + (REVERSE ? P.WT - 1 - i : i);
-                const int c = sh.cut[w][lane];
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float a = sh.A[w][lane][e];
-                    tB[e] = map_over(a, sh.B[w][lane][e], c, tB[e]);
-                    tA[e] *= a;
-                }
-                tc |= c;
+    __device__ __forceinline__ void begin() const {
+        if (threadIdx.x == 0) {
+            for (int i = 0; i < 2; ++i)
+                asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(addr(&sh.arrived[i])) : "memory");
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+            expect(0);
+            expect(1);
+        }
+        cooperative_groups::this_cluster().sync();
+    }
+    __device__ __forceinline__ void send(int buf, int mine, int cp, const Map &m, bool cut) const {
+        for (int r = 0; r < P.CT; ++r) {
+            uint32_t to, flag, bar;
+            asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(addr(&sh.block[buf][mine][cp])), "r"(r));
+            asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(flag) : "r"(addr(&sh.block_cut[buf][mine][cp])), "r"(r));
+            asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(bar) : "r"(addr(&sh.arrived[buf])), "r"(r));
+            asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];"
+                         ::"r"(to), "f"(m.A.x()), "f"(m.A.y()), "f"(m.B.x()), "f"(m.B.y()), "r"(bar) : "memory");
+            asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::"r"(flag),
+                         "r"((int)cut), "r"(bar) : "memory");
+        }
+    }
+    // Waits for the maps of a pass; false where they did not come within about a second.
+    __device__ __forceinline__ bool wait(int buf, uint32_t parity) const {
+        uint64_t began = 0;
+        for (uint32_t i = 0;; ++i) {
+            uint32_t done;
+            asm volatile("{\n\t.reg .pred p;\n\t"
+                         "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+                         "selp.u32 %0, 1, 0, p;\n\t}"
+                         : "=r"(done) : "r"(addr(&sh.arrived[buf])), "r"(parity) : "memory");
+            if (done) return true;
+            if (i % 64 == 63) {
+                uint64_t now;
+                asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
+                if (!began) began = now;
+                else if (now - began > 1000000000ull) return false;
             }
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                sh.tA[buf][lane][e] = tA[e];
-                sh.tB[buf][lane][e] = tB[e];
-            }
-            sh.tcut[buf][lane] = tc;
         }
-        cluster.sync();
-        const int warp = threadIdx.x >> 5;
-        if (warp < P.CT) {                    // each warp fetches one block's map
-            const ScanShared<VEC> *from = cluster.map_shared_rank(&sh, warp);
+    }
+};
+
+// Folds the segment maps over the state before the pass; returns the state before this
+// thread's segment, which is number `me` of Q in the order of the fold. One barrier a pass: the
+// maps have two buffers, and the last segment leaves the state behind in sh.carry.
+template <bool CL, bool LOGIT, int MQ>
+__device__ __forceinline__ F2 fold(ScanShared<CL> &sh, const ScanArgs &P, int me, int cp, int width, int mine,
+                                   int pass, F2 A, F2 B, bool cut, F2 &carry) {
+    const int buf = pass & 1;
+    sh.map[buf][me * width + cp] = Map{finite<LOGIT>(A), B};
+    sh.cut[buf][me * width + cp] = cut;
+    F2 in;
+    if constexpr (!CL) {
+        const bool cuts = __syncthreads_or(cut);
+        in = pass ? sh.carry[buf ^ 1][cp] : carry;
+        // unrolled, so that the maps are read together and only the products wait on one another
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                sh.rA[buf][warp][lane][e] = from->tA[buf][lane][e];
-                sh.rB[buf][warp][lane][e] = from->tB[buf][lane][e];
-            }
-            sh.rcut[buf][warp][lane] = from->tcut[buf][lane];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) in[e] = carry[e];
-        for (int i = 0; i < P.CT; ++i) {
-            const int r = REVERSE ? P.CT - 1 - i : i;
-            if (r == rank)
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) in[e] = carry[e];
-            const int c = sh.rcut[buf][r][lane];
-#pragma unroll
-            for (int e = 0; e < VEC; ++e)
-                carry[e] = map_over(sh.rA[buf][r][lane][e], sh.rB[buf][r][lane][e], c, carry[e]);
-        }
-        for (int i = 0; i < (REVERSE ? P.WT - 1 - wt : wt); ++i) {
-            const int w = w0 + (REVERSE ? P.WT - 1 - i : i);
-            const int c = sh.cut[w][lane];
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) in[e] = map_over(sh.A[w][lane][e], sh.B[w][lane][e], c, in[e]);
-        }
+        for (int i = 0; i < MQ - 1; ++i)
+            if (i < me) in = over(sh.map[buf][i * width + cp], cuts && sh.cut[buf][i * width + cp], in);
     } else {
-        for (int i = 0; i < P.WT; ++i) {
-            const int k = REVERSE ? P.WT - 1 - i : i, w = w0 + k;
-            if (k == wt)
+        const Exchange<CL> ex{sh, P, width};
+        const bool cuts = __syncthreads_or(cut);
+        if (me == 0) {                           // the block's map, handed to every block
+            F2 a = both(1.f), b = both(0.f);
+            bool c = false;
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) in[e] = carry[e];
-            const int c = sh.cut[w][lane];
+            for (int i = 0; i < MQ; ++i) {
+                const Map m = sh.map[buf][i * width + cp];
+                const bool ci = cuts && sh.cut[buf][i * width + cp];
+                b = over(m, ci, b);
+                a = finite<LOGIT>(mul(a, m.A));
+                c |= ci;
+            }
+            ex.send(buf, mine, cp, Map{a, b}, c);
+        }
+        if (!ex.wait(buf, pass >> 1 & 1)) carry = both(__int_as_float(0x7fffffff));
+        if (threadIdx.x == 0) ex.expect(buf);
+        in = carry;
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) carry[e] = map_over(sh.A[w][lane][e], sh.B[w][lane][e], c, carry[e]);
+        for (int i = 0; i < 8; ++i)
+            if (i < P.CT) {
+                carry = over(sh.block[buf][i][cp], sh.block_cut[buf][i][cp], carry);
+                if (i + 1 == mine) in = carry;
+            }
+        if (cuts) {
+            for (int i = 0; i < me; ++i) in = over(sh.map[buf][i * width + cp], sh.cut[buf][i * width + cp], in);
+        } else {
+#pragma unroll
+            for (int i = 0; i < MQ - 1; ++i)
+                if (i < me) in = over(sh.map[buf][i * width + cp], false, in);
         }
     }
+    return in;
 }
 
+template <bool CL> __device__ __forceinline__ void enter_cluster(ScanShared<CL> &sh, const ScanArgs &P, int width) {
+    if constexpr (CL) Exchange<CL>{sh, P, width}.begin();
+}
 template <bool CL> __device__ __forceinline__ void leave_cluster() {
-    if constexpr (CL) cooperative_groups::this_cluster().sync();   // no block's maps are still read
+    if constexpr (CL) cooperative_groups::this_cluster().sync();   // no block's memory is still written
 }
 
-template <typename XT, int VEC, int S, bool LOGIT, bool MIX, bool CL>
-__global__ void __launch_bounds__(256) scan_forward_kernel(const ScanArgs P) {
-    using R = Row<XT, VEC>;
-    __shared__ ScanShared<VEC> sh;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, wt = warp % P.WT, wc = warp / P.WT;
-    const int rank = CL ? blockIdx.x % P.CT : 0;
-    const int64_t m = ((int64_t)(CL ? blockIdx.x / P.CT : blockIdx.x) * P.WC * 32 + wc * 32 + lane) * VEC;
-    const bool on = m < P.M;
-    const int64_t b = on ? m / P.N : 0, off = on ? b * P.sb + m % P.N : 0;
-    float carry[VEC];
+__device__ __forceinline__ void copies_issued() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// Waits for all but the last `N` groups of the thread's copies, then for its warp.
+template <int N> __device__ __forceinline__ void copies_landed() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+    __syncwarp();
+}
+// Pairs between the segments of a stage: half-warps of 4-byte pairs would meet in the same banks.
+template <typename XT, int S> __host__ __device__ constexpr int segment_pairs(int width) {
+    return S * width + (sizeof(XT) == 2 && width == 16 ? 16 : 0);
+}
+
+// Where a thread stands: its pair of channels and its segment.
+template <typename XT, bool WIDE, int S, bool CL> struct Place {
+    using E = Elem<XT>;
+    using One = typename E::One;
+    using Pair = typename E::Pair;
+    int width, cp, q, rank;      // pairs of the block, own pair, own segment, block in the cluster
+    int64_t m, b;                // first channel, its sample
+    bool on, on2;                // the pair, its second channel
+    int64_t sample;              // of the first of the warp's pairs of the segment
+    bool one_sample;             // it is that of the others too
+    int span, step;              // steps of the block, of a pass
+    int64_t base;                // elements to the block's first channel
+    uint32_t off, st;            // bytes to the thread's channels and segment, of a step
+    uint32_t piece_off;          // bytes to the piece of a row that the thread copies
+    bool piece_on;
+    __device__ __forceinline__ explicit Place(const ScanArgs &P) {
+        width = 256 / P.Q;
+        cp = threadIdx.x % width;
+        q = threadIdx.x / width;
+        rank = CL ? blockIdx.x % P.CT : 0;
+        const int64_t g0 = (int64_t)(CL ? blockIdx.x / P.CT : blockIdx.x) * width, g = g0 + cp;
+        on = g < P.pairs;
+        b = on ? g / P.PN : 0;
+        const int64_t n = on ? 2 * (g % P.PN) : 0, b0 = g0 / P.PN, n0 = 2 * (g0 % P.PN);
+        on2 = on && (WIDE || n + 1 < P.N);
+        m = b * P.N + n;
+        span = P.Q * S;
+        step = span * (CL ? P.CT : 1);
+        base = b0 * P.sb + n0;
+        st = (uint32_t)(P.st * sizeof(XT));
+        const int lane = threadIdx.x & 31;
+        sample = __shfl_sync(0xffffffffu, b, lane - lane % min(32, width));
+        one_sample = __all_sync(0xffffffffu, !on || b == sample);
+        off = on ? (uint32_t)(((b - b0) * P.sb + n - n0) * (int64_t)sizeof(XT)) + (uint32_t)(q * S) * st : 0;
+        constexpr int kPairs = 16 / sizeof(Pair);
+        const int64_t gp = g0 + (cp & ~31) + (cp & 31) % (min(32, width) / kPairs) * kPairs;
+        piece_on = gp < P.pairs;
+        piece_off = piece_on ? (uint32_t)((((gp / P.PN) - b0) * P.sb + 2 * (gp % P.PN) - n0) * (int64_t)sizeof(XT)) +
+                                   (uint32_t)(q * S) * st : 0;
+    }
+    // Copies the rows of this thread's segment from `p` into `to`, S rows of `width` pairs; the
+    // threads of a warp share the work where rows are WIDE (16-byte pieces), else each
+    // copies its own pair.
+    __device__ __forceinline__ void copy(Pair *to, const char *p, int left) const {
+        const uint32_t dst = (uint32_t)__cvta_generic_to_shared(to);
+        if constexpr (WIDE) {
+            constexpr int kPairs = 16 / sizeof(Pair), kRows = kPairs;   // pairs of a piece, rows of a round
+            const int across = min(32, width) / kPairs, row = (cp & 31) / across;   // within the warp's pairs
+            const int piece = (cp & ~31) + (cp & 31) % across * kPairs;
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) carry[e] = on && P.h0 ? P.h0[m + e] : 0.f;
+            for (int r = 0; r < S; r += kRows) {
+                const int s = r + row;
+                if (S % kRows == 0 || s < S)
+                    if (piece_on && s < left)
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(
+                                         dst + (uint32_t)((s * width + piece) * sizeof(Pair))),
+                                     "l"(p + (piece_off + s * st)) : "memory");
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < S; ++s)
+                if (on && s < left) {
+                    const One *at = reinterpret_cast<const One *>(p + (off + s * st));
+                    if constexpr (sizeof(One) == 4) {
+                        const uint32_t d = dst + (uint32_t)((s * width + cp) * sizeof(Pair));
+                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(d), "l"(at) : "memory");
+                        if (on2)
+                            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(d + 4), "l"(at + 1) : "memory");
+                    } else {
+                        to[s * width + cp] = E::pair(__ldcs(at), on2 ? __ldcs(at + 1) : One());
+                    }
+                }
+        }
+    }
+    __device__ __forceinline__ void store(char *p, int s, F2 v) const {
+        One *at = reinterpret_cast<One *>(p + (off + s * st));
+        const Pair w = E::pack(v);
+        if constexpr (WIDE) {
+            __stcs(reinterpret_cast<Pair *>(at), w);
+        } else {
+            __stcs(at, E::first(w));
+            if (on2) __stcs(at + 1, E::second(w));
+        }
+    }
+    // States of the pair, [B, N] float32.
+    __device__ __forceinline__ F2 state(const float *p) const {
+        return F2(on && p ? p[m] : 0.f, on2 && p ? p[m + 1] : 0.f);
+    }
+    __device__ __forceinline__ void put_state(float *p, F2 v) const {
+        if (on) p[m] = v.x();
+        if (on2) p[m + 1] = v.y();
+    }
+    // The start flags of the S steps from t0 are requested with the segment's rows (`ask`) and
+    // put together when it begins (`starts`): threads side by side whose pairs are of one
+    // sample read one flag each. Both are called by whole warps.
+    __device__ __forceinline__ uint8_t ask(const ScanArgs &P, int t0) const {
+        const int l = (threadIdx.x & 31) % min(32, width), t = t0 + l;
+        return P.starts && l < S && t >= 0 && t < P.T ? P.starts[(int64_t)t * P.ft + sample * P.fb] : 0;
+    }
+    __device__ __forceinline__ uint32_t starts(const ScanArgs &P, int t0, uint8_t asked) const {
+        if (!P.starts) return 0;
+        const int lane = threadIdx.x & 31, lane0 = lane - lane % min(32, width);
+        if (one_sample) return __ballot_sync(0xffffffffu, asked) >> lane0 & ((1u << S) - 1);
+        uint32_t f = 0;
+        if (on)
+#pragma unroll
+            for (int s = 0; s < S; ++s)
+                if (t0 + s < P.T && P.starts[(int64_t)(t0 + s) * P.ft + b * P.fb]) f |= 1u << s;
+        return f;
+    }
+};
+
+template <typename XT, bool WIDE, int S, int MQ, bool LOGIT, bool MIX, bool CL>
+__global__ void __launch_bounds__(256, 2) scan_forward_kernel(const ScanArgs P) {
+    using E = Elem<XT>;
+    using Pair = typename E::Pair;
+    constexpr int kStages = kForwardStages<XT>;
+    __shared__ ScanShared<CL> sh;
+    const Place<XT, WIDE, S, CL> me(P);
+    enter_cluster<CL>(sh, P, me.width);
+    F2 carry = me.state(P.h0);
     if (P.T == 0) {
-        if (on && wt == 0 && rank == 0 && P.last)
-            for (int e = 0; e < VEC; ++e) P.last[m + e] = carry[e];
+        if (me.q == 0 && me.rank == 0 && P.last) me.put_state(P.last, carry);
         leave_cluster<CL>();
         return;
     }
-    const int span = P.WT * S, step = span * (CL ? P.CT : 1);
-    typename R::Raw gr[S], xr[S];
-    uint32_t st = 0;
-    auto fetch = [&](int t0) {
-        st = 0;
-        if (!on) return;
-#pragma unroll
-        for (int s = 0; s < S; ++s)
-            if (t0 + s < P.T) {
-                gr[s] = load_row<XT, VEC>(P.gate, off + (t0 + s) * P.st);
-                xr[s] = load_row<XT, VEC>(P.x, off + (t0 + s) * P.st);
-            }
-        if (P.starts) {
-#pragma unroll
-            for (int s = 0; s < S; ++s)
-                if (t0 + s < P.T && P.starts[(t0 + s) * P.ft + b * P.fb]) st |= 1u << s;
-        }
+    const int64_t first = (me.base + (int64_t)(me.rank * me.span) * P.st) * (int64_t)sizeof(XT);
+    const int64_t hop = (int64_t)me.step * P.st * (int64_t)sizeof(XT);
+    const char *px = static_cast<const char *>(P.x) + first, *pg = static_cast<const char *>(P.gate) + first;
+    char *ph = static_cast<char *>(P.h) + first;
+    extern __shared__ __align__(16) unsigned char dynamic[];
+    const int seg = segment_pairs<XT, S>(me.width), stage_pairs = 2 * P.Q * seg;
+    Pair *slots = reinterpret_cast<Pair *>(dynamic) + me.q * seg;
+    int t0 = me.rank * me.span + me.q * S;
+    uint8_t asked = me.ask(P, t0), next_asked = 0;
+    // the rows of the pass that begins at step t for this thread
+    auto fetch = [&](int stage, int t) {
+        Pair *to = slots + stage * stage_pairs;
+        me.copy(to, pg, P.T - t);
+        me.copy(to + P.Q * seg, px, P.T - t);
+        copies_issued();
+        pg += hop;
+        px += hop;
     };
-    int t0 = rank * span + wt * S;
-    fetch(t0);
-    for (int pass = 0; pass * (int64_t)step < P.T; ++pass) {
-        float a[S][VEC], u[S][VEC], A[VEC], B[VEC], h[VEC];
-        const uint32_t cut = st;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) { A[e] = 1.f; B[e] = 0.f; }
+    for (int i = 0; i < kStages - 1; ++i) fetch(i, t0 + i * me.step);
+    int stage = 0;
+    for (int pass = 0; (int64_t)pass * me.step < P.T; ++pass) {
+        F2 a[S], u[S], A, B;
+        const uint32_t cut = me.starts(P, t0, asked);
+        const int t1 = t0, left = P.T - t0;       // steps of the sequence from this segment on
+        // the usual segments: whole, without a start in any lane
+        const bool plain = __all_sync(0xffffffffu, left >= S && !cut);
+        copies_landed<kStages - 2>();
+        const Pair *gr = slots + stage * stage_pairs + me.cp, *xr = gr + P.Q * seg;
 #pragma unroll
         for (int s = 0; s < S; ++s) {
-            if (on && t0 + s < P.T) {
-                float g[VEC], x[VEC];
-                R::unpack(gr[s], g);
-                R::unpack(xr[s], x);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    float na;
-                    decay_of<XT, LOGIT>(g[e], a[s][e], na);
-                    u[s][e] = MIX ? na * x[e] : x[e];
-                    A[e] *= a[s][e];
-                    B[e] = cut >> s & 1 ? u[s][e] : fmaf(a[s][e], B[e], u[s][e]);
-                }
-            }
+            F2 na;
+            decay_of<LOGIT>(gr[s * me.width], a[s], na);
+            u[s] = E::unpack(xr[s * me.width]);
+            if (MIX) u[s] = mul(u[s], na);
         }
-        const int t1 = t0;
-        t0 += step;
-        fetch(t0);
-        fold<VEC, CL, false>(sh, P, wt, wc, lane, rank, pass, A, B, cut != 0, carry, h);
-        if (on && t1 < P.T) {
-            if (P.saved && t1 && t1 % kInterval == 0)
+        __syncwarp();                             // the stage before this one is free
+        fetch(stage == 0 ? kStages - 1 : stage - 1, t0 + (kStages - 1) * me.step);
+        if (++stage == kStages) stage = 0;
+        next_asked = me.ask(P, t0 + me.step);
+        if (plain) {
+            A = a[0];
+            B = u[0];
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) P.saved[(int64_t)(t1 / kInterval - 1) * P.M + m + e] = h[e];
+            for (int s = 1; s < S; ++s) {
+                A = mul(A, a[s]);
+                B = fma(a[s], B, u[s]);
+            }
+        } else {
+            A = both(1.f);
+            B = both(0.f);
+#pragma unroll
+            for (int s = 0; s < S; ++s)
+                if (s < left) {
+                    A = mul(A, a[s]);
+                    B = cut >> s & 1 ? u[s] : fma(a[s], B, u[s]);
+                }
+        }
+        t0 += me.step;
+        asked = next_asked;
+        F2 h = fold<CL, LOGIT, MQ>(sh, P, me.q, me.cp, me.width, me.rank, pass, A, B, cut != 0, carry);
+        if (P.saved && t1 && t1 < P.T && t1 % kInterval == 0)
+            me.put_state(P.saved + (int64_t)(t1 / kInterval - 1) * P.M, h);
+        if (plain && me.on) {
 #pragma unroll
             for (int s = 0; s < S; ++s) {
-                if (t1 + s < P.T) {
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e)
-                        h[e] = cut >> s & 1 ? u[s][e] : fmaf(a[s][e], h[e], u[s][e]);
-                    store_row<XT, VEC>(P.h, off + (t1 + s) * P.st, h);
-                }
+                h = fma(a[s], h, u[s]);
+                me.store(ph, s, h);
             }
-            if (P.last && P.T - t1 <= S)
+        } else if (me.on) {
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) P.last[m + e] = h[e];
+            for (int s = 0; s < S; ++s)
+                if (s < left) {
+                    h = cut >> s & 1 ? u[s] : fma(a[s], h, u[s]);
+                    me.store(ph, s, h);
+                }
         }
+        ph += hop;
+        if (P.last && left > 0 && left <= S) me.put_state(P.last, h);
+        if (!CL && me.q == P.Q - 1) sh.carry[pass & 1][me.cp] = h;
     }
     leave_cluster<CL>();
 }
 
-template <typename XT, int VEC, int S, bool LOGIT, bool MIX, bool CL>
-__global__ void __launch_bounds__(256) scan_backward_kernel(const ScanArgs P) {
-    using R = Row<XT, VEC>;
-    __shared__ ScanShared<VEC> sh;
-    __shared__ float fA[8][32][VEC], fB[8][32][VEC];     // the forward maps of the block's warps
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, wt = warp % P.WT, wc = warp / P.WT;
-    const int rank = CL ? blockIdx.x % P.CT : 0;
-    const int64_t m = ((int64_t)(CL ? blockIdx.x / P.CT : blockIdx.x) * P.WC * 32 + wc * 32 + lane) * VEC;
-    const bool on = m < P.M;
-    const int64_t b = on ? m / P.N : 0, off = on ? b * P.sb + m % P.N : 0;
-    float carry[VEC];
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) carry[e] = on && P.glast ? P.glast[m + e] : 0.f;
+template <typename XT, bool WIDE, int S, int MQ, bool LOGIT, bool MIX, bool CL>
+__global__ void __launch_bounds__(256, 2) scan_backward_kernel(const ScanArgs P) {
+    using E = Elem<XT>;
+    using Pair = typename E::Pair;
+    constexpr int kStages = kBackwardStages<XT>;
+    __shared__ ScanShared<CL> sh;
+    __shared__ F2 ends[2][256];                              // B of the segments' forward maps
+    const Place<XT, WIDE, S, CL> me(P);
+    enter_cluster<CL>(sh, P, me.width);
+    F2 carry = me.state(P.glast);
     if (P.T == 0) {
-        if (on && wt == 0 && rank == 0 && P.gh0)
-            for (int e = 0; e < VEC; ++e) P.gh0[m + e] = carry[e];
+        if (me.q == 0 && me.rank == 0 && P.gh0) me.put_state(P.gh0, carry);
         leave_cluster<CL>();
         return;
     }
-    const int span = P.WT * S, step = span * (CL ? P.CT : 1);
-    const int passes = (P.T - 1) / step + 1;
-    typename R::Raw gr[S], xr[S], lr[S];
-    uint32_t st = 0;
-    float start[VEC];                                    // h before the block's first step
-    auto fetch = [&](int t0) {
-        st = 0;
-        if (!on || t0 < 0) return;
+    const int passes = (P.T - 1) / me.step + 1;
+    int t0 = (passes - 1) * me.step + me.rank * me.span + me.q * S;
+    const int64_t hop = (int64_t)me.step * P.st * (int64_t)sizeof(XT);
+    const int64_t first = (me.base + (int64_t)(me.rank * me.span) * P.st) * (int64_t)sizeof(XT) + (passes - 1) * hop;
+    const char *px = static_cast<const char *>(P.x) + first, *pg = static_cast<const char *>(P.gate) + first;
+    const char *pl = static_cast<const char *>(P.gh) + first;
+    char *pgx = static_cast<char *>(P.gx) + first, *pgg = static_cast<char *>(P.gg) + first;
+    extern __shared__ __align__(16) unsigned char dynamic[];
+    const int seg = segment_pairs<XT, S>(me.width), stage_pairs = 3 * P.Q * seg;
+    Pair *slots = reinterpret_cast<Pair *>(dynamic) + me.q * seg;
+    uint8_t asked = me.ask(P, t0);
+    // h before the block's first step of the pass whose segment begins at t
+    auto begin = [&](int t) {
+        const int tb = t - me.q * S;                         // a multiple of the interval, or 0
+        return me.state(tb > 0 && tb < P.T ? P.saved + (int64_t)(tb / kInterval - 1) * P.M : tb == 0 ? P.h0 : nullptr);
+    };
+    F2 start = begin(t0);
+    auto fetch = [&](int stage, int t) {
+        if (t >= 0) {
+            Pair *to = slots + stage * stage_pairs;
+            me.copy(to, pg, P.T - t);
+            me.copy(to + P.Q * seg, px, P.T - t);
+            me.copy(to + 2 * P.Q * seg, pl, P.T - t);
+        }
+        copies_issued();
+        pg -= hop;
+        px -= hop;
+        pl -= hop;
+    };
 #pragma unroll
-        for (int s = 0; s < S; ++s)
-            if (t0 + s < P.T) {
-                gr[s] = load_row<XT, VEC>(P.gate, off + (t0 + s) * P.st);
-                xr[s] = load_row<XT, VEC>(P.x, off + (t0 + s) * P.st);
-                lr[s] = load_row<XT, VEC>(P.gh, off + (t0 + s) * P.st);
+    for (int i = 0; i < kStages - 1; ++i) fetch(i, t0 - i * me.step);
+    int stage = 0;
+    for (int pass = 0; pass < passes; ++pass) {
+        F2 a[S], na[S], A = both(1.f), B = both(0.f), L = both(0.f), h = start;
+        const uint32_t cut = me.starts(P, t0, asked);
+        const int t1 = t0, left = P.T - t0;
+        const bool plain = __all_sync(0xffffffffu, left >= S && !cut);
+        copies_landed<kStages - 2>();
+        const Pair *gr = slots + stage * stage_pairs + me.cp, *xr = gr + P.Q * seg, *lr = xr + P.Q * seg;
+        auto gh_of = [&](int s) { return E::unpack(lr[s * me.width]); };
+        auto x_of = [&](int s) { return E::unpack(xr[s * me.width]); };
+#pragma unroll
+        for (int s = 0; s < S; ++s) decay_of<LOGIT>(gr[s * me.width], a[s], na[s]);
+        // what the state takes up in step s
+        auto input = [&](int s) {
+            const F2 u = x_of(s);
+            return MIX ? mul(u, na[s]) : u;
+        };
+        if (plain) {
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                A = mul(A, a[s]);
+                B = fma(a[s], B, input(s));
             }
-        if (P.starts) {
+#pragma unroll
+            for (int s = S - 1; s >= 0; --s) L = mul(a[s], add(gh_of(s), L));
+        } else {
 #pragma unroll
             for (int s = 0; s < S; ++s)
-                if (t0 + s < P.T && P.starts[(t0 + s) * P.ft + b * P.fb]) st |= 1u << s;
-        }
-        const int tb = t0 - wt * S;                      // a multiple of the interval, or 0
-        if (tb < P.T) {
-#pragma unroll
-            for (int e = 0; e < VEC; ++e)
-                start[e] = tb ? P.saved[(int64_t)(tb / kInterval - 1) * P.M + m + e] : P.h0 ? P.h0[m + e] : 0.f;
-        }
-    };
-    int t0 = (passes - 1) * step + rank * span + wt * S;
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) start[e] = 0.f;
-    fetch(t0);
-    for (int pass = 0; pass < passes; ++pass) {
-        float a[S][VEC], x[S][VEC], g[S][VEC], gh[S][VEC], A[VEC], B[VEC], L[VEC], h[VEC], mu[VEC];
-        const uint32_t cut = st;
-        const int t1 = t0;
-        auto live = [&](int s) { return on && t1 + s < P.T; };
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) { A[e] = 1.f; B[e] = 0.f; L[e] = 0.f; }
-#pragma unroll
-        for (int s = 0; s < S; ++s)
-            if (live(s)) {
-                R::unpack(gr[s], g[s]);
-                R::unpack(xr[s], x[s]);
-                R::unpack(lr[s], gh[s]);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    float na;
-                    decay_of<XT, LOGIT>(g[s][e], a[s][e], na);
-                    if (LOGIT) g[s][e] = na;             // the gate itself is not needed again
-                    const float u = MIX ? na * x[s][e] : x[s][e];
-                    A[e] *= a[s][e];
-                    B[e] = cut >> s & 1 ? u : fmaf(a[s][e], B[e], u);
+                if (s < left) {
+                    A = mul(A, a[s]);
+                    B = cut >> s & 1 ? input(s) : fma(a[s], B, input(s));
                 }
+#pragma unroll
+            for (int s = S - 1; s >= 0; --s)
+                if (s < left) L = cut >> s & 1 ? both(0.f) : mul(a[s], add(gh_of(s), L));
+        }
+        // the stage read in the pass before is free; its readers have passed copies_landed
+        fetch(stage == 0 ? kStages - 1 : stage - 1, t0 - (kStages - 1) * me.step);
+        if (++stage == kStages) stage = 0;
+        t0 -= me.step;
+        asked = me.ask(P, t0);
+        start = begin(t0);
+        const int buf = pass & 1, from_end = P.Q - 1 - me.q;
+        ends[buf][me.q * me.width + me.cp] = B;
+        F2 mu = fold<CL, LOGIT, MQ>(sh, P, from_end, me.cp, me.width, CL ? P.CT - 1 - me.rank : 0, pass, A, L, cut != 0, carry);
+#pragma unroll
+        for (int i = 0; i < MQ - 1; ++i)
+            if (i < me.q) {
+                const int at = (P.Q - 1 - i) * me.width + me.cp;
+                h = map_over(sh.map[buf][at].A, ends[buf][i * me.width + me.cp], sh.cut[buf][at], h);
+            }
+        F2 before[S];
+        // gradients of step s, from the state before it and mu after it
+        auto gradients = [&](int s, F2 ga) {
+            const F2 lam = add(gh_of(s), mu);
+            if (MIX) ga = fma(x_of(s), both(-1.f), ga);
+            ga = mul(ga, lam);
+            if (LOGIT) ga = mul(ga, mul(a[s], na[s]));
+            me.store(pgx, s, MIX ? mul(lam, na[s]) : lam);
+            me.store(pgg, s, ga);
+            mu = mul(a[s], lam);
+        };
+        if (plain && me.on) {
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                before[s] = h;
+                if (s + 1 < S) h = fma(a[s], h, input(s));
             }
 #pragma unroll
-        for (int s = S - 1; s >= 0; --s)
-            if (live(s)) {
+            for (int s = S - 1; s >= 0; --s) gradients(s, before[s]);
+        } else if (me.on) {
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) L[e] = cut >> s & 1 ? 0.f : a[s][e] * (gh[s][e] + L[e]);
-            }
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) h[e] = start[e];
-        t0 -= step;
-        fetch(t0);
-        if (pass) __syncthreads();
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            fA[warp][lane][e] = A[e];
-            fB[warp][lane][e] = B[e];
-        }
-        fold<VEC, CL, true>(sh, P, wt, wc, lane, rank, pass, A, L, cut != 0, carry, mu);
-        for (int i = 0; i < wt; ++i) {
-            const int w = wc * P.WT + i;
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) h[e] = map_over(fA[w][lane][e], fB[w][lane][e], sh.cut[w][lane], h[e]);
-        }
-        float before[S][VEC];
-#pragma unroll
-        for (int s = 0; s < S; ++s)
-            if (live(s)) {
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
+            for (int s = 0; s < S; ++s)
+                if (s < left) {
                     const bool c = cut >> s & 1;
-                    const float u = MIX ? (LOGIT ? g[s][e] : 1.f - a[s][e]) * x[s][e] : x[s][e];
-                    before[s][e] = c ? 0.f : h[e];
-                    h[e] = c ? u : fmaf(a[s][e], h[e], u);
+                    before[s] = c ? both(0.f) : h;
+                    h = c ? input(s) : fma(a[s], h, input(s));
                 }
-            }
 #pragma unroll
-        for (int s = S - 1; s >= 0; --s)
-            if (live(s)) {
-                float gx[VEC], gg[VEC];
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float na = LOGIT ? g[s][e] : 1.f - a[s][e];
-                    const float lam = gh[s][e] + mu[e];
-                    const float ga = lam * (MIX ? before[s][e] - x[s][e] : before[s][e]);
-                    gx[e] = MIX ? lam * na : lam;
-                    gg[e] = LOGIT ? ga * a[s][e] * na : ga;
-                    mu[e] = cut >> s & 1 ? 0.f : a[s][e] * lam;
+            for (int s = S - 1; s >= 0; --s)
+                if (s < left) {
+                    gradients(s, before[s]);
+                    if (cut >> s & 1) mu = both(0.f);
                 }
-                store_row<XT, VEC>(P.gx, off + (t1 + s) * P.st, gx);
-                store_row<XT, VEC>(P.gg, off + (t1 + s) * P.st, gg);
-            }
-        if (on && t1 == 0 && P.gh0)
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) P.gh0[m + e] = mu[e];
+        }
+        pgx -= hop;
+        pgg -= hop;
+        if (t1 == 0 && P.gh0) me.put_state(P.gh0, mu);
+        if (!CL && me.q == 0) sh.carry[buf][me.cp] = mu;
     }
     leave_cluster<CL>();
+}
+
+// Step by step, one thread for a channel: rows so far apart that a block's 32-bit offsets
+// cannot reach them (millions of channels, which fill the card without a split of time).
+template <typename XT, bool LOGIT, bool MIX>
+__global__ void __launch_bounds__(128) scan_forward_far_kernel(const ScanArgs P) {
+    using E = Elem<XT>;
+    using One = typename E::One;
+    const int64_t m = (int64_t)blockIdx.x * 128 + threadIdx.x;
+    if (m >= P.M) return;
+    const int64_t b = m / P.N, off = b * P.sb + m % P.N;
+    float v = P.h0 ? P.h0[m] : 0.f;
+    for (int t = 0; t < P.T; ++t) {
+        const int64_t at = off + t * P.st;
+        F2 a, na;
+        decay_of<LOGIT>(E::pair(__ldcs(static_cast<const One *>(P.gate) + at), One()), a, na);
+        float u = E::unpack(E::pair(__ldcs(static_cast<const One *>(P.x) + at), One())).x();
+        if (MIX) u *= na.x();
+        v = P.starts && P.starts[t * P.ft + b * P.fb] ? u : fmaf(a.x(), v, u);
+        __stcs(static_cast<One *>(P.h) + at, E::first(E::pack(F2(v, 0.f))));
+        if (P.saved && (t + 1) % kInterval == 0 && t + 1 < P.T) P.saved[(int64_t)(t / kInterval) * P.M + m] = v;
+    }
+    if (P.last) P.last[m] = v;
+}
+
+template <typename XT, bool LOGIT, bool MIX>
+__global__ void __launch_bounds__(128) scan_backward_far_kernel(const ScanArgs P) {
+    using E = Elem<XT>;
+    using One = typename E::One;
+    const int64_t m = (int64_t)blockIdx.x * 128 + threadIdx.x;
+    if (m >= P.M) return;
+    const int64_t b = m / P.N, off = b * P.sb + m % P.N;
+    auto value = [](const void *p, int64_t at) { return E::unpack(E::pair(static_cast<const One *>(p)[at], One())).x(); };
+    float before[kInterval];                                 // h[t-1] of the interval's steps
+    float mu = P.glast ? P.glast[m] : 0.f;
+    for (int c = (P.T + kInterval - 1) / kInterval - 1; c >= 0; --c) {
+        const int t0 = c * kInterval, t1 = min(P.T, t0 + kInterval);
+        float v = c ? P.saved[(int64_t)(c - 1) * P.M + m] : P.h0 ? P.h0[m] : 0.f;
+        for (int t = t0; t < t1; ++t) {
+            const int64_t at = off + t * P.st;
+            F2 a, na;
+            decay_of<LOGIT>(E::pair(static_cast<const One *>(P.gate)[at], One()), a, na);
+            const float x = value(P.x, at), u = MIX ? na.x() * x : x;
+            before[t - t0] = v;
+            v = P.starts && P.starts[t * P.ft + b * P.fb] ? u : fmaf(a.x(), v, u);
+        }
+        for (int t = t1 - 1; t >= t0; --t) {
+            const int64_t at = off + t * P.st;
+            F2 a, na;
+            decay_of<LOGIT>(E::pair(static_cast<const One *>(P.gate)[at], One()), a, na);
+            const float x = value(P.x, at);
+            const bool start = P.starts && P.starts[t * P.ft + b * P.fb];
+            const float lam = value(P.gh, at) + mu, hp = start ? 0.f : before[t - t0];
+            const float ga = lam * (MIX ? hp - x : hp);
+            __stcs(static_cast<One *>(P.gx) + at, E::first(E::pack(F2(MIX ? lam * na.x() : lam, 0.f))));
+            __stcs(static_cast<One *>(P.gg) + at, E::first(E::pack(F2(LOGIT ? ga * (a.x() * na.x()) : ga, 0.f))));
+            mu = start ? 0.f : a.x() * lam;
+        }
+    }
+    if (P.gh0) P.gh0[m] = mu;
 }
 
 dendsn_status check(const dendsn_scan_config *cfg, size_t *saved) {
@@ -457,63 +744,70 @@ ScanArgs make_args(const dendsn_scan_config &c) {
 
 // Blocks that keep the card busy: two for each of its 152 SMs.
 constexpr int kBusy = 304;
+// Blocks of a call that takes clusters: all of them resident, also where a cluster of 8 does not
+// fill its GPC.
+constexpr int kMostClustered = 256;
 
-// How a call is split. Time: as many of a block's eight warps as the steps fill, then blocks of
-// a cluster while the channels alone give fewer than kBusy blocks.
-struct Split {
-    int WT, WC, CT;
-    unsigned blocks;
-};
-Split split_of(const ScanArgs &a, int vec, int S) {
-    Split p;
-    p.WT = a.T > 4 * S ? 8 : a.T > 2 * S ? 4 : a.T > S ? 2 : 1;
-    p.WC = 8 / p.WT;
-    const int64_t width = (int64_t)p.WC * 32 * vec, groups = (a.M + width - 1) / width;
-    p.CT = 1;
-    while (p.CT < 8 && groups * p.CT < kBusy && a.T > p.WT * S * p.CT) p.CT *= 2;
-    p.blocks = (unsigned)(groups * p.CT);
-    return p;
-}
-
-template <typename XT, int VEC, int S, bool LOGIT, bool MIX, bool FWD>
+template <typename XT, bool WIDE, bool LOGIT, bool MIX, bool FWD>
 cudaError_t launch(ScanArgs a, cudaStream_t s) {
-    const Split p = split_of(a, VEC, S);
-    a.WT = p.WT;
-    a.WC = p.WC;
-    a.CT = p.CT;
+    // Steps of a segment: 8, and 4 in the float32 backward, whose segments of 8 would leave one
+    // block an SM (a layer of T = 512, 16 x 4096: 172 us against 191).
+    constexpr int S = sizeof(XT) == 4 && !FWD ? 4 : 8;
+    constexpr int kFullQ = kInterval / S;      // segments that make an interval
+    constexpr int W = 16;                      // most segments of a block
+    a.PN = (a.N + 1) / 2;
+    a.pairs = a.M / a.N * a.PN;
+    // Time: as many segments as the steps fill, up to an interval; twice that, and then the
+    // blocks of a cluster, while the channels alone leave SMs without one.
+    a.Q = 1;
+    while (a.Q < kFullQ && a.Q * S < a.T) a.Q *= 2;
+    auto groups = [&] { return (a.pairs + 256 / a.Q - 1) / (256 / a.Q); };
+    if (W > kFullQ && a.Q == kFullQ && a.T > a.Q * S && groups() < kBusy) a.Q *= 2;
+    a.CT = 1;
+    while (a.CT < 8 && groups() * a.CT * 2 <= kMostClustered && a.T > a.Q * S * a.CT) a.CT *= 2;
+    // the farthest offset in a block: its samples apart, its steps apart
+    const int64_t reach = ((256 / a.Q - 1) / a.PN + 1) * a.sb + a.N + (int64_t)a.Q * S * a.st;
+    if (reach * (int64_t)sizeof(XT) > UINT32_MAX) {
+        const unsigned blocks = (unsigned)((a.M + 127) / 128);
+        if constexpr (FWD) scan_forward_far_kernel<XT, LOGIT, MIX><<<blocks, 128, 0, s>>>(a);
+        else scan_backward_far_kernel<XT, LOGIT, MIX><<<blocks, 128, 0, s>>>(a);
+        return cudaGetLastError();
+    }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(p.blocks);
+    cfg.gridDim = dim3((unsigned)(groups() * a.CT));
     cfg.blockDim = dim3(256);
     cfg.stream = s;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = (unsigned)p.CT;
+    at[0].val.clusterDim.x = (unsigned)a.CT;
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
-    cfg.numAttrs = p.CT > 1 ? 1 : 0;
+    cfg.numAttrs = a.CT > 1 ? 1 : 0;
+    const size_t smem = (size_t)(FWD ? 2 * kForwardStages<XT> : 3 * kBackwardStages<XT>) * a.Q *
+                        segment_pairs<XT, S>(256 / a.Q) * sizeof(typename Elem<XT>::Pair);
+    auto start = [&](auto kernel) {
+        cudaError_t e = smem <= 16384 ? cudaSuccess : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+        cfg.dynamicSmemBytes = smem;
+        return cudaLaunchKernelEx(&cfg, kernel, a);
+    };
     if constexpr (FWD)
-        return p.CT > 1 ? cudaLaunchKernelEx(&cfg, scan_forward_kernel<XT, VEC, S, LOGIT, MIX, true>, a)
-                        : cudaLaunchKernelEx(&cfg, scan_forward_kernel<XT, VEC, S, LOGIT, MIX, false>, a);
+        return a.CT > 1       ? start(scan_forward_kernel<XT, WIDE, S, W, LOGIT, MIX, true>)
+               : a.Q > kFullQ ? start(scan_forward_kernel<XT, WIDE, S, W, LOGIT, MIX, false>)
+                              : start(scan_forward_kernel<XT, WIDE, S, kFullQ, LOGIT, MIX, false>);
     else
-        return p.CT > 1 ? cudaLaunchKernelEx(&cfg, scan_backward_kernel<XT, VEC, S, LOGIT, MIX, true>, a)
-                        : cudaLaunchKernelEx(&cfg, scan_backward_kernel<XT, VEC, S, LOGIT, MIX, false>, a);
+        return a.CT > 1       ? start(scan_backward_kernel<XT, WIDE, S, W, LOGIT, MIX, true>)
+               : a.Q > kFullQ ? start(scan_backward_kernel<XT, WIDE, S, W, LOGIT, MIX, false>)
+                              : start(scan_backward_kernel<XT, WIDE, S, kFullQ, LOGIT, MIX, false>);
 }
 
-template <typename XT, int VEC, bool LOGIT, bool MIX>
-cudaError_t launch_vec(bool forward, const ScanArgs &a, cudaStream_t s) {
-    return forward ? launch<XT, VEC, 8, LOGIT, MIX, true>(a, s) : launch<XT, VEC, 8, LOGIT, MIX, false>(a, s);
-}
-
-// Widest vector whose pieces lie within one sample's row and are aligned in every tensor.
+// Rows are copied 16 bytes at a time where they are aligned to 16 bytes in every tensor.
 template <typename XT, bool LOGIT, bool MIX>
 cudaError_t launch_form(bool forward, const ScanArgs &a, cudaStream_t s) {
-    auto fits = [&](int vec) {
-        const size_t bytes = vec * sizeof(XT);
-        return a.N % vec == 0 && seq_aligned(a.x, bytes) && seq_aligned(a.gate, bytes) && seq_aligned(a.h, bytes) &&
-               seq_aligned(a.gh, bytes) && seq_aligned(a.gx, bytes) && seq_aligned(a.gg, bytes);
-    };
-    const int vec = fits(2) ? 2 : 1;
-    return vec == 2 ? launch_vec<XT, 2, LOGIT, MIX>(forward, a, s) : launch_vec<XT, 1, LOGIT, MIX>(forward, a, s);
+    const bool wide = a.N * sizeof(XT) % 16 == 0 && seq_aligned(a.x, 16) && seq_aligned(a.gate, 16) &&
+                      seq_aligned(a.h, 16) && seq_aligned(a.gh, 16) && seq_aligned(a.gx, 16) && seq_aligned(a.gg, 16);
+    if (forward) return wide ? launch<XT, true, LOGIT, MIX, true>(a, s) : launch<XT, false, LOGIT, MIX, true>(a, s);
+    return wide ? launch<XT, true, LOGIT, MIX, false>(a, s) : launch<XT, false, LOGIT, MIX, false>(a, s);
 }
 
 template <typename XT>
