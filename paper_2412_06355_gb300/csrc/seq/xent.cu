@@ -33,6 +33,10 @@ enum { STATS = 0, PIECE = 1, HIDDEN = 2, WEIGHT = 3 };
 
 constexpr int kTileM = 256, kTileN = 256, kTileK = 64;    // of a pair of blocks
 constexpr int kStages = 6;
+// float32 operands: blocks of the sum after which the tile's sums in TMEM are added to float32
+// registers and begin anew. The tensor core's running sums lose more than a float32 addition
+// does (in one run over 10,007 terms the relative error of grad_hidden was 1.5e-6).
+constexpr int kChunk = 4;
 constexpr int kHalfBytes = 128 * kTileK * 2;              // one block's 128 x 64 operand tile
 constexpr int kStageBytes = 2 * kHalfBytes;
 constexpr int kThreads = 320;                             // copies, products, 8 warps of epilogue
@@ -51,9 +55,6 @@ __device__ __forceinline__ int label_of(const void *labels, int64_t r, int V, in
     const int64_t y = static_cast<const I *>(labels)[r];
     return y == ignore ? kIgnored : (y < 0 || y >= V) ? kBadLabel : (int)y;
 }
-template <typename T> __device__ __forceinline__ float to_f(T v);
-template <> __device__ __forceinline__ float to_f<float>(float v) { return v; }
-template <> __device__ __forceinline__ float to_f<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
 template <typename T> __device__ __forceinline__ T from_f(float v);
 template <> __device__ __forceinline__ float from_f<float>(float v) { return v; }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
@@ -96,32 +97,45 @@ template <typename I>
 __global__ void __launch_bounds__(1024) xent_rows_kernel(Rows R, const void *labels, int32_t M, int32_t V,
                                                          int64_t ignore, float *loss, float *lse_out,
                                                          const float *lse, const float *gloss) {
+    constexpr int kEach = 8;                                  // consecutive rows of a thread
     __shared__ int warps[32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int done = 0;
-    for (int64_t r0 = 0; r0 < M; r0 += 1024) {
-        const int64_t r = r0 + threadIdx.x;
-        const int y = r < M ? label_of<I>(labels, r, V, ignore) : kIgnored;
-        const unsigned m = __ballot_sync(0xffffffffu, y >= 0);
-        if (lane == 0) warps[warp] = __popc(m);
+    for (int64_t r0 = 0; r0 < M; r0 += 1024 * kEach) {
+        const int64_t r = r0 + threadIdx.x * kEach;
+        int y[kEach], mine = 0;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) y[j] = r + j < M ? label_of<I>(labels, r + j, V, ignore) : kIgnored;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) mine += y[j] >= 0;
+        int incl = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += v;
+        }
+        if (lane == 31) warps[warp] = incl;
         __syncthreads();
-        int at = done + __popc(m & ((1u << lane) - 1));
+        int at = done + incl - mine;
         for (int w = 0; w < 32; ++w) {
             if (w < warp) at += warps[w];
             done += warps[w];
         }
         __syncthreads();
-        if (r < M) {
-            R.where[r] = y >= 0 ? at : y;
-            if (y >= 0) {
-                R.index[at] = (int32_t)r;
-                R.label[at] = y;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            if (r + j >= M) break;
+            R.where[r + j] = y[j] >= 0 ? at : y[j];
+            if (y[j] >= 0) {
+                R.index[at] = (int32_t)(r + j);
+                R.label[at] = y[j];
                 if (lse) {
-                    R.lse[at] = lse[r];
-                    R.weight[at] = gloss[r];
+                    R.lse[at] = lse[r + j];
+                    R.weight[at] = gloss[r + j];
                 }
+                ++at;
             } else if (loss) {
-                loss[r] = lse_out[r] = y == kIgnored ? 0.f : nan_f();
+                loss[r + j] = lse_out[r + j] = y[j] == kIgnored ? 0.f : nan_f();
             }
         }
     }
@@ -137,9 +151,10 @@ __global__ void __launch_bounds__(1024) xent_rows_kernel(Rows R, const void *lab
     }
 }
 
-// Copies rows of D elements to rows of Dp bfloat16 elements with zeros behind, in `terms` planes.
-// index: the row to copy for each place (negative: zeros), or null: the same row.
-template <typename T>
+// Copies rows of D elements to rows of Dp bfloat16 elements with zeros behind, in three planes
+// for float32; a thread takes 8 elements. index: the row to copy for each place (negative:
+// zeros), or null: the same row. WIDE: rows can be read 16 bytes at a time.
+template <typename T, bool WIDE>
 __global__ void __launch_bounds__(256) xent_pack_kernel(const T *from, __nv_bfloat16 *to, const int32_t *index,
                                                         const Ctl *ctl, int64_t rows, int32_t D, int32_t Dp,
                                                         int64_t plane) {
@@ -151,18 +166,51 @@ __global__ void __launch_bounds__(256) xent_pack_kernel(const T *from, __nv_bflo
         src = index[r];
     }
     const T *p = from + src * D;
-    for (int32_t d = (threadIdx.x & 31) * 2; d < Dp; d += 64) {
-        const float a = src >= 0 && d < D ? to_f<T>(p[d]) : 0.f;
-        const float b = src >= 0 && d + 1 < D ? to_f<T>(p[d + 1]) : 0.f;
-        uint32_t *q = reinterpret_cast<uint32_t *>(to + r * Dp + d);
+    for (int32_t d = (threadIdx.x & 31) * 8; d < Dp; d += 256) {
+        uint4 *q = reinterpret_cast<uint4 *>(to + r * Dp + d);
         if constexpr (sizeof(T) == 2) {
-            *q = two(__float2bfloat16_rn(a), __float2bfloat16_rn(b));
-        } else {
-            __nv_bfloat16 u[3], v[3];
-            split(a, u);
-            split(b, v);
+            uint4 w = make_uint4(0, 0, 0, 0);
+            if (src >= 0) {
+                if (WIDE) {
+                    if (d < D) w = __ldg(reinterpret_cast<const uint4 *>(p + d));
+                } else {
+                    __nv_bfloat16 e[8];
 #pragma unroll
-            for (int t = 0; t < 3; ++t) q[t * (plane / 2)] = two(u[t], v[t]);
+                    for (int j = 0; j < 8; ++j) e[j] = d + j < D ? p[d + j] : __float2bfloat16_rn(0.f);
+                    w = make_uint4(two(e[0], e[1]), two(e[2], e[3]), two(e[4], e[5]), two(e[6], e[7]));
+                }
+            }
+            *q = w;
+        } else {
+            float e[8] = {};
+            if (src >= 0) {
+#pragma unroll
+                for (int h = 0; h < 8; h += 4) {
+                    if (WIDE) {
+                        if (d + h < D) {
+                            const float4 f = __ldg(reinterpret_cast<const float4 *>(p + d + h));
+                            e[h] = f.x;
+                            e[h + 1] = f.y;
+                            e[h + 2] = f.z;
+                            e[h + 3] = f.w;
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = h; j < h + 4; ++j) e[j] = d + j < D ? p[d + j] : 0.f;
+                    }
+                }
+            }
+            uint32_t w[3][4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                __nv_bfloat16 u[3], v[3];
+                split(e[2 * j], u);
+                split(e[2 * j + 1], v);
+#pragma unroll
+                for (int t = 0; t < 3; ++t) w[t][j] = two(u[t], v[t]);
+            }
+#pragma unroll
+            for (int t = 0; t < 3; ++t) q[t * (plane / 8)] = make_uint4(w[t][0], w[t][1], w[t][2], w[t][3]);
         }
     }
 }
@@ -253,9 +301,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             tile_of<MODE>(g, mt, item, m, n, s);
             const int am = m * kTileM + (int)rank * 128, bn = n * kTileN + (int)rank * 128;
             const int k0 = s * g.kb_split, k1 = MODE == WEIGHT ? kb : min(kb, k0 + g.kb_split);
+            const int chunk = kF32 ? kChunk : max(1, k1 - k0);
+            for (int c0 = k0; ok && c0 < k1; c0 += chunk)
             for (int ph = 0; ok && ph < kPhases; ++ph) {
                 const int ta = kF32 ? term_a(ph) : 0, tb = kF32 ? term_b(ph) : 0;
-                for (int k = k0; k < k1; ++k) {
+                for (int k = c0; k < min(k1, c0 + chunk); ++k) {
                     if (!(ok = tc::bar_wait(empty + 8 * stage, phase))) break;
                     if (rank == 0) tc::bar_expect(full + 8 * stage, 2 * kStageBytes);
                     const uint32_t a = stage0 + stage * kStageBytes, b = a + kHalfBytes, bar = full0 + 8 * stage;
@@ -284,8 +334,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             int m, n, s;
             tile_of<MODE>(g, mt, item, m, n, s);
             const int k0 = s * g.kb_split, k1 = MODE == WEIGHT ? kb : min(kb, k0 + g.kb_split);
-            const int steps = (k1 - k0) * kPhases;
-            if (steps <= 0) continue;
+            const int chunk = kF32 ? kChunk : max(1, k1 - k0);
+            for (int c0 = k0; ok && c0 < k1; c0 += chunk) {
+            const int steps = min(chunk, k1 - c0) * kPhases;
             if (!(ok = tc::bar_wait(acc_empty + 8 * acc, acc_phase))) break;
             tc::fence_after_sync();
             for (int i = 0; i < steps; ++i) {
@@ -302,6 +353,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             if (!ok) break;
             tc::commit_both(acc_full + 8 * acc);
             if (++acc == 2) { acc = 0; acc_phase ^= 1; }
+            }
         }
     } else if (warp >= 2) {                                   // epilogue, in both blocks
         const int quad = warp % 4, half = (warp - 2) / 4;
@@ -315,11 +367,40 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             const bool any = k1 > k0;
             const int row = m * kTileM + (int)rank * 128 + quad * 32 + lane;
             const int col0 = n * kTileN + half * 128;
-            if (any) {
-                ok = tc::bar_wait(acc_full + 8 * acc, acc_phase);
-                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+            // the tile's sums are in TMEM; takes them over once they are complete
+            auto take = [&] {
+                ok = __all_sync(0xffffffffu, tc::bar_wait(acc_full + 8 * acc, acc_phase));
                 tc::fence_after_sync();
+            };
+            auto give_back = [&] {
+                tc::fence_before_sync();
+                __syncwarp();
+                if (lane == 0) tc::bar_arrive_cluster(empty0 + 8 * acc);
+                if (++acc == 2) { acc = 0; acc_phase ^= 1; }
+            };
+            auto columns = [&](int c) { return tmem + ((uint32_t)quad << 21) + acc * kTileN + half * 128 + 32 * c; };
+            float sums[kF32 ? 4 : 1][32];
+            if constexpr (kF32) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) sums[c][i] = 0.f;
+                for (int c0 = k0; c0 < k1; c0 += kChunk) {
+                    take();
+                    if (!ok) break;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        float v[32];
+                        tc::tmem_load(v, columns(c));
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) sums[c][i] += v[i];
+                    }
+                    give_back();
+                }
+            } else if (any) {
+                take();
             }
+            if (!ok) break;
             float top = -INFINITY, total = 0.f;
             int y = -1;
             float lse = 0.f, weight = 0.f;
@@ -328,14 +409,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                 lse = g.lse[row];
                 weight = g.weight[row];
             }
-#pragma unroll 1
-            for (int c = 0; c < 4; ++c) {
-                float v[32];
+            auto epilogue = [&](int c, float (&v)[32]) {
                 const int col = col0 + 32 * c;                // within the piece, or within D
-                if (any) tc::tmem_load(v, tmem + ((uint32_t)quad << 21) + acc * kTileN + half * 128 + 32 * c);
-                else
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = 0.f;
                 if (MODE == STATS) {
                     const int left = g.V - col;
                     if (left < 32)
@@ -425,12 +500,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                         }
                     }
                 }
-            }
-            if (any) {
-                tc::fence_before_sync();
-                __syncwarp();
-                if (lane == 0) tc::bar_arrive_cluster(empty0 + 8 * acc);
-                if (++acc == 2) { acc = 0; acc_phase ^= 1; }
+            };
+            if constexpr (kF32) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) epilogue(c, sums[c]);
+            } else {
+#pragma unroll 1
+                for (int c = 0; c < 4; ++c) {
+                    if (any) tc::tmem_load(sums[0], columns(c));
+                    else
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) sums[0][i] = 0.f;
+                    epilogue(c, sums[0]);
+                }
+                if (any) give_back();
             }
             if (MODE == STATS)
                 g.part[(int64_t)(2 * n + half) * g.Mp + row] = make_float2(top == -INFINITY ? 0.f : top * kLog2e, total);
@@ -445,10 +528,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     if (warp == 1) tc::tmem_free(tmem, 512);
 }
 
-// Joins the maxima and sums of a row: 32 rows of a block, its 8 warps take every eighth part.
-__global__ void __launch_bounds__(256) xent_join_kernel(Rows R, const float2 *part, int32_t parts, int64_t Mp,
-                                                        float *loss, float *lse) {
-    __shared__ float2 sh[8][32];
+// Joins the maxima and sums of a row: 32 rows of a block, its 32 warps take every 32nd part,
+// eight of them in flight.
+__global__ void __launch_bounds__(1024) xent_join_kernel(Rows R, const float2 *part, int32_t parts, int64_t Mp,
+                                                         float *loss, float *lse) {
+    __shared__ float2 sh[32][33];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int r = blockIdx.x * 32 + lane;
     const int rows = R.ctl->rows;
@@ -461,31 +545,72 @@ __global__ void __launch_bounds__(256) xent_join_kernel(Rows R, const float2 *pa
         x.x = m;
     };
     if (r < rows)
-        for (int p = warp; p < parts; p += 8) add(a, part[(int64_t)p * Mp + r]);
+        for (int p = warp; p < parts; p += 256) {
+            float2 q[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                q[u] = p + 32 * u < parts ? __ldg(part + (int64_t)(p + 32 * u) * Mp + r) : make_float2(0.f, 0.f);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) add(a, q[u]);
+        }
     sh[warp][lane] = a;
     __syncthreads();
-    if (warp == 0 && r < rows) {
-        for (int w = 1; w < 8; ++w) add(a, sh[w][lane]);
-        const float v = R.ctl->failed ? nan_f() : kLn2 * (a.x + log2f(a.y));
-        lse[R.index[r]] = v;
-        loss[R.index[r]] = v - R.picked[r];
+    // warp w joins the 32 parts of row w, in an order that is always the same
+    float2 b = sh[lane][warp];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        const float2 other = make_float2(__shfl_down_sync(0xffffffffu, b.x, o), __shfl_down_sync(0xffffffffu, b.y, o));
+        add(b, other);
+    }
+    const int row = blockIdx.x * 32 + warp;
+    if (lane == 0 && row < rows) {
+        const float v = R.ctl->failed ? nan_f() : kLn2 * (b.x + log2f(b.y));
+        lse[R.index[row]] = v;
+        loss[R.index[row]] = v - R.picked[row];
     }
 }
 
-// grad_hidden of every row of the call from the sums of its place.
+// grad_hidden of every row of the call from the sums of its place; a thread takes 4 columns.
 template <typename T>
 __global__ void __launch_bounds__(256) xent_hidden_kernel(Rows R, const float *sum, T *gh, int64_t M, int64_t Mp,
                                                           int32_t D, int32_t Dq, int32_t splits) {
-    const int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int32_t quads = (D + 3) / 4;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, r = i / quads;
     if (r >= M) return;
+    const int32_t d = (int32_t)(i % quads) * 4;
     const int at = R.where[r];
-    const bool failed = R.ctl->failed;
-    for (int32_t d = threadIdx.x & 31; d < D; d += 32) {
-        float v = 0.f;
-        if (at >= 0)
-            for (int s = 0; s < splits; ++s) v += sum[((int64_t)s * Mp + at) * Dq + d];
-        if (at == kBadLabel || failed) v = nan_f();
-        gh[r * D + d] = from_f<T>(v);
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (at >= 0) {
+        const float *p = sum + (int64_t)at * Dq + d;
+        for (int s = 0; s < splits; s += 4) {
+            float4 q[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                q[u] = s + u < splits ? __ldg(reinterpret_cast<const float4 *>(p + (int64_t)(s + u) * Mp * Dq))
+                                      : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                v.x += q[u].x;
+                v.y += q[u].y;
+                v.z += q[u].z;
+                v.w += q[u].w;
+            }
+        }
+    }
+    if (at == kBadLabel || R.ctl->failed) v = make_float4(nan_f(), nan_f(), nan_f(), nan_f());
+    T *to = gh + r * D + d;
+    if (D % 4 == 0 && reinterpret_cast<uintptr_t>(gh) % (4 * sizeof(T)) == 0) {
+        if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<float4 *>(to) = v;
+        } else {
+            *reinterpret_cast<uint2 *>(to) = make_uint2(two(__float2bfloat16_rn(v.x), __float2bfloat16_rn(v.y)),
+                                                        two(__float2bfloat16_rn(v.z), __float2bfloat16_rn(v.w)));
+        }
+    } else {
+        const float e[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (d + j < D) to[j] = from_f<T>(e[j]);
     }
 }
 
@@ -508,6 +633,37 @@ struct Plan {
 
 int32_t up(int64_t v, int64_t to) { return (int32_t)((v + to - 1) / to * to); }
 
+// How the backward is cut: into pieces of the vocabulary (G of one within kPieceBytes) and the
+// sum over a piece of HIDDEN into splits. The time of a product is that of its fullest pair of
+// blocks, so both are chosen by what the card's kClusters pairs take in all, in units of one
+// block of kTileK of a tile (0.27 us): xent_large's 256 tiles of HIDDEN are 4 rounds of 76
+// unsplit, and 7 half rounds in two splits.
+void choose_pieces(Plan *pl) {
+    Plan &p = *pl;
+    const int64_t row = std::max<int64_t>(p.Mp, 1) * p.terms * 2, most = std::max<int64_t>(1, (int64_t)kPieceBytes / (row * kTileN));
+    const int32_t fewest = (int32_t)((p.nt + most - 1) / most), kd = p.Dp / kTileK, km = (int32_t)(p.Mp / kTileK);
+    const int64_t mt = std::max(p.mt, 1);
+    auto rounds = [](int64_t tiles) { return (tiles + kClusters - 1) / kClusters; };
+    double best = 1e300;
+    for (int32_t n = fewest; n < fewest + 6 && n <= p.nt; ++n) {
+        const int32_t vt = (p.nt + n - 1) / n, kv = vt * (kTileN / kTileK), pieces = (p.nt + vt - 1) / vt;
+        for (int32_t s = 1; s <= 32; ++s) {
+            const int32_t split = (kv + s - 1) / s;
+            if (s > 1 && split < 8) break;
+            const double join = (double)s * p.Mp * p.Dq * 8 / 1.6e6;   // bytes of the sums, read and written
+            const double cost = pieces * (rounds(mt * vt) * kd + rounds(mt * p.dt * s) * split + rounds((int64_t)vt * p.dt) * km +
+                                          join + 45.0);                // and three launches
+            if (cost < best) {
+                best = cost;
+                p.pieces = pieces;
+                p.pitch = vt * kTileN;
+                p.kb_split = split;
+                p.splits = (kv + split - 1) / split;
+            }
+        }
+    }
+}
+
 dendsn_status make_plan(const dendsn_xent_config *cfg, Plan *pl) {
     if (!cfg) return seq_fail(DENDSN_ERR_INVALID_ARG, "cfg is NULL");
     if (cfg->M < 0 || cfg->V < 1 || cfg->D < 1)
@@ -526,17 +682,7 @@ dendsn_status make_plan(const dendsn_xent_config *cfg, Plan *pl) {
     p.mt = (int32_t)(p.Mp / kTileM);
     p.nt = up(cfg->V, kTileN) / kTileN;
     p.dt = p.Dq / kTileN;
-    // pieces of equal size, each a multiple of the tile and with G within kPieceBytes
-    const int64_t row = std::max<int64_t>(p.Mp, 1) * p.terms * 2;
-    const int64_t most = std::max<int64_t>(1, (int64_t)kPieceBytes / (row * kTileN));
-    p.pieces = (int32_t)((p.nt + most - 1) / most);
-    p.pitch = (p.nt + p.pieces - 1) / p.pieces * kTileN;
-    // few tiles of grad_hidden: the sum over the piece is split over the card
-    const int32_t kb = p.pitch / kTileK;
-    const int64_t tiles = (int64_t)std::max(p.mt, 1) * p.dt;
-    p.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(kClusters / tiles, kb / 8));
-    p.kb_split = (kb + p.splits - 1) / p.splits;
-    p.splits = (kb + p.kb_split - 1) / p.kb_split;
+    choose_pieces(&p);
     size_t at = sizeof(Ctl);
     auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -630,19 +776,24 @@ cudaError_t operands(Call &c, const void *hidden, const void *weight, const __nv
                      int64_t *w_inner) {
     const Plan &p = c.pl;
     const int D = c.cfg->D;
-    xent_pack_kernel<T><<<(unsigned)((p.Mp + 7) / 8), 256, 0, c.s>>>(
-        static_cast<const T *>(hidden), c.at<__nv_bfloat16>(p.H), c.at<int32_t>(p.index), c.at<Ctl>(0), p.Mp, D, p.Dp,
-        p.Mp * p.Dp);
-    c.launches += 1;
+    auto pack = [&](const void *from, size_t to, const int32_t *index, int64_t rows) {
+        const T *f = static_cast<const T *>(from);
+        const unsigned blocks = (unsigned)((rows + 7) / 8);
+        if (D * sizeof(T) % 16 == 0 && seq_aligned(from, 16))
+            xent_pack_kernel<T, true><<<blocks, 256, 0, c.s>>>(f, c.at<__nv_bfloat16>(to), index, c.at<Ctl>(0), rows, D, p.Dp,
+                                                               rows * p.Dp);
+        else
+            xent_pack_kernel<T, false><<<blocks, 256, 0, c.s>>>(f, c.at<__nv_bfloat16>(to), index, c.at<Ctl>(0), rows, D, p.Dp,
+                                                                rows * p.Dp);
+        c.launches += 1;
+    };
+    pack(hidden, p.H, c.at<int32_t>(p.index), p.Mp);
     if (sizeof(T) == 2 && D % 8 == 0 && seq_aligned(weight, 16)) {
         *w = static_cast<const __nv_bfloat16 *>(weight);
         *w_pitch = D;
         *w_inner = D;
     } else {
-        xent_pack_kernel<T><<<(unsigned)(((int64_t)c.cfg->V + 7) / 8), 256, 0, c.s>>>(
-            static_cast<const T *>(weight), c.at<__nv_bfloat16>(p.W), nullptr, nullptr, c.cfg->V, D, p.Dp,
-            (int64_t)c.cfg->V * p.Dp);
-        c.launches += 1;
+        pack(weight, p.W, nullptr, c.cfg->V);
         *w = c.at<__nv_bfloat16>(p.W);
         *w_pitch = p.Dp;
         *w_inner = p.Dp;
@@ -688,7 +839,7 @@ dendsn_status run_forward(Call &c, const void *hidden, const void *weight, const
         c.launches += 1;
     }
     if (e == cudaSuccess) {
-        xent_join_kernel<<<(unsigned)((p.Mp + 31) / 32), 256, 0, c.s>>>(rows_of(c), c.at<float2>(p.part), 2 * p.nt, p.Mp,
+        xent_join_kernel<<<(unsigned)((p.Mp + 31) / 32), 1024, 0, c.s>>>(rows_of(c), c.at<float2>(p.part), 2 * p.nt, p.Mp,
                                                                         loss, lse);
         c.launches += 1;
         e = cudaGetLastError();
@@ -758,7 +909,7 @@ dendsn_status run_backward(Call &c, const void *hidden, const void *weight, cons
         c.launches += 3;
     }
     if (e == cudaSuccess) {
-        xent_hidden_kernel<T><<<(unsigned)(((int64_t)c.cfg->M + 7) / 8), 256, 0, c.s>>>(
+        xent_hidden_kernel<T><<<(unsigned)(((int64_t)c.cfg->M * ((D + 3) / 4) + 255) / 256), 256, 0, c.s>>>(
             rows_of(c), c.at<float>(p.sum), static_cast<T *>(gh), c.cfg->M, p.Mp, D, p.Dq, p.splits);
         c.launches += 1;
         e = cudaGetLastError();
