@@ -153,6 +153,8 @@ def library_path() -> str:
 def load() -> ctypes.CDLL:
     """Load libdendsn.so, building it first when it is missing or stale."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is None:
             path = _build.build()
@@ -203,13 +205,13 @@ def _ptr(t: Optional[torch.Tensor]):
         raise ValueError("DendSN tensors must live on a CUDA device")
     if not t.is_contiguous():
         raise ValueError("DendSN tensors must be contiguous")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
-def _stream(stream) -> ctypes.c_void_p:
+def _stream(stream) -> int:
     if stream is None:
         stream = torch.cuda.current_stream()
-    return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
 def launch_count() -> int:
@@ -379,7 +381,7 @@ def _expect(name, t, shape, dtype, optional=False):
         if optional:
             return
         raise ValueError(f"{name} is required")
-    if tuple(t.shape) != shape or t.dtype != dtype:
+    if t.shape != shape or t.dtype is not dtype:
         raise ValueError(f"{name} must be {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
 
 
@@ -451,21 +453,22 @@ def dendsn_scan_workspace_size(cfg: dendsn_scan_config) -> int:
     return int(s.value)
 
 
-def _scan_expect(cfg, seq, starts, states, saved, needs_saved):
-    batch = cfg.layout == BATCH_FIRST
-    lead = (cfg.B, cfg.T) if batch else (cfg.T, cfg.B)
-    dt = _xdtype(cfg)
-    for name, t in seq.items():
-        _expect(name, t, lead + (cfg.N,), dt)
-    _expect("starts", starts, lead, torch.uint8, optional=True)
-    for name, t in states.items():
-        _expect(name, t, (cfg.B, cfg.N), torch.float32, optional=True)
-    if saved is not None or needs_saved:
-        _bytes("saved", saved, dendsn_scan_workspace_size(cfg))
+def _scan_shapes(cfg):
+    """(shape of a sequence tensor, of starts, of a state, dtype)."""
+    lead = (cfg.B, cfg.T) if cfg.layout == BATCH_FIRST else (cfg.T, cfg.B)
+    return lead + (cfg.N,), lead, (cfg.B, cfg.N), _xdtype(cfg)
 
 
 def dendsn_scan_forward(cfg, x, gate, starts, h0, h, h_last=None, saved=None, stream=None):
-    _scan_expect(cfg, dict(x=x, gate=gate, h=h), starts, dict(h0=h0, h_last=h_last), saved, False)
+    seq, lead, state, dt = _scan_shapes(cfg)
+    _expect("x", x, seq, dt)
+    _expect("gate", gate, seq, dt)
+    _expect("h", h, seq, dt)
+    _expect("starts", starts, lead, torch.uint8, True)
+    _expect("h0", h0, state, torch.float32, True)
+    _expect("h_last", h_last, state, torch.float32, True)
+    if saved is not None:
+        _bytes("saved", saved, dendsn_scan_workspace_size(cfg))
     _check("dendsn_scan_forward", load().dendsn_scan_forward(
         ctypes.byref(cfg), _ptr(x), _ptr(gate), _ptr(starts), _ptr(h0), _ptr(h), _ptr(h_last),
         _ptr(saved), _stream(stream)))
@@ -473,8 +476,17 @@ def dendsn_scan_forward(cfg, x, gate, starts, h0, h, h_last=None, saved=None, st
 
 def dendsn_scan_backward(cfg, x, gate, starts, h0, grad_h, grad_last, saved, grad_x, grad_gate,
                          grad_h0=None, stream=None):
-    _scan_expect(cfg, dict(x=x, gate=gate, grad_h=grad_h, grad_x=grad_x, grad_gate=grad_gate),
-                 starts, dict(h0=h0, grad_last=grad_last, grad_h0=grad_h0), saved, True)
+    seq, lead, state, dt = _scan_shapes(cfg)
+    _expect("x", x, seq, dt)
+    _expect("gate", gate, seq, dt)
+    _expect("grad_h", grad_h, seq, dt)
+    _expect("grad_x", grad_x, seq, dt)
+    _expect("grad_gate", grad_gate, seq, dt)
+    _expect("starts", starts, lead, torch.uint8, True)
+    _expect("h0", h0, state, torch.float32, True)
+    _expect("grad_last", grad_last, state, torch.float32, True)
+    _expect("grad_h0", grad_h0, state, torch.float32, True)
+    _bytes("saved", saved, dendsn_scan_workspace_size(cfg))
     _check("dendsn_scan_backward", load().dendsn_scan_backward(
         ctypes.byref(cfg), _ptr(x), _ptr(gate), _ptr(starts), _ptr(h0), _ptr(grad_h),
         _ptr(grad_last), _ptr(saved), _ptr(grad_x), _ptr(grad_gate), _ptr(grad_h0),
