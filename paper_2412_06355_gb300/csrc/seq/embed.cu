@@ -10,9 +10,13 @@
 // same from run to run. They are found by counting: a slot for every token (integer atomics
 // in any order), offsets by a prefix sum over the vocabulary, positions scattered to offset +
 // slot, and then each row's few positions put in ascending order, by rank within a warp up to
-// 32 of them, and by a bitmap of positions in shared memory above. Text has a few tokens with
-// thousands of positions; those rows are summed in tiles of 64 positions by one warp each,
-// whose float32 sums are joined in order, so that no row waits for one warp.
+// 32 of them, and by a bitmap of positions in shared memory above. All of that is one launch
+// whose blocks meet between the steps: a cluster of 8 up to kFewTokens tokens (its barrier is
+// the hardware's), a cooperative grid above. Text has a few tokens with thousands of positions;
+// those rows are summed in tiles of 32 positions by one warp each, whose float32 sums are joined
+// in order, so that no row waits for one warp. The other rows go 8 to a warp, their positions
+// batched across rows so that four gradient rows are in flight whatever the counts are.
+#include <cooperative_groups.h>
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -23,9 +27,12 @@ namespace dendsn {
 namespace {
 
 constexpr int kFew = 32;          // positions a warp orders by rank
-constexpr int kTile = 64;         // positions of one partial sum of a longer row
-constexpr int kScanRows = 4096;   // vocabulary rows of one prefix block
+constexpr int kTile = 32;         // positions of one partial sum of a longer row
+constexpr int kThreads = 1024;    // of an index block
 constexpr int kMapBits = 1 << 20; // positions one pass of the bitmap covers (128 KB)
+constexpr int kFewTokens = 8192;  // tokens and rows up to which a cluster forms the index
+constexpr int kFewRows = 1 << 18;
+constexpr int kRowsOfWarp = 8;      // vocabulary rows of a warp of the sum
 
 // VEC elements: 16 bytes where rows and tensors are aligned to 16 bytes, else one element.
 template <typename T, int VEC> struct Piece;
@@ -111,10 +118,13 @@ __global__ void __launch_bounds__(256) embed_forward_kernel(const T *table, cons
 
 // ------------------------------------------------------------------ positions by row
 struct Index {
+    int64_t n, V, pad;
+    int32_t chunk;       // vocabulary rows whose prefix sums one block forms
+    int32_t words;       // of the bitmap
     int32_t *count;      // [V] tokens of a row
-    int32_t *base;       // [prefix blocks] tokens before each block of kScanRows rows
-    int32_t *heads;      // [4]: long rows, their tiles, finished prefix blocks
-    int32_t *offset;     // [V] tokens before a row within its block
+    unsigned long long *heads;   // long rows (high half) and their tiles (low half)
+    int32_t *base;       // [blocks] tokens of each chunk, then before it
+    int32_t *offset;     // [V] tokens before a row within its chunk
     int32_t *slot;       // [n]
     int32_t *pos;        // [n] positions by row
     int32_t *long_row;   // [longs] rows with more than kFew tokens
@@ -124,221 +134,308 @@ struct Index {
 };
 
 __device__ __forceinline__ int32_t first_of(const Index &x, int64_t v) {
-    return x.offset[v] + x.base[v / kScanRows];
+    return x.offset[v] + x.base[v / x.chunk];
 }
+__device__ __forceinline__ int32_t long_rows(const Index &x) { return (int32_t)(*x.heads >> 32); }
+__device__ __forceinline__ int32_t long_tiles(const Index &x) { return (int32_t)*x.heads; }
 
 template <typename I> __device__ __forceinline__ int64_t row_of(const I *ids, int64_t i, int64_t V, int64_t pad) {
     const int64_t id = ids[i];
     return id < 0 || id >= V || id == pad ? -1 : id;
 }
 
-// A slot of its own for every token among those of its row; one atomic for the equal tokens of
-// a warp. Which token gets which slot depends on the schedule, the set of slots does not.
-template <typename I>
-__global__ void __launch_bounds__(256) embed_count_kernel(const I *ids, Index x, int64_t n, int64_t V, int64_t pad) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int lane = threadIdx.x & 31;
-    const int64_t v = i < n ? row_of(ids, i, V, pad) : -1;
-    const unsigned same = __match_any_sync(0xffffffffu, (int)v);
-    if (v < 0) return;
-    const int leader = __ffs(same) - 1;
-    int first = 0;
-    if (lane == leader) first = atomicAdd(x.count + v, __popc(same));
-    first = __shfl_sync(same, first, leader);
-    x.slot[i] = first + __popc(same & ((1u << lane) - 1));
-}
-
-// Exclusive prefix sums of the counts within blocks of kScanRows rows; the last block to finish
-// sums up the blocks. Rows with more than kFew tokens are listed with their tiles (the order of
-// the list does not matter to any result).
-__global__ void __launch_bounds__(1024) embed_prefix_kernel(Index x, int64_t V, int32_t blocks) {
-    __shared__ int32_t warps[32];
-    __shared__ bool last;
+// Exclusive prefix sum of one value of each of the block's threads, and the sum of all.
+__device__ __forceinline__ int32_t prefix(int32_t v, int32_t *warps, int32_t &all) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t v0 = (int64_t)blockIdx.x * kScanRows + threadIdx.x * 4;
-    int32_t c[4], sum = 0;
+    int32_t incl = v;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        c[j] = v0 + j < V ? x.count[v0 + j] : 0;
-        sum += c[j];
-    }
-    int32_t incl = sum;
     for (int o = 1; o < 32; o <<= 1) {
-        const int32_t up = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += up;
+        const int32_t u = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += u;
     }
+    __syncthreads();
     if (lane == 31) warps[warp] = incl;
     __syncthreads();
     if (warp == 0) {
         int32_t w = warps[lane];
+#pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int32_t up = __shfl_up_sync(0xffffffffu, w, o);
-            if (lane >= o) w += up;
+            const int32_t u = __shfl_up_sync(0xffffffffu, w, o);
+            if (lane >= o) w += u;
         }
         warps[lane] = w;
     }
     __syncthreads();
-    int32_t before = incl - sum + (warp ? warps[warp - 1] : 0);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        if (v0 + j < V) x.offset[v0 + j] = before;
-        before += c[j];
-        if (c[j] > kFew) {
-            const int at = atomicAdd(x.heads, 1), tiles = (c[j] + kTile - 1) / kTile;
-            const int tile = atomicAdd(x.heads + 1, tiles);
-            x.long_row[at] = (int32_t)(v0 + j);
-            x.long_tile[at] = tile;
-            for (int k = 0; k < tiles; ++k) x.tile_of[tile + k] = at;
-        }
-    }
-    if (threadIdx.x == 0) {
-        x.base[blockIdx.x] = warps[31];
-        __threadfence();
-        last = atomicAdd(x.heads + 2, 1) == blocks - 1;
-    }
-    __syncthreads();
-    if (last && threadIdx.x == 0) {
-        __threadfence();
-        int32_t total = 0;
-        for (int b = 0; b < blocks; ++b) {
-            const int32_t t = __ldcg(x.base + b);
-            x.base[b] = total;
-            total += t;
-        }
-    }
+    all = warps[31];
+    return incl - v + (warp ? warps[warp - 1] : 0);
 }
 
-template <typename I>
-__global__ void __launch_bounds__(256) embed_scatter_kernel(const I *ids, Index x, int64_t n, int64_t V, int64_t pad) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t v = i < n ? row_of(ids, i, V, pad) : -1;
-    if (v >= 0) x.pos[first_of(x, v) + x.slot[i]] = (int32_t)i;
-}
-
-// Puts the positions of each long row in ascending order: one bit for each position of the
-// call, set and read back in order, kMapBits positions at a time.
-__global__ void __launch_bounds__(256) embed_order_kernel(Index x, int64_t n, int32_t words) {
+// CLUSTER: the grid is one cluster.
+template <typename I, bool CLUSTER>
+__global__ void __launch_bounds__(kThreads) embed_index_kernel(const I *ids, Index x) {
+    namespace cg = cooperative_groups;
+    auto meet = [] {
+        if constexpr (CLUSTER) cg::this_cluster().sync();
+        else cg::this_grid().sync();
+    };
     extern __shared__ uint32_t map[];
-    __shared__ int32_t warps[8];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    for (int k = blockIdx.x; k < x.heads[0]; k += gridDim.x) {
-        const int32_t v = x.long_row[k], c = x.count[v];
-        int32_t *pos = x.pos + first_of(x, v);
+    __shared__ int32_t warps[32];
+    const int lane = threadIdx.x & 31;
+    const int64_t at = (int64_t)blockIdx.x * kThreads + threadIdx.x, stride = (int64_t)gridDim.x * kThreads;
+
+    for (int64_t v = at; v < x.V; v += stride) x.count[v] = 0;
+    if (at == 0) *x.heads = 0;
+    meet();
+
+    // A slot of its own for every token among those of its row; one atomic for the equal tokens
+    // of a warp. Which token gets which slot depends on the schedule, the set of slots does not.
+    for (int64_t i0 = at - lane; i0 < x.n; i0 += stride) {
+        const int64_t i = i0 + lane, v = i < x.n ? row_of(ids, i, x.V, x.pad) : -1;
+        const unsigned same = __match_any_sync(0xffffffffu, (int)v);
+        if (v >= 0) {
+            const int leader = __ffs(same) - 1;
+            int first = 0;
+            if (lane == leader) first = atomicAdd(x.count + v, __popc(same));
+            x.slot[i] = __shfl_sync(same, first, leader) + __popc(same & ((1u << lane) - 1));
+        }
+        __syncwarp();
+    }
+    meet();
+
+    // Prefix sums of the counts within the block's chunk of rows. Rows with more than kFew tokens
+    // are listed with their tiles (the order of the list does not matter to any result).
+    {
+        const int64_t v0 = (int64_t)blockIdx.x * x.chunk, v1 = min(x.V, v0 + x.chunk);
+        int32_t done = 0;
+        for (int64_t u = v0; u < v1; u += 4 * kThreads) {
+            const int64_t v = u + threadIdx.x * 4;
+            int32_t c[4], sum = 0, all;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                c[j] = v + j < v1 ? __ldcg(x.count + v + j) : 0;
+                sum += c[j];
+            }
+            int32_t before = done + prefix(sum, warps, all);
+            done += all;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (v + j < v1) x.offset[v + j] = before;
+                before += c[j];
+                if (c[j] > kFew) {
+                    const unsigned tiles = (unsigned)(c[j] + kTile - 1) / kTile;
+                    const unsigned long long h = atomicAdd(x.heads, (1ull << 32) + tiles);
+                    x.long_row[h >> 32] = (int32_t)(v + j);
+                    x.long_tile[h >> 32] = (int32_t)h;
+                }
+            }
+        }
+        if (threadIdx.x == 0) x.base[blockIdx.x] = done;
+    }
+    meet();
+
+    // The chunks' own prefix sums: every block forms them for itself, block 0 also for later.
+    __shared__ int32_t base[kThreads];
+    {
+        int32_t all;
+        const int32_t mine = threadIdx.x < gridDim.x ? __ldcg(x.base + threadIdx.x) : 0;
+        base[threadIdx.x] = prefix(mine, warps, all);
+        __syncthreads();
+    }
+    for (int64_t i = at; i < x.n; i += stride) {
+        const int64_t v = row_of(ids, i, x.V, x.pad);
+        if (v >= 0) x.pos[__ldcg(x.offset + v) + base[v / x.chunk] + x.slot[i]] = (int32_t)i;
+    }
+    meet();
+    if (blockIdx.x == 0 && threadIdx.x < gridDim.x) x.base[threadIdx.x] = base[threadIdx.x];
+
+    // Puts the positions of each long row in ascending order: one bit for each position of the
+    // call, set and read back in order. Few tokens: a warp for each row, with a bitmap of its own;
+    // else a block, kMapBits positions at a time.
+    const int32_t longs = (int32_t)(__ldcg(x.heads) >> 32);
+    if constexpr (CLUSTER) {
+        const int warp = threadIdx.x >> 5;
+        uint32_t *mine = map + warp * x.words;
+        for (int k = blockIdx.x * 32 + warp; k < longs; k += gridDim.x * 32) {
+            const int32_t v = __ldcg(x.long_row + k), c = __ldcg(x.count + v), tile = __ldcg(x.long_tile + k);
+            for (int32_t t = lane; t < (c + kTile - 1) / kTile; t += 32) x.tile_of[tile + t] = k;
+            int32_t *pos = x.pos + __ldcg(x.offset + v) + base[v / x.chunk];
+            for (int w = lane; w < x.words; w += 32) mine[w] = 0;
+            __syncwarp();
+            for (int32_t j = lane; j < c; j += 32) {
+                const int32_t q = __ldcg(pos + j);
+                atomicOr(mine + (q >> 5), 1u << (q & 31));
+            }
+            __syncwarp();
+            const int per = (x.words + 31) / 32, w0 = min(x.words, lane * per), w1 = min(x.words, w0 + per);
+            int32_t here = 0;
+            for (int w = w0; w < w1; ++w) here += __popc(mine[w]);
+            int32_t to = here;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int32_t u = __shfl_up_sync(0xffffffffu, to, o);
+                if (lane >= o) to += u;
+            }
+            to -= here;
+            for (int w = w0; w < w1; ++w)
+                for (uint32_t m = mine[w]; m; m &= m - 1) pos[to++] = 32 * w + __ffs(m) - 1;
+            __syncwarp();
+        }
+    } else
+    for (int k = blockIdx.x; k < longs; k += gridDim.x) {
+        const int32_t v = __ldcg(x.long_row + k), c = __ldcg(x.count + v), tile = __ldcg(x.long_tile + k);
+        for (int32_t t = threadIdx.x; t < (c + kTile - 1) / kTile; t += kThreads) x.tile_of[tile + t] = k;
+        const int64_t first = __ldcg(x.offset + v) + base[v / x.chunk];
+        int32_t *pos = x.pos + first;
         int32_t done = 0;
         // the row's positions are read again for every stretch and overwritten by it only up
         // to the number found so far, so calls of more than one stretch keep them in slot
         const int32_t *src = pos;
-        if (n > kMapBits) {
-            for (int32_t j = threadIdx.x; j < c; j += 256) x.slot[first_of(x, v) + j] = pos[j];
-            src = x.slot + first_of(x, v);
+        if (x.n > kMapBits) {
+            for (int32_t j = threadIdx.x; j < c; j += kThreads) x.slot[first + j] = __ldcg(pos + j);
+            src = x.slot + first;
             __syncthreads();
         }
-        for (int64_t p0 = 0; p0 < n; p0 += kMapBits) {
-            for (int w = threadIdx.x; w < words; w += 256) map[w] = 0;
+        for (int64_t p0 = 0; p0 < x.n; p0 += kMapBits) {
+            for (int w = threadIdx.x; w < x.words; w += kThreads) map[w] = 0;
             __syncthreads();
-            for (int32_t j = threadIdx.x; j < c; j += 256) {
-                const int64_t p = src[j] - p0;
+            for (int32_t j = threadIdx.x; j < c; j += kThreads) {
+                const int64_t p = __ldcg(src + j) - p0;
                 if (p >= 0 && p < kMapBits) atomicOr(map + (p >> 5), 1u << (p & 31));
             }
             __syncthreads();
             // each thread reads back `per` consecutive words
-            const int per = (words + 255) / 256, w0 = threadIdx.x * per, w1 = min(words, w0 + per);
-            int32_t mine = 0;
+            const int per = (x.words + kThreads - 1) / kThreads, w0 = threadIdx.x * per, w1 = min(x.words, w0 + per);
+            int32_t mine = 0, all;
             for (int w = w0; w < w1; ++w) mine += __popc(map[w]);
-            int32_t incl = mine;
-            for (int o = 1; o < 32; o <<= 1) {
-                const int32_t up = __shfl_up_sync(0xffffffffu, incl, o);
-                if (lane >= o) incl += up;
-            }
-            if (lane == 31) warps[warp] = incl;
-            __syncthreads();
-            int32_t at = done + incl - mine;
-            for (int w = 0; w < 8; ++w) {
-                if (w < warp) at += warps[w];
-                done += warps[w];
-            }
+            int32_t to = done + prefix(mine, warps, all);
+            done += all;
             for (int w = w0; w < w1; ++w)
-                for (uint32_t m = map[w]; m; m &= m - 1) pos[at++] = (int32_t)(p0 + 32 * w + __ffs(m) - 1);
+                for (uint32_t m = map[w]; m; m &= m - 1) pos[to++] = (int32_t)(p0 + 32 * w + __ffs(m) - 1);
             __syncthreads();
         }
     }
 }
 
-// Sum of the rows at `c` positions, `p` holding up to 32 of them in the warp's lanes.
-template <typename T, int VEC>
-__device__ __forceinline__ void add_rows(float (&acc)[kAhead][VEC], const T *grad, int32_t nv, int32_t k0,
-                                         int32_t p, int c) {
+// Adds up gradient rows, `m` of them at the positions `p` of the warp's lanes in order, four in
+// flight, for the kAhead vectors from k0 on; calls done(k, sums) after each position k whose bit
+// is set in `ends`, and begins anew.
+template <typename T, int VEC, typename F>
+__device__ __forceinline__ void add_rows(const T *grad, int32_t nv, int32_t k0, int32_t p, int m, uint32_t ends, F done) {
     using P = Piece<T, VEC>;
     using Raw = typename P::Raw;
-    for (int k = 0; k < c; ++k) {
-        const Raw *from = reinterpret_cast<const Raw *>(grad) + (int64_t)__shfl_sync(0xffffffffu, p, k) * nv;
-        Raw r[kAhead];
+    constexpr int kRows = 4;
+    float acc[kAhead][VEC] = {};
+    for (int k = 0; k < m; k += kRows) {
+        Raw r[kRows][kAhead];
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j)
-            if (k0 + 32 * j < nv) r[j] = __ldcs(from + k0 + 32 * j);
+        for (int u = 0; u < kRows; ++u) {
+            const Raw *from = reinterpret_cast<const Raw *>(grad) + (int64_t)__shfl_sync(0xffffffffu, p, min(k + u, 31)) * nv;
+            if (k + u < m)
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j)
-            if (k0 + 32 * j < nv) {
-                float v[VEC];
-                P::unpack(r[j], v);
+                for (int j = 0; j < kAhead; ++j)
+                    if (k0 + 32 * j < nv) r[u][j] = __ldcs(from + k0 + 32 * j);
+        }
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) acc[j][e] += v[e];
+        for (int u = 0; u < kRows; ++u)
+            if (k + u < m) {
+#pragma unroll
+                for (int j = 0; j < kAhead; ++j)
+                    if (k0 + 32 * j < nv) {
+                        float v[VEC];
+                        P::unpack(r[u][j], v);
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) acc[j][e] += v[e];
+                    }
+                if (ends >> (k + u) & 1) {
+                    done(k + u, acc);
+#pragma unroll
+                    for (int j = 0; j < kAhead; ++j)
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) acc[j][e] = 0.f;
+                }
             }
     }
 }
 
-// One warp per task: first the tiles of long rows, then every row of the vocabulary.
+// One warp per task: first the tiles of long rows, then kRowsOfWarp rows of the vocabulary each.
 template <typename T, int VEC>
-__global__ void __launch_bounds__(256) embed_sum_kernel(const T *grad, T *gtable, Index x, int64_t V, int64_t D,
-                                                        int32_t nv, float scale) {
+__global__ void __launch_bounds__(256) embed_sum_kernel(const T *grad, T *gtable, Index x, int64_t D, int32_t nv,
+                                                        float scale) {
     using P = Piece<T, VEC>;
     using Raw = typename P::Raw;
     const int lane = threadIdx.x & 31;
     const int64_t task = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    const int32_t tiles = x.heads[1];
-    int32_t p = 0, c, p2 = 0, c2 = 0;
-    float *part = nullptr;
-    Raw *to = nullptr;
+    const int32_t tiles = x.n > kFew ? long_tiles(x) : 0;
     if (task < tiles) {
         const int32_t at = x.tile_of[task], v = x.long_row[at], k = (int32_t)task - x.long_tile[at];
-        const int32_t *pos = x.pos + first_of(x, v) + k * kTile;
-        const int32_t all = min(kTile, x.count[v] - k * kTile);
-        c = min(32, all);
-        c2 = all - c;
-        if (lane < c) p = pos[lane];
-        if (lane < c2) p2 = pos[32 + lane];
-        part = x.partial + task * D;
-    } else {
-        const int64_t v = task - tiles;
-        if (v >= V) return;
-        c = x.count[v];
-        if (c > kFew) return;
-        to = reinterpret_cast<Raw *>(gtable) + v * nv;
-        const int32_t mine = c && lane < c ? x.pos[first_of(x, v) + lane] : INT32_MAX;
-        int rank = 0;
-        for (int k = 0; k < c; ++k) rank += __shfl_sync(0xffffffffu, mine, k) < mine;
-        // lane r takes the position whose rank is r
-        for (int k = 0; k < c; ++k) {
-            const int32_t q = __shfl_sync(0xffffffffu, mine, k), r = __shfl_sync(0xffffffffu, rank, k);
-            if (r == lane) p = q;
-        }
+        const int32_t c = min(kTile, x.count[v] - k * kTile);
+        const int32_t p = lane < c ? x.pos[first_of(x, v) + k * kTile + lane] : 0;
+        float *part = x.partial + task * D;
+        for (int32_t k0 = lane; k0 - lane < nv; k0 += 32 * kAhead)
+            add_rows<T, VEC>(grad, nv, k0, p, c, 1u << (c - 1), [&](int, float (&acc)[kAhead][VEC]) {
+#pragma unroll
+                for (int j = 0; j < kAhead; ++j)
+                    if (k0 + 32 * j < nv)
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) part[(int64_t)(k0 + 32 * j) * VEC + e] = acc[j][e];
+            });
+        return;
     }
-    for (int32_t k0 = lane; k0 - lane < nv; k0 += 32 * kAhead) {
-        float acc[kAhead][VEC] = {};
-        add_rows<T, VEC>(acc, grad, nv, k0, p, c);
-        if (c2) add_rows<T, VEC>(acc, grad, nv, k0, p2, c2);
+    const int64_t v0 = (task - tiles) * kRowsOfWarp;
+    if (v0 >= x.V) return;
+    const bool row = lane < kRowsOfWarp && v0 + lane < x.V;
+    const int32_t all = row && x.n > 0 ? x.count[v0 + lane] : 0, c = all > kFew ? 0 : all;
+    const int32_t first = c ? first_of(x, v0 + lane) : 0;
+    // rows without tokens
+    for (uint32_t m = __ballot_sync(0xffffffffu, row && all == 0); m; m &= m - 1) {
+        Raw *to = reinterpret_cast<Raw *>(gtable) + (v0 + __ffs(m) - 1) * nv;
+        float zero[VEC] = {};
+        for (int32_t k = lane; k < nv; k += 32) __stcs(to + k, P::pack(zero));
+    }
+    int32_t incl = c;
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j)
-            if (k0 + 32 * j < nv) {
-                if (part) {
+    for (int o = 1; o < kRowsOfWarp; o <<= 1) {
+        const int32_t u = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += u;
+    }
+    // batches of rows with up to 32 positions together
+    const int32_t total = __shfl_sync(0xffffffffu, incl, kRowsOfWarp - 1);
+    for (int32_t done = 0; done < total;) {
+        const uint32_t fits = __ballot_sync(0xffffffffu, lane < kRowsOfWarp && incl - done <= 32);
+        const int last = 31 - __clz(fits);                   // the batch's last row
+        const int m = __shfl_sync(0xffffffffu, incl, last) - done;
+        // lane i takes the batch's position i: its row is the first whose end lies beyond i
+        int mine = 0;
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) part[(int64_t)(k0 + 32 * j) * VEC + e] = acc[j][e];
-                } else {
+        for (int r = 0; r < kRowsOfWarp; ++r) mine += __shfl_sync(0xffffffffu, incl, r) - done <= lane;
+        mine = min(mine, kRowsOfWarp - 1);
+        const int32_t end = __shfl_sync(0xffffffffu, incl, mine) - done, size = __shfl_sync(0xffffffffu, c, mine);
+        const int32_t from = __shfl_sync(0xffffffffu, first, mine), start = end - size;
+        const int32_t q = lane < m ? x.pos[from + lane - start] : 0;
+        // its place among its row's positions in ascending order
+        int rank = start;
+        for (int k = 0; k < m; ++k) {
+            const int32_t other = __shfl_sync(0xffffffffu, q, k);
+            rank += k >= start && k < end && other < q;
+        }
+        int32_t p = 0;
+        for (int k = 0; k < m; ++k) {
+            const int32_t other = __shfl_sync(0xffffffffu, q, k), r = __shfl_sync(0xffffffffu, rank, k);
+            if (r == lane) p = other;
+        }
+        const uint32_t ends = __ballot_sync(0xffffffffu, lane < m && lane == end - 1);
+        for (int32_t k0 = lane; k0 - lane < nv; k0 += 32 * kAhead)
+            add_rows<T, VEC>(grad, nv, k0, p, m, ends, [&](int k, float (&acc)[kAhead][VEC]) {
+                Raw *to = reinterpret_cast<Raw *>(gtable) + (v0 + __shfl_sync(0xffffffffu, mine, k)) * nv;
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) acc[j][e] *= scale;
-                    __stcs(to + k0 + 32 * j, P::pack(acc[j]));
-                }
-            }
+                for (int j = 0; j < kAhead; ++j)
+                    if (k0 + 32 * j < nv) {
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) acc[j][e] *= scale;
+                        __stcs(to + k0 + 32 * j, P::pack(acc[j]));
+                    }
+            });
+        done += m;
     }
 }
 
@@ -347,7 +444,8 @@ template <typename T>
 __global__ void __launch_bounds__(256) embed_join_kernel(T *gtable, Index x, int64_t D, float scale) {
     const int64_t d = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (d >= D) return;
-    for (int at = blockIdx.y; at < x.heads[0]; at += gridDim.y) {
+    const int32_t longs = long_rows(x);
+    for (int at = blockIdx.y; at < longs; at += gridDim.y) {
         const int32_t v = x.long_row[at], tiles = (x.count[v] + kTile - 1) / kTile;
         const float *p = x.partial + (int64_t)x.long_tile[at] * D + d;
         float sum = 0.f;
@@ -365,10 +463,13 @@ __global__ void __launch_bounds__(256) embed_join_kernel(T *gtable, Index x, int
     }
 }
 
+constexpr int kSms = 152;
+
 struct Plan {
-    int32_t blocks;               // of the prefix sum
+    bool cluster;                 // the index kernel is one cluster
+    int32_t blocks, chunk;        // of the index kernel, vocabulary rows of one
     int64_t longs, tiles;         // most long rows and tiles there can be
-    size_t at[10], zeroed, scratch;
+    size_t at[10], scratch;
 };
 
 dendsn_status make_plan(const dendsn_embed_config *cfg, Plan *pl) {
@@ -383,17 +484,21 @@ dendsn_status make_plan(const dendsn_embed_config *cfg, Plan *pl) {
     // the largest grids: a warp for every kAhead vectors of an output row, and for every row and tile
     if ((cfg->n * (((int64_t)cfg->D + 32 * kAhead - 1) / (32 * kAhead)) + 7) / 8 > INT32_MAX)
         return seq_fail(DENDSN_ERR_UNSUPPORTED, "too many elements (n=%lld D=%d)", (long long)cfg->n, cfg->D);
-    pl->blocks = (int32_t)(((int64_t)cfg->V + kScanRows - 1) / kScanRows);
+    // a block for every 1024 tokens or 4096 rows, at most a cluster's or one for each SM
+    const int64_t blocks = std::max((cfg->n + kThreads - 1) / kThreads, ((int64_t)cfg->V + 4 * kThreads - 1) / (4 * kThreads));
+    pl->cluster = cfg->n <= kFewTokens && cfg->V <= kFewRows;
+    pl->blocks = (int32_t)std::min<int64_t>(blocks, pl->cluster ? 8 : kSms);
+    while (pl->cluster && (pl->blocks & (pl->blocks - 1))) ++pl->blocks;
+    pl->chunk = (int32_t)(((int64_t)cfg->V + pl->blocks - 1) / pl->blocks);
     pl->longs = std::min<int64_t>(cfg->V, cfg->n / (kFew + 1));
     pl->tiles = cfg->n / kTile + pl->longs;
-    const size_t sizes[10] = {(size_t)cfg->V * 4, (size_t)pl->blocks * 4, 16, (size_t)cfg->V * 4, (size_t)cfg->n * 4,
+    const size_t sizes[10] = {(size_t)cfg->V * 4, 16, kSms * 4, (size_t)cfg->V * 4, (size_t)cfg->n * 4,
                               (size_t)cfg->n * 4, (size_t)pl->longs * 4, (size_t)pl->longs * 4, (size_t)pl->tiles * 4,
                               (size_t)pl->tiles * cfg->D * 4};
     size_t at = 0;
     for (int i = 0; i < 10; ++i) {
         pl->at[i] = at;
         at += (sizes[i] + 15) / 16 * 16;
-        if (i == 2) pl->zeroed = at;      // count, base and heads start at zero
     }
     pl->scratch = at;
     return DENDSN_OK;
@@ -415,31 +520,44 @@ cudaError_t run_backward(const dendsn_embed_config &c, const Plan &pl, const voi
                          void *gtable, void *scratch, cudaStream_t s, int *launches) {
     char *p = static_cast<char *>(scratch);
     auto ints = [&](int i) { return reinterpret_cast<int32_t *>(p + pl.at[i]); };
-    Index x{ints(0), ints(1), ints(2), ints(3), ints(4), ints(5), ints(6), ints(7), ints(8),
-            reinterpret_cast<float *>(p + pl.at[9])};
+    Index x{c.n, c.V, c.padding_id, pl.chunk, (int32_t)(std::min<int64_t>(c.n, kMapBits) + 31) / 32, ints(0),
+            reinterpret_cast<unsigned long long *>(p + pl.at[1]), ints(2), ints(3), ints(4), ints(5), ints(6), ints(7),
+            ints(8), reinterpret_cast<float *>(p + pl.at[9])};
     const I *ids = static_cast<const I *>(ids_);
     const T *g = static_cast<const T *>(grad);
     T *gt = static_cast<T *>(gtable);
     const int32_t nv = c.D / VEC;
-    const unsigned tokens = (unsigned)((c.n + 255) / 256);
-    cudaError_t e = cudaMemsetAsync(scratch, 0, pl.zeroed, s);
-    if (e != cudaSuccess) return e;
     if (c.n > 0) {
-        embed_count_kernel<I><<<tokens, 256, 0, s>>>(ids, x, c.n, c.V, c.padding_id);
-        embed_prefix_kernel<<<pl.blocks, 1024, 0, s>>>(x, c.V, pl.blocks);
-        embed_scatter_kernel<I><<<tokens, 256, 0, s>>>(ids, x, c.n, c.V, c.padding_id);
-        *launches += 3;
-    }
-    if (pl.longs > 0) {
-        const int32_t words = (int32_t)(std::min<int64_t>(c.n, kMapBits) + 31) / 32;
-        if (words * 4 > 48 * 1024) {
-            e = cudaFuncSetAttribute(embed_order_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, words * 4);
-            if (e != cudaSuccess) return e;
+        const bool few = pl.cluster;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)pl.blocks);
+        cfg.blockDim = dim3(kThreads);
+        cfg.dynamicSmemBytes = pl.longs > 0 ? (size_t)x.words * 4 * (few ? kThreads / 32 : 1) : 0;
+        cfg.stream = s;
+        cudaLaunchAttribute at[1];
+        if (few) {
+            at[0].id = cudaLaunchAttributeClusterDimension;
+            at[0].val.clusterDim.x = (unsigned)pl.blocks;
+            at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+        } else {
+            at[0].id = cudaLaunchAttributeCooperative;
+            at[0].val.cooperative = 1;
         }
-        embed_order_kernel<<<(unsigned)std::min<int64_t>(pl.longs, 608), 256, words * 4, s>>>(x, c.n, words);
+        cfg.attrs = at;
+        cfg.numAttrs = 1;
+        auto start = [&](auto kernel) {
+            if (cfg.dynamicSmemBytes > 32768) {
+                cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                     (int)cfg.dynamicSmemBytes);
+                if (e != cudaSuccess) return e;
+            }
+            return cudaLaunchKernelEx(&cfg, kernel, ids, x);
+        };
+        cudaError_t e = few ? start(embed_index_kernel<I, true>) : start(embed_index_kernel<I, false>);
+        if (e != cudaSuccess) return e;
         *launches += 1;
     }
-    embed_sum_kernel<T, VEC><<<(unsigned)((c.V + pl.tiles + 7) / 8), 256, 0, s>>>(g, gt, x, c.V, c.D, nv, c.scale);
+    embed_sum_kernel<T, VEC><<<(unsigned)(((c.V + kRowsOfWarp - 1) / kRowsOfWarp + pl.tiles + 7) / 8), 256, 0, s>>>(g, gt, x, c.D, nv, c.scale);
     *launches += 1;
     if (pl.longs > 0) {
         const dim3 grid((unsigned)((c.D + 255) / 256), (unsigned)std::min<int64_t>(pl.longs, 1024));
