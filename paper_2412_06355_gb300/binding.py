@@ -208,8 +208,15 @@ def _ptr(t: Optional[torch.Tensor]):
     return t.data_ptr()
 
 
+# The current stream's handle without a Stream object around it (3 us less a call); the public
+# way where torch does not offer it.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream) -> int:
     if stream is None:
+        if _raw_stream is not None:
+            return _raw_stream(torch.cuda.current_device())
         stream = torch.cuda.current_stream()
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
