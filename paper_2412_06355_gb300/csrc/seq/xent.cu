@@ -615,7 +615,7 @@ __global__ void __launch_bounds__(256) xent_hidden_kernel(Rows R, const float *s
 }
 
 // ------------------------------------------------------------------ host
-constexpr size_t kPieceBytes = size_t(256) << 20;   // of G
+constexpr size_t kPieceBytes = size_t(512) << 20;   // of G
 constexpr int kClusters = 76;                        // pairs of the card's 152 SMs
 
 struct Plan {
