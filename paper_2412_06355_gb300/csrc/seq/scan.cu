@@ -9,7 +9,8 @@
 // block, distributed shared memory between the blocks of the cluster), then run the segment
 // from its true state and write. Every element is read and written once; the rows of the
 // passes to come are copied to shared memory meanwhile (cp.async, 16 bytes a thread where rows
-// are aligned), each warp its own segments, so that registers hold one segment only.
+// are aligned), each warp its own segments, so that registers hold one segment only. Results go
+// back through the same slots, to be written 16 bytes at a time.
 // A start makes its segment's map constant; that is kept as a flag and selected, not
 // multiplied by zero, so that what came before it cannot leak as NaN.
 //
@@ -234,25 +235,32 @@ template <bool CL> struct Exchange {
 };
 
 // Folds the segment maps over the state before the pass; returns the state before this
-// thread's segment, which is number `me` of Q in the order of the fold. One barrier a pass: the
-// maps have two buffers, and the last segment leaves the state behind in sh.carry.
+// thread's segment, which is number `me` of Q in the order of the fold, and whether any segment
+// of the block has a start. One barrier a pass: the maps have two buffers, and the last segment
+// leaves the state behind in sh.carry.
 template <bool CL, bool LOGIT, int MQ>
 __device__ __forceinline__ F2 fold(ScanShared<CL> &sh, const ScanArgs &P, int me, int cp, int width, int mine,
-                                   int pass, F2 A, F2 B, bool cut, F2 &carry) {
+                                   int pass, F2 A, F2 B, bool cut, F2 &carry, bool &cuts) {
     const int buf = pass & 1;
     sh.map[buf][me * width + cp] = Map{finite<LOGIT>(A), B};
     sh.cut[buf][me * width + cp] = cut;
     F2 in;
     if constexpr (!CL) {
-        const bool cuts = __syncthreads_or(cut);
+        cuts = __syncthreads_or(cut);
         in = pass ? sh.carry[buf ^ 1][cp] : carry;
         // unrolled, so that the maps are read together and only the products wait on one another
+        if (cuts) {
 #pragma unroll
-        for (int i = 0; i < MQ - 1; ++i)
-            if (i < me) in = over(sh.map[buf][i * width + cp], cuts && sh.cut[buf][i * width + cp], in);
+            for (int i = 0; i < MQ - 1; ++i)
+                if (i < me) in = over(sh.map[buf][i * width + cp], sh.cut[buf][i * width + cp], in);
+        } else {
+#pragma unroll
+            for (int i = 0; i < MQ - 1; ++i)
+                if (i < me) in = over(sh.map[buf][i * width + cp], false, in);
+        }
     } else {
         const Exchange<CL> ex{sh, P, width};
-        const bool cuts = __syncthreads_or(cut);
+        cuts = __syncthreads_or(cut);
         if (me == 0) {                           // the block's map, handed to every block
             F2 a = both(1.f), b = both(0.f);
             bool c = false;
@@ -305,11 +313,12 @@ template <typename XT, int S> __host__ __device__ constexpr int segment_pairs(in
 }
 
 // Where a thread stands: its pair of channels and its segment.
-template <typename XT, bool WIDE, int S, bool CL> struct Place {
+template <typename XT, bool WIDE, int S, int QT, bool CL> struct Place {
     using E = Elem<XT>;
     using One = typename E::One;
     using Pair = typename E::Pair;
-    int width, cp, q, rank;      // pairs of the block, own pair, own segment, block in the cluster
+    int q_all;                   // segments of the block, QT where that is fixed
+    int cp, q, rank;             // own pair, own segment, block in the cluster
     int64_t m, b;                // first channel, its sample
     bool on, on2;                // the pair, its second channel
     int64_t sample;              // of the first of the warp's pairs of the segment
@@ -317,10 +326,16 @@ template <typename XT, bool WIDE, int S, bool CL> struct Place {
     int span, step;              // steps of the block, of a pass
     int64_t base;                // elements to the block's first channel
     uint32_t off, st;            // bytes to the thread's channels and segment, of a step
-    uint32_t piece_off;          // bytes to the piece of a row that the thread copies
-    bool piece_on;
+    // The 16-byte piece that the thread copies of every kPairs-th row: its first row (beyond every
+    // segment where the piece lies beyond the last channel), bytes to it in memory and in a segment's slots.
+    static constexpr int kPairs = 16 / sizeof(Pair);
+    int piece_row;
+    uint32_t piece_off, piece_slot;
+    __device__ __forceinline__ int Q() const { return QT ? QT : q_all; }
+    __device__ __forceinline__ int pairs() const { return QT ? 256 / (QT ? QT : 1) : 256 / q_all; }
     __device__ __forceinline__ explicit Place(const ScanArgs &P) {
-        width = 256 / P.Q;
+        q_all = P.Q;
+        const int width = pairs();
         cp = threadIdx.x % width;
         q = threadIdx.x / width;
         rank = CL ? blockIdx.x % P.CT : 0;
@@ -330,7 +345,7 @@ template <typename XT, bool WIDE, int S, bool CL> struct Place {
         const int64_t n = on ? 2 * (g % P.PN) : 0, b0 = g0 / P.PN, n0 = 2 * (g0 % P.PN);
         on2 = on && (WIDE || n + 1 < P.N);
         m = b * P.N + n;
-        span = P.Q * S;
+        span = Q() * S;
         step = span * (CL ? P.CT : 1);
         base = b0 * P.sb + n0;
         st = (uint32_t)(P.st * sizeof(XT));
@@ -338,30 +353,27 @@ template <typename XT, bool WIDE, int S, bool CL> struct Place {
         sample = __shfl_sync(0xffffffffu, b, lane - lane % min(32, width));
         one_sample = __all_sync(0xffffffffu, !on || b == sample);
         off = on ? (uint32_t)(((b - b0) * P.sb + n - n0) * (int64_t)sizeof(XT)) + (uint32_t)(q * S) * st : 0;
-        constexpr int kPairs = 16 / sizeof(Pair);
-        const int64_t gp = g0 + (cp & ~31) + (cp & 31) % (min(32, width) / kPairs) * kPairs;
-        piece_on = gp < P.pairs;
-        piece_off = piece_on ? (uint32_t)((((gp / P.PN) - b0) * P.sb + 2 * (gp % P.PN) - n0) * (int64_t)sizeof(XT)) +
-                                   (uint32_t)(q * S) * st : 0;
+        const int across = min(32, width) / kPairs, row = (cp & 31) / across;
+        const int piece = (cp & ~31) + (cp & 31) % across * kPairs;
+        const int64_t gp = g0 + piece;
+        piece_row = gp < P.pairs ? row : INT32_MAX / 2;
+        piece_off = gp < P.pairs ? (uint32_t)((((gp / P.PN) - b0) * P.sb + 2 * (gp % P.PN) - n0) * (int64_t)sizeof(XT)) +
+                                       (uint32_t)(q * S + row) * st : 0;
+        piece_slot = (uint32_t)((row * width + piece) * sizeof(Pair));
     }
     // Copies the rows of this thread's segment from `p` into `to`, S rows of `width` pairs; the
     // threads of a warp share the work where rows are WIDE (16-byte pieces), else each
     // copies its own pair.
     __device__ __forceinline__ void copy(Pair *to, const char *p, int left) const {
+        const int width = pairs();
         const uint32_t dst = (uint32_t)__cvta_generic_to_shared(to);
         if constexpr (WIDE) {
-            constexpr int kPairs = 16 / sizeof(Pair), kRows = kPairs;   // pairs of a piece, rows of a round
-            const int across = min(32, width) / kPairs, row = (cp & 31) / across;   // within the warp's pairs
-            const int piece = (cp & ~31) + (cp & 31) % across * kPairs;
 #pragma unroll
-            for (int r = 0; r < S; r += kRows) {
-                const int s = r + row;
-                if (S % kRows == 0 || s < S)
-                    if (piece_on && s < left)
-                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(
-                                         dst + (uint32_t)((s * width + piece) * sizeof(Pair))),
-                                     "l"(p + (piece_off + s * st)) : "memory");
-            }
+            for (int r = 0; r < S; r += kPairs)
+                if (r < left - piece_row)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(
+                                         dst + piece_slot + (uint32_t)(r * width * sizeof(Pair))),
+                                     "l"(p + (piece_off + r * st)) : "memory");
         } else {
 #pragma unroll
             for (int s = 0; s < S; ++s)
@@ -378,14 +390,26 @@ template <typename XT, bool WIDE, int S, bool CL> struct Place {
                 }
         }
     }
-    __device__ __forceinline__ void store(char *p, int s, F2 v) const {
-        One *at = reinterpret_cast<One *>(p + (off + s * st));
-        const Pair w = E::pack(v);
+    // Writes the rows of this thread's segment from `from`, where the threads of the warp have put
+    // them, to `p`: the way of copy, back.
+    __device__ __forceinline__ void write(char *p, const Pair *from, int left) const {
+        const int width = pairs();
         if constexpr (WIDE) {
-            __stcs(reinterpret_cast<Pair *>(at), w);
+            const char *src = reinterpret_cast<const char *>(from) + piece_slot;
+#pragma unroll
+            for (int r = 0; r < S; r += kPairs)
+                if (r < left - piece_row)
+                    __stcs(reinterpret_cast<uint4 *>(p + (piece_off + r * st)),
+                           *reinterpret_cast<const uint4 *>(src + r * width * sizeof(Pair)));
         } else {
-            __stcs(at, E::first(w));
-            if (on2) __stcs(at + 1, E::second(w));
+#pragma unroll
+            for (int s = 0; s < S; ++s)
+                if (on && s < left) {
+                    One *at = reinterpret_cast<One *>(p + (off + s * st));
+                    const Pair w = from[s * width + cp];
+                    __stcs(at, E::first(w));
+                    if (on2) __stcs(at + 1, E::second(w));
+                }
         }
     }
     // States of the pair, [B, N] float32.
@@ -400,12 +424,12 @@ template <typename XT, bool WIDE, int S, bool CL> struct Place {
     // put together when it begins (`starts`): threads side by side whose pairs are of one
     // sample read one flag each. Both are called by whole warps.
     __device__ __forceinline__ uint8_t ask(const ScanArgs &P, int t0) const {
-        const int l = (threadIdx.x & 31) % min(32, width), t = t0 + l;
+        const int l = (threadIdx.x & 31) % min(32, pairs()), t = t0 + l;
         return P.starts && l < S && t >= 0 && t < P.T ? P.starts[(int64_t)t * P.ft + sample * P.fb] : 0;
     }
     __device__ __forceinline__ uint32_t starts(const ScanArgs &P, int t0, uint8_t asked) const {
         if (!P.starts) return 0;
-        const int lane = threadIdx.x & 31, lane0 = lane - lane % min(32, width);
+        const int lane = threadIdx.x & 31, lane0 = lane - lane % min(32, pairs());
         if (one_sample) return __ballot_sync(0xffffffffu, asked) >> lane0 & ((1u << S) - 1);
         uint32_t f = 0;
         if (on)
@@ -416,14 +440,16 @@ template <typename XT, bool WIDE, int S, bool CL> struct Place {
     }
 };
 
-template <typename XT, bool WIDE, int S, int MQ, bool LOGIT, bool MIX, bool CL>
+template <typename XT, bool WIDE, int S, int QT, bool LOGIT, bool MIX, bool CL>
 __global__ void __launch_bounds__(256, 2) scan_forward_kernel(const ScanArgs P) {
     using E = Elem<XT>;
     using Pair = typename E::Pair;
     constexpr int kStages = kForwardStages<XT>;
     __shared__ ScanShared<CL> sh;
-    const Place<XT, WIDE, S, CL> me(P);
-    enter_cluster<CL>(sh, P, me.width);
+    const Place<XT, WIDE, S, QT, CL> me(P);
+    const int width = me.pairs(), Q = me.Q();
+    constexpr int MQ = QT ? QT : 8;                // most segments
+    enter_cluster<CL>(sh, P, width);
     F2 carry = me.state(P.h0);
     if (P.T == 0) {
         if (me.q == 0 && me.rank == 0 && P.last) me.put_state(P.last, carry);
@@ -435,7 +461,7 @@ __global__ void __launch_bounds__(256, 2) scan_forward_kernel(const ScanArgs P) 
     const char *px = static_cast<const char *>(P.x) + first, *pg = static_cast<const char *>(P.gate) + first;
     char *ph = static_cast<char *>(P.h) + first;
     extern __shared__ __align__(16) unsigned char dynamic[];
-    const int seg = segment_pairs<XT, S>(me.width), stage_pairs = 2 * P.Q * seg;
+    const int seg = segment_pairs<XT, S>(width), stage_pairs = 2 * Q * seg;
     Pair *slots = reinterpret_cast<Pair *>(dynamic) + me.q * seg;
     int t0 = me.rank * me.span + me.q * S;
     uint8_t asked = me.ask(P, t0), next_asked = 0;
@@ -443,7 +469,7 @@ __global__ void __launch_bounds__(256, 2) scan_forward_kernel(const ScanArgs P) 
     auto fetch = [&](int stage, int t) {
         Pair *to = slots + stage * stage_pairs;
         me.copy(to, pg, P.T - t);
-        me.copy(to + P.Q * seg, px, P.T - t);
+        me.copy(to + Q * seg, px, P.T - t);
         copies_issued();
         pg += hop;
         px += hop;
@@ -458,12 +484,13 @@ __global__ void __launch_bounds__(256, 2) scan_forward_kernel(const ScanArgs P) 
         // the usual segments: whole, without a start in any lane
         const bool plain = __all_sync(0xffffffffu, left >= S && !cut);
         copies_landed<kStages - 2>();
-        const Pair *gr = slots + stage * stage_pairs + me.cp, *xr = gr + P.Q * seg;
+        Pair *xs = slots + stage * stage_pairs + Q * seg, *xr = xs + me.cp;
+        const Pair *gr = xr - Q * seg;
 #pragma unroll
         for (int s = 0; s < S; ++s) {
             F2 na;
-            decay_of<LOGIT>(gr[s * me.width], a[s], na);
-            u[s] = E::unpack(xr[s * me.width]);
+            decay_of<LOGIT>(gr[s * width], a[s], na);
+            u[s] = E::unpack(xr[s * width]);
             if (MIX) u[s] = mul(u[s], na);
         }
         __syncwarp();                             // the stage before this one is free
@@ -490,39 +517,44 @@ __global__ void __launch_bounds__(256, 2) scan_forward_kernel(const ScanArgs P) 
         }
         t0 += me.step;
         asked = next_asked;
-        F2 h = fold<CL, LOGIT, MQ>(sh, P, me.q, me.cp, me.width, me.rank, pass, A, B, cut != 0, carry);
+        bool cuts;
+        F2 h = fold<CL, LOGIT, MQ>(sh, P, me.q, me.cp, width, me.rank, pass, A, B, cut != 0, carry, cuts);
         if (P.saved && t1 && t1 < P.T && t1 % kInterval == 0)
             me.put_state(P.saved + (int64_t)(t1 / kInterval - 1) * P.M, h);
-        if (plain && me.on) {
+        if (plain) {
 #pragma unroll
             for (int s = 0; s < S; ++s) {
                 h = fma(a[s], h, u[s]);
-                me.store(ph, s, h);
+                xr[s * width] = E::pack(h);
             }
-        } else if (me.on) {
+        } else {
 #pragma unroll
             for (int s = 0; s < S; ++s)
                 if (s < left) {
                     h = cut >> s & 1 ? u[s] : fma(a[s], h, u[s]);
-                    me.store(ph, s, h);
+                    xr[s * width] = E::pack(h);
                 }
         }
+        __syncwarp();
+        me.write(ph, xs, left);
         ph += hop;
         if (P.last && left > 0 && left <= S) me.put_state(P.last, h);
-        if (!CL && me.q == P.Q - 1) sh.carry[pass & 1][me.cp] = h;
+        if (!CL && me.q == Q - 1) sh.carry[pass & 1][me.cp] = h;
     }
     leave_cluster<CL>();
 }
 
-template <typename XT, bool WIDE, int S, int MQ, bool LOGIT, bool MIX, bool CL>
+template <typename XT, bool WIDE, int S, int QT, bool LOGIT, bool MIX, bool CL>
 __global__ void __launch_bounds__(256, 2) scan_backward_kernel(const ScanArgs P) {
     using E = Elem<XT>;
     using Pair = typename E::Pair;
     constexpr int kStages = kBackwardStages<XT>;
     __shared__ ScanShared<CL> sh;
     __shared__ F2 ends[2][256];                              // B of the segments' forward maps
-    const Place<XT, WIDE, S, CL> me(P);
-    enter_cluster<CL>(sh, P, me.width);
+    const Place<XT, WIDE, S, QT, CL> me(P);
+    const int width = me.pairs(), Q = me.Q();
+    constexpr int MQ = QT ? QT : 8;                // most segments
+    enter_cluster<CL>(sh, P, width);
     F2 carry = me.state(P.glast);
     if (P.T == 0) {
         if (me.q == 0 && me.rank == 0 && P.gh0) me.put_state(P.gh0, carry);
@@ -537,7 +569,7 @@ __global__ void __launch_bounds__(256, 2) scan_backward_kernel(const ScanArgs P)
     const char *pl = static_cast<const char *>(P.gh) + first;
     char *pgx = static_cast<char *>(P.gx) + first, *pgg = static_cast<char *>(P.gg) + first;
     extern __shared__ __align__(16) unsigned char dynamic[];
-    const int seg = segment_pairs<XT, S>(me.width), stage_pairs = 3 * P.Q * seg;
+    const int seg = segment_pairs<XT, S>(width), stage_pairs = 3 * Q * seg;
     Pair *slots = reinterpret_cast<Pair *>(dynamic) + me.q * seg;
     uint8_t asked = me.ask(P, t0);
     // h before the block's first step of the pass whose segment begins at t
@@ -550,8 +582,8 @@ __global__ void __launch_bounds__(256, 2) scan_backward_kernel(const ScanArgs P)
         if (t >= 0) {
             Pair *to = slots + stage * stage_pairs;
             me.copy(to, pg, P.T - t);
-            me.copy(to + P.Q * seg, px, P.T - t);
-            me.copy(to + 2 * P.Q * seg, pl, P.T - t);
+            me.copy(to + Q * seg, px, P.T - t);
+            me.copy(to + 2 * Q * seg, pl, P.T - t);
         }
         copies_issued();
         pg -= hop;
@@ -567,11 +599,12 @@ __global__ void __launch_bounds__(256, 2) scan_backward_kernel(const ScanArgs P)
         const int t1 = t0, left = P.T - t0;
         const bool plain = __all_sync(0xffffffffu, left >= S && !cut);
         copies_landed<kStages - 2>();
-        const Pair *gr = slots + stage * stage_pairs + me.cp, *xr = gr + P.Q * seg, *lr = xr + P.Q * seg;
-        auto gh_of = [&](int s) { return E::unpack(lr[s * me.width]); };
-        auto x_of = [&](int s) { return E::unpack(xr[s * me.width]); };
+        Pair *gs = slots + stage * stage_pairs, *xs = gs + Q * seg, *gr = gs + me.cp, *xr = xs + me.cp;
+        const Pair *lr = xr + Q * seg;
+        auto gh_of = [&](int s) { return E::unpack(lr[s * width]); };
+        auto x_of = [&](int s) { return E::unpack(xr[s * width]); };
 #pragma unroll
-        for (int s = 0; s < S; ++s) decay_of<LOGIT>(gr[s * me.width], a[s], na[s]);
+        for (int s = 0; s < S; ++s) decay_of<LOGIT>(gr[s * width], a[s], na[s]);
         // what the state takes up in step s
         auto input = [&](int s) {
             const F2 u = x_of(s);
@@ -602,15 +635,23 @@ __global__ void __launch_bounds__(256, 2) scan_backward_kernel(const ScanArgs P)
         t0 -= me.step;
         asked = me.ask(P, t0);
         start = begin(t0);
-        const int buf = pass & 1, from_end = P.Q - 1 - me.q;
-        ends[buf][me.q * me.width + me.cp] = B;
-        F2 mu = fold<CL, LOGIT, MQ>(sh, P, from_end, me.cp, me.width, CL ? P.CT - 1 - me.rank : 0, pass, A, L, cut != 0, carry);
+        const int buf = pass & 1, from_end = Q - 1 - me.q;
+        ends[buf][me.q * width + me.cp] = B;
+        bool cuts;
+        F2 mu = fold<CL, LOGIT, MQ>(sh, P, from_end, me.cp, width, CL ? P.CT - 1 - me.rank : 0, pass, A, L, cut != 0, carry, cuts);
+        auto step_over = [&](int i, bool with_cuts) {
+            const int at = (Q - 1 - i) * width + me.cp;
+            h = map_over(sh.map[buf][at].A, ends[buf][i * width + me.cp], with_cuts && sh.cut[buf][at], h);
+        };
+        if (cuts) {
 #pragma unroll
-        for (int i = 0; i < MQ - 1; ++i)
-            if (i < me.q) {
-                const int at = (P.Q - 1 - i) * me.width + me.cp;
-                h = map_over(sh.map[buf][at].A, ends[buf][i * me.width + me.cp], sh.cut[buf][at], h);
-            }
+            for (int i = 0; i < MQ - 1; ++i)
+                if (i < me.q) step_over(i, true);
+        } else {
+#pragma unroll
+            for (int i = 0; i < MQ - 1; ++i)
+                if (i < me.q) step_over(i, false);
+        }
         F2 before[S];
         // gradients of step s, from the state before it and mu after it
         auto gradients = [&](int s, F2 ga) {
@@ -618,11 +659,11 @@ __global__ void __launch_bounds__(256, 2) scan_backward_kernel(const ScanArgs P)
             if (MIX) ga = fma(x_of(s), both(-1.f), ga);
             ga = mul(ga, lam);
             if (LOGIT) ga = mul(ga, mul(a[s], na[s]));
-            me.store(pgx, s, MIX ? mul(lam, na[s]) : lam);
-            me.store(pgg, s, ga);
+            xr[s * width] = E::pack(MIX ? mul(lam, na[s]) : lam);
+            gr[s * width] = E::pack(ga);
             mu = mul(a[s], lam);
         };
-        if (plain && me.on) {
+        if (plain) {
 #pragma unroll
             for (int s = 0; s < S; ++s) {
                 before[s] = h;
@@ -630,7 +671,7 @@ __global__ void __launch_bounds__(256, 2) scan_backward_kernel(const ScanArgs P)
             }
 #pragma unroll
             for (int s = S - 1; s >= 0; --s) gradients(s, before[s]);
-        } else if (me.on) {
+        } else {
 #pragma unroll
             for (int s = 0; s < S; ++s)
                 if (s < left) {
@@ -645,6 +686,9 @@ __global__ void __launch_bounds__(256, 2) scan_backward_kernel(const ScanArgs P)
                     if (cut >> s & 1) mu = both(0.f);
                 }
         }
+        __syncwarp();
+        me.write(pgx, xs, left);
+        me.write(pgg, gs, left);
         pgx -= hop;
         pgg -= hop;
         if (t1 == 0 && P.gh0) me.put_state(P.gh0, mu);
@@ -791,14 +835,17 @@ cudaError_t launch(ScanArgs a, cudaStream_t s) {
         cfg.dynamicSmemBytes = smem;
         return cudaLaunchKernelEx(&cfg, kernel, a);
     };
+    // QT: the segments of a block where the steps fill an interval, 0 for shorter sequences
     if constexpr (FWD)
-        return a.CT > 1       ? start(scan_forward_kernel<XT, WIDE, S, W, LOGIT, MIX, true>)
-               : a.Q > kFullQ ? start(scan_forward_kernel<XT, WIDE, S, W, LOGIT, MIX, false>)
-                              : start(scan_forward_kernel<XT, WIDE, S, kFullQ, LOGIT, MIX, false>);
+        return a.CT > 1        ? start(scan_forward_kernel<XT, WIDE, S, W, LOGIT, MIX, true>)
+               : a.Q < kFullQ  ? start(scan_forward_kernel<XT, WIDE, S, 0, LOGIT, MIX, false>)
+               : a.Q == kFullQ ? start(scan_forward_kernel<XT, WIDE, S, kFullQ, LOGIT, MIX, false>)
+                               : start(scan_forward_kernel<XT, WIDE, S, W, LOGIT, MIX, false>);
     else
-        return a.CT > 1       ? start(scan_backward_kernel<XT, WIDE, S, W, LOGIT, MIX, true>)
-               : a.Q > kFullQ ? start(scan_backward_kernel<XT, WIDE, S, W, LOGIT, MIX, false>)
-                              : start(scan_backward_kernel<XT, WIDE, S, kFullQ, LOGIT, MIX, false>);
+        return a.CT > 1        ? start(scan_backward_kernel<XT, WIDE, S, W, LOGIT, MIX, true>)
+               : a.Q < kFullQ  ? start(scan_backward_kernel<XT, WIDE, S, 0, LOGIT, MIX, false>)
+               : a.Q == kFullQ ? start(scan_backward_kernel<XT, WIDE, S, kFullQ, LOGIT, MIX, false>)
+                               : start(scan_backward_kernel<XT, WIDE, S, W, LOGIT, MIX, false>);
 }
 
 // Rows are copied 16 bytes at a time where they are aligned to 16 bytes in every tensor.
