@@ -84,6 +84,7 @@ __global__ void __launch_bounds__(256) embed_forward_kernel(const T *table, cons
                                                             float scale) {
     using P = Piece<T, VEC>;
     using Raw = typename P::Raw;
+    pdl_begin();
     const int lane = threadIdx.x & 31;
     const int64_t task = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
     const int64_t i = task / chunks;
@@ -173,6 +174,7 @@ __device__ __forceinline__ int32_t prefix(int32_t v, int32_t *warps, int32_t &al
 // CLUSTER: the grid is one cluster.
 template <typename I, bool CLUSTER>
 __global__ void __launch_bounds__(kThreads) embed_index_kernel(const I *ids, Index x) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // embed_sum_kernel comes up
     namespace cg = cooperative_groups;
     auto meet = [] {
         if constexpr (CLUSTER) cg::this_cluster().sync();
@@ -363,6 +365,7 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(const T *grad, T *gtable
                                                         float scale) {
     using P = Piece<T, VEC>;
     using Raw = typename P::Raw;
+    pdl_begin();
     const int lane = threadIdx.x & 31;
     const int64_t task = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
     const int32_t tiles = x.n > kFew ? long_tiles(x) : 0;
@@ -442,6 +445,7 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(const T *grad, T *gtable
 // Joins the tiles of the long rows in order: blocks of 256 columns of one row.
 template <typename T>
 __global__ void __launch_bounds__(256) embed_join_kernel(T *gtable, Index x, int64_t D, float scale) {
+    pdl_begin();
     const int64_t d = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (d >= D) return;
     const int32_t longs = long_rows(x);
@@ -509,10 +513,8 @@ cudaError_t run_forward(const dendsn_embed_config &c, const void *table, const v
                         cudaStream_t s) {
     const int32_t nv = c.D / VEC, chunks = (nv + 32 * kAhead - 1) / (32 * kAhead);
     const int64_t blocks = (c.n * chunks + 7) / 8;
-    embed_forward_kernel<T, I, VEC><<<(unsigned)blocks, 256, 0, s>>>(
-        static_cast<const T *>(table), static_cast<const I *>(ids), static_cast<T *>(out), c.n, c.V, nv, chunks,
-        c.padding_id, c.scale);
-    return cudaGetLastError();
+    return seq_launch(embed_forward_kernel<T, I, VEC>, dim3((unsigned)blocks), 256, 0, s, 1, static_cast<const T *>(table),
+                      static_cast<const I *>(ids), static_cast<T *>(out), c.n, c.V, nv, chunks, c.padding_id, c.scale);
 }
 
 template <typename T, typename I, int VEC>
@@ -557,14 +559,15 @@ cudaError_t run_backward(const dendsn_embed_config &c, const Plan &pl, const voi
         if (e != cudaSuccess) return e;
         *launches += 1;
     }
-    embed_sum_kernel<T, VEC><<<(unsigned)(((c.V + kRowsOfWarp - 1) / kRowsOfWarp + pl.tiles + 7) / 8), 256, 0, s>>>(g, gt, x, c.D, nv, c.scale);
+    const int64_t warps = (c.V + kRowsOfWarp - 1) / kRowsOfWarp + pl.tiles;
+    cudaError_t e = seq_launch(embed_sum_kernel<T, VEC>, dim3((unsigned)((warps + 7) / 8)), 256, 0, s, 1, g, gt, x, c.D, nv, c.scale);
     *launches += 1;
-    if (pl.longs > 0) {
+    if (e == cudaSuccess && pl.longs > 0) {
         const dim3 grid((unsigned)((c.D + 255) / 256), (unsigned)std::min<int64_t>(pl.longs, 1024));
-        embed_join_kernel<T><<<grid, 256, 0, s>>>(gt, x, c.D, c.scale);
+        e = seq_launch(embed_join_kernel<T>, grid, 256, 0, s, 1, gt, x, c.D, c.scale);
         *launches += 1;
     }
-    return cudaGetLastError();
+    return e;
 }
 
 // Whether rows of D elements of every tensor can be taken 16 bytes at a time.

@@ -445,6 +445,7 @@ __global__ void __launch_bounds__(256, 2) scan_forward_kernel(const ScanArgs P) 
     using E = Elem<XT>;
     using Pair = typename E::Pair;
     constexpr int kStages = kForwardStages<XT>;
+    pdl_begin();
     __shared__ ScanShared<CL> sh;
     const Place<XT, WIDE, S, QT, CL> me(P);
     const int width = me.pairs(), Q = me.Q();
@@ -549,6 +550,7 @@ __global__ void __launch_bounds__(256, 2) scan_backward_kernel(const ScanArgs P)
     using E = Elem<XT>;
     using Pair = typename E::Pair;
     constexpr int kStages = kBackwardStages<XT>;
+    pdl_begin();
     __shared__ ScanShared<CL> sh;
     __shared__ F2 ends[2][256];                              // B of the segments' forward maps
     const Place<XT, WIDE, S, QT, CL> me(P);
@@ -703,6 +705,7 @@ template <typename XT, bool LOGIT, bool MIX>
 __global__ void __launch_bounds__(128) scan_forward_far_kernel(const ScanArgs P) {
     using E = Elem<XT>;
     using One = typename E::One;
+    pdl_begin();
     const int64_t m = (int64_t)blockIdx.x * 128 + threadIdx.x;
     if (m >= P.M) return;
     const int64_t b = m / P.N, off = b * P.sb + m % P.N;
@@ -724,6 +727,7 @@ template <typename XT, bool LOGIT, bool MIX>
 __global__ void __launch_bounds__(128) scan_backward_far_kernel(const ScanArgs P) {
     using E = Elem<XT>;
     using One = typename E::One;
+    pdl_begin();
     const int64_t m = (int64_t)blockIdx.x * 128 + threadIdx.x;
     if (m >= P.M) return;
     const int64_t b = m / P.N, off = b * P.sb + m % P.N;
@@ -813,27 +817,15 @@ cudaError_t launch(ScanArgs a, cudaStream_t s) {
     const int64_t reach = ((256 / a.Q - 1) / a.PN + 1) * a.sb + a.N + (int64_t)a.Q * S * a.st;
     if (reach * (int64_t)sizeof(XT) > UINT32_MAX) {
         const unsigned blocks = (unsigned)((a.M + 127) / 128);
-        if constexpr (FWD) scan_forward_far_kernel<XT, LOGIT, MIX><<<blocks, 128, 0, s>>>(a);
-        else scan_backward_far_kernel<XT, LOGIT, MIX><<<blocks, 128, 0, s>>>(a);
-        return cudaGetLastError();
+        if constexpr (FWD) return seq_launch(scan_forward_far_kernel<XT, LOGIT, MIX>, dim3(blocks), 128, 0, s, 1, a);
+        else return seq_launch(scan_backward_far_kernel<XT, LOGIT, MIX>, dim3(blocks), 128, 0, s, 1, a);
     }
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(groups() * a.CT));
-    cfg.blockDim = dim3(256);
-    cfg.stream = s;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = (unsigned)a.CT;
-    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = a.CT > 1 ? 1 : 0;
     const size_t smem = (size_t)(FWD ? 2 * kForwardStages<XT> : 3 * kBackwardStages<XT>) * a.Q *
                         segment_pairs<XT, S>(256 / a.Q) * sizeof(typename Elem<XT>::Pair);
     auto start = [&](auto kernel) {
         cudaError_t e = smem <= 16384 ? cudaSuccess : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
-        cfg.dynamicSmemBytes = smem;
-        return cudaLaunchKernelEx(&cfg, kernel, a);
+        return seq_launch(kernel, dim3((unsigned)(groups() * a.CT)), 256, smem, s, a.CT, a);
     };
     // QT: the segments of a block where the steps fill an interval, 0 for shorter sequences
     if constexpr (FWD)

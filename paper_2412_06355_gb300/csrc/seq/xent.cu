@@ -97,6 +97,7 @@ template <typename I>
 __global__ void __launch_bounds__(1024) xent_rows_kernel(Rows R, const void *labels, int32_t M, int32_t V,
                                                          int64_t ignore, float *loss, float *lse_out,
                                                          const float *lse, const float *gloss) {
+    pdl_begin();
     constexpr int kEach = 8;                                  // consecutive rows of a thread
     __shared__ int warps[32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -158,6 +159,7 @@ template <typename T, bool WIDE>
 __global__ void __launch_bounds__(256) xent_pack_kernel(const T *from, __nv_bfloat16 *to, const int32_t *index,
                                                         const Ctl *ctl, int64_t rows, int32_t D, int32_t Dp,
                                                         int64_t plane) {
+    pdl_begin();
     const int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
     if (r >= rows) return;
     int64_t src = r;
@@ -265,10 +267,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     const uint32_t full = bars, empty = bars + 8 * kStages, acc_full = bars + 16 * kStages, acc_empty = acc_full + 16;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = tc::cluster_rank();
-    const int rows = g.ctl->rows;
-    const int mt = MODE == WEIGHT ? g.mt : (rows + kTileM - 1) / kTileM;
-    const int kb = MODE == WEIGHT ? (rows + kTileK - 1) / kTileK : g.kb;
-    const int64_t items = (int64_t)mt * g.nt * g.splits;
     const int64_t first = blockIdx.x / 2, stride = gridDim.x / 2;
 
     if (warp == 0 && lane == 0) {
@@ -291,6 +289,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     tc::fence_after_sync();
     const uint32_t tmem = tmem_base;
     bool ok = true;
+    pdl_begin();                                              // nothing before this reads or writes memory
+    const int rows = g.ctl->rows;
+    const int mt = MODE == WEIGHT ? g.mt : (rows + kTileM - 1) / kTileM;
+    const int kb = MODE == WEIGHT ? (rows + kTileK - 1) / kTileK : g.kb;
+    const int64_t items = (int64_t)mt * g.nt * g.splits;
 
     if (warp == 0 && lane == 0) {                             // copies, in both blocks
         const uint32_t full0 = tc::in_block(full, 0);
@@ -532,6 +535,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 // eight of them in flight.
 __global__ void __launch_bounds__(1024) xent_join_kernel(Rows R, const float2 *part, int32_t parts, int64_t Mp,
                                                          float *loss, float *lse) {
+    pdl_begin();
     __shared__ float2 sh[32][33];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int r = blockIdx.x * 32 + lane;
@@ -574,6 +578,7 @@ __global__ void __launch_bounds__(1024) xent_join_kernel(Rows R, const float2 *p
 template <typename T>
 __global__ void __launch_bounds__(256) xent_hidden_kernel(Rows R, const float *sum, T *gh, int64_t M, int64_t Mp,
                                                           int32_t D, int32_t Dq, int32_t splits) {
+    pdl_begin();
     const int32_t quads = (D + 3) / 4;
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, r = i / quads;
     if (r >= M) return;
@@ -745,8 +750,7 @@ cudaError_t product(const CUtensorMap &a, const CUtensorMap &b, const Gemm &g, i
                                          (int)kSmem);
     if (e != cudaSuccess) return e;
     const unsigned clusters = (unsigned)std::max<int64_t>(1, std::min<int64_t>(items, kClusters));
-    xent_product_kernel<MODE, T><<<2 * clusters, kThreads, kSmem, s>>>(a, b, g);
-    return cudaGetLastError();
+    return seq_launch(xent_product_kernel<MODE, T>, dim3(2 * clusters), kThreads, kSmem, s, 1, a, b, g);
 }
 
 struct Call {
@@ -778,35 +782,36 @@ cudaError_t operands(Call &c, const void *hidden, const void *weight, const __nv
     const int D = c.cfg->D;
     auto pack = [&](const void *from, size_t to, const int32_t *index, int64_t rows) {
         const T *f = static_cast<const T *>(from);
+        cudaError_t e = cudaSuccess;
         const unsigned blocks = (unsigned)((rows + 7) / 8);
         if (D * sizeof(T) % 16 == 0 && seq_aligned(from, 16))
-            xent_pack_kernel<T, true><<<blocks, 256, 0, c.s>>>(f, c.at<__nv_bfloat16>(to), index, c.at<Ctl>(0), rows, D, p.Dp,
-                                                               rows * p.Dp);
+            e = seq_launch(xent_pack_kernel<T, true>, dim3(blocks), 256, 0, c.s, 1, f, c.at<__nv_bfloat16>(to), index,
+                           c.at<Ctl>(0), rows, D, p.Dp, rows * p.Dp);
         else
-            xent_pack_kernel<T, false><<<blocks, 256, 0, c.s>>>(f, c.at<__nv_bfloat16>(to), index, c.at<Ctl>(0), rows, D, p.Dp,
-                                                                rows * p.Dp);
+            e = seq_launch(xent_pack_kernel<T, false>, dim3(blocks), 256, 0, c.s, 1, f, c.at<__nv_bfloat16>(to), index,
+                           c.at<Ctl>(0), rows, D, p.Dp, rows * p.Dp);
         c.launches += 1;
+        return e;
     };
-    pack(hidden, p.H, c.at<int32_t>(p.index), p.Mp);
+    cudaError_t e = pack(hidden, p.H, c.at<int32_t>(p.index), p.Mp);
     if (sizeof(T) == 2 && D % 8 == 0 && seq_aligned(weight, 16)) {
         *w = static_cast<const __nv_bfloat16 *>(weight);
         *w_pitch = D;
         *w_inner = D;
     } else {
-        pack(weight, p.W, nullptr, c.cfg->V);
+        if (e == cudaSuccess) e = pack(weight, p.W, nullptr, c.cfg->V);
         *w = c.at<__nv_bfloat16>(p.W);
         *w_pitch = p.Dp;
         *w_inner = p.Dp;
     }
-    return cudaGetLastError();
+    return e;
 }
 
 template <typename I>
 cudaError_t find_rows(Call &c, const void *labels, float *loss, float *lse_out, const float *lse, const float *gloss) {
-    xent_rows_kernel<I><<<1, 1024, 0, c.s>>>(rows_of(c), labels, c.cfg->M, c.cfg->V, c.cfg->ignore_index, loss, lse_out,
-                                             lse, gloss);
     c.launches += 1;
-    return cudaGetLastError();
+    return seq_launch(xent_rows_kernel<I>, dim3(1), 1024, 0, c.s, 1, rows_of(c), labels, c.cfg->M, c.cfg->V,
+                      c.cfg->ignore_index, loss, lse_out, lse, gloss);
 }
 
 template <typename T>
@@ -839,10 +844,9 @@ dendsn_status run_forward(Call &c, const void *hidden, const void *weight, const
         c.launches += 1;
     }
     if (e == cudaSuccess) {
-        xent_join_kernel<<<(unsigned)((p.Mp + 31) / 32), 1024, 0, c.s>>>(rows_of(c), c.at<float2>(p.part), 2 * p.nt, p.Mp,
-                                                                        loss, lse);
+        e = seq_launch(xent_join_kernel, dim3((unsigned)((p.Mp + 31) / 32)), 1024, 0, c.s, 1, rows_of(c), c.at<float2>(p.part),
+                       2 * p.nt, p.Mp, loss, lse);
         c.launches += 1;
-        e = cudaGetLastError();
     }
     if (e != cudaSuccess) return seq_fail(DENDSN_ERR_CUDA, "xent forward launch failed: %s", cudaGetErrorString(e));
     return DENDSN_OK;
@@ -909,10 +913,10 @@ dendsn_status run_backward(Call &c, const void *hidden, const void *weight, cons
         c.launches += 3;
     }
     if (e == cudaSuccess) {
-        xent_hidden_kernel<T><<<(unsigned)(((int64_t)c.cfg->M * ((D + 3) / 4) + 255) / 256), 256, 0, c.s>>>(
-            rows_of(c), c.at<float>(p.sum), static_cast<T *>(gh), c.cfg->M, p.Mp, D, p.Dq, p.splits);
+        const int64_t threads = (int64_t)c.cfg->M * ((D + 3) / 4);
+        e = seq_launch(xent_hidden_kernel<T>, dim3((unsigned)((threads + 255) / 256)), 256, 0, c.s, 1, rows_of(c),
+                       c.at<float>(p.sum), static_cast<T *>(gh), c.cfg->M, p.Mp, D, p.Dq, p.splits);
         c.launches += 1;
-        e = cudaGetLastError();
     }
     if (e != cudaSuccess) return seq_fail(DENDSN_ERR_CUDA, "xent backward launch failed: %s", cudaGetErrorString(e));
     return DENDSN_OK;
