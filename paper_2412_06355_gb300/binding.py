@@ -527,10 +527,15 @@ def scan_backward(cfg, x, gate, grad_h, starts=None, h0=None, grad_last=None, sa
 
 def dendsn_xent_workspace_size(cfg: dendsn_xent_config):
     """(forward_bytes, backward_bytes) of scratch."""
-    f, b = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    return _xent_scratch(cfg, False), _xent_scratch(cfg, True)
+
+
+def _xent_scratch(cfg, backward) -> int:
+    b = ctypes.c_size_t(0)
+    where = (None, ctypes.byref(b)) if backward else (ctypes.byref(b), None)
     _check("dendsn_xent_workspace_size",
-           load().dendsn_xent_workspace_size(ctypes.byref(cfg), ctypes.byref(f), ctypes.byref(b)))
-    return int(f.value), int(b.value)
+           load().dendsn_xent_workspace_size(ctypes.byref(cfg), *where))
+    return b.value
 
 
 def _xent_expect(cfg, hidden, weight, labels, **rows):
@@ -544,7 +549,7 @@ def _xent_expect(cfg, hidden, weight, labels, **rows):
 
 def dendsn_xent_forward(cfg, hidden, weight, labels, loss, lse, scratch, stream=None):
     _xent_expect(cfg, hidden, weight, labels, loss=loss, lse=lse)
-    _bytes("scratch", scratch, dendsn_xent_workspace_size(cfg)[0])
+    _bytes("scratch", scratch, _xent_scratch(cfg, False))
     _check("dendsn_xent_forward", load().dendsn_xent_forward(
         ctypes.byref(cfg), _ptr(hidden), _ptr(weight), _ptr(labels), _ptr(loss), _ptr(lse),
         _ptr(scratch), _stream(stream)))
@@ -555,7 +560,7 @@ def dendsn_xent_backward(cfg, hidden, weight, labels, lse, grad_loss, grad_hidde
     _xent_expect(cfg, hidden, weight, labels, lse=lse, grad_loss=grad_loss)
     _expect("grad_hidden", grad_hidden, (cfg.M, cfg.D), hidden.dtype)
     _expect("grad_weight", grad_weight, (cfg.V, cfg.D), hidden.dtype)
-    _bytes("scratch", scratch, dendsn_xent_workspace_size(cfg)[1])
+    _bytes("scratch", scratch, _xent_scratch(cfg, True))
     _check("dendsn_xent_backward", load().dendsn_xent_backward(
         ctypes.byref(cfg), _ptr(hidden), _ptr(weight), _ptr(labels), _ptr(lse), _ptr(grad_loss),
         _ptr(grad_hidden), _ptr(grad_weight), _ptr(scratch), _stream(stream)))
@@ -564,7 +569,7 @@ def dendsn_xent_backward(cfg, hidden, weight, labels, lse, grad_loss, grad_hidde
 def xent_forward(cfg, hidden, weight, labels, scratch=None, stream=None):
     """Allocating cross entropy of hidden [M, D] read out by weight [V, D]: (loss [M], lse [M])."""
     if scratch is None:
-        scratch = _scratch(dendsn_xent_workspace_size(cfg)[0], hidden.device)
+        scratch = _scratch(_xent_scratch(cfg, False), hidden.device)
     loss = torch.empty((cfg.M,), dtype=torch.float32, device=hidden.device)
     lse = torch.empty_like(loss)
     dendsn_xent_forward(cfg, hidden, weight, labels, loss, lse, scratch, stream)
@@ -574,7 +579,7 @@ def xent_forward(cfg, hidden, weight, labels, scratch=None, stream=None):
 def xent_backward(cfg, hidden, weight, labels, lse, grad_loss, scratch=None, stream=None):
     """Allocating backward. Returns dict ghidden [M, D], gweight [V, D] in hidden's dtype."""
     if scratch is None:
-        scratch = _scratch(dendsn_xent_workspace_size(cfg)[1], hidden.device)
+        scratch = _scratch(_xent_scratch(cfg, True), hidden.device)
     out = dict(ghidden=torch.empty_like(hidden), gweight=torch.empty_like(weight))
     dendsn_xent_backward(cfg, hidden, weight, labels, lse, grad_loss, out["ghidden"],
                          out["gweight"], scratch, stream)

@@ -152,27 +152,16 @@ __global__ void __launch_bounds__(1024) xent_rows_kernel(Rows R, const void *lab
     }
 }
 
-// Copies rows of D elements to rows of Dp bfloat16 elements with zeros behind, in three planes
-// for float32; a thread takes 8 elements. index: the row to copy for each place (negative:
-// zeros), or null: the same row. WIDE: rows can be read 16 bytes at a time.
+// Copies a row of D elements (none: zeros) to Dp bfloat16 elements with zeros behind, in three
+// planes for float32; a thread of the warp takes 8 elements at a time. WIDE: rows can be read 16
+// bytes at a time.
 template <typename T, bool WIDE>
-__global__ void __launch_bounds__(256) xent_pack_kernel(const T *from, __nv_bfloat16 *to, const int32_t *index,
-                                                        const Ctl *ctl, int64_t rows, int32_t D, int32_t Dp,
-                                                        int64_t plane) {
-    pdl_begin();
-    const int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    if (r >= rows) return;
-    int64_t src = r;
-    if (index) {
-        if (r >= (ctl->rows + kTileM - 1) / kTileM * kTileM) return;
-        src = index[r];
-    }
-    const T *p = from + src * D;
-    for (int32_t d = (threadIdx.x & 31) * 8; d < Dp; d += 256) {
-        uint4 *q = reinterpret_cast<uint4 *>(to + r * Dp + d);
+__device__ __forceinline__ void pack_row(const T *p, __nv_bfloat16 *to, int lane, int32_t D, int32_t Dp, int64_t plane) {
+    for (int32_t d = lane * 8; d < Dp; d += 256) {
+        uint4 *q = reinterpret_cast<uint4 *>(to + d);
         if constexpr (sizeof(T) == 2) {
             uint4 w = make_uint4(0, 0, 0, 0);
-            if (src >= 0) {
+            if (p) {
                 if (WIDE) {
                     if (d < D) w = __ldg(reinterpret_cast<const uint4 *>(p + d));
                 } else {
@@ -185,7 +174,7 @@ __global__ void __launch_bounds__(256) xent_pack_kernel(const T *from, __nv_bflo
             *q = w;
         } else {
             float e[8] = {};
-            if (src >= 0) {
+            if (p) {
 #pragma unroll
                 for (int h = 0; h < 8; h += 4) {
                     if (WIDE) {
@@ -215,6 +204,91 @@ __global__ void __launch_bounds__(256) xent_pack_kernel(const T *from, __nv_bflo
             for (int t = 0; t < 3; ++t) q[t * (plane / 8)] = make_uint4(w[t][0], w[t][1], w[t][2], w[t][3]);
         }
     }
+}
+
+// index: the row to copy for each place (negative: zeros), or null: the same row.
+template <typename T, bool WIDE>
+__global__ void __launch_bounds__(256) xent_pack_kernel(const T *from, __nv_bfloat16 *to, const int32_t *index,
+                                                        const Ctl *ctl, int64_t rows, int32_t D, int32_t Dp,
+                                                        int64_t plane) {
+    pdl_begin();
+    const int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (r >= rows) return;
+    int64_t src = r;
+    if (index) {
+        if (r >= (ctl->rows + kTileM - 1) / kTileM * kTileM) return;
+        src = index[r];
+    }
+    pack_row<T, WIDE>(src >= 0 ? from + src * D : nullptr, to + r * Dp, threadIdx.x & 31, D, Dp, plane);
+}
+
+// xent_rows and xent_pack of the hidden rows in one launch, for up to kFewRows rows: every block
+// lists the rows for itself, block 0 writes the list down, and each warp copies one place.
+constexpr int kFewRows = 1024;
+
+template <typename T, typename I, bool WIDE>
+__global__ void __launch_bounds__(256) xent_rows_pack_kernel(Rows R, const void *labels, int32_t M, int32_t V,
+                                                             int64_t ignore, float *loss, float *lse_out,
+                                                             const float *lse, const float *gloss, const T *from,
+                                                             __nv_bfloat16 *to, int32_t D, int32_t Dp, int64_t plane) {
+    pdl_begin();
+    constexpr int kEach = kFewRows / 256;
+    __shared__ int warps[8], list[kFewRows];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r0 = threadIdx.x * kEach;
+    int y[kEach], mine = 0;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        y[j] = r0 + j < M ? label_of<I>(labels, r0 + j, V, ignore) : kIgnored;
+        mine += y[j] >= 0;
+    }
+    int incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += v;
+    }
+    if (lane == 31) warps[warp] = incl;
+    __syncthreads();
+    int at = incl - mine, rows = 0;
+    for (int w = 0; w < 8; ++w) {
+        if (w < warp) at += warps[w];
+        rows += warps[w];
+    }
+    const int end = (rows + kTileM - 1) / kTileM * kTileM;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        const int r = r0 + j;
+        if (r >= M) break;
+        if (y[j] >= 0) list[at] = r;
+        if (blockIdx.x == 0) {
+            R.where[r] = y[j] >= 0 ? at : y[j];
+            if (y[j] >= 0) {
+                R.index[at] = r;
+                R.label[at] = y[j];
+                if (lse) {
+                    R.lse[at] = lse[r];
+                    R.weight[at] = gloss[r];
+                }
+            } else if (loss) {
+                loss[r] = lse_out[r] = y[j] == kIgnored ? 0.f : nan_f();
+            }
+        }
+        at += y[j] >= 0;
+    }
+    if (blockIdx.x == 0) {
+        for (int i = rows + threadIdx.x; i < end; i += 256) {
+            R.index[i] = R.label[i] = -1;
+            if (lse) R.lse[i] = R.weight[i] = 0.f;
+        }
+        if (threadIdx.x == 0) {
+            R.ctl->rows = rows;
+            R.ctl->failed = 0;
+        }
+    }
+    __syncthreads();
+    const int place = blockIdx.x * 8 + warp;
+    if (place < end)
+        pack_row<T, WIDE>(place < rows ? from + (int64_t)list[place] * D : nullptr, to + (int64_t)place * Dp, lane, D, Dp, plane);
 }
 
 // ------------------------------------------------------------------ the products
@@ -669,7 +743,7 @@ void choose_pieces(Plan *pl) {
     }
 }
 
-dendsn_status make_plan(const dendsn_xent_config *cfg, Plan *pl) {
+dendsn_status make_plan(const dendsn_xent_config *cfg, bool backward, Plan *pl) {
     if (!cfg) return seq_fail(DENDSN_ERR_INVALID_ARG, "cfg is NULL");
     if (cfg->M < 0 || cfg->V < 1 || cfg->D < 1)
         return seq_fail(DENDSN_ERR_INVALID_ARG, "bad size (M=%d V=%d D=%d)", cfg->M, cfg->V, cfg->D);
@@ -687,7 +761,7 @@ dendsn_status make_plan(const dendsn_xent_config *cfg, Plan *pl) {
     p.mt = (int32_t)(p.Mp / kTileM);
     p.nt = up(cfg->V, kTileN) / kTileN;
     p.dt = p.Dq / kTileN;
-    choose_pieces(&p);
+    if (backward) choose_pieces(&p);
     size_t at = sizeof(Ctl);
     auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -704,6 +778,7 @@ dendsn_status make_plan(const dendsn_xent_config *cfg, Plan *pl) {
     p.picked = take(p.Mp * 4);
     p.part = take((size_t)2 * p.nt * p.Mp * 8);
     p.fwd = at;
+    if (!backward) return DENDSN_OK;
     at = shared;
     p.lse = take(p.Mp * 4);
     p.weight = take(p.Mp * 4);
@@ -774,32 +849,45 @@ Rows rows_of(const Call &c) {
     return r;
 }
 
-// The operands both passes share: packed rows, and the weights packed or as they are.
-template <typename T>
-cudaError_t operands(Call &c, const void *hidden, const void *weight, const __nv_bfloat16 **w, int32_t *w_pitch,
-                     int64_t *w_inner) {
+// Per-row inputs and outputs that the list of rows takes along.
+struct PerRow {
+    const void *labels;
+    float *loss, *lse_out;        // of the forward: written for rows that do not take part
+    const float *lse, *gloss;     // of the backward
+};
+
+// The operands both passes share: the rows that take part, packed, and the weights packed or as
+// they are.
+template <typename T, typename I>
+cudaError_t operands(Call &c, const void *hidden, const void *weight, const PerRow &r, const __nv_bfloat16 **w,
+                     int32_t *w_pitch, int64_t *w_inner) {
     const Plan &p = c.pl;
-    const int D = c.cfg->D;
+    const int D = c.cfg->D, M = c.cfg->M, V = c.cfg->V;
+    const int64_t ignore = c.cfg->ignore_index;
+    auto is_wide = [&](const void *from) { return D * sizeof(T) % 16 == 0 && seq_aligned(from, 16); };
     auto pack = [&](const void *from, size_t to, const int32_t *index, int64_t rows) {
-        const T *f = static_cast<const T *>(from);
-        cudaError_t e = cudaSuccess;
-        const unsigned blocks = (unsigned)((rows + 7) / 8);
-        if (D * sizeof(T) % 16 == 0 && seq_aligned(from, 16))
-            e = seq_launch(xent_pack_kernel<T, true>, dim3(blocks), 256, 0, c.s, 1, f, c.at<__nv_bfloat16>(to), index,
-                           c.at<Ctl>(0), rows, D, p.Dp, rows * p.Dp);
-        else
-            e = seq_launch(xent_pack_kernel<T, false>, dim3(blocks), 256, 0, c.s, 1, f, c.at<__nv_bfloat16>(to), index,
-                           c.at<Ctl>(0), rows, D, p.Dp, rows * p.Dp);
+        const auto kernel = is_wide(from) ? xent_pack_kernel<T, true> : xent_pack_kernel<T, false>;
         c.launches += 1;
-        return e;
+        return seq_launch(kernel, dim3((unsigned)((rows + 7) / 8)), 256, 0, c.s, 1, static_cast<const T *>(from),
+                          c.at<__nv_bfloat16>(to), index, c.at<Ctl>(0), rows, D, p.Dp, rows * p.Dp);
     };
-    cudaError_t e = pack(hidden, p.H, c.at<int32_t>(p.index), p.Mp);
+    cudaError_t e;
+    c.launches += 1;
+    if (M <= kFewRows) {
+        const auto kernel = is_wide(hidden) ? xent_rows_pack_kernel<T, I, true> : xent_rows_pack_kernel<T, I, false>;
+        e = seq_launch(kernel, dim3((unsigned)(p.Mp / 8)), 256, 0, c.s, 1, rows_of(c), r.labels, M, V, ignore, r.loss, r.lse_out,
+                       r.lse, r.gloss, static_cast<const T *>(hidden), c.at<__nv_bfloat16>(p.H), D, p.Dp, p.Mp * p.Dp);
+    } else {
+        e = seq_launch(xent_rows_kernel<I>, dim3(1), 1024, 0, c.s, 1, rows_of(c), r.labels, M, V, ignore, r.loss, r.lse_out,
+                       r.lse, r.gloss);
+        if (e == cudaSuccess) e = pack(hidden, p.H, c.at<int32_t>(p.index), p.Mp);
+    }
     if (sizeof(T) == 2 && D % 8 == 0 && seq_aligned(weight, 16)) {
         *w = static_cast<const __nv_bfloat16 *>(weight);
         *w_pitch = D;
         *w_inner = D;
     } else {
-        if (e == cudaSuccess) e = pack(weight, p.W, nullptr, c.cfg->V);
+        if (e == cudaSuccess) e = pack(weight, p.W, nullptr, V);
         *w = c.at<__nv_bfloat16>(p.W);
         *w_pitch = p.Dp;
         *w_inner = p.Dp;
@@ -807,11 +895,11 @@ cudaError_t operands(Call &c, const void *hidden, const void *weight, const __nv
     return e;
 }
 
-template <typename I>
-cudaError_t find_rows(Call &c, const void *labels, float *loss, float *lse_out, const float *lse, const float *gloss) {
-    c.launches += 1;
-    return seq_launch(xent_rows_kernel<I>, dim3(1), 1024, 0, c.s, 1, rows_of(c), labels, c.cfg->M, c.cfg->V,
-                      c.cfg->ignore_index, loss, lse_out, lse, gloss);
+template <typename T>
+cudaError_t operands(Call &c, const void *hidden, const void *weight, const PerRow &r, const __nv_bfloat16 **w,
+                     int32_t *w_pitch, int64_t *w_inner) {
+    return c.cfg->labels_dtype == DENDSN_I64 ? operands<T, int64_t>(c, hidden, weight, r, w, w_pitch, w_inner)
+                                             : operands<T, int32_t>(c, hidden, weight, r, w, w_pitch, w_inner);
 }
 
 template <typename T>
@@ -821,9 +909,7 @@ dendsn_status run_forward(Call &c, const void *hidden, const void *weight, const
     const __nv_bfloat16 *w = nullptr;
     int32_t w_pitch = 0;
     int64_t w_inner = 0;
-    cudaError_t e = c.cfg->labels_dtype == DENDSN_I64 ? find_rows<int64_t>(c, labels, loss, lse, nullptr, nullptr)
-                                                      : find_rows<int32_t>(c, labels, loss, lse, nullptr, nullptr);
-    if (e == cudaSuccess) e = operands<T>(c, hidden, weight, &w, &w_pitch, &w_inner);
+    cudaError_t e = operands<T>(c, hidden, weight, PerRow{labels, loss, lse, nullptr, nullptr}, &w, &w_pitch, &w_inner);
     CUtensorMap a, b;
     if (e == cudaSuccess) {
         if (!make_map(&a, c.at<void>(p.H), p.Dp, p.Mp, p.Dp, p.terms, p.Mp * p.Dp, 128) ||
@@ -860,9 +946,7 @@ dendsn_status run_backward(Call &c, const void *hidden, const void *weight, cons
     const __nv_bfloat16 *w = nullptr;
     int32_t w_pitch = 0;
     int64_t w_inner = 0;
-    cudaError_t e = c.cfg->labels_dtype == DENDSN_I64 ? find_rows<int64_t>(c, labels, nullptr, nullptr, lse, gloss)
-                                                      : find_rows<int32_t>(c, labels, nullptr, nullptr, lse, gloss);
-    if (e == cudaSuccess) e = operands<T>(c, hidden, weight, &w, &w_pitch, &w_inner);
+    cudaError_t e = operands<T>(c, hidden, weight, PerRow{labels, nullptr, nullptr, lse, gloss}, &w, &w_pitch, &w_inner);
     CUtensorMap h_rows, h_cols, w_rows, w_cols;
     const __nv_bfloat16 *H = c.at<__nv_bfloat16>(p.H);
     __nv_bfloat16 *G = c.at<__nv_bfloat16>(p.G);
@@ -932,7 +1016,7 @@ extern "C" {
 dendsn_status dendsn_xent_workspace_size(const dendsn_xent_config *cfg, size_t *forward_bytes,
                                          size_t *backward_bytes) {
     Plan pl;
-    dendsn_status st = make_plan(cfg, &pl);
+    dendsn_status st = make_plan(cfg, backward_bytes != nullptr, &pl);
     if (st != DENDSN_OK) return st;
     if (forward_bytes) *forward_bytes = pl.fwd;
     if (backward_bytes) *backward_bytes = pl.bwd;
@@ -943,7 +1027,7 @@ dendsn_status dendsn_xent_forward(const dendsn_xent_config *cfg, const void *hid
                                   const void *labels, float *loss, float *lse, void *scratch,
                                   void *stream) {
     Call c{};
-    dendsn_status st = make_plan(cfg, &c.pl);
+    dendsn_status st = make_plan(cfg, false, &c.pl);
     if (st != DENDSN_OK) return st;
     if (cfg->M == 0) return DENDSN_OK;
     if (!hidden || !weight || !labels || !loss || !lse)
@@ -967,7 +1051,7 @@ dendsn_status dendsn_xent_backward(const dendsn_xent_config *cfg, const void *hi
                                    const void *labels, const float *lse, const float *grad_loss,
                                    void *grad_hidden, void *grad_weight, void *scratch, void *stream) {
     Call c{};
-    dendsn_status st = make_plan(cfg, &c.pl);
+    dendsn_status st = make_plan(cfg, true, &c.pl);
     if (st != DENDSN_OK) return st;
     if (!grad_weight || !weight) return seq_fail(DENDSN_ERR_INVALID_ARG, "weight or grad_weight is NULL");
     if (cfg->M > 0 && (!hidden || !labels || !lse || !grad_loss || !grad_hidden))
