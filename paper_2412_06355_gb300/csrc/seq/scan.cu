@@ -26,6 +26,7 @@
 
 #include <algorithm>
 
+#include "pairs.cuh"
 #include "seq_common.h"
 
 namespace dendsn {
@@ -51,43 +52,6 @@ struct ScanArgs {
     int32_t PN;                   // pairs of a sample
     int64_t pairs;                // in all
 };
-
-// ------------------------------------------------------------------ pairs
-// Two float32 values in one 64-bit register, as the paired instructions take them.
-struct F2 {
-    uint64_t v;
-    F2() = default;
-    __device__ __forceinline__ explicit F2(uint64_t raw) : v(raw) {}
-    __device__ __forceinline__ F2(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
-    __device__ __forceinline__ float x() const { return __uint_as_float((uint32_t)v); }
-    __device__ __forceinline__ float y() const { return __uint_as_float((uint32_t)(v >> 32)); }
-};
-__device__ __forceinline__ F2 both(float v) { return F2(v, v); }
-__device__ __forceinline__ F2 mul(F2 a, F2 b) {
-    F2 d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v));
-    return d;
-}
-__device__ __forceinline__ F2 add(F2 a, F2 b) {
-    F2 d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v));
-    return d;
-}
-__device__ __forceinline__ F2 fma(F2 a, F2 b, F2 c) {
-    F2 d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-    return d;
-}
-__device__ __forceinline__ float exp2_fast(float v) {
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-    return r;
-}
-__device__ __forceinline__ float rcp_fast(float v) {
-    float r;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-    return r;
-}
 
 // One element and a pair of elements as they lie in memory.
 template <typename XT> struct Elem;

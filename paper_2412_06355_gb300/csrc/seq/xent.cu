@@ -23,6 +23,7 @@
 #include <algorithm>
 #include <mutex>
 
+#include "pairs.cuh"
 #include "seq_common.h"
 #include "tc.cuh"
 
@@ -497,23 +498,40 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
                             if (y == col + i) g.picked[row] = v[i];
+                    // Half an instruction an element for each of the maximum, the exponent and the
+                    // sum; the exponentials themselves (16 a clock and SM) bound the epilogue.
                     float t = top;
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) t = fmaxf(t, v[i]);
+                    for (int i = 0; i < 32; i += 2) t = max3(t, v[i], v[i + 1]);
                     const float ref = t == -INFINITY ? 0.f : t * kLog2e;
                     // the reference 2^ref is what the sum is relative to, so its rounding cancels
                     const float old = top == -INFINITY ? 0.f : top * kLog2e;
-                    total = total == 0.f ? 0.f : total * exp2f(old - ref);
+                    F2 sum[2] = {both(0.f), both(0.f)};
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) total += exp2f(fmaf(v[i], kLog2e, -ref));
+                    for (int i = 0; i < 32; i += 2) {
+                        const F2 e = fma(F2(v[i], v[i + 1]), both(kLog2e), both(-ref));
+                        sum[i / 2 % 2] = add(sum[i / 2 % 2], F2(exp2_fast(e.x()), exp2_fast(e.y())));
+                    }
+                    const F2 s2 = add(sum[0], sum[1]);
+                    total = (total == 0.f ? 0.f : total * exp2_fast(old - ref)) + (s2.x() + s2.y());
                     top = t;
                 } else if (MODE == PIECE) {
-                    const int at = y - g.v0 - col;
+                    // p = exp(l - lse). bfloat16: the exponent in one multiply-add (its error, 2^-24 of
+                    // |lse|, is far below G's rounding); float32: the difference first.
+                    const F2 w = both(weight), base = both(kF32 ? -lse : -lse * kLog2e);
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        const float p = exp2f((v[i] - lse) * kLog2e);
-                        v[i] = weight * (i == at ? p - 1.f : p);
+                    for (int i = 0; i < 32; i += 2) {
+                        const F2 l(v[i], v[i + 1]);
+                        const F2 e = kF32 ? mul(add(l, base), both(kLog2e)) : fma(l, both(kLog2e), base);
+                        const F2 p = mul(F2(exp2_fast(e.x()), exp2_fast(e.y())), w);
+                        v[i] = p.x();
+                        v[i + 1] = p.y();
                     }
+                    const int at = y - g.v0 - col;
+                    if (at >= 0 && at < 32)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (i == at) v[i] -= weight;
                     uint4 *to = reinterpret_cast<uint4 *>(g.G + (int64_t)row * g.pitch + col);
                     if constexpr (!kF32) {
 #pragma unroll
