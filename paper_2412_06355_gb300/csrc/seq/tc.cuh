@@ -97,22 +97,47 @@ __device__ __forceinline__ void commit_both(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
                  ::"r"(bar), "h"((uint16_t)3) : "memory");
 }
-// 32 columns of this warp's 32 lanes. One statement loads and waits, so that no use of the
+// 32 or 64 columns of this warp's 32 lanes. One statement loads and waits, so that no use of the
 // registers can be moved between the two.
 __device__ __forceinline__ void tmem_load(float (&v)[32], uint32_t addr) {
-    uint32_t r[32];
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
                  "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
                  "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
                  "tcgen05.wait::ld.sync.aligned;"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]),
-                   "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]),
-                   "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]),
-                   "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]),
+                   "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+                   "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]),
+                   "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]),
+                   "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]),
+                   "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]),
+                   "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]),
+                   "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
                  : "r"(addr) : "memory");
-#pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_load(float (&v)[2][32], uint32_t addr) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x64.b32 "
+                 "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, "
+                 "%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, "
+                 "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];\n\t"
+                 "tcgen05.wait::ld.sync.aligned;"
+                 : "=f"(v[0][0]), "=f"(v[0][1]), "=f"(v[0][2]), "=f"(v[0][3]),
+                   "=f"(v[0][4]), "=f"(v[0][5]), "=f"(v[0][6]), "=f"(v[0][7]),
+                   "=f"(v[0][8]), "=f"(v[0][9]), "=f"(v[0][10]), "=f"(v[0][11]),
+                   "=f"(v[0][12]), "=f"(v[0][13]), "=f"(v[0][14]), "=f"(v[0][15]),
+                   "=f"(v[0][16]), "=f"(v[0][17]), "=f"(v[0][18]), "=f"(v[0][19]),
+                   "=f"(v[0][20]), "=f"(v[0][21]), "=f"(v[0][22]), "=f"(v[0][23]),
+                   "=f"(v[0][24]), "=f"(v[0][25]), "=f"(v[0][26]), "=f"(v[0][27]),
+                   "=f"(v[0][28]), "=f"(v[0][29]), "=f"(v[0][30]), "=f"(v[0][31]),
+                   "=f"(v[1][0]), "=f"(v[1][1]), "=f"(v[1][2]), "=f"(v[1][3]),
+                   "=f"(v[1][4]), "=f"(v[1][5]), "=f"(v[1][6]), "=f"(v[1][7]),
+                   "=f"(v[1][8]), "=f"(v[1][9]), "=f"(v[1][10]), "=f"(v[1][11]),
+                   "=f"(v[1][12]), "=f"(v[1][13]), "=f"(v[1][14]), "=f"(v[1][15]),
+                   "=f"(v[1][16]), "=f"(v[1][17]), "=f"(v[1][18]), "=f"(v[1][19]),
+                   "=f"(v[1][20]), "=f"(v[1][21]), "=f"(v[1][22]), "=f"(v[1][23]),
+                   "=f"(v[1][24]), "=f"(v[1][25]), "=f"(v[1][26]), "=f"(v[1][27]),
+                   "=f"(v[1][28]), "=f"(v[1][29]), "=f"(v[1][30]), "=f"(v[1][31])
+                 : "r"(addr) : "memory");
 }
 
 // Shared-memory descriptor of a 128-byte-swizzled operand tile of 16-bit elements. Rows that run

@@ -438,11 +438,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const uint32_t empty0 = tc::in_block(acc_empty, 0);
         int acc = 0;
         uint32_t acc_phase = 0;
+        // what the epilogue needs of its row is requested one tile ahead
+        int next_y = -1;
+        float next_lse = 0.f, next_weight = 0.f;
+        auto request = [&](int64_t item) {
+            if ((MODE == STATS || MODE == PIECE) && item < items) {
+                int m, n, s;
+                tile_of<MODE>(g, mt, item, m, n, s);
+                const int row = m * kTileM + (int)rank * 128 + quad * 32 + lane;
+                next_y = g.label[row];
+                if (MODE == PIECE) {
+                    next_lse = g.lse[row];
+                    next_weight = g.weight[row];
+                }
+            }
+        };
+        request(first);
         for (int64_t item = first; item < items; item += stride) {
             int m, n, s;
             tile_of<MODE>(g, mt, item, m, n, s);
             const int k0 = s * g.kb_split, k1 = MODE == WEIGHT ? kb : min(kb, k0 + g.kb_split);
             const bool any = k1 > k0;
+            const int y = next_y;
+            const float lse = next_lse, weight = next_weight;
+            request(item + stride);
             const int row = m * kTileM + (int)rank * 128 + quad * 32 + lane;
             const int col0 = n * kTileN + half * 128;
             // the tile's sums are in TMEM; takes them over once they are complete
@@ -457,7 +476,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                 if (++acc == 2) { acc = 0; acc_phase ^= 1; }
             };
             auto columns = [&](int c) { return tmem + ((uint32_t)quad << 21) + acc * kTileN + half * 128 + 32 * c; };
-            float sums[kF32 ? 4 : 1][32];
+            float sums[kF32 ? 4 : 2][32];
             if constexpr (kF32) {
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
@@ -480,13 +499,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             }
             if (!ok) break;
             float top = -INFINITY, total = 0.f;
-            int y = -1;
-            float lse = 0.f, weight = 0.f;
-            if (MODE == STATS || MODE == PIECE) y = g.label[row];
-            if (MODE == PIECE) {
-                lse = g.lse[row];
-                weight = g.weight[row];
-            }
             auto epilogue = [&](int c, float (&v)[32]) {
                 const int col = col0 + 32 * c;                // within the piece, or within D
                 if (MODE == STATS) {
@@ -601,12 +613,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                 for (int c = 0; c < 4; ++c) epilogue(c, sums[c]);
             } else {
 #pragma unroll 1
-                for (int c = 0; c < 4; ++c) {
-                    if (any) tc::tmem_load(sums[0], columns(c));
+                for (int c = 0; c < 4; c += 2) {
+                    if (any) tc::tmem_load(sums, columns(c));
                     else
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) sums[0][i] = 0.f;
+                        for (int i = 0; i < 32; ++i) sums[0][i] = sums[1][i] = 0.f;
                     epilogue(c, sums[0]);
+                    epilogue(c + 1, sums[1]);
                 }
                 if (any) give_back();
             }
