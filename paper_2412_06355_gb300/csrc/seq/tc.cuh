@@ -64,6 +64,18 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
     }
 }
 
+// ------------------------------------------------------------------ whole sectors
+// 32 bytes at once: a warp whose lanes write 32 rows writes whole sectors of each.
+__device__ __forceinline__ void store32(void *p, const uint32_t (&q)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(q[0]), "r"(q[1]), "r"(q[2]),
+                 "r"(q[3]), "r"(q[4]), "r"(q[5]), "r"(q[6]), "r"(q[7]) : "memory");
+}
+__device__ __forceinline__ void load32(uint32_t (&q)[8], const void *p) {
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(q[0]), "=r"(q[1]), "=r"(q[2]), "=r"(q[3]), "=r"(q[4]), "=r"(q[5]), "=r"(q[6]), "=r"(q[7])
+                 : "l"(p) : "memory");
+}
+
 // ------------------------------------------------------------------ tensor copies
 // Box of `map` at (x, y, z) into this block's shared memory at `dst`; its bytes are counted on
 // `bar`, which may be the other block's.

@@ -307,7 +307,7 @@ struct Gemm {
     int32_t mt, nt, splits; // tiles (mt of the products over rows follows from ctl->rows)
     int32_t kb, kb_split;   // blocks of kTileK along the sum, in all and for one split
     int32_t V, D, v0, vc;
-    bool wide;              // rows of gw can be written 16 bytes at a time
+    bool wide;              // rows of gw can be written 32 bytes at a time
 };
 
 // The operand terms of each pass over the sum, smallest products first.
@@ -544,61 +544,57 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
                             if (i == at) v[i] -= weight;
-                    uint4 *to = reinterpret_cast<uint4 *>(g.G + (int64_t)row * g.pitch + col);
-                    if constexpr (!kF32) {
+                    __nv_bfloat16 *to = g.G + (int64_t)row * g.pitch + col;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            uint32_t q[4];
+                    for (int i = 0; i < 32; i += 16) {
+                        if constexpr (!kF32) {
+                            uint32_t q[8];
 #pragma unroll
-                            for (int j = 0; j < 4; ++j)
-                                q[j] = two(__float2bfloat16_rn(v[8 * i + 2 * j]), __float2bfloat16_rn(v[8 * i + 2 * j + 1]));
-                            to[i] = make_uint4(q[0], q[1], q[2], q[3]);
-                        }
-                    } else {
+                            for (int j = 0; j < 8; ++j)
+                                q[j] = two(__float2bfloat16_rn(v[i + 2 * j]), __float2bfloat16_rn(v[i + 2 * j + 1]));
+                            tc::store32(to + i, q);
+                        } else {
+                            uint32_t q[3][8];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            uint32_t q[3][4];
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
+                            for (int j = 0; j < 8; ++j) {
                                 __nv_bfloat16 a[3], b[3];
-                                split(v[8 * i + 2 * j], a);
-                                split(v[8 * i + 2 * j + 1], b);
+                                split(v[i + 2 * j], a);
+                                split(v[i + 2 * j + 1], b);
 #pragma unroll
                                 for (int t = 0; t < 3; ++t) q[t][j] = two(a[t], b[t]);
                             }
 #pragma unroll
-                            for (int t = 0; t < 3; ++t)
-                                to[i + t * (g.gplane / 8)] = make_uint4(q[t][0], q[t][1], q[t][2], q[t][3]);
+                            for (int t = 0; t < 3; ++t) tc::store32(to + i + t * g.gplane, q[t]);
                         }
                     }
                 } else if (MODE == HIDDEN) {
-                    float4 *to = reinterpret_cast<float4 *>(g.sum + ((int64_t)s * g.Mp + row) * (g.nt * kTileN) + col);
+                    float *to = g.sum + ((int64_t)s * g.Mp + row) * (g.nt * kTileN) + col;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        float4 q = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                    for (int i = 0; i < 32; i += 8) {
+                        uint32_t q[8];
                         if (g.v0) {
-                            const float4 o = to[i];
-                            q = make_float4(q.x + o.x, q.y + o.y, q.z + o.z, q.w + o.w);
+                            tc::load32(q, to + i);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) v[i + j] += __uint_as_float(q[j]);
                         }
-                        to[i] = q;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) q[j] = __float_as_uint(v[i + j]);
+                        tc::store32(to + i, q);
                     }
                 } else {
                     T *to = static_cast<T *>(g.gw) + ((int64_t)g.v0 + row) * g.D + col;
                     if (row < g.vc) {
                         if (g.wide && col + 32 <= g.D) {
-                            if constexpr (kF32) {
+                            constexpr int kEach = 32 / sizeof(T);
 #pragma unroll
-                                for (int i = 0; i < 8; ++i)
-                                    reinterpret_cast<float4 *>(to)[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-                            } else {
+                            for (int i = 0; i < 32; i += kEach) {
+                                uint32_t q[8];
 #pragma unroll
-                                for (int i = 0; i < 4; ++i) {
-                                    uint32_t q[4];
-#pragma unroll
-                                    for (int j = 0; j < 4; ++j)
-                                        q[j] = two(__float2bfloat16_rn(v[8 * i + 2 * j]), __float2bfloat16_rn(v[8 * i + 2 * j + 1]));
-                                    reinterpret_cast<uint4 *>(to)[i] = make_uint4(q[0], q[1], q[2], q[3]);
+                                for (int j = 0; j < 8; ++j) {
+                                    if constexpr (kF32) q[j] = __float_as_uint(v[i + j]);
+                                    else q[j] = two(__float2bfloat16_rn(v[i + 2 * j]), __float2bfloat16_rn(v[i + 2 * j + 1]));
                                 }
+                                tc::store32(to + i, q);
                             }
                         } else {
 #pragma unroll
@@ -1001,7 +997,7 @@ dendsn_status run_backward(Call &c, const void *hidden, const void *weight, cons
     g.pitch = p.pitch;
     g.V = V;
     g.D = D;
-    g.wide = D * sizeof(T) % 16 == 0 && seq_aligned(gw, 16);
+    g.wide = D * sizeof(T) % 32 == 0 && seq_aligned(gw, 32);
     for (int32_t v0 = 0; e == cudaSuccess && v0 < V; v0 += p.pitch) {
         g.v0 = v0;
         g.vc = std::min(p.pitch, V - v0);
