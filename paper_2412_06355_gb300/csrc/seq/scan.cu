@@ -384,17 +384,23 @@ template <typename XT, bool WIDE, int S, int QT, bool CL> struct Place {
         if (on) p[m] = v.x();
         if (on2) p[m + 1] = v.y();
     }
-    // The start flags of the S steps from t0 are requested with the segment's rows (`ask`) and
-    // put together when it begins (`starts`): threads side by side whose pairs are of one
-    // sample read one flag each. Both are called by whole warps.
-    __device__ __forceinline__ uint8_t ask(const ScanArgs &P, int t0) const {
-        const int l = (threadIdx.x & 31) % min(32, pairs()), t = t0 + l;
-        return P.starts && l < S && t >= 0 && t < P.T ? P.starts[(int64_t)t * P.ft + sample * P.fb] : 0;
+    // Start flags. Threads side by side whose pairs are of one sample read one flag each, for as
+    // many passes at once as they reach (`ask`), a group of passes ahead of their use; `starts`
+    // gives the S flags of the segment at t0. (One read a pass cost scan_train's forward 28 us of
+    // 160: its way back is waited for with whatever else the warp reads.) By whole warps.
+    __device__ __forceinline__ int group() const { return min(32, pairs()) / S; }
+    // `hop`: steps from a pass to the next, negative where they run backwards.
+    __device__ __forceinline__ uint32_t ask(const ScanArgs &P, int t0, int hop) const {
+        const int l = (threadIdx.x & 31) % min(32, pairs()), t = t0 + l / S * hop + l % S;
+        return P.starts && one_sample && t >= 0 && t < P.T ? P.starts[(int64_t)t * P.ft + sample * P.fb] : 0;
     }
-    __device__ __forceinline__ uint32_t starts(const ScanArgs &P, int t0, uint8_t asked) const {
+    __device__ __forceinline__ uint32_t gather(uint32_t asked) const {
+        const int lane = threadIdx.x & 31;
+        return __ballot_sync(0xffffffffu, asked) >> (lane - lane % min(32, pairs()));
+    }
+    __device__ __forceinline__ uint32_t starts(const ScanArgs &P, int t0, uint32_t gathered, int pass) const {
         if (!P.starts) return 0;
-        const int lane = threadIdx.x & 31, lane0 = lane - lane % min(32, pairs());
-        if (one_sample) return __ballot_sync(0xffffffffu, asked) >> lane0 & ((1u << S) - 1);
+        if (one_sample) return gathered >> pass % group() * S & ((1u << S) - 1);
         uint32_t f = 0;
         if (on)
 #pragma unroll
@@ -429,7 +435,7 @@ __global__ void __launch_bounds__(256, 2) scan_forward_kernel(const ScanArgs P) 
     const int seg = segment_pairs<XT, S>(width), stage_pairs = 2 * Q * seg;
     Pair *slots = reinterpret_cast<Pair *>(dynamic) + me.q * seg;
     int t0 = me.rank * me.span + me.q * S;
-    uint8_t asked = me.ask(P, t0), next_asked = 0;
+    uint32_t asked = me.ask(P, t0, me.step), gathered = 0;
     // the rows of the pass that begins at step t for this thread
     auto fetch = [&](int stage, int t) {
         Pair *to = slots + stage * stage_pairs;
@@ -444,7 +450,11 @@ __global__ void __launch_bounds__(256, 2) scan_forward_kernel(const ScanArgs P) 
     int stage = 0;
     for (int pass = 0; (int64_t)pass * me.step < P.T; ++pass) {
         F2 a[S], u[S], A, B;
-        const uint32_t cut = me.starts(P, t0, asked);
+        if (pass % me.group() == 0) {
+            gathered = me.gather(asked);
+            asked = me.ask(P, t0 + me.group() * me.step, me.step);
+        }
+        const uint32_t cut = me.starts(P, t0, gathered, pass);
         const int t1 = t0, left = P.T - t0;       // steps of the sequence from this segment on
         // the usual segments: whole, without a start in any lane
         const bool plain = __all_sync(0xffffffffu, left >= S && !cut);
@@ -461,7 +471,6 @@ __global__ void __launch_bounds__(256, 2) scan_forward_kernel(const ScanArgs P) 
         __syncwarp();                             // the stage before this one is free
         fetch(stage == 0 ? kStages - 1 : stage - 1, t0 + (kStages - 1) * me.step);
         if (++stage == kStages) stage = 0;
-        next_asked = me.ask(P, t0 + me.step);
         if (plain) {
             A = a[0];
             B = u[0];
@@ -481,7 +490,6 @@ __global__ void __launch_bounds__(256, 2) scan_forward_kernel(const ScanArgs P) 
                 }
         }
         t0 += me.step;
-        asked = next_asked;
         bool cuts;
         F2 h = fold<CL, LOGIT, MQ>(sh, P, me.q, me.cp, width, me.rank, pass, A, B, cut != 0, carry, cuts);
         if (P.saved && t1 && t1 < P.T && t1 % kInterval == 0)
@@ -537,7 +545,7 @@ __global__ void __launch_bounds__(256, 2) scan_backward_kernel(const ScanArgs P)
     extern __shared__ __align__(16) unsigned char dynamic[];
     const int seg = segment_pairs<XT, S>(width), stage_pairs = 3 * Q * seg;
     Pair *slots = reinterpret_cast<Pair *>(dynamic) + me.q * seg;
-    uint8_t asked = me.ask(P, t0);
+    uint32_t asked = me.ask(P, t0, -me.step);   // one pass ahead: groups of passes were slower here (251 -> 327 us)
     // h before the block's first step of the pass whose segment begins at t
     auto begin = [&](int t) {
         const int tb = t - me.q * S;                         // a multiple of the interval, or 0
@@ -561,7 +569,7 @@ __global__ void __launch_bounds__(256, 2) scan_backward_kernel(const ScanArgs P)
     int stage = 0;
     for (int pass = 0; pass < passes; ++pass) {
         F2 a[S], na[S], A = both(1.f), B = both(0.f), L = both(0.f), h = start;
-        const uint32_t cut = me.starts(P, t0, asked);
+        const uint32_t cut = me.starts(P, t0, me.gather(asked), 0);
         const int t1 = t0, left = P.T - t0;
         const bool plain = __all_sync(0xffffffffu, left >= S && !cut);
         copies_landed<kStages - 2>();
@@ -599,7 +607,7 @@ __global__ void __launch_bounds__(256, 2) scan_backward_kernel(const ScanArgs P)
         fetch(stage == 0 ? kStages - 1 : stage - 1, t0 - (kStages - 1) * me.step);
         if (++stage == kStages) stage = 0;
         t0 -= me.step;
-        asked = me.ask(P, t0);
+        asked = me.ask(P, t0, -me.step);
         start = begin(t0);
         const int buf = pass & 1, from_end = Q - 1 - me.q;
         ends[buf][me.q * width + me.cp] = B;
