@@ -294,6 +294,50 @@ def test_scan_offsets_beyond_32_bits():
     assert torch.count_nonzero(h[:-tail]) == 0
 
 
+def test_scan_rows_far_apart():
+    """So many channels that a block's steps lie more than 4 GB apart."""
+    M, T = 2 ** 28 + 64, 2
+    x = torch.empty(T, 1, M, device="cuda")
+    gate = torch.empty_like(x)
+    ends = [slice(0, 5000), slice(M - 5000, M)]
+    x.fill_(0.5)
+    gate.fill_(0.25)
+    g = gen(12)
+    for e in ends:
+        x[..., e], gate[..., e] = randn((T, 1, 5000), g), randn((T, 1, 5000), g)
+    cfg = binding.make_scan_config(T, 1, M, "f32", "logit", "complement")
+    st = torch.tensor([[0], [1]], dtype=torch.uint8, device="cuda")
+    for starts in (None, st):
+        h, last = binding.scan_forward(cfg, x, gate, starts, want_last=True)
+        got = dict(h=h, last=last)
+        got.update(binding.scan_backward(cfg, x, gate, x, starts))
+        for e in ends:
+            want = ref.scan(x[..., e], gate[..., e], starts, None, x[..., e], None, "logit", "complement", "time")
+            for k in got:
+                check(k, got[k][..., e], want[k])
+        del h, last, got
+
+
+def test_scan_samples_far_apart():
+    """Samples more than 4 GB apart: constant inputs against the recurrence's fixed points."""
+    B, T, N = 2, 270000, 4096
+    x = torch.full((B, T, N), 0.5, device="cuda")         # h -> 0.5 h + 0.5
+    cfg = binding.make_scan_config(T, B, N, layout="batch")
+    saved = binding.scan_workspace(cfg)
+    h, last = binding.scan_forward(cfg, x, x, saved=saved, want_last=True)
+    k = torch.arange(1, 41, dtype=torch.float64, device="cuda")
+    first = 1 - 0.5 ** k
+    for b in range(B):
+        assert torch.equal(h[b, :40].double(), first.unsqueeze(1).expand(40, N).float().double())
+        assert bool((h[b, -100:] == 1).all())
+    assert bool((last == 1).all())
+    got = binding.scan_backward(cfg, x, x, x, saved=saved)
+    for b in range(B):                                    # lambda as h, from the end
+        assert torch.equal(got["gx"][b, -40:].flip(0).double(), first.unsqueeze(1).expand(40, N).float().double())
+        assert bool((got["gx"][b, :100] == 1).all())
+        assert bool((got["ggate"][b, 100:-100] == 1).all())
+
+
 # ------------------------------------------------------------------ cross entropy
 def xent_inputs(M, V, D, dtype, seed, ignored=0.2, spread=2.0):
     g = gen(seed)
