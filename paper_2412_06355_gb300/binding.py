@@ -96,13 +96,19 @@ class dendsn_xent_config(ctypes.Structure):
 
 
 def _code(what, value, codes):
-    if value not in codes:
-        raise ValueError(f"{what} must be one of {sorted(codes)}, got {value!r}")
-    return codes[value]
+    try:
+        return codes[value]
+    except KeyError:
+        raise ValueError(f"{what} must be one of {sorted(codes)}, got {value!r}") from None
 
 
 _DTYPES = {"f32": F32, "bf16": BF16}
 _INDEX = {"i32": I32, "i64": I64}
+
+
+_GATES = {"decay": GATE_DECAY, "logit": GATE_LOGIT}
+_MIXES = {"plain": MIX_PLAIN, "complement": MIX_COMPLEMENT}
+_SCAN_LAYOUTS = {"time": TIME_FIRST, "batch": BATCH_FIRST}
 
 
 def make_embed_config(n, V, D, dtype="f32", scale=1.0, padding_id=None,
@@ -110,15 +116,13 @@ def make_embed_config(n, V, D, dtype="f32", scale=1.0, padding_id=None,
     """padding_id: the token whose row is zero and has no gradient; None: there is none."""
     return dendsn_embed_config(n, -1 if padding_id is None else padding_id, V, D,
                                _code("dtype", dtype, _DTYPES),
-                               _code("ids_dtype", ids_dtype, _INDEX), float(scale))
+                               _code("ids_dtype", ids_dtype, _INDEX), scale)
 
 
 def make_scan_config(T, B, N, dtype="f32", gate="decay", mix="plain",
                      layout="time") -> dendsn_scan_config:
-    return dendsn_scan_config(T, B, N, _code("dtype", dtype, _DTYPES),
-                              _code("gate", gate, {"decay": GATE_DECAY, "logit": GATE_LOGIT}),
-                              _code("mix", mix, {"plain": MIX_PLAIN, "complement": MIX_COMPLEMENT}),
-                              _code("layout", layout, {"time": TIME_FIRST, "batch": BATCH_FIRST}))
+    return dendsn_scan_config(T, B, N, _code("dtype", dtype, _DTYPES), _code("gate", gate, _GATES),
+                              _code("mix", mix, _MIXES), _code("layout", layout, _SCAN_LAYOUTS))
 
 
 def make_xent_config(M, V, D, dtype="f32", ignore_index=-100,
@@ -382,14 +386,19 @@ def lif_workspace(cfg, device=None):
 
 
 # ------------------------------------------------------------------ token-sequence operators
-def _expect(name, t, shape, dtype, optional=False):
-    """Refuses on the host a tensor of another shape or dtype than the config's."""
-    if t is None:
-        if optional:
-            return
-        raise ValueError(f"{name} is required")
-    if t.shape != shape or t.dtype is not dtype:
-        raise ValueError(f"{name} must be {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
+def _expect(shape, dtype, **tensors):
+    """Refuses on the host tensors of another shape or dtype than the config's."""
+    for name, t in tensors.items():
+        if t is None:
+            raise ValueError(f"{name} is required")
+        if t.shape != shape or t.dtype is not dtype:
+            raise ValueError(f"{name} must be {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
+
+
+def _pointers(*tensors):
+    """Device addresses (None for None), checked as _ptr does."""
+    return [None if t is None else t.data_ptr() if t.is_cuda and t.is_contiguous() else _ptr(t)
+            for t in tensors]
 
 
 def _idtype(code) -> torch.dtype:
@@ -414,26 +423,33 @@ def dendsn_embed_workspace_size(cfg: dendsn_embed_config) -> int:
     return int(s.value)
 
 
+def _expect_ids(cfg, ids):
+    _expect(ids.shape if ids.numel() == cfg.n else (cfg.n,), _idtype(cfg.ids_dtype), ids=ids)
+
+
 def dendsn_embed_forward(cfg, table, ids, out, stream=None):
     """out = scale * table[ids]; table [V, D], ids of n tokens (any shape), out n rows of D."""
     dt = _xdtype(cfg)
-    _expect("table", table, (cfg.V, cfg.D), dt)
-    _expect("ids", ids, tuple(ids.shape) if ids.numel() == cfg.n else (cfg.n,), _idtype(cfg.ids_dtype))
-    _expect("out", out, tuple(ids.shape) + (cfg.D,), dt)
+    _expect((cfg.V, cfg.D), dt, table=table)
+    _expect_ids(cfg, ids)
+    _expect((*ids.shape, cfg.D), dt, out=out)
     _check("dendsn_embed_forward", load().dendsn_embed_forward(
-        ctypes.byref(cfg), _ptr(table), _ptr(ids), _ptr(out), _stream(stream)))
+        ctypes.byref(cfg), *_pointers(table, ids, out), _stream(stream)))
+
+
+def _embed_backward(cfg, ids, grad_out, grad_table, scratch, stream):
+    dt = _xdtype(cfg)
+    _expect_ids(cfg, ids)
+    _expect((*ids.shape, cfg.D), dt, grad_out=grad_out)
+    _expect((cfg.V, cfg.D), dt, grad_table=grad_table)
+    _check("dendsn_embed_backward", load().dendsn_embed_backward(
+        ctypes.byref(cfg), *_pointers(ids, grad_out, grad_table, scratch), _stream(stream)))
 
 
 def dendsn_embed_backward(cfg, ids, grad_out, grad_table, scratch, stream=None):
     """grad_table [V, D] (overwritten) from grad_out, n rows of D."""
-    dt = _xdtype(cfg)
-    _expect("ids", ids, tuple(ids.shape) if ids.numel() == cfg.n else (cfg.n,), _idtype(cfg.ids_dtype))
-    _expect("grad_out", grad_out, tuple(ids.shape) + (cfg.D,), dt)
-    _expect("grad_table", grad_table, (cfg.V, cfg.D), dt)
     _bytes("scratch", scratch, dendsn_embed_workspace_size(cfg))
-    _check("dendsn_embed_backward", load().dendsn_embed_backward(
-        ctypes.byref(cfg), _ptr(ids), _ptr(grad_out), _ptr(grad_table), _ptr(scratch),
-        _stream(stream)))
+    _embed_backward(cfg, ids, grad_out, grad_table, scratch, stream)
 
 
 def embed_forward(cfg, table, ids, stream=None):
@@ -445,10 +461,12 @@ def embed_forward(cfg, table, ids, stream=None):
 
 def embed_backward(cfg, ids, grad_out, scratch=None, stream=None):
     """Allocating gradient of the embedding table, [V, D] in grad_out's dtype."""
+    need = dendsn_embed_workspace_size(cfg)
     if scratch is None:
-        scratch = _scratch(dendsn_embed_workspace_size(cfg), ids.device)
+        scratch = _scratch(need, ids.device)
+    _bytes("scratch", scratch, need)
     gtable = torch.empty((cfg.V, cfg.D), dtype=grad_out.dtype, device=grad_out.device)
-    dendsn_embed_backward(cfg, ids, grad_out, gtable, scratch, stream)
+    _embed_backward(cfg, ids, grad_out, gtable, scratch, stream)
     return gtable
 
 
@@ -460,43 +478,30 @@ def dendsn_scan_workspace_size(cfg: dendsn_scan_config) -> int:
     return int(s.value)
 
 
-def _scan_shapes(cfg):
-    """(shape of a sequence tensor, of starts, of a state, dtype)."""
+def _scan_expect(cfg, starts, states, **seq):
     lead = (cfg.B, cfg.T) if cfg.layout == BATCH_FIRST else (cfg.T, cfg.B)
-    return lead + (cfg.N,), lead, (cfg.B, cfg.N), _xdtype(cfg)
+    _expect((*lead, cfg.N), _xdtype(cfg), **seq)
+    if starts is not None:
+        _expect(lead, torch.uint8, starts=starts)
+    _expect((cfg.B, cfg.N), torch.float32, **{k: t for k, t in states.items() if t is not None})
 
 
 def dendsn_scan_forward(cfg, x, gate, starts, h0, h, h_last=None, saved=None, stream=None):
-    seq, lead, state, dt = _scan_shapes(cfg)
-    _expect("x", x, seq, dt)
-    _expect("gate", gate, seq, dt)
-    _expect("h", h, seq, dt)
-    _expect("starts", starts, lead, torch.uint8, True)
-    _expect("h0", h0, state, torch.float32, True)
-    _expect("h_last", h_last, state, torch.float32, True)
+    _scan_expect(cfg, starts, dict(h0=h0, h_last=h_last), x=x, gate=gate, h=h)
     if saved is not None:
         _bytes("saved", saved, dendsn_scan_workspace_size(cfg))
     _check("dendsn_scan_forward", load().dendsn_scan_forward(
-        ctypes.byref(cfg), _ptr(x), _ptr(gate), _ptr(starts), _ptr(h0), _ptr(h), _ptr(h_last),
-        _ptr(saved), _stream(stream)))
+        ctypes.byref(cfg), *_pointers(x, gate, starts, h0, h, h_last, saved), _stream(stream)))
 
 
 def dendsn_scan_backward(cfg, x, gate, starts, h0, grad_h, grad_last, saved, grad_x, grad_gate,
                          grad_h0=None, stream=None):
-    seq, lead, state, dt = _scan_shapes(cfg)
-    _expect("x", x, seq, dt)
-    _expect("gate", gate, seq, dt)
-    _expect("grad_h", grad_h, seq, dt)
-    _expect("grad_x", grad_x, seq, dt)
-    _expect("grad_gate", grad_gate, seq, dt)
-    _expect("starts", starts, lead, torch.uint8, True)
-    _expect("h0", h0, state, torch.float32, True)
-    _expect("grad_last", grad_last, state, torch.float32, True)
-    _expect("grad_h0", grad_h0, state, torch.float32, True)
+    _scan_expect(cfg, starts, dict(h0=h0, grad_last=grad_last, grad_h0=grad_h0), x=x, gate=gate,
+                 grad_h=grad_h, grad_x=grad_x, grad_gate=grad_gate)
     _bytes("saved", saved, dendsn_scan_workspace_size(cfg))
     _check("dendsn_scan_backward", load().dendsn_scan_backward(
-        ctypes.byref(cfg), _ptr(x), _ptr(gate), _ptr(starts), _ptr(h0), _ptr(grad_h),
-        _ptr(grad_last), _ptr(saved), _ptr(grad_x), _ptr(grad_gate), _ptr(grad_h0),
+        ctypes.byref(cfg),
+        *_pointers(x, gate, starts, h0, grad_h, grad_last, saved, grad_x, grad_gate, grad_h0),
         _stream(stream)))
 
 
@@ -540,48 +545,64 @@ def _xent_scratch(cfg, backward) -> int:
 
 def _xent_expect(cfg, hidden, weight, labels, **rows):
     dt = _xdtype(cfg)
-    _expect("hidden", hidden, (cfg.M, cfg.D), dt)
-    _expect("weight", weight, (cfg.V, cfg.D), dt)
-    _expect("labels", labels, (cfg.M,), _idtype(cfg.labels_dtype))
-    for name, t in rows.items():
-        _expect(name, t, (cfg.M,), torch.float32)
+    _expect((cfg.M, cfg.D), dt, hidden=hidden)
+    _expect((cfg.V, cfg.D), dt, weight=weight)
+    _expect((cfg.M,), _idtype(cfg.labels_dtype), labels=labels)
+    _expect((cfg.M,), torch.float32, **rows)
+
+
+def _xent_forward(cfg, hidden, weight, labels, loss, lse, scratch, stream):
+    _xent_expect(cfg, hidden, weight, labels, loss=loss, lse=lse)
+    _check("dendsn_xent_forward", load().dendsn_xent_forward(
+        ctypes.byref(cfg), *_pointers(hidden, weight, labels, loss, lse, scratch),
+        _stream(stream)))
 
 
 def dendsn_xent_forward(cfg, hidden, weight, labels, loss, lse, scratch, stream=None):
     _xent_expect(cfg, hidden, weight, labels, loss=loss, lse=lse)
     _bytes("scratch", scratch, _xent_scratch(cfg, False))
-    _check("dendsn_xent_forward", load().dendsn_xent_forward(
-        ctypes.byref(cfg), _ptr(hidden), _ptr(weight), _ptr(labels), _ptr(loss), _ptr(lse),
-        _ptr(scratch), _stream(stream)))
+    _xent_forward(cfg, hidden, weight, labels, loss, lse, scratch, stream)
+
+
+def _xent_backward(cfg, hidden, weight, labels, lse, grad_loss, grad_hidden, grad_weight, scratch,
+                   stream):
+    _xent_expect(cfg, hidden, weight, labels, lse=lse, grad_loss=grad_loss)
+    _expect((cfg.M, cfg.D), hidden.dtype, grad_hidden=grad_hidden)
+    _expect((cfg.V, cfg.D), hidden.dtype, grad_weight=grad_weight)
+    _check("dendsn_xent_backward", load().dendsn_xent_backward(
+        ctypes.byref(cfg),
+        *_pointers(hidden, weight, labels, lse, grad_loss, grad_hidden, grad_weight, scratch),
+        _stream(stream)))
 
 
 def dendsn_xent_backward(cfg, hidden, weight, labels, lse, grad_loss, grad_hidden, grad_weight,
                          scratch, stream=None):
     _xent_expect(cfg, hidden, weight, labels, lse=lse, grad_loss=grad_loss)
-    _expect("grad_hidden", grad_hidden, (cfg.M, cfg.D), hidden.dtype)
-    _expect("grad_weight", grad_weight, (cfg.V, cfg.D), hidden.dtype)
     _bytes("scratch", scratch, _xent_scratch(cfg, True))
-    _check("dendsn_xent_backward", load().dendsn_xent_backward(
-        ctypes.byref(cfg), _ptr(hidden), _ptr(weight), _ptr(labels), _ptr(lse), _ptr(grad_loss),
-        _ptr(grad_hidden), _ptr(grad_weight), _ptr(scratch), _stream(stream)))
+    _xent_backward(cfg, hidden, weight, labels, lse, grad_loss, grad_hidden, grad_weight, scratch,
+                   stream)
 
 
 def xent_forward(cfg, hidden, weight, labels, scratch=None, stream=None):
     """Allocating cross entropy of hidden [M, D] read out by weight [V, D]: (loss [M], lse [M])."""
+    need = _xent_scratch(cfg, False)
     if scratch is None:
-        scratch = _scratch(_xent_scratch(cfg, False), hidden.device)
+        scratch = _scratch(need, hidden.device)
+    _bytes("scratch", scratch, need)
     loss = torch.empty((cfg.M,), dtype=torch.float32, device=hidden.device)
     lse = torch.empty_like(loss)
-    dendsn_xent_forward(cfg, hidden, weight, labels, loss, lse, scratch, stream)
+    _xent_forward(cfg, hidden, weight, labels, loss, lse, scratch, stream)
     return loss, lse
 
 
 def xent_backward(cfg, hidden, weight, labels, lse, grad_loss, scratch=None, stream=None):
     """Allocating backward. Returns dict ghidden [M, D], gweight [V, D] in hidden's dtype."""
+    need = _xent_scratch(cfg, True)
     if scratch is None:
-        scratch = _scratch(_xent_scratch(cfg, True), hidden.device)
+        scratch = _scratch(need, hidden.device)
+    _bytes("scratch", scratch, need)
     out = dict(ghidden=torch.empty_like(hidden), gweight=torch.empty_like(weight))
-    dendsn_xent_backward(cfg, hidden, weight, labels, lse, grad_loss, out["ghidden"],
+    _xent_backward(cfg, hidden, weight, labels, lse, grad_loss, out["ghidden"],
                          out["gweight"], scratch, stream)
     return out
 

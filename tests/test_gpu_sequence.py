@@ -579,6 +579,38 @@ def test_operators_run_on_the_given_stream():
             assert torch.equal(a, b)
 
 
+def test_operators_in_a_cuda_graph():
+    """A step captured once gives, replayed on new inputs, the bits of the calls themselves."""
+    M, V, D = 700, 900, 64
+    H, W, y, c = xent_inputs(M, V, D, "bf16", 42)
+    cx, ce = binding.make_xent_config(M, V, D, "bf16"), binding.make_embed_config(M, V, D, "bf16")
+    cs = binding.make_scan_config(M, 1, D, "bf16", "logit", "complement")
+    ids, x = y.clamp_min(0), H.view(M, 1, D)
+    saved = binding.scan_workspace(cs)
+
+    def step():
+        h, _ = binding.scan_forward(cs, x, x, saved=saved)
+        loss, lse = binding.xent_forward(cx, h.view(M, D), W, y)
+        g = binding.xent_backward(cx, h.view(M, D), W, y, lse, c)
+        gs = binding.scan_backward(cs, x, x, g["ghidden"].view(M, 1, D), saved=saved)
+        return [loss, g["gweight"], gs["gx"], gs["ggate"], binding.embed_backward(ce, ids, gs["gx"].view(M, D))]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step()
+    for seed in (43, 44):
+        H.copy_(xent_inputs(M, V, D, "bf16", seed)[0])
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(outs, step()):
+            assert torch.equal(a, b)
+
+
 def test_operators_count_their_launches():
     n0 = binding.launch_count()
     cfg = binding.make_scan_config(3, 2, 8)
