@@ -22,6 +22,7 @@
 #include <cuda_bf16.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "seq_common.h"
 
@@ -487,6 +488,7 @@ dendsn_status make_plan(const dendsn_embed_config *cfg, Plan *pl) {
         return seq_fail(DENDSN_ERR_INVALID_ARG, "bad x_dtype %d", cfg->x_dtype);
     if (cfg->ids_dtype != DENDSN_I32 && cfg->ids_dtype != DENDSN_I64)
         return seq_fail(DENDSN_ERR_INVALID_ARG, "bad ids_dtype %d", cfg->ids_dtype);
+    if (!std::isfinite(cfg->scale)) return seq_fail(DENDSN_ERR_INVALID_ARG, "scale must be finite");
     // the largest grids: a warp for every kAhead vectors of an output row, and for every row and tile
     if ((cfg->n * (((int64_t)cfg->D + 32 * kAhead - 1) / (32 * kAhead)) + 7) / 8 > INT32_MAX)
         return seq_fail(DENDSN_ERR_UNSUPPORTED, "too many elements (n=%lld D=%d)", (long long)cfg->n, cfg->D);

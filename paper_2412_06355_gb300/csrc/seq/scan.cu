@@ -425,8 +425,8 @@ __global__ void __launch_bounds__(256, 2) scan_forward_kernel(const ScanArgs P) 
     const Place<XT, WIDE, S, QT, CL> me(P);
     const int width = me.pairs(), Q = me.Q();
     constexpr int MQ = QT ? QT : 8;                // most segments
+    F2 carry = me.state(P.h0);                     // read by every block before any can write h_last over it
     enter_cluster<CL>(sh, P, width);
-    F2 carry = me.state(P.h0);
     if (P.T == 0) {
         if (me.q == 0 && me.rank == 0 && P.last) me.put_state(P.last, carry);
         leave_cluster<CL>();
@@ -533,8 +533,8 @@ __global__ void __launch_bounds__(256, 2) scan_backward_kernel(const ScanArgs P)
     const Place<XT, WIDE, S, QT, CL> me(P);
     const int width = me.pairs(), Q = me.Q();
     constexpr int MQ = QT ? QT : 8;                // most segments
+    F2 carry = me.state(P.glast);                  // read by every block before any can write grad_h0 over it
     enter_cluster<CL>(sh, P, width);
-    F2 carry = me.state(P.glast);
     if (P.T == 0) {
         if (me.q == 0 && me.rank == 0 && P.gh0) me.put_state(P.gh0, carry);
         leave_cluster<CL>();

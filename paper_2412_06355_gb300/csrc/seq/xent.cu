@@ -724,7 +724,8 @@ __global__ void __launch_bounds__(256) xent_hidden_kernel(Rows R, const float *s
 }
 
 // ------------------------------------------------------------------ host
-constexpr size_t kPieceBytes = size_t(512) << 20;   // of G
+constexpr size_t kPieceBytes = size_t(512) << 20;   // of G, but at least
+constexpr int kLeastTiles = 16;                     // tiles of columns: shorter sums would be bound by joining them
 constexpr int kClusters = 76;                        // pairs of the card's 152 SMs
 
 struct Plan {
@@ -749,7 +750,7 @@ int32_t up(int64_t v, int64_t to) { return (int32_t)((v + to - 1) / to * to); }
 // 2048) are 4 rounds of 76 unsplit, and 7 half rounds in two splits.
 void choose_pieces(Plan *pl) {
     Plan &p = *pl;
-    const int64_t row = std::max<int64_t>(p.Mp, 1) * p.terms * 2, most = std::max<int64_t>(1, (int64_t)kPieceBytes / (row * kTileN));
+    const int64_t row = std::max<int64_t>(p.Mp, 1) * p.terms * 2, most = std::max<int64_t>(kLeastTiles, (int64_t)kPieceBytes / (row * kTileN));
     const int32_t fewest = (int32_t)((p.nt + most - 1) / most), kd = p.Dp / kTileK, km = (int32_t)(p.Mp / kTileK);
     const int64_t mt = std::max(p.mt, 1);
     auto rounds = [](int64_t tiles) { return (tiles + kClusters - 1) / kClusters; };

@@ -259,6 +259,18 @@ def test_scan_serving_steps_in_place(B, N):
     check("last", state, whole["last"])
 
 
+def test_scan_long_sequence_with_the_state_in_place():
+    """h_last over h0 where several blocks share the sequence."""
+    T, B, N = 3000, 1, 32
+    x, gate, _, h0, _, _ = scan_inputs(T, B, N, "f32", "logit", "time", 0, 10)
+    gate += 6.0                                           # decays near 1: h0 reaches far
+    cfg = binding.make_scan_config(T, B, N, gate="logit", mix="complement")
+    h, last = binding.scan_forward(cfg, x, gate, None, h0, want_last=True)
+    state, h2 = h0.clone(), torch.empty_like(h)
+    binding.dendsn_scan_forward(cfg, x, gate, None, state, h2, state)
+    assert torch.equal(h, h2) and torch.equal(state, last)
+
+
 def test_scan_empty():
     h0, glast = torch.ones(2, 3, device="cuda"), torch.full((2, 3), 2.0, device="cuda")
     cfg = binding.make_scan_config(0, 2, 3)

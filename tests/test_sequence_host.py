@@ -52,6 +52,21 @@ def test_xent_config_is_checked(field, value, status):
     assert test_abi_host.status_of(binding.dendsn_xent_workspace_size, cfg) == status
 
 
+@pytest.mark.parametrize("scale", [float("nan"), float("inf")])
+def test_embed_scale_has_to_be_finite(scale):
+    cfg = binding.make_embed_config(10, 20, 8, scale=scale)
+    assert test_abi_host.status_of(binding.dendsn_embed_workspace_size, cfg) == 1
+
+
+def test_xent_scratch_is_bounded():
+    """The backward's scratch holds one piece of the vocabulary, not M V values."""
+    M, V, D = 8192, 131072, 64
+    fwd, bwd = binding.dendsn_xent_workspace_size(binding.make_xent_config(M, V, D, "bf16"))
+    assert bwd < M * V * 2 / 3 and fwd < M * V * 4 / 16
+    _, more = binding.dendsn_xent_workspace_size(binding.make_xent_config(M, 4 * V, D, "bf16"))
+    assert more - bwd < 3 * V * D * 2 + (1 << 20)          # the packed weights, nothing of G
+
+
 def test_make_configs_refuse_unknown_names():
     for f, kw in ((binding.make_embed_config, dict(n=1, V=2, D=3)),
                   (binding.make_scan_config, dict(T=1, B=2, N=3)),
