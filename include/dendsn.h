@@ -243,7 +243,8 @@ dendsn_status dendsn_lif_backward(const dendsn_lif_config *cfg, const void *x,
  * dendsn_last_error(). All sums and states are float32; a bfloat16 output is rounded once.
  * Every result is the same for the same inputs from run to run (no floating-point atomics).
  * Tensors are naturally aligned (one element); rows whose addresses and lengths are multiples
- * of 16 bytes take wider loads.
+ * of 16 bytes take wider loads. A scratch buffer serves one call at a time. Kernels that wait on
+ * other blocks give up after a second or more and return NaN states, losses or grad_hidden.
  */
 typedef enum { DENDSN_I32 = 0, DENDSN_I64 = 1 } dendsn_index;
 
