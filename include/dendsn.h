@@ -328,7 +328,7 @@ dendsn_status dendsn_scan_backward(const dendsn_scan_config *cfg, const void *x,
  * bfloat16 inputs: products are exact and sums float32; G is rounded to bfloat16 before the
  * two products that take it. float32 inputs: every operand is split into three bfloat16
  * terms, whose six leading products are summed (a relative error of about 2^-24 of each
- * product).
+ * product); the forward of up to 32 rows multiplies and adds in float32.
  *   hidden, grad_hidden [M, D], weight, grad_weight [V, D]   dtype x_dtype
  *   labels [M] dtype labels_dtype;  loss, lse, grad_loss [M] float32
  *   grad_hidden and grad_weight are OVERWRITTEN. V, D >= 1; M >= 0.

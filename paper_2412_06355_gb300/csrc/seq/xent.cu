@@ -635,6 +635,136 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     if (warp == 1) tc::tmem_free(tmem, 512);
 }
 
+// ------------------------------------------------------------------ few float32 rows
+// The statistics of up to 32 float32 rows straight from the float32 operands: three bfloat16
+// terms of all the weights would be written and read for a handful of rows (16 bytes a weight
+// against 4). A block forms the logits of MT rows with 64 vocabulary rows by multiply-adds on
+// pairs along the sum, 32 terms a stage copied ahead (cp.async), and keeps each row's maximum and
+// sum of exponentials. A thread takes all MT rows of one or two vocabulary rows, so that every
+// weight is read from shared memory once and the hidden values are broadcast; the warps share
+// the terms of a stage and are added up at the end. Rows of a stage lie 36 floats apart, so that
+// no two lanes of a wide read meet in a bank. Whole calls at V = 50000, D = 1024: 16 rows 81 us
+// (187 in terms; 205 MB of weights would take 30), 32 rows 164 us (191); 64 rows would take 296 us (194 in
+// terms), so the terms begin at 33 rows. Stages of 64 terms: 92 and 163 us.
+constexpr int kFewF32 = 32, kFewV = 64, kFewK = 32, kFewPitch = kFewK + 4, kFewStages = 3;
+template <int MT> constexpr size_t kFewSmem = (size_t)kFewStages * (MT + kFewV) * kFewPitch * 4;
+static_assert(8 * 16 * (kFewV + 1) * 4 <= kFewSmem<16> && 4 * 32 * (kFewV + 1) * 4 <= kFewSmem<32>, "the warps' logits fit");
+
+template <int MT, bool WIDE>
+__global__ void __launch_bounds__(256) xent_few_kernel(Rows R, const float *hidden, const float *weight, float2 *part,
+                                                       int32_t V, int32_t D, int64_t Mp) {
+    pdl_begin();
+    constexpr int kV = MT == 16 ? 2 : 1;                      // vocabulary rows of a thread
+    constexpr int kVWarps = kFewV / (32 * kV), kKWarps = 8 / kVWarps;
+    constexpr int kStage = (MT + kFewV) * kFewPitch;
+    extern __shared__ __align__(16) float few[];
+    const int rows = R.ctl->rows, v0 = blockIdx.x * kFewV;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int col = warp % kVWarps * 32 * kV + lane, kw = warp / kVWarps;
+    const int chunks = (D + kFewK - 1) / kFewK;
+    // 8 threads copy 32 terms of a row; rows beyond the operands and terms beyond D become zeros
+    constexpr int kLines = 32, kW = kFewV / kLines, kH = (MT + kLines - 1) / kLines;
+    const int quad = threadIdx.x % 8 * 4, line = threadIdx.x / 8;
+    auto copy = [&](float *to, const float *from, bool there, int k) {
+        const uint32_t dst = tc::smem_addr(to);
+        if constexpr (WIDE) {
+            const int bytes = there && k < D ? 16 : 0;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(bytes ? from + k : from), "r"(bytes)
+                         : "memory");
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int bytes = there && k + j < D ? 4 : 0;
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst + 4 * j),
+                             "l"(bytes ? from + k + j : from), "r"(bytes) : "memory");
+            }
+        }
+    };
+    const float *w_from[kW], *h_from[kH];
+    bool w_there[kW], h_there[kH];
+#pragma unroll
+    for (int i = 0; i < kW; ++i) {
+        const int v = v0 + line + kLines * i;
+        w_there[i] = v < V;
+        w_from[i] = weight + (w_there[i] ? (int64_t)v * D : 0);
+    }
+#pragma unroll
+    for (int i = 0; i < kH; ++i) {
+        const int r = line + kLines * i;
+        h_there[i] = r < rows;
+        h_from[i] = hidden + (h_there[i] ? (int64_t)R.index[r] * D : 0);
+    }
+    auto fetch = [&](int chunk) {
+        if (chunk < chunks) {
+            float *w = few + chunk % kFewStages * kStage, *h = w + kFewV * kFewPitch;
+            const int k = chunk * kFewK + quad;
+#pragma unroll
+            for (int i = 0; i < kW; ++i) copy(w + (line + kLines * i) * kFewPitch + quad, w_from[i], w_there[i], k);
+#pragma unroll
+            for (int i = 0; i < kH; ++i)
+                if (line + kLines * i < MT) copy(h + (line + kLines * i) * kFewPitch + quad, h_from[i], h_there[i], k);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    F2 acc[MT][kV];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < kV; ++j) acc[i][j] = both(0.f);
+#pragma unroll
+    for (int i = 0; i < kFewStages - 1; ++i) fetch(i);
+    for (int chunk = 0; chunk < chunks; ++chunk) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kFewStages - 2) : "memory");
+        __syncthreads();                                      // the chunk is there, the one before it is read
+        fetch(chunk + kFewStages - 1);
+        const float *w = few + chunk % kFewStages * kStage, *h = w + kFewV * kFewPitch;
+#pragma unroll
+        for (int u = 0; u < kFewK; u += 4 * kKWarps) {
+            const int k = u + 4 * kw;
+            float4 b[kV];
+#pragma unroll
+            for (int j = 0; j < kV; ++j) b[j] = *reinterpret_cast<const float4 *>(w + (col + 32 * j) * kFewPitch + k);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                const float4 a = *reinterpret_cast<const float4 *>(h + i * kFewPitch + k);
+#pragma unroll
+                for (int j = 0; j < kV; ++j)
+                    acc[i][j] = fma(F2(a.z, a.w), F2(b[j].z, b[j].w), fma(F2(a.x, a.y), F2(b[j].x, b[j].y), acc[i][j]));
+            }
+        }
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();
+    constexpr int kRow = kFewV + 1;
+    float *logits = few;                                      // [kKWarps][MT][kRow]
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < kV; ++j) logits[(kw * MT + i) * kRow + col + 32 * j] = acc[i][j].x() + acc[i][j].y();
+    __syncthreads();
+    for (int r = warp; r < min(MT, rows); r += 8) {
+        const int y = R.label[r];
+        float l[2], top = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int v = v0 + lane + 32 * j;
+            l[j] = 0.f;
+#pragma unroll
+            for (int k = 0; k < kKWarps; ++k) l[j] += logits[(k * MT + r) * kRow + lane + 32 * j];
+            if (v >= V) l[j] = -INFINITY;
+            if (v == y) R.picked[r] = l[j];
+            top = fmaxf(top, l[j]);
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const float ref = top == -INFINITY ? 0.f : top * kLog2e;
+        float total = exp2_fast(fmaf(l[0], kLog2e, -ref)) + exp2_fast(fmaf(l[1], kLog2e, -ref));
+#pragma unroll
+        for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+        if (lane == 0) part[(int64_t)blockIdx.x * Mp + r] = make_float2(ref, total);
+    }
+}
+
 // Joins the maxima and sums of a row: 32 rows of a block, its 32 warps take every 32nd part,
 // eight of them in flight.
 __global__ void __launch_bounds__(1024) xent_join_kernel(Rows R, const float2 *part, int32_t parts, int64_t Mp,
@@ -735,7 +865,8 @@ struct Plan {
     int32_t nt, dt, mt;             // tiles along the vocabulary, D and the rows
     int32_t pitch;                  // columns of a piece
     int32_t splits, kb_split;       // of the sum over a piece in HIDDEN
-    bool pack_w;
+    bool few;                       // the forward takes the float32 operands as they are
+    int32_t parts;                  // partial maxima and sums of a row
     // offsets in the scratch buffer
     size_t index, label, where, lse, weight, picked, part, H, W, G, sum;
     size_t fwd, bwd;
@@ -801,12 +932,15 @@ dendsn_status make_plan(const dendsn_xent_config *cfg, bool backward, Plan *pl) 
     p.index = take(p.Mp * 4);
     p.label = take(p.Mp * 4);
     p.where = take((size_t)cfg->M * 4);
-    p.H = take((size_t)p.terms * p.Mp * p.Dp * 2);
+    p.few = cfg->x_dtype == DENDSN_F32 && cfg->M <= kFewF32;
+    const bool packed = backward || !p.few;
+    p.H = take(packed ? (size_t)p.terms * p.Mp * p.Dp * 2 : 0);
     // weights are packed unless their rows can be copied as they are (also asked of their address)
-    p.W = take((size_t)p.terms * cfg->V * p.Dp * 2);
+    p.W = take(packed ? (size_t)p.terms * cfg->V * p.Dp * 2 : 0);
     const size_t shared = at;
     p.picked = take(p.Mp * 4);
-    p.part = take((size_t)2 * p.nt * p.Mp * 8);
+    p.parts = p.few ? up(cfg->V, kFewV) / kFewV : 2 * p.nt;
+    p.part = take((size_t)p.parts * p.Mp * 8);
     p.fwd = at;
     if (!backward) return DENDSN_OK;
     at = shared;
@@ -932,6 +1066,25 @@ cudaError_t operands(Call &c, const void *hidden, const void *weight, const PerR
                                              : operands<T, int32_t>(c, hidden, weight, r, w, w_pitch, w_inner);
 }
 
+// The statistics of few float32 rows.
+cudaError_t few_statistics(Call &c, const void *hidden, const void *weight, const void *labels, float *loss, float *lse) {
+    const Plan &p = c.pl;
+    const int D = c.cfg->D, M = c.cfg->M, V = c.cfg->V;
+    c.launches += 2;
+    const auto rows = c.cfg->labels_dtype == DENDSN_I64 ? xent_rows_kernel<int64_t> : xent_rows_kernel<int32_t>;
+    cudaError_t e = seq_launch(rows, dim3(1), 1024, 0, c.s, 1, rows_of(c), labels, M, V, c.cfg->ignore_index, loss, lse,
+                               nullptr, nullptr);
+    if (e != cudaSuccess) return e;
+    const bool wide = D % 4 == 0 && seq_aligned(hidden, 16) && seq_aligned(weight, 16), small = M <= 16;
+    const auto kernel = small ? (wide ? xent_few_kernel<16, true> : xent_few_kernel<16, false>)
+                              : (wide ? xent_few_kernel<32, true> : xent_few_kernel<32, false>);
+    const size_t smem = small ? kFewSmem<16> : kFewSmem<32>;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    return seq_launch(kernel, dim3((unsigned)p.parts), 256, smem, c.s, 1, rows_of(c), static_cast<const float *>(hidden),
+                      static_cast<const float *>(weight), c.at<float2>(p.part), V, D, p.Mp);
+}
+
 template <typename T>
 dendsn_status run_forward(Call &c, const void *hidden, const void *weight, const void *labels, float *loss, float *lse) {
     const Plan &p = c.pl;
@@ -939,9 +1092,14 @@ dendsn_status run_forward(Call &c, const void *hidden, const void *weight, const
     const __nv_bfloat16 *w = nullptr;
     int32_t w_pitch = 0;
     int64_t w_inner = 0;
-    cudaError_t e = operands<T>(c, hidden, weight, PerRow{labels, loss, lse, nullptr, nullptr}, &w, &w_pitch, &w_inner);
+    cudaError_t e;
+    if (p.few) {
+        e = few_statistics(c, hidden, weight, labels, loss, lse);
+    } else {
+        e = operands<T>(c, hidden, weight, PerRow{labels, loss, lse, nullptr, nullptr}, &w, &w_pitch, &w_inner);
+    }
     CUtensorMap a, b;
-    if (e == cudaSuccess) {
+    if (e == cudaSuccess && !p.few) {
         if (!make_map(&a, c.at<void>(p.H), p.Dp, p.Mp, p.Dp, p.terms, p.Mp * p.Dp, 128) ||
             !make_map(&b, w, w_inner, V, w_pitch, p.terms, (int64_t)V * w_pitch, 128))
             return seq_fail(DENDSN_ERR_CUDA, "tensor map refused");
@@ -961,7 +1119,7 @@ dendsn_status run_forward(Call &c, const void *hidden, const void *weight, const
     }
     if (e == cudaSuccess) {
         e = seq_launch(xent_join_kernel, dim3((unsigned)((p.Mp + 31) / 32)), 1024, 0, c.s, 1, rows_of(c), c.at<float2>(p.part),
-                       2 * p.nt, p.Mp, loss, lse);
+                       p.parts, p.Mp, loss, lse);
         c.launches += 1;
     }
     if (e != cudaSuccess) return seq_fail(DENDSN_ERR_CUDA, "xent forward launch failed: %s", cudaGetErrorString(e));

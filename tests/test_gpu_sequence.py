@@ -395,6 +395,21 @@ def test_xent(dtype, M, V, D):
     run_xent(*xent_inputs(M, V, D, dtype, M + V + D), dtype)
 
 
+@pytest.mark.parametrize("M", [1, 5, 15, 16, 17, 40, 63, 64, 65])
+@pytest.mark.parametrize("V,D", [(1, 4), (64, 32), (65, 31), (1000, 100), (4097, 33), (300, 2048)])
+def test_xent_few_float32_rows(M, V, D):
+    run_xent(*xent_inputs(M, V, D, "f32", M + V + D, ignored=0.2 if M > 1 else 0.0), "f32")
+
+
+def test_xent_few_float32_rows_ignored_and_out_of_range():
+    H, W, y, c = xent_inputs(50, 301, 40, "f32", 11, ignored=0.5)
+    H[y == -100] = float("inf")
+    y[7] = 301
+    run_xent(offset_copy(H, 1), W, y, c, "f32")
+    y[:] = -100
+    run_xent(H, W, y.int(), c, "f32")
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_xent_label_types_and_ignore_index(dtype):
     H, W, y, c = xent_inputs(150, 301, 48, dtype, 1, ignored=0.0)
