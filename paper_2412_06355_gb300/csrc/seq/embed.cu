@@ -285,38 +285,39 @@ __global__ void __launch_bounds__(kThreads) embed_index_kernel(const I *ids, Ind
                 for (uint32_t m = mine[w]; m; m &= m - 1) pos[to++] = 32 * w + __ffs(m) - 1;
             __syncwarp();
         }
-    } else
-    for (int k = blockIdx.x; k < longs; k += gridDim.x) {
-        const int32_t v = __ldcg(x.long_row + k), c = __ldcg(x.count + v), tile = __ldcg(x.long_tile + k);
-        for (int32_t t = threadIdx.x; t < (c + kTile - 1) / kTile; t += kThreads) x.tile_of[tile + t] = k;
-        const int64_t first = __ldcg(x.offset + v) + base[v / x.chunk];
-        int32_t *pos = x.pos + first;
-        int32_t done = 0;
-        // the row's positions are read again for every stretch and overwritten by it only up
-        // to the number found so far, so calls of more than one stretch keep them in slot
-        const int32_t *src = pos;
-        if (x.n > kMapBits) {
-            for (int32_t j = threadIdx.x; j < c; j += kThreads) x.slot[first + j] = __ldcg(pos + j);
-            src = x.slot + first;
-            __syncthreads();
-        }
-        for (int64_t p0 = 0; p0 < x.n; p0 += kMapBits) {
-            for (int w = threadIdx.x; w < x.words; w += kThreads) map[w] = 0;
-            __syncthreads();
-            for (int32_t j = threadIdx.x; j < c; j += kThreads) {
-                const int64_t p = __ldcg(src + j) - p0;
-                if (p >= 0 && p < kMapBits) atomicOr(map + (p >> 5), 1u << (p & 31));
+    } else {
+        for (int k = blockIdx.x; k < longs; k += gridDim.x) {
+            const int32_t v = __ldcg(x.long_row + k), c = __ldcg(x.count + v), tile = __ldcg(x.long_tile + k);
+            for (int32_t t = threadIdx.x; t < (c + kTile - 1) / kTile; t += kThreads) x.tile_of[tile + t] = k;
+            const int64_t first = __ldcg(x.offset + v) + base[v / x.chunk];
+            int32_t *pos = x.pos + first;
+            int32_t done = 0;
+            // the row's positions are read again for every stretch and overwritten by it only up
+            // to the number found so far, so calls of more than one stretch keep them in slot
+            const int32_t *src = pos;
+            if (x.n > kMapBits) {
+                for (int32_t j = threadIdx.x; j < c; j += kThreads) x.slot[first + j] = __ldcg(pos + j);
+                src = x.slot + first;
+                __syncthreads();
             }
-            __syncthreads();
-            // each thread reads back `per` consecutive words
-            const int per = (x.words + kThreads - 1) / kThreads, w0 = threadIdx.x * per, w1 = min(x.words, w0 + per);
-            int32_t mine = 0, all;
-            for (int w = w0; w < w1; ++w) mine += __popc(map[w]);
-            int32_t to = done + prefix(mine, warps, all);
-            done += all;
-            for (int w = w0; w < w1; ++w)
-                for (uint32_t m = map[w]; m; m &= m - 1) pos[to++] = (int32_t)(p0 + 32 * w + __ffs(m) - 1);
-            __syncthreads();
+            for (int64_t p0 = 0; p0 < x.n; p0 += kMapBits) {
+                for (int w = threadIdx.x; w < x.words; w += kThreads) map[w] = 0;
+                __syncthreads();
+                for (int32_t j = threadIdx.x; j < c; j += kThreads) {
+                    const int64_t p = __ldcg(src + j) - p0;
+                    if (p >= 0 && p < kMapBits) atomicOr(map + (p >> 5), 1u << (p & 31));
+                }
+                __syncthreads();
+                // each thread reads back `per` consecutive words
+                const int per = (x.words + kThreads - 1) / kThreads, w0 = threadIdx.x * per, w1 = min(x.words, w0 + per);
+                int32_t mine = 0, all;
+                for (int w = w0; w < w1; ++w) mine += __popc(map[w]);
+                int32_t to = done + prefix(mine, warps, all);
+                done += all;
+                for (int w = w0; w < w1; ++w)
+                    for (uint32_t m = map[w]; m; m &= m - 1) pos[to++] = (int32_t)(p0 + 32 * w + __ffs(m) - 1);
+                __syncthreads();
+            }
         }
     }
 }

@@ -383,27 +383,28 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             const int am = m * kTileM + (int)rank * 128, bn = n * kTileN + (int)rank * 128;
             const int k0 = s * g.kb_split, k1 = MODE == WEIGHT ? kb : min(kb, k0 + g.kb_split);
             const int chunk = kF32 ? kChunk : max(1, k1 - k0);
-            for (int c0 = k0; ok && c0 < k1; c0 += chunk)
-            for (int ph = 0; ok && ph < kPhases; ++ph) {
-                const int ta = kF32 ? term_a(ph) : 0, tb = kF32 ? term_b(ph) : 0;
-                for (int k = c0; k < min(k1, c0 + chunk); ++k) {
-                    if (!(ok = tc::bar_wait(empty + 8 * stage, phase))) break;
-                    if (rank == 0) tc::bar_expect(full + 8 * stage, 2 * kStageBytes);
-                    const uint32_t a = stage0 + stage * kStageBytes, b = a + kHalfBytes, bar = full0 + 8 * stage;
-                    if (kRowsA) {
-                        tc::load_box(a, &map_a, bar, k * kTileK, am, ta);
-                    } else {
-                        tc::load_box(a, &map_a, bar, am, k * kTileK, ta);
-                        tc::load_box(a + kHalfBytes / 2, &map_a, bar, am + 64, k * kTileK, ta);
+            for (int c0 = k0; ok && c0 < k1; c0 += chunk) {
+                for (int ph = 0; ok && ph < kPhases; ++ph) {
+                    const int ta = kF32 ? term_a(ph) : 0, tb = kF32 ? term_b(ph) : 0;
+                    for (int k = c0; k < min(k1, c0 + chunk); ++k) {
+                        if (!(ok = tc::bar_wait(empty + 8 * stage, phase))) break;
+                        if (rank == 0) tc::bar_expect(full + 8 * stage, 2 * kStageBytes);
+                        const uint32_t a = stage0 + stage * kStageBytes, b = a + kHalfBytes, bar = full0 + 8 * stage;
+                        if (kRowsA) {
+                            tc::load_box(a, &map_a, bar, k * kTileK, am, ta);
+                        } else {
+                            tc::load_box(a, &map_a, bar, am, k * kTileK, ta);
+                            tc::load_box(a + kHalfBytes / 2, &map_a, bar, am + 64, k * kTileK, ta);
+                        }
+                        if (kRowsB) {
+                            tc::load_box(b, &map_b, bar, k * kTileK, g.v0 + bn, tb);
+                        } else {
+                            const int row = MODE == HIDDEN ? g.v0 + k * kTileK : k * kTileK;
+                            tc::load_box(b, &map_b, bar, bn, row, tb);
+                            tc::load_box(b + kHalfBytes / 2, &map_b, bar, bn + 64, row, tb);
+                        }
+                        if (++stage == kStages) { stage = 0; phase ^= 1; }
                     }
-                    if (kRowsB) {
-                        tc::load_box(b, &map_b, bar, k * kTileK, g.v0 + bn, tb);
-                    } else {
-                        const int row = MODE == HIDDEN ? g.v0 + k * kTileK : k * kTileK;
-                        tc::load_box(b, &map_b, bar, bn, row, tb);
-                        tc::load_box(b + kHalfBytes / 2, &map_b, bar, bn + 64, row, tb);
-                    }
-                    if (++stage == kStages) { stage = 0; phase ^= 1; }
                 }
             }
         }
@@ -417,23 +418,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             const int k0 = s * g.kb_split, k1 = MODE == WEIGHT ? kb : min(kb, k0 + g.kb_split);
             const int chunk = kF32 ? kChunk : max(1, k1 - k0);
             for (int c0 = k0; ok && c0 < k1; c0 += chunk) {
-            const int steps = min(chunk, k1 - c0) * kPhases;
-            if (!(ok = tc::bar_wait(acc_empty + 8 * acc, acc_phase))) break;
-            tc::fence_after_sync();
-            for (int i = 0; i < steps; ++i) {
-                if (!(ok = tc::bar_wait(full + 8 * stage, phase))) break;
+                const int steps = min(chunk, k1 - c0) * kPhases;
+                if (!(ok = tc::bar_wait(acc_empty + 8 * acc, acc_phase))) break;
                 tc::fence_after_sync();
-                const uint32_t a = stage0 + stage * kStageBytes, b = a + kHalfBytes;
+                for (int i = 0; i < steps; ++i) {
+                    if (!(ok = tc::bar_wait(full + 8 * stage, phase))) break;
+                    tc::fence_after_sync();
+                    const uint32_t a = stage0 + stage * kStageBytes, b = a + kHalfBytes;
 #pragma unroll
-                for (int j = 0; j < kTileK / 16; ++j)
-                    tc::mma(tmem + acc * kTileN, tc::operand(a + j * (kRowsA ? 32 : 2048), kRowsA, kHalfBytes / 2),
-                            tc::operand(b + j * (kRowsB ? 32 : 2048), kRowsB, kHalfBytes / 2), idesc, i + j > 0);
-                tc::commit_both(empty + 8 * stage);
-                if (++stage == kStages) { stage = 0; phase ^= 1; }
-            }
-            if (!ok) break;
-            tc::commit_both(acc_full + 8 * acc);
-            if (++acc == 2) { acc = 0; acc_phase ^= 1; }
+                    for (int j = 0; j < kTileK / 16; ++j)
+                        tc::mma(tmem + acc * kTileN, tc::operand(a + j * (kRowsA ? 32 : 2048), kRowsA, kHalfBytes / 2),
+                                tc::operand(b + j * (kRowsB ? 32 : 2048), kRowsB, kHalfBytes / 2), idesc, i + j > 0);
+                    tc::commit_both(empty + 8 * stage);
+                    if (++stage == kStages) { stage = 0; phase ^= 1; }
+                }
+                if (!ok) break;
+                tc::commit_both(acc_full + 8 * acc);
+                if (++acc == 2) { acc = 0; acc_phase ^= 1; }
             }
         }
     } else if (warp >= 2) {                                   // epilogue, in both blocks
