@@ -325,20 +325,25 @@ dendsn_status dendsn_scan_backward(const dendsn_scan_config *cfg, const void *x,
  * A row whose label is ignore_index has loss 0, lse 0 and zero gradient, whatever its hidden
  * values are (also infinities and NaN). A row with any other label outside [0, V) has loss,
  * lse and grad_hidden NaN and takes no part in grad_weight.
- * bfloat16 inputs: products are exact and sums float32; G is rounded to bfloat16 before the
- * two products that take it. float32 inputs: every operand is split into three bfloat16
- * terms, whose six leading products are summed (a relative error of about 2^-24 of each
- * product); the forward of up to 32 rows multiplies and adds in float32.
+ * bfloat16 inputs: products are exact and sums float32; the two products that take G have it as
+ * the sum of two bfloat16 terms (logit_grad SPLIT, within 2^-16), or rounded to one where the
+ * caller chooses so (logit_grad BF16: two fifths fewer operations in the backward, and a rounding of
+ * up to 2^-8 of each logit's gradient beside the output's own). float32 inputs: every operand is
+ * split into three bfloat16 terms, whose six leading products are summed (a relative error of
+ * about 2^-24 of each product); the forward of up to 32 rows multiplies and adds in float32.
  *   hidden, grad_hidden [M, D], weight, grad_weight [V, D]   dtype x_dtype
  *   labels [M] dtype labels_dtype;  loss, lse, grad_loss [M] float32
  *   grad_hidden and grad_weight are OVERWRITTEN. V, D >= 1; M >= 0.
  *   scratch: 256-byte aligned; forward_bytes for the forward, backward_bytes for the backward.
  */
+typedef enum { DENDSN_LOGIT_GRAD_SPLIT = 0, DENDSN_LOGIT_GRAD_BF16 = 1 } dendsn_logit_grad;
+
 typedef struct {
     int64_t ignore_index;
     int32_t M, V, D;        /* rows, vocabulary, row length */
     int32_t x_dtype;        /* dendsn_dtype of hidden, weight and their gradients */
     int32_t labels_dtype;   /* dendsn_index of labels */
+    int32_t logit_grad;     /* dendsn_logit_grad; float32 inputs: SPLIT (three terms) */
 } dendsn_xent_config;
 
 dendsn_status dendsn_xent_workspace_size(const dendsn_xent_config *cfg, size_t *forward_bytes,

@@ -72,6 +72,7 @@ I32, I64 = 0, 1
 GATE_DECAY, GATE_LOGIT = 0, 1
 MIX_PLAIN, MIX_COMPLEMENT = 0, 1
 TIME_FIRST, BATCH_FIRST = 0, 1
+LOGIT_GRAD_SPLIT, LOGIT_GRAD_BF16 = 0, 1
 
 
 class dendsn_embed_config(ctypes.Structure):
@@ -92,7 +93,7 @@ class dendsn_xent_config(ctypes.Structure):
     """Mirror of the C struct dendsn_xent_config (cross entropy of a linear readout)."""
     _fields_ = [("ignore_index", ctypes.c_int64), ("M", ctypes.c_int32), ("V", ctypes.c_int32),
                 ("D", ctypes.c_int32), ("x_dtype", ctypes.c_int32),
-                ("labels_dtype", ctypes.c_int32)]
+                ("labels_dtype", ctypes.c_int32), ("logit_grad", ctypes.c_int32)]
 
 
 def _code(what, value, codes):
@@ -109,6 +110,7 @@ _INDEX = {"i32": I32, "i64": I64}
 _GATES = {"decay": GATE_DECAY, "logit": GATE_LOGIT}
 _MIXES = {"plain": MIX_PLAIN, "complement": MIX_COMPLEMENT}
 _SCAN_LAYOUTS = {"time": TIME_FIRST, "batch": BATCH_FIRST}
+_LOGIT_GRADS = {"split": LOGIT_GRAD_SPLIT, "bf16": LOGIT_GRAD_BF16}
 
 
 def make_embed_config(n, V, D, dtype="f32", scale=1.0, padding_id=None,
@@ -126,9 +128,12 @@ def make_scan_config(T, B, N, dtype="f32", gate="decay", mix="plain",
 
 
 def make_xent_config(M, V, D, dtype="f32", ignore_index=-100,
-                     labels_dtype="i64") -> dendsn_xent_config:
+                     labels_dtype="i64", logit_grad="split") -> dendsn_xent_config:
+    """logit_grad: how bfloat16 products take the logits' gradient, "split" in two terms or "bf16"
+    rounded to one (faster; an error of up to 2^-8 of each)."""
     return dendsn_xent_config(ignore_index, M, V, D, _code("dtype", dtype, _DTYPES),
-                              _code("labels_dtype", labels_dtype, _INDEX))
+                              _code("labels_dtype", labels_dtype, _INDEX),
+                              _code("logit_grad", logit_grad, _LOGIT_GRADS))
 
 
 class dendsn_lif_config(ctypes.Structure):
@@ -769,13 +774,15 @@ class ScanFunction(torch.autograd.Function):
 
 
 class XentFunction(torch.autograd.Function):
-    """autograd wrapper: the row losses [M] of hidden [M, D] read out by weight [V, D]."""
+    """autograd wrapper: the row losses [M] of hidden [M, D] read out by weight [V, D].
+    logit_grad as in make_xent_config."""
 
     @staticmethod
-    def forward(ctx, hidden, weight, labels, ignore_index=-100):
+    def forward(ctx, hidden, weight, labels, ignore_index=-100, logit_grad="split"):
         hidden, weight, labels = hidden.contiguous(), weight.contiguous(), labels.contiguous()
         ctx.cfg = make_xent_config(hidden.shape[0], weight.shape[0], hidden.shape[1],
-                                   _dtype_name(hidden), ignore_index, _index_name(labels))
+                                   _dtype_name(hidden), ignore_index, _index_name(labels),
+                                   logit_grad)
         loss, lse = xent_forward(ctx.cfg, hidden, weight, labels)
         ctx.save_for_backward(hidden, weight, labels, lse)
         return loss
@@ -784,4 +791,4 @@ class XentFunction(torch.autograd.Function):
     def backward(ctx, gloss):
         hidden, weight, labels, lse = ctx.saved_tensors
         g = xent_backward(ctx.cfg, hidden, weight, labels, lse, gloss.float().contiguous())
-        return g["ghidden"], g["gweight"], None, None
+        return g["ghidden"], g["gweight"], None, None, None

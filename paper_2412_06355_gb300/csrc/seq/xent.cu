@@ -6,13 +6,15 @@
 //   STATS   l = H W^T of all the vocabulary; the epilogue keeps each row's maximum and sum of
 //           exponentials of 128 columns, and the label's logit; a small kernel joins them
 //   PIECE   l again for one piece of the vocabulary; the epilogue writes
-//           G = c (exp(l - lse) - [label]) in bfloat16
+//           G = c (exp(l - lse) - [label]) as bfloat16 terms
 //   HIDDEN  grad_hidden += G W of the piece, in float32
 //   WEIGHT  grad_weight of the piece = G^T H
-// so 2 M V D operations in the forward and 6 M V D in the backward, a third of those to form
-// the logits again instead of keeping M V of them. Bound by the tensor cores: 8192 rows, V =
-// 131072, D = 2048, bfloat16: forward 2.34-2.49 ms (1.7-1.9 PFLOP/s), backward 7.9-8.1 ms (1.6), under the
-// card's power limit, where cuBLAS sustains 1.75; 4096 rows, V = 50000, D = 1024: 228 and 760 us.
+// so 2 M V D operations in the forward; in the backward 10 M V D for bfloat16 operands with G in
+// two terms (6 M V D with G rounded to one, which the caller may choose), of which 2 M V D form the
+// logits again instead of keeping M V of them. G in one term costs 8192 rows, V = 131072, D = 2048
+// 10.4 ms forward and backward, in two 15.6 ms; the error of the gradients against 64 bits is 2.4e-3 and
+// 1.7e-3, that of rounding the exact gradients. Bound by the tensor cores: the forward of that
+// size takes 2.34-2.49 ms (1.7-1.9 PFLOP/s) under the card's power limit, where cuBLAS sustains 1.75.
 // Few rows are bound by reading the weights and by three launches (16 rows, V = 32768, D = 384: 15 us).
 //
 // Rows that are ignored are left out before the products: the others are copied together
@@ -83,6 +85,12 @@ __device__ __forceinline__ void split(float x, __nv_bfloat16 (&t)[3]) {
     const float r = x - __bfloat162float(t[0]);
     t[1] = __float2bfloat16_rn(r);
     t[2] = __float2bfloat16_rn(r - __bfloat162float(t[1]));
+}
+
+// The second of two terms x = x0 + x1 (within 2^-16 of x); none where x0 is not finite.
+__device__ __forceinline__ __nv_bfloat16 remainder_of(float x, __nv_bfloat16 first) {
+    const float f = __bfloat162float(first);
+    return __float2bfloat16_rn(isfinite(f) ? x - f : 0.f);
 }
 
 // ------------------------------------------------------------------ rows that take part
@@ -302,13 +310,14 @@ struct Gemm {
     const float *lse, *weight;
     float *picked;
     float2 *part;           // [2 * nt][Mp]
-    __nv_bfloat16 *G;       // [terms][Mp][pitch]
+    __nv_bfloat16 *G;       // [gterms][Mp][pitch]
     float *sum;             // [splits][Mp][nt * kTileN]
     void *gw;               // [V][D]
     int64_t Mp, gplane;
     int32_t pitch;
     int32_t mt, nt, splits; // tiles (mt of the products over rows follows from ctl->rows)
     int32_t kb, kb_split;   // blocks of kTileK along the sum, in all and for one split
+    int32_t gterms;         // of G
     int32_t V, D, v0, vc;
     bool wide;              // rows of gw can be written 32 bytes at a time
 };
@@ -335,7 +344,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                         const Gemm g) {
     constexpr bool kF32 = sizeof(T) == 4;
-    constexpr int kPhases = kF32 ? 6 : 1;
+    // Products of terms for each block of the sum. bfloat16 inputs have one term, their G as many
+    // as the caller chose.
+    const int phases = kF32 ? 6 : MODE == HIDDEN || MODE == WEIGHT ? g.gterms : 1;
     constexpr bool kRowsA = MODE != WEIGHT;                   // operand rows run along the sum
     constexpr bool kRowsB = MODE == STATS || MODE == PIECE;
     extern __shared__ uint8_t raw[];
@@ -384,26 +395,33 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             const int k0 = s * g.kb_split, k1 = MODE == WEIGHT ? kb : min(kb, k0 + g.kb_split);
             const int chunk = kF32 ? kChunk : max(1, k1 - k0);
             for (int c0 = k0; ok && c0 < k1; c0 += chunk) {
-                for (int ph = 0; ok && ph < kPhases; ++ph) {
-                    const int ta = kF32 ? term_a(ph) : 0, tb = kF32 ? term_b(ph) : 0;
-                    for (int k = c0; k < min(k1, c0 + chunk); ++k) {
-                        if (!(ok = tc::bar_wait(empty + 8 * stage, phase))) break;
-                        if (rank == 0) tc::bar_expect(full + 8 * stage, 2 * kStageBytes);
-                        const uint32_t a = stage0 + stage * kStageBytes, b = a + kHalfBytes, bar = full0 + 8 * stage;
-                        if (kRowsA) {
-                            tc::load_box(a, &map_a, bar, k * kTileK, am, ta);
-                        } else {
-                            tc::load_box(a, &map_a, bar, am, k * kTileK, ta);
-                            tc::load_box(a + kHalfBytes / 2, &map_a, bar, am + 64, k * kTileK, ta);
-                        }
-                        if (kRowsB) {
-                            tc::load_box(b, &map_b, bar, k * kTileK, g.v0 + bn, tb);
-                        } else {
-                            const int row = MODE == HIDDEN ? g.v0 + k * kTileK : k * kTileK;
-                            tc::load_box(b, &map_b, bar, bn, row, tb);
-                            tc::load_box(b + kHalfBytes / 2, &map_b, bar, bn + 64, row, tb);
-                        }
-                        if (++stage == kStages) { stage = 0; phase ^= 1; }
+                const int end = min(k1, c0 + chunk);
+                // float32: the chunk's blocks for one product of terms after the other; bfloat16: the
+                // terms of G for one block after the other, which find the other operand in L2
+                for (int k = c0, ph = 0; k < end && ph < phases;) {
+                    const int ta = kF32 ? term_a(ph) : phases - 1 - ph, tb = kF32 ? term_b(ph) : 0;
+                    if (!(ok = tc::bar_wait(empty + 8 * stage, phase))) break;
+                    if (rank == 0) tc::bar_expect(full + 8 * stage, 2 * kStageBytes);
+                    const uint32_t a = stage0 + stage * kStageBytes, b = a + kHalfBytes, bar = full0 + 8 * stage;
+                    if (kRowsA) {
+                        tc::load_box(a, &map_a, bar, k * kTileK, am, ta);
+                    } else {
+                        tc::load_box(a, &map_a, bar, am, k * kTileK, ta);
+                        tc::load_box(a + kHalfBytes / 2, &map_a, bar, am + 64, k * kTileK, ta);
+                    }
+                    if (kRowsB) {
+                        tc::load_box(b, &map_b, bar, k * kTileK, g.v0 + bn, tb);
+                    } else {
+                        const int row = MODE == HIDDEN ? g.v0 + k * kTileK : k * kTileK;
+                        tc::load_box(b, &map_b, bar, bn, row, tb);
+                        tc::load_box(b + kHalfBytes / 2, &map_b, bar, bn + 64, row, tb);
+                    }
+                    if (++stage == kStages) { stage = 0; phase ^= 1; }
+                    if (kF32) {
+                        if (++k == end) { k = c0; ++ph; }
+                    } else if (++ph == phases) {
+                        ph = 0;
+                        ++k;
                     }
                 }
             }
@@ -418,7 +436,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             const int k0 = s * g.kb_split, k1 = MODE == WEIGHT ? kb : min(kb, k0 + g.kb_split);
             const int chunk = kF32 ? kChunk : max(1, k1 - k0);
             for (int c0 = k0; ok && c0 < k1; c0 += chunk) {
-                const int steps = min(chunk, k1 - c0) * kPhases;
+                const int steps = min(chunk, k1 - c0) * phases;
                 if (!(ok = tc::bar_wait(acc_empty + 8 * acc, acc_phase))) break;
                 tc::fence_after_sync();
                 for (int i = 0; i < steps; ++i) {
@@ -552,11 +570,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll
                     for (int i = 0; i < 32; i += 16) {
                         if constexpr (!kF32) {
-                            uint32_t q[8];
+                            uint32_t q[8], rest[8];
 #pragma unroll
-                            for (int j = 0; j < 8; ++j)
-                                q[j] = two(__float2bfloat16_rn(v[i + 2 * j]), __float2bfloat16_rn(v[i + 2 * j + 1]));
+                            for (int j = 0; j < 8; ++j) {
+                                const __nv_bfloat16 a = __float2bfloat16_rn(v[i + 2 * j]), b = __float2bfloat16_rn(v[i + 2 * j + 1]);
+                                q[j] = two(a, b);
+                                rest[j] = two(remainder_of(v[i + 2 * j], a), remainder_of(v[i + 2 * j + 1], b));
+                            }
                             tc::store32(to + i, q);
+                            if (g.gterms == 2) tc::store32(to + i + g.gplane, rest);
                         } else {
                             uint32_t q[3][8];
 #pragma unroll
@@ -860,7 +882,8 @@ constexpr int kLeastTiles = 16;                     // tiles of columns: shorter
 constexpr int kClusters = 76;                        // pairs of the card's 152 SMs
 
 struct Plan {
-    int terms;
+    int terms;                      // of the operands
+    int gterms;                     // of G
     int64_t Mp;                     // rows, a multiple of the tile
     int32_t Dp, Dq;                 // packed row, row of the sums
     int32_t nt, dt, mt;             // tiles along the vocabulary, D and the rows
@@ -882,9 +905,10 @@ int32_t up(int64_t v, int64_t to) { return (int32_t)((v + to - 1) / to * to); }
 // 2048) are 4 rounds of 76 unsplit, and 7 half rounds in two splits.
 void choose_pieces(Plan *pl) {
     Plan &p = *pl;
-    const int64_t row = std::max<int64_t>(p.Mp, 1) * p.terms * 2, most = std::max<int64_t>(kLeastTiles, (int64_t)kPieceBytes / (row * kTileN));
+    const int64_t row = std::max<int64_t>(p.Mp, 1) * p.gterms * 2, most = std::max<int64_t>(kLeastTiles, (int64_t)kPieceBytes / (row * kTileN));
     const int32_t fewest = (int32_t)((p.nt + most - 1) / most), kd = p.Dp / kTileK, km = (int32_t)(p.Mp / kTileK);
     const int64_t mt = std::max(p.mt, 1);
+    const int times = p.terms == 1 ? p.gterms : 1;   // products of terms in HIDDEN and WEIGHT for one in PIECE
     auto rounds = [](int64_t tiles) { return (tiles + kClusters - 1) / kClusters; };
     double best = 1e300;
     for (int32_t n = fewest; n < fewest + 6 && n <= p.nt; ++n) {
@@ -893,7 +917,7 @@ void choose_pieces(Plan *pl) {
             const int32_t split = (kv + s - 1) / s;
             if (s > 1 && split < 8) break;
             const double join = (double)s * p.Mp * p.Dq * 8 / 1.6e6;   // bytes of the sums, read and written
-            const double cost = pieces * (rounds(mt * vt) * kd + rounds(mt * p.dt * s) * split + rounds((int64_t)vt * p.dt) * km +
+            const double cost = pieces * (rounds(mt * vt) * kd + times * (rounds(mt * p.dt * s) * split + rounds((int64_t)vt * p.dt) * km) +
                                           join + 45.0);                // and three launches
             if (cost < best) {
                 best = cost;
@@ -913,10 +937,15 @@ dendsn_status make_plan(const dendsn_xent_config *cfg, bool backward, Plan *pl) 
         return seq_fail(DENDSN_ERR_INVALID_ARG, "bad x_dtype %d", cfg->x_dtype);
     if (cfg->labels_dtype != DENDSN_I32 && cfg->labels_dtype != DENDSN_I64)
         return seq_fail(DENDSN_ERR_INVALID_ARG, "bad labels_dtype %d", cfg->labels_dtype);
+    if (cfg->logit_grad != DENDSN_LOGIT_GRAD_SPLIT && cfg->logit_grad != DENDSN_LOGIT_GRAD_BF16)
+        return seq_fail(DENDSN_ERR_INVALID_ARG, "bad logit_grad %d", cfg->logit_grad);
+    if (cfg->logit_grad == DENDSN_LOGIT_GRAD_BF16 && cfg->x_dtype == DENDSN_F32)
+        return seq_fail(DENDSN_ERR_INVALID_ARG, "a bfloat16 logit_grad is for bfloat16 operands");
     if (cfg->M > (1 << 30) || cfg->V > (1 << 30) || cfg->D > (1 << 24))
         return seq_fail(DENDSN_ERR_UNSUPPORTED, "size out of range (M=%d V=%d D=%d)", cfg->M, cfg->V, cfg->D);
     Plan &p = *pl;
     p.terms = cfg->x_dtype == DENDSN_F32 ? 3 : 1;
+    p.gterms = cfg->x_dtype == DENDSN_F32 ? 3 : cfg->logit_grad == DENDSN_LOGIT_GRAD_BF16 ? 1 : 2;
     p.Mp = up(cfg->M, kTileM);
     p.Dp = up(cfg->D, kTileK);
     p.Dq = up(cfg->D, kTileN);
@@ -947,7 +976,7 @@ dendsn_status make_plan(const dendsn_xent_config *cfg, bool backward, Plan *pl) 
     at = shared;
     p.lse = take(p.Mp * 4);
     p.weight = take(p.Mp * 4);
-    p.G = take((size_t)p.terms * p.Mp * p.pitch * 2);
+    p.G = take((size_t)p.gterms * p.Mp * p.pitch * 2);
     p.sum = take((size_t)p.splits * p.Mp * p.Dq * 4);
     p.bwd = at;
     return DENDSN_OK;
@@ -1156,6 +1185,7 @@ dendsn_status run_backward(Call &c, const void *hidden, const void *weight, cons
     g.gw = gw;
     g.Mp = p.Mp;
     g.gplane = gplane;
+    g.gterms = p.gterms;
     g.pitch = p.pitch;
     g.V = V;
     g.D = D;
@@ -1164,8 +1194,8 @@ dendsn_status run_backward(Call &c, const void *hidden, const void *weight, cons
         g.v0 = v0;
         g.vc = std::min(p.pitch, V - v0);
         CUtensorMap g_rows, g_cols;
-        if (!make_map(&g_rows, G, g.vc, p.Mp, p.pitch, p.terms, gplane, 128) ||
-            !make_map(&g_cols, G, g.vc, p.Mp, p.pitch, p.terms, gplane, 64))
+        if (!make_map(&g_rows, G, g.vc, p.Mp, p.pitch, p.gterms, gplane, 128) ||
+            !make_map(&g_cols, G, g.vc, p.Mp, p.pitch, p.gterms, gplane, 64))
             return seq_fail(DENDSN_ERR_CUDA, "tensor map refused");
         const int32_t vt = up(g.vc, kTileM) / kTileM;
         g.nt = vt;

@@ -1,0 +1,75 @@
+"""Precision of the readout's cross entropy on the GPU, against float64: what the kernels hold in
+fewer bits than float32 only where the caller chose it."""
+import math
+
+import pytest
+import torch
+
+import seq_reference as ref
+from paper_2412_06355_gb300 import XentFunction, binding
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _cuda():
+    if not torch.cuda.is_available():
+        pytest.fail("these tests need a CUDA device")
+    binding.load()
+
+
+def inputs(M, V, D, dtype, seed, spread=2.0):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    H = torch.randn((M, D), generator=g, device="cuda").to(dtype)
+    W = (torch.randn((V, D), generator=g, device="cuda") * (spread / math.sqrt(D))).to(dtype)
+    y = torch.randint(0, V, (M,), generator=g, device="cuda")
+    y[::7] = -100
+    c = torch.rand(M, generator=g, device="cuda") + 0.5
+    return H, W, y, c
+
+
+def terms_reference(H, W, y, c):
+    """Gradients in float64 and the bounds of a float32 evaluation that has G within 2^-16 and
+    rounds its results to bfloat16 once."""
+    want = ref.xent(H.float(), W.float(), y, -100, c)
+    keep = (y >= 0).unsqueeze(1)
+    Hd, Wd = torch.where(keep, H.double(), 0.0), W.double()
+    G = torch.softmax(Hd @ Wd.t(), 1)
+    G[torch.arange(len(y), device=y.device), y.clamp_min(0)] -= 1
+    G = (G * torch.where(keep, c.double().unsqueeze(1), 0.0)).abs()
+    add = dict(ghidden=G @ Wd.abs(), gweight=G.t() @ Hd.abs())
+    return {k: (want[k][0], want[k][1] + 2.0 ** -16 * add[k] + ref.rounding(torch.bfloat16, want[k][0]))
+            for k in add}
+
+
+@pytest.mark.parametrize("M,V,D", [(1, 300, 64), (70, 1000, 72), (300, 5000, 520), (513, 777, 65)])
+def test_bfloat16_gradients_round_only_the_result(M, V, D):
+    H, W, y, c = inputs(M, V, D, torch.bfloat16, M + V)
+    if M == 1:
+        y[:] = 5
+    cfg = binding.make_xent_config(M, V, D, "bf16")
+    _, lse = binding.xent_forward(cfg, H, W, y)
+    got = binding.xent_backward(cfg, H, W, y, lse, c)
+    want = terms_reference(H, W, y, c)
+    for k in want:
+        ref.check(k, got[k], want[k])
+
+
+def test_a_rounded_logit_gradient_is_the_callers_choice():
+    H, W, y, c = inputs(300, 5000, 264, torch.bfloat16, 3)
+    want = ref.xent(H, W, y, -100, c)
+    full = terms_reference(H, W, y, c)
+    out = {}
+    for choice in ("split", "bf16"):
+        cfg = binding.make_xent_config(300, 5000, 264, "bf16", logit_grad=choice)
+        _, lse = binding.xent_forward(cfg, H, W, y)
+        out[choice] = binding.xent_backward(cfg, H, W, y, lse, c)
+        h, w = H.clone().requires_grad_(), W.clone().requires_grad_()
+        (XentFunction.apply(h, w, y, -100, choice) * c).sum().backward()
+        for k, p in (("ghidden", h), ("gweight", w)):
+            ref.check(k, p.grad, want[k])
+    for k in full:
+        ref.check(k, out["bf16"][k], want[k])
+        over = (out["bf16"][k].double() - full[k][0]).abs() > full[k][1]
+        assert bool(over.any()), k               # the two forms do differ
