@@ -7,6 +7,8 @@ There is no fallback: if the library cannot be loaded, every call raises.
 from __future__ import annotations
 
 import ctypes
+import functools
+import inspect
 import os
 import threading
 from typing import Optional
@@ -230,6 +232,27 @@ def _stream(stream) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _allocates(fn):
+    """Decorates an allocating wrapper with a `stream` argument (a torch stream or a raw handle,
+    None: the current one): its outputs and its scratch belong to that stream. Scratch given back on
+    return is then handed out again behind the kernels that use it, which the current stream's
+    memory would not be. The inputs have to be ready on the stream, and a caller who takes the
+    outputs to another stream orders the two, as with any torch operator."""
+    at = list(inspect.signature(fn).parameters).index("stream")
+
+    @functools.wraps(fn)
+    def wrapper(*args, **kw):
+        stream = args[at] if len(args) > at else kw.get("stream")
+        if stream is None:
+            return fn(*args, **kw)
+        if not hasattr(stream, "cuda_stream"):
+            handle = int(stream)                  # 1 is the driver's other name of the default stream
+            stream = torch.cuda.ExternalStream(0 if handle == 1 else handle)
+        with torch.cuda.stream(stream):
+            return fn(*args, **kw)
+    return wrapper
+
+
 def launch_count() -> int:
     """Kernels the library has enqueued since it was loaded."""
     return int(load().dendsn_launch_count())
@@ -367,6 +390,7 @@ def dendsn_lif_backward(cfg, x, grad_spikes, grad_v, saved, grad_x, stream=None)
         _ptr(grad_x), _stream(stream)))
 
 
+@_allocates
 def lif_forward(cfg, x, want_v=False, saved=None, stream=None):
     """Allocating LIF forward of x [T, B, N]. Returns (spikes, v or None)."""
     if tuple(x.shape) != (cfg.T, cfg.B, cfg.N) or x.dtype != _xdtype(cfg):
@@ -377,6 +401,7 @@ def lif_forward(cfg, x, want_v=False, saved=None, stream=None):
     return spikes, v
 
 
+@_allocates
 def lif_backward(cfg, x, grad_spikes, grad_v=None, saved=None, stream=None):
     """Allocating LIF backward. Returns dL/dX with x's shape and dtype."""
     gx = torch.empty_like(x)
@@ -457,6 +482,7 @@ def dendsn_embed_backward(cfg, ids, grad_out, grad_table, scratch, stream=None):
     _embed_backward(cfg, ids, grad_out, grad_table, scratch, stream)
 
 
+@_allocates
 def embed_forward(cfg, table, ids, stream=None):
     """Allocating embedding: scale * table[ids], of shape [*ids.shape, D]."""
     out = torch.empty(tuple(ids.shape) + (cfg.D,), dtype=table.dtype, device=table.device)
@@ -464,6 +490,7 @@ def embed_forward(cfg, table, ids, stream=None):
     return out
 
 
+@_allocates
 def embed_backward(cfg, ids, grad_out, scratch=None, stream=None):
     """Allocating gradient of the embedding table, [V, D] in grad_out's dtype."""
     need = dendsn_embed_workspace_size(cfg)
@@ -515,6 +542,7 @@ def scan_workspace(cfg, device=None):
     return _scratch(dendsn_scan_workspace_size(cfg), device or torch.device("cuda"))
 
 
+@_allocates
 def scan_forward(cfg, x, gate, starts=None, h0=None, saved=None, want_last=False, stream=None):
     """Allocating gated scan. Returns (h, h_last or None); h_last [B, N] float32."""
     h = torch.empty_like(x)
@@ -523,6 +551,7 @@ def scan_forward(cfg, x, gate, starts=None, h0=None, saved=None, want_last=False
     return h, last
 
 
+@_allocates
 def scan_backward(cfg, x, gate, grad_h, starts=None, h0=None, grad_last=None, saved=None,
                   stream=None):
     """Allocating backward of the gated scan. Returns dict gx, ggate, and gh0 where h0 is given."""
@@ -588,6 +617,7 @@ def dendsn_xent_backward(cfg, hidden, weight, labels, lse, grad_loss, grad_hidde
                    stream)
 
 
+@_allocates
 def xent_forward(cfg, hidden, weight, labels, scratch=None, stream=None):
     """Allocating cross entropy of hidden [M, D] read out by weight [V, D]: (loss [M], lse [M])."""
     need = _xent_scratch(cfg, False)
@@ -600,6 +630,7 @@ def xent_forward(cfg, hidden, weight, labels, scratch=None, stream=None):
     return loss, lse
 
 
+@_allocates
 def xent_backward(cfg, hidden, weight, labels, lse, grad_loss, scratch=None, stream=None):
     """Allocating backward. Returns dict ghidden [M, D], gweight [V, D] in hidden's dtype."""
     need = _xent_scratch(cfg, True)
@@ -645,6 +676,7 @@ def workspace(cfg, device=None):
     return saved, scratch
 
 
+@_allocates
 def forward(cfg, x, alpha, xi, zeta, kappa, mask=None, want_v=False, saved=None, stream=None):
     """Allocating forward. Returns (spikes, v or None)."""
     _check_shapes(cfg, x, alpha, xi, zeta, kappa, mask)
@@ -655,6 +687,7 @@ def forward(cfg, x, alpha, xi, zeta, kappa, mask=None, want_v=False, saved=None,
     return spikes, v
 
 
+@_allocates
 def backward(cfg, x, alpha, xi, zeta, kappa, mask, grad_spikes, grad_v=None, saved=None,
              scratch=None, stream=None, want_beta=False):
     """Allocating backward. Returns dict gx, galpha, gxi, gzeta, gkappa, and with want_beta

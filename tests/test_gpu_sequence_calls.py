@@ -1,0 +1,75 @@
+"""How the token-sequence operators are called on the GPU: other streams than the current one,
+several host threads, graphs, and the sizes at which other kernels take over."""
+
+import pytest
+import torch
+
+from paper_2412_06355_gb300 import binding
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _cuda():
+    if not torch.cuda.is_available():
+        pytest.fail("these tests need a CUDA device")
+    binding.load()
+
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+@pytest.mark.parametrize("raw", [False, True])
+def test_wrappers_on_a_stream_that_is_not_current(raw):
+    """The current stream allocates and fills memory right after each call, while the kernels
+    still wait behind slow work on their own stream."""
+    n, V, D = 3000, 900, 64
+    g = gen(1)
+    W = torch.randn((V, D), generator=g, device="cuda").bfloat16()
+    y = torch.randint(0, V, (n,), generator=g, device="cuda")
+    c = torch.rand(n, generator=g, device="cuda")
+    ce = binding.make_embed_config(n, V, D, "bf16")
+    cs = binding.make_scan_config(n, 1, D, "bf16", "logit", "complement")
+    cx = binding.make_xent_config(n, V, D, "bf16")
+    saved = binding.scan_workspace(cs)
+
+    def step(stream, between):
+        kw = {} if stream is None else dict(stream=stream)
+        e = binding.embed_forward(ce, W, y, **kw).view(n, 1, D)
+        between()
+        h, last = binding.scan_forward(cs, e, e, saved=saved, want_last=True, **kw)
+        between()
+        loss, lse = binding.xent_forward(cx, h.view(n, D), W, y, **kw)
+        between()
+        gx = binding.xent_backward(cx, h.view(n, D), W, y, lse, c, **kw)
+        between()
+        gs = binding.scan_backward(cs, e, e, gx["ghidden"].view(n, 1, D), saved=saved, **kw)
+        between()
+        gt = binding.embed_backward(ce, y, gs["gx"].view(n, D), **kw)
+        between()
+        return [e, h, last, loss, gx["gweight"], gs["gx"], gs["ggate"], gt]
+
+    want = step(None, lambda: None)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    sizes = [s for c_ in (cx,) for s in binding.dendsn_xent_workspace_size(c_)]
+    sizes += [binding.dendsn_embed_workspace_size(ce), n * D * 2, n * 4, V * D * 2]
+
+    def fill():                                       # takes whatever memory looks free, and writes it
+        for s in sizes:
+            for _ in range(3):
+                torch.full((s,), 255, dtype=torch.uint8, device="cuda")
+
+    for _ in range(3):
+        big = torch.randn(4096, 4096, device="cuda")
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            for _ in range(20):
+                big = big @ big * 1e-3
+        got = step(side.cuda_stream if raw else side, fill)
+        side.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)

@@ -1,5 +1,8 @@
 """Host-side checks of the token-sequence operators' options: no GPU, no kernel is launched."""
+import contextlib
+
 import pytest
+import torch
 
 import test_abi_host
 from paper_2412_06355_gb300 import binding
@@ -14,3 +17,84 @@ def test_logit_grad_is_checked():
     assert test_abi_host.status_of(binding.dendsn_xent_workspace_size, cfg) == 1
     with pytest.raises(ValueError, match="logit_grad"):
         binding.make_xent_config(10, 20, 8, "bf16", logit_grad="f16")
+
+
+# ------------------------------------------------------------------ wrappers and streams
+class FakeLibrary:
+    """The library with calls that launch replaced by nothing."""
+
+    def __init__(self, lib):
+        self.lib = lib
+
+    def __getattr__(self, name):
+        real = getattr(self.lib, name)
+        return real if name.endswith(("_size", "_error")) else lambda *a: 0
+
+
+class Recorder:
+    """Stands in for torch.cuda.stream: which stream is current at every allocation."""
+
+    def __init__(self, monkeypatch):
+        self.current, self.seen = None, []
+        lib = FakeLibrary(binding.load())
+        monkeypatch.setattr(binding, "load", lambda: lib)
+        monkeypatch.setattr(binding, "_pointers", lambda *t: [None] * len(t))
+        monkeypatch.setattr(binding, "_ptr", lambda t: None)
+        monkeypatch.setattr(binding, "_stream", lambda s: None)
+        monkeypatch.setattr(torch.cuda, "stream", self.use)
+        monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle: ("external", handle))
+        for name in ("empty", "empty_like"):
+            monkeypatch.setattr(torch, name, self.recorded(getattr(torch, name)))
+
+    @contextlib.contextmanager
+    def use(self, stream):
+        before, self.current = self.current, stream
+        yield
+        self.current = before
+
+    def recorded(self, fn):
+        def call(*a, **kw):
+            self.seen.append(self.current)
+            return fn(*a, **kw)
+        return call
+
+
+def wrappers():
+    """name -> (call of an allocating wrapper with a stream, tensors it allocates)."""
+    z = torch.zeros
+    ce, ids = binding.make_embed_config(4, 10, 8), z(4, dtype=torch.int64)
+    cs, x = binding.make_scan_config(3, 2, 8), z(3, 2, 8)
+    cx, h, w, y, r = binding.make_xent_config(4, 10, 8), z(4, 8), z(10, 8), z(4, dtype=torch.int64), z(4)
+    cl = binding.make_lif_config(3, 2, 8)
+    cd = binding.make_config(T=4, B=2, N=64, K=4, C=4, inner=16)
+    xd, ck, cb, sp = z(4, 2, 64, 4), z(4, 4), z(4, 4 // cd.G), z(4, 2, 64)
+    return {
+        "embed_forward": (lambda s: binding.embed_forward(ce, w, ids, stream=s), 1),
+        "embed_backward": (lambda s: binding.embed_backward(ce, ids, h, stream=s), 2),
+        "scan_forward": (lambda s: binding.scan_forward(cs, x, x, want_last=True, stream=s), 2),
+        "scan_backward": (lambda s: binding.scan_backward(cs, x, x, x, None, z(2, 8), stream=s), 3),
+        "xent_forward": (lambda s: binding.xent_forward(cx, h, w, y, stream=s), 3),
+        "xent_backward": (lambda s: binding.xent_backward(cx, h, w, y, r, r, None, s), 3),
+        "lif_forward": (lambda s: binding.lif_forward(cl, x, True, None, s), 2),
+        "lif_backward": (lambda s: binding.lif_backward(cl, x, x, stream=s), 1),
+        "forward": (lambda s: binding.forward(cd, xd, ck, ck, cb, cb, want_v=True, stream=s), 2),
+        "backward": (lambda s: binding.backward(cd, xd, ck, ck, cb, cb, None, sp, stream=s), 6),
+    }
+
+
+class SideStream:
+    cuda_stream = 64
+
+
+@pytest.mark.parametrize("name", list(wrappers()))
+def test_wrappers_allocate_under_the_stream_they_launch_on(name, monkeypatch):
+    """Memory of another stream could be handed out again while the kernels still use it."""
+    call, count = wrappers()[name]
+    rec = Recorder(monkeypatch)
+    side = SideStream()
+    for given, current in ((None, None), (side, side), (4096, ("external", 4096)),
+                           (1, ("external", 0))):
+        rec.seen.clear()
+        call(given)
+        assert len(rec.seen) >= count and all(s == current for s in rec.seen), (given, rec.seen)
+        assert rec.current is None
