@@ -48,7 +48,7 @@ constexpr int kStageBytes = 2 * kHalfBytes;
 constexpr int kThreads = 320;                             // copies, products, 8 warps of epilogue
 constexpr size_t kSmem = kStages * kStageBytes + 1024 + 256;
 constexpr int kIgnored = -1, kBadLabel = -2;
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLog2e = 1.4426950408889634f;
 
 struct Ctl {                // at the start of the scratch buffer
     int32_t rows;           // rows that take part
@@ -537,26 +537,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     float t = top;
 #pragma unroll
                     for (int i = 0; i < 32; i += 2) t = max3(t, v[i], v[i + 1]);
-                    const float ref = t == -INFINITY ? 0.f : t * kLog2e;
-                    // the reference 2^ref is what the sum is relative to, so its rounding cancels
-                    const float old = top == -INFINITY ? 0.f : top * kLog2e;
+                    // the maximum is subtracted first: the difference is exact for the terms that
+                    // count, whatever the logits' size
+                    const float ref = t == -INFINITY ? 0.f : t;
                     F2 sum[2] = {both(0.f), both(0.f)};
 #pragma unroll
                     for (int i = 0; i < 32; i += 2) {
-                        const F2 e = fma(F2(v[i], v[i + 1]), both(kLog2e), both(-ref));
+                        const F2 e = mul(add(F2(v[i], v[i + 1]), both(-ref)), both(kLog2e));
                         sum[i / 2 % 2] = add(sum[i / 2 % 2], F2(exp2_fast(e.x()), exp2_fast(e.y())));
                     }
                     const F2 s2 = add(sum[0], sum[1]);
-                    total = (total == 0.f ? 0.f : total * exp2_fast(old - ref)) + (s2.x() + s2.y());
+                    total = (total == 0.f ? 0.f : total * exp2_fast((top - ref) * kLog2e)) + (s2.x() + s2.y());
                     top = t;
                 } else if (MODE == PIECE) {
-                    // p = exp(l - lse). bfloat16: the exponent in one multiply-add (its error, 2^-24 of
-                    // |lse|, is far below G's rounding); float32: the difference first.
-                    const F2 w = both(weight), base = both(kF32 ? -lse : -lse * kLog2e);
+                    // p = exp(l - lse), the difference first, whose size alone decides its rounding
+                    const F2 w = both(weight), base = both(-lse);
 #pragma unroll
                     for (int i = 0; i < 32; i += 2) {
                         const F2 l(v[i], v[i + 1]);
-                        const F2 e = kF32 ? mul(add(l, base), both(kLog2e)) : fma(l, both(kLog2e), base);
+                        const F2 e = mul(add(l, base), both(kLog2e));
                         const F2 p = mul(F2(exp2_fast(e.x()), exp2_fast(e.y())), w);
                         v[i] = p.x();
                         v[i + 1] = p.y();
@@ -646,7 +645,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                 if (any) give_back();
             }
             if (MODE == STATS)
-                g.part[(int64_t)(2 * n + half) * g.Mp + row] = make_float2(top == -INFINITY ? 0.f : top * kLog2e, total);
+                g.part[(int64_t)(2 * n + half) * g.Mp + row] = make_float2(top, total);
         }
     }
     if (!ok) g.ctl->failed = 1;
@@ -780,11 +779,11 @@ __global__ void __launch_bounds__(256) xent_few_kernel(Rows R, const float *hidd
         }
 #pragma unroll
         for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        const float ref = top == -INFINITY ? 0.f : top * kLog2e;
-        float total = exp2_fast(fmaf(l[0], kLog2e, -ref)) + exp2_fast(fmaf(l[1], kLog2e, -ref));
+        const float ref = top == -INFINITY ? 0.f : top;
+        float total = exp2_fast((l[0] - ref) * kLog2e) + exp2_fast((l[1] - ref) * kLog2e);
 #pragma unroll
         for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-        if (lane == 0) part[(int64_t)blockIdx.x * Mp + r] = make_float2(ref, total);
+        if (lane == 0) part[(int64_t)blockIdx.x * Mp + r] = make_float2(top, total);
     }
 }
 
@@ -802,7 +801,7 @@ __global__ void __launch_bounds__(1024) xent_join_kernel(Rows R, const float2 *p
     auto add = [](float2 &x, const float2 &y) {
         if (y.y == 0.f) return;                               // nothing in it
         const float m = fmaxf(x.x, y.x);
-        x.y = (x.y == 0.f ? 0.f : x.y * exp2f(x.x - m)) + y.y * exp2f(y.x - m);
+        x.y = (x.y == 0.f ? 0.f : x.y * expf(x.x - m)) + y.y * expf(y.x - m);
         x.x = m;
     };
     if (r < rows)
@@ -825,9 +824,11 @@ __global__ void __launch_bounds__(1024) xent_join_kernel(Rows R, const float2 *p
     }
     const int row = blockIdx.x * 32 + warp;
     if (lane == 0 && row < rows) {
-        const float v = R.ctl->failed ? nan_f() : kLn2 * (b.x + log2f(b.y));
-        lse[R.index[row]] = v;
-        loss[R.index[row]] = v - R.picked[row];
+        // max + log(sum): one rounding of lse, and a loss that is exact to that of log(sum) where
+        // the label has the largest logit
+        const float rest = R.ctl->failed ? nan_f() : logf(b.y);
+        lse[R.index[row]] = b.x + rest;
+        loss[R.index[row]] = b.x - R.picked[row] + rest;
     }
 }
 

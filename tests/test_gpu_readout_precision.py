@@ -73,3 +73,52 @@ def test_a_rounded_logit_gradient_is_the_callers_choice():
         ref.check(k, out["bf16"][k], want[k])
         over = (out["bf16"][k].double() - full[k][0]).abs() > full[k][1]
         assert bool(over.any()), k               # the two forms do differ
+
+
+def exact_logits(M, V, dtype, first, seed):
+    """Operands whose logits, first 64 + k with small whole k, are exact in any order of the sum."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    H = torch.zeros(M, 8, device="cuda")
+    H[:, 0], H[:, 5] = 64.0, 1.0
+    W = torch.zeros(V, 8, device="cuda")
+    W[:, 0] = first
+    W[:, 5] = torch.randint(-9, 10, (V,), generator=g, device="cuda").float()
+    return H.to(dtype), W.to(dtype), torch.randint(0, V, (M,), generator=g, device="cuda")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M", [3, 20, 200])
+@pytest.mark.parametrize("first", [0.0, 62.5, -62.5])
+def test_loss_rounds_no_more_than_the_logarithm(dtype, M, first):
+    """Exact logits around +-4000: the loss keeps the precision of log(sum exp(l - max)), whose
+    terms and sum are off by 2^-18 of it at most, and lse has one rounding of its own."""
+    V = 1500
+    H, W, y = exact_logits(M, V, torch.float32 if dtype == "f32" else torch.bfloat16, first, M)
+    loss, lse = binding.xent_forward(binding.make_xent_config(M, V, 8, dtype), H, W, y)
+    logits = H.double() @ W.double().t()
+    want = torch.logsumexp(logits, 1)
+    wloss = want - logits.gather(1, y.unsqueeze(1)).squeeze(1)
+    assert bool(((loss.double() - wloss).abs() <= 2.0 ** -18 + 2 * ref.U32 * wloss.abs()).all())
+    assert bool(((lse.double() - want).abs() <= 2.0 ** -18 + ref.U32 * want.abs()).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M", [3, 20, 200])
+@pytest.mark.parametrize("scale", [2.0 ** 31, 2.0 ** 60, 2.0 ** 120])
+def test_logits_of_any_finite_size(dtype, M, scale):
+    """Two equal logits far above the others, or far below zero with them: the loss is log 2."""
+    V = 700
+    H = torch.zeros(M, 8, device="cuda")
+    H[:, 0] = 2.0 ** 20
+    W = torch.full((V, 8), -3.0, device="cuda")
+    W[5] = W[650] = -2.0
+    W[:, 0] *= scale / 2.0 ** 20
+    y = torch.full((M,), 650, device="cuda")
+    y[0] = 5
+    H[1::2] *= 0.5
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    loss, lse = binding.xent_forward(binding.make_xent_config(M, V, 8, dtype), H.to(dt), W.to(dt), y)
+    assert bool(((loss.double() - math.log(2)).abs() <= 2.0 ** -20).all())
+    top = H[:, 0].double() * W[5, 0].double()
+    assert torch.equal(lse.double(), top)
