@@ -331,12 +331,18 @@ dendsn_status dendsn_scan_backward(const dendsn_scan_config *cfg, const void *x,
  * up to 2^-8 of each logit's gradient beside the output's own). float32 inputs: every operand is
  * split into three bfloat16 terms, whose six leading products are summed (a relative error of
  * about 2^-24 of each product); the forward of up to 32 rows multiplies and adds in float32.
+ * What the forward leaves in lse for the backward (statistics): LSE, lse [M] as above, whose
+ * rounding is an error of up to 2^-24 |lse| of every probability in the backward; for up to 32
+ * float32 rows the logits that the backward forms are also rounded otherwise than the forward's.
+ * MAX_SUM, lse [2, M]: the largest logit and the sum of exp(l - largest), from which the backward
+ * forms the probabilities without that rounding, and of the same logits at any size.
  *   hidden, grad_hidden [M, D], weight, grad_weight [V, D]   dtype x_dtype
- *   labels [M] dtype labels_dtype;  loss, lse, grad_loss [M] float32
+ *   labels [M] dtype labels_dtype;  loss, grad_loss [M], lse [M] or [2, M] float32
  *   grad_hidden and grad_weight are OVERWRITTEN. V, D >= 1; M >= 0.
  *   scratch: 256-byte aligned; forward_bytes for the forward, backward_bytes for the backward.
  */
 typedef enum { DENDSN_LOGIT_GRAD_SPLIT = 0, DENDSN_LOGIT_GRAD_BF16 = 1 } dendsn_logit_grad;
+typedef enum { DENDSN_STATISTICS_LSE = 0, DENDSN_STATISTICS_MAX_SUM = 1 } dendsn_statistics;
 
 typedef struct {
     int64_t ignore_index;
@@ -344,6 +350,7 @@ typedef struct {
     int32_t x_dtype;        /* dendsn_dtype of hidden, weight and their gradients */
     int32_t labels_dtype;   /* dendsn_index of labels */
     int32_t logit_grad;     /* dendsn_logit_grad; float32 inputs: SPLIT (three terms) */
+    int32_t statistics;     /* dendsn_statistics of lse */
 } dendsn_xent_config;
 
 dendsn_status dendsn_xent_workspace_size(const dendsn_xent_config *cfg, size_t *forward_bytes,

@@ -75,6 +75,7 @@ GATE_DECAY, GATE_LOGIT = 0, 1
 MIX_PLAIN, MIX_COMPLEMENT = 0, 1
 TIME_FIRST, BATCH_FIRST = 0, 1
 LOGIT_GRAD_SPLIT, LOGIT_GRAD_BF16 = 0, 1
+STATISTICS_LSE, STATISTICS_MAX_SUM = 0, 1
 
 
 class dendsn_embed_config(ctypes.Structure):
@@ -95,7 +96,8 @@ class dendsn_xent_config(ctypes.Structure):
     """Mirror of the C struct dendsn_xent_config (cross entropy of a linear readout)."""
     _fields_ = [("ignore_index", ctypes.c_int64), ("M", ctypes.c_int32), ("V", ctypes.c_int32),
                 ("D", ctypes.c_int32), ("x_dtype", ctypes.c_int32),
-                ("labels_dtype", ctypes.c_int32), ("logit_grad", ctypes.c_int32)]
+                ("labels_dtype", ctypes.c_int32), ("logit_grad", ctypes.c_int32),
+                ("statistics", ctypes.c_int32)]
 
 
 def _code(what, value, codes):
@@ -113,6 +115,7 @@ _GATES = {"decay": GATE_DECAY, "logit": GATE_LOGIT}
 _MIXES = {"plain": MIX_PLAIN, "complement": MIX_COMPLEMENT}
 _SCAN_LAYOUTS = {"time": TIME_FIRST, "batch": BATCH_FIRST}
 _LOGIT_GRADS = {"split": LOGIT_GRAD_SPLIT, "bf16": LOGIT_GRAD_BF16}
+_STATISTICS = {"lse": STATISTICS_LSE, "max_sum": STATISTICS_MAX_SUM}
 
 
 def make_embed_config(n, V, D, dtype="f32", scale=1.0, padding_id=None,
@@ -130,12 +133,16 @@ def make_scan_config(T, B, N, dtype="f32", gate="decay", mix="plain",
 
 
 def make_xent_config(M, V, D, dtype="f32", ignore_index=-100,
-                     labels_dtype="i64", logit_grad="split") -> dendsn_xent_config:
+                     labels_dtype="i64", logit_grad="split",
+                     statistics="lse") -> dendsn_xent_config:
     """logit_grad: how bfloat16 products take the logits' gradient, "split" in two terms or "bf16"
-    rounded to one (faster; an error of up to 2^-8 of each)."""
+    rounded to one (faster; an error of up to 2^-8 of each). statistics: the rows that the forward
+    leaves for the backward, "lse" [M] (rounded to float32) or "max_sum" [2, M], each row's largest
+    logit and the sum relative to it, which keep the probabilities' precision."""
     return dendsn_xent_config(ignore_index, M, V, D, _code("dtype", dtype, _DTYPES),
                               _code("labels_dtype", labels_dtype, _INDEX),
-                              _code("logit_grad", logit_grad, _LOGIT_GRADS))
+                              _code("logit_grad", logit_grad, _LOGIT_GRADS),
+                              _code("statistics", statistics, _STATISTICS))
 
 
 class dendsn_lif_config(ctypes.Structure):
@@ -577,8 +584,13 @@ def _xent_scratch(cfg, backward) -> int:
     return b.value
 
 
-def _xent_expect(cfg, hidden, weight, labels, **rows):
+def _statistics_shape(cfg):
+    return (2, cfg.M) if cfg.statistics == STATISTICS_MAX_SUM else (cfg.M,)
+
+
+def _xent_expect(cfg, hidden, weight, labels, lse, **rows):
     dt = _xdtype(cfg)
+    _expect(_statistics_shape(cfg), torch.float32, lse=lse)
     _expect((cfg.M, cfg.D), dt, hidden=hidden)
     _expect((cfg.V, cfg.D), dt, weight=weight)
     _expect((cfg.M,), _idtype(cfg.labels_dtype), labels=labels)
@@ -619,13 +631,14 @@ def dendsn_xent_backward(cfg, hidden, weight, labels, lse, grad_loss, grad_hidde
 
 @_allocates
 def xent_forward(cfg, hidden, weight, labels, scratch=None, stream=None):
-    """Allocating cross entropy of hidden [M, D] read out by weight [V, D]: (loss [M], lse [M])."""
+    """Allocating cross entropy of hidden [M, D] read out by weight [V, D]: (loss [M], lse), lse
+    [M] or, where the config's statistics are "max_sum", [2, M]."""
     need = _xent_scratch(cfg, False)
     if scratch is None:
         scratch = _scratch(need, hidden.device)
     _bytes("scratch", scratch, need)
     loss = torch.empty((cfg.M,), dtype=torch.float32, device=hidden.device)
-    lse = torch.empty_like(loss)
+    lse = torch.empty(_statistics_shape(cfg), dtype=torch.float32, device=hidden.device)
     _xent_forward(cfg, hidden, weight, labels, loss, lse, scratch, stream)
     return loss, lse
 
@@ -815,7 +828,7 @@ class XentFunction(torch.autograd.Function):
         hidden, weight, labels = hidden.contiguous(), weight.contiguous(), labels.contiguous()
         ctx.cfg = make_xent_config(hidden.shape[0], weight.shape[0], hidden.shape[1],
                                    _dtype_name(hidden), ignore_index, _index_name(labels),
-                                   logit_grad)
+                                   logit_grad, "max_sum" if any(ctx.needs_input_grad) else "lse")
         loss, lse = xent_forward(ctx.cfg, hidden, weight, labels)
         ctx.save_for_backward(hidden, weight, labels, lse)
         return loss

@@ -99,16 +99,33 @@ struct Rows {
     int32_t *index;         // [Mp] row of the call
     int32_t *label;         // [Mp]
     int32_t *where;         // [M] place of a row, or kIgnored, kBadLabel
-    float *lse, *weight;    // [Mp] of the backward: its lse and grad_loss
+    float *lse, *scale, *weight;   // [Mp] of the backward: G = scale exp(l - lse), minus weight at the label
     float *picked;          // [Mp] of the forward: the label's logit
 };
+
+// Per-row inputs and outputs that the list of rows takes along. lse_sum: the second row of
+// statistics, the sums beside the maxima in lse, or null where lse is one number.
+struct PerRow {
+    const void *labels;
+    float *loss, *lse_out, *sum_out;              // of the forward: written for rows that do not take part
+    const float *lse, *lse_sum, *gloss;           // of the backward
+};
+__device__ __forceinline__ void leave_out(const PerRow &p, int64_t r, int y) {
+    const float v = y == kIgnored ? 0.f : nan_f();
+    p.loss[r] = p.lse_out[r] = v;
+    if (p.sum_out) p.sum_out[r] = v;
+}
+__device__ __forceinline__ void take_along(const Rows &R, const PerRow &p, int at, int64_t r) {
+    const float w = p.gloss[r];
+    R.lse[at] = p.lse[r];
+    R.scale[at] = p.lse_sum ? w / p.lse_sum[r] : w;
+    R.weight[at] = w;
+}
 
 // One block: lists the rows with a label in the vocabulary, in order, and fills the places up
 // to the next multiple of 256 with rows of weight zero.
 template <typename I>
-__global__ void __launch_bounds__(1024) xent_rows_kernel(Rows R, const void *labels, int32_t M, int32_t V,
-                                                         int64_t ignore, float *loss, float *lse_out,
-                                                         const float *lse, const float *gloss) {
+__global__ void __launch_bounds__(1024) xent_rows_kernel(Rows R, PerRow p, int32_t M, int32_t V, int64_t ignore) {
     pdl_begin();
     constexpr int kEach = 8;                                  // consecutive rows of a thread
     __shared__ int warps[32];
@@ -118,7 +135,7 @@ __global__ void __launch_bounds__(1024) xent_rows_kernel(Rows R, const void *lab
         const int64_t r = r0 + threadIdx.x * kEach;
         int y[kEach], mine = 0;
 #pragma unroll
-        for (int j = 0; j < kEach; ++j) y[j] = r + j < M ? label_of<I>(labels, r + j, V, ignore) : kIgnored;
+        for (int j = 0; j < kEach; ++j) y[j] = r + j < M ? label_of<I>(p.labels, r + j, V, ignore) : kIgnored;
 #pragma unroll
         for (int j = 0; j < kEach; ++j) mine += y[j] >= 0;
         int incl = mine;
@@ -142,13 +159,10 @@ __global__ void __launch_bounds__(1024) xent_rows_kernel(Rows R, const void *lab
             if (y[j] >= 0) {
                 R.index[at] = (int32_t)(r + j);
                 R.label[at] = y[j];
-                if (lse) {
-                    R.lse[at] = lse[r + j];
-                    R.weight[at] = gloss[r + j];
-                }
+                if (p.lse) take_along(R, p, at, r + j);
                 ++at;
-            } else if (loss) {
-                loss[r + j] = lse_out[r + j] = y[j] == kIgnored ? 0.f : nan_f();
+            } else if (p.loss) {
+                leave_out(p, r + j, y[j]);
             }
         }
     }
@@ -156,7 +170,7 @@ __global__ void __launch_bounds__(1024) xent_rows_kernel(Rows R, const void *lab
     for (int i = done + threadIdx.x; i < end; i += 1024) {
         R.index[i] = -1;
         R.label[i] = -1;
-        if (lse) R.lse[i] = R.weight[i] = 0.f;
+        if (p.lse) R.lse[i] = R.scale[i] = R.weight[i] = 0.f;
     }
     if (threadIdx.x == 0) {
         R.ctl->rows = done;
@@ -239,10 +253,9 @@ __global__ void __launch_bounds__(256) xent_pack_kernel(const T *from, __nv_bflo
 constexpr int kFewRows = 1024;
 
 template <typename T, typename I, bool WIDE>
-__global__ void __launch_bounds__(256) xent_rows_pack_kernel(Rows R, const void *labels, int32_t M, int32_t V,
-                                                             int64_t ignore, float *loss, float *lse_out,
-                                                             const float *lse, const float *gloss, const T *from,
-                                                             __nv_bfloat16 *to, int32_t D, int32_t Dp, int64_t plane) {
+__global__ void __launch_bounds__(256) xent_rows_pack_kernel(Rows R, PerRow p, int32_t M, int32_t V, int64_t ignore,
+                                                             const T *from, __nv_bfloat16 *to, int32_t D, int32_t Dp,
+                                                             int64_t plane) {
     pdl_begin();
     constexpr int kEach = kFewRows / 256;
     __shared__ int warps[8], list[kFewRows];
@@ -250,7 +263,7 @@ __global__ void __launch_bounds__(256) xent_rows_pack_kernel(Rows R, const void 
     int y[kEach], mine = 0;
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
-        y[j] = r0 + j < M ? label_of<I>(labels, r0 + j, V, ignore) : kIgnored;
+        y[j] = r0 + j < M ? label_of<I>(p.labels, r0 + j, V, ignore) : kIgnored;
         mine += y[j] >= 0;
     }
     int incl = mine;
@@ -277,12 +290,9 @@ __global__ void __launch_bounds__(256) xent_rows_pack_kernel(Rows R, const void 
             if (y[j] >= 0) {
                 R.index[at] = r;
                 R.label[at] = y[j];
-                if (lse) {
-                    R.lse[at] = lse[r];
-                    R.weight[at] = gloss[r];
-                }
-            } else if (loss) {
-                loss[r] = lse_out[r] = y[j] == kIgnored ? 0.f : nan_f();
+                if (p.lse) take_along(R, p, at, r);
+            } else if (p.loss) {
+                leave_out(p, r, y[j]);
             }
         }
         at += y[j] >= 0;
@@ -290,7 +300,7 @@ __global__ void __launch_bounds__(256) xent_rows_pack_kernel(Rows R, const void 
     if (blockIdx.x == 0) {
         for (int i = rows + threadIdx.x; i < end; i += 256) {
             R.index[i] = R.label[i] = -1;
-            if (lse) R.lse[i] = R.weight[i] = 0.f;
+            if (p.lse) R.lse[i] = R.scale[i] = R.weight[i] = 0.f;
         }
         if (threadIdx.x == 0) {
             R.ctl->rows = rows;
@@ -307,7 +317,7 @@ __global__ void __launch_bounds__(256) xent_rows_pack_kernel(Rows R, const void 
 struct Gemm {
     Ctl *ctl;
     const int32_t *label;
-    const float *lse, *weight;
+    const float *lse, *scale, *weight;
     float *picked;
     float2 *part;           // [2 * nt][Mp]
     __nv_bfloat16 *G;       // [gterms][Mp][pitch]
@@ -462,7 +472,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         uint32_t acc_phase = 0;
         // what the epilogue needs of its row is requested one tile ahead
         int next_y = -1;
-        float next_lse = 0.f, next_weight = 0.f;
+        float next_lse = 0.f, next_scale = 0.f, next_weight = 0.f;
         auto request = [&](int64_t item) {
             if ((MODE == STATS || MODE == PIECE) && item < items) {
                 int m, n, s;
@@ -471,6 +481,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                 next_y = g.label[row];
                 if (MODE == PIECE) {
                     next_lse = g.lse[row];
+                    next_scale = g.scale[row];
                     next_weight = g.weight[row];
                 }
             }
@@ -482,7 +493,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             const int k0 = s * g.kb_split, k1 = MODE == WEIGHT ? kb : min(kb, k0 + g.kb_split);
             const bool any = k1 > k0;
             const int y = next_y;
-            const float lse = next_lse, weight = next_weight;
+            const float lse = next_lse, scale = next_scale, weight = next_weight;
             request(item + stride);
             const int row = m * kTileM + (int)rank * 128 + quad * 32 + lane;
             const int col0 = n * kTileN + half * 128;
@@ -550,8 +561,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     total = (total == 0.f ? 0.f : total * exp2_fast((top - ref) * kLog2e)) + (s2.x() + s2.y());
                     top = t;
                 } else if (MODE == PIECE) {
-                    // p = exp(l - lse), the difference first, whose size alone decides its rounding
-                    const F2 w = both(weight), base = both(-lse);
+                    // c p = scale exp(l - lse), the difference first, whose size alone decides its rounding
+                    const F2 w = both(scale), base = both(-lse);
 #pragma unroll
                     for (int i = 0; i < 32; i += 2) {
                         const F2 l(v[i], v[i + 1]);
@@ -790,7 +801,7 @@ __global__ void __launch_bounds__(256) xent_few_kernel(Rows R, const float *hidd
 // Joins the maxima and sums of a row: 32 rows of a block, its 32 warps take every 32nd part,
 // eight of them in flight.
 __global__ void __launch_bounds__(1024) xent_join_kernel(Rows R, const float2 *part, int32_t parts, int64_t Mp,
-                                                         float *loss, float *lse) {
+                                                         float *loss, float *lse, float *sum) {
     pdl_begin();
     __shared__ float2 sh[32][33];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -827,7 +838,8 @@ __global__ void __launch_bounds__(1024) xent_join_kernel(Rows R, const float2 *p
         // max + log(sum): one rounding of lse, and a loss that is exact to that of log(sum) where
         // the label has the largest logit
         const float rest = R.ctl->failed ? nan_f() : logf(b.y);
-        lse[R.index[row]] = b.x + rest;
+        lse[R.index[row]] = R.ctl->failed ? nan_f() : sum ? b.x : b.x + rest;
+        if (sum) sum[R.index[row]] = b.y;
         loss[R.index[row]] = b.x - R.picked[row] + rest;
     }
 }
@@ -893,7 +905,7 @@ struct Plan {
     bool few;                       // the forward takes the float32 operands as they are
     int32_t parts;                  // partial maxima and sums of a row
     // offsets in the scratch buffer
-    size_t index, label, where, lse, weight, picked, part, H, W, G, sum;
+    size_t index, label, where, lse, scale, weight, picked, part, H, W, G, sum;
     size_t fwd, bwd;
 };
 
@@ -942,6 +954,8 @@ dendsn_status make_plan(const dendsn_xent_config *cfg, bool backward, Plan *pl) 
         return seq_fail(DENDSN_ERR_INVALID_ARG, "bad logit_grad %d", cfg->logit_grad);
     if (cfg->logit_grad == DENDSN_LOGIT_GRAD_BF16 && cfg->x_dtype == DENDSN_F32)
         return seq_fail(DENDSN_ERR_INVALID_ARG, "a bfloat16 logit_grad is for bfloat16 operands");
+    if (cfg->statistics != DENDSN_STATISTICS_LSE && cfg->statistics != DENDSN_STATISTICS_MAX_SUM)
+        return seq_fail(DENDSN_ERR_INVALID_ARG, "bad statistics %d", cfg->statistics);
     if (cfg->M > (1 << 30) || cfg->V > (1 << 30) || cfg->D > (1 << 24))
         return seq_fail(DENDSN_ERR_UNSUPPORTED, "size out of range (M=%d V=%d D=%d)", cfg->M, cfg->V, cfg->D);
     Plan &p = *pl;
@@ -963,7 +977,8 @@ dendsn_status make_plan(const dendsn_xent_config *cfg, bool backward, Plan *pl) 
     p.index = take(p.Mp * 4);
     p.label = take(p.Mp * 4);
     p.where = take((size_t)cfg->M * 4);
-    p.few = cfg->x_dtype == DENDSN_F32 && cfg->M <= kFewF32;
+    // statistics for a backward are those of the logits that it will form
+    p.few = cfg->x_dtype == DENDSN_F32 && cfg->M <= kFewF32 && cfg->statistics == DENDSN_STATISTICS_LSE;
     const bool packed = backward || !p.few;
     p.H = take(packed ? (size_t)p.terms * p.Mp * p.Dp * 2 : 0);
     // weights are packed unless their rows can be copied as they are (also asked of their address)
@@ -976,6 +991,7 @@ dendsn_status make_plan(const dendsn_xent_config *cfg, bool backward, Plan *pl) 
     if (!backward) return DENDSN_OK;
     at = shared;
     p.lse = take(p.Mp * 4);
+    p.scale = take(p.Mp * 4);
     p.weight = take(p.Mp * 4);
     p.G = take((size_t)p.gterms * p.Mp * p.pitch * 2);
     p.sum = take((size_t)p.splits * p.Mp * p.Dq * 4);
@@ -1039,17 +1055,11 @@ Rows rows_of(const Call &c) {
     r.label = c.at<int32_t>(c.pl.label);
     r.where = c.at<int32_t>(c.pl.where);
     r.lse = c.at<float>(c.pl.lse);
+    r.scale = c.at<float>(c.pl.scale);
     r.weight = c.at<float>(c.pl.weight);
     r.picked = c.at<float>(c.pl.picked);
     return r;
 }
-
-// Per-row inputs and outputs that the list of rows takes along.
-struct PerRow {
-    const void *labels;
-    float *loss, *lse_out;        // of the forward: written for rows that do not take part
-    const float *lse, *gloss;     // of the backward
-};
 
 // The operands both passes share: the rows that take part, packed, and the weights packed or as
 // they are.
@@ -1070,11 +1080,9 @@ cudaError_t operands(Call &c, const void *hidden, const void *weight, const PerR
     c.launches += 1;
     if (M <= kFewRows) {
         const auto kernel = is_wide(hidden) ? xent_rows_pack_kernel<T, I, true> : xent_rows_pack_kernel<T, I, false>;
-        e = seq_launch(kernel, dim3((unsigned)(p.Mp / 8)), 256, 0, c.s, 1, rows_of(c), r.labels, M, V, ignore, r.loss, r.lse_out,
-                       r.lse, r.gloss, static_cast<const T *>(hidden), c.at<__nv_bfloat16>(p.H), D, p.Dp, p.Mp * p.Dp);
+        e = seq_launch(kernel, dim3((unsigned)(p.Mp / 8)), 256, 0, c.s, 1, rows_of(c), r, M, V, ignore, static_cast<const T *>(hidden), c.at<__nv_bfloat16>(p.H), D, p.Dp, p.Mp * p.Dp);
     } else {
-        e = seq_launch(xent_rows_kernel<I>, dim3(1), 1024, 0, c.s, 1, rows_of(c), r.labels, M, V, ignore, r.loss, r.lse_out,
-                       r.lse, r.gloss);
+        e = seq_launch(xent_rows_kernel<I>, dim3(1), 1024, 0, c.s, 1, rows_of(c), r, M, V, ignore);
         if (e == cudaSuccess) e = pack(hidden, p.H, c.at<int32_t>(p.index), p.Mp);
     }
     if (sizeof(T) == 2 && D % 8 == 0 && seq_aligned(weight, 16)) {
@@ -1098,13 +1106,12 @@ cudaError_t operands(Call &c, const void *hidden, const void *weight, const PerR
 }
 
 // The statistics of few float32 rows.
-cudaError_t few_statistics(Call &c, const void *hidden, const void *weight, const void *labels, float *loss, float *lse) {
+cudaError_t few_statistics(Call &c, const void *hidden, const void *weight, const PerRow &r) {
     const Plan &p = c.pl;
     const int D = c.cfg->D, M = c.cfg->M, V = c.cfg->V;
     c.launches += 2;
     const auto rows = c.cfg->labels_dtype == DENDSN_I64 ? xent_rows_kernel<int64_t> : xent_rows_kernel<int32_t>;
-    cudaError_t e = seq_launch(rows, dim3(1), 1024, 0, c.s, 1, rows_of(c), labels, M, V, c.cfg->ignore_index, loss, lse,
-                               nullptr, nullptr);
+    cudaError_t e = seq_launch(rows, dim3(1), 1024, 0, c.s, 1, rows_of(c), r, M, V, c.cfg->ignore_index);
     if (e != cudaSuccess) return e;
     const bool wide = D % 4 == 0 && seq_aligned(hidden, 16) && seq_aligned(weight, 16), small = M <= 16;
     const auto kernel = small ? (wide ? xent_few_kernel<16, true> : xent_few_kernel<16, false>)
@@ -1124,10 +1131,12 @@ dendsn_status run_forward(Call &c, const void *hidden, const void *weight, const
     int32_t w_pitch = 0;
     int64_t w_inner = 0;
     cudaError_t e;
+    float *sum = c.cfg->statistics == DENDSN_STATISTICS_MAX_SUM ? lse + c.cfg->M : nullptr;
+    const PerRow r{labels, loss, lse, sum, nullptr, nullptr, nullptr};
     if (p.few) {
-        e = few_statistics(c, hidden, weight, labels, loss, lse);
+        e = few_statistics(c, hidden, weight, r);
     } else {
-        e = operands<T>(c, hidden, weight, PerRow{labels, loss, lse, nullptr, nullptr}, &w, &w_pitch, &w_inner);
+        e = operands<T>(c, hidden, weight, r, &w, &w_pitch, &w_inner);
     }
     CUtensorMap a, b;
     if (e == cudaSuccess && !p.few) {
@@ -1150,7 +1159,7 @@ dendsn_status run_forward(Call &c, const void *hidden, const void *weight, const
     }
     if (e == cudaSuccess) {
         e = seq_launch(xent_join_kernel, dim3((unsigned)((p.Mp + 31) / 32)), 1024, 0, c.s, 1, rows_of(c), c.at<float2>(p.part),
-                       p.parts, p.Mp, loss, lse);
+                       p.parts, p.Mp, loss, lse, sum);
         c.launches += 1;
     }
     if (e != cudaSuccess) return seq_fail(DENDSN_ERR_CUDA, "xent forward launch failed: %s", cudaGetErrorString(e));
@@ -1165,7 +1174,8 @@ dendsn_status run_backward(Call &c, const void *hidden, const void *weight, cons
     const __nv_bfloat16 *w = nullptr;
     int32_t w_pitch = 0;
     int64_t w_inner = 0;
-    cudaError_t e = operands<T>(c, hidden, weight, PerRow{labels, nullptr, nullptr, lse, gloss}, &w, &w_pitch, &w_inner);
+    const float *sums = c.cfg->statistics == DENDSN_STATISTICS_MAX_SUM ? lse + c.cfg->M : nullptr;
+    cudaError_t e = operands<T>(c, hidden, weight, PerRow{labels, nullptr, nullptr, nullptr, lse, sums, gloss}, &w, &w_pitch, &w_inner);
     CUtensorMap h_rows, h_cols, w_rows, w_cols;
     const __nv_bfloat16 *H = c.at<__nv_bfloat16>(p.H);
     __nv_bfloat16 *G = c.at<__nv_bfloat16>(p.G);
@@ -1180,6 +1190,7 @@ dendsn_status run_backward(Call &c, const void *hidden, const void *weight, cons
     g.ctl = c.at<Ctl>(0);
     g.label = c.at<int32_t>(p.label);
     g.lse = c.at<float>(p.lse);
+    g.scale = c.at<float>(p.scale);
     g.weight = c.at<float>(p.weight);
     g.G = G;
     g.sum = c.at<float>(p.sum);

@@ -122,3 +122,57 @@ def test_logits_of_any_finite_size(dtype, M, scale):
     assert bool(((loss.double() - math.log(2)).abs() <= 2.0 ** -20).all())
     top = H[:, 0].double() * W[5, 0].double()
     assert torch.equal(lse.double(), top)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M", [3, 20, 200, 1500])
+def test_probabilities_of_an_autograd_step_keep_their_precision(dtype, M):
+    """Exact logits around 4000 (no two rows with the same), one label 10 above the others. The
+    probabilities of a row sum to 1 within 2^-18 (exponentials, their sum, the quotient), and with G
+    in two bfloat16 terms within another 2^-16; a float32 lse there is off by up to 2^-13. All
+    weights share their first column, so grad_hidden's first column is that sum."""
+    V = 1500
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    H, W, y = exact_logits(M, V, dt, 62.5, M)
+    H[:, 0] = 64 + torch.arange(M, device="cuda") % 50 / 2
+    W[:, 5] = -1 - (torch.arange(V, device="cuda") % 9).to(dt)
+    W[0, 5] = 9
+    y[:] = 0
+    y[1::3] = 700
+    H.requires_grad_()
+    W.requires_grad_()
+    loss = XentFunction.apply(H, W, y)
+    loss.sum().backward()
+    p = torch.softmax(H.detach().double() @ W.detach().double().t(), 1)
+    p[torch.arange(M, device="cuda"), y] -= 1
+    tol = 2.0 ** -18 + (2.0 ** -15 if dtype == "bf16" else 0)
+    assert bool((H.grad[:, 0].double().abs() <= 62.5 * tol).all())
+    want = p @ W.detach().double()
+    bound = 62.5 * tol + ref.rounding(dt, want) * (1 if dtype == "bf16" else 16)
+    assert bool(((H.grad.double() - want).abs() <= bound).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M", [20, 300, 1100])
+def test_statistics_as_maximum_and_sum(dtype, M):
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    H, W, y, c = inputs(M, 500, 72, dt, 11)
+    y[2] = 500
+    out = {}
+    for form in ("lse", "max_sum"):
+        cfg = binding.make_xent_config(M, 500, 72, dtype, statistics=form)
+        loss, lse = binding.xent_forward(cfg, H, W, y)
+        out[form] = loss, lse, binding.xent_backward(cfg, H, W, y, lse, c)
+    top, total = out["max_sum"][1]
+    keep = (y >= 0) & (y < 500)
+    assert bool((top[y < 0] == 0).all() and (total[y < 0] == 0).all())
+    assert bool(torch.isnan(top[2]) and torch.isnan(total[2]))
+    lse = (top.double() + total.double().log())[keep]
+    assert bool(((lse - out["lse"][1][keep].double()).abs() <= 4 * (72 ** 0.5) * 2.0 ** -20).all())
+    want = ref.xent(H, W, y, -100, c)
+    for form in out:
+        ref.check("loss", out[form][0], want["loss"])
+        for k in ("ghidden", "gweight"):
+            ref.check(k, out[form][2][k], want[k])
+    with pytest.raises(ValueError, match="lse"):
+        binding.xent_backward(cfg, H, W, y, out["lse"][1], c)

@@ -98,3 +98,12 @@ def test_wrappers_allocate_under_the_stream_they_launch_on(name, monkeypatch):
         call(given)
         assert len(rec.seen) >= count and all(s == current for s in rec.seen), (given, rec.seen)
         assert rec.current is None
+
+
+def test_statistics_are_checked():
+    cfg = binding.make_xent_config(10, 20, 8, "bf16", statistics="max_sum")
+    assert test_abi_host.status_of(binding.dendsn_xent_workspace_size, cfg) == 0
+    cfg.statistics = 2
+    assert test_abi_host.status_of(binding.dendsn_xent_workspace_size, cfg) == 1
+    with pytest.raises(ValueError, match="statistics"):
+        binding.make_xent_config(10, 20, 8, "bf16", statistics="sum")
