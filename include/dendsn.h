@@ -243,8 +243,11 @@ dendsn_status dendsn_lif_backward(const dendsn_lif_config *cfg, const void *x,
  * dendsn_last_error(). All sums and states are float32; a bfloat16 output is rounded once.
  * Every result is the same for the same inputs from run to run (no floating-point atomics).
  * Tensors are naturally aligned (one element); rows whose addresses and lengths are multiples
- * of 16 bytes take wider loads. A scratch buffer serves one call at a time. Kernels that wait on
- * other blocks give up after a second or more and return NaN states, losses or grad_hidden.
+ * of 16 bytes take wider loads. A scratch buffer serves one call at a time. Waits of the scan and
+ * the cross entropy on other blocks or on copies give up after a second or more: the scan's block
+ * goes on with NaN for the state that did not come (until a sequence starts), and the losses, or
+ * grad_hidden with a grad_weight of no meaning, are NaN. The embedding's gradient meets at the
+ * barriers of one cluster or of a cooperative grid, whose blocks all run at the same time.
  */
 typedef enum { DENDSN_I32 = 0, DENDSN_I64 = 1 } dendsn_index;
 

@@ -25,12 +25,12 @@
 // (4.9 TB/s; 40 instructions an element); their 1024 blocks are 3.4 rounds of the 304 that fit.
 // 16384 steps of 1024 float32 channels: 48 us (4.2 TB/s) and 109 us (3.1 TB/s), 256 blocks in
 // clusters of 8 along time. One step of 262144 bfloat16 channels: 7 us, a launch.
-#include <cooperative_groups.h>
 #include <cuda_bf16.h>
 
 #include <algorithm>
 
 #include "pairs.cuh"
+#include "scan_fold.cuh"
 #include "seq_common.h"
 
 namespace dendsn {
@@ -118,156 +118,6 @@ template <bool LOGIT> __device__ __forceinline__ void decay_of(float2 raw, F2 &a
         a = F2(raw.x, raw.y);
         na = fma(a, both(-1.f), both(1.f));
     }
-}
-
-// A h + B of a segment's map over a state, B alone where the segment has a start.
-__device__ __forceinline__ F2 map_over(F2 A, F2 B, bool cut, F2 h) {
-    const F2 r = fma(A, h, B);
-    return cut ? B : r;
-}
-// A product of decays, kept finite: a state of zero stays zero under decays above 1 whose
-// product overflows. (Where a decay is NaN, so is the segment's end.)
-template <bool LOGIT> __device__ __forceinline__ F2 finite(F2 A) {
-    constexpr float top = 3.402823466e38f;
-    if constexpr (LOGIT) return A;
-    else return F2(fminf(fmaxf(A.x(), -top), top), fminf(fmaxf(A.y(), -top), top));
-}
-struct alignas(16) Map {
-    F2 A, B;
-};
-__device__ __forceinline__ F2 over(const Map &m, bool cut, F2 h) { return map_over(m.A, m.B, cut, h); }
-
-// Maps of the segments, in two buffers of alternating passes.
-template <bool CL> struct ScanShared {
-    Map map[2][256];                             // [segment in the order of the fold][pair]
-    F2 carry[2][256];                            // the state at the end of a pass
-    Map block[2][CL ? 8 : 1][CL ? 32 : 1];       // maps of the cluster's blocks
-    int32_t block_cut[2][CL ? 8 : 1][CL ? 32 : 1];
-    uint64_t arrived[2];                         // barriers that count their bytes
-    bool cut[2][256];
-};
-
-// Blocks of a cluster hand one another their maps by asynchronous stores, which count
-// themselves in on the receiver's barrier: a cluster-wide barrier would also wait for every
-// write of h on its way to memory (16384 steps of 1024 float32 channels: 71 us with one, 51 without).
-// Buffers need no other guard: a block sends pass k + 2 after it has every map of pass k + 1,
-// and a block sends those after its threads have read pass k.
-template <bool CL> struct Exchange {
-    ScanShared<CL> &sh;
-    const ScanArgs &P;
-    int width;
-    __device__ __forceinline__ static uint32_t addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-    __device__ __forceinline__ void expect(int buf) const {
-        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(addr(&sh.arrived[buf])),
-                     "r"(P.CT * width * 20) : "memory");
-    }
-    __device__ __forceinline__ void begin() const {
-        if (threadIdx.x == 0) {
-            for (int i = 0; i < 2; ++i)
-                asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(addr(&sh.arrived[i])) : "memory");
-            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-            expect(0);
-            expect(1);
-        }
-        cooperative_groups::this_cluster().sync();
-    }
-    __device__ __forceinline__ void send(int buf, int mine, int cp, const Map &m, bool cut) const {
-        for (int r = 0; r < P.CT; ++r) {
-            uint32_t to, flag, bar;
-            asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(addr(&sh.block[buf][mine][cp])), "r"(r));
-            asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(flag) : "r"(addr(&sh.block_cut[buf][mine][cp])), "r"(r));
-            asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(bar) : "r"(addr(&sh.arrived[buf])), "r"(r));
-            asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];"
-                         ::"r"(to), "f"(m.A.x()), "f"(m.A.y()), "f"(m.B.x()), "f"(m.B.y()), "r"(bar) : "memory");
-            asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::"r"(flag),
-                         "r"((int)cut), "r"(bar) : "memory");
-        }
-    }
-    // Waits for the maps of a pass; false where they did not come within about a second.
-    __device__ __forceinline__ bool wait(int buf, uint32_t parity) const {
-        uint64_t began = 0;
-        for (uint32_t i = 0;; ++i) {
-            uint32_t done;
-            asm volatile("{\n\t.reg .pred p;\n\t"
-                         "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-                         "selp.u32 %0, 1, 0, p;\n\t}"
-                         : "=r"(done) : "r"(addr(&sh.arrived[buf])), "r"(parity) : "memory");
-            if (done) return true;
-            if (i % 64 == 63) {
-                uint64_t now;
-                asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
-                if (!began) began = now;
-                else if (now - began > 1000000000ull) return false;
-            }
-        }
-    }
-};
-
-// Folds the segment maps over the state before the pass; returns the state before this
-// thread's segment, which is number `me` of Q in the order of the fold, and whether any segment
-// of the block has a start. One barrier a pass: the maps have two buffers, and the last segment
-// leaves the state behind in sh.carry.
-template <bool CL, bool LOGIT, int MQ>
-__device__ __forceinline__ F2 fold(ScanShared<CL> &sh, const ScanArgs &P, int me, int cp, int width, int mine,
-                                   int pass, F2 A, F2 B, bool cut, F2 &carry, bool &cuts) {
-    const int buf = pass & 1;
-    sh.map[buf][me * width + cp] = Map{finite<LOGIT>(A), B};
-    sh.cut[buf][me * width + cp] = cut;
-    F2 in;
-    if constexpr (!CL) {
-        cuts = __syncthreads_or(cut);
-        in = pass ? sh.carry[buf ^ 1][cp] : carry;
-        // unrolled, so that the maps are read together and only the products wait on one another
-        if (cuts) {
-#pragma unroll
-            for (int i = 0; i < MQ - 1; ++i)
-                if (i < me) in = over(sh.map[buf][i * width + cp], sh.cut[buf][i * width + cp], in);
-        } else {
-#pragma unroll
-            for (int i = 0; i < MQ - 1; ++i)
-                if (i < me) in = over(sh.map[buf][i * width + cp], false, in);
-        }
-    } else {
-        const Exchange<CL> ex{sh, P, width};
-        cuts = __syncthreads_or(cut);
-        if (me == 0) {                           // the block's map, handed to every block
-            F2 a = both(1.f), b = both(0.f);
-            bool c = false;
-#pragma unroll
-            for (int i = 0; i < MQ; ++i) {
-                const Map m = sh.map[buf][i * width + cp];
-                const bool ci = cuts && sh.cut[buf][i * width + cp];
-                b = over(m, ci, b);
-                a = finite<LOGIT>(mul(a, m.A));
-                c |= ci;
-            }
-            ex.send(buf, mine, cp, Map{a, b}, c);
-        }
-        if (!ex.wait(buf, pass >> 1 & 1)) carry = both(__int_as_float(0x7fffffff));
-        if (threadIdx.x == 0) ex.expect(buf);
-        in = carry;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < P.CT) {
-                carry = over(sh.block[buf][i][cp], sh.block_cut[buf][i][cp], carry);
-                if (i + 1 == mine) in = carry;
-            }
-        if (cuts) {
-            for (int i = 0; i < me; ++i) in = over(sh.map[buf][i * width + cp], sh.cut[buf][i * width + cp], in);
-        } else {
-#pragma unroll
-            for (int i = 0; i < MQ - 1; ++i)
-                if (i < me) in = over(sh.map[buf][i * width + cp], false, in);
-        }
-    }
-    return in;
-}
-
-template <bool CL> __device__ __forceinline__ void enter_cluster(ScanShared<CL> &sh, const ScanArgs &P, int width) {
-    if constexpr (CL) Exchange<CL>{sh, P, width}.begin();
-}
-template <bool CL> __device__ __forceinline__ void leave_cluster() {
-    if constexpr (CL) cooperative_groups::this_cluster().sync();   // no block's memory is still written
 }
 
 __device__ __forceinline__ void copies_issued() { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -426,10 +276,10 @@ __global__ void __launch_bounds__(256, 2) scan_forward_kernel(const ScanArgs P) 
     const int width = me.pairs(), Q = me.Q();
     constexpr int MQ = QT ? QT : 8;                // most segments
     F2 carry = me.state(P.h0);                     // read by every block before any can write h_last over it
-    enter_cluster<CL>(sh, P, width);
+    enter_cluster<CL>(sh, P.CT, width);
     if (P.T == 0) {
         if (me.q == 0 && me.rank == 0 && P.last) me.put_state(P.last, carry);
-        leave_cluster<CL>();
+        leave_cluster<CL>(sh);
         return;
     }
     const int64_t first = (me.base + (int64_t)(me.rank * me.span) * P.st) * (int64_t)sizeof(XT);
@@ -496,7 +346,7 @@ __global__ void __launch_bounds__(256, 2) scan_forward_kernel(const ScanArgs P) 
         }
         t0 += me.step;
         bool cuts;
-        F2 h = fold<CL, LOGIT, MQ>(sh, P, me.q, me.cp, width, me.rank, pass, A, B, cut != 0, carry, cuts);
+        F2 h = fold<CL, LOGIT, MQ>(sh, P.CT, me.q, me.cp, width, me.rank, pass, A, B, cut != 0, carry, cuts);
         if (P.saved && t1 && t1 < P.T && t1 % kInterval == 0)
             me.put_state(P.saved + (int64_t)(t1 / kInterval - 1) * P.M, h);
         if (plain) {
@@ -519,7 +369,7 @@ __global__ void __launch_bounds__(256, 2) scan_forward_kernel(const ScanArgs P) 
         if (P.last && left > 0 && left <= S) me.put_state(P.last, h);
         if (!CL && me.q == Q - 1) sh.carry[pass & 1][me.cp] = h;
     }
-    leave_cluster<CL>();
+    leave_cluster<CL>(sh);
 }
 
 template <typename XT, bool WIDE, int S, int QT, bool LOGIT, bool MIX, bool CL>
@@ -534,10 +384,10 @@ __global__ void __launch_bounds__(256, 2) scan_backward_kernel(const ScanArgs P)
     const int width = me.pairs(), Q = me.Q();
     constexpr int MQ = QT ? QT : 8;                // most segments
     F2 carry = me.state(P.glast);                  // read by every block before any can write grad_h0 over it
-    enter_cluster<CL>(sh, P, width);
+    enter_cluster<CL>(sh, P.CT, width);
     if (P.T == 0) {
         if (me.q == 0 && me.rank == 0 && P.gh0) me.put_state(P.gh0, carry);
-        leave_cluster<CL>();
+        leave_cluster<CL>(sh);
         return;
     }
     const int passes = (P.T - 1) / me.step + 1;
@@ -617,7 +467,7 @@ __global__ void __launch_bounds__(256, 2) scan_backward_kernel(const ScanArgs P)
         const int buf = pass & 1, from_end = Q - 1 - me.q;
         ends[buf][me.q * width + me.cp] = B;
         bool cuts;
-        F2 mu = fold<CL, LOGIT, MQ>(sh, P, from_end, me.cp, width, CL ? P.CT - 1 - me.rank : 0, pass, A, L, cut != 0, carry, cuts);
+        F2 mu = fold<CL, LOGIT, MQ>(sh, P.CT, from_end, me.cp, width, CL ? P.CT - 1 - me.rank : 0, pass, A, L, cut != 0, carry, cuts);
         auto step_over = [&](int i, bool with_cuts) {
             const int at = (Q - 1 - i) * width + me.cp;
             h = map_over(sh.map[buf][at].A, ends[buf][i * width + me.cp], with_cuts && sh.cut[buf][at], h);
@@ -673,7 +523,7 @@ __global__ void __launch_bounds__(256, 2) scan_backward_kernel(const ScanArgs P)
         if (t1 == 0 && P.gh0) me.put_state(P.gh0, mu);
         if (!CL && me.q == 0) sh.carry[buf][me.cp] = mu;
     }
-    leave_cluster<CL>();
+    leave_cluster<CL>(sh);
 }
 
 // Step by step, one thread for a channel: rows so far apart that a block's 32-bit offsets
