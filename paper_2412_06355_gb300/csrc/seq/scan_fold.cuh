@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "pairs.cuh"
+#include "waits.cuh"
 
 namespace dendsn {
 
@@ -87,8 +88,7 @@ template <bool CL> struct Exchange {
                          : "=r"(done) : "r"(addr(&sh.arrived[buf])), "r"(parity) : "memory");
             if (done) return true;
             if (i % 64 == 63) {
-                uint64_t now;
-                asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
+                const uint64_t now = now_ns();
                 if (lost()) return false;
                 if (!began) began = now;
                 else if (now - began > 1000000000ull) return false;
@@ -175,8 +175,7 @@ template <bool CL> __device__ __forceinline__ void leave_cluster(ScanShared<CL> 
         cooperative_groups::this_cluster().sync();   // no block sends any more
         // a block that has every map has seen its stores land; one that lost some lets those on
         // their way land first
-        if (Exchange<CL>{sh, 0, 0}.lost())
-            for (int i = 0; i < 1000; ++i) __nanosleep(1000);
+        if (Exchange<CL>{sh, 0, 0}.lost()) let_land();
     }
 }
 

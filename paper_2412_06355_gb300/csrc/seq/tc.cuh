@@ -4,6 +4,8 @@
 #include <cuda.h>
 #include <stdint.h>
 
+#include "waits.cuh"
+
 namespace dendsn {
 namespace tc {
 
@@ -38,11 +40,6 @@ __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
 // One arrival at a barrier of any block of the cluster (an address of in_block).
 __device__ __forceinline__ void bar_arrive_cluster(uint32_t bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ uint64_t now_ns() {
-    uint64_t t;
-    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-    return t;
 }
 constexpr uint64_t kWaitNs = 4000000000ull;   // a wait that lasts longer has failed
 

@@ -662,7 +662,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     if (!ok) g.ctl->failed = 1;
     __syncwarp();
     tc::fence_before_sync();
-    __syncthreads();
+    // where a wait ran out, copies and products may still be on their way: they land before the
+    // pair's shared memory and TMEM are given back
+    if (!__syncthreads_and(ok)) let_land();
     tc::cluster_sync();
     tc::fence_after_sync();
     if (warp == 1) tc::tmem_free(tmem, 512);

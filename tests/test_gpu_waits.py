@@ -24,6 +24,7 @@ def probe(tmp_path_factory):
     lib = ctypes.CDLL(so)
     lib.run_lost_maps.argtypes = [ctypes.c_void_p, ctypes.c_int, ctypes.c_int]
     lib.run_no_arrival.argtypes = [ctypes.c_void_p]
+    lib.run_landing.argtypes = [ctypes.c_void_p]
     return lib
 
 
@@ -65,3 +66,9 @@ def test_a_barrier_without_arrivals(probe):
     began = time.time()
     assert probe.run_no_arrival(out.data_ptr()) == 0
     assert int(out) == 2 and 2.0 < time.time() - began < 10.0
+
+
+def test_memory_is_given_back_late_after_a_wait_that_ran_out(probe):
+    out = torch.zeros(1, dtype=torch.int32, device="cuda")
+    assert probe.run_landing(out.data_ptr()) == 0
+    assert 10000 <= int(out) < 1000000

@@ -39,6 +39,17 @@ __global__ void no_arrival(int *result) {
     *result = tc::bar_wait(tc::smem_addr(&bar), 0) ? 1 : 2;
 }
 
+__global__ void landing(int *us) {
+    const uint64_t began = now_ns();
+    let_land();
+    *us = (int)((now_ns() - began) / 1000);
+}
+
+extern "C" int run_landing(int *us) {
+    landing<<<1, 1>>>(us);
+    const cudaError_t e = cudaGetLastError();
+    return (int)(e != cudaSuccess ? e : cudaDeviceSynchronize());
+}
 extern "C" int run_lost_maps(float *out, int passes, int silent) {
     lost_maps<<<2, 256>>>(reinterpret_cast<float2 *>(out), passes, silent);
     const cudaError_t e = cudaGetLastError();
