@@ -553,9 +553,10 @@ cudaError_t run_backward(const dendsn_embed_config &c, const Plan &pl, const voi
         cfg.attrs = at;
         cfg.numAttrs = 1;
         auto start = [&](auto kernel) {
+            // the limit is the kernel's, not the call's: always the largest, so that no other host
+            // thread lowers it before this launch
             if (cfg.dynamicSmemBytes > 32768) {
-                cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                     (int)cfg.dynamicSmemBytes);
+                cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMapBits / 8);
                 if (e != cudaSuccess) return e;
             }
             return cudaLaunchKernelEx(&cfg, kernel, ids, x);

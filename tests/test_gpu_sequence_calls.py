@@ -1,6 +1,8 @@
 """How the token-sequence operators are called on the GPU: other streams than the current one,
 several host threads, graphs, and the sizes at which other kernels take over."""
 
+import threading
+
 import pytest
 import torch
 
@@ -73,3 +75,37 @@ def test_wrappers_on_a_stream_that_is_not_current(raw):
         side.synchronize()
         for a, b in zip(got, want):
             assert torch.equal(a, b)
+
+
+def test_embedding_gradients_from_two_host_threads():
+    """Two sizes whose index kernels want different amounts of shared memory, called at once."""
+    V, D = 50, 8
+    cases, errors = [], []
+    for n in (300000, 1100000):
+        g = gen(n)
+        ids = torch.randint(0, V, (n,), generator=g, device="cuda")
+        grad = torch.ones((n, D), device="cuda")
+        cfg = binding.make_embed_config(n, V, D)
+        scratch = torch.empty(binding.dendsn_embed_workspace_size(cfg), dtype=torch.uint8, device="cuda")
+        cases.append((cfg, ids, grad, torch.empty(V, D, device="cuda"), scratch,
+                      torch.bincount(ids, minlength=V).float()))
+    torch.cuda.synchronize()
+    go = threading.Barrier(2)
+
+    def work(cfg, ids, grad, out, scratch, _):
+        go.wait()
+        try:
+            for _ in range(1500):
+                binding.dendsn_embed_backward(cfg, ids, grad, out, scratch)
+        except Exception as e:              # noqa: BLE001
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=c) for c in cases]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not errors, errors
+    for _, _, _, out, _, count in cases:
+        assert torch.equal(out, count.unsqueeze(1).expand(V, D))
