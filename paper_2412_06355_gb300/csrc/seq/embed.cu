@@ -24,6 +24,7 @@
 #include <algorithm>
 #include <cmath>
 
+#include "embed_plan.h"
 #include "seq_common.h"
 
 namespace dendsn {
@@ -31,10 +32,8 @@ namespace {
 
 constexpr int kFew = 32;          // positions a warp orders by rank
 constexpr int kTile = 32;         // positions of one partial sum of a longer row
-constexpr int kThreads = 1024;    // of an index block
+constexpr int kThreads = kIndexThreads;
 constexpr int kMapBits = 1 << 20; // positions one pass of the bitmap covers (128 KB)
-constexpr int kFewTokens = 8192;  // tokens and rows up to which a cluster forms the index
-constexpr int kFewRows = 1 << 18;
 constexpr int kRowsOfWarp = 8;      // vocabulary rows of a warp of the sum
 
 // VEC elements: 16 bytes where rows and tensors are aligned to 16 bytes, else one element.
@@ -471,11 +470,15 @@ __global__ void __launch_bounds__(256) embed_join_kernel(T *gtable, Index x, int
     }
 }
 
-constexpr int kSms = 152;
+// SMs of the current device.
+int device_sms() {
+    int dev = 0, n = 0;
+    const bool ok = cudaGetDevice(&dev) == cudaSuccess &&
+                    cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && n > 0;
+    return ok ? n : 1;
+}
 
 struct Plan {
-    bool cluster;                 // the index kernel is one cluster
-    int32_t blocks, chunk;        // of the index kernel, vocabulary rows of one
     int64_t longs, tiles;         // most long rows and tiles there can be
     size_t at[10], scratch;
 };
@@ -493,15 +496,9 @@ dendsn_status make_plan(const dendsn_embed_config *cfg, Plan *pl) {
     // the largest grids: a warp for every kAhead vectors of an output row, and for every row and tile
     if ((cfg->n * (((int64_t)cfg->D + 32 * kAhead - 1) / (32 * kAhead)) + 7) / 8 > INT32_MAX)
         return seq_fail(DENDSN_ERR_UNSUPPORTED, "too many elements (n=%lld D=%d)", (long long)cfg->n, cfg->D);
-    // a block for every 1024 tokens or 4096 rows, at most a cluster's or one for each SM
-    const int64_t blocks = std::max((cfg->n + kThreads - 1) / kThreads, ((int64_t)cfg->V + 4 * kThreads - 1) / (4 * kThreads));
-    pl->cluster = cfg->n <= kFewTokens && cfg->V <= kFewRows;
-    pl->blocks = (int32_t)std::min<int64_t>(blocks, pl->cluster ? 8 : kSms);
-    while (pl->cluster && (pl->blocks & (pl->blocks - 1))) ++pl->blocks;
-    pl->chunk = (int32_t)(((int64_t)cfg->V + pl->blocks - 1) / pl->blocks);
     pl->longs = std::min<int64_t>(cfg->V, cfg->n / (kFew + 1));
     pl->tiles = cfg->n / kTile + pl->longs;
-    const size_t sizes[10] = {(size_t)cfg->V * 4, 16, kSms * 4, (size_t)cfg->V * 4, (size_t)cfg->n * 4,
+    const size_t sizes[10] = {(size_t)cfg->V * 4, 16, kMostIndexBlocks * 4, (size_t)cfg->V * 4, (size_t)cfg->n * 4,
                               (size_t)cfg->n * 4, (size_t)pl->longs * 4, (size_t)pl->longs * 4, (size_t)pl->tiles * 4,
                               (size_t)pl->tiles * cfg->D * 4};
     size_t at = 0;
@@ -527,7 +524,8 @@ cudaError_t run_backward(const dendsn_embed_config &c, const Plan &pl, const voi
                          void *gtable, void *scratch, cudaStream_t s, int *launches) {
     char *p = static_cast<char *>(scratch);
     auto ints = [&](int i) { return reinterpret_cast<int32_t *>(p + pl.at[i]); };
-    Index x{c.n, c.V, c.padding_id, pl.chunk, (int32_t)(std::min<int64_t>(c.n, kMapBits) + 31) / 32, ints(0),
+    const IndexGrid grid = index_grid(c.n, c.V, device_sms());
+    Index x{c.n, c.V, c.padding_id, grid.chunk, (int32_t)(std::min<int64_t>(c.n, kMapBits) + 31) / 32, ints(0),
             reinterpret_cast<unsigned long long *>(p + pl.at[1]), ints(2), ints(3), ints(4), ints(5), ints(6), ints(7),
             ints(8), reinterpret_cast<float *>(p + pl.at[9])};
     const I *ids = static_cast<const I *>(ids_);
@@ -535,16 +533,16 @@ cudaError_t run_backward(const dendsn_embed_config &c, const Plan &pl, const voi
     T *gt = static_cast<T *>(gtable);
     const int32_t nv = c.D / VEC;
     if (c.n > 0) {
-        const bool few = pl.cluster;
+        const bool few = grid.cluster;
         cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3((unsigned)pl.blocks);
+        cfg.gridDim = dim3((unsigned)grid.blocks);
         cfg.blockDim = dim3(kThreads);
         cfg.dynamicSmemBytes = pl.longs > 0 ? (size_t)x.words * 4 * (few ? kThreads / 32 : 1) : 0;
         cfg.stream = s;
         cudaLaunchAttribute at[1];
         if (few) {
             at[0].id = cudaLaunchAttributeClusterDimension;
-            at[0].val.clusterDim.x = (unsigned)pl.blocks;
+            at[0].val.clusterDim.x = (unsigned)grid.blocks;
             at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
         } else {
             at[0].id = cudaLaunchAttributeCooperative;
@@ -569,8 +567,8 @@ cudaError_t run_backward(const dendsn_embed_config &c, const Plan &pl, const voi
     cudaError_t e = seq_launch(embed_sum_kernel<T, VEC>, dim3((unsigned)((warps + 7) / 8)), 256, 0, s, 1, g, gt, x, c.D, nv, c.scale);
     *launches += 1;
     if (e == cudaSuccess && pl.longs > 0) {
-        const dim3 grid((unsigned)((c.D + 255) / 256), (unsigned)std::min<int64_t>(pl.longs, 1024));
-        e = seq_launch(embed_join_kernel<T>, grid, 256, 0, s, 1, gt, x, c.D, c.scale);
+        const dim3 columns((unsigned)((c.D + 255) / 256), (unsigned)std::min<int64_t>(pl.longs, 1024));
+        e = seq_launch(embed_join_kernel<T>, columns, 256, 0, s, 1, gt, x, c.D, c.scale);
         *launches += 1;
     }
     return e;

@@ -6,6 +6,7 @@ import threading
 import pytest
 import torch
 
+import seq_reference as ref
 from paper_2412_06355_gb300 import binding
 
 pytestmark = pytest.mark.gpu
@@ -109,3 +110,34 @@ def test_embedding_gradients_from_two_host_threads():
     assert not errors, errors
     for _, _, _, out, _, count in cases:
         assert torch.equal(out, count.unsqueeze(1).expand(V, D))
+
+
+def test_the_cooperative_index_in_a_cuda_graph():
+    """More than 8192 tokens: captured once, replayed on other tokens and gradients."""
+    n, V, D = 20000, 3000, 40
+    cfg = binding.make_embed_config(n, V, D)
+    scratch = torch.empty(binding.dendsn_embed_workspace_size(cfg), dtype=torch.uint8, device="cuda")
+
+    def inputs(seed):
+        g = gen(seed)
+        ids = torch.randint(0, V, (n,), generator=g, device="cuda")
+        ids[::3] = 7
+        return ids, torch.randn((n, D), generator=g, device="cuda")
+
+    ids, grad = inputs(1)
+    out = torch.empty(V, D, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        binding.dendsn_embed_backward(cfg, ids, grad, out, scratch)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        binding.dendsn_embed_backward(cfg, ids, grad, out, scratch)
+    for seed in (2, 3):
+        new = inputs(seed)
+        ids.copy_(new[0])
+        grad.copy_(new[1])
+        graph.replay()
+        torch.cuda.synchronize()
+        ref.check("gtable", out, ref.embed_backward(ids, grad, V, 1.0, None))

@@ -1,11 +1,12 @@
 """Host-side checks of the token-sequence operators' options: no GPU, no kernel is launched."""
 import contextlib
+import subprocess
 
 import pytest
 import torch
 
 import test_abi_host
-from paper_2412_06355_gb300 import binding
+from paper_2412_06355_gb300 import binding, build
 
 
 def test_logit_grad_is_checked():
@@ -107,3 +108,35 @@ def test_statistics_are_checked():
     assert test_abi_host.status_of(binding.dendsn_xent_workspace_size, cfg) == 1
     with pytest.raises(ValueError, match="statistics"):
         binding.make_xent_config(10, 20, 8, "bf16", statistics="sum")
+
+
+# ------------------------------------------------------------------ the embedding's index
+INDEX_GRID = r"""
+#include <stdio.h>
+#include "seq/embed_plan.h"
+int main() {
+    long long n, V;
+    int sms;
+    while (scanf("%lld %lld %d", &n, &V, &sms) == 3) {
+        const dendsn::IndexGrid g = dendsn::index_grid(n, V, sms);
+        printf("%d %d %d\n", (int)g.cluster, g.blocks, g.chunk);
+    }
+}
+"""
+
+
+def test_the_index_grid_fits_the_device(tmp_path):
+    """A cooperative grid with more blocks than run at the same time is refused at the launch."""
+    src, exe = tmp_path / "grid.cpp", str(tmp_path / "grid")
+    src.write_text(INDEX_GRID)
+    subprocess.run(["g++", "-std=c++17", f"-I{build.CSRC}", str(src), "-o", exe], check=True)
+    cases = [(n, V, sms) for n in (1, 1000, 8192, 8193, 100000, 155648, 151553, 2 ** 31 - 1)
+             for V in (1, 5000, 2 ** 18, 2 ** 18 + 1, 2 ** 31 - 1) for sms in (1, 7, 76, 148, 152, 200)]
+    out = subprocess.run([exe], input="\n".join("%d %d %d" % c for c in cases), check=True,
+                         capture_output=True, text=True).stdout.split("\n")
+    for (n, V, sms), line in zip(cases, out):
+        cluster, blocks, chunk = (int(v) for v in line.split())
+        assert 1 <= blocks <= (8 if cluster else min(sms, 152)), (n, V, sms)
+        assert blocks * chunk >= V and (not cluster or blocks in (1, 2, 4, 8))
+        if sms >= 152 and not cluster:
+            assert blocks == min(152, max(-(-n // 1024), -(-V // 4096)))
