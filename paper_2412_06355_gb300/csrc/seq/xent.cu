@@ -908,7 +908,7 @@ struct Plan {
     int32_t parts;                  // partial maxima and sums of a row
     // offsets in the scratch buffer
     size_t index, label, where, lse, scale, weight, picked, part, H, W, G, sum;
-    size_t fwd, bwd;
+    size_t bytes;                   // of the scratch buffer, for the pass that was asked for
 };
 
 int32_t up(int64_t v, int64_t to) { return (int32_t)((v + to - 1) / to * to); }
@@ -945,6 +945,7 @@ void choose_pieces(Plan *pl) {
 }
 
 dendsn_status make_plan(const dendsn_xent_config *cfg, bool backward, Plan *pl) {
+    *pl = Plan{};
     if (!cfg) return seq_fail(DENDSN_ERR_INVALID_ARG, "cfg is NULL");
     if (cfg->M < 0 || cfg->V < 1 || cfg->D < 1)
         return seq_fail(DENDSN_ERR_INVALID_ARG, "bad size (M=%d V=%d D=%d)", cfg->M, cfg->V, cfg->D);
@@ -985,19 +986,19 @@ dendsn_status make_plan(const dendsn_xent_config *cfg, bool backward, Plan *pl) 
     p.H = take(packed ? (size_t)p.terms * p.Mp * p.Dp * 2 : 0);
     // weights are packed unless their rows can be copied as they are (also asked of their address)
     p.W = take(packed ? (size_t)p.terms * cfg->V * p.Dp * 2 : 0);
-    const size_t shared = at;
-    p.picked = take(p.Mp * 4);
-    p.parts = p.few ? up(cfg->V, kFewV) / kFewV : 2 * p.nt;
-    p.part = take((size_t)p.parts * p.Mp * 8);
-    p.fwd = at;
-    if (!backward) return DENDSN_OK;
-    at = shared;
+    if (!backward) {
+        p.picked = take(p.Mp * 4);
+        p.parts = p.few ? up(cfg->V, kFewV) / kFewV : 2 * p.nt;
+        p.part = take((size_t)p.parts * p.Mp * 8);
+        p.bytes = at;
+        return DENDSN_OK;
+    }
     p.lse = take(p.Mp * 4);
     p.scale = take(p.Mp * 4);
     p.weight = take(p.Mp * 4);
     p.G = take((size_t)p.gterms * p.Mp * p.pitch * 2);
     p.sum = take((size_t)p.splits * p.Mp * p.Dq * 4);
-    p.bwd = at;
+    p.bytes = at;
     return DENDSN_OK;
 }
 
@@ -1248,11 +1249,12 @@ extern "C" {
 
 dendsn_status dendsn_xent_workspace_size(const dendsn_xent_config *cfg, size_t *forward_bytes,
                                          size_t *backward_bytes) {
-    Plan pl;
-    dendsn_status st = make_plan(cfg, backward_bytes != nullptr, &pl);
+    Plan forward, backward;
+    dendsn_status st = make_plan(cfg, false, &forward);
+    if (st == DENDSN_OK && backward_bytes) st = make_plan(cfg, true, &backward);
     if (st != DENDSN_OK) return st;
-    if (forward_bytes) *forward_bytes = pl.fwd;
-    if (backward_bytes) *backward_bytes = pl.bwd;
+    if (forward_bytes) *forward_bytes = forward.bytes;
+    if (backward_bytes) *backward_bytes = backward.bytes;
     return DENDSN_OK;
 }
 

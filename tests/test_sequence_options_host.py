@@ -1,5 +1,6 @@
 """Host-side checks of the token-sequence operators' options: no GPU, no kernel is launched."""
 import contextlib
+import ctypes
 import subprocess
 
 import pytest
@@ -140,3 +141,18 @@ def test_the_index_grid_fits_the_device(tmp_path):
         assert blocks * chunk >= V and (not cluster or blocks in (1, 2, 4, 8))
         if sms >= 152 and not cluster:
             assert blocks == min(152, max(-(-n // 1024), -(-V // 4096)))
+
+
+# ------------------------------------------------------------------ scratch of the cross entropy
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,V,D", [(1, 1000, 64), (16, 131072, 1024), (32, 5000, 100),
+                                   (33, 5000, 100), (4096, 50000, 1024)])
+def test_scratch_sizes_do_not_depend_on_what_else_is_asked(dtype, M, V, D):
+    lib, cfg = binding.load(), binding.make_xent_config(M, V, D, dtype)
+    size = [ctypes.c_size_t(0) for _ in range(4)]
+    ask = lambda f, b: lib.dendsn_xent_workspace_size(ctypes.byref(cfg), f, b)
+    assert ask(ctypes.byref(size[0]), ctypes.byref(size[1])) == 0
+    assert ask(ctypes.byref(size[2]), None) == 0 and ask(None, ctypes.byref(size[3])) == 0
+    assert size[0].value == size[2].value and size[1].value == size[3].value
+    if dtype == "f32" and M <= 32:             # no copy of the weights
+        assert size[0].value < V * D * 4
