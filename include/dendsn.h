@@ -354,6 +354,8 @@ typedef struct {
     int32_t labels_dtype;   /* dendsn_index of labels */
     int32_t logit_grad;     /* dendsn_logit_grad; float32 inputs: SPLIT (three terms) */
     int32_t statistics;     /* dendsn_statistics of lse */
+    int32_t weight_aligned; /* 1: weight is 16-byte aligned. Scratch then has no room for a copy of
+                               bfloat16 weights with D a multiple of 8, which are read in place */
 } dendsn_xent_config;
 
 dendsn_status dendsn_xent_workspace_size(const dendsn_xent_config *cfg, size_t *forward_bytes,

@@ -97,7 +97,7 @@ class dendsn_xent_config(ctypes.Structure):
     _fields_ = [("ignore_index", ctypes.c_int64), ("M", ctypes.c_int32), ("V", ctypes.c_int32),
                 ("D", ctypes.c_int32), ("x_dtype", ctypes.c_int32),
                 ("labels_dtype", ctypes.c_int32), ("logit_grad", ctypes.c_int32),
-                ("statistics", ctypes.c_int32)]
+                ("statistics", ctypes.c_int32), ("weight_aligned", ctypes.c_int32)]
 
 
 def _code(what, value, codes):
@@ -134,15 +134,17 @@ def make_scan_config(T, B, N, dtype="f32", gate="decay", mix="plain",
 
 def make_xent_config(M, V, D, dtype="f32", ignore_index=-100,
                      labels_dtype="i64", logit_grad="split",
-                     statistics="lse") -> dendsn_xent_config:
+                     statistics="lse", weight_aligned=False) -> dendsn_xent_config:
     """logit_grad: how bfloat16 products take the logits' gradient, "split" in two terms or "bf16"
     rounded to one (faster; an error of up to 2^-8 of each). statistics: the rows that the forward
     leaves for the backward, "lse" [M] (rounded to float32) or "max_sum" [2, M], each row's largest
-    logit and the sum relative to it, which keep the probabilities' precision."""
+    logit and the sum relative to it, which keep the probabilities' precision. weight_aligned: the
+    weight's address is a multiple of 16 bytes, so that scratch needs no room for a copy of it (the
+    wrappers that allocate their scratch find out by themselves)."""
     return dendsn_xent_config(ignore_index, M, V, D, _code("dtype", dtype, _DTYPES),
                               _code("labels_dtype", labels_dtype, _INDEX),
                               _code("logit_grad", logit_grad, _LOGIT_GRADS),
-                              _code("statistics", statistics, _STATISTICS))
+                              _code("statistics", statistics, _STATISTICS), int(weight_aligned))
 
 
 class dendsn_lif_config(ctypes.Structure):
@@ -584,6 +586,14 @@ def _xent_scratch(cfg, backward) -> int:
     return b.value
 
 
+def _for_weight(cfg, weight):
+    """cfg with weight_aligned where that saves scratch and is so."""
+    if cfg.x_dtype == BF16 and cfg.D % 8 == 0 and not cfg.weight_aligned and weight.data_ptr() % 16 == 0:
+        cfg = dendsn_xent_config.from_buffer_copy(cfg)
+        cfg.weight_aligned = 1
+    return cfg
+
+
 def _statistics_shape(cfg):
     return (2, cfg.M) if cfg.statistics == STATISTICS_MAX_SUM else (cfg.M,)
 
@@ -633,10 +643,11 @@ def dendsn_xent_backward(cfg, hidden, weight, labels, lse, grad_loss, grad_hidde
 def xent_forward(cfg, hidden, weight, labels, scratch=None, stream=None):
     """Allocating cross entropy of hidden [M, D] read out by weight [V, D]: (loss [M], lse), lse
     [M] or, where the config's statistics are "max_sum", [2, M]."""
-    need = _xent_scratch(cfg, False)
     if scratch is None:
-        scratch = _scratch(need, hidden.device)
-    _bytes("scratch", scratch, need)
+        cfg = _for_weight(cfg, weight)
+        scratch = _scratch(_xent_scratch(cfg, False), hidden.device)
+    else:
+        _bytes("scratch", scratch, _xent_scratch(cfg, False))
     loss = torch.empty((cfg.M,), dtype=torch.float32, device=hidden.device)
     lse = torch.empty(_statistics_shape(cfg), dtype=torch.float32, device=hidden.device)
     _xent_forward(cfg, hidden, weight, labels, loss, lse, scratch, stream)
@@ -646,10 +657,11 @@ def xent_forward(cfg, hidden, weight, labels, scratch=None, stream=None):
 @_allocates
 def xent_backward(cfg, hidden, weight, labels, lse, grad_loss, scratch=None, stream=None):
     """Allocating backward. Returns dict ghidden [M, D], gweight [V, D] in hidden's dtype."""
-    need = _xent_scratch(cfg, True)
     if scratch is None:
-        scratch = _scratch(need, hidden.device)
-    _bytes("scratch", scratch, need)
+        cfg = _for_weight(cfg, weight)
+        scratch = _scratch(_xent_scratch(cfg, True), hidden.device)
+    else:
+        _bytes("scratch", scratch, _xent_scratch(cfg, True))
     out = dict(ghidden=torch.empty_like(hidden), gweight=torch.empty_like(weight))
     _xent_backward(cfg, hidden, weight, labels, lse, grad_loss, out["ghidden"],
                          out["gweight"], scratch, stream)

@@ -957,6 +957,7 @@ dendsn_status make_plan(const dendsn_xent_config *cfg, bool backward, Plan *pl) 
         return seq_fail(DENDSN_ERR_INVALID_ARG, "bad logit_grad %d", cfg->logit_grad);
     if (cfg->logit_grad == DENDSN_LOGIT_GRAD_BF16 && cfg->x_dtype == DENDSN_F32)
         return seq_fail(DENDSN_ERR_INVALID_ARG, "a bfloat16 logit_grad is for bfloat16 operands");
+    if (cfg->weight_aligned & ~1) return seq_fail(DENDSN_ERR_INVALID_ARG, "weight_aligned must be 0 or 1");
     if (cfg->statistics != DENDSN_STATISTICS_LSE && cfg->statistics != DENDSN_STATISTICS_MAX_SUM)
         return seq_fail(DENDSN_ERR_INVALID_ARG, "bad statistics %d", cfg->statistics);
     if (cfg->M > (1 << 30) || cfg->V > (1 << 30) || cfg->D > (1 << 24))
@@ -984,8 +985,10 @@ dendsn_status make_plan(const dendsn_xent_config *cfg, bool backward, Plan *pl) 
     p.few = cfg->x_dtype == DENDSN_F32 && cfg->M <= kFewF32 && cfg->statistics == DENDSN_STATISTICS_LSE;
     const bool packed = backward || !p.few;
     p.H = take(packed ? (size_t)p.terms * p.Mp * p.Dp * 2 : 0);
-    // weights are packed unless their rows can be copied as they are (also asked of their address)
-    p.W = take(packed ? (size_t)p.terms * cfg->V * p.Dp * 2 : 0);
+    // weights are packed unless their rows can be copied as they are, which also their address
+    // decides: the caller may say that it is aligned
+    const bool as_they_are = cfg->x_dtype == DENDSN_BF16 && cfg->D % 8 == 0 && cfg->weight_aligned;
+    p.W = take(packed && !as_they_are ? (size_t)p.terms * cfg->V * p.Dp * 2 : 0);
     if (!backward) {
         p.picked = take(p.Mp * 4);
         p.parts = p.few ? up(cfg->V, kFewV) / kFewV : 2 * p.nt;
@@ -1271,6 +1274,8 @@ dendsn_status dendsn_xent_forward(const dendsn_xent_config *cfg, const void *hid
     if (!seq_aligned(hidden, bf ? 2 : 4) || !seq_aligned(weight, bf ? 2 : 4) || !seq_aligned(labels, i64 ? 8 : 4) ||
         !seq_aligned(loss, 4) || !seq_aligned(lse, 4))
         return seq_fail(DENDSN_ERR_MISALIGNED, "a tensor is misaligned");
+    if (cfg->weight_aligned && !seq_aligned(weight, 16))
+        return seq_fail(DENDSN_ERR_MISALIGNED, "weight is not 16-byte aligned, as weight_aligned says");
     if (!scratch) return seq_fail(DENDSN_ERR_INVALID_ARG, "scratch is NULL");
     if (!seq_aligned(scratch, 256)) return seq_fail(DENDSN_ERR_MISALIGNED, "scratch must be 256-byte aligned");
     c.cfg = cfg;
@@ -1297,6 +1302,8 @@ dendsn_status dendsn_xent_backward(const dendsn_xent_config *cfg, const void *hi
         !seq_aligned(grad_weight, sx) || !seq_aligned(labels, i64 ? 8 : 4) || !seq_aligned(lse, 4) ||
         !seq_aligned(grad_loss, 4))
         return seq_fail(DENDSN_ERR_MISALIGNED, "a tensor is misaligned");
+    if (cfg->weight_aligned && !seq_aligned(weight, 16))
+        return seq_fail(DENDSN_ERR_MISALIGNED, "weight is not 16-byte aligned, as weight_aligned says");
     if (!scratch) return seq_fail(DENDSN_ERR_INVALID_ARG, "scratch is NULL");
     if (!seq_aligned(scratch, 256)) return seq_fail(DENDSN_ERR_MISALIGNED, "scratch must be 256-byte aligned");
     c.cfg = cfg;

@@ -176,3 +176,20 @@ def test_statistics_as_maximum_and_sum(dtype, M):
             ref.check(k, out[form][2][k], want[k])
     with pytest.raises(ValueError, match="lse"):
         binding.xent_backward(cfg, H, W, y, out["lse"][1], c)
+
+
+@pytest.mark.parametrize("M", [20, 300])
+@pytest.mark.parametrize("offset", [0, 1])
+def test_weights_read_in_place_or_copied_give_the_same(M, offset):
+    H, W, y, c = inputs(M, 500, 72, torch.bfloat16, 12)
+    buf = torch.empty(500 * 72 + 8, dtype=torch.bfloat16, device="cuda")
+    moved = buf[offset:offset + 500 * 72].view(500, 72).copy_(W)
+    cfg = binding.make_xent_config(M, 500, 72, "bf16")
+    sizes = binding.dendsn_xent_workspace_size(cfg)
+    scratch = torch.empty(max(sizes), dtype=torch.uint8, device="cuda")
+    want = binding.xent_forward(cfg, H, W, y, scratch)
+    got = binding.xent_forward(cfg, H, moved, y)
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    a = binding.xent_backward(cfg, H, W, y, want[1], c, scratch)
+    b = binding.xent_backward(cfg, H, moved, y, want[1], c)
+    assert all(torch.equal(a[k], b[k]) for k in a)

@@ -156,3 +156,40 @@ def test_scratch_sizes_do_not_depend_on_what_else_is_asked(dtype, M, V, D):
     assert size[0].value == size[2].value and size[1].value == size[3].value
     if dtype == "f32" and M <= 32:             # no copy of the weights
         assert size[0].value < V * D * 4
+
+
+def test_scratch_without_a_copy_of_aligned_weights():
+    """bfloat16 weights whose rows are read in place take no room in either pass."""
+    M, V, D = 64, 100000, 1024
+    free = binding.dendsn_xent_workspace_size(binding.make_xent_config(M, V, D, "bf16"))
+    sure = binding.dendsn_xent_workspace_size(binding.make_xent_config(M, V, D, "bf16", weight_aligned=True))
+    assert all(a - b >= V * D * 2 for a, b in zip(free, sure)) and sure[0] < V * D * 2 / 10
+    for kw in (dict(dtype="f32", D=1024), dict(dtype="bf16", D=1023)):      # copied in any case
+        a, b = (binding.dendsn_xent_workspace_size(binding.make_xent_config(M, V, weight_aligned=w, **kw))
+                for w in (False, True))
+        assert a == b
+    cfg = binding.make_xent_config(4, 20, 8, "bf16")
+    cfg.weight_aligned = 2
+    assert test_abi_host.status_of(binding.dendsn_xent_workspace_size, cfg) == 1
+    lib, P = binding.load(), ctypes.c_void_p
+    ok, odd = P(4096), P(4104)
+    x = ctypes.byref(binding.make_xent_config(4, 20, 8, "bf16", weight_aligned=True))
+    assert lib.dendsn_xent_forward(x, ok, odd, ok, ok, ok, ok, None) == 3
+    assert b"weight_aligned" in lib.dendsn_last_error()
+    assert lib.dendsn_xent_backward(x, ok, odd, ok, ok, ok, ok, ok, ok, None) == 3
+
+
+@pytest.mark.parametrize("offset,aligned", [(0, 1), (8, 1), (3, 0)])
+def test_wrappers_ask_the_weights_address(offset, aligned, monkeypatch):
+    Recorder(monkeypatch)
+    cfg = binding.make_xent_config(4, 100, 64, "bf16")
+    buf = torch.zeros(100 * 64 + 64, dtype=torch.bfloat16)
+    first = (-buf.data_ptr() // 2) % 8 + offset
+    w, h = buf[first:first + 6400].view(100, 64), torch.zeros(4, 64, dtype=torch.bfloat16)
+    asked = []
+    real = binding._xent_scratch
+    monkeypatch.setattr(binding, "_xent_scratch", lambda c, b: asked.append(c.weight_aligned) or real(c, b))
+    y, r = torch.zeros(4, dtype=torch.int64), torch.zeros(4)
+    binding.xent_forward(cfg, h, w, y)
+    binding.xent_backward(cfg, h, w, y, r, r)
+    assert asked == [aligned, aligned] and cfg.weight_aligned == 0
