@@ -13,6 +13,9 @@
 // back through the same slots, to be written 16 bytes at a time.
 // A start makes its segment's map constant; that is kept as a flag and selected, not
 // multiplied by zero, so that what came before it cannot leak as NaN.
+// Products of decays above 1 are kept as mantissa and exponent, so that they may leave float32 where
+// the states do not (decays of at most 1 only pay for the look at them: 16384 steps of 1024 float32
+// channels, forward and backward, 133 -> 138 us).
 //
 // The backward runs the passes from the last step to the first with the map
 // mu -> A mu + L of mu[t] = a[t] (grad_h[t] + mu[t+1]), and recomputes h from x, gate and the
@@ -345,8 +348,10 @@ __global__ void __launch_bounds__(256, 2) scan_forward_kernel(const ScanArgs P) 
                 }
         }
         t0 += me.step;
-        bool cuts;
-        F2 h = fold<CL, LOGIT, MQ>(sh, P.CT, me.q, me.cp, width, me.rank, pass, A, B, cut != 0, carry, cuts);
+        int flag = cut ? kCut : 0;
+        if (!LOGIT && !cut) flag = growth<S>(a, left, A);
+        bool flags;
+        F2 h = fold<CL, LOGIT, MQ>(sh, P.CT, me.q, me.cp, width, me.rank, pass, A, B, flag, carry, flags);
         if (P.saved && t1 && t1 < P.T && t1 % kInterval == 0)
             me.put_state(P.saved + (int64_t)(t1 / kInterval - 1) * P.M, h);
         if (plain) {
@@ -466,21 +471,14 @@ __global__ void __launch_bounds__(256, 2) scan_backward_kernel(const ScanArgs P)
         start = begin(t0);
         const int buf = pass & 1, from_end = Q - 1 - me.q;
         ends[buf][me.q * width + me.cp] = B;
-        bool cuts;
-        F2 mu = fold<CL, LOGIT, MQ>(sh, P.CT, from_end, me.cp, width, CL ? P.CT - 1 - me.rank : 0, pass, A, L, cut != 0, carry, cuts);
-        auto step_over = [&](int i, bool with_cuts) {
-            const int at = (Q - 1 - i) * width + me.cp;
-            h = map_over(sh.map[buf][at].A, ends[buf][i * width + me.cp], with_cuts && sh.cut[buf][at], h);
-        };
-        if (cuts) {
-#pragma unroll
-            for (int i = 0; i < MQ - 1; ++i)
-                if (i < me.q) step_over(i, true);
-        } else {
-#pragma unroll
-            for (int i = 0; i < MQ - 1; ++i)
-                if (i < me.q) step_over(i, false);
-        }
+        int flag = cut ? kCut : 0;
+        if (!LOGIT && !cut) flag = growth<S>(a, left, A);
+        bool flags;
+        F2 mu = fold<CL, LOGIT, MQ>(sh, P.CT, from_end, me.cp, width, CL ? P.CT - 1 - me.rank : 0, pass, A, L, flag, carry, flags);
+        // the forward maps have the same products of decays
+        auto map = [&](int i) { return Map{sh.map[buf][(Q - 1 - i) * width + me.cp].A, ends[buf][i * width + me.cp]}; };
+        auto flag_of = [&](int i) { return sh.flag[buf][(Q - 1 - i) * width + me.cp]; };
+        h = flags ? fold_before<LOGIT, MQ, true>(me.q, h, map, flag_of) : fold_before<LOGIT, MQ, false>(me.q, h, map, flag_of);
         F2 before[S];
         // gradients of step s, from the state before it and mu after it
         auto gradients = [&](int s, F2 ga) {

@@ -15,7 +15,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(256) lost_maps(float
     const int rank = blockIdx.x, me = threadIdx.x / 16, cp = threadIdx.x % 16;
     for (int i = threadIdx.x; i < 2 * 8 * 32; i += 256) {
         (&sh.block[0][0][0])[i] = Map{both(1.f), both(7.f)};
-        (&sh.block_cut[0][0][0])[i] = 1;
+        (&sh.block_flag[0][0][0])[i] = kCut;
     }
     __syncthreads();
     enter_cluster<true>(sh, 2, 16);
@@ -25,7 +25,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(256) lost_maps(float
             bool cuts;
             // every segment doubles the state; a sequence starts in segment 12 of the last pass
             const bool cut = pass == passes - 1 && me == 12;
-            const F2 in = fold<true, true, 16>(sh, 2, me, cp, 16, rank, pass, both(2.f), both(cut ? 5.f : 0.f), cut, carry, cuts);
+            const F2 in = fold<true, true, 16>(sh, 2, me, cp, 16, rank, pass, both(2.f), both(cut ? 5.f : 0.f), cut ? kCut : 0, carry, cuts);
             out[((rank * passes + pass) * 16 + me) * 16 + cp] = make_float2(in.x(), in.y());
         }
     }
