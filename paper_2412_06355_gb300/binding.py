@@ -14,6 +14,7 @@ import threading
 from typing import Optional
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import build as _build
 
@@ -765,6 +766,7 @@ class DendSNFunction(torch.autograd.Function):
         return s
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, gs):
         x, a, xi, zeta, kappa, mask = ctx.saved_tensors
         saved, scratch = ctx.ws
@@ -801,6 +803,7 @@ class EmbedFunction(torch.autograd.Function):
         return embed_forward(ctx.cfg, table.contiguous(), ids)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, g):
         ids, = ctx.saved_tensors
         return embed_backward(ctx.cfg, ids, g.contiguous()), None, None, None
@@ -824,6 +827,7 @@ class ScanFunction(torch.autograd.Function):
         return h, last
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, gh, glast):
         x, gate, starts, h0 = ctx.saved_tensors
         g = scan_backward(ctx.cfg, x, gate, gh.contiguous(), starts, h0,
@@ -846,6 +850,7 @@ class XentFunction(torch.autograd.Function):
         return loss
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, gloss):
         hidden, weight, labels, lse = ctx.saved_tensors
         g = xent_backward(ctx.cfg, hidden, weight, labels, lse, gloss.float().contiguous())
