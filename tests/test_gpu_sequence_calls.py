@@ -141,3 +141,48 @@ def test_the_cooperative_index_in_a_cuda_graph():
         graph.replay()
         torch.cuda.synchronize()
         ref.check("gtable", out, ref.embed_backward(ids, grad, V, 1.0, None))
+
+
+def test_operators_from_two_host_threads_on_their_own_streams():
+    """Each thread gets the bits of a run alone."""
+    def inputs(M, seed):
+        g = gen(seed)
+        V, D = 900, 64
+        W = torch.randn((V, D), generator=g, device="cuda").bfloat16()
+        y = torch.randint(0, V, (M,), generator=g, device="cuda")
+        return (M, V, D, W, y, torch.rand(M, generator=g, device="cuda"))
+
+    def step(M, V, D, W, y, c):
+        cx = binding.make_xent_config(M, V, D, "bf16")
+        ce = binding.make_embed_config(M, V, D, "bf16")
+        cs = binding.make_scan_config(M, 1, D, "bf16", "logit", "complement")
+        e = binding.embed_forward(ce, W, y).view(M, 1, D)
+        saved = binding.scan_workspace(cs)
+        h, _ = binding.scan_forward(cs, e, e, saved=saved)
+        loss, lse = binding.xent_forward(cx, h.view(M, D), W, y)
+        g = binding.xent_backward(cx, h.view(M, D), W, y, lse, c)
+        gs = binding.scan_backward(cs, e, e, g["ghidden"].view(M, 1, D), saved=saved)
+        return [loss, g["gweight"], binding.embed_backward(ce, y, gs["gx"].view(M, D))]
+
+    data = [inputs(700, 1), inputs(3000, 2)]
+    want = [step(*d) for d in data]
+    torch.cuda.synchronize()
+    go, errors = threading.Barrier(2), []
+
+    def work(k):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                go.wait()
+                for _ in range(100):
+                    got = step(*data[k])
+                torch.cuda.current_stream().synchronize()
+                assert all(torch.equal(a, b) for a, b in zip(got, want[k]))
+        except Exception as e:              # noqa: BLE001
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors
