@@ -22,7 +22,7 @@
 // reach a product as 0 * inf. That copy also gives rows of any D the 16-byte pitch that
 // tensor copies need, and float32 operands their three bfloat16 terms: x = x0 + x1 + x2 with
 // 8 bits each; the products x_i y_j with i + j <= 2 are summed, the smallest first, and the
-// others are below 2^-26 of x y.
+// others are at most 2^-24 of x y together.
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -71,8 +71,8 @@ __device__ __forceinline__ uint32_t two(__nv_bfloat16 a, __nv_bfloat16 b) {
     return (uint32_t)__bfloat16_as_ushort(a) | (uint32_t)__bfloat16_as_ushort(b) << 16;
 }
 
-// Term `term` of x = x0 + x1 + x2. A finite x whose rounding would overflow is truncated; what
-// is not finite stays in the first term alone.
+// The terms of x = x0 + x1 + x2, each the rounding of what the ones before it leave. A finite x whose
+// rounding would overflow is truncated; what is not finite stays in the first term alone.
 __device__ __forceinline__ void split(float x, __nv_bfloat16 (&t)[3]) {
     t[0] = __float2bfloat16_rn(x);
     if (!isfinite(__bfloat162float(t[0]))) {

@@ -193,3 +193,20 @@ def test_weights_read_in_place_or_copied_give_the_same(M, offset):
     a = binding.xent_backward(cfg, H, W, y, want[1], c, scratch)
     b = binding.xent_backward(cfg, H, moved, y, want[1], c)
     assert all(torch.equal(a[k], b[k]) for k in a)
+
+
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_terms_that_are_left_out_of_float32_products(sign):
+    """Operands whose left-out products of terms all have one sign, 2^-24 of each product: the
+    logit, which the loss of a hopeless label is, stays within that, its sum's roundings (at most
+    2^-23 of the running sum for each of 10 instructions, which are partial) and its own."""
+    x = 1 + 2.0 ** -9 * (1 + 126 / 128 + 1 / 256)
+    M, V, D = 40, 300, 64
+    H = torch.full((M, D), x, device="cuda")
+    W = torch.zeros(V, D, device="cuda")
+    W[7] = sign * x
+    y = torch.full((M,), 3 if sign > 0 else 7, device="cuda")
+    loss, _ = binding.xent_forward(binding.make_xent_config(M, V, D), H, W, y)
+    l = D * float(torch.tensor(x)) ** 2
+    want = l if sign > 0 else math.log(V - 1) + l
+    assert bool(((loss.double() - want).abs() <= l * 2.0 ** -21 + 2.0 ** -20).all())
