@@ -328,12 +328,13 @@ dendsn_status dendsn_scan_backward(const dendsn_scan_config *cfg, const void *x,
  * A row whose label is ignore_index has loss 0, lse 0 and zero gradient, whatever its hidden
  * values are (also infinities and NaN). A row with any other label outside [0, V) has loss,
  * lse and grad_hidden NaN and takes no part in grad_weight.
- * bfloat16 inputs: products are exact and sums float32; the two products that take G have it as
- * the sum of two bfloat16 terms (logit_grad SPLIT, within 2^-16), or rounded to one where the
- * caller chooses so (logit_grad BF16: two fifths fewer operations in the backward, and a rounding of
- * up to 2^-8 of each logit's gradient beside the output's own). float32 inputs: every operand is
- * split into three bfloat16 terms, whose six leading products are summed (a relative error of
- * about 2^-24 of each product); the forward of up to 32 rows multiplies and adds in float32.
+ * bfloat16 inputs: products are exact, sums float32 in the tensor cores (which cost the losses 8e-7
+ * of their norm at D = 2048); the two products that take G have it as the sum of two bfloat16
+ * terms (logit_grad SPLIT, within 2^-16), or rounded to one where the caller chooses so (logit_grad
+ * BF16: two fifths fewer operations in the backward, and a rounding of up to 2^-8 of each logit's
+ * gradient beside the output's own). float32 inputs: every operand is split into three bfloat16
+ * terms, whose six leading products are summed (a relative error of about 2^-24 of each product);
+ * the forward of up to 32 rows multiplies and adds in float32.
  * What the forward leaves in lse for the backward (statistics): LSE, lse [M] as above, whose
  * rounding is an error of up to 2^-24 |lse| of every probability in the backward; for up to 32
  * float32 rows the logits that the backward forms are also rounded otherwise than the forward's.

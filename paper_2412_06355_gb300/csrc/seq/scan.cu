@@ -24,10 +24,10 @@
 //
 // Bound: 6 (forward) and 10 bytes (backward) of a bfloat16 element against the instructions on
 // it; the arithmetic runs on pairs (f32x2), which halves it. Measured, 2048 steps of 65536
-// bfloat16 channels, logistic decays, sequence starts: forward 151 us (5.3 TB/s), backward 272 us
-// (4.9 TB/s; 40 instructions an element); their 1024 blocks are 3.4 rounds of the 304 that fit.
-// 16384 steps of 1024 float32 channels: 48 us (4.2 TB/s) and 109 us (3.1 TB/s), 256 blocks in
-// clusters of 8 along time. One step of 262144 bfloat16 channels: 7 us, a launch.
+// bfloat16 channels, logistic decays, sequence starts: forward 148 us (5.5 TB/s), backward 277 us
+// (4.8 TB/s); their 1024 blocks are 3.4 rounds of the 304 that fit.
+// 16384 steps of 1024 float32 channels: 49 us (4.1 TB/s) and 98 us (3.4 TB/s), 256 blocks in
+// clusters of 8 along time. One step of 262144 bfloat16 channels: 8 us, a launch and one pass's latency.
 #include <cuda_bf16.h>
 
 #include <algorithm>

@@ -11,11 +11,17 @@
 //   WEIGHT  grad_weight of the piece = G^T H
 // so 2 M V D operations in the forward; in the backward 10 M V D for bfloat16 operands with G in
 // two terms (6 M V D with G rounded to one, which the caller may choose), of which 2 M V D form the
-// logits again instead of keeping M V of them. G in one term costs 8192 rows, V = 131072, D = 2048
-// 10.4 ms forward and backward, in two 15.6 ms; the error of the gradients against 64 bits is 2.4e-3 and
-// 1.7e-3, that of rounding the exact gradients. Bound by the tensor cores: the forward of that
-// size takes 2.34-2.49 ms (1.7-1.9 PFLOP/s) under the card's power limit, where cuBLAS sustains 1.75.
-// Few rows are bound by reading the weights and by three launches (16 rows, V = 32768, D = 384: 15 us).
+// logits again instead of keeping M V of them. Forward and backward of 8192 rows, V = 131072, D = 2048
+// take 10.4 ms with G in one term and 15.4 ms in two; the error of the gradients against 64 bits is
+// 2.4e-3 and 1.7e-3, that of rounding the exact gradients. Bound by the tensor cores: that size takes
+// 2.36-2.41 ms forward and 12.8 ms backward (1.7-1.8 PFLOP/s) under the card's power limit, where cuBLAS
+// sustains 1.75; 4096 rows, V = 50000, D = 1024: 228 and 1270 us. Few rows are bound by reading
+// the weights and by three launches (16 rows, V = 32768, D = 384: 16 us).
+//
+// The logits are float32 sums of the tensor core, which loses more than float32 additions do: the
+// loss of bfloat16 operands is off by 4.0e-8 of itself at D = 64, 1.3e-7 at 384, 7.7e-7 at 2048, where
+// float32 additions leave 4.0e-8, 4.4e-8 and 8.0e-8. Adding the sums to registers every 256 terms,
+// as is done for float32 operands, gives 8.7e-8 and costs the forward 27% at D = 1024: not done.
 //
 // Rows that are ignored are left out before the products: the others are copied together
 // (xent_rows, xent_pack), so ignored rows cost nothing and no infinity or NaN in them can
