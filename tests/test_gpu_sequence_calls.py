@@ -186,3 +186,20 @@ def test_operators_from_two_host_threads_on_their_own_streams():
     for t in threads:
         t.join()
     assert not errors, errors
+
+
+@pytest.mark.parametrize("handle", [0, 1, 2])
+def test_the_drivers_own_stream_handles(handle):
+    """0 and 1 are the default stream, 2 the calling thread's."""
+    g = gen(4)
+    table = torch.randn((50, 16), generator=g, device="cuda")
+    ids = torch.randint(0, 50, (300,), generator=g, device="cuda")
+    cfg = binding.make_embed_config(300, 50, 16)
+    torch.cuda.synchronize()
+    before = torch.cuda.current_stream()
+    out = binding.embed_forward(cfg, table, ids, stream=handle)
+    grad = binding.embed_backward(cfg, ids, out, stream=handle)
+    assert torch.cuda.current_stream() == before
+    torch.cuda.synchronize()
+    assert torch.equal(out, table[ids])
+    ref.check("gtable", grad, ref.embed_backward(ids, out, 50, 1.0, None))
