@@ -369,6 +369,143 @@ dendsn_status dendsn_xent_backward(const dendsn_xent_config *cfg, const void *hi
                                    const float *grad_loss, void *grad_hidden,
                                    void *grad_weight, void *scratch, void *stream);
 
+/*
+ * Root-mean-square norm with the residual's addition, as it stands before a token block's mixer and
+ * before the readout, and its gradient. Same conventions as the token-sequence operators.
+ *   sum = round(x + residual) in x_dtype (sum = x where residual is NULL)
+ *   y   = sum / sqrt(mean(sum^2) + eps) * weight
+ * out SAME: y [M, D] in x_dtype. out E4M3: y [M, D] one-byte e4m3 codes with scales [M, groups]
+ * float32, value = code * scale: one scale for a row (group 0) or for each 128 columns (group 128; the
+ * last one may have fewer). The largest of a group becomes 448; a group whose values are all below
+ * 2^-100 has scale 1. NaN and infinities stay within their row (its sum's mean takes them in).
+ * Backward, from sum: grad_x (the gradient of x and of residual alike), grad_sum added where it is
+ * not NULL (what reached sum by another way), and grad_weight summed over the rows.
+ *   x, residual, sum, grad_y, grad_sum, grad_x  [M, D] x_dtype;  weight, grad_weight [D] float32
+ *   residual and sum (output) are both given or both NULL; sum may be x or residual itself, grad_x
+ *   may be grad_y or grad_sum itself. grad_weight is OVERWRITTEN (zeros for M = 0).
+ *   scratch of the backward: scratch_bytes, 16-byte aligned. 1 <= D <= 16384.
+ */
+typedef enum { DENDSN_NORM_SAME = 0, DENDSN_NORM_E4M3 = 1 } dendsn_norm_out;
+
+typedef struct {
+    int64_t M;              /* rows */
+    int32_t D;              /* columns */
+    int32_t x_dtype;        /* dendsn_dtype of x, residual, sum and their gradients */
+    int32_t out;            /* dendsn_norm_out */
+    int32_t group;          /* E4M3: columns of a scale, 0 (the row) or 128 */
+    float eps;
+} dendsn_norm_config;
+
+dendsn_status dendsn_norm_workspace_size(const dendsn_norm_config *cfg, size_t *scratch_bytes);
+dendsn_status dendsn_norm_forward(const dendsn_norm_config *cfg, const void *x, const void *residual,
+                                  const float *weight, void *sum, void *y, float *scales,
+                                  void *stream);
+dendsn_status dendsn_norm_backward(const dendsn_norm_config *cfg, const void *sum,
+                                   const float *weight, const void *grad_y, const void *grad_sum,
+                                   void *grad_x, float *grad_weight, void *scratch, void *stream);
+
+/*
+ * Gated delta rule: the scan's sibling with a matrix of fast weights for each head, which a token's key
+ * reads, corrects and writes.
+ *   S_t = a_t S_{t-1} + k_t u_t^T,  u_t = beta_t (v_t - a_t S_{t-1}^T k_t),  a_t = exp(gate_t)
+ *   o_t = scale S_t^T q_t,  S_{-1} = s0
+ * for every sequence and each of Hv value heads; value head h has key head h / (Hv / Hk).
+ *   q, k       tokens x [Hk, Dk],  v, o tokens x [Hv, Dv]  x_dtype, and their gradients likewise
+ *   gate, beta tokens x [Hv] float32, and their gradients
+ *   s0, last, grad_s0, grad_last  [B, Hv, Dk, Dv] float32, or NULL (s0, grad_last NULL: zeros)
+ * layout: TIME tokens [T, B], BATCH tokens [B, T], PACKED T tokens of B sequences one behind the other,
+ * sequence b from offsets[b] up to offsets[b + 1] (int32 [B + 1] in device memory, ascending; elsewhere
+ * NULL). Sequences may be empty: their last is s0, and grad_s0 is grad_last. Tokens of no sequence keep
+ * what was in the outputs (rest KEEP) or get zeros (ZERO). Offsets out of order or range give results of
+ * no meaning, within the buffers.
+ * A gate below -200 (also -infinity) counts as -200, whose decay is 0 in float32: the state before is
+ * multiplied by zero (it has to be finite) and the gate's gradient is 0.
+ * bfloat16 inputs enter the products exactly, float32 inputs as three bfloat16 terms (2^-24); states and
+ * everything between the products are float32. grad_q and grad_k of bfloat16 inputs come of states in two
+ * bfloat16 terms (2^-17), and so does grad_gate's part in q's gradient.
+ * last may be s0 itself. saved: written by the forward where not NULL and read by the backward, which
+ * needs the same config and offsets, and neither the inputs nor s0. scratch: forward_bytes where saved is
+ * NULL, else none; backward_bytes. Both 256-byte aligned. 1 <= Dk, Dv <= 128.
+ */
+typedef enum { DENDSN_DELTA_TIME = 0, DENDSN_DELTA_BATCH = 1, DENDSN_DELTA_PACKED = 2 } dendsn_delta_layout;
+typedef enum { DENDSN_REST_KEEP = 0, DENDSN_REST_ZERO = 1 } dendsn_rest;
+
+typedef struct {
+    int32_t T, B;           /* steps (PACKED: tokens in all), sequences */
+    int32_t Hk, Hv;         /* heads of q and k, of v */
+    int32_t Dk, Dv;
+    int32_t x_dtype;        /* dendsn_dtype of q, k, v, o and their gradients */
+    int32_t layout;         /* dendsn_delta_layout */
+    int32_t rest;           /* dendsn_rest: tokens of no sequence (PACKED) */
+    float scale;
+} dendsn_delta_config;
+
+dendsn_status dendsn_delta_workspace_size(const dendsn_delta_config *cfg, size_t *saved_bytes,
+                                          size_t *forward_bytes, size_t *backward_bytes);
+dendsn_status dendsn_delta_forward(const dendsn_delta_config *cfg, const void *q, const void *k,
+                                   const void *v, const float *gate, const float *beta,
+                                   const int32_t *offsets, const float *s0, void *o, float *last,
+                                   void *saved, void *scratch, void *stream);
+dendsn_status dendsn_delta_backward(const dendsn_delta_config *cfg, const void *grad_o,
+                                    const int32_t *offsets, const float *grad_last,
+                                    const void *saved, void *grad_q, void *grad_k, void *grad_v,
+                                    float *grad_gate, float *grad_beta, float *grad_s0,
+                                    void *scratch, void *stream);
+
+/*
+ * One AdamW step over many tensors, each with a gradient of its own type.
+ *   g = grad * min(1, max_norm / |grads|)     |grads|: over all tensors; max_norm 0: no clipping
+ *   m += (1 - beta1) (g - m);  v += (1 - beta2) (g^2 - v);  t = step + 1
+ *   param = param (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + eps)
+ * all in float32, rounded once where param or copy is bfloat16 (copy: bfloat16 copy of param for the
+ * next forward, or NULL).
+ * state F32: m and v float32 [n]. state E4M3: m and sqrt(v) as one-byte e4m3 codes [n], scales
+ * float32 [ceil(n / 256), 2] (of m, of sqrt(v)) of 256 elements each, value = code * scale; the
+ * largest of a block becomes 448, and the others are rounded to one of their two neighbours at
+ * random so that the expectations of m and of v are right. The random numbers come from seed, the
+ * step, the tensor's place in the list and the element's place alone: the same step gives the same
+ * bits. Zeros in m, v and scales are the states at the start, for both. A block whose largest value
+ * is below 2^-110 is stored as zeros; NaN and infinities spread over their block of 256.
+ * A tensor whose gradient is NULL stays as it is, its states too, and takes no part in the norm.
+ * A norm that is infinite scales finite gradients to zero; one that is NaN scales nothing.
+ *
+ * dendsn_adamw_plan fills a table in HOST memory (table NULL: only its size) that the caller copies to
+ * 16-byte aligned device memory once, and for new addresses; the step takes it there. The table
+ * holds the step's sums as well: steps with one table run one after another. sizes: n of each
+ * tensor in the plan's order; grads: device addresses, an array in host memory that is read during
+ * the call (as are all host arrays here), so that a captured graph keeps them.
+ *   step  device int64, steps done so far; the call adds 1
+ *   lr    device float32 that is used instead of cfg->lr, or NULL
+ *   norm  device float32 that receives |grads| where clipping is on, or NULL
+ * Tensors may not overlap. 16-byte (bfloat16) and 32-byte (float32) aligned tensors of a multiple of 8
+ * elements take wide loads.
+ */
+typedef enum { DENDSN_STATE_F32 = 0, DENDSN_STATE_E4M3 = 1 } dendsn_state;
+
+typedef struct {
+    double lr, beta1, beta2, eps, max_norm;
+    uint32_t seed;
+    int32_t state;          /* dendsn_state */
+} dendsn_adamw_config;
+
+typedef struct {
+    void *param;            /* [n] */
+    void *m, *v;            /* [n] */
+    float *scales;          /* [ceil(n / 256), 2], or NULL for F32 states */
+    void *copy;             /* [n] bfloat16, or NULL */
+    int64_t n;
+    double weight_decay;
+    int32_t param_dtype;    /* dendsn_dtype */
+    int32_t reserved;       /* 0 */
+} dendsn_adamw_tensor;
+
+dendsn_status dendsn_adamw_plan(const dendsn_adamw_config *cfg, const dendsn_adamw_tensor *tensors,
+                                int32_t count, void *table, size_t *table_bytes);
+dendsn_status dendsn_adamw_step(const dendsn_adamw_config *cfg, void *plan, const int64_t *sizes,
+                                int32_t count, const void *const *grads,
+                                const int32_t *grad_dtypes, int64_t *step, const float *lr,
+                                float *norm, void *stream);
+
 /* Static description of a status code. */
 const char *dendsn_status_string(dendsn_status status);
 

@@ -101,6 +101,41 @@ class dendsn_xent_config(ctypes.Structure):
                 ("statistics", ctypes.c_int32), ("weight_aligned", ctypes.c_int32)]
 
 
+NORM_SAME, NORM_E4M3 = 0, 1
+DELTA_TIME, DELTA_BATCH, DELTA_PACKED = 0, 1, 2
+REST_KEEP, REST_ZERO = 0, 1
+STATE_F32, STATE_E4M3 = 0, 1
+
+
+class dendsn_norm_config(ctypes.Structure):
+    """Mirror of the C struct dendsn_norm_config (norm with the residual's addition)."""
+    _fields_ = [("M", ctypes.c_int64), ("D", ctypes.c_int32), ("x_dtype", ctypes.c_int32),
+                ("out", ctypes.c_int32), ("group", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class dendsn_delta_config(ctypes.Structure):
+    """Mirror of the C struct dendsn_delta_config (the gated delta rule)."""
+    _fields_ = [("T", ctypes.c_int32), ("B", ctypes.c_int32), ("Hk", ctypes.c_int32),
+                ("Hv", ctypes.c_int32), ("Dk", ctypes.c_int32), ("Dv", ctypes.c_int32),
+                ("x_dtype", ctypes.c_int32), ("layout", ctypes.c_int32), ("rest", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
+
+
+class dendsn_adamw_config(ctypes.Structure):
+    """Mirror of the C struct dendsn_adamw_config."""
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("max_norm", ctypes.c_double),
+                ("seed", ctypes.c_uint32), ("state", ctypes.c_int32)]
+
+
+class dendsn_adamw_tensor(ctypes.Structure):
+    """Mirror of the C struct dendsn_adamw_tensor."""
+    _fields_ = [("param", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("scales", ctypes.c_void_p), ("copy", ctypes.c_void_p), ("n", ctypes.c_int64),
+                ("weight_decay", ctypes.c_double), ("param_dtype", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
 def _code(what, value, codes):
     try:
         return codes[value]
@@ -146,6 +181,37 @@ def make_xent_config(M, V, D, dtype="f32", ignore_index=-100,
                               _code("labels_dtype", labels_dtype, _INDEX),
                               _code("logit_grad", logit_grad, _LOGIT_GRADS),
                               _code("statistics", statistics, _STATISTICS), int(weight_aligned))
+
+
+_NORM_OUTS = {"same": NORM_SAME, "e4m3": NORM_E4M3}
+_DELTA_LAYOUTS = {"time": DELTA_TIME, "batch": DELTA_BATCH, "packed": DELTA_PACKED}
+_RESTS = {"keep": REST_KEEP, "zero": REST_ZERO}
+_STATES = {"f32": STATE_F32, "e4m3": STATE_E4M3}
+
+
+def make_norm_config(M, D, dtype="f32", eps=1e-6, out="same", group=0) -> dendsn_norm_config:
+    """out: "same" (the inputs' type) or "e4m3", codes with one scale for each `group` columns (128)
+    or for the row (0)."""
+    return dendsn_norm_config(M, D, _code("dtype", dtype, _DTYPES), _code("out", out, _NORM_OUTS),
+                              group, eps)
+
+
+def make_delta_config(T, B, Hk, Hv, Dk, Dv, dtype="f32", layout="time", scale=1.0,
+                      rest="keep") -> dendsn_delta_config:
+    """layout: tokens "time" [T, B], "batch" [B, T] or "packed" (T tokens of B sequences one behind
+    the other). rest: what outputs hold for tokens of no sequence, "keep" (what was there) or "zero"
+    (the allocating wrappers always give zeros)."""
+    return dendsn_delta_config(T, B, Hk, Hv, Dk, Dv, _code("dtype", dtype, _DTYPES),
+                               _code("layout", layout, _DELTA_LAYOUTS), _code("rest", rest, _RESTS),
+                               scale)
+
+
+def make_adamw_config(lr=1e-3, betas=(0.9, 0.999), eps=1e-8, state="f32", max_norm=0.0,
+                      seed=0) -> dendsn_adamw_config:
+    """state: how m and v are held, "f32" or "e4m3" (codes with scales of 256 elements, drawn from
+    seed). max_norm: the gradients are scaled down to this norm over all tensors; 0: they are not."""
+    return dendsn_adamw_config(lr, betas[0], betas[1], eps, max_norm, seed & 0xffffffff,
+                               _code("state", state, _STATES))
 
 
 class dendsn_lif_config(ctypes.Structure):
@@ -197,13 +263,19 @@ def load() -> ctypes.CDLL:
                 fn.restype = ctypes.c_int
             for name, cfg_t, sizes, forward, backward in (
                     ("embed", dendsn_embed_config, 1, 4, 5), ("scan", dendsn_scan_config, 1, 8, 11),
-                    ("xent", dendsn_xent_config, 2, 7, 9)):
+                    ("xent", dendsn_xent_config, 2, 7, 9), ("norm", dendsn_norm_config, 1, 7, 8),
+                    ("delta", dendsn_delta_config, 3, 12, 12)):
                 cp = ctypes.POINTER(cfg_t)
                 for fn, args in (("workspace_size", [ctypes.POINTER(ctypes.c_size_t)] * sizes),
                                  ("forward", [P] * forward), ("backward", [P] * backward)):
                     f = getattr(lib, f"dendsn_{name}_{fn}")
                     f.argtypes = [cp] + args
                     f.restype = ctypes.c_int
+            acfgp = ctypes.POINTER(dendsn_adamw_config)
+            lib.dendsn_adamw_plan.argtypes = [acfgp, ctypes.POINTER(dendsn_adamw_tensor),
+                                              ctypes.c_int32, P, ctypes.POINTER(ctypes.c_size_t)]
+            lib.dendsn_adamw_step.argtypes = [acfgp, P, P, ctypes.c_int32] + [P] * 6
+            lib.dendsn_adamw_plan.restype = lib.dendsn_adamw_step.restype = ctypes.c_int
             lib.dendsn_status_string.argtypes = [ctypes.c_int]
             lib.dendsn_status_string.restype = ctypes.c_char_p
             lib.dendsn_last_error.argtypes = []
@@ -669,6 +741,280 @@ def xent_backward(cfg, hidden, weight, labels, lse, grad_loss, scratch=None, str
     return out
 
 
+# ------------------------------------------------------------------ token blocks
+E4M3 = torch.float8_e4m3fn
+
+
+def dendsn_norm_workspace_size(cfg: dendsn_norm_config) -> int:
+    """scratch_bytes of the norm's backward."""
+    s = ctypes.c_size_t(0)
+    _check("dendsn_norm_workspace_size",
+           load().dendsn_norm_workspace_size(ctypes.byref(cfg), ctypes.byref(s)))
+    return s.value
+
+
+def _norm_rows(cfg, **rows):
+    """Tensors of M rows of D, whatever the shape before the last axis."""
+    dt = _xdtype(cfg)
+    for name, t in rows.items():
+        if t is not None and (t.dtype is not dt or t.dim() == 0 or t.shape[-1] != cfg.D or
+                              t.numel() != cfg.M * cfg.D):
+            raise ValueError(f"{name} must be {dt}, {cfg.M} rows of {cfg.D}, got {t.dtype} "
+                             f"{list(t.shape)}")
+
+
+def _norm_groups(cfg) -> int:
+    return (cfg.D + cfg.group - 1) // cfg.group if cfg.group else 1
+
+
+def dendsn_norm_forward(cfg, x, residual, weight, sum, y, scales=None, stream=None):
+    """y (and, with a residual, sum = x + residual) from x; scales [M, groups] for e4m3 outputs."""
+    eight = cfg.out == NORM_E4M3
+    for name, t in (("x", x), ("y", y)):
+        if t is None:
+            raise ValueError(f"{name} is required")
+    _norm_rows(cfg, x=x, residual=residual, sum=sum, **({} if eight else {"y": y}))
+    _expect((cfg.D,), torch.float32, weight=weight)
+    if eight:
+        _expect(x.shape, E4M3, y=y)
+        _expect((cfg.M, _norm_groups(cfg)), torch.float32, scales=scales)
+    _check("dendsn_norm_forward", load().dendsn_norm_forward(
+        ctypes.byref(cfg), *_pointers(x, residual, weight, sum, y, scales if eight else None),
+        _stream(stream)))
+
+
+def dendsn_norm_backward(cfg, sum, weight, grad_y, grad_sum, grad_x, grad_weight, scratch,
+                         stream=None):
+    for name, t in (("sum", sum), ("grad_y", grad_y), ("grad_x", grad_x)):
+        if t is None:
+            raise ValueError(f"{name} is required")
+    _norm_rows(cfg, sum=sum, grad_y=grad_y, grad_sum=grad_sum, grad_x=grad_x)
+    _expect((cfg.D,), torch.float32, weight=weight, grad_weight=grad_weight)
+    _bytes("scratch", scratch, dendsn_norm_workspace_size(cfg))
+    _check("dendsn_norm_backward", load().dendsn_norm_backward(
+        ctypes.byref(cfg), *_pointers(sum, weight, grad_y, grad_sum, grad_x, grad_weight, scratch),
+        _stream(stream)))
+
+
+@_allocates
+def norm_forward(cfg, x, weight, residual=None, stream=None):
+    """Allocating norm. Returns (y, sum, scales): sum is x + residual (x itself without one), scales
+    None unless y are e4m3 codes."""
+    total = x if residual is None else torch.empty_like(x)
+    scales = None
+    if cfg.out == NORM_E4M3:
+        y = torch.empty(x.shape, dtype=E4M3, device=x.device)
+        scales = torch.empty((cfg.M, _norm_groups(cfg)), dtype=torch.float32, device=x.device)
+    else:
+        y = torch.empty_like(x)
+    dendsn_norm_forward(cfg, x, residual, weight, None if residual is None else total, y, scales,
+                        stream)
+    return y, total, scales
+
+
+@_allocates
+def norm_backward(cfg, sum, weight, grad_y, grad_sum=None, scratch=None, stream=None):
+    """Allocating backward from the forward's sum. Returns dict gx (of x and of residual alike) and
+    gweight [D] float32."""
+    if scratch is None:
+        scratch = _scratch(dendsn_norm_workspace_size(cfg), sum.device)
+    out = dict(gx=torch.empty_like(sum), gweight=torch.empty_like(weight))
+    dendsn_norm_backward(cfg, sum, weight, grad_y, grad_sum, out["gx"], out["gweight"], scratch,
+                         stream)
+    return out
+
+
+def dendsn_delta_workspace_size(cfg: dendsn_delta_config):
+    """(saved_bytes, forward_bytes, backward_bytes) of the gated delta rule."""
+    b = [ctypes.c_size_t(0) for _ in range(3)]
+    _check("dendsn_delta_workspace_size",
+           load().dendsn_delta_workspace_size(ctypes.byref(cfg), *map(ctypes.byref, b)))
+    return tuple(x.value for x in b)
+
+
+def _delta_lead(cfg):
+    return {DELTA_TIME: (cfg.T, cfg.B), DELTA_BATCH: (cfg.B, cfg.T), DELTA_PACKED: (cfg.T,)}[cfg.layout]
+
+
+def _delta_expect(cfg, offsets, qk, vo, gates, states):
+    lead, dt = _delta_lead(cfg), _xdtype(cfg)
+    _expect((*lead, cfg.Hk, cfg.Dk), dt, **qk)
+    _expect((*lead, cfg.Hv, cfg.Dv), dt, **vo)
+    _expect((*lead, cfg.Hv), torch.float32, **gates)
+    _expect((cfg.B, cfg.Hv, cfg.Dk, cfg.Dv), torch.float32,
+            **{n: t for n, t in states.items() if t is not None})
+    if cfg.layout == DELTA_PACKED:
+        _expect((cfg.B + 1,), torch.int32, offsets=offsets)
+    elif offsets is not None:
+        raise ValueError("offsets go with the packed layout")
+
+
+def dendsn_delta_forward(cfg, q, k, v, gate, beta, offsets, s0, o, last=None, saved=None,
+                         scratch=None, stream=None):
+    _delta_expect(cfg, offsets, dict(q=q, k=k), dict(v=v, o=o), dict(gate=gate, beta=beta),
+                  dict(s0=s0, last=last))
+    sizes = dendsn_delta_workspace_size(cfg)
+    if saved is not None:
+        _bytes("saved", saved, sizes[0])
+    else:
+        _bytes("scratch", scratch, sizes[1])
+    _check("dendsn_delta_forward", load().dendsn_delta_forward(
+        ctypes.byref(cfg), *_pointers(q, k, v, gate, beta, offsets, s0, o, last, saved, scratch),
+        _stream(stream)))
+
+
+def dendsn_delta_backward(cfg, grad_o, offsets, grad_last, saved, grad_q, grad_k, grad_v, grad_gate,
+                          grad_beta, grad_s0, scratch, stream=None):
+    _delta_expect(cfg, offsets, dict(grad_q=grad_q, grad_k=grad_k), dict(grad_o=grad_o, grad_v=grad_v),
+                  dict(grad_gate=grad_gate, grad_beta=grad_beta),
+                  dict(grad_last=grad_last, grad_s0=grad_s0))
+    sizes = dendsn_delta_workspace_size(cfg)
+    _bytes("saved", saved, sizes[0])
+    _bytes("scratch", scratch, sizes[2])
+    _check("dendsn_delta_backward", load().dendsn_delta_backward(
+        ctypes.byref(cfg), *_pointers(grad_o, offsets, grad_last, saved, grad_q, grad_k, grad_v,
+                                      grad_gate, grad_beta, grad_s0, scratch), _stream(stream)))
+
+
+def delta_workspace(cfg, device=None):
+    """The buffer in which the forward leaves what the backward needs (None where that is nothing)."""
+    return _scratch(dendsn_delta_workspace_size(cfg)[0], device or torch.device("cuda"))
+
+
+def _no_rest(cfg):
+    """cfg with zeros for tokens of no sequence: new tensors hold nothing there to keep."""
+    if cfg.layout == DELTA_PACKED and cfg.rest == REST_KEEP:
+        cfg = dendsn_delta_config.from_buffer_copy(cfg)
+        cfg.rest = REST_ZERO
+    return cfg
+
+
+@_allocates
+def delta_forward(cfg, q, k, v, gate, beta, offsets=None, s0=None, last=None, saved=None,
+                  want_last=False, stream=None):
+    """Allocating gated delta rule. Returns (o, last): last is the given tensor (which may be s0), a
+    new one where want_last is true, or None."""
+    o = torch.empty_like(v)
+    if last is None and want_last:
+        last = torch.empty((cfg.B, cfg.Hv, cfg.Dk, cfg.Dv), dtype=torch.float32, device=v.device)
+    scratch = None
+    if saved is None:
+        scratch = _scratch(dendsn_delta_workspace_size(cfg)[1], v.device)
+    dendsn_delta_forward(_no_rest(cfg), q, k, v, gate, beta, offsets, s0, o, last, saved, scratch, stream)
+    return o, last
+
+
+@_allocates
+def delta_backward(cfg, q, k, v, gate, beta, grad_o, offsets=None, s0=None, grad_last=None, saved=None,
+                   scratch=None, stream=None):
+    """Allocating backward. Returns dict gq, gk, gv, ggate, gbeta, and gs0 where s0 is given. The
+    inputs' values come from `saved` as the forward left it."""
+    if scratch is None:
+        scratch = _scratch(dendsn_delta_workspace_size(cfg)[2], q.device)
+    out = {"g" + n: torch.empty_like(t) for n, t in
+           (("q", q), ("k", k), ("v", v), ("gate", gate), ("beta", beta))}
+    if s0 is not None:
+        out["gs0"] = torch.empty_like(s0)
+    dendsn_delta_backward(_no_rest(cfg), grad_o, offsets, grad_last, saved, out["gq"], out["gk"],
+                          out["gv"], out["ggate"], out["gbeta"], out.get("gs0"), scratch, stream)
+    return out
+
+
+class AdamwPlan:
+    """Tensors of an AdamW step and their table in device memory. Holds the tensors alive."""
+
+    def __init__(self, cfg, params, ms, vs, scales, copies, weight_decay):
+        n = len(params)
+        eight = cfg.state == STATE_E4M3
+        if eight and scales is None:
+            raise ValueError("scales are required for e4m3 states")
+        decays = list(weight_decay) if hasattr(weight_decay, "__iter__") else [weight_decay] * n
+        lists = [("ms", ms), ("vs", vs), ("weight_decay", decays)]
+        lists += [("scales", scales)] if eight else []
+        lists += [("copies", copies)] if copies is not None else []
+        for name, x in lists:
+            if len(x) != n:
+                raise ValueError(f"{name}: {len(x)} entries for {n} params")
+        entries = (dendsn_adamw_tensor * n)()
+        for i, p in enumerate(params):
+            _dtype_name(p)
+            state = E4M3 if eight else torch.float32
+            for name, t in (("m", ms[i]), ("v", vs[i])):
+                if t.dtype is not state or t.numel() != p.numel():
+                    raise ValueError(f"{name} of tensor {i} must be {state}, {p.numel()} elements")
+            scale = scales[i] if eight else None
+            copy = copies[i] if copies is not None else None
+            if scale is not None:
+                _expect(((p.numel() + 255) // 256, 2), torch.float32, scales=scale)
+            if copy is not None and (copy.dtype is not torch.bfloat16 or copy.numel() != p.numel()):
+                raise ValueError(f"copy of tensor {i} must be bfloat16, {p.numel()} elements")
+            if p.numel() == 0:
+                ptrs = [None] * 5
+            else:
+                ptrs = _pointers(p, ms[i], vs[i], scale, copy)
+            entries[i] = dendsn_adamw_tensor(*ptrs, p.numel(), decays[i],
+                                             BF16 if p.dtype is torch.bfloat16 else F32, 0)
+        need = ctypes.c_size_t(0)
+        _check("dendsn_adamw_plan",
+               load().dendsn_adamw_plan(ctypes.byref(cfg), entries, n, None, ctypes.byref(need)))
+        host = torch.empty(need.value, dtype=torch.uint8)
+        _check("dendsn_adamw_plan",
+               load().dendsn_adamw_plan(ctypes.byref(cfg), entries, n, host.data_ptr(), None))
+        devices = {p.device for p in params} or {torch.device("cuda")}
+        if len(devices) > 1:
+            raise ValueError("params on more than one device")
+        self.table = host.to(devices.pop())
+        self.count, self.state = n, cfg.state
+        self.sizes = [p.numel() for p in params]
+        self.c_sizes = (ctypes.c_int64 * n)(*self.sizes)
+        self.held = (params, ms, vs, scales, copies)
+
+
+def adamw_plan(cfg, params, ms, vs, scales=None, copies=None, weight_decay=0.0) -> AdamwPlan:
+    """The plan of a step over `params` (float32 or bfloat16) with their states m and v (float32, or
+    e4m3 with scales [ceil(n / 256), 2]); copies: bfloat16 tensors that receive the new parameters too
+    (entries may be None); weight_decay: one for all or one each. All states start as zeros."""
+    return AdamwPlan(cfg, list(params), list(ms), list(vs), None if scales is None else list(scales),
+                     None if copies is None else list(copies), weight_decay)
+
+
+def adamw_step(cfg, plan, grads, step, lr=None, norm=None, stream=None):
+    """One step in place. grads: a tensor or None (left as it is) for each of the plan's params, float32
+    or bfloat16; step: int64 tensor [1] on the device, counted up; lr: float32 tensor [1] on the device
+    that stands in for cfg's. Returns the gradients' norm (float32 [1]; `norm` itself where given) where
+    the config clips, else None."""
+    n = plan.count
+    if cfg.state != plan.state:
+        raise ValueError("the config's state is not the plan's")
+    if len(grads) != n:
+        raise ValueError(f"grads: {len(grads)} entries for {n} params")
+    _expect((1,), torch.int64, step=step)
+    if lr is not None:
+        _expect((1,), torch.float32, lr=lr)
+    ptrs, dtypes = (ctypes.c_void_p * n)(), (ctypes.c_int32 * n)()
+    for i, (g, size) in enumerate(zip(grads, plan.sizes)):
+        if g is None:
+            continue
+        if g.dtype is torch.bfloat16:
+            dtypes[i] = BF16
+        elif g.dtype is not torch.float32:
+            raise ValueError(f"gradient {i} must be float32 or bfloat16, got {g.dtype}")
+        if g.numel() != size:
+            raise ValueError(f"gradient {i}: {g.numel()} elements, the param has {size}")
+        if size:
+            ptrs[i] = g.data_ptr() if g.is_cuda and g.is_contiguous() else _ptr(g)
+    if cfg.max_norm > 0:
+        if norm is None:
+            norm = _allocates(lambda like, stream: torch.empty(1, dtype=torch.float32, device=like.device))(step, stream)
+        _expect((1,), torch.float32, norm=norm)
+    else:
+        norm = None
+    _check("dendsn_adamw_step", load().dendsn_adamw_step(
+        ctypes.byref(cfg), plan.table.data_ptr(), plan.c_sizes, n, ptrs, dtypes,
+        *_pointers(step, lr, norm), _stream(stream)))
+    return norm
+
+
 # ------------------------------------------------------------------ tensor-level helpers
 def _xdtype(cfg) -> torch.dtype:
     return torch.bfloat16 if cfg.x_dtype == BF16 else torch.float32
@@ -833,6 +1179,64 @@ class ScanFunction(torch.autograd.Function):
         g = scan_backward(ctx.cfg, x, gate, gh.contiguous(), starts, h0,
                           None if glast is None else glast.contiguous(), ctx.saved)
         return g["gx"], g["ggate"], None, g.get("gh0"), None, None, None
+
+
+class NormFunction(torch.autograd.Function):
+    """autograd wrapper of the root-mean-square norm: (y, sum) of x, its residual (or None) and
+    weight [D] float32; sum = x + residual is the next residual (x itself where there is none)."""
+
+    @staticmethod
+    def forward(ctx, x, residual, weight, eps=1e-6):
+        x, weight = x.contiguous(), weight.contiguous()
+        D = x.shape[-1]
+        ctx.cfg = make_norm_config(x.numel() // D if D else 0, D, _dtype_name(x), eps)
+        y, total, _ = norm_forward(ctx.cfg, x, weight, None if residual is None else residual.contiguous())
+        ctx.added = residual is not None
+        ctx.save_for_backward(total, weight)
+        ctx.set_materialize_grads(False)
+        return y, total
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, gy, gsum):
+        total, weight = ctx.saved_tensors
+        if gy is None and gsum is None:
+            return None, None, None, None
+        gy = torch.zeros_like(total) if gy is None else gy.contiguous()
+        g = norm_backward(ctx.cfg, total, weight, gy, None if gsum is None else gsum.contiguous())
+        return g["gx"], g["gx"] if ctx.added else None, g["gweight"], None
+
+
+class DeltaFunction(torch.autograd.Function):
+    """autograd wrapper of the gated delta rule: (o, last) of q, k [tokens, Hk, Dk], v [tokens, Hv, Dv],
+    gate and beta [tokens, Hv] float32 and s0 [B, Hv, Dk, Dv] float32 or None. layout "time": tokens
+    [T, B]; "batch": [B, T]; "packed": all tokens in one axis and offsets int32 [B + 1]."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, gate, beta, s0=None, offsets=None, scale=1.0, layout="time"):
+        q, k, v, gate, beta = (t.contiguous() for t in (q, k, v, gate, beta))
+        s0 = None if s0 is None else s0.contiguous()
+        if layout == "packed":
+            T, B = q.shape[0], offsets.numel() - 1
+        else:
+            T, B = q.shape[:2] if layout == "time" else (q.shape[1], q.shape[0])
+        ctx.cfg = make_delta_config(T, B, q.shape[-2], v.shape[-2], q.shape[-1], v.shape[-1],
+                                    _dtype_name(q), layout, scale)
+        ctx.saved = delta_workspace(ctx.cfg, q.device) if any(ctx.needs_input_grad) else None
+        o, last = delta_forward(ctx.cfg, q, k, v, gate, beta, offsets, s0, saved=ctx.saved,
+                                want_last=True)
+        ctx.save_for_backward(q, k, v, gate, beta, s0, offsets)
+        ctx.set_materialize_grads(False)
+        return o, last
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, go, glast):
+        q, k, v, gate, beta, s0, offsets = ctx.saved_tensors
+        go = torch.zeros_like(v) if go is None else go.contiguous()
+        g = delta_backward(ctx.cfg, q, k, v, gate, beta, go, offsets, s0,
+                           None if glast is None else glast.contiguous(), ctx.saved)
+        return g["gq"], g["gk"], g["gv"], g["ggate"], g["gbeta"], g.get("gs0"), None, None, None
 
 
 class XentFunction(torch.autograd.Function):

@@ -1,0 +1,517 @@
+// One step of AdamW over many tensors at once:
+//   g' = g min(1, max_norm / |g|)           (|g| over all tensors; where clipping is on)
+//   m += (1 - beta1) (g' - m),  v += (1 - beta2) (g'^2 - v),  t = step + 1
+//   p = p (1 - lr decay) - lr / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + eps)
+// with states in float32, or m and sqrt(v) as e4m3 codes with a float32 scale for each 256 elements
+// (the largest becomes 448). A code is drawn from the two neighbours of its value so that the
+// expectation of m and of v is right: a step moves a state by a thousandth, far less than the
+// distance of two codes, and would be lost in rounding to the nearest.
+//
+// Bound by memory: every state is read and written once, in one launch for all tensors. Tensors are
+// cut into chunks of 4096 elements; a table in device memory says which tensor a chunk belongs to, and
+// the gradients' addresses, which change from step to step, come as the launch's arguments. A warp
+// takes 256 elements at a time, 8 neighbours a lane, so that a scale's elements are one warp's.
+// Clipping reads the gradients once more before (a launch that leaves one float64 sum a block).
+#include <cuda_fp16.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "pieces.cuh"
+#include "seq_common.h"
+#include "tc.cuh"
+
+namespace dendsn {
+namespace {
+
+constexpr int kBlock = 256;            // elements of a warp's turn, and of a scale
+constexpr int kChunk = 4096;           // elements of a block's turn
+constexpr int kThreads = 256;
+constexpr int kGrads = 500;            // tensors of a launch: their gradients' addresses are its arguments
+constexpr int kMostBlocks = 152 * 4;
+constexpr uint32_t kStride = 0x9E3779B1u;
+
+enum : int32_t { kParamBf16 = 1, kWide = 2 };
+
+struct Tensor {
+    void *param, *m, *v;
+    float *scales;
+    __nv_bfloat16 *copy;
+    int64_t n;
+    int32_t first;             // its first chunk
+    int32_t flags;
+    float decay;
+    int32_t pad;
+};
+static_assert(sizeof(Tensor) == 64, "one tensor's entry");
+
+// The device table: a header, the sums of squares of each block, the tensors, the tensor of each chunk.
+struct Header {
+    uint32_t ticket;           // blocks of a launch that have read the step; 0 between launches
+    uint32_t pad[15];
+};
+constexpr size_t kSumsAt = sizeof(Header), kTensorsAt = kSumsAt + kMostBlocks * sizeof(double);
+
+// Addresses of gradients, with 1 added where a gradient is bfloat16; 0: none, the tensor stays as it is.
+struct Grads {
+    uint64_t at[kGrads];
+};
+
+struct Step {
+    uint8_t *plan;
+    int64_t *step;
+    const float *lr_at;        // or NULL: lr
+    float *norm;               // or NULL
+    int32_t tensors, first;    // of the plan; the first of this launch
+    int32_t chunk, chunks;     // of this launch: the first, and the one behind the last
+    int32_t sums;              // sums of squares in the table (0: no clipping)
+    bool last;                 // launch of the step
+    float lr, eps, max_norm, rest1, rest2;
+    float log1_hi, log1_lo, log2_hi, log2_lo;     // logarithms of the betas
+    uint32_t seed;
+};
+
+__device__ __forceinline__ uint32_t mix(uint32_t h) {
+    h = (h ^ (h >> 16)) * 0x6A09E667u;
+    h = (h ^ (h >> 15)) * 0xADF85459u;
+    return h ^ (h >> 16);
+}
+
+// 8 elements of a lane: neighbours (WIDE), or every 32nd of the block's, as far as there are.
+template <bool WIDE>
+__device__ __forceinline__ int element(int lane, int j) { return WIDE ? lane * 8 + j : j * 32 + lane; }
+
+template <bool WIDE>
+__device__ __forceinline__ void load8(float (&v)[8], const float *p, int lane, int left) {
+    if (WIDE) {
+        uint32_t q[8] = {};
+        if (lane * 8 < left) tc::load32(q, p + lane * 8);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(q[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = j * 32 + lane < left ? p[j * 32 + lane] : 0.f;
+    }
+}
+template <bool WIDE>
+__device__ __forceinline__ void load8(float (&v)[8], const __nv_bfloat16 *p, int lane, int left) {
+    if (WIDE) {
+        Lot<__nv_bfloat16, 8> q;
+        q.zero();
+        if (lane * 8 < left) q = reinterpret_cast<const Lot<__nv_bfloat16, 8> *>(p)[lane];
+        q.get(v);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = j * 32 + lane < left ? __bfloat162float(p[j * 32 + lane]) : 0.f;
+    }
+}
+template <bool WIDE>
+__device__ __forceinline__ void store8(const float (&v)[8], float *p, int lane, int left) {
+    if (WIDE) {
+        uint32_t q[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q[j] = __float_as_uint(v[j]);
+        if (lane * 8 < left) tc::store32(p + lane * 8, q);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j * 32 + lane < left) p[j * 32 + lane] = v[j];
+    }
+}
+template <bool WIDE>
+__device__ __forceinline__ void store8(const float (&v)[8], __nv_bfloat16 *p, int lane, int left) {
+    if (WIDE) {
+        Lot<__nv_bfloat16, 8> q;
+        q.set(v);
+        if (lane * 8 < left) reinterpret_cast<Lot<__nv_bfloat16, 8> *>(p)[lane] = q;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j * 32 + lane < left) p[j * 32 + lane] = __float2bfloat16_rn(v[j]);
+    }
+}
+// Codes as they lie: two words of four.
+template <bool WIDE>
+__device__ __forceinline__ void load_codes(uint32_t (&q)[2], const uint8_t *p, int lane, int left) {
+    q[0] = q[1] = 0;
+    if (WIDE) {
+        if (lane * 8 < left) {
+            const uint2 r = reinterpret_cast<const uint2 *>(p)[lane];
+            q[0] = r.x, q[1] = r.y;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j * 32 + lane < left) q[j >> 2] |= (uint32_t)p[j * 32 + lane] << (j & 3) * 8;
+    }
+}
+template <bool WIDE>
+__device__ __forceinline__ void store_codes(const uint32_t (&q)[2], uint8_t *p, int lane, int left) {
+    if (WIDE) {
+        if (lane * 8 < left) reinterpret_cast<uint2 *>(p)[lane] = make_uint2(q[0], q[1]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j * 32 + lane < left) p[j * 32 + lane] = (uint8_t)(q[j >> 2] >> (j & 3) * 8);
+    }
+}
+__device__ __forceinline__ void decode(float (&v)[8], const uint32_t (&q)[2], float scale) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t h;
+        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)(q[i >> 1] >> (i & 1) * 16)));
+        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h));
+        v[2 * i] = f.x * scale, v[2 * i + 1] = f.y * scale;
+    }
+}
+
+// e4m3 code of value (0 to 448) from one of its neighbours. Above 2^-6 a code is the float's leading
+// bits; below, adding 2^-6 gives the codes' even steps to a float's mantissa.
+struct Code {
+    uint32_t bits;             // of the float
+    uint32_t base;             // what its leading bits are above the code
+};
+__device__ __forceinline__ Code code_of(float value) {
+    const bool small = value < 0x1p-6f;
+    return {__float_as_uint(small ? value + 0x1p-6f : value), small ? 121u << 3 : 120u << 3};
+}
+// The upper neighbour where 16 random bits, as a number in (0, 1), are below the value's share of the way.
+__device__ __forceinline__ uint32_t round_code(float value, uint32_t random) {
+    const Code c = code_of(value);
+    return min(((c.bits + (0xfffffu - 8u - 16u * random)) >> 20) - c.base, 0x7eu);
+}
+// The same for the square: its share of the way between the neighbours' squares.
+__device__ __forceinline__ uint32_t round_square(float value, uint32_t random) {
+    const Code c = code_of(value);
+    const float off = c.base == 121u << 3 ? 0x1p-6f : 0.f;
+    const uint32_t low_bits = c.bits & 0xfff00000u;
+    const float low = __uint_as_float(low_bits) - off, high = __uint_as_float(low_bits + 0x100000u) - off;
+    const float u = ((float)random + 0.5f) * 0x1p-16f;
+    const bool up = u * ((high - low) * (high + low)) < (value - low) * (value + low);
+    return min((low_bits >> 20) - c.base + (up ? 1u : 0u), 0x7eu);
+}
+__device__ __forceinline__ uint32_t warp_top(float v) {
+    uint32_t t = __float_as_uint(v);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) t = max(t, __shfl_xor_sync(0xffffffffu, t, o));
+    return t;
+}
+__device__ __forceinline__ float sqrt_fast(float v) {
+    float r;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+// sqrt(a)/b is within 2^-22 of itself: a rounding of the update, which is a thousandth of p.
+__device__ __forceinline__ float divide(float a, float b) { return __fdividef(a, b); }
+
+struct Scalars {
+    float factor, rate, inverse_root, lr;
+    uint32_t start;
+};
+
+// 1 - beta^t; the product of t and the logarithm keeps the bits below a float's.
+__device__ __forceinline__ float rest_of_power(float t, float hi, float lo) {
+    const float a = t * hi;
+    return -expm1f(a + (fmaf(t, hi, -a) + t * lo));
+}
+
+template <bool EIGHT, bool WIDE>
+__device__ __forceinline__ void update(const Tensor &x, uint64_t grad, int64_t at, int lane, const Scalars &c, const Step &s, uint32_t start) {
+    const int left = (int)min((int64_t)kBlock, x.n - at);
+    float g[8], m[8], v[8], p[8];
+    uint32_t qm[2], qv[2];
+    float2 sc = make_float2(0.f, 0.f);
+    if (grad & 1) load8<WIDE>(g, reinterpret_cast<const __nv_bfloat16 *>(grad - 1) + at, lane, left);
+    else load8<WIDE>(g, reinterpret_cast<const float *>(grad) + at, lane, left);
+    if (x.flags & kParamBf16) load8<WIDE>(p, static_cast<const __nv_bfloat16 *>(x.param) + at, lane, left);
+    else load8<WIDE>(p, static_cast<const float *>(x.param) + at, lane, left);
+    if (EIGHT) {
+        load_codes<WIDE>(qm, static_cast<const uint8_t *>(x.m) + at, lane, left);
+        load_codes<WIDE>(qv, static_cast<const uint8_t *>(x.v) + at, lane, left);
+        sc = *reinterpret_cast<const float2 *>(x.scales + at / kBlock * 2);
+        decode(m, qm, sc.x);
+        decode(v, qv, sc.y);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] *= v[j];
+    } else {
+        load8<WIDE>(m, static_cast<const float *>(x.m) + at, lane, left);
+        load8<WIDE>(v, static_cast<const float *>(x.v) + at, lane, left);
+    }
+    const float kept = fmaf(-c.lr, x.decay, 1.f);
+    float root[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float gj = g[j] * c.factor;
+        m[j] = fmaf(s.rest1, gj - m[j], m[j]);
+        v[j] = fmaf(s.rest2, fmaf(gj, gj, -v[j]), v[j]);
+        root[j] = EIGHT ? sqrt_fast(v[j]) : sqrtf(v[j]);
+        const float below = fmaf(root[j], c.inverse_root, s.eps), above = c.rate * m[j];
+        p[j] = fmaf(p[j], kept, -(EIGHT ? divide(above, below) : __fdiv_rn(above, below)));
+    }
+    if (x.flags & kParamBf16) store8<WIDE>(p, static_cast<__nv_bfloat16 *>(x.param) + at, lane, left);
+    else store8<WIDE>(p, static_cast<float *>(x.param) + at, lane, left);
+    if (x.copy) store8<WIDE>(p, x.copy + at, lane, left);
+    if (!EIGHT) {
+        store8<WIDE>(m, static_cast<float *>(x.m) + at, lane, left);
+        store8<WIDE>(v, static_cast<float *>(x.v) + at, lane, left);
+        return;
+    }
+    // sizes as unsigned integers order as the sizes do, with a NaN above them all
+    uint32_t top_m = 0, top_v = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (element<WIDE>(lane, j) < left) {
+            top_m = max(top_m, __float_as_uint(m[j]) & 0x7fffffffu);
+            top_v = max(top_v, __float_as_uint(root[j]) & 0x7fffffffu);
+        }
+    const float tm = __uint_as_float(warp_top(__uint_as_float(top_m))), tv = __uint_as_float(warp_top(__uint_as_float(top_v)));
+    // below 2^-110 a block's states are zeros: 448 / top would leave float32
+    const float im = tm < 0x1p-110f ? 0.f : __fdiv_rn(448.f, tm), iv = tv < 0x1p-110f ? 0.f : __fdiv_rn(448.f, tv);
+    if (lane == 0)
+        *reinterpret_cast<float2 *>(x.scales + at / kBlock * 2) =
+            make_float2(tm < 0x1p-110f ? 0.f : __fdiv_rn(tm, 448.f), tv < 0x1p-110f ? 0.f : __fdiv_rn(tv, 448.f));
+    qm[0] = qm[1] = qv[0] = qv[1] = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t h = mix((uint32_t)(at + element<WIDE>(lane, j)) * kStride + start);
+        const float am = fminf(fabsf(m[j] * im), 448.f), av = fminf(root[j] * iv, 448.f);
+        const uint32_t cm = round_code(am, h & 0xffffu) | (__float_as_uint(m[j]) >> 24 & 0x80u);
+        const uint32_t cv = round_square(av, h >> 16);
+        qm[j >> 2] |= cm << (j & 3) * 8;
+        qv[j >> 2] |= cv << (j & 3) * 8;
+    }
+    store_codes<WIDE>(qm, static_cast<uint8_t *>(x.m) + at, lane, left);
+    store_codes<WIDE>(qv, static_cast<uint8_t *>(x.v) + at, lane, left);
+}
+
+template <bool EIGHT>
+__global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ Step s, const __grid_constant__ Grads grads) {
+    __shared__ Scalars shared;
+    __shared__ double part[kThreads / 32];
+    pdl_begin();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const double *sums = reinterpret_cast<const double *>(s.plan + kSumsAt);
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < s.sums; i += kThreads) sum += sums[i];
+    if (s.sums) {
+#pragma unroll
+        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (lane == 0) part[warp] = sum;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) {
+        const int64_t t = *s.step + 1;
+        Scalars c;
+        c.factor = 1.f;
+        if (s.sums) {
+            sum = 0.0;
+            for (int i = 0; i < kThreads / 32; ++i) sum += part[i];
+            const float norm = (float)sqrt(sum);
+            if (norm > s.max_norm) c.factor = __fdiv_rn(s.max_norm, norm);
+            if (blockIdx.x == 0 && s.norm) *s.norm = norm;
+        }
+        c.lr = s.lr_at ? *s.lr_at : s.lr;
+        c.rate = __fdiv_rn(c.lr, rest_of_power((float)t, s.log1_hi, s.log1_lo));
+        c.inverse_root = __fdiv_rn(1.f, sqrtf(rest_of_power((float)t, s.log2_hi, s.log2_lo)));
+        c.start = mix((uint32_t)t * kStride + s.seed);
+        shared = c;
+        if (s.last) {        // the block that reads the step last moves it on
+            Header *h = reinterpret_cast<Header *>(s.plan);
+            __threadfence();
+            if (atomicAdd(&h->ticket, 1u) == gridDim.x - 1) {
+                h->ticket = 0;
+                *s.step = t;
+            }
+        }
+    }
+    __syncthreads();
+    const Scalars c = shared;
+    const Tensor *tensors = reinterpret_cast<const Tensor *>(s.plan + kTensorsAt);
+    const int32_t *of = reinterpret_cast<const int32_t *>(tensors + s.tensors);
+    for (int32_t chunk = s.chunk + blockIdx.x; chunk < s.chunks; chunk += gridDim.x) {
+        const int32_t i = of[chunk];
+        const uint64_t grad = grads.at[i - s.first];
+        if (!grad) continue;
+        const Tensor x = tensors[i];
+        const uint32_t start = mix(c.start + (uint32_t)i);
+        const bool wide = (x.flags & kWide) && (grad & 1 ? grad % 16 == 1 : grad % 32 == 0);
+        int64_t at = (int64_t)(chunk - x.first) * kChunk + warp * kBlock;
+        const int64_t end = min(x.n, (int64_t)(chunk - x.first + 1) * kChunk);
+        for (; at < end; at += kThreads / 32 * kBlock) {
+            if (wide) update<EIGHT, true>(x, grad, at, lane, c, s, start);
+            else update<EIGHT, false>(x, grad, at, lane, c, s, start);
+        }
+    }
+}
+
+// Sum of squares of a block's chunks; `sum` says where in the table.
+__global__ void __launch_bounds__(kThreads) adamw_norm_kernel(const __grid_constant__ Step s, const __grid_constant__ Grads grads, int32_t to) {
+    __shared__ double part[kThreads / 32];
+    pdl_begin();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const Tensor *tensors = reinterpret_cast<const Tensor *>(s.plan + kTensorsAt);
+    const int32_t *of = reinterpret_cast<const int32_t *>(tensors + s.tensors);
+    double sum = 0.0;
+    for (int32_t chunk = s.chunk + blockIdx.x; chunk < s.chunks; chunk += gridDim.x) {
+        const int32_t i = of[chunk];
+        const uint64_t grad = grads.at[i - s.first];
+        if (!grad) continue;
+        const int64_t n = tensors[i].n, first = (int64_t)(chunk - tensors[i].first) * kChunk;
+        const bool bf = grad & 1, wide = n % 8 == 0 && (bf ? grad % 16 == 1 : grad % 32 == 0);
+        float g[kChunk / kThreads / 8][8];
+#pragma unroll
+        for (int k = 0; k < kChunk / kThreads / 8; ++k) {
+            const int64_t at = first + (k * (kThreads / 32) + warp) * kBlock;
+            const int left = (int)max((int64_t)0, min((int64_t)kBlock, n - at));
+            if (bf) {
+                const __nv_bfloat16 *q = reinterpret_cast<const __nv_bfloat16 *>(grad - 1) + at;
+                wide ? load8<true>(g[k], q, lane, left) : load8<false>(g[k], q, lane, left);
+            } else {
+                const float *q = reinterpret_cast<const float *>(grad) + at;
+                wide ? load8<true>(g[k], q, lane, left) : load8<false>(g[k], q, lane, left);
+            }
+        }
+        float squares = 0.f;
+#pragma unroll
+        for (int k = 0; k < kChunk / kThreads / 8; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) squares = fmaf(g[k][j], g[k][j], squares);
+        sum += (double)squares;
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) part[warp] = sum;
+    __syncthreads();
+    if (threadIdx.x) return;
+    sum = 0.0;
+    for (int i = 0; i < kThreads / 32; ++i) sum += part[i];
+    reinterpret_cast<double *>(s.plan + kSumsAt)[to + blockIdx.x] = sum;
+}
+
+dendsn_status check(const dendsn_adamw_config *c) {
+    if (!c) return seq_fail(DENDSN_ERR_INVALID_ARG, "cfg is NULL");
+    if (!std::isfinite(c->lr) || !(c->beta1 >= 0 && c->beta1 < 1) || !(c->beta2 >= 0 && c->beta2 < 1) ||
+        !(c->eps >= 0 && std::isfinite(c->eps)) || !(c->max_norm >= 0 && std::isfinite(c->max_norm)))
+        return seq_fail(DENDSN_ERR_INVALID_ARG, "lr must be finite, the betas in [0, 1), eps and max_norm finite and not negative");
+    if (c->state != DENDSN_STATE_F32 && c->state != DENDSN_STATE_E4M3) return seq_fail(DENDSN_ERR_INVALID_ARG, "unknown state");
+    return DENDSN_OK;
+}
+
+int64_t chunks_of(int64_t n) { return (n + kChunk - 1) / kChunk; }
+
+}  // namespace
+}  // namespace dendsn
+
+using namespace dendsn;
+
+extern "C" {
+
+dendsn_status dendsn_adamw_plan(const dendsn_adamw_config *cfg, const dendsn_adamw_tensor *tensors, int32_t count, void *table, size_t *table_bytes) {
+    dendsn_status st = check(cfg);
+    if (st != DENDSN_OK) return st;
+    if (count < 0 || (count && !tensors)) return seq_fail(DENDSN_ERR_INVALID_ARG, "tensors is NULL or count negative");
+    const bool eight = cfg->state == DENDSN_STATE_E4M3;
+    const size_t ss = eight ? 1 : 4;
+    int64_t chunks = 0;
+    for (int32_t i = 0; i < count; ++i) {
+        const dendsn_adamw_tensor &t = tensors[i];
+        if (t.n < 0 || (t.param_dtype != DENDSN_F32 && t.param_dtype != DENDSN_BF16) || !std::isfinite(t.weight_decay))
+            return seq_fail(DENDSN_ERR_INVALID_ARG, "tensor %d: n negative, unknown param_dtype or weight_decay not finite", i);
+        if (t.n && (!t.param || !t.m || !t.v || (eight && !t.scales)))
+            return seq_fail(DENDSN_ERR_INVALID_ARG, "tensor %d: param, m, v or scales is NULL", i);
+        if (!seq_aligned(t.param, t.param_dtype == DENDSN_BF16 ? 2 : 4) || !seq_aligned(t.m, ss) || !seq_aligned(t.v, ss) ||
+            !seq_aligned(t.scales, 8) || !seq_aligned(t.copy, 2))
+            return seq_fail(DENDSN_ERR_MISALIGNED, "tensor %d: param, m, v, scales (8 bytes) or copy misaligned", i);
+        chunks += chunks_of(t.n);
+    }
+    if (chunks > INT32_MAX) return seq_fail(DENDSN_ERR_UNSUPPORTED, "more than 2^31 chunks of %d elements", kChunk);
+    if (table_bytes) *table_bytes = kTensorsAt + (size_t)count * sizeof(Tensor) + (size_t)chunks * 4;
+    if (!table) return DENDSN_OK;
+    if (!seq_aligned(table, 8)) return seq_fail(DENDSN_ERR_MISALIGNED, "table must be 8-byte aligned");
+    uint8_t *to = static_cast<uint8_t *>(table);
+    std::fill(to, to + kTensorsAt, (uint8_t)0);
+    Tensor *x = reinterpret_cast<Tensor *>(to + kTensorsAt);
+    int32_t *of = reinterpret_cast<int32_t *>(x + count);
+    int32_t first = 0;
+    for (int32_t i = 0; i < count; ++i) {
+        const dendsn_adamw_tensor &t = tensors[i];
+        const bool bf = t.param_dtype == DENDSN_BF16;
+        const bool wide = t.n % 8 == 0 && seq_aligned(t.param, bf ? 16 : 32) && seq_aligned(t.m, 8 * ss) && seq_aligned(t.v, 8 * ss) && seq_aligned(t.copy, 16);
+        x[i] = Tensor{t.param, t.m, t.v, t.scales, static_cast<__nv_bfloat16 *>(t.copy), t.n, first,
+                      (bf ? kParamBf16 : 0) | (wide ? kWide : 0), (float)t.weight_decay, 0};
+        const int32_t end = first + (int32_t)chunks_of(t.n);
+        for (; first < end; ++first) of[first] = i;
+    }
+    return DENDSN_OK;
+}
+
+dendsn_status dendsn_adamw_step(const dendsn_adamw_config *cfg, void *plan, const int64_t *sizes, int32_t count, const void *const *grads,
+                                const int32_t *grad_dtypes, int64_t *step, const float *lr, float *norm, void *stream) {
+    dendsn_status st = check(cfg);
+    if (st != DENDSN_OK) return st;
+    if (count < 0 || (count && (!sizes || !grads || !grad_dtypes))) return seq_fail(DENDSN_ERR_INVALID_ARG, "sizes, grads or grad_dtypes is NULL or count negative");
+    if (!plan || !step) return seq_fail(DENDSN_ERR_INVALID_ARG, "plan or step is NULL");
+    if (!seq_aligned(plan, 16) || !seq_aligned(step, 8) || !seq_aligned(lr, 4) || !seq_aligned(norm, 4))
+        return seq_fail(DENDSN_ERR_MISALIGNED, "plan (16 bytes), step, lr or norm misaligned");
+    for (int32_t i = 0; i < count; ++i) {
+        if (sizes[i] < 0 || (grad_dtypes[i] != DENDSN_F32 && grad_dtypes[i] != DENDSN_BF16))
+            return seq_fail(DENDSN_ERR_INVALID_ARG, "tensor %d: size negative or unknown grad_dtype", i);
+        if (!seq_aligned(grads[i], grad_dtypes[i] == DENDSN_BF16 ? 2 : 4))
+            return seq_fail(DENDSN_ERR_MISALIGNED, "tensor %d: gradient misaligned", i);
+    }
+    const bool clip = cfg->max_norm > 0;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    Step a = {};
+    a.plan = static_cast<uint8_t *>(plan);
+    a.step = step;
+    a.lr_at = lr;
+    a.norm = norm;
+    a.tensors = count;
+    a.lr = (float)cfg->lr;
+    a.eps = (float)cfg->eps;
+    a.max_norm = (float)cfg->max_norm;
+    a.rest1 = (float)(1.0 - cfg->beta1);
+    a.rest2 = (float)(1.0 - cfg->beta2);
+    // the logarithm of a beta of 0 as one whose power is 0 from the first step on
+    const double l1 = cfg->beta1 > 0 ? std::log(cfg->beta1) : -1e4, l2 = cfg->beta2 > 0 ? std::log(cfg->beta2) : -1e4;
+    a.log1_hi = (float)l1, a.log1_lo = (float)(l1 - (double)a.log1_hi);
+    a.log2_hi = (float)l2, a.log2_lo = (float)(l2 - (double)a.log2_hi);
+    a.seed = cfg->seed;
+    const int rounds = std::max(1, (count + kGrads - 1) / kGrads);
+    // blocks of each launch: the sums of squares of all launches have to fit the table
+    const int most = std::max(1, kMostBlocks / rounds);
+    if (clip && rounds > kMostBlocks) return seq_fail(DENDSN_ERR_UNSUPPORTED, "clipping over more than %d tensors", kGrads * kMostBlocks);
+    Grads g;
+    int launches = 0;
+    cudaError_t e = cudaSuccess;
+    for (int pass = clip ? 0 : 1; pass < 2 && e == cudaSuccess; ++pass) {
+        int32_t chunk = 0;
+        int sums = 0;
+        for (int r = 0; r < rounds && e == cudaSuccess; ++r) {
+            a.first = r * kGrads;
+            a.chunk = chunk;
+            const int32_t end = std::min(count, a.first + kGrads);
+            for (int32_t i = a.first; i < end; ++i) {
+                g.at[i - a.first] = grads[i] ? reinterpret_cast<uint64_t>(grads[i]) + (grad_dtypes[i] == DENDSN_BF16 ? 1 : 0) : 0;
+                chunk += (int32_t)chunks_of(sizes[i]);
+            }
+            a.chunks = chunk;
+            a.last = r == rounds - 1;
+            const int blocks = std::max(1, std::min(a.chunks - a.chunk, pass ? kMostBlocks : most));
+            if (pass == 0) {
+                e = seq_launch(adamw_norm_kernel, dim3((unsigned)blocks), kThreads, 0, s, 1, a, g, sums);
+                sums += blocks;
+            } else {
+                e = cfg->state == DENDSN_STATE_E4M3 ? seq_launch(adamw_kernel<true>, dim3((unsigned)blocks), kThreads, 0, s, 1, a, g)
+                                                     : seq_launch(adamw_kernel<false>, dim3((unsigned)blocks), kThreads, 0, s, 1, a, g);
+            }
+            ++launches;
+        }
+        if (pass == 0) a.sums = sums;
+    }
+    if (e != cudaSuccess) return seq_fail(DENDSN_ERR_CUDA, "adamw launch failed: %s", cudaGetErrorString(e));
+    seq_count_launches(launches);
+    return DENDSN_OK;
+}
+
+}  // extern "C"

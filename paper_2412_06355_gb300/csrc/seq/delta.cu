@@ -1,0 +1,1395 @@
+// Gated delta rule: a matrix of fast weights for every head that a token's key reads, corrects and
+// writes,
+//   S_t = a_t S_{t-1} + k_t u_t^T,  u_t = b_t (v_t - a_t S_{t-1}^T k_t),  a_t = exp(gate_t),
+//   o_t = scale S_t^T q_t
+// and its gradient, in chunks of 64 tokens. Within a chunk, with G_i the sum of the gates up to token i,
+// L_ij = exp(G_i - G_j) (k_i . k_j) below the diagonal, P_ij = exp(G_i - G_j) (q_i . k_j) up to it,
+// first_i = exp(G_i), rest_i = exp(G_last - G_i) and S the state before the chunk:
+//   e  = (1 + L diag(b))^-1 (v - first k S),   u = b e
+//   o  = scale (first q S + P u),              S' = exp(G_last) S + k^T (rest u)
+// and back, with D the gradient of the state behind the chunk:
+//   d  = scale P^T go + rest k D,  y = ((1 + diag(b) L)^-1)^T d,  gv = b y,  gb = e . y
+//   D' = exp(G_last) D + q^T (scale first go) - k^T (first b y)
+//   gq = scale first go S^T + A k,           A_ij  = scale exp(G_i - G_j) go_i . u_j   (j <= i)
+//   gk = rest u D^T - first b y S^T + A^T q + (C + C^T) k, C_ij = -exp(G_i - G_j) b_i y_i . u_j   (j < i)
+//   ggate_t = <D, S'> + the sum over i >= t of the chunk of (q_i . gq_i - v_i . gv_i)
+// (every exponent in q's gradient raises a product of q, and so on: the sum of what each G_i gains).
+//
+// What has no order runs for all chunks at once: the square matrices (delta_prepare_kernel), the
+// gradients of q, k and the gates (delta_gradients_kernel). In between a block carries the state of one
+// head, or the gradient of it, from chunk to chunk (delta_forward_kernel, delta_backward_kernel): a warp
+// has 16 columns of v in registers, state and results turned (columns of v are the products' rows), so
+// that each product's result is the next one's left factor without leaving the registers; the warps
+// meet once a chunk, for the tiles.
+//
+// All sums are float32. Products run on the matrix instruction for 16-bit operands: bfloat16 inputs are
+// exact, everything else (float32 inputs, states, results on their way to the next product) is split into
+// three bfloat16 terms, whose leading products (three with an exact factor, six without) leave 2^-24.
+// Where only a bfloat16 gradient of q or k comes of it, two terms (2^-17 of each factor).
+#include <cuda_bf16.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "delta_plan.h"
+#include "fragments.cuh"
+#include "seq_common.h"
+
+namespace dendsn {
+namespace {
+
+constexpr int C = kDeltaChunk;
+constexpr int kWarps = 8;
+constexpr float kLeastGate = -200.f;       // exp of it is 0 in float32
+
+// Places in a chunk's gate values.
+enum { kFirst = 0, kRest = 64, kBeta = 128, kHigh = 192, kLow = 256, kKeep = 320 };
+
+struct Args {
+    int32_t T, B, Hk, Hv, Dk, Dv, layout;
+    float scale;
+    const int32_t *offsets;
+    DeltaPlan p;
+};
+
+struct Sequence {
+    int64_t row, step;         // its first token, tokens between two of its own
+    int64_t slot;              // its first chunk's
+    int32_t length;
+};
+
+__device__ __forceinline__ Sequence sequence(const Args &a, int b) {
+    Sequence s;
+    if (a.layout == DENDSN_DELTA_PACKED) {
+        const int32_t lo = min(max(a.offsets[b], 0), a.T), hi = min(max(a.offsets[b + 1], lo), a.T);
+        s.row = lo, s.step = 1, s.length = hi - lo;
+        s.slot = lo / C + b;
+    } else {
+        const bool time = a.layout == DENDSN_DELTA_TIME;
+        s.row = time ? b : (int64_t)b * a.T, s.step = time ? a.B : 1, s.length = a.T;
+        s.slot = (int64_t)b * ((a.T + C - 1) / C);
+    }
+    return s;
+}
+
+// Which sequence a chunk's slot belongs to; false: to none. A packed sequence from token lo on has the
+// slots from lo / 64 + (its number) on: no two meet, and the last one's stay below T / 64 + B.
+__device__ __forceinline__ bool locate(const Args &a, int64_t slot, int *b, int *chunk, Sequence *s) {
+    if (a.layout == DENDSN_DELTA_PACKED) {
+        int lo = 0, hi = a.B - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) / 2;
+            if (min(max(a.offsets[mid], 0), a.T) / C + mid <= slot) lo = mid;
+            else hi = mid - 1;
+        }
+        *b = lo;
+    } else {
+        *b = (int)(slot / ((a.T + C - 1) / C));
+    }
+    *s = sequence(a, *b);
+    const int64_t c = slot - s->slot;
+    *chunk = (int)c;
+    return c >= 0 && c * C < s->length;
+}
+
+template <typename T>
+__device__ __forceinline__ float value(const T *p) { return __bfloat162float(*p); }
+template <>
+__device__ __forceinline__ float value<float>(const float *p) { return *p; }
+
+// 8 neighbours of a row from `at` on, zeros behind its end.
+template <typename T>
+__device__ __forceinline__ void eight(float (&v)[8], const T *row, int at, int end, bool wide) {
+    if (wide && at + 8 <= end) {
+        if constexpr (sizeof(T) == 2) {
+            const auto q = *reinterpret_cast<const Lot<T, 8> *>(row + at);
+            q.get(v);
+        } else {
+            const float4 x = *reinterpret_cast<const float4 *>(row + at), y = *reinterpret_cast<const float4 *>(row + at + 4);
+            v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w, v[4] = y.x, v[5] = y.y, v[6] = y.z, v[7] = y.w;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = at + e < end ? value(row + at + e) : 0.f;
+    }
+}
+
+// ------------------------------------------------------------------ values as tiles
+// A chunk's rows of v or go, turned: [term][columns of 8][tokens of 8] blocks whose rows are columns of v.
+template <typename T>
+__global__ void __launch_bounds__(256) delta_turn_kernel(const __grid_constant__ Args a, const T *from, uint8_t *to, bool wide) {
+    constexpr int NT = sizeof(T) == 2 ? 1 : 3;
+    __shared__ float tile[C * (kDeltaMost + 1)];
+    pdl_begin();
+    int b, chunk;
+    Sequence s;
+    if (!locate(a, blockIdx.x, &b, &chunk, &s)) return;
+    const int h = blockIdx.y, DVP = a.p.DVP, left = min(C, s.length - chunk * C), stride = DVP + 1;
+    for (int i = threadIdx.x; i < C * DVP / 8; i += 256) {
+        const int tok = i / (DVP / 8), at = i % (DVP / 8) * 8;
+        float v[8] = {};
+        if (tok < left) eight(v, from + ((s.row + (int64_t)(chunk * C + tok) * s.step) * a.Hv + h) * a.Dv, at, a.Dv, wide);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) tile[tok * stride + at + e] = v[e];
+    }
+    __syncthreads();
+    uint32_t *out = reinterpret_cast<uint32_t *>(to + ((int64_t)blockIdx.x * a.Hv + h) * a.p.value_bytes);
+    const int lane = threadIdx.x & 31, words = C * DVP / 2;
+    for (int i = threadIdx.x; i < words; i += 256) {
+        const int cell = i / 32, col = cell / 8 * 8 + lane / 4, tok = cell % 8 * 8 + lane % 4 * 2;
+        uint32_t q[NT];
+        split<NT>(q, tile[tok * stride + col], tile[(tok + 1) * stride + col]);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) out[t * words + i] = q[t];
+    }
+}
+
+// ------------------------------------------------------------------ square matrices of a chunk
+// exp(G_i - G_j): the sums as two floats each, so that far below zero no bits of a difference are lost.
+__device__ __forceinline__ float between(const float *gates, int i, int j) {
+    return expf((gates[kHigh + i] - gates[kHigh + j]) + (gates[kLow + i] - gates[kLow + j]));
+}
+
+// One block of 128 threads for a chunk and value head: tiles of k and q (by the first value head of a
+// key head), the gates' sums and exponentials, P, and the inverses (1 + L diag(b))^-1 and, for the
+// backward, (1 + diag(b) L)^-1 by columns: a thread solves one column by substitution, its results in
+// registers, L's rows read by all.
+template <typename T, int DKP, bool KEEP>
+__global__ void __launch_bounds__(128) delta_prepare_kernel(const __grid_constant__ Args a, const T *q, const T *k, const float *gate,
+                                                            const float *beta, uint8_t *kept, bool wide) {
+    constexpr int NT = sizeof(T) == 2 ? 1 : 3, W = DKP / 8, TILE = 64 * DKP * 2;
+    extern __shared__ __align__(128) uint8_t smem[];
+    float *L = reinterpret_cast<float *>(smem);                        // [64][64]
+    float *gates = L + 64 * 64;
+    uint8_t *ktile = reinterpret_cast<uint8_t *>(gates + kGateFloats), *qtile = ktile + NT * TILE;
+    float *X = reinterpret_cast<float *>(ktile);                        // [2][64][65], after the products
+    pdl_begin();
+    int b, chunk;
+    Sequence s;
+    if (!locate(a, blockIdx.x, &b, &chunk, &s)) return;
+    const int h = blockIdx.y, group = a.Hv / a.Hk, hk = h / group, left = min(C, s.length - chunk * C);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane / 4, t = lane % 4;
+    const int64_t first = s.row + (int64_t)chunk * C * s.step, head = (int64_t)blockIdx.x * a.Hv + h;
+    for (int i = threadIdx.x; i < 2 * C * W; i += 128) {
+        const bool isq = i >= C * W;
+        const int j = i % (C * W), tok = j / W, cell = j % W;
+        float v[8] = {};
+        if (tok < left) eight(v, (isq ? q : k) + ((first + tok * s.step) * a.Hk + hk) * a.Dk, cell * 8, a.Dk, wide);
+        uint32_t x[4][NT];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) split<NT>(x[e], v[2 * e], v[2 * e + 1]);
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+            *reinterpret_cast<uint4 *>((isq ? qtile : ktile) + n * TILE + ((tok / 8) * W + cell) * kCell + (tok & 7) * 16) =
+                make_uint4(x[0][n], x[1][n], x[2][n], x[3][n]);
+    }
+    if (warp == 0) {           // sums of the gates, in float64: lane l has tokens 2l and 2l + 1
+        float r[2], bt[2];
+        double sum[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int i = 2 * lane + e;
+            const int64_t at = (first + i * s.step) * a.Hv + h;
+            r[e] = i < left ? gate[at] : 0.f;
+            bt[e] = i < left ? beta[at] : 0.f;
+            if (r[e] < kLeastGate) r[e] = kLeastGate;
+        }
+        sum[0] = (double)r[0];
+        sum[1] = sum[0] + (double)r[1];
+        double before = sum[1];
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const double up = __shfl_up_sync(0xffffffffu, before, o);
+            if (lane >= o) before += up;
+        }
+        before -= sum[1];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const double G = before + sum[e];
+            const int i = 2 * lane + e;
+            gates[kHigh + i] = (float)G;
+            gates[kLow + i] = (float)(G - (double)gates[kHigh + i]);
+            gates[kBeta + i] = bt[e];
+        }
+        __syncwarp();
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int i = 2 * lane + e;
+            gates[kFirst + i] = expf(gates[kHigh + i] + gates[kLow + i]);
+            gates[kRest + i] = between(gates, C - 1, i);
+            gates[kKeep + i] = expf(gates[kHigh + C - 1] + gates[kLow + C - 1]);
+        }
+    }
+    __syncthreads();
+    uint8_t *kimage = kept + a.p.k + ((int64_t)blockIdx.x * a.Hk + hk) * a.p.key_bytes, *qimage = kept + a.p.q + ((int64_t)blockIdx.x * a.Hk + hk) * a.p.key_bytes;
+    if (h % group == 0)
+        for (int i = threadIdx.x; i < NT * TILE / 16; i += 128) {
+            reinterpret_cast<uint4 *>(kimage)[i] = reinterpret_cast<const uint4 *>(ktile)[i];
+            reinterpret_cast<uint4 *>(qimage)[i] = reinterpret_cast<const uint4 *>(qtile)[i];
+        }
+    float *gout = reinterpret_cast<float *>(kept + a.p.gates) + head * kGateFloats;
+    for (int i = threadIdx.x; i < kGateFloats; i += 128) gout[i] = gates[i];
+    // k k^T and q k^T, 16 rows a warp
+    float kk[8][4] = {}, qk[8][4] = {};
+    const uint32_t kt = tc::smem_addr(ktile), qt = tc::smem_addr(qtile);
+#pragma unroll 2
+    for (int ks = 0; ks < W / 2; ++ks) {
+        uint32_t ak[NT][4], aq[NT][4], r[4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            left_rows(ak[n], kt + n * TILE, W, 2 * warp, 2 * ks);
+            left_rows(aq[n], qt + n * TILE, W, 2 * warp, 2 * ks);
+        }
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+            if (p > warp) break;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                right_rows(r, kt + n * TILE, W, 2 * p, 2 * ks);
+#pragma unroll
+                for (int m = 0; m + n < NT; ++m) {
+                    multiply(kk[2 * p], ak[m], r[0], r[1]);
+                    multiply(kk[2 * p + 1], ak[m], r[2], r[3]);
+                    multiply(qk[2 * p], aq[m], r[0], r[1]);
+                    multiply(qk[2 * p + 1], aq[m], r[2], r[3]);
+                }
+            }
+        }
+    }
+    uint32_t *pout = reinterpret_cast<uint32_t *>(kept + a.p.p + head * kSquare);
+#pragma unroll
+    for (int n = 0; n < 8; ++n)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int i = warp * 16 + half * 8 + g, j = n * 8 + 2 * t;
+            float w[2], lo[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float x = j + e <= i ? between(gates, i, j + e) : 0.f;
+                w[e] = j + e <= i ? x * qk[n][2 * half + e] : 0.f;
+                lo[e] = j + e < i ? x * kk[n][2 * half + e] : 0.f;
+            }
+            uint32_t x[3];
+            split<3>(x, w[0], w[1]);
+#pragma unroll
+            for (int m = 0; m < 3; ++m) pout[m * 2048 + ((warp * 2 + half) * 8 + n) * 32 + lane] = x[m];
+            *reinterpret_cast<float2 *>(L + i * 64 + j) = make_float2(lo[0], lo[1]);
+        }
+    __syncthreads();
+    if (KEEP || threadIdx.x < 64) {
+        const int c = threadIdx.x & 63;
+        const bool back = threadIdx.x >= 64;
+        float z[64];
+        float *x = X + (back ? 64 * 65 : 0) + c;
+#pragma unroll
+        for (int i = 0; i < 64; ++i) {
+            float d[4] = {};
+#pragma unroll
+            for (int j = 0; j < i; j += 4) {
+                const float4 l = *reinterpret_cast<const float4 *>(L + i * 64 + j);
+                d[0] = fmaf(l.x, z[j], d[0]);
+                if (j + 1 < i) d[1] = fmaf(l.y, z[j + 1], d[1]);
+                if (j + 2 < i) d[2] = fmaf(l.z, z[j + 2], d[2]);
+                if (j + 3 < i) d[3] = fmaf(l.w, z[j + 3], d[3]);
+            }
+            const float sum = (d[0] + d[1]) + (d[2] + d[3]), one = i == c ? 1.f : 0.f, bi = gates[kBeta + i];
+            const float r = back ? fmaf(-bi, sum, one) : one - sum;
+            z[i] = back ? r : bi * r;
+            x[i * 65] = r;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int m = 0; m < (KEEP ? 2 : 1); ++m) {
+        uint32_t *out = reinterpret_cast<uint32_t *>(kept + (m ? a.p.xu : a.p.xe) + head * kSquare);
+        const float *x = X + m * 64 * 65;
+        for (int i = threadIdx.x; i < 2048; i += 128) {
+            const int cell = i / 32, row = cell / 8 * 8 + g, col = cell % 8 * 8 + 2 * t;
+            uint32_t w[3];
+            split<3>(w, x[row * 65 + col], x[row * 65 + col + 1]);
+#pragma unroll
+            for (int n = 0; n < 3; ++n) out[n * 2048 + i] = w[n];
+        }
+    }
+}
+
+// ------------------------------------------------------------------ from chunk to chunk
+// A stage of shared memory: a chunk's tiles.
+struct Stage {
+    uint32_t k, q, x, p, v, gates, bytes;
+};
+__host__ __device__ inline Stage stage_of(const DeltaPlan &p, int warps) {
+    Stage s;
+    s.k = 0;
+    s.q = s.k + (uint32_t)p.key_bytes;
+    s.x = s.q + (uint32_t)p.key_bytes;
+    s.p = s.x + kSquare;
+    s.v = s.p + kSquare;
+    s.gates = s.v + (uint32_t)(p.terms * warps * 2048);
+    s.bytes = s.gates + kGateFloats * 4;
+    return s;
+}
+
+struct Tiles {                 // of a chunk and head, in global memory
+    const uint8_t *k, *q, *x, *p, *v, *gates;
+};
+__device__ __forceinline__ Tiles tiles_of(const Args &a, const uint8_t *kept, const uint8_t *values, size_t x, int64_t slot, int h) {
+    const int64_t hk = slot * a.Hk + h / (a.Hv / a.Hk), hv = slot * a.Hv + h;
+    return {kept + a.p.k + hk * a.p.key_bytes, kept + a.p.q + hk * a.p.key_bytes, kept + x + hv * kSquare,
+            kept + a.p.p + hv * kSquare, values + hv * a.p.value_bytes, kept + a.p.gates + hv * kGateFloats * 4};
+}
+// One thread: the chunk's tiles into a stage, of v the `warps` * 16 columns from `tile` * 16 on.
+template <int NT>
+__device__ __forceinline__ void load_stage(const Args &a, const Stage &st, uint32_t smem, uint32_t bar, const Tiles &g, int tile, int warps) {
+    tc::bar_expect(bar, st.bytes);
+    load_bytes(smem + st.k, g.k, (uint32_t)a.p.key_bytes, bar);
+    load_bytes(smem + st.q, g.q, (uint32_t)a.p.key_bytes, bar);
+    load_bytes(smem + st.x, g.x, kSquare, bar);
+    load_bytes(smem + st.p, g.p, kSquare, bar);
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+        load_bytes(smem + st.v + n * warps * 2048, g.v + ((size_t)n * a.p.DVP / 16 + tile) * 2048, warps * 2048, bar);
+    load_bytes(smem + st.gates, g.gates, kGateFloats * 4, bar);
+}
+
+// The pair of values of a lane in block (column block c, token block n) of a slice of `warps` * 16
+// columns: the sum of its terms.
+template <int NT>
+__device__ __forceinline__ float2 pair_of(const uint8_t *tile, size_t term, int cell) {
+    float2 r = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int n = NT - 1; n >= 0; --n) {
+        const uint32_t w = *reinterpret_cast<const uint32_t *>(tile + n * term + cell * kCell + (threadIdx.x & 31) * 4);
+        r.x += bf16_low(w), r.y += bf16_high(w);
+    }
+    return r;
+}
+// A warp's 16 columns and `cells` * 8 places as blocks of N terms: [term][columns of 8][places of 8].
+template <int N, int CELLS>
+__device__ __forceinline__ void keep_blocks(uint8_t *to, size_t term, int tile, const float (&v)[CELLS][4]) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int n = 0; n < CELLS; ++n)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            uint32_t q[N];
+            split<N>(q, v[n][2 * half], v[n][2 * half + 1]);
+#pragma unroll
+            for (int m = 0; m < N; ++m)
+                *reinterpret_cast<uint32_t *>(to + m * term + ((tile * 2 + half) * CELLS + n) * kCell + lane * 4) = q[m];
+        }
+}
+
+// State of 16 columns of v (rows) and all Dk places, from and to [Dk, Dv] float32.
+template <int CELLS>
+__device__ __forceinline__ void read_state(float (&s)[CELLS][4], const float *from, int col, int Dk, int Dv) {
+    const int lane = threadIdx.x & 31, g = lane / 4, t = lane % 4;
+#pragma unroll
+    for (int n = 0; n < CELLS; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int c = col + g + (e >> 1) * 8, d = n * 8 + 2 * t + (e & 1);
+            s[n][e] = from && c < Dv && d < Dk ? from[(int64_t)d * Dv + c] : 0.f;
+        }
+}
+template <int CELLS>
+__device__ __forceinline__ void write_state(const float (&s)[CELLS][4], float *to, int col, int Dk, int Dv) {
+    const int lane = threadIdx.x & 31, g = lane / 4, t = lane % 4;
+#pragma unroll
+    for (int n = 0; n < CELLS; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int c = col + g + (e >> 1) * 8, d = n * 8 + 2 * t + (e & 1);
+            if (c < Dv && d < Dk) to[(int64_t)d * Dv + c] = s[n][e];
+        }
+}
+template <typename T>
+__device__ __forceinline__ void put(T *p, float v);
+template <>
+__device__ __forceinline__ void put<float>(float *p, float v) { *p = v; }
+template <>
+__device__ __forceinline__ void put<__nv_bfloat16>(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
+
+// A block's walk over its sequence's chunks: two stages where they fit, the next chunk's tiles on their
+// way while one is worked on. After a wait that ran out the states are NaN and no more is fetched.
+template <typename T, int DKP, bool KEEP>
+__global__ void __launch_bounds__(kWarps * 32, 1) delta_forward_kernel(const __grid_constant__ Args a, uint8_t *kept, const float *s0, T *o,
+                                                                       float *last, int stages) {
+    constexpr int NT = sizeof(T) == 2 ? 1 : 3, NS = sizeof(T) == 2 ? 2 : 3, W = DKP / 8, TILE = 64 * DKP * 2, SQ = kSquare / 3;
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ __align__(8) uint64_t bars[2];
+    pdl_begin();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, g = lane / 4, t = lane % 4;
+    const int b = blockIdx.x / a.Hv, h = blockIdx.x % a.Hv, tile0 = blockIdx.y * warps, tile = tile0 + warp;
+    const Sequence s = sequence(a, b);
+    const int chunks = (s.length + C - 1) / C;
+    const Stage st = stage_of(a.p, warps);
+    const uint32_t base = tc::smem_addr(smem), bar = tc::smem_addr(bars);
+    if (threadIdx.x == 0) {
+        tc::bar_init(bar, 1);
+        tc::bar_init(bar + 8, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        for (int n = 0; n < min(stages, chunks); ++n)
+            load_stage<NT>(a, st, base + n * st.bytes, bar + 8 * n, tiles_of(a, kept, kept + a.p.v, a.p.xe, s.slot + n, h), tile0, warps);
+    }
+    const int64_t state = ((int64_t)b * a.Hv + h) * a.Dk * a.Dv;
+    float S[W][4];
+    read_state<W>(S, s0 ? s0 + state : nullptr, tile * 16, a.Dk, a.Dv);
+    __syncthreads();
+    bool ok = true;
+    for (int n = 0; n < chunks; ++n) {
+        const int at = n % stages;
+        const int64_t hv = (s.slot + n) * a.Hv + h;
+        if (KEEP) keep_blocks<NS, W>(kept + a.p.s + hv * a.p.state_bytes, (size_t)a.p.DVP * DKP * 2, tile, S);
+        ok = ok && tc::bar_wait(bar + 8 * at, n / stages & 1);
+        if (!ok)
+#pragma unroll
+            for (int i = 0; i < W; ++i) S[i][0] = S[i][1] = S[i][2] = S[i][3] = __int_as_float(0x7fffffff);
+        const uint8_t *here = smem + at * st.bytes;
+        const uint32_t sk = base + at * st.bytes + st.k, sq = sk + st.q, sx = sk + st.x, sp = sk + st.p;
+        const float *gates = reinterpret_cast<const float *>(here + st.gates);
+        // k S and q S
+        float r[8][4] = {}, out[8][4] = {};
+#pragma unroll
+        for (int ks = 0; ks < W / 2; ++ks) {
+            if (ks * 16 >= a.Dk) break;
+            uint32_t x[3][4];
+            split_left<3>(x, S[2 * ks], S[2 * ks + 1]);
+#pragma unroll
+            for (int p = 0; p < 4; ++p)
+#pragma unroll
+                for (int m = 0; m < NT; ++m) {
+                    uint32_t f[4], f2[4];
+                    right_rows(f, sk + m * TILE, W, 2 * p, 2 * ks);
+                    right_rows(f2, sq + m * TILE, W, 2 * p, 2 * ks);
+#pragma unroll
+                    for (int i = 0; i + m < 3; ++i) {
+                        multiply(r[2 * p], x[i], f[0], f[1]);
+                        multiply(r[2 * p + 1], x[i], f[2], f[3]);
+                        multiply(out[2 * p], x[i], f2[0], f2[1]);
+                        multiply(out[2 * p + 1], x[i], f2[2], f2[3]);
+                    }
+                }
+        }
+        // v - first k S; the decayed state
+        const float keep = gates[kKeep];
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) S[i][e] *= keep;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float2 f = *reinterpret_cast<const float2 *>(gates + kFirst + i * 8 + 2 * t);
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const float2 v = pair_of<NT>(here + st.v, warps * 2048, (warp * 2 + half) * 8 + i);
+                r[i][2 * half] = fmaf(-f.x, r[i][2 * half], v.x);
+                r[i][2 * half + 1] = fmaf(-f.y, r[i][2 * half + 1], v.y);
+                out[i][2 * half] *= f.x;
+                out[i][2 * half + 1] *= f.y;
+            }
+        }
+        float e[8][4] = {};
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+            uint32_t x[3][4];
+            split_left<3>(x, r[2 * ks], r[2 * ks + 1]);
+#pragma unroll
+            for (int p = ks; p < 4; ++p)
+#pragma unroll
+                for (int m = 0; m < 3; ++m) {
+                    uint32_t f[4];
+                    right_rows(f, sx + m * SQ, 8, 2 * p, 2 * ks);
+#pragma unroll
+                    for (int i = 0; i + m < 3; ++i) {
+                        multiply(e[2 * p], x[i], f[0], f[1]);
+                        multiply(e[2 * p + 1], x[i], f[2], f[3]);
+                    }
+                }
+        }
+        if (KEEP) keep_blocks<3, 8>(kept + a.p.e + hv * a.p.kept_bytes, (size_t)a.p.DVP * C * 2, tile, e);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float2 bt = *reinterpret_cast<const float2 *>(gates + kBeta + i * 8 + 2 * t);
+            e[i][0] *= bt.x, e[i][1] *= bt.y, e[i][2] *= bt.x, e[i][3] *= bt.y;
+        }
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+            uint32_t x[3][4];
+            split_left<3>(x, e[2 * ks], e[2 * ks + 1]);
+#pragma unroll
+            for (int p = ks; p < 4; ++p)
+#pragma unroll
+                for (int m = 0; m < 3; ++m) {
+                    uint32_t f[4];
+                    right_rows(f, sp + m * SQ, 8, 2 * p, 2 * ks);
+#pragma unroll
+                    for (int i = 0; i + m < 3; ++i) {
+                        multiply(out[2 * p], x[i], f[0], f[1]);
+                        multiply(out[2 * p + 1], x[i], f[2], f[3]);
+                    }
+                }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float2 re = *reinterpret_cast<const float2 *>(gates + kRest + (2 * ks + i) * 8 + 2 * t);
+                float(&u)[4] = e[2 * ks + i];
+                u[0] *= re.x, u[1] *= re.y, u[2] *= re.x, u[3] *= re.y;
+            }
+            split_left<3>(x, e[2 * ks], e[2 * ks + 1]);
+#pragma unroll
+            for (int p = 0; p < W / 2; ++p) {
+                if (p * 16 >= a.Dk) break;
+#pragma unroll
+                for (int m = 0; m < NT; ++m) {
+                    uint32_t f[4];
+                    right_columns(f, sk + m * TILE, W, 2 * ks, 2 * p);
+#pragma unroll
+                    for (int i = 0; i + m < 3; ++i) {
+                        multiply(S[2 * p], x[i], f[0], f[1]);
+                        multiply(S[2 * p + 1], x[i], f[2], f[3]);
+                    }
+                }
+            }
+        }
+        __syncthreads();
+        if (threadIdx.x == 0 && ok && n + stages < chunks)
+            load_stage<NT>(a, st, base + at * st.bytes, bar + 8 * at, tiles_of(a, kept, kept + a.p.v, a.p.xe, s.slot + n + stages, h), tile0, warps);
+        const int left = s.length - n * C;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int col = tile * 16 + g + (j >> 1) * 8, tok = i * 8 + 2 * t + (j & 1);
+                if (col < a.Dv && tok < left)
+                    put(o + ((s.row + (int64_t)(n * C + tok) * s.step) * a.Hv + h) * a.Dv + col, a.scale * out[i][j]);
+            }
+    }
+    if (!ok) let_land();
+    if (last) write_state<W>(S, last + state, tile * 16, a.Dk, a.Dv);
+}
+
+template <typename T, int DKP>
+__global__ void __launch_bounds__(kWarps * 32, 1) delta_backward_kernel(const __grid_constant__ Args a, const uint8_t *kept, uint8_t *scratch,
+                                                                        const float *glast, float *gs0, int stages) {
+    constexpr int NT = sizeof(T) == 2 ? 1 : 3, NS = sizeof(T) == 2 ? 2 : 3, W = DKP / 8, TILE = 64 * DKP * 2, SQ = kSquare / 3;
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ __align__(8) uint64_t bars[2];
+    pdl_begin();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, t = lane % 4;
+    const int b = blockIdx.x / a.Hv, h = blockIdx.x % a.Hv, tile0 = blockIdx.y * warps, tile = tile0 + warp;
+    const Sequence s = sequence(a, b);
+    const int chunks = (s.length + C - 1) / C;
+    const Stage st = stage_of(a.p, warps);
+    const uint32_t base = tc::smem_addr(smem), bar = tc::smem_addr(bars);
+    if (threadIdx.x == 0) {
+        tc::bar_init(bar, 1);
+        tc::bar_init(bar + 8, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        for (int n = 0; n < min(stages, chunks); ++n)
+            load_stage<NT>(a, st, base + n * st.bytes, bar + 8 * n, tiles_of(a, kept, scratch + a.p.go, a.p.xu, s.slot + chunks - 1 - n, h), tile0, warps);
+    }
+    const int64_t state = ((int64_t)b * a.Hv + h) * a.Dk * a.Dv;
+    float D[W][4];
+    read_state<W>(D, glast ? glast + state : nullptr, tile * 16, a.Dk, a.Dv);
+    __syncthreads();
+    bool ok = true;
+    for (int n = 0; n < chunks; ++n) {
+        const int at = n % stages;
+        const int64_t hv = (s.slot + chunks - 1 - n) * a.Hv + h;
+        keep_blocks<NS, W>(scratch + a.p.d + hv * a.p.state_bytes, (size_t)a.p.DVP * DKP * 2, tile, D);
+        ok = ok && tc::bar_wait(bar + 8 * at, n / stages & 1);
+        if (!ok)
+#pragma unroll
+            for (int i = 0; i < W; ++i) D[i][0] = D[i][1] = D[i][2] = D[i][3] = __int_as_float(0x7fffffff);
+        const uint8_t *here = smem + at * st.bytes, *gob = here + st.v;
+        const uint32_t sk = base + at * st.bytes + st.k, sq = sk + st.q, sx = sk + st.x, sp = sk + st.p;
+        const float *gates = reinterpret_cast<const float *>(here + st.gates);
+        float d[8][4] = {}, r[8][4] = {};
+        // P^T go
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+            uint32_t x[NT][4];
+#pragma unroll
+            for (int m = 0; m < NT; ++m)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    x[m][i] = *reinterpret_cast<const uint32_t *>(gob + m * warps * 2048 + ((warp * 2 + (i & 1)) * 8 + 2 * ks + (i >> 1)) * kCell + lane * 4);
+#pragma unroll
+            for (int p = 0; p <= ks; ++p)
+#pragma unroll
+                for (int m = 0; m < 3; ++m) {
+                    uint32_t f[4];
+                    right_columns(f, sp + m * SQ, 8, 2 * ks, 2 * p);
+#pragma unroll
+                    for (int i = 0; i < NT && i + m < 3; ++i) {
+                        multiply(d[2 * p], x[i], f[0], f[1]);
+                        multiply(d[2 * p + 1], x[i], f[2], f[3]);
+                    }
+                }
+        }
+        // k D
+#pragma unroll
+        for (int ks = 0; ks < W / 2; ++ks) {
+            if (ks * 16 >= a.Dk) break;
+            uint32_t x[3][4];
+            split_left<3>(x, D[2 * ks], D[2 * ks + 1]);
+#pragma unroll
+            for (int p = 0; p < 4; ++p)
+#pragma unroll
+                for (int m = 0; m < NT; ++m) {
+                    uint32_t f[4];
+                    right_rows(f, sk + m * TILE, W, 2 * p, 2 * ks);
+#pragma unroll
+                    for (int i = 0; i + m < 3; ++i) {
+                        multiply(r[2 * p], x[i], f[0], f[1]);
+                        multiply(r[2 * p + 1], x[i], f[2], f[3]);
+                    }
+                }
+        }
+        const float keep = gates[kKeep];
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) D[i][e] *= keep;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float2 re = *reinterpret_cast<const float2 *>(gates + kRest + i * 8 + 2 * t);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) d[i][e] = fmaf(e & 1 ? re.y : re.x, r[i][e], a.scale * d[i][e]);
+        }
+        float y[8][4] = {};
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+            uint32_t x[3][4];
+            split_left<3>(x, d[2 * ks], d[2 * ks + 1]);
+#pragma unroll
+            for (int p = 0; p <= ks; ++p)
+#pragma unroll
+                for (int m = 0; m < 3; ++m) {
+                    uint32_t f[4];
+                    right_columns(f, sx + m * SQ, 8, 2 * ks, 2 * p);
+#pragma unroll
+                    for (int i = 0; i + m < 3; ++i) {
+                        multiply(y[2 * p], x[i], f[0], f[1]);
+                        multiply(y[2 * p + 1], x[i], f[2], f[3]);
+                    }
+                }
+        }
+        keep_blocks<3, 8>(scratch + a.p.y + hv * a.p.kept_bytes, (size_t)a.p.DVP * C * 2, tile, y);
+        // q^T (scale first go) - k^T (first b y)
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+            uint32_t x[3][4], z[3][4];
+            float go[2][4];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float2 fi = *reinterpret_cast<const float2 *>(gates + kFirst + (2 * ks + i) * 8 + 2 * t);
+                const float2 bt = *reinterpret_cast<const float2 *>(gates + kBeta + (2 * ks + i) * 8 + 2 * t);
+                float(&w)[4] = y[2 * ks + i];
+                w[0] *= -fi.x * bt.x, w[1] *= -fi.y * bt.y, w[2] *= -fi.x * bt.x, w[3] *= -fi.y * bt.y;
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const float2 v = pair_of<NT>(gob, warps * 2048, (warp * 2 + half) * 8 + 2 * ks + i);
+                    go[i][2 * half] = a.scale * fi.x * v.x, go[i][2 * half + 1] = a.scale * fi.y * v.y;
+                }
+            }
+            split_left<3>(x, go[0], go[1]);
+            split_left<3>(z, y[2 * ks], y[2 * ks + 1]);
+#pragma unroll
+            for (int p = 0; p < W / 2; ++p) {
+                if (p * 16 >= a.Dk) break;
+#pragma unroll
+                for (int m = 0; m < NT; ++m) {
+                    uint32_t f[4], f2[4];
+                    right_columns(f, sq + m * TILE, W, 2 * ks, 2 * p);
+                    right_columns(f2, sk + m * TILE, W, 2 * ks, 2 * p);
+#pragma unroll
+                    for (int i = 0; i + m < 3; ++i) {
+                        multiply(D[2 * p], x[i], f[0], f[1]);
+                        multiply(D[2 * p + 1], x[i], f[2], f[3]);
+                        multiply(D[2 * p], z[i], f2[0], f2[1]);
+                        multiply(D[2 * p + 1], z[i], f2[2], f2[3]);
+                    }
+                }
+            }
+        }
+        __syncthreads();
+        if (threadIdx.x == 0 && ok && n + stages < chunks)
+            load_stage<NT>(a, st, base + at * st.bytes, bar + 8 * at, tiles_of(a, kept, scratch + a.p.go, a.p.xu, s.slot + chunks - 1 - n - stages, h), tile0, warps);
+    }
+    if (!ok) let_land();
+    if (gs0) write_state<W>(D, gs0 + state, tile * 16, a.Dk, a.Dv);
+}
+
+// ------------------------------------------------------------------ gradients of q, k and the gates
+// Columns of v that a round takes, and the places of their tiles in a stage.
+constexpr int kRound = 32;
+template <int NT, int NS, int DKP>
+struct Parts {
+    static constexpr uint32_t state = kRound * DKP * 2, values = kRound * C * 2;      // bytes of a term
+    static constexpr uint32_t s = 0, d = s + NS * state, go = d + NS * state, v = go + NT * values, y = v + NT * values,
+                              e = y + 3 * values, bytes = e + 3 * values;
+    static constexpr uint32_t keys = NT * C * DKP * 2;
+    // k and q: behind the stages, or (three terms) in the second one when the rounds are over
+    static constexpr uint32_t key_at = NT == 1 ? 2 * bytes : bytes, end = NT == 1 ? 2 * bytes + 2 * keys : 2 * bytes;
+};
+
+// A block for a chunk and value head: all products over v in rounds of 32 columns, then those within the
+// chunk. Eight warps: 16 tokens each, one half of Dk (and of the square matrices' columns). Gradients of
+// shared heads go out in float32 for each value head and are added up by delta_join_kernel.
+template <typename T, int DKP>
+__global__ void __launch_bounds__(kWarps * 32, 1) delta_gradients_kernel(const __grid_constant__ Args a, const uint8_t *kept, uint8_t *scratch,
+                                                                         T *gq, T *gk, T *gv, float *ggate, float *gbeta) {
+    constexpr int NT = sizeof(T) == 2 ? 1 : 3, NS = sizeof(T) == 2 ? 2 : 3, W = DKP / 8, TILE = 64 * DKP * 2, SQ = kSquare / 3;
+    constexpr int N8 = DKP / 16, FEW = sizeof(T) == 2 ? 2 : 3;       // blocks of a warp; terms where a bfloat16 comes of it
+    using P = Parts<NT, NS, DKP>;
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ __align__(8) uint64_t bars[3];
+    __shared__ __align__(16) float gates[kGateFloats];
+    __shared__ float qdot[2][C], edot[C], vdot[C], sums[kWarps];
+    pdl_begin();
+    int b, chunk;
+    Sequence s;
+    if (!locate(a, blockIdx.x, &b, &chunk, &s)) return;
+    const int h = blockIdx.y, group = a.Hv / a.Hk, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane / 4, t = lane % 4;
+    const int wr = warp & 3, wh = warp >> 2;
+    const int64_t hv = (int64_t)blockIdx.x * a.Hv + h, hk = (int64_t)blockIdx.x * a.Hk + h / group;
+    const uint32_t base = tc::smem_addr(smem), bar = tc::smem_addr(bars);
+    const int rounds = (a.p.DVP + kRound - 1) / kRound;
+    const uint8_t *kimage = kept + a.p.k + hk * a.p.key_bytes, *qimage = kept + a.p.q + hk * a.p.key_bytes;
+    auto load = [&](int n) {
+        const uint32_t to = base + (n & 1) * P::bytes, on = bar + 8 * (n & 1);
+        const int v0 = n * kRound, count = min(kRound, a.p.DVP - v0);
+        const size_t sterm = (size_t)a.p.DVP * DKP * 2, vterm = (size_t)a.p.DVP * C * 2;
+        const uint32_t sb = count * DKP * 2, vb = count * C * 2;
+        tc::bar_expect(on, 2 * NS * sb + (2 * NT + 6) * vb);
+        for (int m = 0; m < NS; ++m) {
+            load_bytes(to + P::s + m * P::state, kept + a.p.s + hv * a.p.state_bytes + m * sterm + (size_t)v0 * DKP * 2, sb, on);
+            load_bytes(to + P::d + m * P::state, scratch + a.p.d + hv * a.p.state_bytes + m * sterm + (size_t)v0 * DKP * 2, sb, on);
+        }
+        for (int m = 0; m < NT; ++m) {
+            load_bytes(to + P::go + m * P::values, scratch + a.p.go + hv * a.p.value_bytes + m * vterm + (size_t)v0 * C * 2, vb, on);
+            load_bytes(to + P::v + m * P::values, kept + a.p.v + hv * a.p.value_bytes + m * vterm + (size_t)v0 * C * 2, vb, on);
+        }
+        for (int m = 0; m < 3; ++m) {
+            load_bytes(to + P::y + m * P::values, scratch + a.p.y + hv * a.p.kept_bytes + m * vterm + (size_t)v0 * C * 2, vb, on);
+            load_bytes(to + P::e + m * P::values, kept + a.p.e + hv * a.p.kept_bytes + m * vterm + (size_t)v0 * C * 2, vb, on);
+        }
+    };
+    auto load_keys = [&] {
+        tc::bar_expect(bar + 16, 2 * P::keys);
+        load_bytes(base + P::key_at, kimage, P::keys, bar + 16);
+        load_bytes(base + P::key_at + P::keys, qimage, P::keys, bar + 16);
+    };
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 3; ++i) tc::bar_init(bar + 8 * i, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        for (int n = 0; n < min(2, rounds); ++n) load(n);
+        if (NT == 1) load_keys();
+    }
+    const float *gin = reinterpret_cast<const float *>(kept + a.p.gates) + hv * kGateFloats;
+    for (int i = threadIdx.x; i < kGateFloats; i += kWarps * 32) gates[i] = gin[i];
+    __syncthreads();
+    const int left = min(C, s.length - chunk * C);
+    const int64_t row = s.row + (int64_t)chunk * C * s.step;
+    const float2 mybeta = *reinterpret_cast<const float2 *>(gates + kBeta + warp * 8 + 2 * t);
+
+    float goS[N8][4] = {}, yS[N8][4] = {}, eD[N8][4] = {}, A[4][4] = {}, E[4][4] = {};
+    float ey[2] = {}, vy[2] = {}, ds = 0.f;
+    bool ok = true;
+    for (int n = 0; n < rounds; ++n) {
+        const uint32_t here = base + (n & 1) * P::bytes;
+        const uint8_t *mem = smem + (n & 1) * P::bytes;
+        const int count = min(kRound, a.p.DVP - n * kRound);
+        ok = ok && tc::bar_wait(bar + 8 * (n & 1), n / 2 & 1);
+        for (int ks = 0; ks < count / 16; ++ks) {
+            uint32_t ago[NT][4], ay[3][4], ae[3][4];
+#pragma unroll
+            for (int m = 0; m < NT; ++m) left_columns(ago[m], here + P::go + m * P::values, 8, 2 * ks, 2 * wr);
+#pragma unroll
+            for (int m = 0; m < FEW; ++m) {
+                left_columns(ay[m], here + P::y + m * P::values, 8, 2 * ks, 2 * wr);
+                left_columns(ae[m], here + P::e + m * P::values, 8, 2 * ks, 2 * wr);
+            }
+#pragma unroll
+            for (int p = 0; p < N8 / 2; ++p) {
+                if ((wh * N8 + 2 * p) * 8 >= a.Dk) break;
+#pragma unroll
+                for (int m = 0; m < NS; ++m) {
+                    uint32_t f[4];
+                    right_columns(f, here + P::s + m * P::state, W, 2 * ks, wh * N8 + 2 * p);
+#pragma unroll
+                    for (int i = 0; i < NT && i + m < NS; ++i) {
+                        multiply(goS[2 * p], ago[i], f[0], f[1]);
+                        multiply(goS[2 * p + 1], ago[i], f[2], f[3]);
+                    }
+#pragma unroll
+                    for (int i = 0; i + m < FEW; ++i) {
+                        multiply(yS[2 * p], ay[i], f[0], f[1]);
+                        multiply(yS[2 * p + 1], ay[i], f[2], f[3]);
+                    }
+                    right_columns(f, here + P::d + m * P::state, W, 2 * ks, wh * N8 + 2 * p);
+#pragma unroll
+                    for (int i = 0; i + m < FEW; ++i) {
+                        multiply(eD[2 * p], ae[i], f[0], f[1]);
+                        multiply(eD[2 * p + 1], ae[i], f[2], f[3]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                if (2 * wh + p > wr) break;
+#pragma unroll
+                for (int m = 0; m < 3; ++m) {
+                    uint32_t f[4];
+                    right_columns(f, here + P::e + m * P::values, 8, 2 * ks, 4 * wh + 2 * p);
+#pragma unroll
+                    for (int i = 0; i < NT && i + m < 3; ++i) {
+                        multiply(A[2 * p], ago[i], f[0], f[1]);
+                        multiply(A[2 * p + 1], ago[i], f[2], f[3]);
+                    }
+#pragma unroll
+                    for (int i = 0; i + m < FEW; ++i) {
+                        multiply(E[2 * p], ay[i], f[0], f[1]);
+                        multiply(E[2 * p + 1], ay[i], f[2], f[3]);
+                    }
+                }
+            }
+        }
+        // e . y, v . y and the gradient of v: tokens warp * 8 + 2 t and the next
+        for (int c = 0; c < count / 8; ++c) {
+            const float2 y = pair_of<3>(mem + P::y, P::values, c * 8 + warp), e = pair_of<3>(mem + P::e, P::values, c * 8 + warp);
+            const float2 v = pair_of<NT>(mem + P::v, P::values, c * 8 + warp);
+            ey[0] = fmaf(e.x, y.x, ey[0]), ey[1] = fmaf(e.y, y.y, ey[1]);
+            vy[0] = fmaf(v.x, y.x, vy[0]), vy[1] = fmaf(v.y, y.y, vy[1]);
+            const int col = n * kRound + c * 8 + g, tok = warp * 8 + 2 * t;
+            if (col < a.Dv && tok < left) put(gv + ((row + tok * s.step) * a.Hv + h) * a.Dv + col, mybeta.x * y.x);
+            if (col < a.Dv && tok + 1 < left) put(gv + ((row + (tok + 1) * s.step) * a.Hv + h) * a.Dv + col, mybeta.y * y.y);
+        }
+        for (int c = warp; c < count / 8 * W; c += kWarps) {
+            const float2 x = pair_of<NS>(mem + P::s, P::state, c), y = pair_of<NS>(mem + P::d, P::state, c);
+            ds = fmaf(x.x, y.x, fmaf(x.y, y.y, ds));
+        }
+        __syncthreads();
+        if (threadIdx.x == 0 && ok && n + 2 < rounds) load(n + 2);
+    }
+    if (NT > 1 && threadIdx.x == 0 && ok) load_keys();
+#pragma unroll
+    for (int o = 4; o < 32; o <<= 1)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            ey[i] += __shfl_xor_sync(0xffffffffu, ey[i], o);
+            vy[i] += __shfl_xor_sync(0xffffffffu, vy[i], o);
+        }
+    if (g == 0) {
+        edot[warp * 8 + 2 * t] = ey[0], edot[warp * 8 + 2 * t + 1] = ey[1];
+        vdot[warp * 8 + 2 * t] = mybeta.x * vy[0], vdot[warp * 8 + 2 * t + 1] = mybeta.y * vy[1];
+    }
+    // the square matrices, as terms, where the first stage was
+    const uint32_t At = base, Ct = base + kSquare;
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int i = wr * 16 + half * 8 + g, j = wh * 32 + n * 8 + 2 * t;
+            float x[2], c[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float w = j + e <= i ? between(gates, i, j + e) * gates[kBeta + j + e] : 0.f;
+                x[e] = j + e <= i ? a.scale * w * A[n][2 * half + e] : 0.f;
+                c[e] = j + e < i ? -gates[kBeta + i] * w * E[n][2 * half + e] : 0.f;
+            }
+            uint32_t xs[3], cs[3];
+            split<3>(xs, x[0], x[1]);
+            split<3>(cs, c[0], c[1]);
+            uint8_t *to = smem + ((wr * 2 + half) * 8 + wh * 4 + n) * kCell + lane * 4;
+#pragma unroll
+            for (int m = 0; m < 3; ++m) {
+                *reinterpret_cast<uint32_t *>(to + m * SQ) = xs[m];
+                *reinterpret_cast<uint32_t *>(to + kSquare + m * SQ) = cs[m];
+            }
+        }
+    __syncthreads();
+    ok = ok && tc::bar_wait(bar + 16, 0);
+    const uint8_t *km = smem + P::key_at, *qm = km + P::keys;
+    const uint32_t kt = base + P::key_at, qt = kt + P::keys;
+    float kd = 0.f;
+#pragma unroll
+    for (int n = 0; n < N8; ++n)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int i = wr * 16 + half * 8 + g;
+            const float f = gates[kFirst + i], bt = gates[kBeta + i], re = gates[kRest + i];
+            const float2 k = pair_of<NT>(km, TILE, (wr * 2 + half) * W + wh * N8 + n);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float &x = goS[n][2 * half + e], &y = yS[n][2 * half + e];
+                const float d = re * bt * eD[n][2 * half + e];
+                kd = fmaf(e ? k.y : k.x, d, kd);
+                x *= a.scale * f;
+                y = fmaf(-f * bt, y, d);
+            }
+        }
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+        uint32_t la[3][4], lc[3][4];
+        if (ks <= wr) {        // A k and C k
+#pragma unroll
+            for (int m = 0; m < 3; ++m) left_rows(la[m], At + m * SQ, 8, 2 * wr, 2 * ks);
+#pragma unroll
+            for (int m = 0; m < FEW; ++m) left_rows(lc[m], Ct + m * SQ, 8, 2 * wr, 2 * ks);
+#pragma unroll
+            for (int p = 0; p < N8 / 2; ++p) {
+                if ((wh * N8 + 2 * p) * 8 >= a.Dk) break;
+#pragma unroll
+                for (int m = 0; m < NT; ++m) {
+                    uint32_t f[4];
+                    right_columns(f, kt + m * TILE, W, 2 * ks, wh * N8 + 2 * p);
+#pragma unroll
+                    for (int i = 0; i + m < 3; ++i) {
+                        multiply(goS[2 * p], la[i], f[0], f[1]);
+                        multiply(goS[2 * p + 1], la[i], f[2], f[3]);
+                    }
+#pragma unroll
+                    for (int i = 0; i + m < FEW; ++i) {
+                        multiply(yS[2 * p], lc[i], f[0], f[1]);
+                        multiply(yS[2 * p + 1], lc[i], f[2], f[3]);
+                    }
+                }
+            }
+        }
+        if (ks >= wr) {        // A^T q and C^T k
+#pragma unroll
+            for (int m = 0; m < FEW; ++m) {
+                left_columns(la[m], At + m * SQ, 8, 2 * ks, 2 * wr);
+                left_columns(lc[m], Ct + m * SQ, 8, 2 * ks, 2 * wr);
+            }
+#pragma unroll
+            for (int p = 0; p < N8 / 2; ++p) {
+                if ((wh * N8 + 2 * p) * 8 >= a.Dk) break;
+#pragma unroll
+                for (int m = 0; m < NT; ++m) {
+                    uint32_t f[4], f2[4];
+                    right_columns(f, qt + m * TILE, W, 2 * ks, wh * N8 + 2 * p);
+                    right_columns(f2, kt + m * TILE, W, 2 * ks, wh * N8 + 2 * p);
+#pragma unroll
+                    for (int i = 0; i + m < FEW; ++i) {
+                        multiply(yS[2 * p], la[i], f[0], f[1]);
+                        multiply(yS[2 * p + 1], la[i], f[2], f[3]);
+                        multiply(yS[2 * p], lc[i], f2[0], f2[1]);
+                        multiply(yS[2 * p + 1], lc[i], f2[2], f2[3]);
+                    }
+                }
+            }
+        }
+    }
+    if (!ok)
+#pragma unroll
+        for (int n = 0; n < N8; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) goS[n][e] = yS[n][e] = kd = __int_as_float(0x7fffffff);
+    float *parts = reinterpret_cast<float *>(scratch + a.p.parts);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        const int i = wr * 16 + half * 8 + g;
+        const int64_t tok = row + i * s.step;
+        float dot = 0.f;
+#pragma unroll
+        for (int n = 0; n < N8; ++n) {
+            const float2 q = pair_of<NT>(qm, TILE, (wr * 2 + half) * W + wh * N8 + n);
+            dot = fmaf(q.x, goS[n][2 * half], fmaf(q.y, goS[n][2 * half + 1], dot));
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int d = (wh * N8 + n) * 8 + 2 * t + e;
+                if (i >= left || d >= a.Dk) continue;
+                if (group == 1) {
+                    put(gq + (tok * a.Hk + h) * a.Dk + d, goS[n][2 * half + e]);
+                    put(gk + (tok * a.Hk + h) * a.Dk + d, yS[n][2 * half + e]);
+                } else {
+                    parts[(tok * a.Hv + h) * a.Dk + d] = goS[n][2 * half + e];
+                    parts[((a.p.tokens + tok) * a.Hv + h) * a.Dk + d] = yS[n][2 * half + e];
+                }
+            }
+        }
+        dot += __shfl_xor_sync(0xffffffffu, dot, 1);
+        dot += __shfl_xor_sync(0xffffffffu, dot, 2);
+        if (t == 0) qdot[wh][i] = dot;
+    }
+    kd = fmaf(gates[kKeep], ds, kd);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) kd += __shfl_xor_sync(0xffffffffu, kd, o);
+    if (lane == 0) sums[warp] = kd;
+    __syncthreads();
+    if (!ok) let_land();
+    if (warp) return;
+    // the gates: sums from each token to the chunk's end, and what comes back through the state
+    double tail = 0.0, mine[2];
+    for (int i = 0; i < kWarps; ++i) tail += (double)sums[i];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const int i = 2 * lane + e;
+        mine[e] = (double)qdot[0][i] + (double)qdot[1][i] - (double)vdot[i];
+    }
+    double behind = mine[0] + mine[1];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const double down = __shfl_down_sync(0xffffffffu, behind, o);
+        if (lane + o < 32) behind += down;
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const int i = 2 * lane + e;
+        if (i >= left) continue;
+        const int64_t at = (row + i * s.step) * a.Hv + h;
+        ggate[at] = (float)(tail + behind - (e ? mine[0] : 0.0));
+        gbeta[at] = edot[i];
+    }
+}
+
+// Gradients of a key head: those of its value heads added up in order. blockIdx.y: of q, of k.
+template <typename T>
+__global__ void __launch_bounds__(256) delta_join_kernel(const __grid_constant__ Args a, const float *parts, T *gq, T *gk) {
+    pdl_begin();
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / (a.Hk * a.Dk);
+    if (row >= a.p.tokens) return;
+    if (a.layout == DENDSN_DELTA_PACKED && (row < a.offsets[0] || row >= a.offsets[a.B])) return;
+    const int h = (int)(i % (a.Hk * a.Dk)) / a.Dk, d = (int)(i % a.Dk), group = a.Hv / a.Hk;
+    const float *from = parts + ((blockIdx.y * a.p.tokens + row) * a.Hv + (int64_t)h * group) * a.Dk + d;
+    float v = 0.f;
+    for (int j = 0; j < group; ++j) v += from[(int64_t)j * a.Dk];
+    put((blockIdx.y ? gk : gq) + i, v);
+}
+
+// Rows of no sequence, as zeros.
+struct Rest {
+    uint8_t *to[5];
+    int64_t bytes[5];          // of a row
+};
+__global__ void __launch_bounds__(256) delta_rest_kernel(const __grid_constant__ Args a, const __grid_constant__ Rest r) {
+    pdl_begin();
+    const int64_t lo = min(max(a.offsets[0], 0), a.T), hi = min(max(a.offsets[a.B], 0), a.T), step = (int64_t)gridDim.x * 256;
+    for (int n = 0; n < 5; ++n) {
+        if (!r.to[n]) continue;
+        for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < lo * r.bytes[n] / 2; i += step) reinterpret_cast<uint16_t *>(r.to[n])[i] = 0;
+        for (int64_t i = hi * r.bytes[n] / 2 + (int64_t)blockIdx.x * 256 + threadIdx.x; i < a.T * r.bytes[n] / 2; i += step)
+            reinterpret_cast<uint16_t *>(r.to[n])[i] = 0;
+    }
+}
+
+// ------------------------------------------------------------------ few tokens
+// A token at a time, as the formulas are written: a block has one head's state in registers, `lanes`
+// threads a row of VEC columns each. Bound by the state's read and write for one token; a step of a few
+// tokens costs two sums over the block each.
+template <typename T, int VEC>
+__global__ void __launch_bounds__(256) delta_step_kernel(const __grid_constant__ Args a, const T *q, const T *k, const T *v, const float *gate,
+                                                         const float *beta, const float *s0, T *o, float *last, int lanes) {
+    constexpr int ROWS = VEC == 4 ? 16 : 64;
+    __shared__ float ks[kDeltaMost], qs[kDeltaMost], part[2][8][kDeltaMost], us[kDeltaMost];
+    pdl_begin();
+    const int b = blockIdx.x / a.Hv, h = blockIdx.x % a.Hv, hk = h / (a.Hv / a.Hk), tid = threadIdx.x;
+    const int rows = 256 / lanes, r0 = tid / lanes, col = tid % lanes * VEC, parts = min(8, rows), mine = lanes >= 32 ? r0 : tid / 32;
+    const Sequence s = sequence(a, b);
+    const int64_t state = ((int64_t)b * a.Hv + h) * a.Dk * a.Dv;
+    float S[ROWS][VEC];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        const int r = r0 + i * rows;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) S[i][e] = 0.f;
+        if (s0 && r < a.Dk && col < a.Dv) {
+            const float *from = s0 + state + (int64_t)r * a.Dv + col;
+            if constexpr (VEC == 4) {
+                const float4 x = *reinterpret_cast<const float4 *>(from);
+                S[i][0] = x.x, S[i][1] = x.y, S[i][2] = x.z, S[i][3] = x.w;
+            } else {
+                S[i][0] = *from;
+            }
+        }
+    }
+    // sums over the rows of every column: within a warp, then over the warps' (or rows') parts
+    auto gather = [&](float (&x)[VEC], float (*to)[kDeltaMost]) {
+        for (int w = lanes; w < 32; w <<= 1)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) x[e] += __shfl_xor_sync(0xffffffffu, x[e], w);
+        if (col < a.Dv && (lanes >= 32 || (tid & 31) < lanes))
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) to[mine][col + e] = x[e];
+    };
+    for (int n = 0; n < s.length; ++n) {
+        const int64_t tok = s.row + n * s.step;
+        __syncthreads();
+        for (int i = tid; i < a.Dk; i += 256) {
+            ks[i] = value(k + (tok * a.Hk + hk) * a.Dk + i);
+            qs[i] = value(q + (tok * a.Hk + hk) * a.Dk + i);
+        }
+        const float g = gate[tok * a.Hv + h], decay = expf(g), bt = beta[tok * a.Hv + h];
+        const float vt = tid < a.Dv ? value(v + (tok * a.Hv + h) * a.Dv + tid) : 0.f;
+        __syncthreads();
+        float x[VEC] = {};
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            const int r = r0 + i * rows;
+            const float kr = r < a.Dk ? ks[r] : 0.f;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                S[i][e] *= decay;
+                x[e] = fmaf(kr, S[i][e], x[e]);
+            }
+        }
+        gather(x, part[0]);
+        __syncthreads();
+        if (tid < a.Dv) {
+            float read = 0.f;
+            for (int i = 0; i < parts; ++i) read += part[0][i][tid];
+            us[tid] = bt * (vt - read);
+        }
+        __syncthreads();
+        float u[VEC], z[VEC] = {};
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) u[e] = col + e < a.Dv ? us[col + e] : 0.f;
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            const int r = r0 + i * rows;
+            const float kr = r < a.Dk ? ks[r] : 0.f, qr = r < a.Dk ? qs[r] : 0.f;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                S[i][e] = fmaf(kr, u[e], S[i][e]);
+                z[e] = fmaf(qr, S[i][e], z[e]);
+            }
+        }
+        gather(z, part[1]);
+        __syncthreads();
+        if (tid < a.Dv) {
+            float out = 0.f;
+            for (int i = 0; i < parts; ++i) out += part[1][i][tid];
+            put(o + (tok * a.Hv + h) * a.Dv + tid, a.scale * out);
+        }
+    }
+    if (!last) return;
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        const int r = r0 + i * rows;
+        if (r >= a.Dk || col >= a.Dv) continue;
+        float *to = last + state + (int64_t)r * a.Dv + col;
+        if constexpr (VEC == 4) *reinterpret_cast<float4 *>(to) = make_float4(S[i][0], S[i][1], S[i][2], S[i][3]);
+        else *to = S[i][0];
+    }
+}
+
+// ------------------------------------------------------------------ host
+dendsn_status check(const dendsn_delta_config *c) {
+    if (!c) return seq_fail(DENDSN_ERR_INVALID_ARG, "cfg is NULL");
+    if (c->T < 0 || c->B < 0 || c->Hk < 1 || c->Hv < 1 || c->Dk < 1 || c->Dv < 1)
+        return seq_fail(DENDSN_ERR_INVALID_ARG, "T and B must be >= 0, Hk, Hv, Dk and Dv >= 1");
+    if (c->Hv % c->Hk) return seq_fail(DENDSN_ERR_INVALID_ARG, "Hv must be a multiple of Hk");
+    if (c->x_dtype != DENDSN_F32 && c->x_dtype != DENDSN_BF16) return seq_fail(DENDSN_ERR_INVALID_ARG, "unknown x_dtype");
+    if (c->layout < DENDSN_DELTA_TIME || c->layout > DENDSN_DELTA_PACKED) return seq_fail(DENDSN_ERR_INVALID_ARG, "unknown layout");
+    if (c->rest != DENDSN_REST_KEEP && c->rest != DENDSN_REST_ZERO) return seq_fail(DENDSN_ERR_INVALID_ARG, "unknown rest");
+    if (!std::isfinite(c->scale)) return seq_fail(DENDSN_ERR_INVALID_ARG, "scale must be finite");
+    if (c->Dk > kDeltaMost || c->Dv > kDeltaMost) return seq_fail(DENDSN_ERR_UNSUPPORTED, "Dk or Dv above %d", kDeltaMost);
+    if (c->Hv > 65535) return seq_fail(DENDSN_ERR_UNSUPPORTED, "more than 65535 value heads");
+    const int64_t most = INT32_MAX, slots = c->layout == DENDSN_DELTA_PACKED ? (int64_t)c->T / C + c->B : (int64_t)c->B * ((c->T + (int64_t)C - 1) / C);
+    if (slots > most || (int64_t)c->B * c->Hv > most) return seq_fail(DENDSN_ERR_UNSUPPORTED, "more than 2^31 chunks or states");
+    return DENDSN_OK;
+}
+
+Args args_of(const dendsn_delta_config &c, const int32_t *offsets) {
+    return {c.T, c.B, c.Hk, c.Hv, c.Dk, c.Dv, c.layout, c.scale, offsets, delta_plan(c, DENDSN_DELTA_PACKED, c.x_dtype == DENDSN_BF16)};
+}
+
+template <typename K>
+cudaError_t room(K kernel, size_t smem) {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+}
+
+// Tokens of a call that the step kernel takes one by one: a token's step is about 1.5 us, a chunk's way
+// through the chunked kernels 15 us.
+constexpr int kFewTokens = 8;
+bool by_steps(const dendsn_delta_config &c, const void *kept) {
+    if (kept) return false;
+    return c.T <= kFewTokens;
+}
+
+template <typename T>
+cudaError_t run_step(const Args &a, const void *q, const void *k, const void *v, const float *gate, const float *beta, const float *s0, void *o,
+                     float *last, cudaStream_t s) {
+    const bool four = a.Dv % 4 == 0 && seq_aligned(s0, 16) && seq_aligned(last, 16);
+    int lanes = 1;
+    while (lanes * (four ? 4 : 1) < a.Dv) lanes *= 2;
+    const dim3 grid((unsigned)(a.B * a.Hv));
+    return four ? seq_launch(delta_step_kernel<T, 4>, grid, 256, 0, s, 1, a, (const T *)q, (const T *)k, (const T *)v, gate, beta, s0, (T *)o, last, lanes)
+                : seq_launch(delta_step_kernel<T, 1>, grid, 256, 0, s, 1, a, (const T *)q, (const T *)k, (const T *)v, gate, beta, s0, (T *)o, last, lanes);
+}
+
+template <typename T>
+bool wide_of(const void *p, int D) { return seq_aligned(p, 16) && D % (16 / (int)sizeof(T)) == 0; }
+
+// Warps of a block that carries states, and how many chunks' tiles fit its shared memory.
+struct Walk {
+    int warps, blocks, stages;
+    size_t smem;
+};
+Walk walk_of(const Args &a) {
+    Walk w;
+    w.warps = a.p.DVP / 16;
+    w.blocks = 1;
+    const size_t stage = stage_of(a.p, w.warps).bytes;
+    w.stages = 2 * stage <= 225 * 1024 ? 2 : 1;
+    w.smem = w.stages * stage;
+    return w;
+}
+
+template <typename T, int DKP>
+cudaError_t run_forward(const Args &a, const void *q, const void *k, const void *v, const float *gate, const float *beta, const float *s0, void *o,
+                        float *last, uint8_t *kept, bool keep, cudaStream_t s, int *launches) {
+    constexpr int NT = sizeof(T) == 2 ? 1 : 3;
+    cudaError_t e = cudaSuccess;
+    if (a.p.slots) {
+        const dim3 grid((unsigned)a.p.slots, (unsigned)a.Hv);
+        const bool wide = wide_of<T>(q, a.Dk) && wide_of<T>(k, a.Dk);
+        const size_t smem = (64 * 64 + kGateFloats) * 4 + std::max<size_t>(2 * NT * 64 * DKP * 2, (keep ? 2 : 1) * 64 * 65 * 4);
+        e = keep ? room(delta_prepare_kernel<T, DKP, true>, smem) : room(delta_prepare_kernel<T, DKP, false>, smem);
+        if (e == cudaSuccess)
+            e = keep ? seq_launch(delta_prepare_kernel<T, DKP, true>, grid, 128, smem, s, 1, a, (const T *)q, (const T *)k, gate, beta, kept, wide)
+                     : seq_launch(delta_prepare_kernel<T, DKP, false>, grid, 128, smem, s, 1, a, (const T *)q, (const T *)k, gate, beta, kept, wide);
+        if (e == cudaSuccess) e = seq_launch(delta_turn_kernel<T>, grid, 256, 0, s, 1, a, (const T *)v, kept + a.p.v, wide_of<T>(v, a.Dv));
+        *launches += 2;
+    }
+    const Walk w = walk_of(a);
+    const dim3 grid((unsigned)(a.B * a.Hv), (unsigned)w.blocks);
+    if (e == cudaSuccess) e = keep ? room(delta_forward_kernel<T, DKP, true>, w.smem) : room(delta_forward_kernel<T, DKP, false>, w.smem);
+    if (e == cudaSuccess)
+        e = keep ? seq_launch(delta_forward_kernel<T, DKP, true>, grid, w.warps * 32, w.smem, s, 1, a, kept, s0, (T *)o, last, w.stages)
+                 : seq_launch(delta_forward_kernel<T, DKP, false>, grid, w.warps * 32, w.smem, s, 1, a, kept, s0, (T *)o, last, w.stages);
+    ++*launches;
+    return e;
+}
+
+template <typename T, int DKP>
+cudaError_t run_backward(const Args &a, const void *go, const float *glast, const uint8_t *kept, void *gq, void *gk, void *gv, float *ggate,
+                         float *gbeta, float *gs0, uint8_t *scratch, cudaStream_t s, int *launches) {
+    constexpr int NT = sizeof(T) == 2 ? 1 : 3, NS = sizeof(T) == 2 ? 2 : 3;
+    const dim3 chunks((unsigned)a.p.slots, (unsigned)a.Hv);
+    cudaError_t e = cudaSuccess;
+    if (a.p.slots) {
+        e = seq_launch(delta_turn_kernel<T>, chunks, 256, 0, s, 1, a, (const T *)go, scratch + a.p.go, wide_of<T>(go, a.Dv));
+        ++*launches;
+    }
+    const Walk w = walk_of(a);
+    if (e == cudaSuccess) e = room(delta_backward_kernel<T, DKP>, w.smem);
+    if (e == cudaSuccess)
+        e = seq_launch(delta_backward_kernel<T, DKP>, dim3((unsigned)(a.B * a.Hv), (unsigned)w.blocks), w.warps * 32, w.smem, s, 1, a, kept, scratch, glast, gs0, w.stages);
+    ++*launches;
+    if (!a.p.slots || e != cudaSuccess) return e;
+    constexpr size_t smem = Parts<NT, NS, DKP>::end;
+    e = room(delta_gradients_kernel<T, DKP>, smem);
+    if (e == cudaSuccess)
+        e = seq_launch(delta_gradients_kernel<T, DKP>, chunks, kWarps * 32, smem, s, 1, a, kept, scratch, (T *)gq, (T *)gk, (T *)gv, ggate, gbeta);
+    ++*launches;
+    if (a.Hv > a.Hk && e == cudaSuccess) {
+        const int64_t n = a.p.tokens * a.Hk * a.Dk;
+        e = seq_launch(delta_join_kernel<T>, dim3((unsigned)((n + 255) / 256), 2), 256, 0, s, 1, a, (const float *)(scratch + a.p.parts), (T *)gq, (T *)gk);
+        ++*launches;
+    }
+    return e;
+}
+
+cudaError_t fill_rest(const Args &a, const Rest &r, cudaStream_t s, int *launches) {
+    ++*launches;
+    return seq_launch(delta_rest_kernel, dim3(152), 256, 0, s, 1, a, r);
+}
+
+}  // namespace
+}  // namespace dendsn
+
+using namespace dendsn;
+
+extern "C" {
+
+dendsn_status dendsn_delta_workspace_size(const dendsn_delta_config *cfg, size_t *saved_bytes, size_t *forward_bytes, size_t *backward_bytes) {
+    dendsn_status st = check(cfg);
+    if (st != DENDSN_OK) return st;
+    const DeltaPlan p = delta_plan(*cfg, DENDSN_DELTA_PACKED, cfg->x_dtype == DENDSN_BF16);
+    if (saved_bytes) *saved_bytes = p.kept_end;
+    if (forward_bytes) *forward_bytes = by_steps(*cfg, nullptr) ? 0 : p.forward_end;
+    if (backward_bytes) *backward_bytes = p.backward_end;
+    return DENDSN_OK;
+}
+
+dendsn_status dendsn_delta_forward(const dendsn_delta_config *cfg, const void *q, const void *k, const void *v, const float *gate,
+                                   const float *beta, const int32_t *offsets, const float *s0, void *o, float *last, void *saved,
+                                   void *scratch, void *stream) {
+    dendsn_status st = check(cfg);
+    if (st != DENDSN_OK) return st;
+    const bool packed = cfg->layout == DENDSN_DELTA_PACKED, bf = cfg->x_dtype == DENDSN_BF16;
+    const int64_t tokens = packed ? cfg->T : (int64_t)cfg->T * cfg->B;
+    if (packed != (offsets != nullptr)) return seq_fail(DENDSN_ERR_INVALID_ARG, "offsets go with the packed layout and no other");
+    if (tokens && (!q || !k || !v || !gate || !beta || !o)) return seq_fail(DENDSN_ERR_INVALID_ARG, "q, k, v, gate, beta or o is NULL");
+    const size_t sx = bf ? 2 : 4;
+    if (!seq_aligned(q, sx) || !seq_aligned(k, sx) || !seq_aligned(v, sx) || !seq_aligned(o, sx) || !seq_aligned(gate, 4) ||
+        !seq_aligned(beta, 4) || !seq_aligned(offsets, 4) || !seq_aligned(s0, 4) || !seq_aligned(last, 4))
+        return seq_fail(DENDSN_ERR_MISALIGNED, "q, k, v, gate, beta, offsets, s0, o or last misaligned");
+    if (!seq_aligned(saved, 256) || !seq_aligned(scratch, 256)) return seq_fail(DENDSN_ERR_MISALIGNED, "saved and scratch must be 256-byte aligned");
+    const Args a = args_of(*cfg, offsets);
+    const bool steps = by_steps(*cfg, saved);
+    uint8_t *kept = static_cast<uint8_t *>(saved ? saved : scratch);
+    if (!steps && a.p.forward_end && !kept) return seq_fail(DENDSN_ERR_INVALID_ARG, "saved and scratch are both NULL");
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    int launches = 0;
+    cudaError_t e = cudaSuccess;
+    if (cfg->B) {
+        if (steps) {
+            e = bf ? run_step<__nv_bfloat16>(a, q, k, v, gate, beta, s0, o, last, s) : run_step<float>(a, q, k, v, gate, beta, s0, o, last, s);
+            ++launches;
+        } else {
+            auto go = [&](auto run) { return run(a, q, k, v, gate, beta, s0, o, last, kept, saved != nullptr, s, &launches); };
+            e = bf ? (a.p.DKP == 64 ? go(run_forward<__nv_bfloat16, 64>) : go(run_forward<__nv_bfloat16, 128>))
+                   : (a.p.DKP == 64 ? go(run_forward<float, 64>) : go(run_forward<float, 128>));
+        }
+        if (e == cudaSuccess && packed && cfg->rest == DENDSN_REST_ZERO && tokens)
+            e = fill_rest(a, {{static_cast<uint8_t *>(o)}, {(int64_t)sx * cfg->Hv * cfg->Dv}}, s, &launches);
+    }
+    if (e != cudaSuccess) return seq_fail(DENDSN_ERR_CUDA, "delta forward launch failed: %s", cudaGetErrorString(e));
+    seq_count_launches(launches);
+    return DENDSN_OK;
+}
+
+dendsn_status dendsn_delta_backward(const dendsn_delta_config *cfg, const void *grad_o, const int32_t *offsets, const float *grad_last,
+                                    const void *saved, void *grad_q, void *grad_k, void *grad_v, float *grad_gate, float *grad_beta,
+                                    float *grad_s0, void *scratch, void *stream) {
+    dendsn_status st = check(cfg);
+    if (st != DENDSN_OK) return st;
+    const bool packed = cfg->layout == DENDSN_DELTA_PACKED, bf = cfg->x_dtype == DENDSN_BF16;
+    const int64_t tokens = packed ? cfg->T : (int64_t)cfg->T * cfg->B;
+    if (packed != (offsets != nullptr)) return seq_fail(DENDSN_ERR_INVALID_ARG, "offsets go with the packed layout and no other");
+    if (tokens && (!grad_o || !grad_q || !grad_k || !grad_v || !grad_gate || !grad_beta))
+        return seq_fail(DENDSN_ERR_INVALID_ARG, "grad_o, grad_q, grad_k, grad_v, grad_gate or grad_beta is NULL");
+    const Args a = args_of(*cfg, offsets);
+    if (a.p.slots && (!saved || !scratch)) return seq_fail(DENDSN_ERR_INVALID_ARG, "saved or scratch is NULL");
+    const size_t sx = bf ? 2 : 4;
+    if (!seq_aligned(grad_o, sx) || !seq_aligned(grad_q, sx) || !seq_aligned(grad_k, sx) || !seq_aligned(grad_v, sx) || !seq_aligned(grad_gate, 4) ||
+        !seq_aligned(grad_beta, 4) || !seq_aligned(grad_s0, 4) || !seq_aligned(grad_last, 4) || !seq_aligned(offsets, 4))
+        return seq_fail(DENDSN_ERR_MISALIGNED, "a gradient or offsets misaligned");
+    if (!seq_aligned(saved, 256) || !seq_aligned(scratch, 256)) return seq_fail(DENDSN_ERR_MISALIGNED, "saved and scratch must be 256-byte aligned");
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    int launches = 0;
+    cudaError_t e = cudaSuccess;
+    if (cfg->B) {
+        auto go = [&](auto run) {
+            return run(a, grad_o, grad_last, static_cast<const uint8_t *>(saved), grad_q, grad_k, grad_v, grad_gate, grad_beta, grad_s0,
+                       static_cast<uint8_t *>(scratch), s, &launches);
+        };
+        e = bf ? (a.p.DKP == 64 ? go(run_backward<__nv_bfloat16, 64>) : go(run_backward<__nv_bfloat16, 128>))
+               : (a.p.DKP == 64 ? go(run_backward<float, 64>) : go(run_backward<float, 128>));
+        if (e == cudaSuccess && packed && cfg->rest == DENDSN_REST_ZERO && tokens) {
+            const int64_t nk = (int64_t)sx * cfg->Hk * cfg->Dk, nv = (int64_t)sx * cfg->Hv * cfg->Dv, ng = 4 * (int64_t)cfg->Hv;
+            e = fill_rest(a, {{static_cast<uint8_t *>(grad_q), static_cast<uint8_t *>(grad_k), static_cast<uint8_t *>(grad_v),
+                               reinterpret_cast<uint8_t *>(grad_gate), reinterpret_cast<uint8_t *>(grad_beta)}, {nk, nk, nv, ng, ng}}, s, &launches);
+        }
+    }
+    if (e != cudaSuccess) return seq_fail(DENDSN_ERR_CUDA, "delta backward launch failed: %s", cudaGetErrorString(e));
+    seq_count_launches(launches);
+    return DENDSN_OK;
+}
+
+}  // extern "C"
