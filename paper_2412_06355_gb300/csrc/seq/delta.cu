@@ -234,7 +234,7 @@ __global__ void __launch_bounds__(128) delta_prepare_kernel(const __grid_constan
     const uint32_t kt = tc::smem_addr(ktile), qt = tc::smem_addr(qtile);
 #pragma unroll 2
     for (int ks = 0; ks < W / 2; ++ks) {
-        uint32_t ak[NT][4], aq[NT][4], r[4];
+        uint32_t ak[NT][4], aq[NT][4], r[NT][4];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             left_rows(ak[n], kt + n * TILE, W, 2 * warp, 2 * ks);
@@ -244,16 +244,9 @@ __global__ void __launch_bounds__(128) delta_prepare_kernel(const __grid_constan
         for (int p = 0; p < 4; ++p) {
             if (p > warp) break;
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                right_rows(r, kt + n * TILE, W, 2 * p, 2 * ks);
-#pragma unroll
-                for (int m = 0; m + n < NT; ++m) {
-                    multiply(kk[2 * p], ak[m], r[0], r[1]);
-                    multiply(kk[2 * p + 1], ak[m], r[2], r[3]);
-                    multiply(qk[2 * p], aq[m], r[0], r[1]);
-                    multiply(qk[2 * p + 1], aq[m], r[2], r[3]);
-                }
-            }
+            for (int n = 0; n < NT; ++n) right_rows(r[n], kt + n * TILE, W, 2 * p, 2 * ks);
+            products<NT, NT, NT>(kk[2 * p], kk[2 * p + 1], ak, r);
+            products<NT, NT, NT>(qk[2 * p], qk[2 * p + 1], aq, r);
         }
     }
     uint32_t *pout = reinterpret_cast<uint32_t *>(kept + a.p.p + head * kSquare);
@@ -364,20 +357,17 @@ __device__ __forceinline__ float2 pair_of(const uint8_t *tile, size_t term, int 
     }
     return r;
 }
-// A warp's 16 columns and `cells` * 8 places as blocks of N terms: [term][columns of 8][places of 8].
-template <int N, int CELLS>
-__device__ __forceinline__ void keep_blocks(uint8_t *to, size_t term, int tile, const float (&v)[CELLS][4]) {
+// A warp's 16 columns and CELLS * 8 places as float32 blocks of 8 x 8, a pair of neighbours a lane:
+// [columns of 8][places of 8].
+constexpr int kWide = 2 * kCell;           // bytes of a float32 block
+template <int CELLS>
+__device__ __forceinline__ void keep_blocks(uint8_t *to, int tile, const float (&v)[CELLS][4]) {
     const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int n = 0; n < CELLS; ++n)
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            uint32_t q[N];
-            split<N>(q, v[n][2 * half], v[n][2 * half + 1]);
-#pragma unroll
-            for (int m = 0; m < N; ++m)
-                *reinterpret_cast<uint32_t *>(to + m * term + ((tile * 2 + half) * CELLS + n) * kCell + lane * 4) = q[m];
-        }
+        for (int half = 0; half < 2; ++half)
+            *reinterpret_cast<float2 *>(to + ((tile * 2 + half) * CELLS + n) * kWide + lane * 8) = make_float2(v[n][2 * half], v[n][2 * half + 1]);
 }
 
 // State of 16 columns of v (rows) and all Dk places, from and to [Dk, Dv] float32.
@@ -415,7 +405,7 @@ __device__ __forceinline__ void put<__nv_bfloat16>(__nv_bfloat16 *p, float v) { 
 template <typename T, int DKP, bool KEEP>
 __global__ void __launch_bounds__(kWarps * 32, 1) delta_forward_kernel(const __grid_constant__ Args a, uint8_t *kept, const float *s0, T *o,
                                                                        float *last, int stages) {
-    constexpr int NT = sizeof(T) == 2 ? 1 : 3, NS = sizeof(T) == 2 ? 2 : 3, W = DKP / 8, TILE = 64 * DKP * 2, SQ = kSquare / 3;
+    constexpr int NT = sizeof(T) == 2 ? 1 : 3, W = DKP / 8, TILE = 64 * DKP * 2, SQ = kSquare / 3;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ __align__(8) uint64_t bars[2];
     pdl_begin();
@@ -440,7 +430,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) delta_forward_kernel(const __g
     for (int n = 0; n < chunks; ++n) {
         const int at = n % stages;
         const int64_t hv = (s.slot + n) * a.Hv + h;
-        if (KEEP) keep_blocks<NS, W>(kept + a.p.s + hv * a.p.state_bytes, (size_t)a.p.DVP * DKP * 2, tile, S);
+        if (KEEP) keep_blocks<W>(kept + a.p.s + hv * a.p.state_bytes, tile, S);
         ok = ok && tc::bar_wait(bar + 8 * at, n / stages & 1);
         if (!ok)
 #pragma unroll
@@ -456,20 +446,15 @@ __global__ void __launch_bounds__(kWarps * 32, 1) delta_forward_kernel(const __g
             uint32_t x[3][4];
             split_left<3>(x, S[2 * ks], S[2 * ks + 1]);
 #pragma unroll
-            for (int p = 0; p < 4; ++p)
+            for (int p = 0; p < 4; ++p) {
+                uint32_t f[NT][4];
 #pragma unroll
-                for (int m = 0; m < NT; ++m) {
-                    uint32_t f[4], f2[4];
-                    right_rows(f, sk + m * TILE, W, 2 * p, 2 * ks);
-                    right_rows(f2, sq + m * TILE, W, 2 * p, 2 * ks);
+                for (int m = 0; m < NT; ++m) right_rows(f[m], sk + m * TILE, W, 2 * p, 2 * ks);
+                products<3, NT, 3>(r[2 * p], r[2 * p + 1], x, f);
 #pragma unroll
-                    for (int i = 0; i + m < 3; ++i) {
-                        multiply(r[2 * p], x[i], f[0], f[1]);
-                        multiply(r[2 * p + 1], x[i], f[2], f[3]);
-                        multiply(out[2 * p], x[i], f2[0], f2[1]);
-                        multiply(out[2 * p + 1], x[i], f2[2], f2[3]);
-                    }
-                }
+                for (int m = 0; m < NT; ++m) right_rows(f[m], sq + m * TILE, W, 2 * p, 2 * ks);
+                products<3, NT, 3>(out[2 * p], out[2 * p + 1], x, f);
+            }
         }
         // v - first k S; the decayed state
         const float keep = gates[kKeep];
@@ -495,19 +480,14 @@ __global__ void __launch_bounds__(kWarps * 32, 1) delta_forward_kernel(const __g
             uint32_t x[3][4];
             split_left<3>(x, r[2 * ks], r[2 * ks + 1]);
 #pragma unroll
-            for (int p = ks; p < 4; ++p)
+            for (int p = ks; p < 4; ++p) {
+                uint32_t f[3][4];
 #pragma unroll
-                for (int m = 0; m < 3; ++m) {
-                    uint32_t f[4];
-                    right_rows(f, sx + m * SQ, 8, 2 * p, 2 * ks);
-#pragma unroll
-                    for (int i = 0; i + m < 3; ++i) {
-                        multiply(e[2 * p], x[i], f[0], f[1]);
-                        multiply(e[2 * p + 1], x[i], f[2], f[3]);
-                    }
-                }
+                for (int m = 0; m < 3; ++m) right_rows(f[m], sx + m * SQ, 8, 2 * p, 2 * ks);
+                products<3, 3, 3>(e[2 * p], e[2 * p + 1], x, f);
+            }
         }
-        if (KEEP) keep_blocks<3, 8>(kept + a.p.e + hv * a.p.kept_bytes, (size_t)a.p.DVP * C * 2, tile, e);
+        if (KEEP) keep_blocks<8>(kept + a.p.e + hv * a.p.kept_bytes, tile, e);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float2 bt = *reinterpret_cast<const float2 *>(gates + kBeta + i * 8 + 2 * t);
@@ -518,17 +498,12 @@ __global__ void __launch_bounds__(kWarps * 32, 1) delta_forward_kernel(const __g
             uint32_t x[3][4];
             split_left<3>(x, e[2 * ks], e[2 * ks + 1]);
 #pragma unroll
-            for (int p = ks; p < 4; ++p)
+            for (int p = ks; p < 4; ++p) {
+                uint32_t f[3][4];
 #pragma unroll
-                for (int m = 0; m < 3; ++m) {
-                    uint32_t f[4];
-                    right_rows(f, sp + m * SQ, 8, 2 * p, 2 * ks);
-#pragma unroll
-                    for (int i = 0; i + m < 3; ++i) {
-                        multiply(out[2 * p], x[i], f[0], f[1]);
-                        multiply(out[2 * p + 1], x[i], f[2], f[3]);
-                    }
-                }
+                for (int m = 0; m < 3; ++m) right_rows(f[m], sp + m * SQ, 8, 2 * p, 2 * ks);
+                products<3, 3, 3>(out[2 * p], out[2 * p + 1], x, f);
+            }
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const float2 re = *reinterpret_cast<const float2 *>(gates + kRest + (2 * ks + i) * 8 + 2 * t);
@@ -539,16 +514,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1) delta_forward_kernel(const __g
 #pragma unroll
             for (int p = 0; p < W / 2; ++p) {
                 if (p * 16 >= a.Dk) break;
+                uint32_t f[NT][4];
 #pragma unroll
-                for (int m = 0; m < NT; ++m) {
-                    uint32_t f[4];
-                    right_columns(f, sk + m * TILE, W, 2 * ks, 2 * p);
-#pragma unroll
-                    for (int i = 0; i + m < 3; ++i) {
-                        multiply(S[2 * p], x[i], f[0], f[1]);
-                        multiply(S[2 * p + 1], x[i], f[2], f[3]);
-                    }
-                }
+                for (int m = 0; m < NT; ++m) right_columns(f[m], sk + m * TILE, W, 2 * ks, 2 * p);
+                products<3, NT, 3>(S[2 * p], S[2 * p + 1], x, f);
             }
         }
         __syncthreads();
@@ -565,13 +534,14 @@ __global__ void __launch_bounds__(kWarps * 32, 1) delta_forward_kernel(const __g
             }
     }
     if (!ok) let_land();
+    if (KEEP) keep_blocks<W>(kept + a.p.end + ((int64_t)b * a.Hv + h) * a.p.state_bytes, tile, S);
     if (last) write_state<W>(S, last + state, tile * 16, a.Dk, a.Dv);
 }
 
 template <typename T, int DKP>
 __global__ void __launch_bounds__(kWarps * 32, 1) delta_backward_kernel(const __grid_constant__ Args a, const uint8_t *kept, uint8_t *scratch,
                                                                         const float *glast, float *gs0, int stages) {
-    constexpr int NT = sizeof(T) == 2 ? 1 : 3, NS = sizeof(T) == 2 ? 2 : 3, W = DKP / 8, TILE = 64 * DKP * 2, SQ = kSquare / 3;
+    constexpr int NT = sizeof(T) == 2 ? 1 : 3, W = DKP / 8, TILE = 64 * DKP * 2, SQ = kSquare / 3;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ __align__(8) uint64_t bars[2];
     pdl_begin();
@@ -596,7 +566,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) delta_backward_kernel(const __
     for (int n = 0; n < chunks; ++n) {
         const int at = n % stages;
         const int64_t hv = (s.slot + chunks - 1 - n) * a.Hv + h;
-        keep_blocks<NS, W>(scratch + a.p.d + hv * a.p.state_bytes, (size_t)a.p.DVP * DKP * 2, tile, D);
+        keep_blocks<W>(scratch + a.p.d + hv * a.p.state_bytes, tile, D);
         ok = ok && tc::bar_wait(bar + 8 * at, n / stages & 1);
         if (!ok)
 #pragma unroll
@@ -615,17 +585,12 @@ __global__ void __launch_bounds__(kWarps * 32, 1) delta_backward_kernel(const __
                 for (int i = 0; i < 4; ++i)
                     x[m][i] = *reinterpret_cast<const uint32_t *>(gob + m * warps * 2048 + ((warp * 2 + (i & 1)) * 8 + 2 * ks + (i >> 1)) * kCell + lane * 4);
 #pragma unroll
-            for (int p = 0; p <= ks; ++p)
+            for (int p = 0; p <= ks; ++p) {
+                uint32_t f[3][4];
 #pragma unroll
-                for (int m = 0; m < 3; ++m) {
-                    uint32_t f[4];
-                    right_columns(f, sp + m * SQ, 8, 2 * ks, 2 * p);
-#pragma unroll
-                    for (int i = 0; i < NT && i + m < 3; ++i) {
-                        multiply(d[2 * p], x[i], f[0], f[1]);
-                        multiply(d[2 * p + 1], x[i], f[2], f[3]);
-                    }
-                }
+                for (int m = 0; m < 3; ++m) right_columns(f[m], sp + m * SQ, 8, 2 * ks, 2 * p);
+                products<NT, 3, 3>(d[2 * p], d[2 * p + 1], x, f);
+            }
         }
         // k D
 #pragma unroll
@@ -634,17 +599,12 @@ __global__ void __launch_bounds__(kWarps * 32, 1) delta_backward_kernel(const __
             uint32_t x[3][4];
             split_left<3>(x, D[2 * ks], D[2 * ks + 1]);
 #pragma unroll
-            for (int p = 0; p < 4; ++p)
+            for (int p = 0; p < 4; ++p) {
+                uint32_t f[NT][4];
 #pragma unroll
-                for (int m = 0; m < NT; ++m) {
-                    uint32_t f[4];
-                    right_rows(f, sk + m * TILE, W, 2 * p, 2 * ks);
-#pragma unroll
-                    for (int i = 0; i + m < 3; ++i) {
-                        multiply(r[2 * p], x[i], f[0], f[1]);
-                        multiply(r[2 * p + 1], x[i], f[2], f[3]);
-                    }
-                }
+                for (int m = 0; m < NT; ++m) right_rows(f[m], sk + m * TILE, W, 2 * p, 2 * ks);
+                products<3, NT, 3>(r[2 * p], r[2 * p + 1], x, f);
+            }
         }
         const float keep = gates[kKeep];
 #pragma unroll
@@ -663,19 +623,14 @@ __global__ void __launch_bounds__(kWarps * 32, 1) delta_backward_kernel(const __
             uint32_t x[3][4];
             split_left<3>(x, d[2 * ks], d[2 * ks + 1]);
 #pragma unroll
-            for (int p = 0; p <= ks; ++p)
+            for (int p = 0; p <= ks; ++p) {
+                uint32_t f[3][4];
 #pragma unroll
-                for (int m = 0; m < 3; ++m) {
-                    uint32_t f[4];
-                    right_columns(f, sx + m * SQ, 8, 2 * ks, 2 * p);
-#pragma unroll
-                    for (int i = 0; i + m < 3; ++i) {
-                        multiply(y[2 * p], x[i], f[0], f[1]);
-                        multiply(y[2 * p + 1], x[i], f[2], f[3]);
-                    }
-                }
+                for (int m = 0; m < 3; ++m) right_columns(f[m], sx + m * SQ, 8, 2 * ks, 2 * p);
+                products<3, 3, 3>(y[2 * p], y[2 * p + 1], x, f);
+            }
         }
-        keep_blocks<3, 8>(scratch + a.p.y + hv * a.p.kept_bytes, (size_t)a.p.DVP * C * 2, tile, y);
+        keep_blocks<8>(scratch + a.p.y + hv * a.p.kept_bytes, tile, y);
         // q^T (scale first go) - k^T (first b y)
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) {
@@ -698,19 +653,13 @@ __global__ void __launch_bounds__(kWarps * 32, 1) delta_backward_kernel(const __
 #pragma unroll
             for (int p = 0; p < W / 2; ++p) {
                 if (p * 16 >= a.Dk) break;
+                uint32_t f[NT][4];
 #pragma unroll
-                for (int m = 0; m < NT; ++m) {
-                    uint32_t f[4], f2[4];
-                    right_columns(f, sq + m * TILE, W, 2 * ks, 2 * p);
-                    right_columns(f2, sk + m * TILE, W, 2 * ks, 2 * p);
+                for (int m = 0; m < NT; ++m) right_columns(f[m], sq + m * TILE, W, 2 * ks, 2 * p);
+                products<3, NT, 3>(D[2 * p], D[2 * p + 1], x, f);
 #pragma unroll
-                    for (int i = 0; i + m < 3; ++i) {
-                        multiply(D[2 * p], x[i], f[0], f[1]);
-                        multiply(D[2 * p + 1], x[i], f[2], f[3]);
-                        multiply(D[2 * p], z[i], f2[0], f2[1]);
-                        multiply(D[2 * p + 1], z[i], f2[2], f2[3]);
-                    }
-                }
+                for (int m = 0; m < NT; ++m) right_columns(f[m], sk + m * TILE, W, 2 * ks, 2 * p);
+                products<3, NT, 3>(D[2 * p], D[2 * p + 1], z, f);
             }
         }
         __syncthreads();
@@ -724,15 +673,33 @@ __global__ void __launch_bounds__(kWarps * 32, 1) delta_backward_kernel(const __
 // ------------------------------------------------------------------ gradients of q, k and the gates
 // Columns of v that a round takes, and the places of their tiles in a stage.
 constexpr int kRound = 32;
-template <int NT, int NS, int DKP>
+template <int NT, int DKP>
 struct Parts {
+    static constexpr int FEW = NT == 1 ? 2 : 3;           // terms where a bfloat16 comes of it
+    // a stage: float32 blocks of the states and of e and y, tiles of go and v
     static constexpr uint32_t state = kRound * DKP * 2, values = kRound * C * 2;      // bytes of a term
-    static constexpr uint32_t s = 0, d = s + NS * state, go = d + NS * state, v = go + NT * values, y = v + NT * values,
-                              e = y + 3 * values, bytes = e + 3 * values;
+    static constexpr uint32_t s = 0, d = s + 2 * state, y = d + 2 * state, e = y + 2 * values, go = e + 2 * values,
+                              v = go + NT * values, bytes = v + NT * values;
+    // the round's tiles of the former, as terms
+    static constexpr uint32_t ts = 2 * bytes, td = ts + 3 * state, ty = td + FEW * state, te = ty + FEW * values, tiles_end = te + 3 * values;
     static constexpr uint32_t keys = NT * C * DKP * 2;
-    // k and q: behind the stages, or (three terms) in the second one when the rounds are over
-    static constexpr uint32_t key_at = NT == 1 ? 2 * bytes : bytes, end = NT == 1 ? 2 * bytes + 2 * keys : 2 * bytes;
+    // k and q: behind the tiles, or (three terms) where the stages were when the rounds are over; the
+    // square matrices of the chunk: where the first stage, or the tiles were
+    static constexpr uint32_t key_at = NT == 1 ? tiles_end : 0, square_at = NT == 1 ? 0 : ts, end = NT == 1 ? tiles_end + 2 * keys : tiles_end;
+    static_assert(NT == 1 ? 2 * kSquare <= 2 * bytes : 2 * keys <= 2 * bytes && 2 * kSquare <= end - ts, "what is laid over fits");
 };
+// float32 blocks as tiles of N terms, by all of a block's threads.
+template <int N>
+__device__ __forceinline__ void tiles_from(uint8_t *to, uint32_t term, const uint8_t *from, int cells) {
+    const int lane = threadIdx.x & 31;
+    for (int c = threadIdx.x >> 5; c < cells; c += kWarps) {
+        const float2 v = *reinterpret_cast<const float2 *>(from + c * kWide + lane * 8);
+        uint32_t q[N];
+        split<N>(q, v.x, v.y);
+#pragma unroll
+        for (int m = 0; m < N; ++m) *reinterpret_cast<uint32_t *>(to + m * term + c * kCell + lane * 4) = q[m];
+    }
+}
 
 // A block for a chunk and value head: all products over v in rounds of 32 columns, then those within the
 // chunk. Eight warps: 16 tokens each, one half of Dk (and of the square matrices' columns). Gradients of
@@ -740,9 +707,9 @@ struct Parts {
 template <typename T, int DKP>
 __global__ void __launch_bounds__(kWarps * 32, 1) delta_gradients_kernel(const __grid_constant__ Args a, const uint8_t *kept, uint8_t *scratch,
                                                                          T *gq, T *gk, T *gv, float *ggate, float *gbeta) {
-    constexpr int NT = sizeof(T) == 2 ? 1 : 3, NS = sizeof(T) == 2 ? 2 : 3, W = DKP / 8, TILE = 64 * DKP * 2, SQ = kSquare / 3;
-    constexpr int N8 = DKP / 16, FEW = sizeof(T) == 2 ? 2 : 3;       // blocks of a warp; terms where a bfloat16 comes of it
-    using P = Parts<NT, NS, DKP>;
+    constexpr int NT = sizeof(T) == 2 ? 1 : 3, W = DKP / 8, TILE = 64 * DKP * 2, SQ = kSquare / 3, N8 = DKP / 16;
+    using P = Parts<NT, DKP>;
+    constexpr int FEW = P::FEW;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ __align__(8) uint64_t bars[3];
     __shared__ __align__(16) float gates[kGateFloats];
@@ -760,20 +727,16 @@ __global__ void __launch_bounds__(kWarps * 32, 1) delta_gradients_kernel(const _
     auto load = [&](int n) {
         const uint32_t to = base + (n & 1) * P::bytes, on = bar + 8 * (n & 1);
         const int v0 = n * kRound, count = min(kRound, a.p.DVP - v0);
-        const size_t sterm = (size_t)a.p.DVP * DKP * 2, vterm = (size_t)a.p.DVP * C * 2;
-        const uint32_t sb = count * DKP * 2, vb = count * C * 2;
-        tc::bar_expect(on, 2 * NS * sb + (2 * NT + 6) * vb);
-        for (int m = 0; m < NS; ++m) {
-            load_bytes(to + P::s + m * P::state, kept + a.p.s + hv * a.p.state_bytes + m * sterm + (size_t)v0 * DKP * 2, sb, on);
-            load_bytes(to + P::d + m * P::state, scratch + a.p.d + hv * a.p.state_bytes + m * sterm + (size_t)v0 * DKP * 2, sb, on);
-        }
+        const size_t term = (size_t)a.p.DVP * C * 2;
+        const uint32_t sb = count * DKP * 4, vb = count * C * 2;
+        tc::bar_expect(on, 2 * sb + (2 * NT + 4) * vb);
+        load_bytes(to + P::s, kept + a.p.s + hv * a.p.state_bytes + (size_t)v0 * DKP * 4, sb, on);
+        load_bytes(to + P::d, scratch + a.p.d + hv * a.p.state_bytes + (size_t)v0 * DKP * 4, sb, on);
+        load_bytes(to + P::y, scratch + a.p.y + hv * a.p.kept_bytes + (size_t)v0 * C * 4, 2 * vb, on);
+        load_bytes(to + P::e, kept + a.p.e + hv * a.p.kept_bytes + (size_t)v0 * C * 4, 2 * vb, on);
         for (int m = 0; m < NT; ++m) {
-            load_bytes(to + P::go + m * P::values, scratch + a.p.go + hv * a.p.value_bytes + m * vterm + (size_t)v0 * C * 2, vb, on);
-            load_bytes(to + P::v + m * P::values, kept + a.p.v + hv * a.p.value_bytes + m * vterm + (size_t)v0 * C * 2, vb, on);
-        }
-        for (int m = 0; m < 3; ++m) {
-            load_bytes(to + P::y + m * P::values, scratch + a.p.y + hv * a.p.kept_bytes + m * vterm + (size_t)v0 * C * 2, vb, on);
-            load_bytes(to + P::e + m * P::values, kept + a.p.e + hv * a.p.kept_bytes + m * vterm + (size_t)v0 * C * 2, vb, on);
+            load_bytes(to + P::go + m * P::values, scratch + a.p.go + hv * a.p.value_bytes + m * term + (size_t)v0 * C * 2, vb, on);
+            load_bytes(to + P::v + m * P::values, kept + a.p.v + hv * a.p.value_bytes + m * term + (size_t)v0 * C * 2, vb, on);
         }
     };
     auto load_keys = [&] {
@@ -794,71 +757,30 @@ __global__ void __launch_bounds__(kWarps * 32, 1) delta_gradients_kernel(const _
     const int64_t row = s.row + (int64_t)chunk * C * s.step;
     const float2 mybeta = *reinterpret_cast<const float2 *>(gates + kBeta + warp * 8 + 2 * t);
 
+    // the state behind the chunk: the next chunk's, or the sequence's last
+    const bool ends = (chunk + 1) * C >= s.length;
+    const uint8_t *next = ends ? kept + a.p.end + ((int64_t)b * a.Hv + h) * a.p.state_bytes : kept + a.p.s + (hv + a.Hv) * a.p.state_bytes;
     float goS[N8][4] = {}, yS[N8][4] = {}, eD[N8][4] = {}, A[4][4] = {}, E[4][4] = {};
-    float ey[2] = {}, vy[2] = {}, ds = 0.f;
+    float ey[2] = {}, vy[2] = {}, tail = 0.f;
     bool ok = true;
     for (int n = 0; n < rounds; ++n) {
-        const uint32_t here = base + (n & 1) * P::bytes;
         const uint8_t *mem = smem + (n & 1) * P::bytes;
+        const uint32_t here = base + (n & 1) * P::bytes;
         const int count = min(kRound, a.p.DVP - n * kRound);
         ok = ok && tc::bar_wait(bar + 8 * (n & 1), n / 2 & 1);
-        for (int ks = 0; ks < count / 16; ++ks) {
-            uint32_t ago[NT][4], ay[3][4], ae[3][4];
-#pragma unroll
-            for (int m = 0; m < NT; ++m) left_columns(ago[m], here + P::go + m * P::values, 8, 2 * ks, 2 * wr);
-#pragma unroll
-            for (int m = 0; m < FEW; ++m) {
-                left_columns(ay[m], here + P::y + m * P::values, 8, 2 * ks, 2 * wr);
-                left_columns(ae[m], here + P::e + m * P::values, 8, 2 * ks, 2 * wr);
-            }
-#pragma unroll
-            for (int p = 0; p < N8 / 2; ++p) {
-                if ((wh * N8 + 2 * p) * 8 >= a.Dk) break;
-#pragma unroll
-                for (int m = 0; m < NS; ++m) {
-                    uint32_t f[4];
-                    right_columns(f, here + P::s + m * P::state, W, 2 * ks, wh * N8 + 2 * p);
-#pragma unroll
-                    for (int i = 0; i < NT && i + m < NS; ++i) {
-                        multiply(goS[2 * p], ago[i], f[0], f[1]);
-                        multiply(goS[2 * p + 1], ago[i], f[2], f[3]);
-                    }
-#pragma unroll
-                    for (int i = 0; i + m < FEW; ++i) {
-                        multiply(yS[2 * p], ay[i], f[0], f[1]);
-                        multiply(yS[2 * p + 1], ay[i], f[2], f[3]);
-                    }
-                    right_columns(f, here + P::d + m * P::state, W, 2 * ks, wh * N8 + 2 * p);
-#pragma unroll
-                    for (int i = 0; i + m < FEW; ++i) {
-                        multiply(eD[2 * p], ae[i], f[0], f[1]);
-                        multiply(eD[2 * p + 1], ae[i], f[2], f[3]);
-                    }
-                }
-            }
-#pragma unroll
-            for (int p = 0; p < 2; ++p) {
-                if (2 * wh + p > wr) break;
-#pragma unroll
-                for (int m = 0; m < 3; ++m) {
-                    uint32_t f[4];
-                    right_columns(f, here + P::e + m * P::values, 8, 2 * ks, 4 * wh + 2 * p);
-#pragma unroll
-                    for (int i = 0; i < NT && i + m < 3; ++i) {
-                        multiply(A[2 * p], ago[i], f[0], f[1]);
-                        multiply(A[2 * p + 1], ago[i], f[2], f[3]);
-                    }
-#pragma unroll
-                    for (int i = 0; i + m < FEW; ++i) {
-                        multiply(E[2 * p], ay[i], f[0], f[1]);
-                        multiply(E[2 * p + 1], ay[i], f[2], f[3]);
-                    }
-                }
-            }
+        tiles_from<3>(smem + P::ts, P::state, mem + P::s, count / 8 * W);
+        tiles_from<FEW>(smem + P::td, P::state, mem + P::d, count / 8 * W);
+        tiles_from<FEW>(smem + P::ty, P::values, mem + P::y, count);
+        tiles_from<3>(smem + P::te, P::values, mem + P::e, count);
+        for (int c = warp; c < count / 8 * W; c += kWarps) {
+            const float2 x = *reinterpret_cast<const float2 *>(next + ((size_t)n * kRound / 8 * W + c) * kWide + lane * 8);
+            const float2 y = *reinterpret_cast<const float2 *>(mem + P::d + c * kWide + lane * 8);
+            tail = fmaf(x.x, y.x, fmaf(x.y, y.y, tail));
         }
         // e . y, v . y and the gradient of v: tokens warp * 8 + 2 t and the next
         for (int c = 0; c < count / 8; ++c) {
-            const float2 y = pair_of<3>(mem + P::y, P::values, c * 8 + warp), e = pair_of<3>(mem + P::e, P::values, c * 8 + warp);
+            const float2 y = *reinterpret_cast<const float2 *>(mem + P::y + (c * 8 + warp) * kWide + lane * 8);
+            const float2 e = *reinterpret_cast<const float2 *>(mem + P::e + (c * 8 + warp) * kWide + lane * 8);
             const float2 v = pair_of<NT>(mem + P::v, P::values, c * 8 + warp);
             ey[0] = fmaf(e.x, y.x, ey[0]), ey[1] = fmaf(e.y, y.y, ey[1]);
             vy[0] = fmaf(v.x, y.x, vy[0]), vy[1] = fmaf(v.y, y.y, vy[1]);
@@ -866,9 +788,37 @@ __global__ void __launch_bounds__(kWarps * 32, 1) delta_gradients_kernel(const _
             if (col < a.Dv && tok < left) put(gv + ((row + tok * s.step) * a.Hv + h) * a.Dv + col, mybeta.x * y.x);
             if (col < a.Dv && tok + 1 < left) put(gv + ((row + (tok + 1) * s.step) * a.Hv + h) * a.Dv + col, mybeta.y * y.y);
         }
-        for (int c = warp; c < count / 8 * W; c += kWarps) {
-            const float2 x = pair_of<NS>(mem + P::s, P::state, c), y = pair_of<NS>(mem + P::d, P::state, c);
-            ds = fmaf(x.x, y.x, fmaf(x.y, y.y, ds));
+        __syncthreads();
+        for (int ks = 0; ks < count / 16; ++ks) {
+            uint32_t ago[NT][4], ay[FEW][4], ae[FEW][4];
+#pragma unroll
+            for (int m = 0; m < NT; ++m) left_columns(ago[m], here + P::go + m * P::values, 8, 2 * ks, 2 * wr);
+#pragma unroll
+            for (int m = 0; m < FEW; ++m) {
+                left_columns(ay[m], base + P::ty + m * P::values, 8, 2 * ks, 2 * wr);
+                left_columns(ae[m], base + P::te + m * P::values, 8, 2 * ks, 2 * wr);
+            }
+#pragma unroll
+            for (int p = 0; p < N8 / 2; ++p) {
+                if ((wh * N8 + 2 * p) * 8 >= a.Dk) break;
+                uint32_t f[3][4], f2[FEW][4];
+#pragma unroll
+                for (int m = 0; m < 3; ++m) right_columns(f[m], base + P::ts + m * P::state, W, 2 * ks, wh * N8 + 2 * p);
+                products<NT, 3, 3>(goS[2 * p], goS[2 * p + 1], ago, f);
+                products<FEW, 3, FEW>(yS[2 * p], yS[2 * p + 1], ay, f);
+#pragma unroll
+                for (int m = 0; m < FEW; ++m) right_columns(f2[m], base + P::td + m * P::state, W, 2 * ks, wh * N8 + 2 * p);
+                products<FEW, FEW, FEW>(eD[2 * p], eD[2 * p + 1], ae, f2);
+            }
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                if (2 * wh + p > wr) break;
+                uint32_t f[3][4];
+#pragma unroll
+                for (int m = 0; m < 3; ++m) right_columns(f[m], base + P::te + m * P::values, 8, 2 * ks, 4 * wh + 2 * p);
+                products<NT, 3, 3>(A[2 * p], A[2 * p + 1], ago, f);
+                products<FEW, 3, FEW>(E[2 * p], E[2 * p + 1], ay, f);
+            }
         }
         __syncthreads();
         if (threadIdx.x == 0 && ok && n + 2 < rounds) load(n + 2);
@@ -885,8 +835,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) delta_gradients_kernel(const _
         edot[warp * 8 + 2 * t] = ey[0], edot[warp * 8 + 2 * t + 1] = ey[1];
         vdot[warp * 8 + 2 * t] = mybeta.x * vy[0], vdot[warp * 8 + 2 * t + 1] = mybeta.y * vy[1];
     }
-    // the square matrices, as terms, where the first stage was
-    const uint32_t At = base, Ct = base + kSquare;
+    // the square matrices, as terms
+    const uint32_t At = base + P::square_at, Ct = At + kSquare;
 #pragma unroll
     for (int n = 0; n < 4; ++n)
 #pragma unroll
@@ -902,7 +852,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) delta_gradients_kernel(const _
             uint32_t xs[3], cs[3];
             split<3>(xs, x[0], x[1]);
             split<3>(cs, c[0], c[1]);
-            uint8_t *to = smem + ((wr * 2 + half) * 8 + wh * 4 + n) * kCell + lane * 4;
+            uint8_t *to = smem + P::square_at + ((wr * 2 + half) * 8 + wh * 4 + n) * kCell + lane * 4;
 #pragma unroll
             for (int m = 0; m < 3; ++m) {
                 *reinterpret_cast<uint32_t *>(to + m * SQ) = xs[m];
@@ -911,29 +861,25 @@ __global__ void __launch_bounds__(kWarps * 32, 1) delta_gradients_kernel(const _
         }
     __syncthreads();
     ok = ok && tc::bar_wait(bar + 16, 0);
-    const uint8_t *km = smem + P::key_at, *qm = km + P::keys;
+    const uint8_t *qm = smem + P::key_at + P::keys;
     const uint32_t kt = base + P::key_at, qt = kt + P::keys;
-    float kd = 0.f;
 #pragma unroll
     for (int n = 0; n < N8; ++n)
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             const int i = wr * 16 + half * 8 + g;
             const float f = gates[kFirst + i], bt = gates[kBeta + i], re = gates[kRest + i];
-            const float2 k = pair_of<NT>(km, TILE, (wr * 2 + half) * W + wh * N8 + n);
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 float &x = goS[n][2 * half + e], &y = yS[n][2 * half + e];
-                const float d = re * bt * eD[n][2 * half + e];
-                kd = fmaf(e ? k.y : k.x, d, kd);
                 x *= a.scale * f;
-                y = fmaf(-f * bt, y, d);
+                y = bt * fmaf(-f, y, re * eD[n][2 * half + e]);
             }
         }
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) {
-        uint32_t la[3][4], lc[3][4];
         if (ks <= wr) {        // A k and C k
+            uint32_t la[3][4], lc[FEW][4];
 #pragma unroll
             for (int m = 0; m < 3; ++m) left_rows(la[m], At + m * SQ, 8, 2 * wr, 2 * ks);
 #pragma unroll
@@ -941,24 +887,15 @@ __global__ void __launch_bounds__(kWarps * 32, 1) delta_gradients_kernel(const _
 #pragma unroll
             for (int p = 0; p < N8 / 2; ++p) {
                 if ((wh * N8 + 2 * p) * 8 >= a.Dk) break;
+                uint32_t f[NT][4];
 #pragma unroll
-                for (int m = 0; m < NT; ++m) {
-                    uint32_t f[4];
-                    right_columns(f, kt + m * TILE, W, 2 * ks, wh * N8 + 2 * p);
-#pragma unroll
-                    for (int i = 0; i + m < 3; ++i) {
-                        multiply(goS[2 * p], la[i], f[0], f[1]);
-                        multiply(goS[2 * p + 1], la[i], f[2], f[3]);
-                    }
-#pragma unroll
-                    for (int i = 0; i + m < FEW; ++i) {
-                        multiply(yS[2 * p], lc[i], f[0], f[1]);
-                        multiply(yS[2 * p + 1], lc[i], f[2], f[3]);
-                    }
-                }
+                for (int m = 0; m < NT; ++m) right_columns(f[m], kt + m * TILE, W, 2 * ks, wh * N8 + 2 * p);
+                products<3, NT, 3>(goS[2 * p], goS[2 * p + 1], la, f);
+                products<FEW, NT, FEW>(yS[2 * p], yS[2 * p + 1], lc, f);
             }
         }
         if (ks >= wr) {        // A^T q and C^T k
+            uint32_t la[FEW][4], lc[FEW][4];
 #pragma unroll
             for (int m = 0; m < FEW; ++m) {
                 left_columns(la[m], At + m * SQ, 8, 2 * ks, 2 * wr);
@@ -967,19 +904,13 @@ __global__ void __launch_bounds__(kWarps * 32, 1) delta_gradients_kernel(const _
 #pragma unroll
             for (int p = 0; p < N8 / 2; ++p) {
                 if ((wh * N8 + 2 * p) * 8 >= a.Dk) break;
+                uint32_t f[NT][4];
 #pragma unroll
-                for (int m = 0; m < NT; ++m) {
-                    uint32_t f[4], f2[4];
-                    right_columns(f, qt + m * TILE, W, 2 * ks, wh * N8 + 2 * p);
-                    right_columns(f2, kt + m * TILE, W, 2 * ks, wh * N8 + 2 * p);
+                for (int m = 0; m < NT; ++m) right_columns(f[m], qt + m * TILE, W, 2 * ks, wh * N8 + 2 * p);
+                products<FEW, NT, FEW>(yS[2 * p], yS[2 * p + 1], la, f);
 #pragma unroll
-                    for (int i = 0; i + m < FEW; ++i) {
-                        multiply(yS[2 * p], la[i], f[0], f[1]);
-                        multiply(yS[2 * p + 1], la[i], f[2], f[3]);
-                        multiply(yS[2 * p], lc[i], f2[0], f2[1]);
-                        multiply(yS[2 * p + 1], lc[i], f2[2], f2[3]);
-                    }
-                }
+                for (int m = 0; m < NT; ++m) right_columns(f[m], kt + m * TILE, W, 2 * ks, wh * N8 + 2 * p);
+                products<FEW, NT, FEW>(yS[2 * p], yS[2 * p + 1], lc, f);
             }
         }
     }
@@ -987,7 +918,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) delta_gradients_kernel(const _
 #pragma unroll
         for (int n = 0; n < N8; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) goS[n][e] = yS[n][e] = kd = __int_as_float(0x7fffffff);
+            for (int e = 0; e < 4; ++e) goS[n][e] = yS[n][e] = tail = __int_as_float(0x7fffffff);
     float *parts = reinterpret_cast<float *>(scratch + a.p.parts);
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
@@ -1015,16 +946,15 @@ __global__ void __launch_bounds__(kWarps * 32, 1) delta_gradients_kernel(const _
         dot += __shfl_xor_sync(0xffffffffu, dot, 2);
         if (t == 0) qdot[wh][i] = dot;
     }
-    kd = fmaf(gates[kKeep], ds, kd);
 #pragma unroll
-    for (int o = 16; o; o >>= 1) kd += __shfl_xor_sync(0xffffffffu, kd, o);
-    if (lane == 0) sums[warp] = kd;
+    for (int o = 16; o; o >>= 1) tail += __shfl_xor_sync(0xffffffffu, tail, o);
+    if (lane == 0) sums[warp] = tail;
     __syncthreads();
     if (!ok) let_land();
     if (warp) return;
     // the gates: sums from each token to the chunk's end, and what comes back through the state
-    double tail = 0.0, mine[2];
-    for (int i = 0; i < kWarps; ++i) tail += (double)sums[i];
+    double behind_all = 0.0, mine[2];
+    for (int i = 0; i < kWarps; ++i) behind_all += (double)sums[i];
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
         const int i = 2 * lane + e;
@@ -1041,7 +971,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) delta_gradients_kernel(const _
         const int i = 2 * lane + e;
         if (i >= left) continue;
         const int64_t at = (row + i * s.step) * a.Hv + h;
-        ggate[at] = (float)(tail + behind - (e ? mine[0] : 0.0));
+        ggate[at] = (float)(behind_all + behind - (e ? mine[0] : 0.0));
         gbeta[at] = edot[i];
     }
 }
@@ -1268,7 +1198,7 @@ cudaError_t run_forward(const Args &a, const void *q, const void *k, const void 
 template <typename T, int DKP>
 cudaError_t run_backward(const Args &a, const void *go, const float *glast, const uint8_t *kept, void *gq, void *gk, void *gv, float *ggate,
                          float *gbeta, float *gs0, uint8_t *scratch, cudaStream_t s, int *launches) {
-    constexpr int NT = sizeof(T) == 2 ? 1 : 3, NS = sizeof(T) == 2 ? 2 : 3;
+    constexpr int NT = sizeof(T) == 2 ? 1 : 3;
     const dim3 chunks((unsigned)a.p.slots, (unsigned)a.Hv);
     cudaError_t e = cudaSuccess;
     if (a.p.slots) {
@@ -1281,7 +1211,7 @@ cudaError_t run_backward(const Args &a, const void *go, const float *glast, cons
         e = seq_launch(delta_backward_kernel<T, DKP>, dim3((unsigned)(a.B * a.Hv), (unsigned)w.blocks), w.warps * 32, w.smem, s, 1, a, kept, scratch, glast, gs0, w.stages);
     ++*launches;
     if (!a.p.slots || e != cudaSuccess) return e;
-    constexpr size_t smem = Parts<NT, NS, DKP>::end;
+    constexpr size_t smem = Parts<NT, DKP>::end;
     e = room(delta_gradients_kernel<T, DKP>, smem);
     if (e == cudaSuccess)
         e = seq_launch(delta_gradients_kernel<T, DKP>, chunks, kWarps * 32, smem, s, 1, a, kept, scratch, (T *)gq, (T *)gk, (T *)gv, ggate, gbeta);

@@ -13,13 +13,13 @@ constexpr int kGateFloats = 6 * 64;        // of a chunk and value head: see the
 
 // Places in bytes; sizes of one chunk (and head).
 struct DeltaPlan {
-    int32_t terms, state_terms;            // bfloat16 terms of an input, of a kept state
+    int32_t terms;                         // bfloat16 terms of an input
     int32_t DKP, DVP;                      // Dk as the tiles have it (64 or 128), Dv up to a multiple of 16
     int64_t slots;                         // chunks there can be
     int64_t tokens;
-    size_t key_bytes, value_bytes, kept_bytes, state_bytes;   // a tile of k or q, of v, of e (three terms), a state
+    size_t key_bytes, value_bytes, kept_bytes, state_bytes;   // a tile of k or q, of v; e and a state in float32
     // kept: what the backward needs of the forward; without it the forward's scratch starts with the same
-    size_t k, q, v, xe, p, gates, forward_end, xu, e, s, kept_end;
+    size_t k, q, v, xe, p, gates, forward_end, xu, e, s, end, kept_end;
     // the backward's scratch
     size_t go, y, d, parts, backward_end;
 };
@@ -28,7 +28,6 @@ template <typename Config>
 inline DeltaPlan delta_plan(const Config &c, int layout_packed, bool bf16) {
     DeltaPlan p;
     p.terms = bf16 ? 1 : 3;
-    p.state_terms = bf16 ? 2 : 3;
     p.DKP = c.Dk <= 64 ? 64 : 128;
     p.DVP = (c.Dv + 15) / 16 * 16;
     const int64_t T = c.T, B = c.B;
@@ -36,8 +35,8 @@ inline DeltaPlan delta_plan(const Config &c, int layout_packed, bool bf16) {
     p.tokens = c.layout == layout_packed ? T : T * B;
     p.key_bytes = (size_t)p.terms * 64 * p.DKP * 2;
     p.value_bytes = (size_t)p.terms * 64 * p.DVP * 2;
-    p.kept_bytes = (size_t)3 * 64 * p.DVP * 2;
-    p.state_bytes = (size_t)p.state_terms * p.DVP * p.DKP * 2;
+    p.kept_bytes = (size_t)64 * p.DVP * 4;
+    p.state_bytes = (size_t)p.DVP * p.DKP * 4;
     const size_t nk = (size_t)p.slots * c.Hk, nv = (size_t)p.slots * c.Hv;
     size_t at = 0;
     auto take = [&](size_t bytes) { size_t was = at; at += (bytes + 255) / 256 * 256; return was; };
@@ -51,6 +50,7 @@ inline DeltaPlan delta_plan(const Config &c, int layout_packed, bool bf16) {
     p.xu = take(nv * kSquare);
     p.e = take(nv * p.kept_bytes);
     p.s = take(nv * p.state_bytes);
+    p.end = take((size_t)B * c.Hv * p.state_bytes);
     p.kept_end = at;
     at = 0;
     p.go = take(nv * p.value_bytes);

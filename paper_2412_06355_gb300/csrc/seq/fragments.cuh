@@ -77,6 +77,26 @@ __device__ __forceinline__ void left_columns(uint32_t (&a)[4], uint32_t tile, in
     fetch4_turned(a, tile + ((k + (m >> 1)) * width + i + (m & 1)) * kCell + (lane & 7) * 16);
 }
 
+// Adds to the 16 x 16 results c0, c1 the product of a left factor in NA terms and a right one in NB: the
+// products of terms i and j with i + j < KEEP, the smallest first, summed by themselves. The matrix
+// instruction cuts its sums off where it should round them: a long sum in one accumulator lost up to
+// 2e-6 of its norm, this way (one addition of float32 each 16 summed places) 2e-7.
+template <int NA, int NB, int KEEP>
+__device__ __forceinline__ void products(float (&c0)[4], float (&c1)[4], const uint32_t (&a)[NA][4], const uint32_t (&f)[NB][4]) {
+    float t0[4] = {}, t1[4] = {};
+#pragma unroll
+    for (int sum = KEEP - 1; sum >= 0; --sum)
+#pragma unroll
+        for (int i = 0; i < NA; ++i) {
+            const int j = sum - i;
+            if (j < 0 || j >= NB) continue;
+            multiply(t0, a[i], f[j < 0 || j >= NB ? 0 : j][0], f[j < 0 || j >= NB ? 0 : j][1]);
+            multiply(t1, a[i], f[j < 0 || j >= NB ? 0 : j][2], f[j < 0 || j >= NB ? 0 : j][3]);
+        }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c0[e] += t0[e], c1[e] += t1[e];
+}
+
 // `bytes` (a multiple of 16) from global into this block's shared memory, counted on `bar`.
 __device__ __forceinline__ void load_bytes(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
