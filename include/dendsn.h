@@ -419,7 +419,8 @@ dendsn_status dendsn_norm_backward(const dendsn_norm_config *cfg, const void *su
  * what was in the outputs (rest KEEP) or get zeros (ZERO). Offsets out of order or range give results of
  * no meaning, within the buffers.
  * A gate below -200 (also -infinity) counts as -200, whose decay is 0 in float32: the state before is
- * multiplied by zero (it has to be finite) and the gate's gradient is 0.
+ * multiplied by zero (it has to be finite) and the gate's gradient is 0. NaN and infinities in a sequence
+ * reach the tokens behind them and all of their own chunk of 64 tokens, no other sequence.
  * bfloat16 inputs enter the products exactly, float32 inputs as three bfloat16 terms (2^-24); states and
  * everything between the products are float32. grad_q and grad_k of bfloat16 inputs come of states in two
  * bfloat16 terms (2^-17), and so does grad_gate's part in q's gradient.

@@ -28,7 +28,8 @@ constexpr int kBlock = 256;            // elements of a warp's turn, and of a sc
 constexpr int kChunk = 4096;           // elements of a block's turn
 constexpr int kThreads = 256;
 constexpr int kGrads = 500;            // tensors of a launch: their gradients' addresses are its arguments
-constexpr int kMostBlocks = 152 * 4;
+constexpr int kMostBlocks = 152 * 4;   // sums of squares a step can have; blocks of the norm's launch
+constexpr int kResident = 3;           // blocks of the update on an SM: 24 warps with up to 80 registers
 constexpr uint32_t kStride = 0x9E3779B1u;
 
 enum : int32_t { kParamBf16 = 1, kWide = 2 };
@@ -180,29 +181,35 @@ __device__ __forceinline__ uint32_t round_code(float value, uint32_t random) {
     const Code c = code_of(value);
     return min(((c.bits + (0xfffffu - 8u - 16u * random)) >> 20) - c.base, 0x7eu);
 }
-// The same for the square: its share of the way between the neighbours' squares.
-__device__ __forceinline__ uint32_t round_square(float value, uint32_t random) {
+// The same for the square: its share of the way between the neighbours' squares. u in (0, 1).
+__device__ __forceinline__ uint32_t round_square(float value, float u) {
     const Code c = code_of(value);
-    const float off = c.base == 121u << 3 ? 0x1p-6f : 0.f;
+    const float twice = c.base == 121u << 3 ? -0x1p-5f : 0.f;           // what was added, off two of them
     const uint32_t low_bits = c.bits & 0xfff00000u;
-    const float low = __uint_as_float(low_bits) - off, high = __uint_as_float(low_bits + 0x100000u) - off;
-    const float u = ((float)random + 0.5f) * 0x1p-16f;
-    const bool up = u * ((high - low) * (high + low)) < (value - low) * (value + low);
+    const float at = __uint_as_float(c.bits), low = __uint_as_float(low_bits), high = __uint_as_float(low_bits + 0x100000u);
+    const bool up = u * ((high - low) * (high + low + twice)) < (at - low) * (at + low + twice);
     return min((low_bits >> 20) - c.base + (up ? 1u : 0u), 0x7eu);
 }
-__device__ __forceinline__ uint32_t warp_top(float v) {
-    uint32_t t = __float_as_uint(v);
+// 16 bits as a number in (0, 1): (h / 65536) + 2^-17 of a word's upper half.
+__device__ __forceinline__ float upper_half(uint32_t h) { return __uint_as_float(0x3f800000u | (h >> 9 & 0x7fff80u)) - (1.f - 0x1p-17f); }
+__device__ __forceinline__ uint32_t warp_top(uint32_t t) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) t = max(t, __shfl_xor_sync(0xffffffffu, t, o));
     return t;
 }
+// The hardware's square root and reciprocal are within 2^-22 of themselves: roundings of the update, which is
+// a thousandth of p, and of what an 8-bit code of v's root is drawn from. The exact ones cost some twenty
+// instructions more an element, of the sixty that memory leaves time for.
 __device__ __forceinline__ float sqrt_fast(float v) {
     float r;
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
-// sqrt(a)/b is within 2^-22 of itself: a rounding of the update, which is a thousandth of p.
-__device__ __forceinline__ float divide(float a, float b) { return __fdividef(a, b); }
+__device__ __forceinline__ float rcp_fast(float v) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
 
 struct Scalars {
     float factor, rate, inverse_root, lr;
@@ -215,80 +222,117 @@ __device__ __forceinline__ float rest_of_power(float t, float hi, float lo) {
     return -expm1f(a + (fmaf(t, hi, -a) + t * lo));
 }
 
-template <bool EIGHT, bool WIDE>
-__device__ __forceinline__ void update(const Tensor &x, uint64_t grad, int64_t at, int lane, const Scalars &c, const Step &s, uint32_t start) {
-    const int left = (int)min((int64_t)kBlock, x.n - at);
-    float g[8], m[8], v[8], p[8];
+// A lane's share of 256 elements.
+template <bool EIGHT>
+struct Share {
+    float g[8], p[8];
+    float m[EIGHT ? 1 : 8], v[EIGHT ? 1 : 8];
     uint32_t qm[2], qv[2];
-    float2 sc = make_float2(0.f, 0.f);
-    if (grad & 1) load8<WIDE>(g, reinterpret_cast<const __nv_bfloat16 *>(grad - 1) + at, lane, left);
-    else load8<WIDE>(g, reinterpret_cast<const float *>(grad) + at, lane, left);
-    if (x.flags & kParamBf16) load8<WIDE>(p, static_cast<const __nv_bfloat16 *>(x.param) + at, lane, left);
-    else load8<WIDE>(p, static_cast<const float *>(x.param) + at, lane, left);
-    if (EIGHT) {
-        load_codes<WIDE>(qm, static_cast<const uint8_t *>(x.m) + at, lane, left);
-        load_codes<WIDE>(qv, static_cast<const uint8_t *>(x.v) + at, lane, left);
-        sc = *reinterpret_cast<const float2 *>(x.scales + at / kBlock * 2);
-        decode(m, qm, sc.x);
-        decode(v, qv, sc.y);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] *= v[j];
+    float2 scale;
+    int left;
+};
+
+template <bool EIGHT, bool WIDE>
+__device__ __forceinline__ void load(Share<EIGHT> &r, const Tensor &x, uint64_t grad, int64_t at, int lane) {
+    const int left = r.left = (int)min((int64_t)kBlock, x.n - at);
+    if (grad & 1) load8<WIDE>(r.g, reinterpret_cast<const __nv_bfloat16 *>(grad - 1) + at, lane, left);
+    else load8<WIDE>(r.g, reinterpret_cast<const float *>(grad) + at, lane, left);
+    if (x.flags & kParamBf16) load8<WIDE>(r.p, static_cast<const __nv_bfloat16 *>(x.param) + at, lane, left);
+    else load8<WIDE>(r.p, static_cast<const float *>(x.param) + at, lane, left);
+    if constexpr (EIGHT) {
+        load_codes<WIDE>(r.qm, static_cast<const uint8_t *>(x.m) + at, lane, left);
+        load_codes<WIDE>(r.qv, static_cast<const uint8_t *>(x.v) + at, lane, left);
+        r.scale = *reinterpret_cast<const float2 *>(x.scales + at / kBlock * 2);
     } else {
-        load8<WIDE>(m, static_cast<const float *>(x.m) + at, lane, left);
-        load8<WIDE>(v, static_cast<const float *>(x.v) + at, lane, left);
+        load8<WIDE>(r.m, static_cast<const float *>(x.m) + at, lane, left);
+        load8<WIDE>(r.v, static_cast<const float *>(x.v) + at, lane, left);
     }
-    const float kept = fmaf(-c.lr, x.decay, 1.f);
-    float root[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const float gj = g[j] * c.factor;
-        m[j] = fmaf(s.rest1, gj - m[j], m[j]);
-        v[j] = fmaf(s.rest2, fmaf(gj, gj, -v[j]), v[j]);
-        root[j] = EIGHT ? sqrt_fast(v[j]) : sqrtf(v[j]);
-        const float below = fmaf(root[j], c.inverse_root, s.eps), above = c.rate * m[j];
-        p[j] = fmaf(p[j], kept, -(EIGHT ? divide(above, below) : __fdiv_rn(above, below)));
-    }
-    if (x.flags & kParamBf16) store8<WIDE>(p, static_cast<__nv_bfloat16 *>(x.param) + at, lane, left);
-    else store8<WIDE>(p, static_cast<float *>(x.param) + at, lane, left);
-    if (x.copy) store8<WIDE>(p, x.copy + at, lane, left);
-    if (!EIGHT) {
-        store8<WIDE>(m, static_cast<float *>(x.m) + at, lane, left);
-        store8<WIDE>(v, static_cast<float *>(x.v) + at, lane, left);
-        return;
-    }
-    // sizes as unsigned integers order as the sizes do, with a NaN above them all
-    uint32_t top_m = 0, top_v = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-        if (element<WIDE>(lane, j) < left) {
-            top_m = max(top_m, __float_as_uint(m[j]) & 0x7fffffffu);
-            top_v = max(top_v, __float_as_uint(root[j]) & 0x7fffffffu);
-        }
-    const float tm = __uint_as_float(warp_top(__uint_as_float(top_m))), tv = __uint_as_float(warp_top(__uint_as_float(top_v)));
-    // below 2^-110 a block's states are zeros: 448 / top would leave float32
-    const float im = tm < 0x1p-110f ? 0.f : __fdiv_rn(448.f, tm), iv = tv < 0x1p-110f ? 0.f : __fdiv_rn(448.f, tv);
-    if (lane == 0)
-        *reinterpret_cast<float2 *>(x.scales + at / kBlock * 2) =
-            make_float2(tm < 0x1p-110f ? 0.f : __fdiv_rn(tm, 448.f), tv < 0x1p-110f ? 0.f : __fdiv_rn(tv, 448.f));
-    qm[0] = qm[1] = qv[0] = qv[1] = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const uint32_t h = mix((uint32_t)(at + element<WIDE>(lane, j)) * kStride + start);
-        const float am = fminf(fabsf(m[j] * im), 448.f), av = fminf(root[j] * iv, 448.f);
-        const uint32_t cm = round_code(am, h & 0xffffu) | (__float_as_uint(m[j]) >> 24 & 0x80u);
-        const uint32_t cv = round_square(av, h >> 16);
-        qm[j >> 2] |= cm << (j & 3) * 8;
-        qv[j >> 2] |= cv << (j & 3) * 8;
-    }
-    store_codes<WIDE>(qm, static_cast<uint8_t *>(x.m) + at, lane, left);
-    store_codes<WIDE>(qv, static_cast<uint8_t *>(x.v) + at, lane, left);
 }
 
-template <bool EIGHT>
-__global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ Step s, const __grid_constant__ Grads grads) {
-    __shared__ Scalars shared;
-    __shared__ double part[kThreads / 32];
-    pdl_begin();
+template <bool EIGHT, bool WIDE>
+__device__ __forceinline__ void update(Share<EIGHT> &r, const Tensor &x, int64_t at, int lane, const Scalars &c, const Step &s, uint32_t start) {
+    const int left = r.left;
+    const float kept = fmaf(-c.lr, x.decay, 1.f);
+    float m[8], v[8], root[8];
+    if constexpr (EIGHT) {
+        decode(m, r.qm, r.scale.x);
+        decode(v, r.qv, r.scale.y);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        if constexpr (EIGHT) v[j] *= v[j];
+        else m[j] = r.m[j], v[j] = r.v[j];
+        const float g = r.g[j] * c.factor;
+        m[j] = fmaf(s.rest1, g - m[j], m[j]);
+        v[j] = fmaf(s.rest2, fmaf(g, g, -v[j]), v[j]);
+        root[j] = EIGHT ? sqrt_fast(v[j]) : sqrtf(v[j]);
+        const float below = fmaf(root[j], c.inverse_root, s.eps), above = c.rate * m[j];
+        r.p[j] = fmaf(r.p[j], kept, -(EIGHT ? above * rcp_fast(below) : __fdiv_rn(above, below)));
+    }
+    if (x.flags & kParamBf16) store8<WIDE>(r.p, static_cast<__nv_bfloat16 *>(x.param) + at, lane, left);
+    else store8<WIDE>(r.p, static_cast<float *>(x.param) + at, lane, left);
+    if (x.copy) store8<WIDE>(r.p, x.copy + at, lane, left);
+    if constexpr (!EIGHT) {
+        store8<WIDE>(m, static_cast<float *>(x.m) + at, lane, left);
+        store8<WIDE>(v, static_cast<float *>(x.v) + at, lane, left);
+    } else {
+        // sizes as unsigned integers order as the sizes do, with a NaN above them all (elements behind the
+        // tensor's end are zeros)
+        uint32_t top_m = 0, top_v = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            top_m = max(top_m, __float_as_uint(m[j]) & 0x7fffffffu);
+            top_v = max(top_v, __float_as_uint(root[j]));
+        }
+        const float tm = __uint_as_float(warp_top(top_m)), tv = __uint_as_float(warp_top(top_v));
+        // below 2^-110 a block's states are zeros: 448 / top would leave float32
+        const float im = tm < 0x1p-110f ? 0.f : 448.f * rcp_fast(tm), iv = tv < 0x1p-110f ? 0.f : 448.f * rcp_fast(tv);
+        if (lane == 0)
+            *reinterpret_cast<float2 *>(x.scales + at / kBlock * 2) =
+                make_float2(tm < 0x1p-110f ? 0.f : tm * (1.f / 448.f), tv < 0x1p-110f ? 0.f : tv * (1.f / 448.f));
+        uint32_t qm[2] = {}, qv[2] = {};
+        const uint32_t first = ((uint32_t)at + (WIDE ? lane * 8 : lane)) * kStride + start;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t h = mix(first + (uint32_t)(WIDE ? j : j * 32) * kStride);
+            const uint32_t cm = round_code(fabsf(m[j]) * im, h & 0xffffu) | (__float_as_uint(m[j]) >> 24 & 0x80u);
+            const uint32_t cv = round_square(root[j] * iv, upper_half(h));
+            qm[j >> 2] |= cm << (j & 3) * 8;
+            qv[j >> 2] |= cv << (j & 3) * 8;
+        }
+        store_codes<WIDE>(qm, static_cast<uint8_t *>(x.m) + at, lane, left);
+        store_codes<WIDE>(qv, static_cast<uint8_t *>(x.v) + at, lane, left);
+    }
+}
+
+// A block's run of chunks, and the tensor it is in.
+struct Run {
+    const Tensor *tensors;
+    int32_t chunk, end, i, next;       // this chunk, behind the last; its tensor, the next tensor's first chunk
+    Tensor x;
+    __device__ __forceinline__ explicit Run(const Step &s) {
+        tensors = reinterpret_cast<const Tensor *>(s.plan + kTensorsAt);
+        const int64_t n = s.chunks - s.chunk;
+        chunk = s.chunk + (int32_t)(n * blockIdx.x / gridDim.x);
+        end = s.chunk + (int32_t)(n * (blockIdx.x + 1) / gridDim.x);
+        next = chunk;
+        if (chunk < end) enter(reinterpret_cast<const int32_t *>(tensors + s.tensors)[chunk]);
+    }
+    __device__ __forceinline__ void enter(int32_t to) {
+        i = to;
+        x = tensors[i];
+        next = x.first + (int32_t)((x.n + kChunk - 1) / kChunk);
+    }
+    __device__ __forceinline__ void advance() {
+        if (++chunk >= next && chunk < end) {
+            do enter(i + 1);
+            while (chunk >= next);     // tensors without elements have no chunk
+        }
+    }
+};
+
+// The values that depend on the step: the norm from the sums of squares in order, the powers of the betas.
+__device__ void scalars(Scalars &shared, const Step &s, double *part) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const double *sums = reinterpret_cast<const double *>(s.plan + kSumsAt);
     double sum = 0.0;
@@ -325,38 +369,49 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
         }
     }
     __syncthreads();
-    const Scalars c = shared;
-    const Tensor *tensors = reinterpret_cast<const Tensor *>(s.plan + kTensorsAt);
-    const int32_t *of = reinterpret_cast<const int32_t *>(tensors + s.tensors);
-    for (int32_t chunk = s.chunk + blockIdx.x; chunk < s.chunks; chunk += gridDim.x) {
-        const int32_t i = of[chunk];
-        const uint64_t grad = grads.at[i - s.first];
-        if (!grad) continue;
-        const Tensor x = tensors[i];
-        const uint32_t start = mix(c.start + (uint32_t)i);
-        const bool wide = (x.flags & kWide) && (grad & 1 ? grad % 16 == 1 : grad % 32 == 0);
-        int64_t at = (int64_t)(chunk - x.first) * kChunk + warp * kBlock;
-        const int64_t end = min(x.n, (int64_t)(chunk - x.first + 1) * kChunk);
-        for (; at < end; at += kThreads / 32 * kBlock) {
-            if (wide) update<EIGHT, true>(x, grad, at, lane, c, s, start);
-            else update<EIGHT, false>(x, grad, at, lane, c, s, start);
-        }
-    }
 }
 
-// Sum of squares of a block's chunks; `sum` says where in the table.
+template <bool EIGHT>
+__global__ void __launch_bounds__(kThreads, kResident) adamw_kernel(const __grid_constant__ Step s, const __grid_constant__ Grads grads) {
+    __shared__ Scalars shared;
+    __shared__ double part[kThreads / 32];
+    pdl_begin();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    Scalars c;
+    bool known = false;
+    for (Run r(s); r.chunk < r.end; r.advance()) {
+        const uint64_t grad = grads.at[r.i - s.first];
+        if (!grad) continue;
+        const bool wide = (r.x.flags & kWide) && (grad & 1 ? grad % 16 == 1 : grad % 32 == 0);
+        uint32_t start = 0;
+#pragma unroll 1
+        for (int turn = 0; turn < kChunk / kThreads / 8; ++turn) {
+            const int64_t at = (int64_t)(r.chunk - r.x.first) * kChunk + (turn * (kThreads / 32) + warp) * kBlock;
+            const bool here = at < r.x.n;
+            Share<EIGHT> e;
+            if (here) wide ? load<EIGHT, true>(e, r.x, grad, at, lane) : load<EIGHT, false>(e, r.x, grad, at, lane);
+            if (!known) {          // while the first elements are on their way
+                scalars(shared, s, part);
+                c = shared;
+                known = true;
+            }
+            if (!turn) start = mix(c.start + (uint32_t)r.i);
+            if (here) wide ? update<EIGHT, true>(e, r.x, at, lane, c, s, start) : update<EIGHT, false>(e, r.x, at, lane, c, s, start);
+        }
+    }
+    if (!known) scalars(shared, s, part);
+}
+
+// Sum of squares of a block's chunks; `to` says where in the table.
 __global__ void __launch_bounds__(kThreads) adamw_norm_kernel(const __grid_constant__ Step s, const __grid_constant__ Grads grads, int32_t to) {
     __shared__ double part[kThreads / 32];
     pdl_begin();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const Tensor *tensors = reinterpret_cast<const Tensor *>(s.plan + kTensorsAt);
-    const int32_t *of = reinterpret_cast<const int32_t *>(tensors + s.tensors);
     double sum = 0.0;
-    for (int32_t chunk = s.chunk + blockIdx.x; chunk < s.chunks; chunk += gridDim.x) {
-        const int32_t i = of[chunk];
-        const uint64_t grad = grads.at[i - s.first];
+    for (Run r(s); r.chunk < r.end; r.advance()) {
+        const uint64_t grad = grads.at[r.i - s.first];
         if (!grad) continue;
-        const int64_t n = tensors[i].n, first = (int64_t)(chunk - tensors[i].first) * kChunk;
+        const int64_t n = r.x.n, first = (int64_t)(r.chunk - r.x.first) * kChunk;
         const bool bf = grad & 1, wide = n % 8 == 0 && (bf ? grad % 16 == 1 : grad % 32 == 0);
         float g[kChunk / kThreads / 8][8];
 #pragma unroll
@@ -497,7 +552,7 @@ dendsn_status dendsn_adamw_step(const dendsn_adamw_config *cfg, void *plan, cons
             }
             a.chunks = chunk;
             a.last = r == rounds - 1;
-            const int blocks = std::max(1, std::min(a.chunks - a.chunk, pass ? kMostBlocks : most));
+            const int blocks = std::max(1, std::min(a.chunks - a.chunk, pass ? 152 * kResident : most));
             if (pass == 0) {
                 e = seq_launch(adamw_norm_kernel, dim3((unsigned)blocks), kThreads, 0, s, 1, a, g, sums);
                 sums += blocks;

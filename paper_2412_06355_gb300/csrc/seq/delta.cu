@@ -406,6 +406,7 @@ template <typename T, int DKP, bool KEEP>
 __global__ void __launch_bounds__(kWarps * 32, 1) delta_forward_kernel(const __grid_constant__ Args a, uint8_t *kept, const float *s0, T *o,
                                                                        float *last, int stages) {
     constexpr int NT = sizeof(T) == 2 ? 1 : 3, W = DKP / 8, TILE = 64 * DKP * 2, SQ = kSquare / 3;
+    constexpr int FEW = sizeof(T) == 2 ? 2 : 3;        // terms where only a bfloat16 output comes of it
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ __align__(8) uint64_t bars[2];
     pdl_begin();
@@ -453,7 +454,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) delta_forward_kernel(const __g
                 products<3, NT, 3>(r[2 * p], r[2 * p + 1], x, f);
 #pragma unroll
                 for (int m = 0; m < NT; ++m) right_rows(f[m], sq + m * TILE, W, 2 * p, 2 * ks);
-                products<3, NT, 3>(out[2 * p], out[2 * p + 1], x, f);
+                products<3, NT, FEW>(out[2 * p], out[2 * p + 1], x, f);
             }
         }
         // v - first k S; the decayed state
@@ -499,10 +500,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1) delta_forward_kernel(const __g
             split_left<3>(x, e[2 * ks], e[2 * ks + 1]);
 #pragma unroll
             for (int p = ks; p < 4; ++p) {
-                uint32_t f[3][4];
+                uint32_t f[FEW][4];
 #pragma unroll
-                for (int m = 0; m < 3; ++m) right_rows(f[m], sp + m * SQ, 8, 2 * p, 2 * ks);
-                products<3, 3, 3>(out[2 * p], out[2 * p + 1], x, f);
+                for (int m = 0; m < FEW; ++m) right_rows(f[m], sp + m * SQ, 8, 2 * p, 2 * ks);
+                products<3, FEW, FEW>(out[2 * p], out[2 * p + 1], x, f);
             }
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
@@ -688,11 +689,14 @@ struct Parts {
     static constexpr uint32_t key_at = NT == 1 ? tiles_end : 0, square_at = NT == 1 ? 0 : ts, end = NT == 1 ? tiles_end + 2 * keys : tiles_end;
     static_assert(NT == 1 ? 2 * kSquare <= 2 * bytes : 2 * keys <= 2 * bytes && 2 * kSquare <= end - ts, "what is laid over fits");
 };
-// float32 blocks as tiles of N terms, by all of a block's threads.
-template <int N>
+// Up to CELLS float32 blocks as tiles of N terms, by all of a block's threads.
+template <int N, int CELLS>
 __device__ __forceinline__ void tiles_from(uint8_t *to, uint32_t term, const uint8_t *from, int cells) {
-    const int lane = threadIdx.x & 31;
-    for (int c = threadIdx.x >> 5; c < cells; c += kWarps) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int i = 0; i < CELLS / kWarps; ++i) {
+        const int c = warp + i * kWarps;
+        if (c >= cells) break;
         const float2 v = *reinterpret_cast<const float2 *>(from + c * kWide + lane * 8);
         uint32_t q[N];
         split<N>(q, v.x, v.y);
@@ -767,18 +771,27 @@ __global__ void __launch_bounds__(kWarps * 32, 1) delta_gradients_kernel(const _
         const uint8_t *mem = smem + (n & 1) * P::bytes;
         const uint32_t here = base + (n & 1) * P::bytes;
         const int count = min(kRound, a.p.DVP - n * kRound);
+        constexpr int OWN = kRound / 8 * W / kWarps;       // float32 blocks of a state that a warp looks at
+        float2 behind[OWN];
+#pragma unroll
+        for (int i = 0; i < OWN; ++i)
+            if (warp + i * kWarps < count / 8 * W)
+                behind[i] = *reinterpret_cast<const float2 *>(next + ((size_t)n * kRound / 8 * W + warp + i * kWarps) * kWide + lane * 8);
         ok = ok && tc::bar_wait(bar + 8 * (n & 1), n / 2 & 1);
-        tiles_from<3>(smem + P::ts, P::state, mem + P::s, count / 8 * W);
-        tiles_from<FEW>(smem + P::td, P::state, mem + P::d, count / 8 * W);
-        tiles_from<FEW>(smem + P::ty, P::values, mem + P::y, count);
-        tiles_from<3>(smem + P::te, P::values, mem + P::e, count);
-        for (int c = warp; c < count / 8 * W; c += kWarps) {
-            const float2 x = *reinterpret_cast<const float2 *>(next + ((size_t)n * kRound / 8 * W + c) * kWide + lane * 8);
-            const float2 y = *reinterpret_cast<const float2 *>(mem + P::d + c * kWide + lane * 8);
-            tail = fmaf(x.x, y.x, fmaf(x.y, y.y, tail));
+        tiles_from<3, kRound / 8 * W>(smem + P::ts, P::state, mem + P::s, count / 8 * W);
+        tiles_from<FEW, kRound / 8 * W>(smem + P::td, P::state, mem + P::d, count / 8 * W);
+        tiles_from<FEW, kRound>(smem + P::ty, P::values, mem + P::y, count);
+        tiles_from<3, kRound>(smem + P::te, P::values, mem + P::e, count);
+#pragma unroll
+        for (int i = 0; i < OWN; ++i) {
+            if (warp + i * kWarps >= count / 8 * W) break;
+            const float2 y = *reinterpret_cast<const float2 *>(mem + P::d + (warp + i * kWarps) * kWide + lane * 8);
+            tail = fmaf(behind[i].x, y.x, fmaf(behind[i].y, y.y, tail));
         }
         // e . y, v . y and the gradient of v: tokens warp * 8 + 2 t and the next
-        for (int c = 0; c < count / 8; ++c) {
+#pragma unroll
+        for (int c = 0; c < kRound / 8; ++c) {
+            if (c >= count / 8) break;
             const float2 y = *reinterpret_cast<const float2 *>(mem + P::y + (c * 8 + warp) * kWide + lane * 8);
             const float2 e = *reinterpret_cast<const float2 *>(mem + P::e + (c * 8 + warp) * kWide + lane * 8);
             const float2 v = pair_of<NT>(mem + P::v, P::values, c * 8 + warp);
@@ -971,23 +984,35 @@ __global__ void __launch_bounds__(kWarps * 32, 1) delta_gradients_kernel(const _
         const int i = 2 * lane + e;
         if (i >= left) continue;
         const int64_t at = (row + i * s.step) * a.Hv + h;
-        ggate[at] = (float)(behind_all + behind - (e ? mine[0] : 0.0));
+        // a decay that is 0 in float32 (exp(-104)) has no gradient
+        const float gate = gates[kHigh + i] - (i ? gates[kHigh + i - 1] : 0.f) + (gates[kLow + i] - (i ? gates[kLow + i - 1] : 0.f));
+        ggate[at] = gate < -104.f ? 0.f : (float)(behind_all + behind - (e ? mine[0] : 0.0));
         gbeta[at] = edot[i];
     }
 }
 
-// Gradients of a key head: those of its value heads added up in order. blockIdx.y: of q, of k.
-template <typename T>
-__global__ void __launch_bounds__(256) delta_join_kernel(const __grid_constant__ Args a, const float *parts, T *gq, T *gk) {
+// Gradients of a key head: those of its value heads added up in order, VEC neighbours a thread. blockIdx.y:
+// of q, of k. `width`: vectors of a token.
+template <typename T, int VEC>
+__global__ void __launch_bounds__(256) delta_join_kernel(const __grid_constant__ Args a, const float *parts, T *gq, T *gk, uint32_t width) {
     pdl_begin();
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / (a.Hk * a.Dk);
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / width;
     if (row >= a.p.tokens) return;
     if (a.layout == DENDSN_DELTA_PACKED && (row < a.offsets[0] || row >= a.offsets[a.B])) return;
-    const int h = (int)(i % (a.Hk * a.Dk)) / a.Dk, d = (int)(i % a.Dk), group = a.Hv / a.Hk;
+    const int at = (int)(i - row * width) * VEC, h = at / a.Dk, d = at - h * a.Dk, group = a.Hv / a.Hk;
     const float *from = parts + ((blockIdx.y * a.p.tokens + row) * a.Hv + (int64_t)h * group) * a.Dk + d;
-    float v = 0.f;
-    for (int j = 0; j < group; ++j) v += from[(int64_t)j * a.Dk];
-    put((blockIdx.y ? gk : gq) + i, v);
+    float v[VEC] = {};
+    for (int j = 0; j < group; ++j) {
+        if constexpr (VEC == 4) {
+            const float4 x = *reinterpret_cast<const float4 *>(from + (int64_t)j * a.Dk);
+            v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
+        } else {
+            v[0] += from[(int64_t)j * a.Dk];
+        }
+    }
+    T *to = (blockIdx.y ? gk : gq) + i * VEC;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) put(to + e, v[e]);
 }
 
 // Rows of no sequence, as zeros.
@@ -1007,23 +1032,25 @@ __global__ void __launch_bounds__(256) delta_rest_kernel(const __grid_constant__
 }
 
 // ------------------------------------------------------------------ few tokens
-// A token at a time, as the formulas are written: a block has one head's state in registers, `lanes`
-// threads a row of VEC columns each. Bound by the state's read and write for one token; a step of a few
-// tokens costs two sums over the block each.
+// A token at a time, as the formulas are written. Columns of v do not meet: a block has 32 of one head's in
+// registers, 32 values a thread, LANES threads a row of VEC columns each. Bound by the state's read and
+// write: many small blocks keep loads and stores of different blocks on their way at once (64 sequences of 8
+// heads of 128 x 128, one token: a block for all columns 19 us, the state's bytes alone 10).
+constexpr int kStepColumns = 32, kStepThreads = 128;
 template <typename T, int VEC>
-__global__ void __launch_bounds__(256) delta_step_kernel(const __grid_constant__ Args a, const T *q, const T *k, const T *v, const float *gate,
-                                                         const float *beta, const float *s0, T *o, float *last, int lanes) {
-    constexpr int ROWS = VEC == 4 ? 16 : 64;
-    __shared__ float ks[kDeltaMost], qs[kDeltaMost], part[2][8][kDeltaMost], us[kDeltaMost];
+__global__ void __launch_bounds__(kStepThreads, 7) delta_step_kernel(const __grid_constant__ Args a, const T *q, const T *k, const T *v, const float *gate,
+                                                                     const float *beta, const float *s0, T *o, float *last) {
+    constexpr int LANES = kStepColumns / VEC, PASS = kStepThreads / LANES, ROWS = kDeltaMost / PASS;
+    __shared__ float ks[kDeltaMost], qs[kDeltaMost], part[2][kStepThreads / 32][kStepColumns];
     pdl_begin();
     const int b = blockIdx.x / a.Hv, h = blockIdx.x % a.Hv, hk = h / (a.Hv / a.Hk), tid = threadIdx.x;
-    const int rows = 256 / lanes, r0 = tid / lanes, col = tid % lanes * VEC, parts = min(8, rows), mine = lanes >= 32 ? r0 : tid / 32;
+    const int r0 = tid / LANES, in = tid % LANES * VEC, first = blockIdx.y * kStepColumns, col = first + in;
     const Sequence s = sequence(a, b);
     const int64_t state = ((int64_t)b * a.Hv + h) * a.Dk * a.Dv;
     float S[ROWS][VEC];
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
-        const int r = r0 + i * rows;
+        const int r = r0 + i * PASS;
 #pragma unroll
         for (int e = 0; e < VEC; ++e) S[i][e] = 0.f;
         if (s0 && r < a.Dk && col < a.Dv) {
@@ -1036,29 +1063,38 @@ __global__ void __launch_bounds__(256) delta_step_kernel(const __grid_constant__
             }
         }
     }
-    // sums over the rows of every column: within a warp, then over the warps' (or rows') parts
-    auto gather = [&](float (&x)[VEC], float (*to)[kDeltaMost]) {
-        for (int w = lanes; w < 32; w <<= 1)
+    // sums over the rows of every column: within a warp, then of the warps
+    auto gather = [&](float (&x)[VEC], float (*to)[kStepColumns]) {
+#pragma unroll
+        for (int w = LANES; w < 32; w <<= 1)
 #pragma unroll
             for (int e = 0; e < VEC; ++e) x[e] += __shfl_xor_sync(0xffffffffu, x[e], w);
-        if (col < a.Dv && (lanes >= 32 || (tid & 31) < lanes))
+        if ((tid & 31) < LANES)
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) to[mine][col + e] = x[e];
+            for (int e = 0; e < VEC; ++e) to[tid / 32][in + e] = x[e];
+        __syncthreads();
+    };
+    auto total = [&](const float (*from)[kStepColumns], int c) {
+        float x = 0.f;
+#pragma unroll
+        for (int w = 0; w < kStepThreads / 32; ++w) x += from[w][c];
+        return x;
     };
     for (int n = 0; n < s.length; ++n) {
         const int64_t tok = s.row + n * s.step;
-        __syncthreads();
-        for (int i = tid; i < a.Dk; i += 256) {
+        if (n) __syncthreads();
+        for (int i = tid; i < a.Dk; i += kStepThreads) {
             ks[i] = value(k + (tok * a.Hk + hk) * a.Dk + i);
             qs[i] = value(q + (tok * a.Hk + hk) * a.Dk + i);
         }
-        const float g = gate[tok * a.Hv + h], decay = expf(g), bt = beta[tok * a.Hv + h];
-        const float vt = tid < a.Dv ? value(v + (tok * a.Hv + h) * a.Dv + tid) : 0.f;
+        const float decay = expf(gate[tok * a.Hv + h]), bt = beta[tok * a.Hv + h];
+        float u[VEC], x[VEC] = {}, z[VEC] = {};
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) u[e] = col + e < a.Dv ? value(v + (tok * a.Hv + h) * a.Dv + col + e) : 0.f;
         __syncthreads();
-        float x[VEC] = {};
 #pragma unroll
         for (int i = 0; i < ROWS; ++i) {
-            const int r = r0 + i * rows;
+            const int r = r0 + i * PASS;
             const float kr = r < a.Dk ? ks[r] : 0.f;
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
@@ -1067,19 +1103,11 @@ __global__ void __launch_bounds__(256) delta_step_kernel(const __grid_constant__
             }
         }
         gather(x, part[0]);
-        __syncthreads();
-        if (tid < a.Dv) {
-            float read = 0.f;
-            for (int i = 0; i < parts; ++i) read += part[0][i][tid];
-            us[tid] = bt * (vt - read);
-        }
-        __syncthreads();
-        float u[VEC], z[VEC] = {};
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) u[e] = col + e < a.Dv ? us[col + e] : 0.f;
+        for (int e = 0; e < VEC; ++e) u[e] = bt * (u[e] - total(part[0], in + e));
 #pragma unroll
         for (int i = 0; i < ROWS; ++i) {
-            const int r = r0 + i * rows;
+            const int r = r0 + i * PASS;
             const float kr = r < a.Dk ? ks[r] : 0.f, qr = r < a.Dk ? qs[r] : 0.f;
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
@@ -1088,17 +1116,12 @@ __global__ void __launch_bounds__(256) delta_step_kernel(const __grid_constant__
             }
         }
         gather(z, part[1]);
-        __syncthreads();
-        if (tid < a.Dv) {
-            float out = 0.f;
-            for (int i = 0; i < parts; ++i) out += part[1][i][tid];
-            put(o + (tok * a.Hv + h) * a.Dv + tid, a.scale * out);
-        }
+        if (tid < kStepColumns && first + tid < a.Dv) put(o + (tok * a.Hv + h) * a.Dv + first + tid, a.scale * total(part[1], tid));
     }
     if (!last) return;
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
-        const int r = r0 + i * rows;
+        const int r = r0 + i * PASS;
         if (r >= a.Dk || col >= a.Dv) continue;
         float *to = last + state + (int64_t)r * a.Dv + col;
         if constexpr (VEC == 4) *reinterpret_cast<float4 *>(to) = make_float4(S[i][0], S[i][1], S[i][2], S[i][3]);
@@ -1144,11 +1167,9 @@ template <typename T>
 cudaError_t run_step(const Args &a, const void *q, const void *k, const void *v, const float *gate, const float *beta, const float *s0, void *o,
                      float *last, cudaStream_t s) {
     const bool four = a.Dv % 4 == 0 && seq_aligned(s0, 16) && seq_aligned(last, 16);
-    int lanes = 1;
-    while (lanes * (four ? 4 : 1) < a.Dv) lanes *= 2;
-    const dim3 grid((unsigned)(a.B * a.Hv));
-    return four ? seq_launch(delta_step_kernel<T, 4>, grid, 256, 0, s, 1, a, (const T *)q, (const T *)k, (const T *)v, gate, beta, s0, (T *)o, last, lanes)
-                : seq_launch(delta_step_kernel<T, 1>, grid, 256, 0, s, 1, a, (const T *)q, (const T *)k, (const T *)v, gate, beta, s0, (T *)o, last, lanes);
+    const dim3 grid((unsigned)(a.B * a.Hv), (unsigned)((a.Dv + kStepColumns - 1) / kStepColumns));
+    return four ? seq_launch(delta_step_kernel<T, 4>, grid, kStepThreads, 0, s, 1, a, (const T *)q, (const T *)k, (const T *)v, gate, beta, s0, (T *)o, last)
+                : seq_launch(delta_step_kernel<T, 1>, grid, kStepThreads, 0, s, 1, a, (const T *)q, (const T *)k, (const T *)v, gate, beta, s0, (T *)o, last);
 }
 
 template <typename T>
@@ -1217,8 +1238,12 @@ cudaError_t run_backward(const Args &a, const void *go, const float *glast, cons
         e = seq_launch(delta_gradients_kernel<T, DKP>, chunks, kWarps * 32, smem, s, 1, a, kept, scratch, (T *)gq, (T *)gk, (T *)gv, ggate, gbeta);
     ++*launches;
     if (a.Hv > a.Hk && e == cudaSuccess) {
-        const int64_t n = a.p.tokens * a.Hk * a.Dk;
-        e = seq_launch(delta_join_kernel<T>, dim3((unsigned)((n + 255) / 256), 2), 256, 0, s, 1, a, (const float *)(scratch + a.p.parts), (T *)gq, (T *)gk);
+        const int vec = a.Dk % 4 == 0 ? 4 : 1;
+        const int64_t width = (int64_t)a.Hk * a.Dk / vec, n = a.p.tokens * width;
+        const dim3 grid((unsigned)((n + 255) / 256), 2);
+        const float *parts = (const float *)(scratch + a.p.parts);
+        e = vec == 4 ? seq_launch(delta_join_kernel<T, 4>, grid, 256, 0, s, 1, a, parts, (T *)gq, (T *)gk, (uint32_t)width)
+                     : seq_launch(delta_join_kernel<T, 1>, grid, 256, 0, s, 1, a, parts, (T *)gq, (T *)gk, (uint32_t)width);
         ++*launches;
     }
     return e;

@@ -24,7 +24,7 @@ constexpr int kMostColumns = 16384;
 constexpr int kWarpRows = 4;          // rows of a block whose rows have a warp each
 constexpr int kGroup = 128;           // columns that share a scale
 constexpr int kBlocks = 152 * 4;      // of the backward at most: rows of the table of column sums
-constexpr int kSumColumns = 32, kSumRows = 16;
+constexpr int kSumColumns = 8, kSumRows = 64;
 
 // Where vector j of a thread lies in its row. Vectors of 16 bytes are dealt out lane by lane;
 // single elements in runs of 128, so that the columns of a scale belong to one warp.
@@ -224,8 +224,9 @@ __global__ void __launch_bounds__(512) norm_forward_kernel(const T *x, const T *
     }
 }
 
-template <typename T, int VEC, int NV>
-__global__ void __launch_bounds__(512) norm_backward_kernel(const T *sum, const float *weight, const T *gy,
+// BLOCK: threads it is built for. A block of 128 may have more registers than one of 512.
+template <typename T, int VEC, int NV, int BLOCK>
+__global__ void __launch_bounds__(BLOCK) norm_backward_kernel(const T *sum, const float *weight, const T *gy,
                                                             const T *gsum, T *gx, float *table, Rows p) {
     using L = Lot<T, VEC>;
     __shared__ float2 red[2][16];
@@ -238,13 +239,16 @@ __global__ void __launch_bounds__(512) norm_backward_kernel(const T *sum, const 
     int turn = 0;
     for (int64_t row = (int64_t)blockIdx.x * rows + mine; row < p.M; row += (int64_t)gridDim.x * rows, turn ^= 1) {
         const L *zr = reinterpret_cast<const L *>(sum) + row * p.nv, *gr = reinterpret_cast<const L *>(gy) + row * p.nv;
-        L z[NV], g[NV];
+        const L *ar = reinterpret_cast<const L *>(gsum) + row * p.nv;
+        L z[NV], g[NV], q[NV];
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int k = place<VEC>(j, thread, p.threads);
             z[j].zero();
             g[j].zero();
+            q[j].zero();
             if (k < p.nv) z[j] = zr[k], g[j] = gr[k];
+            if (k < p.nv && gsum) q[j] = ar[k];
         }
         float ss = 0.f, hz = 0.f;
 #pragma unroll
@@ -266,20 +270,14 @@ __global__ void __launch_bounds__(512) norm_backward_kernel(const T *sum, const 
         const float2 s = row_sums(ss, hz, p.threads, red[turn]);
         const float r = __fdiv_rn(1.f, sqrtf(s.x / (float)p.D + p.eps));
         const float along = r * r * (s.y / (float)p.D);
-        const L *ar = reinterpret_cast<const L *>(gsum) + row * p.nv;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int k = place<VEC>(j, thread, p.threads);
             float v[VEC], h[VEC], a[VEC];
             z[j].get(v);
             g[j].get(h);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) a[e] = 0.f;
+            q[j].get(a);
             if (k < p.nv) {
-                if (gsum) {
-                    const L t = ar[k];
-                    t.get(a);
-                }
                 float w[VEC];
                 weights<VEC>(w, weight, k);
 #pragma unroll
@@ -312,14 +310,15 @@ __global__ void __launch_bounds__(512) norm_backward_kernel(const T *sum, const 
     }
 }
 
-// The table's columns added up, 16 rows of it at a time by 16 threads of a column.
+// The table's columns added up: 8 columns (a sector) a block, every 64th row by each of a column's threads, in
+// order. 16384 rows, D = 1024: 32 columns and 16 threads 8 us.
 __global__ void __launch_bounds__(kSumColumns *kSumRows) norm_columns_kernel(const float *table, float *gweight, int32_t blocks, int32_t D) {
-    __shared__ float part[kSumRows][kSumColumns + 1];
+    __shared__ float part[kSumRows][kSumColumns];
     pdl_begin();
     const int c = threadIdx.x % kSumColumns, t = threadIdx.x / kSumColumns, col = blockIdx.x * kSumColumns + c;
     float v = 0.f;
     if (col < D) {
-#pragma unroll 8
+#pragma unroll 10
         for (int b = t; b < blocks; b += kSumRows) v += table[(int64_t)b * D + col];
     }
     part[t][c] = v;
@@ -330,11 +329,12 @@ __global__ void __launch_bounds__(kSumColumns *kSumRows) norm_columns_kernel(con
     gweight[col] = v;
 }
 
+template <int N> struct Int { static constexpr int value = N; };
+
 struct Plan {
     Rows rows;
     int block, blocks;         // threads of a block, blocks of the grid
     int vectors;               // NV
-    size_t scratch;
 };
 
 dendsn_status check(const dendsn_norm_config *cfg) {
@@ -352,17 +352,18 @@ int blocks_of(const dendsn_norm_config &c, int rows, int most) {
     return (int)std::max<int64_t>(1, std::min<int64_t>(((int64_t)c.M + rows - 1) / rows, most));
 }
 
-// Up to 32 values a thread. Rows of one warp's are dealt out four to a block.
+// Vectors: up to 32 values a thread, a warp for a row where that holds it, four such rows a block. Single
+// elements: 8 a thread while a block's 512 threads hold the row so, as each load moves little (1009 rows of
+// 1001 floats, backward: 32 a thread 32 us).
 Plan plan_of(const dendsn_norm_config &c, bool wide) {
     Plan p;
-    const int vec = !wide ? 1 : c.x_dtype == DENDSN_BF16 ? 8 : 4, most = 32 / vec;
+    const int vec = !wide ? 1 : c.x_dtype == DENDSN_BF16 ? 8 : 4;
     p.rows = {c.M, c.D, c.D / vec, 32, c.eps};
-    const int step = vec == 1 ? 4 : 1, nv = (p.rows.nv + 31) / 32;
-    p.vectors = step;
+    const int nv = (p.rows.nv + 31) / 32, most = vec > 1 ? 32 / vec : nv <= 8 * 16 ? 8 : nv <= 16 * 16 ? 16 : 32;
+    p.vectors = vec == 1 ? 4 : 1;
     while (p.vectors < most && p.vectors < nv) p.vectors *= 2;
     if (nv > p.vectors) p.rows.threads = (nv + p.vectors - 1) / p.vectors * 32;
     p.block = p.rows.threads == 32 ? 32 * kWarpRows : p.rows.threads;
-    p.scratch = 0;
     return p;
 }
 
@@ -387,17 +388,21 @@ cudaError_t forward_out(const dendsn_norm_config &c, const Plan &p, const void *
 }
 template <typename T, int VEC>
 cudaError_t backward_of(const Plan &p, const void *sum, const float *w, const void *gy, const void *gsum, void *gx, float *table, cudaStream_t s) {
-    auto go = [&](auto kernel, int values) {
-        const size_t smem = p.rows.threads == 32 ? (size_t)(kWarpRows - 1) * values * 32 * 4 : 0;
-        return seq_launch(kernel, dim3((unsigned)p.blocks), p.block, smem, s, 1, (const T *)sum, w, (const T *)gy, (const T *)gsum, (T *)gx, table, p.rows);
+    auto go = [&](auto nv) {
+        constexpr int NV = decltype(nv)::value;
+        const size_t smem = p.rows.threads == 32 ? (size_t)(kWarpRows - 1) * NV * VEC * 32 * 4 : 0;
+        auto run = [&](auto kernel) {
+            return seq_launch(kernel, dim3((unsigned)p.blocks), p.block, smem, s, 1, (const T *)sum, w, (const T *)gy, (const T *)gsum, (T *)gx, table, p.rows);
+        };
+        return p.block <= 128 ? run(norm_backward_kernel<T, VEC, NV, 128>) : run(norm_backward_kernel<T, VEC, NV, 512>);
     };
     switch (p.vectors) {
-        case 1: return go(norm_backward_kernel<T, VEC, VEC == 1 ? 4 : 1>, VEC == 1 ? 4 : VEC);
-        case 2: return go(norm_backward_kernel<T, VEC, VEC == 1 ? 4 : 2>, VEC == 1 ? 4 : 2 * VEC);
-        case 4: return go(norm_backward_kernel<T, VEC, 4>, 4 * VEC);
-        case 8: return go(norm_backward_kernel<T, VEC, VEC == 8 ? 4 : 8>, VEC == 8 ? 32 : 8 * VEC);
-        case 16: return go(norm_backward_kernel<T, VEC, VEC == 1 ? 16 : 4>, VEC == 1 ? 16 : 4 * VEC);
-        default: return go(norm_backward_kernel<T, VEC, VEC == 1 ? 32 : 4>, VEC == 1 ? 32 : 4 * VEC);
+        case 1: return go(Int<VEC == 1 ? 4 : 1>());
+        case 2: return go(Int<VEC == 1 ? 4 : 2>());
+        case 4: return go(Int<4>());
+        case 8: return go(Int<VEC == 8 ? 4 : 8>());
+        case 16: return go(Int<VEC == 1 ? 16 : 4>());
+        default: return go(Int<VEC == 1 ? 32 : 4>());
     }
 }
 
