@@ -17,10 +17,7 @@
 //
 // What has no order runs for all chunks at once: the square matrices (delta_prepare_kernel), the
 // gradients of q, k and the gates (delta_gradients_kernel). In between a block carries the state of one
-// head, or the gradient of it, from chunk to chunk (delta_forward_kernel, delta_backward_kernel): a warp
-// has 16 columns of v in registers, state and results turned (columns of v are the products' rows), so
-// that each product's result is the next one's left factor without leaving the registers; the warps
-// meet once a chunk, for the tiles.
+// head, or the gradient of it, from chunk to chunk (delta_walk.cu).
 //
 // All sums are float32. Products run on the matrix instruction for 16-bit operands: bfloat16 inputs are
 // exact, everything else (float32 inputs, states, results on their way to the next product) is split into
@@ -31,71 +28,13 @@
 #include <algorithm>
 #include <cmath>
 
-#include "delta_plan.h"
-#include "fragments.cuh"
-#include "seq_common.h"
+#include "delta_common.cuh"
 
 namespace dendsn {
+using namespace delta;
 namespace {
 
-constexpr int C = kDeltaChunk;
 constexpr int kWarps = 8;
-constexpr float kLeastGate = -200.f;       // exp of it is 0 in float32
-
-// Places in a chunk's gate values.
-enum { kFirst = 0, kRest = 64, kBeta = 128, kHigh = 192, kLow = 256, kKeep = 320 };
-
-struct Args {
-    int32_t T, B, Hk, Hv, Dk, Dv, layout;
-    float scale;
-    const int32_t *offsets;
-    DeltaPlan p;
-};
-
-struct Sequence {
-    int64_t row, step;         // its first token, tokens between two of its own
-    int64_t slot;              // its first chunk's
-    int32_t length;
-};
-
-__device__ __forceinline__ Sequence sequence(const Args &a, int b) {
-    Sequence s;
-    if (a.layout == DENDSN_DELTA_PACKED) {
-        const int32_t lo = min(max(a.offsets[b], 0), a.T), hi = min(max(a.offsets[b + 1], lo), a.T);
-        s.row = lo, s.step = 1, s.length = hi - lo;
-        s.slot = lo / C + b;
-    } else {
-        const bool time = a.layout == DENDSN_DELTA_TIME;
-        s.row = time ? b : (int64_t)b * a.T, s.step = time ? a.B : 1, s.length = a.T;
-        s.slot = (int64_t)b * ((a.T + C - 1) / C);
-    }
-    return s;
-}
-
-// Which sequence a chunk's slot belongs to; false: to none. A packed sequence from token lo on has the
-// slots from lo / 64 + (its number) on: no two meet, and the last one's stay below T / 64 + B.
-__device__ __forceinline__ bool locate(const Args &a, int64_t slot, int *b, int *chunk, Sequence *s) {
-    if (a.layout == DENDSN_DELTA_PACKED) {
-        int lo = 0, hi = a.B - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) / 2;
-            if (min(max(a.offsets[mid], 0), a.T) / C + mid <= slot) lo = mid;
-            else hi = mid - 1;
-        }
-        *b = lo;
-    } else {
-        *b = (int)(slot / ((a.T + C - 1) / C));
-    }
-    *s = sequence(a, *b);
-    const int64_t c = slot - s->slot;
-    *chunk = (int)c;
-    return c >= 0 && c * C < s->length;
-}
-
-template <typename T>
-__device__ __forceinline__ float value(const T *p) { return __bfloat162float(*p); }
-template <>
-__device__ __forceinline__ float value<float>(const float *p) { return *p; }
 
 // 8 neighbours of a row from `at` on, zeros behind its end.
 template <typename T>
@@ -111,36 +50,6 @@ __device__ __forceinline__ void eight(float (&v)[8], const T *row, int at, int e
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = at + e < end ? value(row + at + e) : 0.f;
-    }
-}
-
-// ------------------------------------------------------------------ values as tiles
-// A chunk's rows of v or go, turned: [term][columns of 8][tokens of 8] blocks whose rows are columns of v.
-template <typename T>
-__global__ void __launch_bounds__(256) delta_turn_kernel(const __grid_constant__ Args a, const T *from, uint8_t *to, bool wide) {
-    constexpr int NT = sizeof(T) == 2 ? 1 : 3;
-    __shared__ float tile[C * (kDeltaMost + 1)];
-    pdl_begin();
-    int b, chunk;
-    Sequence s;
-    if (!locate(a, blockIdx.x, &b, &chunk, &s)) return;
-    const int h = blockIdx.y, DVP = a.p.DVP, left = min(C, s.length - chunk * C), stride = DVP + 1;
-    for (int i = threadIdx.x; i < C * DVP / 8; i += 256) {
-        const int tok = i / (DVP / 8), at = i % (DVP / 8) * 8;
-        float v[8] = {};
-        if (tok < left) eight(v, from + ((s.row + (int64_t)(chunk * C + tok) * s.step) * a.Hv + h) * a.Dv, at, a.Dv, wide);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) tile[tok * stride + at + e] = v[e];
-    }
-    __syncthreads();
-    uint32_t *out = reinterpret_cast<uint32_t *>(to + ((int64_t)blockIdx.x * a.Hv + h) * a.p.value_bytes);
-    const int lane = threadIdx.x & 31, words = C * DVP / 2;
-    for (int i = threadIdx.x; i < words; i += 256) {
-        const int cell = i / 32, col = cell / 8 * 8 + lane / 4, tok = cell % 8 * 8 + lane % 4 * 2;
-        uint32_t q[NT];
-        split<NT>(q, tile[tok * stride + col], tile[(tok + 1) * stride + col]);
-#pragma unroll
-        for (int t = 0; t < NT; ++t) out[t * words + i] = q[t];
     }
 }
 
@@ -306,45 +215,7 @@ __global__ void __launch_bounds__(128) delta_prepare_kernel(const __grid_constan
     }
 }
 
-// ------------------------------------------------------------------ from chunk to chunk
-// A stage of shared memory: a chunk's tiles.
-struct Stage {
-    uint32_t k, q, x, p, v, gates, bytes;
-};
-__host__ __device__ inline Stage stage_of(const DeltaPlan &p, int warps) {
-    Stage s;
-    s.k = 0;
-    s.q = s.k + (uint32_t)p.key_bytes;
-    s.x = s.q + (uint32_t)p.key_bytes;
-    s.p = s.x + kSquare;
-    s.v = s.p + kSquare;
-    s.gates = s.v + (uint32_t)(p.terms * warps * 2048);
-    s.bytes = s.gates + kGateFloats * 4;
-    return s;
-}
-
-struct Tiles {                 // of a chunk and head, in global memory
-    const uint8_t *k, *q, *x, *p, *v, *gates;
-};
-__device__ __forceinline__ Tiles tiles_of(const Args &a, const uint8_t *kept, const uint8_t *values, size_t x, int64_t slot, int h) {
-    const int64_t hk = slot * a.Hk + h / (a.Hv / a.Hk), hv = slot * a.Hv + h;
-    return {kept + a.p.k + hk * a.p.key_bytes, kept + a.p.q + hk * a.p.key_bytes, kept + x + hv * kSquare,
-            kept + a.p.p + hv * kSquare, values + hv * a.p.value_bytes, kept + a.p.gates + hv * kGateFloats * 4};
-}
-// One thread: the chunk's tiles into a stage, of v the `warps` * 16 columns from `tile` * 16 on.
-template <int NT>
-__device__ __forceinline__ void load_stage(const Args &a, const Stage &st, uint32_t smem, uint32_t bar, const Tiles &g, int tile, int warps) {
-    tc::bar_expect(bar, st.bytes);
-    load_bytes(smem + st.k, g.k, (uint32_t)a.p.key_bytes, bar);
-    load_bytes(smem + st.q, g.q, (uint32_t)a.p.key_bytes, bar);
-    load_bytes(smem + st.x, g.x, kSquare, bar);
-    load_bytes(smem + st.p, g.p, kSquare, bar);
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-        load_bytes(smem + st.v + n * warps * 2048, g.v + ((size_t)n * a.p.DVP / 16 + tile) * 2048, warps * 2048, bar);
-    load_bytes(smem + st.gates, g.gates, kGateFloats * 4, bar);
-}
-
+// ------------------------------------------------------------------ gradients of q, k and the gates
 // The pair of values of a lane in block (column block c, token block n) of a slice of `warps` * 16
 // columns: the sum of its terms.
 template <int NT>
@@ -357,321 +228,6 @@ __device__ __forceinline__ float2 pair_of(const uint8_t *tile, size_t term, int 
     }
     return r;
 }
-// A warp's 16 columns and CELLS * 8 places as float32 blocks of 8 x 8, a pair of neighbours a lane:
-// [columns of 8][places of 8].
-constexpr int kWide = 2 * kCell;           // bytes of a float32 block
-template <int CELLS>
-__device__ __forceinline__ void keep_blocks(uint8_t *to, int tile, const float (&v)[CELLS][4]) {
-    const int lane = threadIdx.x & 31;
-#pragma unroll
-    for (int n = 0; n < CELLS; ++n)
-#pragma unroll
-        for (int half = 0; half < 2; ++half)
-            *reinterpret_cast<float2 *>(to + ((tile * 2 + half) * CELLS + n) * kWide + lane * 8) = make_float2(v[n][2 * half], v[n][2 * half + 1]);
-}
-
-// State of 16 columns of v (rows) and all Dk places, from and to [Dk, Dv] float32.
-template <int CELLS>
-__device__ __forceinline__ void read_state(float (&s)[CELLS][4], const float *from, int col, int Dk, int Dv) {
-    const int lane = threadIdx.x & 31, g = lane / 4, t = lane % 4;
-#pragma unroll
-    for (int n = 0; n < CELLS; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int c = col + g + (e >> 1) * 8, d = n * 8 + 2 * t + (e & 1);
-            s[n][e] = from && c < Dv && d < Dk ? from[(int64_t)d * Dv + c] : 0.f;
-        }
-}
-template <int CELLS>
-__device__ __forceinline__ void write_state(const float (&s)[CELLS][4], float *to, int col, int Dk, int Dv) {
-    const int lane = threadIdx.x & 31, g = lane / 4, t = lane % 4;
-#pragma unroll
-    for (int n = 0; n < CELLS; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int c = col + g + (e >> 1) * 8, d = n * 8 + 2 * t + (e & 1);
-            if (c < Dv && d < Dk) to[(int64_t)d * Dv + c] = s[n][e];
-        }
-}
-template <typename T>
-__device__ __forceinline__ void put(T *p, float v);
-template <>
-__device__ __forceinline__ void put<float>(float *p, float v) { *p = v; }
-template <>
-__device__ __forceinline__ void put<__nv_bfloat16>(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
-
-// A block's walk over its sequence's chunks: two stages where they fit, the next chunk's tiles on their
-// way while one is worked on. After a wait that ran out the states are NaN and no more is fetched.
-template <typename T, int DKP, bool KEEP>
-__global__ void __launch_bounds__(kWarps * 32, 1) delta_forward_kernel(const __grid_constant__ Args a, uint8_t *kept, const float *s0, T *o,
-                                                                       float *last, int stages) {
-    constexpr int NT = sizeof(T) == 2 ? 1 : 3, W = DKP / 8, TILE = 64 * DKP * 2, SQ = kSquare / 3;
-    constexpr int FEW = sizeof(T) == 2 ? 2 : 3;        // terms where only a bfloat16 output comes of it
-    extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ __align__(8) uint64_t bars[2];
-    pdl_begin();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, g = lane / 4, t = lane % 4;
-    const int b = blockIdx.x / a.Hv, h = blockIdx.x % a.Hv, tile0 = blockIdx.y * warps, tile = tile0 + warp;
-    const Sequence s = sequence(a, b);
-    const int chunks = (s.length + C - 1) / C;
-    const Stage st = stage_of(a.p, warps);
-    const uint32_t base = tc::smem_addr(smem), bar = tc::smem_addr(bars);
-    if (threadIdx.x == 0) {
-        tc::bar_init(bar, 1);
-        tc::bar_init(bar + 8, 1);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        for (int n = 0; n < min(stages, chunks); ++n)
-            load_stage<NT>(a, st, base + n * st.bytes, bar + 8 * n, tiles_of(a, kept, kept + a.p.v, a.p.xe, s.slot + n, h), tile0, warps);
-    }
-    const int64_t state = ((int64_t)b * a.Hv + h) * a.Dk * a.Dv;
-    float S[W][4];
-    read_state<W>(S, s0 ? s0 + state : nullptr, tile * 16, a.Dk, a.Dv);
-    __syncthreads();
-    bool ok = true;
-    for (int n = 0; n < chunks; ++n) {
-        const int at = n % stages;
-        const int64_t hv = (s.slot + n) * a.Hv + h;
-        if (KEEP) keep_blocks<W>(kept + a.p.s + hv * a.p.state_bytes, tile, S);
-        ok = ok && tc::bar_wait(bar + 8 * at, n / stages & 1);
-        if (!ok)
-#pragma unroll
-            for (int i = 0; i < W; ++i) S[i][0] = S[i][1] = S[i][2] = S[i][3] = __int_as_float(0x7fffffff);
-        const uint8_t *here = smem + at * st.bytes;
-        const uint32_t sk = base + at * st.bytes + st.k, sq = sk + st.q, sx = sk + st.x, sp = sk + st.p;
-        const float *gates = reinterpret_cast<const float *>(here + st.gates);
-        // k S and q S
-        float r[8][4] = {}, out[8][4] = {};
-#pragma unroll
-        for (int ks = 0; ks < W / 2; ++ks) {
-            if (ks * 16 >= a.Dk) break;
-            uint32_t x[3][4];
-            split_left<3>(x, S[2 * ks], S[2 * ks + 1]);
-#pragma unroll
-            for (int p = 0; p < 4; ++p) {
-                uint32_t f[NT][4];
-#pragma unroll
-                for (int m = 0; m < NT; ++m) right_rows(f[m], sk + m * TILE, W, 2 * p, 2 * ks);
-                products<3, NT, 3>(r[2 * p], r[2 * p + 1], x, f);
-#pragma unroll
-                for (int m = 0; m < NT; ++m) right_rows(f[m], sq + m * TILE, W, 2 * p, 2 * ks);
-                products<3, NT, FEW>(out[2 * p], out[2 * p + 1], x, f);
-            }
-        }
-        // v - first k S; the decayed state
-        const float keep = gates[kKeep];
-#pragma unroll
-        for (int i = 0; i < W; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) S[i][e] *= keep;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float2 f = *reinterpret_cast<const float2 *>(gates + kFirst + i * 8 + 2 * t);
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const float2 v = pair_of<NT>(here + st.v, warps * 2048, (warp * 2 + half) * 8 + i);
-                r[i][2 * half] = fmaf(-f.x, r[i][2 * half], v.x);
-                r[i][2 * half + 1] = fmaf(-f.y, r[i][2 * half + 1], v.y);
-                out[i][2 * half] *= f.x;
-                out[i][2 * half + 1] *= f.y;
-            }
-        }
-        float e[8][4] = {};
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-            uint32_t x[3][4];
-            split_left<3>(x, r[2 * ks], r[2 * ks + 1]);
-#pragma unroll
-            for (int p = ks; p < 4; ++p) {
-                uint32_t f[3][4];
-#pragma unroll
-                for (int m = 0; m < 3; ++m) right_rows(f[m], sx + m * SQ, 8, 2 * p, 2 * ks);
-                products<3, 3, 3>(e[2 * p], e[2 * p + 1], x, f);
-            }
-        }
-        if (KEEP) keep_blocks<8>(kept + a.p.e + hv * a.p.kept_bytes, tile, e);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float2 bt = *reinterpret_cast<const float2 *>(gates + kBeta + i * 8 + 2 * t);
-            e[i][0] *= bt.x, e[i][1] *= bt.y, e[i][2] *= bt.x, e[i][3] *= bt.y;
-        }
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-            uint32_t x[3][4];
-            split_left<3>(x, e[2 * ks], e[2 * ks + 1]);
-#pragma unroll
-            for (int p = ks; p < 4; ++p) {
-                uint32_t f[FEW][4];
-#pragma unroll
-                for (int m = 0; m < FEW; ++m) right_rows(f[m], sp + m * SQ, 8, 2 * p, 2 * ks);
-                products<3, FEW, FEW>(out[2 * p], out[2 * p + 1], x, f);
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const float2 re = *reinterpret_cast<const float2 *>(gates + kRest + (2 * ks + i) * 8 + 2 * t);
-                float(&u)[4] = e[2 * ks + i];
-                u[0] *= re.x, u[1] *= re.y, u[2] *= re.x, u[3] *= re.y;
-            }
-            split_left<3>(x, e[2 * ks], e[2 * ks + 1]);
-#pragma unroll
-            for (int p = 0; p < W / 2; ++p) {
-                if (p * 16 >= a.Dk) break;
-                uint32_t f[NT][4];
-#pragma unroll
-                for (int m = 0; m < NT; ++m) right_columns(f[m], sk + m * TILE, W, 2 * ks, 2 * p);
-                products<3, NT, 3>(S[2 * p], S[2 * p + 1], x, f);
-            }
-        }
-        __syncthreads();
-        if (threadIdx.x == 0 && ok && n + stages < chunks)
-            load_stage<NT>(a, st, base + at * st.bytes, bar + 8 * at, tiles_of(a, kept, kept + a.p.v, a.p.xe, s.slot + n + stages, h), tile0, warps);
-        const int left = s.length - n * C;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int col = tile * 16 + g + (j >> 1) * 8, tok = i * 8 + 2 * t + (j & 1);
-                if (col < a.Dv && tok < left)
-                    put(o + ((s.row + (int64_t)(n * C + tok) * s.step) * a.Hv + h) * a.Dv + col, a.scale * out[i][j]);
-            }
-    }
-    if (!ok) let_land();
-    if (KEEP) keep_blocks<W>(kept + a.p.end + ((int64_t)b * a.Hv + h) * a.p.state_bytes, tile, S);
-    if (last) write_state<W>(S, last + state, tile * 16, a.Dk, a.Dv);
-}
-
-template <typename T, int DKP>
-__global__ void __launch_bounds__(kWarps * 32, 1) delta_backward_kernel(const __grid_constant__ Args a, const uint8_t *kept, uint8_t *scratch,
-                                                                        const float *glast, float *gs0, int stages) {
-    constexpr int NT = sizeof(T) == 2 ? 1 : 3, W = DKP / 8, TILE = 64 * DKP * 2, SQ = kSquare / 3;
-    extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ __align__(8) uint64_t bars[2];
-    pdl_begin();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, t = lane % 4;
-    const int b = blockIdx.x / a.Hv, h = blockIdx.x % a.Hv, tile0 = blockIdx.y * warps, tile = tile0 + warp;
-    const Sequence s = sequence(a, b);
-    const int chunks = (s.length + C - 1) / C;
-    const Stage st = stage_of(a.p, warps);
-    const uint32_t base = tc::smem_addr(smem), bar = tc::smem_addr(bars);
-    if (threadIdx.x == 0) {
-        tc::bar_init(bar, 1);
-        tc::bar_init(bar + 8, 1);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        for (int n = 0; n < min(stages, chunks); ++n)
-            load_stage<NT>(a, st, base + n * st.bytes, bar + 8 * n, tiles_of(a, kept, scratch + a.p.go, a.p.xu, s.slot + chunks - 1 - n, h), tile0, warps);
-    }
-    const int64_t state = ((int64_t)b * a.Hv + h) * a.Dk * a.Dv;
-    float D[W][4];
-    read_state<W>(D, glast ? glast + state : nullptr, tile * 16, a.Dk, a.Dv);
-    __syncthreads();
-    bool ok = true;
-    for (int n = 0; n < chunks; ++n) {
-        const int at = n % stages;
-        const int64_t hv = (s.slot + chunks - 1 - n) * a.Hv + h;
-        keep_blocks<W>(scratch + a.p.d + hv * a.p.state_bytes, tile, D);
-        ok = ok && tc::bar_wait(bar + 8 * at, n / stages & 1);
-        if (!ok)
-#pragma unroll
-            for (int i = 0; i < W; ++i) D[i][0] = D[i][1] = D[i][2] = D[i][3] = __int_as_float(0x7fffffff);
-        const uint8_t *here = smem + at * st.bytes, *gob = here + st.v;
-        const uint32_t sk = base + at * st.bytes + st.k, sq = sk + st.q, sx = sk + st.x, sp = sk + st.p;
-        const float *gates = reinterpret_cast<const float *>(here + st.gates);
-        float d[8][4] = {}, r[8][4] = {};
-        // P^T go
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-            uint32_t x[NT][4];
-#pragma unroll
-            for (int m = 0; m < NT; ++m)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    x[m][i] = *reinterpret_cast<const uint32_t *>(gob + m * warps * 2048 + ((warp * 2 + (i & 1)) * 8 + 2 * ks + (i >> 1)) * kCell + lane * 4);
-#pragma unroll
-            for (int p = 0; p <= ks; ++p) {
-                uint32_t f[3][4];
-#pragma unroll
-                for (int m = 0; m < 3; ++m) right_columns(f[m], sp + m * SQ, 8, 2 * ks, 2 * p);
-                products<NT, 3, 3>(d[2 * p], d[2 * p + 1], x, f);
-            }
-        }
-        // k D
-#pragma unroll
-        for (int ks = 0; ks < W / 2; ++ks) {
-            if (ks * 16 >= a.Dk) break;
-            uint32_t x[3][4];
-            split_left<3>(x, D[2 * ks], D[2 * ks + 1]);
-#pragma unroll
-            for (int p = 0; p < 4; ++p) {
-                uint32_t f[NT][4];
-#pragma unroll
-                for (int m = 0; m < NT; ++m) right_rows(f[m], sk + m * TILE, W, 2 * p, 2 * ks);
-                products<3, NT, 3>(r[2 * p], r[2 * p + 1], x, f);
-            }
-        }
-        const float keep = gates[kKeep];
-#pragma unroll
-        for (int i = 0; i < W; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) D[i][e] *= keep;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float2 re = *reinterpret_cast<const float2 *>(gates + kRest + i * 8 + 2 * t);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) d[i][e] = fmaf(e & 1 ? re.y : re.x, r[i][e], a.scale * d[i][e]);
-        }
-        float y[8][4] = {};
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-            uint32_t x[3][4];
-            split_left<3>(x, d[2 * ks], d[2 * ks + 1]);
-#pragma unroll
-            for (int p = 0; p <= ks; ++p) {
-                uint32_t f[3][4];
-#pragma unroll
-                for (int m = 0; m < 3; ++m) right_columns(f[m], sx + m * SQ, 8, 2 * ks, 2 * p);
-                products<3, 3, 3>(y[2 * p], y[2 * p + 1], x, f);
-            }
-        }
-        keep_blocks<8>(scratch + a.p.y + hv * a.p.kept_bytes, tile, y);
-        // q^T (scale first go) - k^T (first b y)
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-            uint32_t x[3][4], z[3][4];
-            float go[2][4];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const float2 fi = *reinterpret_cast<const float2 *>(gates + kFirst + (2 * ks + i) * 8 + 2 * t);
-                const float2 bt = *reinterpret_cast<const float2 *>(gates + kBeta + (2 * ks + i) * 8 + 2 * t);
-                float(&w)[4] = y[2 * ks + i];
-                w[0] *= -fi.x * bt.x, w[1] *= -fi.y * bt.y, w[2] *= -fi.x * bt.x, w[3] *= -fi.y * bt.y;
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const float2 v = pair_of<NT>(gob, warps * 2048, (warp * 2 + half) * 8 + 2 * ks + i);
-                    go[i][2 * half] = a.scale * fi.x * v.x, go[i][2 * half + 1] = a.scale * fi.y * v.y;
-                }
-            }
-            split_left<3>(x, go[0], go[1]);
-            split_left<3>(z, y[2 * ks], y[2 * ks + 1]);
-#pragma unroll
-            for (int p = 0; p < W / 2; ++p) {
-                if (p * 16 >= a.Dk) break;
-                uint32_t f[NT][4];
-#pragma unroll
-                for (int m = 0; m < NT; ++m) right_columns(f[m], sq + m * TILE, W, 2 * ks, 2 * p);
-                products<3, NT, 3>(D[2 * p], D[2 * p + 1], x, f);
-#pragma unroll
-                for (int m = 0; m < NT; ++m) right_columns(f[m], sk + m * TILE, W, 2 * ks, 2 * p);
-                products<3, NT, 3>(D[2 * p], D[2 * p + 1], z, f);
-            }
-        }
-        __syncthreads();
-        if (threadIdx.x == 0 && ok && n + stages < chunks)
-            load_stage<NT>(a, st, base + at * st.bytes, bar + 8 * at, tiles_of(a, kept, scratch + a.p.go, a.p.xu, s.slot + chunks - 1 - n - stages, h), tile0, warps);
-    }
-    if (!ok) let_land();
-    if (gs0) write_state<W>(D, gs0 + state, tile * 16, a.Dk, a.Dv);
-}
-
-// ------------------------------------------------------------------ gradients of q, k and the gates
 // Columns of v that a round takes, and the places of their tiles in a stage.
 constexpr int kRound = 32;
 template <int NT, int DKP>
@@ -1175,21 +731,6 @@ cudaError_t run_step(const Args &a, const void *q, const void *k, const void *v,
 template <typename T>
 bool wide_of(const void *p, int D) { return seq_aligned(p, 16) && D % (16 / (int)sizeof(T)) == 0; }
 
-// Warps of a block that carries states, and how many chunks' tiles fit its shared memory.
-struct Walk {
-    int warps, blocks, stages;
-    size_t smem;
-};
-Walk walk_of(const Args &a) {
-    Walk w;
-    w.warps = a.p.DVP / 16;
-    w.blocks = 1;
-    const size_t stage = stage_of(a.p, w.warps).bytes;
-    w.stages = 2 * stage <= 225 * 1024 ? 2 : 1;
-    w.smem = w.stages * stage;
-    return w;
-}
-
 template <typename T, int DKP>
 cudaError_t run_forward(const Args &a, const void *q, const void *k, const void *v, const float *gate, const float *beta, const float *s0, void *o,
                         float *last, uint8_t *kept, bool keep, cudaStream_t s, int *launches) {
@@ -1203,15 +744,9 @@ cudaError_t run_forward(const Args &a, const void *q, const void *k, const void 
         if (e == cudaSuccess)
             e = keep ? seq_launch(delta_prepare_kernel<T, DKP, true>, grid, 128, smem, s, 1, a, (const T *)q, (const T *)k, gate, beta, kept, wide)
                      : seq_launch(delta_prepare_kernel<T, DKP, false>, grid, 128, smem, s, 1, a, (const T *)q, (const T *)k, gate, beta, kept, wide);
-        if (e == cudaSuccess) e = seq_launch(delta_turn_kernel<T>, grid, 256, 0, s, 1, a, (const T *)v, kept + a.p.v, wide_of<T>(v, a.Dv));
-        *launches += 2;
+        ++*launches;
     }
-    const Walk w = walk_of(a);
-    const dim3 grid((unsigned)(a.B * a.Hv), (unsigned)w.blocks);
-    if (e == cudaSuccess) e = keep ? room(delta_forward_kernel<T, DKP, true>, w.smem) : room(delta_forward_kernel<T, DKP, false>, w.smem);
-    if (e == cudaSuccess)
-        e = keep ? seq_launch(delta_forward_kernel<T, DKP, true>, grid, w.warps * 32, w.smem, s, 1, a, kept, s0, (T *)o, last, w.stages)
-                 : seq_launch(delta_forward_kernel<T, DKP, false>, grid, w.warps * 32, w.smem, s, 1, a, kept, s0, (T *)o, last, w.stages);
+    if (e == cudaSuccess) e = delta_walk_forward(a, NT == 1, v, s0, o, last, kept, keep, s);
     ++*launches;
     return e;
 }
@@ -1221,15 +756,7 @@ cudaError_t run_backward(const Args &a, const void *go, const float *glast, cons
                          float *gbeta, float *gs0, uint8_t *scratch, cudaStream_t s, int *launches) {
     constexpr int NT = sizeof(T) == 2 ? 1 : 3;
     const dim3 chunks((unsigned)a.p.slots, (unsigned)a.Hv);
-    cudaError_t e = cudaSuccess;
-    if (a.p.slots) {
-        e = seq_launch(delta_turn_kernel<T>, chunks, 256, 0, s, 1, a, (const T *)go, scratch + a.p.go, wide_of<T>(go, a.Dv));
-        ++*launches;
-    }
-    const Walk w = walk_of(a);
-    if (e == cudaSuccess) e = room(delta_backward_kernel<T, DKP>, w.smem);
-    if (e == cudaSuccess)
-        e = seq_launch(delta_backward_kernel<T, DKP>, dim3((unsigned)(a.B * a.Hv), (unsigned)w.blocks), w.warps * 32, w.smem, s, 1, a, kept, scratch, glast, gs0, w.stages);
+    cudaError_t e = delta_walk_backward(a, NT == 1, go, glast, kept, scratch, gs0, s);
     ++*launches;
     if (!a.p.slots || e != cudaSuccess) return e;
     constexpr size_t smem = Parts<NT, DKP>::end;

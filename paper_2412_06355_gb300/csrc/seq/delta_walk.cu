@@ -1,0 +1,489 @@
+// The states of the gated delta rule, and their gradients, from chunk to chunk: what has an order. The formulas and
+// what happens before and after stand in delta.cu.
+//
+// A block has one head of one sequence. Columns of v do not meet, so the products are turned: 128 lanes of tensor
+// memory are the columns, and everything a chunk needs comes from three rounds of tcgen05 products (forward: k S and
+// q S; e; P u and k^T (rest u). backward: P^T go and k D; y; q^T go and k^T y), whose left factors the threads write to
+// tensor memory as bfloat16 terms and whose right factors are the chunk's tiles in shared memory. The state itself
+// stays in registers as float32: two threads a column, half of the places each. Eight warps compute, a ninth fetches
+// tiles and issues products; in between they wait for each other on mbarriers.
+//
+// What bounds it is the chain: a chunk is three rounds of (registers -> tensor memory -> products -> registers), and
+// a block has all of an SM's tensor memory, so that 128 sequences and heads are 128 SMs at work.
+#include <algorithm>
+
+#include "delta_common.cuh"
+#include "tc_one.cuh"
+
+namespace dendsn {
+namespace delta {
+namespace {
+
+constexpr int kThreads = 384;              // eight warps that compute, the one that issues, and three that only share
+                                           // its registers out (168 each at the launch: 40 and 232 after)
+constexpr uint32_t kColumns = 512;         // of tensor memory: all there are
+
+// A stage of shared memory: a chunk's tiles.
+struct Stage {
+    uint32_t k, q, x, p, gates, bytes;
+};
+__host__ __device__ inline Stage stage_of(const DeltaPlan &p) {
+    Stage s;
+    s.k = 0;
+    s.q = s.k + (uint32_t)p.key_bytes;
+    s.x = s.q + (uint32_t)p.key_bytes;
+    s.p = s.x + kSquare;
+    s.gates = s.p + kSquare;
+    s.bytes = s.gates + kGateFloats * 4;
+    return s;
+}
+// One thread: the chunk's tiles into a stage.
+__device__ __forceinline__ void load_stage(const Args &a, const Stage &st, uint32_t smem, uint32_t bar, const uint8_t *kept, size_t x, int64_t slot, int h) {
+    const int64_t hk = slot * a.Hk + h / (a.Hv / a.Hk), hv = slot * a.Hv + h;
+    tc::bar_expect(bar, st.bytes);
+    load_bytes(smem + st.k, kept + a.p.k + hk * a.p.key_bytes, (uint32_t)a.p.key_bytes, bar);
+    load_bytes(smem + st.q, kept + a.p.q + hk * a.p.key_bytes, (uint32_t)a.p.key_bytes, bar);
+    load_bytes(smem + st.x, kept + x + hv * kSquare, kSquare, bar);
+    load_bytes(smem + st.p, kept + a.p.p + hv * kSquare, kSquare, bar);
+    load_bytes(smem + st.gates, kept + a.p.gates + hv * kGateFloats * 4, kGateFloats * 4, bar);
+}
+
+// 32 tokens of one column of v or go, fetched ahead of their use.
+template <typename T>
+struct Ahead;
+template <>
+struct Ahead<float> {
+    float r[32];
+    __device__ __forceinline__ void set(int i, const float *p) { r[i] = p ? *p : 0.f; }
+    __device__ __forceinline__ float get(int i) const { return r[i]; }
+};
+template <>
+struct Ahead<__nv_bfloat16> {
+    uint16_t r[32];
+    __device__ __forceinline__ void set(int i, const __nv_bfloat16 *p) { r[i] = p ? *reinterpret_cast<const uint16_t *>(p) : (uint16_t)0; }
+    __device__ __forceinline__ float get(int i) const { return __uint_as_float((uint32_t)r[i] << 16); }
+};
+template <typename T>
+__device__ __forceinline__ void fetch(Ahead<T> &x, const T *from, int64_t stride, int left) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) x.set(i, i < left ? from + i * stride : nullptr);
+}
+
+// Terms of 2 * W values as left factors: `to` and each further 16 columns take 32 values; terms lie `term` apart.
+template <int N, int W>
+__device__ __forceinline__ void to_lanes(uint32_t to, uint32_t term, const float (&v)[2 * W]) {
+#pragma unroll
+    for (int part = 0; part < W / 16; ++part) {
+        uint32_t q[N][16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            uint32_t t[N];
+            split<N>(t, v[part * 32 + 2 * i], v[part * 32 + 2 * i + 1]);
+#pragma unroll
+            for (int n = 0; n < N; ++n) q[n][i] = t[n];
+        }
+#pragma unroll
+        for (int n = 0; n < N; ++n) tc::tmem_store(to + n * term + part * 16, q[n]);
+    }
+}
+// A warp has written its left factors: its lane 0 arrives for it.
+__device__ __forceinline__ void ready(uint32_t bar) {
+    tc::tmem_stored();
+    tc::fence_before_sync();
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) tc::bar_arrive(bar);
+}
+// 32 values a thread of row `row` as float32 blocks [columns of 8][tokens (or places) of 8], `width` blocks a row.
+template <int N>
+__device__ __forceinline__ void keep_row(uint8_t *to, int row, int width, int first, const float (&v)[N]) {
+#pragma unroll
+    for (int n = 0; n < N / 8; ++n) {
+        uint32_t q[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) q[e] = __float_as_uint(v[n * 8 + e]);
+        tc::store32(to + ((size_t)(row / 8) * width + first + n) * kWide + (row & 7) * 32, q);
+    }
+}
+// 32 tokens of a column as tiles of bfloat16 terms [term][columns of 8][tokens of 8].
+template <int NT, typename T>
+__device__ __forceinline__ void keep_values(uint8_t *to, size_t term, int row, int first, const Ahead<T> &x) {
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+        uint32_t q[4][NT];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) split<NT>(q[i], x.get(n * 8 + 2 * i), x.get(n * 8 + 2 * i + 1));
+#pragma unroll
+        for (int m = 0; m < NT; ++m)
+            *reinterpret_cast<uint4 *>(to + m * term + ((size_t)(row / 8) * 8 + first + n) * kCell + (row & 7) * 16) = make_uint4(q[0][m], q[1][m], q[2][m], q[3][m]);
+    }
+}
+
+// Products of NA terms in tensor memory (STEPS blocks of 16 summed places, 8 columns each) and NB terms in shared
+// memory, those whose terms' numbers add up to less than KEEP, the smallest first. TURNED: the right factor's rows
+// run along the summed index, else along the other one. `width`: blocks of a row. TRI: of a lower triangle's rows only
+// those from the step on (1), of its columns only those up to the step (2).
+template <int NA, int NB, int KEEP, int STEPS, int N, bool TURNED, int TRI>
+__device__ __forceinline__ void issue(uint32_t d, uint32_t a, uint32_t aterm, uint32_t b, uint32_t bterm, int width, bool add) {
+#pragma unroll
+    for (int sum = KEEP - 1; sum >= 0; --sum)
+#pragma unroll
+        for (int i = 0; i < NA; ++i) {
+            const int j = sum - i;
+            if (j < 0 || j >= NB) continue;
+#pragma unroll
+            for (int n = 0; n < STEPS; ++n) {
+                const int s = TRI == 2 ? STEPS - 1 - n : n;
+                const int from = TRI == 1 ? 16 * s : 0, count = TRI == 1 ? N - 16 * s : TRI == 2 ? 16 * (s + 1) : N;
+                const uint32_t at = b + j * bterm + (TURNED ? 2 * s * width : from / 8 * width + 2 * s) * kCell;
+                tc::mma_lanes(d + from, a + i * aterm + 8 * s, TURNED ? tc::blocks(at, width * kCell, kCell) : tc::blocks(at, kCell, width * kCell),
+                              tc::product_of(128, count, false, TURNED), add);
+                add = true;
+            }
+        }
+}
+
+struct Bars {
+    uint64_t tiles[2], first, second, third, one, two, three, four;
+};
+struct Waits {
+    bool ok;
+    __device__ __forceinline__ void operator()(uint64_t &bar, uint32_t phase) { ok = ok && tc::bar_wait(tc::smem_addr(&bar), phase & 1); }
+};
+
+// What both walks begin and end with.
+__device__ __forceinline__ uint32_t begin(Bars &bars, uint32_t &where) {
+    if (threadIdx.x == 0) {
+        uint64_t *all[] = {&bars.tiles[0], &bars.tiles[1], &bars.one, &bars.two, &bars.three, &bars.four};
+        for (uint64_t *b : all) tc::bar_init(tc::smem_addr(b), 1);
+        tc::bar_init(tc::smem_addr(&bars.first), 8);
+        tc::bar_init(tc::smem_addr(&bars.second), 8);
+        tc::bar_init(tc::smem_addr(&bars.third), 8);
+        tc::bar_init_fence();
+    }
+    if (threadIdx.x < 32) tc::tmem_alloc_one(tc::smem_addr(&where), kColumns);
+    tc::fence_before_sync();
+    __syncthreads();
+    tc::fence_after_sync();
+    return where;
+}
+__device__ __forceinline__ void finish(bool ok, uint32_t tmem) {
+    if (!ok) let_land();
+    tc::fence_before_sync();
+    __syncthreads();
+    if (threadIdx.x < 32) tc::tmem_free_one(tmem, kColumns);
+}
+
+// Columns of tensor memory, forward: the state's terms, then those of rest u | k S and q S, then the state's change |
+// terms of v - first k S, then of u | e, then P u.
+constexpr uint32_t kState = 0, kSeen = 192, kError = 320, kOut = 416;
+
+template <typename T, int DKP, bool KEEP>
+__global__ void __launch_bounds__(kThreads, 1) delta_forward_kernel(const __grid_constant__ Args a, const T *v, const float *s0, T *o, float *last,
+                                                                    uint8_t *kept, int stages) {
+    constexpr int NT = sizeof(T) == 2 ? 1 : 3, W = DKP / 8, TILE = 64 * DKP * 2, SQ = kSquare / 3, HALF = DKP / 2;
+    constexpr int FEW = sizeof(T) == 2 ? 2 : 3;        // terms where only a bfloat16 output comes of it
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ Bars bars;
+    __shared__ uint32_t where;
+    pdl_begin();
+    const int b = blockIdx.x / a.Hv, h = blockIdx.x % a.Hv, warp = threadIdx.x >> 5;
+    const Sequence s = sequence(a, b);
+    const int chunks = (s.length + C - 1) / C;
+    const Stage st = stage_of(a.p);
+    const uint32_t base = tc::smem_addr(smem), tmem = begin(bars, where);
+    Waits wait{true};
+    if (warp >= 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        if (threadIdx.x == 256) {
+            const uint32_t tiles = tc::smem_addr(bars.tiles);
+            for (int n = 0; n < min(stages, chunks); ++n) load_stage(a, st, base + n * st.bytes, tiles + 8 * n, kept, a.p.xe, s.slot + n, h);
+            for (int n = 0; n < chunks; ++n) {
+                const uint32_t here = base + n % stages * st.bytes, k = here + st.k, q = here + st.q, x = here + st.x, p = here + st.p;
+                wait(bars.tiles[n % stages], n / stages);
+                wait(bars.first, n);
+                if (!wait.ok) break;
+                tc::fence_after_sync();
+                issue<3, NT, 3, DKP / 16, 64, false, 0>(tmem + kSeen, tmem + kState, HALF, k, TILE, W, false);
+                tc::commit_one(tc::smem_addr(&bars.one));
+                issue<3, NT, FEW, DKP / 16, 64, false, 0>(tmem + kSeen + 64, tmem + kState, HALF, q, TILE, W, false);
+                wait(bars.second, n);
+                if (!wait.ok) break;
+                tc::fence_after_sync();
+                issue<3, 3, 3, 4, 64, false, 1>(tmem + kOut, tmem + kError, 32, x, SQ, 8, false);
+                tc::commit_one(tc::smem_addr(&bars.two));
+                wait(bars.third, n);
+                if (!wait.ok) break;
+                tc::fence_after_sync();
+                issue<3, NT, 3, 4, DKP, true, 0>(tmem + kSeen, tmem + kState, 32, k, TILE, W, false);
+                tc::commit_one(tc::smem_addr(&bars.three));
+                issue<3, FEW, FEW, 4, 64, false, 1>(tmem + kOut, tmem + kError, 32, p, SQ, 8, false);
+                tc::commit_one(tc::smem_addr(&bars.four));
+                if (n + stages < chunks) {             // the stage is free when all that reads it is done
+                    wait(bars.four, n);
+                    if (!wait.ok) break;
+                    load_stage(a, st, here, tiles + 8 * (n % stages), kept, a.p.xe, s.slot + n + stages, h);
+                }
+            }
+        }
+        __syncwarp();
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+        const int half = warp >> 2, lane = threadIdx.x & 31, col = (warp & 3) * 32 + lane, tok0 = half * 32;
+        const uint32_t mine = tmem + ((uint32_t)(warp & 3) << 21);          // this warp's lanes
+        const bool here = col < a.Dv;
+        const int64_t state = ((int64_t)b * a.Hv + h) * a.Dk * a.Dv, stride = s.step * a.Hv * a.Dv;
+        float S[HALF];
+#pragma unroll
+        for (int i = 0; i < HALF; ++i) {
+            const int d = half * HALF + i;
+            S[i] = s0 && here && d < a.Dk ? s0[state + (int64_t)d * a.Dv + col] : 0.f;
+        }
+        const int64_t first = ((s.row + tok0 * s.step) * a.Hv + h) * a.Dv + col;
+        Ahead<T> ahead;
+        fetch(ahead, v + first, stride, here ? s.length - tok0 : 0);
+        float out[32];
+        auto put_out = [&](int n) {        // o of chunk n: what of it lies in registers and P u
+            wait(bars.four, n);
+            float u[32];
+            tc::fence_after_sync();
+            tc::tmem_load(u, mine + kOut + tok0);
+            if (!wait.ok) u[0] = __int_as_float(0x7fffffff);
+            T *to = o + first + (int64_t)n * C * stride;
+            const int left = here ? s.length - n * C - tok0 : 0;
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (i < left) put(to + i * stride, wait.ok ? a.scale * (out[i] + u[i]) : u[0]);
+        };
+        for (int n = 0; n < chunks; ++n) {
+            const int64_t hv = (s.slot + n) * a.Hv + h;
+            to_lanes<3, HALF / 2>(mine + kState + half * (HALF / 2), HALF, S);
+            ready(tc::smem_addr(&bars.first));
+            if (n) put_out(n - 1);
+            if (KEEP && col < a.p.DVP) {
+                keep_row(kept + a.p.s + hv * a.p.state_bytes, col, W, half * (W / 2), S);
+                keep_values<NT>(kept + a.p.v + hv * a.p.value_bytes, (size_t)C * a.p.DVP * 2, col, half * 4, ahead);
+            }
+            wait(bars.tiles[n % stages], n / stages);
+            const float *gates = reinterpret_cast<const float *>(smem + n % stages * st.bytes + st.gates);
+            const float keep = gates[kKeep];
+            wait(bars.one, n);
+            tc::fence_after_sync();
+            float r[32];
+            tc::tmem_load(r, mine + kSeen + tok0);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) r[i] = fmaf(-gates[kFirst + tok0 + i], r[i], ahead.get(i));
+            to_lanes<3, 16>(mine + kError + half * 16, 32, r);
+            ready(tc::smem_addr(&bars.second));
+            fetch(ahead, v + first + (int64_t)(n + 1) * C * stride, stride, here ? s.length - (n + 1) * C - tok0 : 0);
+            wait(bars.two, n);
+            tc::fence_after_sync();
+            tc::tmem_load(out, mine + kSeen + 64 + tok0);
+            tc::tmem_load(r, mine + kOut + tok0);
+            float u[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                u[i] = r[i] * gates[kBeta + tok0 + i];
+                out[i] *= gates[kFirst + tok0 + i];
+            }
+            to_lanes<3, 16>(mine + kError + half * 16, 32, u);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) u[i] *= gates[kRest + tok0 + i];
+            to_lanes<3, 16>(mine + kState + half * 16, 32, u);
+            ready(tc::smem_addr(&bars.third));
+            if (KEEP && col < a.p.DVP) keep_row(kept + a.p.e + hv * a.p.kept_bytes, col, 8, half * 4, r);
+            wait(bars.three, n);
+            tc::fence_after_sync();
+#pragma unroll
+            for (int part = 0; part < HALF / 32; ++part) {
+                float d[32];
+                tc::tmem_load(d, mine + kSeen + half * HALF + part * 32);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) S[part * 32 + i] = fmaf(keep, S[part * 32 + i], d[i]);
+            }
+            if (!wait.ok)
+#pragma unroll
+                for (int i = 0; i < HALF; ++i) S[i] = __int_as_float(0x7fffffff);
+        }
+        if (chunks) put_out(chunks - 1);
+        if (KEEP && col < a.p.DVP) keep_row(kept + a.p.end + ((int64_t)b * a.Hv + h) * a.p.state_bytes, col, W, half * (W / 2), S);
+        if (last && here)
+#pragma unroll
+            for (int i = 0; i < HALF; ++i) {
+                const int d = half * HALF + i;
+                if (d < a.Dk) last[state + (int64_t)d * a.Dv + col] = S[i];
+            }
+    }
+    finish(wait.ok, tmem);
+}
+
+// Columns of tensor memory, backward: terms of the state's gradient, then (from the same place) those of scale first
+// go | those of go | of d, then of -first b y | k D, then y | P^T go. The change of the state's gradient: q's part in
+// the place of its terms' last third and of go's terms, k's where y and P^T go were, when these are done with.
+// (Two sums: the matrix instruction cuts off where it should round, a little more with every 16 summed places.)
+constexpr uint32_t kGrad = 0, kGo = 192, kD = 288, kY = 384, kPg = 448, kChange = 96;
+
+template <typename T, int DKP>
+__global__ void __launch_bounds__(kThreads, 1) delta_backward_kernel(const __grid_constant__ Args a, const T *go, const uint8_t *kept, uint8_t *scratch,
+                                                                     const float *glast, float *gs0, int stages) {
+    constexpr int NT = sizeof(T) == 2 ? 1 : 3, W = DKP / 8, TILE = 64 * DKP * 2, SQ = kSquare / 3, HALF = DKP / 2;
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ Bars bars;
+    __shared__ uint32_t where;
+    pdl_begin();
+    const int b = blockIdx.x / a.Hv, h = blockIdx.x % a.Hv, warp = threadIdx.x >> 5;
+    const Sequence s = sequence(a, b);
+    const int chunks = (s.length + C - 1) / C;
+    const Stage st = stage_of(a.p);
+    const uint32_t base = tc::smem_addr(smem), tmem = begin(bars, where);
+    Waits wait{true};
+    if (warp >= 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        if (threadIdx.x == 256) {
+            const uint32_t tiles = tc::smem_addr(bars.tiles);
+            for (int n = 0; n < min(stages, chunks); ++n) load_stage(a, st, base + n * st.bytes, tiles + 8 * n, kept, a.p.xu, s.slot + chunks - 1 - n, h);
+            for (int n = 0; n < chunks; ++n) {
+                const uint32_t here = base + n % stages * st.bytes, k = here + st.k, q = here + st.q, x = here + st.x, p = here + st.p;
+                wait(bars.tiles[n % stages], n / stages);
+                wait(bars.first, n);
+                if (!wait.ok) break;
+                tc::fence_after_sync();
+                issue<3, NT, 3, DKP / 16, 64, false, 0>(tmem + kY, tmem + kGrad, HALF, k, TILE, W, false);
+                issue<NT, 3, 3, 4, 64, true, 2>(tmem + kPg, tmem + kGo, 32, p, SQ, 8, false);
+                tc::commit_one(tc::smem_addr(&bars.one));
+                wait(bars.second, n);
+                if (!wait.ok) break;
+                tc::fence_after_sync();
+                issue<3, 3, 3, 4, 64, true, 2>(tmem + kY, tmem + kD, 32, x, SQ, 8, false);
+                tc::commit_one(tc::smem_addr(&bars.two));
+                issue<3, NT, 3, 4, DKP, true, 0>(tmem + kChange, tmem + kGrad, 32, q, TILE, W, false);
+                wait(bars.third, n);
+                if (!wait.ok) break;
+                tc::fence_after_sync();
+                issue<3, NT, 3, 4, DKP, true, 0>(tmem + kY, tmem + kD, 32, k, TILE, W, false);
+                tc::commit_one(tc::smem_addr(&bars.three));
+                if (n + stages < chunks) {
+                    wait(bars.three, n);
+                    if (!wait.ok) break;
+                    load_stage(a, st, here, tiles + 8 * (n % stages), kept, a.p.xu, s.slot + chunks - 1 - n - stages, h);
+                }
+            }
+        }
+        __syncwarp();
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+        const int half = warp >> 2, lane = threadIdx.x & 31, col = (warp & 3) * 32 + lane, tok0 = half * 32;
+        const uint32_t mine = tmem + ((uint32_t)(warp & 3) << 21);
+        const bool here = col < a.Dv;
+        const int64_t state = ((int64_t)b * a.Hv + h) * a.Dk * a.Dv, stride = s.step * a.Hv * a.Dv;
+        const int64_t first = ((s.row + tok0 * s.step) * a.Hv + h) * a.Dv + col;
+        float D[HALF];
+#pragma unroll
+        for (int i = 0; i < HALF; ++i) {
+            const int d = half * HALF + i;
+            D[i] = glast && here && d < a.Dk ? glast[state + (int64_t)d * a.Dv + col] : 0.f;
+        }
+        Ahead<T> ahead;
+        fetch(ahead, go + first + (int64_t)(chunks - 1) * C * stride, stride, here && chunks ? s.length - (chunks - 1) * C - tok0 : 0);
+        for (int n = 0; n < chunks; ++n) {
+            const int chunk = chunks - 1 - n;
+            const int64_t hv = (s.slot + chunk) * a.Hv + h;
+            to_lanes<3, HALF / 2>(mine + kGrad + half * (HALF / 2), HALF, D);
+            float g[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) g[i] = ahead.get(i);
+            to_lanes<NT, 16>(mine + kGo + half * 16, 32, g);
+            ready(tc::smem_addr(&bars.first));
+            if (col < a.p.DVP) {
+                keep_row(scratch + a.p.d + hv * a.p.state_bytes, col, W, half * (W / 2), D);
+                keep_values<NT>(scratch + a.p.go + hv * a.p.value_bytes, (size_t)C * a.p.DVP * 2, col, half * 4, ahead);
+            }
+            if (n + 1 < chunks) fetch(ahead, go + first + (int64_t)(chunk - 1) * C * stride, stride, here ? 32 : 0);
+            wait(bars.tiles[n % stages], n / stages);
+            const float *gates = reinterpret_cast<const float *>(smem + n % stages * st.bytes + st.gates);
+            const float keep = gates[kKeep];
+            wait(bars.one, n);
+            tc::fence_after_sync();
+            float r[32], d[32];
+            tc::tmem_load(r, mine + kY + tok0);
+            tc::tmem_load(d, mine + kPg + tok0);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                d[i] = fmaf(gates[kRest + tok0 + i], r[i], a.scale * d[i]);
+                g[i] *= a.scale * gates[kFirst + tok0 + i];
+            }
+            to_lanes<3, 16>(mine + kD + half * 16, 32, d);
+            to_lanes<3, 16>(mine + kGrad + half * 16, 32, g);
+            ready(tc::smem_addr(&bars.second));
+            wait(bars.two, n);
+            tc::fence_after_sync();
+            tc::tmem_load(r, mine + kY + tok0);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) d[i] = r[i] * (-gates[kFirst + tok0 + i] * gates[kBeta + tok0 + i]);
+            to_lanes<3, 16>(mine + kD + half * 16, 32, d);
+            ready(tc::smem_addr(&bars.third));
+            if (col < a.p.DVP) keep_row(scratch + a.p.y + hv * a.p.kept_bytes, col, 8, half * 4, r);
+            wait(bars.three, n);
+            tc::fence_after_sync();
+#pragma unroll
+            for (int part = 0; part < HALF / 32; ++part) {
+                tc::tmem_load(r, mine + kChange + half * HALF + part * 32);
+                tc::tmem_load(d, mine + kY + half * HALF + part * 32);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) D[part * 32 + i] = fmaf(keep, D[part * 32 + i], r[i] + d[i]);
+            }
+            if (!wait.ok)
+#pragma unroll
+                for (int i = 0; i < HALF; ++i) D[i] = __int_as_float(0x7fffffff);
+            // the other warp of these lanes has read its half before terms are written over it
+            asm volatile("bar.sync %0, 64;" ::"r"(1 + (warp & 3)) : "memory");
+        }
+        if (gs0 && here)
+#pragma unroll
+            for (int i = 0; i < HALF; ++i) {
+                const int d = half * HALF + i;
+                if (d < a.Dk) gs0[state + (int64_t)d * a.Dv + col] = D[i];
+            }
+    }
+    finish(wait.ok, tmem);
+}
+
+// One or two stages of shared memory.
+int stages_of(const Args &a) { return 2 * stage_of(a.p).bytes <= 225 * 1024 ? 2 : 1; }
+
+template <typename K, typename... A>
+cudaError_t walk(K kernel, const Args &a, cudaStream_t s, A... args) {
+    const size_t smem = (size_t)stages_of(a) * stage_of(a.p).bytes;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    return e != cudaSuccess ? e : seq_launch(kernel, dim3((unsigned)(a.B * a.Hv)), kThreads, smem, s, 1, a, args..., stages_of(a));
+}
+template <typename T, int DKP>
+cudaError_t forward(const Args &a, const void *v, const float *s0, void *o, float *last, uint8_t *kept, bool keep, cudaStream_t s) {
+    return keep ? walk(delta_forward_kernel<T, DKP, true>, a, s, (const T *)v, s0, (T *)o, last, kept)
+                : walk(delta_forward_kernel<T, DKP, false>, a, s, (const T *)v, s0, (T *)o, last, kept);
+}
+
+}  // namespace
+}  // namespace delta
+
+cudaError_t delta_walk_forward(const delta::Args &a, bool bf16, const void *v, const float *s0, void *o, float *last, uint8_t *kept, bool keep,
+                               cudaStream_t s) {
+    using namespace delta;
+    auto go = [&](auto run) { return run(a, v, s0, o, last, kept, keep, s); };
+    return bf16 ? (a.p.DKP == 64 ? go(forward<__nv_bfloat16, 64>) : go(forward<__nv_bfloat16, 128>))
+                : (a.p.DKP == 64 ? go(forward<float, 64>) : go(forward<float, 128>));
+}
+
+cudaError_t delta_walk_backward(const delta::Args &a, bool bf16, const void *go, const float *glast, const uint8_t *kept, uint8_t *scratch,
+                                float *gs0, cudaStream_t s) {
+    using namespace delta;
+    if (bf16) {
+        const __nv_bfloat16 *g = static_cast<const __nv_bfloat16 *>(go);
+        return a.p.DKP == 64 ? walk(delta_backward_kernel<__nv_bfloat16, 64>, a, s, g, kept, scratch, glast, gs0)
+                             : walk(delta_backward_kernel<__nv_bfloat16, 128>, a, s, g, kept, scratch, glast, gs0);
+    }
+    const float *g = static_cast<const float *>(go);
+    return a.p.DKP == 64 ? walk(delta_backward_kernel<float, 64>, a, s, g, kept, scratch, glast, gs0)
+                         : walk(delta_backward_kernel<float, 128>, a, s, g, kept, scratch, glast, gs0);
+}
+
+}  // namespace dendsn

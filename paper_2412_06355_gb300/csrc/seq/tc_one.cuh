@@ -1,0 +1,50 @@
+// tcgen05 in a block of its own (cta_group::1): products of 128 rows whose left factor lies in tensor memory, or in
+// shared memory, and whose right factor lies in shared memory as 8 x 8 blocks (fragments.cuh) without a swizzle.
+#pragma once
+
+#include "fragments.cuh"
+
+namespace dendsn {
+namespace tc {
+
+__device__ __forceinline__ void tmem_alloc_one(uint32_t dst, uint32_t cols) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst), "r"(cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+}
+__device__ __forceinline__ void tmem_free_one(uint32_t addr, uint32_t cols) {
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols));
+}
+// Left factor in tensor memory: a lane a row, a column two neighbours of the summed index.
+__device__ __forceinline__ void mma_lanes(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc),
+                 "r"((uint32_t)add) : "memory");
+}
+__device__ __forceinline__ void mma_tiles(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc),
+                 "r"((uint32_t)add) : "memory");
+}
+// Arrives at `bar` once the products this thread issued so far are done.
+__device__ __forceinline__ void commit_one(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// A tile of 8 x 8 blocks as an operand. `summed`: bytes between blocks along the summed index; `other`: along the other
+// one. Which of the two runs along a block's 16-byte rows is the instruction's to say (product_of).
+__device__ __forceinline__ uint64_t blocks(uint32_t addr, uint32_t summed, uint32_t other) {
+    return (uint64_t)((addr >> 4) & 0x3fff) | (uint64_t)(summed >> 4) << 16 | (uint64_t)(other >> 4) << 32 | 1ull << 46;
+}
+// 16 or 32 columns of this warp's 32 lanes; tmem_stored waits for all of them.
+__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&v)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+                 "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+                 ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
+                   "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
+}
+__device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+}  // namespace tc
+}  // namespace dendsn

@@ -2,12 +2,14 @@
 
 Tolerances. With keys of length up to 1, beta in [0, 1] and gates up to 0 a token's step does not lengthen
 the state, so errors do not grow along a sequence. Each output is at the end of a chain of at most six
-products (k S, the inverse, the state, q S, and the two of the gradient), each of which is off by a few
-roundings: 2^-24 for what three terms leave out, 2^-24 for each of its up to four partial sums of an
-output. Taken as independent that is below 16 U32 in norm for a chain; twice that for the gates, whose
-gradient is a difference of sums. Element by element no value is off by more than 16 times its tensor's
-share of that. Half a step more where the output is rounded to bfloat16; and the gradients of bfloat16 q
-and k come of factors in two terms (2^-17 each, 2^-16 together).
+products (k S, the inverse, the state, q S, and the two of the gradient). Three terms leave 2^-24 of a
+product. The matrix instruction adds 16 places at a time and cuts the sum off instead of rounding it: half
+of 2^-23 on average, always toward zero, so the steps of a product add up: 4 U32 for 64 places, 8 U32 for
+128. A state takes in k S (8), the inverse (4) and its own product (4): 16 U32; what is read from it (q S,
+or the gradients' sums over v) another 8, the chunk's own square matrices 4 and what three terms leave 4:
+32 U32 in norm for a chain. Element by element no value is off by more than 16 times its tensor's share of
+that. Half a step more where the output is rounded to bfloat16; and the gradients of bfloat16 q and k come
+of factors in two terms (2^-17 each, 2^-16 together).
 
 A gate's gradient is, by definition of how it is formed, a difference of sums over the rest of its chunk:
 <D, S'> + sum of (q . gq - v . gv). Each factor in it is off by CHAIN of its own norm, whatever the
@@ -22,7 +24,7 @@ from paper_2412_06355_gb300 import DeltaFunction, binding
 
 pytestmark = pytest.mark.gpu
 DT = {"f32": torch.float32, "bf16": torch.bfloat16}
-CHAIN = 16 * U32
+CHAIN = 32 * U32
 
 
 @pytest.fixture(scope="module", autouse=True)
