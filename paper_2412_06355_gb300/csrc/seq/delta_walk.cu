@@ -5,8 +5,8 @@
 // memory are the columns, and everything a chunk needs comes from three rounds of tcgen05 products (forward: k S and
 // q S; e; P u and k^T (rest u). backward: P^T go and k D; y; q^T go and k^T y), whose left factors the threads write to
 // tensor memory as bfloat16 terms and whose right factors are the chunk's tiles in shared memory. The state itself
-// stays in registers as float32: two threads a column, half of the places each. Eight warps compute, a ninth fetches
-// tiles and issues products; in between they wait for each other on mbarriers.
+// stays in registers as float32: four threads a column, a quarter of the places each. A thread of the first warp
+// fetches tiles and issues products; in between the warps wait for each other on mbarriers.
 //
 // What bounds it is the chain: a chunk is three rounds of (registers -> tensor memory -> products -> registers), and
 // a block has all of an SM's tensor memory, so that 128 sequences and heads are 128 SMs at work.
@@ -19,8 +19,9 @@ namespace dendsn {
 namespace delta {
 namespace {
 
-constexpr int kThreads = 384;              // eight warps that compute, the one that issues, and three that only share
-                                           // its registers out (168 each at the launch: 40 and 232 after)
+constexpr int kWarps = 16, kThreads = kWarps * 32;
+constexpr int kParts = kWarps / 4;         // threads of a column of v
+constexpr int kTokens = C / kParts;        // tokens of a thread
 constexpr uint32_t kColumns = 512;         // of tensor memory: all there are
 
 // A stage of shared memory: a chunk's tiles.
@@ -48,82 +49,120 @@ __device__ __forceinline__ void load_stage(const Args &a, const Stage &st, uint3
     load_bytes(smem + st.gates, kept + a.p.gates + hv * kGateFloats * 4, kGateFloats * 4, bar);
 }
 
-// 32 tokens of one column of v or go, fetched ahead of their use.
+// A thread's tokens of one column of v or go, fetched ahead of their use.
 template <typename T>
 struct Ahead;
 template <>
 struct Ahead<float> {
-    float r[32];
-    __device__ __forceinline__ void set(int i, const float *p) { r[i] = p ? *p : 0.f; }
+    float r[kTokens];
+    __device__ __forceinline__ void set(int i, const float *p) { r[i] = *p; }
+    __device__ __forceinline__ void zero(int i) { r[i] = 0.f; }
     __device__ __forceinline__ float get(int i) const { return r[i]; }
+    template <int N>
+    __device__ __forceinline__ void pair(uint32_t (&q)[N], int i) const { split<N>(q, r[2 * i], r[2 * i + 1]); }
 };
 template <>
 struct Ahead<__nv_bfloat16> {
-    uint16_t r[32];
-    __device__ __forceinline__ void set(int i, const __nv_bfloat16 *p) { r[i] = p ? *reinterpret_cast<const uint16_t *>(p) : (uint16_t)0; }
-    __device__ __forceinline__ float get(int i) const { return __uint_as_float((uint32_t)r[i] << 16); }
+    uint32_t r[kTokens];
+    __device__ __forceinline__ void set(int i, const __nv_bfloat16 *p) { r[i] = *reinterpret_cast<const uint16_t *>(p); }
+    __device__ __forceinline__ void zero(int i) { r[i] = 0; }
+    __device__ __forceinline__ float get(int i) const { return __uint_as_float(r[i] << 16); }
+    template <int N>
+    __device__ __forceinline__ void pair(uint32_t (&q)[N], int i) const { q[0] = r[2 * i] | r[2 * i + 1] << 16; }
 };
 template <typename T>
 __device__ __forceinline__ void fetch(Ahead<T> &x, const T *from, int64_t stride, int left) {
+    if (left >= kTokens) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) x.set(i, i < left ? from + i * stride : nullptr);
+        for (int i = 0; i < kTokens; ++i, from += stride) x.set(i, from);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kTokens; ++i, from += stride) {
+            x.zero(i);
+            if (i < left) x.set(i, from);
+        }
+    }
+}
+// A thread's tokens of one of a chunk's gate values.
+__device__ __forceinline__ void gates_of(float (&g)[kTokens], const float *from) {
+#pragma unroll
+    for (int i = 0; i < kTokens / 4; ++i) {
+        const float4 x = reinterpret_cast<const float4 *>(from)[i];
+        g[4 * i] = x.x, g[4 * i + 1] = x.y, g[4 * i + 2] = x.z, g[4 * i + 3] = x.w;
+    }
 }
 
-// Terms of 2 * W values as left factors: `to` and each further 16 columns take 32 values; terms lie `term` apart.
-template <int N, int W>
-__device__ __forceinline__ void to_lanes(uint32_t to, uint32_t term, const float (&v)[2 * W]) {
+// Terms of values as left factors: 8 columns for each 16 values; terms lie `term` columns apart.
+template <int N, int K>
+__device__ __forceinline__ void to_lanes(uint32_t to, uint32_t term, const float (&v)[K]) {
 #pragma unroll
-    for (int part = 0; part < W / 16; ++part) {
-        uint32_t q[N][16];
+    for (int part = 0; part < K / 16; ++part) {
+        uint32_t q[N][8];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
+        for (int i = 0; i < 8; ++i) {
             uint32_t t[N];
-            split<N>(t, v[part * 32 + 2 * i], v[part * 32 + 2 * i + 1]);
+            split<N>(t, v[part * 16 + 2 * i], v[part * 16 + 2 * i + 1]);
 #pragma unroll
             for (int n = 0; n < N; ++n) q[n][i] = t[n];
         }
 #pragma unroll
-        for (int n = 0; n < N; ++n) tc::tmem_store(to + n * term + part * 16, q[n]);
+        for (int n = 0; n < N; ++n) tc::tmem_store(to + n * term + part * 8, q[n]);
     }
 }
+template <int N, typename T>
+__device__ __forceinline__ void to_lanes(uint32_t to, uint32_t term, const Ahead<T> &x) {
+    uint32_t q[N][8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        uint32_t t[N];
+        x.template pair<N>(t, i);
+#pragma unroll
+        for (int n = 0; n < N; ++n) q[n][i] = t[n];
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) tc::tmem_store(to + n * term, q[n]);
+}
 // A warp has written its left factors: its lane 0 arrives for it.
-__device__ __forceinline__ void ready(uint32_t bar) {
+__device__ __forceinline__ void ready(uint64_t &bar) {
     tc::tmem_stored();
     tc::fence_before_sync();
     __syncwarp();
-    if ((threadIdx.x & 31) == 0) tc::bar_arrive(bar);
+    if ((threadIdx.x & 31) == 0) tc::bar_arrive(tc::smem_addr(&bar));
 }
-// 32 values a thread of row `row` as float32 blocks [columns of 8][tokens (or places) of 8], `width` blocks a row.
+// Values of row `row` from block `first` on as float32 blocks, `width` blocks a row.
 template <int N>
 __device__ __forceinline__ void keep_row(uint8_t *to, int row, int width, int first, const float (&v)[N]) {
+    to += (uint32_t)((row / 8 * width + first) * kWide + (row & 7) * 32);
 #pragma unroll
     for (int n = 0; n < N / 8; ++n) {
         uint32_t q[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) q[e] = __float_as_uint(v[n * 8 + e]);
-        tc::store32(to + ((size_t)(row / 8) * width + first + n) * kWide + (row & 7) * 32, q);
+        tc::store32(to + n * kWide, q);
     }
 }
-// 32 tokens of a column as tiles of bfloat16 terms [term][columns of 8][tokens of 8].
+// A thread's tokens of a column as tiles of bfloat16 terms [term][columns of 8][tokens of 8].
 template <int NT, typename T>
-__device__ __forceinline__ void keep_values(uint8_t *to, size_t term, int row, int first, const Ahead<T> &x) {
+__device__ __forceinline__ void keep_values(uint8_t *to, uint32_t term, int row, int first, const Ahead<T> &x) {
+    to += (uint32_t)((row / 8 * 8 + first) * kCell + (row & 7) * 16);
 #pragma unroll
-    for (int n = 0; n < 4; ++n) {
+    for (int n = 0; n < kTokens / 8; ++n) {
         uint32_t q[4][NT];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) split<NT>(q[i], x.get(n * 8 + 2 * i), x.get(n * 8 + 2 * i + 1));
+        for (int i = 0; i < 4; ++i) x.template pair<NT>(q[i], n * 4 + i);
 #pragma unroll
-        for (int m = 0; m < NT; ++m)
-            *reinterpret_cast<uint4 *>(to + m * term + ((size_t)(row / 8) * 8 + first + n) * kCell + (row & 7) * 16) = make_uint4(q[0][m], q[1][m], q[2][m], q[3][m]);
+        for (int m = 0; m < NT; ++m) *reinterpret_cast<uint4 *>(to + m * term + n * kCell) = make_uint4(q[0][m], q[1][m], q[2][m], q[3][m]);
     }
 }
 
 // Products of NA terms in tensor memory (STEPS blocks of 16 summed places, 8 columns each) and NB terms in shared
 // memory, those whose terms' numbers add up to less than KEEP, the smallest first. TURNED: the right factor's rows
-// run along the summed index, else along the other one. `width`: blocks of a row. TRI: of a lower triangle's rows only
+// run along the summed index, else along the other one. WIDTH: blocks of a row. TRI: of a lower triangle's rows only
 // those from the step on (1), of its columns only those up to the step (2).
-template <int NA, int NB, int KEEP, int STEPS, int N, bool TURNED, int TRI>
-__device__ __forceinline__ void issue(uint32_t d, uint32_t a, uint32_t aterm, uint32_t b, uint32_t bterm, int width, bool add) {
+template <int NA, int NB, int KEEP, int STEPS, int N, int WIDTH, bool TURNED, int TRI>
+__device__ __forceinline__ void issue(uint32_t d, uint32_t a, uint32_t aterm, uint32_t b, uint32_t bterm) {
+    const tc::Blocks tile = TURNED ? tc::Blocks(b, WIDTH * kCell, kCell) : tc::Blocks(b, kCell, WIDTH * kCell);
+    bool add = false;
 #pragma unroll
     for (int sum = KEEP - 1; sum >= 0; --sum)
 #pragma unroll
@@ -134,8 +173,7 @@ __device__ __forceinline__ void issue(uint32_t d, uint32_t a, uint32_t aterm, ui
             for (int n = 0; n < STEPS; ++n) {
                 const int s = TRI == 2 ? STEPS - 1 - n : n;
                 const int from = TRI == 1 ? 16 * s : 0, count = TRI == 1 ? N - 16 * s : TRI == 2 ? 16 * (s + 1) : N;
-                const uint32_t at = b + j * bterm + (TURNED ? 2 * s * width : from / 8 * width + 2 * s) * kCell;
-                tc::mma_lanes(d + from, a + i * aterm + 8 * s, TURNED ? tc::blocks(at, width * kCell, kCell) : tc::blocks(at, kCell, width * kCell),
+                tc::mma_lanes(d + from, a + i * aterm + 8 * s, tile.at(j * bterm + (TURNED ? 2 * s * WIDTH : from / 8 * WIDTH + 2 * s) * kCell),
                               tc::product_of(128, count, false, TURNED), add);
                 add = true;
             }
@@ -143,11 +181,18 @@ __device__ __forceinline__ void issue(uint32_t d, uint32_t a, uint32_t aterm, ui
 }
 
 struct Bars {
-    uint64_t tiles[2], first, second, third, one, two, three, four;
+    uint64_t tiles[2];                     // a stage's tiles have come
+    uint64_t first, second, third;         // all warps have written a round's left factors
+    uint64_t one, two, three, four;        // products are done
 };
 struct Waits {
     bool ok;
     __device__ __forceinline__ void operator()(uint64_t &bar, uint32_t phase) { ok = ok && tc::bar_wait(tc::smem_addr(&bar), phase & 1); }
+    // of products: what they wrote may be read then
+    __device__ __forceinline__ void done(uint64_t &bar, uint32_t phase) {
+        operator()(bar, phase);
+        tc::fence_after_sync();
+    }
 };
 
 // What both walks begin and end with.
@@ -155,9 +200,9 @@ __device__ __forceinline__ uint32_t begin(Bars &bars, uint32_t &where) {
     if (threadIdx.x == 0) {
         uint64_t *all[] = {&bars.tiles[0], &bars.tiles[1], &bars.one, &bars.two, &bars.three, &bars.four};
         for (uint64_t *b : all) tc::bar_init(tc::smem_addr(b), 1);
-        tc::bar_init(tc::smem_addr(&bars.first), 8);
-        tc::bar_init(tc::smem_addr(&bars.second), 8);
-        tc::bar_init(tc::smem_addr(&bars.third), 8);
+        tc::bar_init(tc::smem_addr(&bars.first), kWarps);
+        tc::bar_init(tc::smem_addr(&bars.second), kWarps);
+        tc::bar_init(tc::smem_addr(&bars.third), kWarps);
         tc::bar_init_fence();
     }
     if (threadIdx.x < 32) tc::tmem_alloc_one(tc::smem_addr(&where), kColumns);
@@ -180,139 +225,151 @@ constexpr uint32_t kState = 0, kSeen = 192, kError = 320, kOut = 416;
 template <typename T, int DKP, bool KEEP>
 __global__ void __launch_bounds__(kThreads, 1) delta_forward_kernel(const __grid_constant__ Args a, const T *v, const float *s0, T *o, float *last,
                                                                     uint8_t *kept, int stages) {
-    constexpr int NT = sizeof(T) == 2 ? 1 : 3, W = DKP / 8, TILE = 64 * DKP * 2, SQ = kSquare / 3, HALF = DKP / 2;
+    constexpr int NT = sizeof(T) == 2 ? 1 : 3, W = DKP / 8, TILE = 64 * DKP * 2, SQ = kSquare / 3, OWN = DKP / kParts;
     constexpr int FEW = sizeof(T) == 2 ? 2 : 3;        // terms where only a bfloat16 output comes of it
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ Bars bars;
     __shared__ uint32_t where;
     pdl_begin();
-    const int b = blockIdx.x / a.Hv, h = blockIdx.x % a.Hv, warp = threadIdx.x >> 5;
+    const int b = blockIdx.x / a.Hv, h = blockIdx.x % a.Hv, warp = threadIdx.x >> 5, part = warp >> 2;
+    const int col = (warp & 3) * 32 + (threadIdx.x & 31), tok0 = part * kTokens;
     const Sequence s = sequence(a, b);
     const int chunks = (s.length + C - 1) / C;
     const Stage st = stage_of(a.p);
+    const bool here = col < a.Dv, kept_here = KEEP && col < a.p.DVP, issuer = threadIdx.x == 0;
+    const int64_t state = ((int64_t)b * a.Hv + h) * a.Dk * a.Dv, stride = s.step * a.Hv * a.Dv;
+    const int64_t first = ((s.row + tok0 * s.step) * a.Hv + h) * a.Dv + col;
     const uint32_t base = tc::smem_addr(smem), tmem = begin(bars, where);
+    const uint32_t mine = tmem + ((uint32_t)(warp & 3) << 21);          // this warp's lanes
     Waits wait{true};
-    if (warp >= 8) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
-        if (threadIdx.x == 256) {
-            const uint32_t tiles = tc::smem_addr(bars.tiles);
-            for (int n = 0; n < min(stages, chunks); ++n) load_stage(a, st, base + n * st.bytes, tiles + 8 * n, kept, a.p.xe, s.slot + n, h);
-            for (int n = 0; n < chunks; ++n) {
-                const uint32_t here = base + n % stages * st.bytes, k = here + st.k, q = here + st.q, x = here + st.x, p = here + st.p;
-                wait(bars.tiles[n % stages], n / stages);
-                wait(bars.first, n);
-                if (!wait.ok) break;
-                tc::fence_after_sync();
-                issue<3, NT, 3, DKP / 16, 64, false, 0>(tmem + kSeen, tmem + kState, HALF, k, TILE, W, false);
+    if (issuer)
+        for (int n = 0; n < min(stages, chunks); ++n)
+            load_stage(a, st, base + n * st.bytes, tc::smem_addr(&bars.tiles[n]), kept, a.p.xe, s.slot + n, h);
+    float S[OWN];
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) {
+        const int d = part * OWN + i;
+        S[i] = s0 && here && d < a.Dk ? s0[state + (int64_t)d * a.Dv + col] : 0.f;
+    }
+    Ahead<T> ahead;
+    fetch(ahead, v + first, stride, here ? s.length - tok0 : 0);
+    float out[kTokens];
+    auto put_out = [&](int n) {        // o of chunk n: what of it lies in registers and P u
+        wait.done(bars.four, n);
+        float u[kTokens];
+        tc::tmem_load(u, mine + kOut + tok0);
+#pragma unroll
+        for (int i = 0; i < kTokens; ++i) u[i] = a.scale * (out[i] + u[i]);
+        if (!wait.ok)
+#pragma unroll
+            for (int i = 0; i < kTokens; ++i) u[i] = __int_as_float(0x7fffffff);
+        T *to = o + first + (int64_t)n * C * stride;
+        const int left = here ? s.length - n * C - tok0 : 0;
+        if (left >= kTokens) {
+#pragma unroll
+            for (int i = 0; i < kTokens; ++i, to += stride) put(to, u[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kTokens; ++i, to += stride)
+                if (i < left) put(to, u[i]);
+        }
+    };
+    auto refill = [&](int n) {         // chunk n's stage is free when all that reads it is done
+        if (issuer && n + stages < chunks) {
+            wait(bars.four, n);
+            if (wait.ok)
+                load_stage(a, st, base + n % stages * st.bytes, tc::smem_addr(&bars.tiles[n % stages]), kept, a.p.xe, s.slot + n + stages, h);
+        }
+        __syncwarp();
+    };
+    for (int n = 0; n < chunks; ++n) {
+        const int at = n % stages;
+        const int64_t hv = (s.slot + n) * a.Hv + h;
+        const uint32_t tiles = base + at * st.bytes, k = tiles + st.k, q = tiles + st.q, x = tiles + st.x, p = tiles + st.p;
+        to_lanes<3>(mine + kState + part * (OWN / 2), DKP / 2, S);
+        ready(bars.first);
+        wait(bars.tiles[at], n / stages);
+        if (issuer) {
+            wait.done(bars.first, n);
+            if (wait.ok) {
+                issue<3, NT, 3, DKP / 16, 64, W, false, 0>(tmem + kSeen, tmem + kState, DKP / 2, k, TILE);
                 tc::commit_one(tc::smem_addr(&bars.one));
-                issue<3, NT, FEW, DKP / 16, 64, false, 0>(tmem + kSeen + 64, tmem + kState, HALF, q, TILE, W, false);
-                wait(bars.second, n);
-                if (!wait.ok) break;
-                tc::fence_after_sync();
-                issue<3, 3, 3, 4, 64, false, 1>(tmem + kOut, tmem + kError, 32, x, SQ, 8, false);
-                tc::commit_one(tc::smem_addr(&bars.two));
-                wait(bars.third, n);
-                if (!wait.ok) break;
-                tc::fence_after_sync();
-                issue<3, NT, 3, 4, DKP, true, 0>(tmem + kSeen, tmem + kState, 32, k, TILE, W, false);
-                tc::commit_one(tc::smem_addr(&bars.three));
-                issue<3, FEW, FEW, 4, 64, false, 1>(tmem + kOut, tmem + kError, 32, p, SQ, 8, false);
-                tc::commit_one(tc::smem_addr(&bars.four));
-                if (n + stages < chunks) {             // the stage is free when all that reads it is done
-                    wait(bars.four, n);
-                    if (!wait.ok) break;
-                    load_stage(a, st, here, tiles + 8 * (n % stages), kept, a.p.xe, s.slot + n + stages, h);
-                }
+                issue<3, NT, FEW, DKP / 16, 64, W, false, 0>(tmem + kSeen + 64, tmem + kState, DKP / 2, q, TILE);
             }
         }
         __syncwarp();
-    } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
-        const int half = warp >> 2, lane = threadIdx.x & 31, col = (warp & 3) * 32 + lane, tok0 = half * 32;
-        const uint32_t mine = tmem + ((uint32_t)(warp & 3) << 21);          // this warp's lanes
-        const bool here = col < a.Dv;
-        const int64_t state = ((int64_t)b * a.Hv + h) * a.Dk * a.Dv, stride = s.step * a.Hv * a.Dv;
-        float S[HALF];
-#pragma unroll
-        for (int i = 0; i < HALF; ++i) {
-            const int d = half * HALF + i;
-            S[i] = s0 && here && d < a.Dk ? s0[state + (int64_t)d * a.Dv + col] : 0.f;
+        if (n) put_out(n - 1);
+        if (n && stages > 1) refill(n - 1);
+        if (kept_here) {
+            keep_row(kept + a.p.s + hv * a.p.state_bytes, col, W, part * (W / kParts), S);
+            keep_values<NT>(kept + a.p.v + hv * a.p.value_bytes, (uint32_t)(C * a.p.DVP * 2), col, part * (kTokens / 8), ahead);
         }
-        const int64_t first = ((s.row + tok0 * s.step) * a.Hv + h) * a.Dv + col;
-        Ahead<T> ahead;
-        fetch(ahead, v + first, stride, here ? s.length - tok0 : 0);
-        float out[32];
-        auto put_out = [&](int n) {        // o of chunk n: what of it lies in registers and P u
-            wait(bars.four, n);
-            float u[32];
-            tc::fence_after_sync();
-            tc::tmem_load(u, mine + kOut + tok0);
-            if (!wait.ok) u[0] = __int_as_float(0x7fffffff);
-            T *to = o + first + (int64_t)n * C * stride;
-            const int left = here ? s.length - n * C - tok0 : 0;
+        const float *gates = reinterpret_cast<const float *>(smem + at * st.bytes + st.gates);
+        const float keep = gates[kKeep];
+        float f[kTokens], r[kTokens];
+        gates_of(f, gates + kFirst + tok0);
+        wait.done(bars.one, n);
+        tc::tmem_load(r, mine + kSeen + tok0);
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (i < left) put(to + i * stride, wait.ok ? a.scale * (out[i] + u[i]) : u[0]);
-        };
-        for (int n = 0; n < chunks; ++n) {
-            const int64_t hv = (s.slot + n) * a.Hv + h;
-            to_lanes<3, HALF / 2>(mine + kState + half * (HALF / 2), HALF, S);
-            ready(tc::smem_addr(&bars.first));
-            if (n) put_out(n - 1);
-            if (KEEP && col < a.p.DVP) {
-                keep_row(kept + a.p.s + hv * a.p.state_bytes, col, W, half * (W / 2), S);
-                keep_values<NT>(kept + a.p.v + hv * a.p.value_bytes, (size_t)C * a.p.DVP * 2, col, half * 4, ahead);
+        for (int i = 0; i < kTokens; ++i) r[i] = fmaf(-f[i], r[i], ahead.get(i));
+        to_lanes<3>(mine + kError + part * (kTokens / 2), 32, r);
+        ready(bars.second);
+        if (issuer) {
+            wait.done(bars.second, n);
+            if (wait.ok) {
+                issue<3, 3, 3, 4, 64, 8, false, 1>(tmem + kOut, tmem + kError, 32, x, SQ);
+                tc::commit_one(tc::smem_addr(&bars.two));
             }
-            wait(bars.tiles[n % stages], n / stages);
-            const float *gates = reinterpret_cast<const float *>(smem + n % stages * st.bytes + st.gates);
-            const float keep = gates[kKeep];
-            wait(bars.one, n);
-            tc::fence_after_sync();
-            float r[32];
-            tc::tmem_load(r, mine + kSeen + tok0);
-#pragma unroll
-            for (int i = 0; i < 32; ++i) r[i] = fmaf(-gates[kFirst + tok0 + i], r[i], ahead.get(i));
-            to_lanes<3, 16>(mine + kError + half * 16, 32, r);
-            ready(tc::smem_addr(&bars.second));
-            fetch(ahead, v + first + (int64_t)(n + 1) * C * stride, stride, here ? s.length - (n + 1) * C - tok0 : 0);
-            wait(bars.two, n);
-            tc::fence_after_sync();
-            tc::tmem_load(out, mine + kSeen + 64 + tok0);
-            tc::tmem_load(r, mine + kOut + tok0);
-            float u[32];
-#pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                u[i] = r[i] * gates[kBeta + tok0 + i];
-                out[i] *= gates[kFirst + tok0 + i];
-            }
-            to_lanes<3, 16>(mine + kError + half * 16, 32, u);
-#pragma unroll
-            for (int i = 0; i < 32; ++i) u[i] *= gates[kRest + tok0 + i];
-            to_lanes<3, 16>(mine + kState + half * 16, 32, u);
-            ready(tc::smem_addr(&bars.third));
-            if (KEEP && col < a.p.DVP) keep_row(kept + a.p.e + hv * a.p.kept_bytes, col, 8, half * 4, r);
-            wait(bars.three, n);
-            tc::fence_after_sync();
-#pragma unroll
-            for (int part = 0; part < HALF / 32; ++part) {
-                float d[32];
-                tc::tmem_load(d, mine + kSeen + half * HALF + part * 32);
-#pragma unroll
-                for (int i = 0; i < 32; ++i) S[part * 32 + i] = fmaf(keep, S[part * 32 + i], d[i]);
-            }
-            if (!wait.ok)
-#pragma unroll
-                for (int i = 0; i < HALF; ++i) S[i] = __int_as_float(0x7fffffff);
         }
-        if (chunks) put_out(chunks - 1);
-        if (KEEP && col < a.p.DVP) keep_row(kept + a.p.end + ((int64_t)b * a.Hv + h) * a.p.state_bytes, col, W, half * (W / 2), S);
-        if (last && here)
+        __syncwarp();
+        fetch(ahead, v + first + (int64_t)(n + 1) * C * stride, stride, here ? s.length - (n + 1) * C - tok0 : 0);
+        float u[kTokens], g[kTokens];
+        gates_of(u, gates + kBeta + tok0);
+        gates_of(g, gates + kRest + tok0);
+        wait.done(bars.two, n);
+        tc::tmem_load(r, mine + kOut + tok0);
 #pragma unroll
-            for (int i = 0; i < HALF; ++i) {
-                const int d = half * HALF + i;
-                if (d < a.Dk) last[state + (int64_t)d * a.Dv + col] = S[i];
+        for (int i = 0; i < kTokens; ++i) u[i] *= r[i];
+        to_lanes<3>(mine + kError + part * (kTokens / 2), 32, u);
+#pragma unroll
+        for (int i = 0; i < kTokens; ++i) u[i] *= g[i];
+        to_lanes<3>(mine + kState + part * (kTokens / 2), 32, u);
+        tc::tmem_load(out, mine + kSeen + 64 + tok0);
+        ready(bars.third);
+        if (issuer) {
+            wait.done(bars.third, n);
+            if (wait.ok) {
+                issue<3, NT, 3, 4, DKP, W, true, 0>(tmem + kSeen, tmem + kState, 32, k, TILE);
+                tc::commit_one(tc::smem_addr(&bars.three));
+                issue<3, FEW, FEW, 4, 64, 8, false, 1>(tmem + kOut, tmem + kError, 32, p, SQ);
+                tc::commit_one(tc::smem_addr(&bars.four));
             }
+        }
+        __syncwarp();
+        if (kept_here) keep_row(kept + a.p.e + hv * a.p.kept_bytes, col, 8, part * (kTokens / 8), r);
+#pragma unroll
+        for (int i = 0; i < kTokens; ++i) out[i] *= f[i];
+        if (stages == 1) refill(n);
+        wait.done(bars.three, n);
+#pragma unroll
+        for (int w = 0; w < OWN / 16; ++w) {
+            float d[16];
+            tc::tmem_load(d, mine + kSeen + part * OWN + w * 16);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) S[w * 16 + i] = fmaf(keep, S[w * 16 + i], d[i]);
+        }
+        if (!wait.ok)
+#pragma unroll
+            for (int i = 0; i < OWN; ++i) S[i] = __int_as_float(0x7fffffff);
     }
+    if (chunks) put_out(chunks - 1);
+    if (kept_here) keep_row(kept + a.p.end + ((int64_t)b * a.Hv + h) * a.p.state_bytes, col, W, part * (W / kParts), S);
+    if (last && here)
+#pragma unroll
+        for (int i = 0; i < OWN; ++i) {
+            const int d = part * OWN + i;
+            if (d < a.Dk) last[state + (int64_t)d * a.Dv + col] = S[i];
+        }
     finish(wait.ok, tmem);
 }
 
@@ -325,125 +382,119 @@ constexpr uint32_t kGrad = 0, kGo = 192, kD = 288, kY = 384, kPg = 448, kChange 
 template <typename T, int DKP>
 __global__ void __launch_bounds__(kThreads, 1) delta_backward_kernel(const __grid_constant__ Args a, const T *go, const uint8_t *kept, uint8_t *scratch,
                                                                      const float *glast, float *gs0, int stages) {
-    constexpr int NT = sizeof(T) == 2 ? 1 : 3, W = DKP / 8, TILE = 64 * DKP * 2, SQ = kSquare / 3, HALF = DKP / 2;
+    constexpr int NT = sizeof(T) == 2 ? 1 : 3, W = DKP / 8, TILE = 64 * DKP * 2, SQ = kSquare / 3, OWN = DKP / kParts;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ Bars bars;
     __shared__ uint32_t where;
     pdl_begin();
-    const int b = blockIdx.x / a.Hv, h = blockIdx.x % a.Hv, warp = threadIdx.x >> 5;
+    const int b = blockIdx.x / a.Hv, h = blockIdx.x % a.Hv, warp = threadIdx.x >> 5, part = warp >> 2;
+    const int col = (warp & 3) * 32 + (threadIdx.x & 31), tok0 = part * kTokens;
     const Sequence s = sequence(a, b);
     const int chunks = (s.length + C - 1) / C;
     const Stage st = stage_of(a.p);
+    const bool here = col < a.Dv, kept_here = col < a.p.DVP, issuer = threadIdx.x == 0;
+    const int64_t state = ((int64_t)b * a.Hv + h) * a.Dk * a.Dv, stride = s.step * a.Hv * a.Dv;
+    const int64_t first = ((s.row + tok0 * s.step) * a.Hv + h) * a.Dv + col;
     const uint32_t base = tc::smem_addr(smem), tmem = begin(bars, where);
+    const uint32_t mine = tmem + ((uint32_t)(warp & 3) << 21);
     Waits wait{true};
-    if (warp >= 8) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
-        if (threadIdx.x == 256) {
-            const uint32_t tiles = tc::smem_addr(bars.tiles);
-            for (int n = 0; n < min(stages, chunks); ++n) load_stage(a, st, base + n * st.bytes, tiles + 8 * n, kept, a.p.xu, s.slot + chunks - 1 - n, h);
-            for (int n = 0; n < chunks; ++n) {
-                const uint32_t here = base + n % stages * st.bytes, k = here + st.k, q = here + st.q, x = here + st.x, p = here + st.p;
-                wait(bars.tiles[n % stages], n / stages);
-                wait(bars.first, n);
-                if (!wait.ok) break;
-                tc::fence_after_sync();
-                issue<3, NT, 3, DKP / 16, 64, false, 0>(tmem + kY, tmem + kGrad, HALF, k, TILE, W, false);
-                issue<NT, 3, 3, 4, 64, true, 2>(tmem + kPg, tmem + kGo, 32, p, SQ, 8, false);
+    if (issuer)
+        for (int n = 0; n < min(stages, chunks); ++n)
+            load_stage(a, st, base + n * st.bytes, tc::smem_addr(&bars.tiles[n]), kept, a.p.xu, s.slot + chunks - 1 - n, h);
+    float D[OWN];
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) {
+        const int d = part * OWN + i;
+        D[i] = glast && here && d < a.Dk ? glast[state + (int64_t)d * a.Dv + col] : 0.f;
+    }
+    Ahead<T> ahead;
+    fetch(ahead, go + first + (int64_t)(chunks - 1) * C * stride, stride, here && chunks ? s.length - (chunks - 1) * C - tok0 : 0);
+    for (int n = 0; n < chunks; ++n) {
+        const int chunk = chunks - 1 - n, at = n % stages;
+        const int64_t hv = (s.slot + chunk) * a.Hv + h;
+        const uint32_t tiles = base + at * st.bytes, k = tiles + st.k, q = tiles + st.q, x = tiles + st.x, p = tiles + st.p;
+        to_lanes<3>(mine + kGrad + part * (OWN / 2), DKP / 2, D);
+        to_lanes<NT>(mine + kGo + part * (kTokens / 2), 32, ahead);
+        ready(bars.first);
+        wait(bars.tiles[at], n / stages);
+        if (issuer) {
+            wait.done(bars.first, n);
+            if (wait.ok) {
+                issue<3, NT, 3, DKP / 16, 64, W, false, 0>(tmem + kY, tmem + kGrad, DKP / 2, k, TILE);
+                issue<NT, 3, 3, 4, 64, 8, true, 2>(tmem + kPg, tmem + kGo, 32, p, SQ);
                 tc::commit_one(tc::smem_addr(&bars.one));
-                wait(bars.second, n);
-                if (!wait.ok) break;
-                tc::fence_after_sync();
-                issue<3, 3, 3, 4, 64, true, 2>(tmem + kY, tmem + kD, 32, x, SQ, 8, false);
-                tc::commit_one(tc::smem_addr(&bars.two));
-                issue<3, NT, 3, 4, DKP, true, 0>(tmem + kChange, tmem + kGrad, 32, q, TILE, W, false);
-                wait(bars.third, n);
-                if (!wait.ok) break;
-                tc::fence_after_sync();
-                issue<3, NT, 3, 4, DKP, true, 0>(tmem + kY, tmem + kD, 32, k, TILE, W, false);
-                tc::commit_one(tc::smem_addr(&bars.three));
-                if (n + stages < chunks) {
-                    wait(bars.three, n);
-                    if (!wait.ok) break;
-                    load_stage(a, st, here, tiles + 8 * (n % stages), kept, a.p.xu, s.slot + chunks - 1 - n - stages, h);
-                }
             }
         }
         __syncwarp();
-    } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
-        const int half = warp >> 2, lane = threadIdx.x & 31, col = (warp & 3) * 32 + lane, tok0 = half * 32;
-        const uint32_t mine = tmem + ((uint32_t)(warp & 3) << 21);
-        const bool here = col < a.Dv;
-        const int64_t state = ((int64_t)b * a.Hv + h) * a.Dk * a.Dv, stride = s.step * a.Hv * a.Dv;
-        const int64_t first = ((s.row + tok0 * s.step) * a.Hv + h) * a.Dv + col;
-        float D[HALF];
-#pragma unroll
-        for (int i = 0; i < HALF; ++i) {
-            const int d = half * HALF + i;
-            D[i] = glast && here && d < a.Dk ? glast[state + (int64_t)d * a.Dv + col] : 0.f;
+        if (kept_here) {
+            keep_row(scratch + a.p.d + hv * a.p.state_bytes, col, W, part * (W / kParts), D);
+            keep_values<NT>(scratch + a.p.go + hv * a.p.value_bytes, (uint32_t)(C * a.p.DVP * 2), col, part * (kTokens / 8), ahead);
         }
-        Ahead<T> ahead;
-        fetch(ahead, go + first + (int64_t)(chunks - 1) * C * stride, stride, here && chunks ? s.length - (chunks - 1) * C - tok0 : 0);
-        for (int n = 0; n < chunks; ++n) {
-            const int chunk = chunks - 1 - n;
-            const int64_t hv = (s.slot + chunk) * a.Hv + h;
-            to_lanes<3, HALF / 2>(mine + kGrad + half * (HALF / 2), HALF, D);
-            float g[32];
+        const float *gates = reinterpret_cast<const float *>(smem + at * st.bytes + st.gates);
+        const float keep = gates[kKeep];
+        float f[kTokens], r[kTokens], d[kTokens], g[kTokens];
+        gates_of(f, gates + kFirst + tok0);
+        gates_of(g, gates + kRest + tok0);
+        wait.done(bars.one, n);
+        tc::tmem_load(r, mine + kY + tok0);
+        tc::tmem_load(d, mine + kPg + tok0);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) g[i] = ahead.get(i);
-            to_lanes<NT, 16>(mine + kGo + half * 16, 32, g);
-            ready(tc::smem_addr(&bars.first));
-            if (col < a.p.DVP) {
-                keep_row(scratch + a.p.d + hv * a.p.state_bytes, col, W, half * (W / 2), D);
-                keep_values<NT>(scratch + a.p.go + hv * a.p.value_bytes, (size_t)C * a.p.DVP * 2, col, half * 4, ahead);
+        for (int i = 0; i < kTokens; ++i) d[i] = fmaf(g[i], r[i], a.scale * d[i]);
+        to_lanes<3>(mine + kD + part * (kTokens / 2), 32, d);
+#pragma unroll
+        for (int i = 0; i < kTokens; ++i) g[i] = a.scale * f[i] * ahead.get(i);
+        to_lanes<3>(mine + kGrad + part * (kTokens / 2), 32, g);
+        ready(bars.second);
+        if (issuer) {
+            wait.done(bars.second, n);
+            if (wait.ok) {
+                issue<3, 3, 3, 4, 64, 8, true, 2>(tmem + kY, tmem + kD, 32, x, SQ);
+                tc::commit_one(tc::smem_addr(&bars.two));
+                issue<3, NT, 3, 4, DKP, W, true, 0>(tmem + kChange, tmem + kGrad, 32, q, TILE);
             }
-            if (n + 1 < chunks) fetch(ahead, go + first + (int64_t)(chunk - 1) * C * stride, stride, here ? 32 : 0);
-            wait(bars.tiles[n % stages], n / stages);
-            const float *gates = reinterpret_cast<const float *>(smem + n % stages * st.bytes + st.gates);
-            const float keep = gates[kKeep];
-            wait(bars.one, n);
-            tc::fence_after_sync();
-            float r[32], d[32];
-            tc::tmem_load(r, mine + kY + tok0);
-            tc::tmem_load(d, mine + kPg + tok0);
-#pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                d[i] = fmaf(gates[kRest + tok0 + i], r[i], a.scale * d[i]);
-                g[i] *= a.scale * gates[kFirst + tok0 + i];
-            }
-            to_lanes<3, 16>(mine + kD + half * 16, 32, d);
-            to_lanes<3, 16>(mine + kGrad + half * 16, 32, g);
-            ready(tc::smem_addr(&bars.second));
-            wait(bars.two, n);
-            tc::fence_after_sync();
-            tc::tmem_load(r, mine + kY + tok0);
-#pragma unroll
-            for (int i = 0; i < 32; ++i) d[i] = r[i] * (-gates[kFirst + tok0 + i] * gates[kBeta + tok0 + i]);
-            to_lanes<3, 16>(mine + kD + half * 16, 32, d);
-            ready(tc::smem_addr(&bars.third));
-            if (col < a.p.DVP) keep_row(scratch + a.p.y + hv * a.p.kept_bytes, col, 8, half * 4, r);
-            wait(bars.three, n);
-            tc::fence_after_sync();
-#pragma unroll
-            for (int part = 0; part < HALF / 32; ++part) {
-                tc::tmem_load(r, mine + kChange + half * HALF + part * 32);
-                tc::tmem_load(d, mine + kY + half * HALF + part * 32);
-#pragma unroll
-                for (int i = 0; i < 32; ++i) D[part * 32 + i] = fmaf(keep, D[part * 32 + i], r[i] + d[i]);
-            }
-            if (!wait.ok)
-#pragma unroll
-                for (int i = 0; i < HALF; ++i) D[i] = __int_as_float(0x7fffffff);
-            // the other warp of these lanes has read its half before terms are written over it
-            asm volatile("bar.sync %0, 64;" ::"r"(1 + (warp & 3)) : "memory");
         }
-        if (gs0 && here)
+        __syncwarp();
+        if (n + 1 < chunks) fetch(ahead, go + first + (int64_t)(chunk - 1) * C * stride, stride, here ? kTokens : 0);
+        gates_of(g, gates + kBeta + tok0);
+        wait.done(bars.two, n);
+        tc::tmem_load(r, mine + kY + tok0);
 #pragma unroll
-            for (int i = 0; i < HALF; ++i) {
-                const int d = half * HALF + i;
-                if (d < a.Dk) gs0[state + (int64_t)d * a.Dv + col] = D[i];
+        for (int i = 0; i < kTokens; ++i) d[i] = r[i] * (-f[i] * g[i]);
+        to_lanes<3>(mine + kD + part * (kTokens / 2), 32, d);
+        ready(bars.third);
+        if (issuer) {
+            wait.done(bars.third, n);
+            if (wait.ok) {
+                issue<3, NT, 3, 4, DKP, W, true, 0>(tmem + kY, tmem + kD, 32, k, TILE);
+                tc::commit_one(tc::smem_addr(&bars.three));
             }
+        }
+        __syncwarp();
+        if (kept_here) keep_row(scratch + a.p.y + hv * a.p.kept_bytes, col, 8, part * (kTokens / 8), r);
+        wait.done(bars.three, n);
+        if (issuer && wait.ok && n + stages < chunks)
+            load_stage(a, st, base + at * st.bytes, tc::smem_addr(&bars.tiles[at]), kept, a.p.xu, s.slot + chunk - stages, h);
+        __syncwarp();
+#pragma unroll
+        for (int w = 0; w < OWN / 16; ++w) {
+            float y[16], z[16];
+            tc::tmem_load(y, mine + kChange + part * OWN + w * 16);
+            tc::tmem_load(z, mine + kY + part * OWN + w * 16);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) D[w * 16 + i] = fmaf(keep, D[w * 16 + i], y[i] + z[i]);
+        }
+        if (!wait.ok)
+#pragma unroll
+            for (int i = 0; i < OWN; ++i) D[i] = __int_as_float(0x7fffffff);
+        // the other warps of these lanes have read their parts before terms are written over them
+        asm volatile("bar.sync %0, %1;" ::"r"(1 + (warp & 3)), "n"(32 * kParts) : "memory");
     }
+    if (gs0 && here)
+#pragma unroll
+        for (int i = 0; i < OWN; ++i) {
+            const int d = part * OWN + i;
+            if (d < a.Dk) gs0[state + (int64_t)d * a.Dv + col] = D[i];
+        }
     finish(wait.ok, tmem);
 }
 

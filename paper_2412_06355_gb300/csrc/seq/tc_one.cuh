@@ -33,18 +33,29 @@ __device__ __forceinline__ void bar_arrive(uint32_t bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 // A tile of 8 x 8 blocks as an operand. `summed`: bytes between blocks along the summed index; `other`: along the other
-// one. Which of the two runs along a block's 16-byte rows is the instruction's to say (product_of).
-__device__ __forceinline__ uint64_t blocks(uint32_t addr, uint32_t summed, uint32_t other) {
-    return (uint64_t)((addr >> 4) & 0x3fff) | (uint64_t)(summed >> 4) << 16 | (uint64_t)(other >> 4) << 32 | 1ull << 46;
-}
-// 16 or 32 columns of this warp's 32 lanes; tmem_stored waits for all of them.
-__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&v)[16]) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
-                 "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-                 ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
-                   "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
+// one. Which of the two runs along a block's 16-byte rows is the instruction's to say (product_of). `further` bytes on
+// in the tile (addresses stay below 2^18, so the low word's upper half is not touched).
+struct Blocks {
+    uint32_t low, high;
+    __device__ __forceinline__ Blocks(uint32_t addr, uint32_t summed, uint32_t other)
+        : low(addr >> 4 | (summed >> 4) << 16), high(other >> 4 | 1u << 14) {}
+    __device__ __forceinline__ uint64_t at(uint32_t further) const { return (uint64_t)high << 32 | (low + (further >> 4)); }
+};
+// 8 columns of this warp's 32 lanes; tmem_stored waits for all of them.
+__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&v)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
 __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// 16 columns; one statement loads and waits.
+__device__ __forceinline__ void tmem_load(float (&v)[16], uint32_t addr) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+                 "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+                 "tcgen05.wait::ld.sync.aligned;"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+                   "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+                 : "r"(addr) : "memory");
+}
 
 }  // namespace tc
 }  // namespace dendsn
