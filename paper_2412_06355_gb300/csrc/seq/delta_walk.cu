@@ -5,8 +5,9 @@
 // memory are the columns, and everything a chunk needs comes from three rounds of tcgen05 products (forward: k S and
 // q S; e; P u and k^T (rest u). backward: P^T go and k D; y; q^T go and k^T y), whose left factors the threads write to
 // tensor memory as bfloat16 terms and whose right factors are the chunk's tiles in shared memory. The state itself
-// stays in registers as float32: four threads a column, a quarter of the places each. A thread of the first warp
-// fetches tiles and issues products; in between the warps wait for each other on mbarriers.
+// stays in registers as float32: four threads a column, a quarter of the places each. Sixteen warps compute, one more
+// fetches tiles and issues products; in between they wait for each other on mbarriers. (8 x 2048 tokens, 16 heads of
+// 128 x 128, forward: eight warps 470 us, sixteen of which one issues 226 us.)
 //
 // What bounds it is the chain: a chunk is three rounds of (registers -> tensor memory -> products -> registers), and
 // a block has all of an SM's tensor memory, so that 128 sequences and heads are 128 SMs at work.
@@ -19,7 +20,8 @@ namespace dendsn {
 namespace delta {
 namespace {
 
-constexpr int kWarps = 16, kThreads = kWarps * 32;
+constexpr int kWarps = 16;                 // that compute
+constexpr int kThreads = (kWarps + 4) * 32;            // one more issues; three only share its registers out
 constexpr int kParts = kWarps / 4;         // threads of a column of v
 constexpr int kTokens = C / kParts;        // tokens of a thread
 constexpr uint32_t kColumns = 512;         // of tensor memory: all there are
@@ -83,12 +85,13 @@ __device__ __forceinline__ void fetch(Ahead<T> &x, const T *from, int64_t stride
         }
     }
 }
-// A thread's tokens of one of a chunk's gate values.
-__device__ __forceinline__ void gates_of(float (&g)[kTokens], const float *from) {
+// For every of a thread's tokens, its place and one of a chunk's gate values.
+template <typename F>
+__device__ __forceinline__ void each(const float *from, F f) {
 #pragma unroll
-    for (int i = 0; i < kTokens / 4; ++i) {
-        const float4 x = reinterpret_cast<const float4 *>(from)[i];
-        g[4 * i] = x.x, g[4 * i + 1] = x.y, g[4 * i + 2] = x.z, g[4 * i + 3] = x.w;
+    for (int i = 0; i < kTokens; i += 4) {
+        const float4 x = *reinterpret_cast<const float4 *>(from + i);
+        f(i, x.x), f(i + 1, x.y), f(i + 2, x.z), f(i + 3, x.w);
     }
 }
 
@@ -195,6 +198,16 @@ struct Waits {
     }
 };
 
+// 96 registers a thread at the launch (the compiler's choice for 640 threads), 104 and 64 after: as many in all.
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 104;"); }
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 64;"); }
+// One lane of a whole warp, in a way that leaves the compiler's uniform registers usable.
+__device__ __forceinline__ bool elected() {
+    uint32_t yes;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+    return yes != 0;
+}
+
 // What both walks begin and end with.
 __device__ __forceinline__ uint32_t begin(Bars &bars, uint32_t &where) {
     if (threadIdx.x == 0) {
@@ -231,20 +244,55 @@ __global__ void __launch_bounds__(kThreads, 1) delta_forward_kernel(const __grid
     __shared__ Bars bars;
     __shared__ uint32_t where;
     pdl_begin();
-    const int b = blockIdx.x / a.Hv, h = blockIdx.x % a.Hv, warp = threadIdx.x >> 5, part = warp >> 2;
+    const int b = blockIdx.x / a.Hv, h = blockIdx.x % a.Hv, warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), part = warp >> 2;
     const int col = (warp & 3) * 32 + (threadIdx.x & 31), tok0 = part * kTokens;
     const Sequence s = sequence(a, b);
     const int chunks = (s.length + C - 1) / C;
     const Stage st = stage_of(a.p);
-    const bool here = col < a.Dv, kept_here = KEEP && col < a.p.DVP, issuer = threadIdx.x == 0;
+    const bool here = col < a.Dv, kept_here = KEEP && col < a.p.DVP;
     const int64_t state = ((int64_t)b * a.Hv + h) * a.Dk * a.Dv, stride = s.step * a.Hv * a.Dv;
     const int64_t first = ((s.row + tok0 * s.step) * a.Hv + h) * a.Dv + col;
     const uint32_t base = tc::smem_addr(smem), tmem = begin(bars, where);
     const uint32_t mine = tmem + ((uint32_t)(warp & 3) << 21);          // this warp's lanes
     Waits wait{true};
-    if (issuer)
-        for (int n = 0; n < min(stages, chunks); ++n)
-            load_stage(a, st, base + n * st.bytes, tc::smem_addr(&bars.tiles[n]), kept, a.p.xe, s.slot + n, h);
+    if (warp >= kWarps) {
+        fewer_registers();
+        if (warp == kWarps && elected()) {
+            const uint32_t bar = tc::smem_addr(bars.tiles);
+            for (int n = 0; n < min(stages, chunks); ++n) load_stage(a, st, base + n * st.bytes, bar + 8 * n, kept, a.p.xe, s.slot + n, h);
+            // the stage of chunk n is free when all that reads it is done
+            auto refill = [&](int n) {
+                wait(bars.four, n);
+                if (wait.ok && n + stages < chunks)
+                    load_stage(a, st, base + n % stages * st.bytes, bar + 8 * (n % stages), kept, a.p.xe, s.slot + n + stages, h);
+            };
+            for (int n = 0; n < chunks && wait.ok; ++n) {
+                const uint32_t tiles = base + n % stages * st.bytes, k = tiles + st.k, q = tiles + st.q, x = tiles + st.x, p = tiles + st.p;
+                wait(bars.tiles[n % stages], n / stages);
+                wait.done(bars.first, n);
+                if (!wait.ok) break;
+                issue<3, NT, 3, DKP / 16, 64, W, false, 0>(tmem + kSeen, tmem + kState, DKP / 2, k, TILE);
+                tc::commit_one(tc::smem_addr(&bars.one));
+                issue<3, NT, FEW, DKP / 16, 64, W, false, 0>(tmem + kSeen + 64, tmem + kState, DKP / 2, q, TILE);
+                if (n && stages > 1) refill(n - 1);
+                wait.done(bars.second, n);
+                if (!wait.ok) break;
+                issue<3, 3, 3, 4, 64, 8, false, 1>(tmem + kOut, tmem + kError, 32, x, SQ);
+                tc::commit_one(tc::smem_addr(&bars.two));
+                wait.done(bars.third, n);
+                if (!wait.ok) break;
+                issue<3, NT, 3, 4, DKP, W, true, 0>(tmem + kSeen, tmem + kState, 32, k, TILE);
+                tc::commit_one(tc::smem_addr(&bars.three));
+                issue<3, FEW, FEW, 4, 64, 8, false, 1>(tmem + kOut, tmem + kError, 32, p, SQ);
+                tc::commit_one(tc::smem_addr(&bars.four));
+                if (stages == 1) refill(n);
+            }
+        }
+        __syncwarp();
+        finish(wait.ok, tmem);
+        return;
+    }
+    more_registers();
     float S[OWN];
 #pragma unroll
     for (int i = 0; i < OWN; ++i) {
@@ -274,82 +322,35 @@ __global__ void __launch_bounds__(kThreads, 1) delta_forward_kernel(const __grid
                 if (i < left) put(to, u[i]);
         }
     };
-    auto refill = [&](int n) {         // chunk n's stage is free when all that reads it is done
-        if (issuer && n + stages < chunks) {
-            wait(bars.four, n);
-            if (wait.ok)
-                load_stage(a, st, base + n % stages * st.bytes, tc::smem_addr(&bars.tiles[n % stages]), kept, a.p.xe, s.slot + n + stages, h);
-        }
-        __syncwarp();
-    };
     for (int n = 0; n < chunks; ++n) {
         const int at = n % stages;
         const int64_t hv = (s.slot + n) * a.Hv + h;
-        const uint32_t tiles = base + at * st.bytes, k = tiles + st.k, q = tiles + st.q, x = tiles + st.x, p = tiles + st.p;
         to_lanes<3>(mine + kState + part * (OWN / 2), DKP / 2, S);
         ready(bars.first);
-        wait(bars.tiles[at], n / stages);
-        if (issuer) {
-            wait.done(bars.first, n);
-            if (wait.ok) {
-                issue<3, NT, 3, DKP / 16, 64, W, false, 0>(tmem + kSeen, tmem + kState, DKP / 2, k, TILE);
-                tc::commit_one(tc::smem_addr(&bars.one));
-                issue<3, NT, FEW, DKP / 16, 64, W, false, 0>(tmem + kSeen + 64, tmem + kState, DKP / 2, q, TILE);
-            }
-        }
-        __syncwarp();
         if (n) put_out(n - 1);
-        if (n && stages > 1) refill(n - 1);
-        if (kept_here) {
-            keep_row(kept + a.p.s + hv * a.p.state_bytes, col, W, part * (W / kParts), S);
-            keep_values<NT>(kept + a.p.v + hv * a.p.value_bytes, (uint32_t)(C * a.p.DVP * 2), col, part * (kTokens / 8), ahead);
-        }
+        // what the backward needs goes out a little in each round: an SM's stores take 64 bytes a cycle at best
+        if (kept_here) keep_values<NT>(kept + a.p.v + hv * a.p.value_bytes, (uint32_t)(C * a.p.DVP * 2), col, part * (kTokens / 8), ahead);
+        wait(bars.tiles[at], n / stages);
         const float *gates = reinterpret_cast<const float *>(smem + at * st.bytes + st.gates);
         const float keep = gates[kKeep];
-        float f[kTokens], r[kTokens];
-        gates_of(f, gates + kFirst + tok0);
+        float r[kTokens];
         wait.done(bars.one, n);
         tc::tmem_load(r, mine + kSeen + tok0);
-#pragma unroll
-        for (int i = 0; i < kTokens; ++i) r[i] = fmaf(-f[i], r[i], ahead.get(i));
+        each(gates + kFirst + tok0, [&](int i, float f) { r[i] = fmaf(-f, r[i], ahead.get(i)); });
         to_lanes<3>(mine + kError + part * (kTokens / 2), 32, r);
         ready(bars.second);
-        if (issuer) {
-            wait.done(bars.second, n);
-            if (wait.ok) {
-                issue<3, 3, 3, 4, 64, 8, false, 1>(tmem + kOut, tmem + kError, 32, x, SQ);
-                tc::commit_one(tc::smem_addr(&bars.two));
-            }
-        }
-        __syncwarp();
         fetch(ahead, v + first + (int64_t)(n + 1) * C * stride, stride, here ? s.length - (n + 1) * C - tok0 : 0);
-        float u[kTokens], g[kTokens];
-        gates_of(u, gates + kBeta + tok0);
-        gates_of(g, gates + kRest + tok0);
+        if (kept_here) keep_row(kept + a.p.s + hv * a.p.state_bytes, col, W, part * (W / kParts), S);
         wait.done(bars.two, n);
         tc::tmem_load(r, mine + kOut + tok0);
-#pragma unroll
-        for (int i = 0; i < kTokens; ++i) u[i] *= r[i];
-        to_lanes<3>(mine + kError + part * (kTokens / 2), 32, u);
-#pragma unroll
-        for (int i = 0; i < kTokens; ++i) u[i] *= g[i];
-        to_lanes<3>(mine + kState + part * (kTokens / 2), 32, u);
-        tc::tmem_load(out, mine + kSeen + 64 + tok0);
-        ready(bars.third);
-        if (issuer) {
-            wait.done(bars.third, n);
-            if (wait.ok) {
-                issue<3, NT, 3, 4, DKP, W, true, 0>(tmem + kSeen, tmem + kState, 32, k, TILE);
-                tc::commit_one(tc::smem_addr(&bars.three));
-                issue<3, FEW, FEW, 4, 64, 8, false, 1>(tmem + kOut, tmem + kError, 32, p, SQ);
-                tc::commit_one(tc::smem_addr(&bars.four));
-            }
-        }
-        __syncwarp();
         if (kept_here) keep_row(kept + a.p.e + hv * a.p.kept_bytes, col, 8, part * (kTokens / 8), r);
-#pragma unroll
-        for (int i = 0; i < kTokens; ++i) out[i] *= f[i];
-        if (stages == 1) refill(n);
+        each(gates + kBeta + tok0, [&](int i, float g) { r[i] *= g; });
+        to_lanes<3>(mine + kError + part * (kTokens / 2), 32, r);
+        each(gates + kRest + tok0, [&](int i, float g) { r[i] *= g; });
+        to_lanes<3>(mine + kState + part * (kTokens / 2), 32, r);
+        tc::tmem_load(out, mine + kSeen + 64 + tok0);
+        each(gates + kFirst + tok0, [&](int i, float f) { out[i] *= f; });
+        ready(bars.third);
         wait.done(bars.three, n);
 #pragma unroll
         for (int w = 0; w < OWN / 16; ++w) {
@@ -387,20 +388,50 @@ __global__ void __launch_bounds__(kThreads, 1) delta_backward_kernel(const __gri
     __shared__ Bars bars;
     __shared__ uint32_t where;
     pdl_begin();
-    const int b = blockIdx.x / a.Hv, h = blockIdx.x % a.Hv, warp = threadIdx.x >> 5, part = warp >> 2;
+    const int b = blockIdx.x / a.Hv, h = blockIdx.x % a.Hv, warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), part = warp >> 2;
     const int col = (warp & 3) * 32 + (threadIdx.x & 31), tok0 = part * kTokens;
     const Sequence s = sequence(a, b);
     const int chunks = (s.length + C - 1) / C;
     const Stage st = stage_of(a.p);
-    const bool here = col < a.Dv, kept_here = col < a.p.DVP, issuer = threadIdx.x == 0;
+    const bool here = col < a.Dv, kept_here = col < a.p.DVP;
     const int64_t state = ((int64_t)b * a.Hv + h) * a.Dk * a.Dv, stride = s.step * a.Hv * a.Dv;
     const int64_t first = ((s.row + tok0 * s.step) * a.Hv + h) * a.Dv + col;
     const uint32_t base = tc::smem_addr(smem), tmem = begin(bars, where);
     const uint32_t mine = tmem + ((uint32_t)(warp & 3) << 21);
     Waits wait{true};
-    if (issuer)
-        for (int n = 0; n < min(stages, chunks); ++n)
-            load_stage(a, st, base + n * st.bytes, tc::smem_addr(&bars.tiles[n]), kept, a.p.xu, s.slot + chunks - 1 - n, h);
+    if (warp >= kWarps) {
+        fewer_registers();
+        if (warp == kWarps && elected()) {
+            const uint32_t bar = tc::smem_addr(bars.tiles);
+            for (int n = 0; n < min(stages, chunks); ++n) load_stage(a, st, base + n * st.bytes, bar + 8 * n, kept, a.p.xu, s.slot + chunks - 1 - n, h);
+            for (int n = 0; n < chunks; ++n) {
+                const uint32_t tiles = base + n % stages * st.bytes, k = tiles + st.k, q = tiles + st.q, x = tiles + st.x, p = tiles + st.p;
+                wait(bars.tiles[n % stages], n / stages);
+                wait.done(bars.first, n);
+                if (!wait.ok) break;
+                issue<3, NT, 3, DKP / 16, 64, W, false, 0>(tmem + kY, tmem + kGrad, DKP / 2, k, TILE);
+                issue<NT, 3, 3, 4, 64, 8, true, 2>(tmem + kPg, tmem + kGo, 32, p, SQ);
+                tc::commit_one(tc::smem_addr(&bars.one));
+                wait.done(bars.second, n);
+                if (!wait.ok) break;
+                issue<3, 3, 3, 4, 64, 8, true, 2>(tmem + kY, tmem + kD, 32, x, SQ);
+                tc::commit_one(tc::smem_addr(&bars.two));
+                issue<3, NT, 3, 4, DKP, W, true, 0>(tmem + kChange, tmem + kGrad, 32, q, TILE);
+                wait.done(bars.third, n);
+                if (!wait.ok) break;
+                issue<3, NT, 3, 4, DKP, W, true, 0>(tmem + kY, tmem + kD, 32, k, TILE);
+                tc::commit_one(tc::smem_addr(&bars.three));
+                if (n + stages >= chunks) continue;
+                wait(bars.three, n);
+                if (!wait.ok) break;
+                load_stage(a, st, tiles, bar + 8 * (n % stages), kept, a.p.xu, s.slot + chunks - 1 - n - stages, h);
+            }
+        }
+        __syncwarp();
+        finish(wait.ok, tmem);
+        return;
+    }
+    more_registers();
     float D[OWN];
 #pragma unroll
     for (int i = 0; i < OWN; ++i) {
@@ -412,69 +443,35 @@ __global__ void __launch_bounds__(kThreads, 1) delta_backward_kernel(const __gri
     for (int n = 0; n < chunks; ++n) {
         const int chunk = chunks - 1 - n, at = n % stages;
         const int64_t hv = (s.slot + chunk) * a.Hv + h;
-        const uint32_t tiles = base + at * st.bytes, k = tiles + st.k, q = tiles + st.q, x = tiles + st.x, p = tiles + st.p;
         to_lanes<3>(mine + kGrad + part * (OWN / 2), DKP / 2, D);
         to_lanes<NT>(mine + kGo + part * (kTokens / 2), 32, ahead);
         ready(bars.first);
+        if (kept_here) keep_values<NT>(scratch + a.p.go + hv * a.p.value_bytes, (uint32_t)(C * a.p.DVP * 2), col, part * (kTokens / 8), ahead);
         wait(bars.tiles[at], n / stages);
-        if (issuer) {
-            wait.done(bars.first, n);
-            if (wait.ok) {
-                issue<3, NT, 3, DKP / 16, 64, W, false, 0>(tmem + kY, tmem + kGrad, DKP / 2, k, TILE);
-                issue<NT, 3, 3, 4, 64, 8, true, 2>(tmem + kPg, tmem + kGo, 32, p, SQ);
-                tc::commit_one(tc::smem_addr(&bars.one));
-            }
-        }
-        __syncwarp();
-        if (kept_here) {
-            keep_row(scratch + a.p.d + hv * a.p.state_bytes, col, W, part * (W / kParts), D);
-            keep_values<NT>(scratch + a.p.go + hv * a.p.value_bytes, (uint32_t)(C * a.p.DVP * 2), col, part * (kTokens / 8), ahead);
-        }
         const float *gates = reinterpret_cast<const float *>(smem + at * st.bytes + st.gates);
         const float keep = gates[kKeep];
-        float f[kTokens], r[kTokens], d[kTokens], g[kTokens];
-        gates_of(f, gates + kFirst + tok0);
-        gates_of(g, gates + kRest + tok0);
+        float r[kTokens];
         wait.done(bars.one, n);
-        tc::tmem_load(r, mine + kY + tok0);
-        tc::tmem_load(d, mine + kPg + tok0);
-#pragma unroll
-        for (int i = 0; i < kTokens; ++i) d[i] = fmaf(g[i], r[i], a.scale * d[i]);
-        to_lanes<3>(mine + kD + part * (kTokens / 2), 32, d);
-#pragma unroll
-        for (int i = 0; i < kTokens; ++i) g[i] = a.scale * f[i] * ahead.get(i);
-        to_lanes<3>(mine + kGrad + part * (kTokens / 2), 32, g);
-        ready(bars.second);
-        if (issuer) {
-            wait.done(bars.second, n);
-            if (wait.ok) {
-                issue<3, 3, 3, 4, 64, 8, true, 2>(tmem + kY, tmem + kD, 32, x, SQ);
-                tc::commit_one(tc::smem_addr(&bars.two));
-                issue<3, NT, 3, 4, DKP, W, true, 0>(tmem + kChange, tmem + kGrad, 32, q, TILE);
-            }
+        {
+            float d[kTokens];
+            tc::tmem_load(r, mine + kY + tok0);
+            tc::tmem_load(d, mine + kPg + tok0);
+            each(gates + kRest + tok0, [&](int i, float g) { r[i] = fmaf(g, r[i], a.scale * d[i]); });
         }
-        __syncwarp();
+        to_lanes<3>(mine + kD + part * (kTokens / 2), 32, r);
+        each(gates + kFirst + tok0, [&](int i, float f) { r[i] = a.scale * f * ahead.get(i); });
+        to_lanes<3>(mine + kGrad + part * (kTokens / 2), 32, r);
+        ready(bars.second);
         if (n + 1 < chunks) fetch(ahead, go + first + (int64_t)(chunk - 1) * C * stride, stride, here ? kTokens : 0);
-        gates_of(g, gates + kBeta + tok0);
+        if (kept_here) keep_row(scratch + a.p.d + hv * a.p.state_bytes, col, W, part * (W / kParts), D);
         wait.done(bars.two, n);
         tc::tmem_load(r, mine + kY + tok0);
-#pragma unroll
-        for (int i = 0; i < kTokens; ++i) d[i] = r[i] * (-f[i] * g[i]);
-        to_lanes<3>(mine + kD + part * (kTokens / 2), 32, d);
-        ready(bars.third);
-        if (issuer) {
-            wait.done(bars.third, n);
-            if (wait.ok) {
-                issue<3, NT, 3, 4, DKP, W, true, 0>(tmem + kY, tmem + kD, 32, k, TILE);
-                tc::commit_one(tc::smem_addr(&bars.three));
-            }
-        }
-        __syncwarp();
         if (kept_here) keep_row(scratch + a.p.y + hv * a.p.kept_bytes, col, 8, part * (kTokens / 8), r);
+        each(gates + kFirst + tok0, [&](int i, float f) { r[i] *= -f; });
+        each(gates + kBeta + tok0, [&](int i, float g) { r[i] *= g; });
+        to_lanes<3>(mine + kD + part * (kTokens / 2), 32, r);
+        ready(bars.third);
         wait.done(bars.three, n);
-        if (issuer && wait.ok && n + stages < chunks)
-            load_stage(a, st, base + at * st.bytes, tc::smem_addr(&bars.tiles[at]), kept, a.p.xu, s.slot + chunk - stages, h);
-        __syncwarp();
 #pragma unroll
         for (int w = 0; w < OWN / 16; ++w) {
             float y[16], z[16];
