@@ -29,12 +29,11 @@
 #include <cmath>
 
 #include "delta_common.cuh"
+#include "tc_one.cuh"
 
 namespace dendsn {
 using namespace delta;
 namespace {
-
-constexpr int kWarps = 8;
 
 // 8 neighbours of a row from `at` on, zeros behind its end.
 template <typename T>
@@ -216,320 +215,324 @@ __global__ void __launch_bounds__(128) delta_prepare_kernel(const __grid_constan
 }
 
 // ------------------------------------------------------------------ gradients of q, k and the gates
-// The pair of values of a lane in block (column block c, token block n) of a slice of `warps` * 16
-// columns: the sum of its terms.
-template <int NT>
-__device__ __forceinline__ float2 pair_of(const uint8_t *tile, size_t term, int cell) {
-    float2 r = make_float2(0.f, 0.f);
-#pragma unroll
-    for (int n = NT - 1; n >= 0; --n) {
-        const uint32_t w = *reinterpret_cast<const uint32_t *>(tile + n * term + cell * kCell + (threadIdx.x & 31) * 4);
-        r.x += bf16_low(w), r.y += bf16_high(w);
-    }
-    return r;
-}
-// Columns of v that a round takes, and the places of their tiles in a stage.
+// Columns of v that a round takes, and places in shared memory. A round's tiles have rows along v: go and y side by
+// side (16 blocks a row: both are the left factor of A and C at once), e, the states.
 constexpr int kRound = 32;
 template <int NT, int DKP>
 struct Parts {
     static constexpr int FEW = NT == 1 ? 2 : 3;           // terms where a bfloat16 comes of it
-    // a stage: float32 blocks of the states and of e and y, tiles of go and v
-    static constexpr uint32_t state = kRound * DKP * 2, values = kRound * C * 2;      // bytes of a term
-    static constexpr uint32_t s = 0, d = s + 2 * state, y = d + 2 * state, e = y + 2 * values, go = e + 2 * values,
-                              v = go + NT * values, bytes = v + NT * values;
-    // the round's tiles of the former, as terms
-    static constexpr uint32_t ts = 2 * bytes, td = ts + 3 * state, ty = td + FEW * state, te = ty + FEW * values, tiles_end = te + 3 * values;
-    static constexpr uint32_t keys = NT * C * DKP * 2;
-    // k and q: behind the tiles, or (three terms) where the stages were when the rounds are over; the
-    // square matrices of the chunk: where the first stage, or the tiles were
-    static constexpr uint32_t key_at = NT == 1 ? tiles_end : 0, square_at = NT == 1 ? 0 : ts, end = NT == 1 ? tiles_end + 2 * keys : tiles_end;
-    static_assert(NT == 1 ? 2 * kSquare <= 2 * bytes : 2 * keys <= 2 * bytes && 2 * kSquare <= end - ts, "what is laid over fits");
+    static constexpr uint32_t pair = kRound / 8 * 16 * kCell, error = kRound / 8 * 8 * kCell, state = kRound * DKP * 2;     // bytes of a term
+    static constexpr uint32_t t = 0, e = t + FEW * pair, s = e + 3 * error, d = s + 3 * state, key = d + FEW * state;
+    static constexpr uint32_t keys = NT * C * DKP * 2, end = key + 2 * keys + kCell * 8;    // (64 places: left factors read past their rows)
+    // the square matrices of the chunk, where the rounds' tiles were
+    static constexpr uint32_t a = 0, c = kSquare;
+    static_assert(c + FEW * (kSquare / 3) <= key, "what is laid over fits");
 };
-// Up to CELLS float32 blocks as tiles of N terms, by all of a block's threads.
-template <int N, int CELLS>
-__device__ __forceinline__ void tiles_from(uint8_t *to, uint32_t term, const uint8_t *from, int cells) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+// 8 values as bfloat16 terms, 16 bytes each.
+template <int N>
+__device__ __forceinline__ void put_terms(uint8_t *to, uint32_t term, const float (&v)[8]) {
+    uint32_t q[4][N];
 #pragma unroll
-    for (int i = 0; i < CELLS / kWarps; ++i) {
-        const int c = warp + i * kWarps;
-        if (c >= cells) break;
-        const float2 v = *reinterpret_cast<const float2 *>(from + c * kWide + lane * 8);
-        uint32_t q[N];
-        split<N>(q, v.x, v.y);
+    for (int i = 0; i < 4; ++i) split<N>(q[i], v[2 * i], v[2 * i + 1]);
 #pragma unroll
-        for (int m = 0; m < N; ++m) *reinterpret_cast<uint32_t *>(to + m * term + c * kCell + lane * 4) = q[m];
+    for (int m = 0; m < N; ++m) *reinterpret_cast<uint4 *>(to + m * term) = make_uint4(q[0][m], q[1][m], q[2][m], q[3][m]);
+}
+__device__ __forceinline__ void floats(float (&v)[8], const uint8_t *from) {
+    uint32_t q[8];
+    tc::load32(q, from);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(q[i]);
+}
+// 8 values of NT terms, as they lie in a tile.
+template <int NT>
+struct Eight {
+    uint4 r[NT];
+    __device__ __forceinline__ void load(const uint8_t *from, size_t term) {
+#pragma unroll
+        for (int m = 0; m < NT; ++m) r[m] = *reinterpret_cast<const uint4 *>(from + m * term);
     }
+    __device__ __forceinline__ void get(float (&v)[8]) const {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = 0.f;
+#pragma unroll
+        for (int m = NT - 1; m >= 0; --m) {
+            const uint32_t q[4] = {r[m].x, r[m].y, r[m].z, r[m].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[2 * i] += bf16_low(q[i]), v[2 * i + 1] += bf16_high(q[i]);
+        }
+    }
+};
+// Sums over a warp's lanes of 16 values each: lane l returns that of value l / 2.
+__device__ __forceinline__ float sums_of(float (&v)[16]) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int n = 8; n; n >>= 1) {
+        const bool up = lane & (2 * n);
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            const float other = __shfl_xor_sync(0xffffffffu, up ? v[i] : v[i + n], 2 * n);
+            v[i] = (up ? v[i + n] : v[i]) + other;
+        }
+    }
+    return v[0] + __shfl_xor_sync(0xffffffffu, v[0], 1);
 }
 
-// A block for a chunk and value head: all products over v in rounds of 32 columns, then those within the
-// chunk. Eight warps: 16 tokens each, one half of Dk (and of the square matrices' columns). Gradients of
-// shared heads go out in float32 for each value head and are added up by delta_join_kernel.
+// A block for a chunk and value head. Products with places of Dk as rows (lanes of tensor memory) and tokens as
+// columns: S go, S y and D e, over rounds of 32 columns of v, with A and C's sums beside them (rows: tokens of go, of
+// y); then those within the chunk. A warp has 8 tokens of a round's go, v, y and e, a lane one column of v. Two blocks
+// share an SM (bfloat16), so that one's loads go on beside the other's products. Gradients of shared heads go out in
+// float32 for each value head and are added up by delta_join_kernel.
+// Columns of tensor memory:
+constexpr uint32_t kGoS = 0, kYS = 64, kED = 128, kAE = 192, kGradColumns = 256;
 template <typename T, int DKP>
-__global__ void __launch_bounds__(kWarps * 32, 1) delta_gradients_kernel(const __grid_constant__ Args a, const uint8_t *kept, uint8_t *scratch,
-                                                                         T *gq, T *gk, T *gv, float *ggate, float *gbeta) {
-    constexpr int NT = sizeof(T) == 2 ? 1 : 3, W = DKP / 8, TILE = 64 * DKP * 2, SQ = kSquare / 3, N8 = DKP / 16;
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) delta_gradients_kernel(const __grid_constant__ Args a, const uint8_t *kept, uint8_t *scratch,
+                                                                                       T *gq, T *gk, T *gv, float *ggate, float *gbeta) {
+    constexpr int NT = sizeof(T) == 2 ? 1 : 3, W = DKP / 8, TILE = C * DKP * 2, SQ = kSquare / 3;
     using P = Parts<NT, DKP>;
     constexpr int FEW = P::FEW;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ __align__(8) uint64_t bars[3];
+    __shared__ uint64_t keys_bar, done_bar;
+    __shared__ uint32_t where;
     __shared__ __align__(16) float gates[kGateFloats];
-    __shared__ float qdot[2][C], edot[C], vdot[C], sums[kWarps];
+    __shared__ float qdot[4][C], edot[C], vdot[C], sums[8];
     pdl_begin();
     int b, chunk;
     Sequence s;
     if (!locate(a, blockIdx.x, &b, &chunk, &s)) return;
-    const int h = blockIdx.y, group = a.Hv / a.Hk, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane / 4, t = lane % 4;
-    const int wr = warp & 3, wh = warp >> 2;
+    const int h = blockIdx.y, group = a.Hv / a.Hk, lane = threadIdx.x & 31, warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
     const int64_t hv = (int64_t)blockIdx.x * a.Hv + h, hk = (int64_t)blockIdx.x * a.Hk + h / group;
-    const uint32_t base = tc::smem_addr(smem), bar = tc::smem_addr(bars);
-    const int rounds = (a.p.DVP + kRound - 1) / kRound;
-    const uint8_t *kimage = kept + a.p.k + hk * a.p.key_bytes, *qimage = kept + a.p.q + hk * a.p.key_bytes;
-    auto load = [&](int n) {
-        const uint32_t to = base + (n & 1) * P::bytes, on = bar + 8 * (n & 1);
-        const int v0 = n * kRound, count = min(kRound, a.p.DVP - v0);
-        const size_t term = (size_t)a.p.DVP * C * 2;
-        const uint32_t sb = count * DKP * 4, vb = count * C * 2;
-        tc::bar_expect(on, 2 * sb + (2 * NT + 4) * vb);
-        load_bytes(to + P::s, kept + a.p.s + hv * a.p.state_bytes + (size_t)v0 * DKP * 4, sb, on);
-        load_bytes(to + P::d, scratch + a.p.d + hv * a.p.state_bytes + (size_t)v0 * DKP * 4, sb, on);
-        load_bytes(to + P::y, scratch + a.p.y + hv * a.p.kept_bytes + (size_t)v0 * C * 4, 2 * vb, on);
-        load_bytes(to + P::e, kept + a.p.e + hv * a.p.kept_bytes + (size_t)v0 * C * 4, 2 * vb, on);
-        for (int m = 0; m < NT; ++m) {
-            load_bytes(to + P::go + m * P::values, scratch + a.p.go + hv * a.p.value_bytes + m * term + (size_t)v0 * C * 2, vb, on);
-            load_bytes(to + P::v + m * P::values, kept + a.p.v + hv * a.p.value_bytes + m * term + (size_t)v0 * C * 2, vb, on);
-        }
-    };
-    auto load_keys = [&] {
-        tc::bar_expect(bar + 16, 2 * P::keys);
-        load_bytes(base + P::key_at, kimage, P::keys, bar + 16);
-        load_bytes(base + P::key_at + P::keys, qimage, P::keys, bar + 16);
-    };
+    const uint32_t base = tc::smem_addr(smem), keys_at = tc::smem_addr(&keys_bar), done = tc::smem_addr(&done_bar);
     if (threadIdx.x == 0) {
-        for (int i = 0; i < 3; ++i) tc::bar_init(bar + 8 * i, 1);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        for (int n = 0; n < min(2, rounds); ++n) load(n);
-        if (NT == 1) load_keys();
+        tc::bar_init(keys_at, 1);
+        tc::bar_init(done, 1);
+        tc::bar_init_fence();
+        tc::bar_expect(keys_at, 2 * P::keys);
+        load_bytes(base + P::key, kept + a.p.k + hk * a.p.key_bytes, P::keys, keys_at);
+        load_bytes(base + P::key + P::keys, kept + a.p.q + hk * a.p.key_bytes, P::keys, keys_at);
     }
+    if (warp == 0) tc::tmem_alloc_one(tc::smem_addr(&where), kGradColumns);
     const float *gin = reinterpret_cast<const float *>(kept + a.p.gates) + hv * kGateFloats;
-    for (int i = threadIdx.x; i < kGateFloats; i += kWarps * 32) gates[i] = gin[i];
+    for (int i = threadIdx.x; i < kGateFloats; i += 256) gates[i] = gin[i];
+    if (NT == 1)       // go has no second term
+        for (int i = threadIdx.x; i < kRound / 8 * 64; i += 256)
+            *reinterpret_cast<uint4 *>(smem + P::t + P::pair + (i / 64 * 16 * kCell) + i % 64 * 16) = make_uint4(0, 0, 0, 0);
+    tc::fence_before_sync();
     __syncthreads();
+    tc::fence_after_sync();
+    const uint32_t tmem = where;
     const int left = min(C, s.length - chunk * C);
     const int64_t row = s.row + (int64_t)chunk * C * s.step;
-    const float2 mybeta = *reinterpret_cast<const float2 *>(gates + kBeta + warp * 8 + 2 * t);
 
     // the state behind the chunk: the next chunk's, or the sequence's last
     const bool ends = (chunk + 1) * C >= s.length;
     const uint8_t *next = ends ? kept + a.p.end + ((int64_t)b * a.Hv + h) * a.p.state_bytes : kept + a.p.s + (hv + a.Hv) * a.p.state_bytes;
-    float goS[N8][4] = {}, yS[N8][4] = {}, eD[N8][4] = {}, A[4][4] = {}, E[4][4] = {};
-    float ey[2] = {}, vy[2] = {}, tail = 0.f;
+    const uint8_t *sat = kept + a.p.s + hv * a.p.state_bytes, *dat = scratch + a.p.d + hv * a.p.state_bytes;
+    const uint8_t *yat = scratch + a.p.y + hv * a.p.kept_bytes, *eat = kept + a.p.e + hv * a.p.kept_bytes;
+    const uint8_t *goat = scratch + a.p.go + hv * a.p.value_bytes, *vat = kept + a.p.v + hv * a.p.value_bytes;
+    const size_t term = (size_t)a.p.DVP * C * 2;
+    const int rounds = (a.p.DVP + kRound - 1) / kRound, own = lane / 8 * 8 + warp;     // own: the lane's block of 8 columns and 8 tokens
+    float ey[8] = {}, vy[8] = {}, tail = 0.f;
     bool ok = true;
     for (int n = 0; n < rounds; ++n) {
-        const uint8_t *mem = smem + (n & 1) * P::bytes;
-        const uint32_t here = base + (n & 1) * P::bytes;
         const int count = min(kRound, a.p.DVP - n * kRound);
-        constexpr int OWN = kRound / 8 * W / kWarps;       // float32 blocks of a state that a warp looks at
-        float2 behind[OWN];
-#pragma unroll
-        for (int i = 0; i < OWN; ++i)
-            if (warp + i * kWarps < count / 8 * W)
-                behind[i] = *reinterpret_cast<const float2 *>(next + ((size_t)n * kRound / 8 * W + warp + i * kWarps) * kWide + lane * 8);
-        ok = ok && tc::bar_wait(bar + 8 * (n & 1), n / 2 & 1);
-        tiles_from<3, kRound / 8 * W>(smem + P::ts, P::state, mem + P::s, count / 8 * W);
-        tiles_from<FEW, kRound / 8 * W>(smem + P::td, P::state, mem + P::d, count / 8 * W);
-        tiles_from<FEW, kRound>(smem + P::ty, P::values, mem + P::y, count);
-        tiles_from<3, kRound>(smem + P::te, P::values, mem + P::e, count);
-#pragma unroll
-        for (int i = 0; i < OWN; ++i) {
-            if (warp + i * kWarps >= count / 8 * W) break;
-            const float2 y = *reinterpret_cast<const float2 *>(mem + P::d + (warp + i * kWarps) * kWide + lane * 8);
-            tail = fmaf(behind[i].x, y.x, fmaf(behind[i].y, y.y, tail));
+        const bool here = lane < count;
+        constexpr int LOTS = kRound * W / 256;             // 8 places of a state each
+        float y[8] = {}, e[8] = {};
+        Eight<NT> go, v;
+        if (here) {
+            const size_t cell = (size_t)n * kRound + own;
+            floats(y, yat + cell * kWide + (lane & 7) * 32);
+            floats(e, eat + cell * kWide + (lane & 7) * 32);
+            go.load(goat + cell * kCell + (lane & 7) * 16, term);
+            v.load(vat + cell * kCell + (lane & 7) * 16, term);
         }
-        // e . y, v . y and the gradient of v: tokens warp * 8 + 2 t and the next
+        float S[LOTS][8], D[LOTS][8], behind[LOTS][8];
 #pragma unroll
-        for (int c = 0; c < kRound / 8; ++c) {
-            if (c >= count / 8) break;
-            const float2 y = *reinterpret_cast<const float2 *>(mem + P::y + (c * 8 + warp) * kWide + lane * 8);
-            const float2 e = *reinterpret_cast<const float2 *>(mem + P::e + (c * 8 + warp) * kWide + lane * 8);
-            const float2 v = pair_of<NT>(mem + P::v, P::values, c * 8 + warp);
-            ey[0] = fmaf(e.x, y.x, ey[0]), ey[1] = fmaf(e.y, y.y, ey[1]);
-            vy[0] = fmaf(v.x, y.x, vy[0]), vy[1] = fmaf(v.y, y.y, vy[1]);
-            const int col = n * kRound + c * 8 + g, tok = warp * 8 + 2 * t;
-            if (col < a.Dv && tok < left) put(gv + ((row + tok * s.step) * a.Hv + h) * a.Dv + col, mybeta.x * y.x);
-            if (col < a.Dv && tok + 1 < left) put(gv + ((row + (tok + 1) * s.step) * a.Hv + h) * a.Dv + col, mybeta.y * y.y);
+        for (int i = 0; i < LOTS; ++i) {
+            const int lot = threadIdx.x + i * 256;
+            if (lot < count * W) {
+                const size_t at = (size_t)n * kRound * W * 32 + lot * 32;
+                floats(S[i], sat + at);
+                floats(D[i], dat + at);
+                floats(behind[i], next + at);
+            }
         }
+        if (n) {       // the last round's products have read their tiles
+            ok = ok && tc::bar_wait(done, (n - 1) & 1);
+        }
+        if (here) {
+            uint8_t *to = smem + P::t + (lane / 8 * 16 + warp) * kCell + (lane & 7) * 16;
+#pragma unroll
+            for (int m = 0; m < NT; ++m) *reinterpret_cast<uint4 *>(to + m * P::pair) = go.r[m];
+            put_terms<FEW>(to + 8 * kCell, P::pair, y);
+            put_terms<3>(smem + P::e + own * kCell + (lane & 7) * 16, P::error, e);
+            float x[8];
+            v.get(x);
+            const int col = n * kRound + lane, tok0 = warp * 8;
+            T *to_v = gv + ((row + tok0 * s.step) * a.Hv + h) * a.Dv + col;
+#pragma unroll
+            for (int i = 0; i < 8; ++i, to_v += s.step * a.Hv * a.Dv) {
+                ey[i] = fmaf(e[i], y[i], ey[i]);
+                vy[i] = fmaf(x[i], y[i], vy[i]);
+                if (col < a.Dv && tok0 + i < left) put(to_v, gates[kBeta + tok0 + i] * y[i]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < LOTS; ++i) {
+            const int lot = threadIdx.x + i * 256;
+            if (lot < count * W) {
+                put_terms<3>(smem + P::s + lot * 16, P::state, S[i]);
+                put_terms<FEW>(smem + P::d + lot * 16, P::state, D[i]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) tail = fmaf(behind[i][j], D[i][j], tail);
+            }
+        }
+        tc::fence_tiles();
         __syncthreads();
-        for (int ks = 0; ks < count / 16; ++ks) {
-            uint32_t ago[NT][4], ay[FEW][4], ae[FEW][4];
-#pragma unroll
-            for (int m = 0; m < NT; ++m) left_columns(ago[m], here + P::go + m * P::values, 8, 2 * ks, 2 * wr);
-#pragma unroll
-            for (int m = 0; m < FEW; ++m) {
-                left_columns(ay[m], base + P::ty + m * P::values, 8, 2 * ks, 2 * wr);
-                left_columns(ae[m], base + P::te + m * P::values, 8, 2 * ks, 2 * wr);
+        if (warp == 0 && ok && tc::elected()) {
+            tc::fence_after_sync();
+            const int steps = count / 16;
+            const uint32_t go_at = base + P::t, y_at = go_at + 8 * kCell;
+            tc::issue_tiles<3, NT, 3, 64, W, 16, true, 0>(tmem + kGoS, base + P::s, P::state, go_at, P::pair, steps, n);
+            tc::issue_tiles<3, FEW, FEW, 64, W, 16, true, 0>(tmem + kYS, base + P::s, P::state, y_at, P::pair, steps, n);
+            tc::issue_tiles<FEW, 3, FEW, 64, W, 8, true, 0>(tmem + kED, base + P::d, P::state, base + P::e, P::error, steps, n);
+            if (NT == 1) {
+                tc::issue_tiles<1, 1, 1, 64, 16, 8, true, 0>(tmem + kAE, go_at + P::pair, P::pair, base + P::e, P::error, steps, n);
+                tc::issue_tiles<1, 3, 3, 64, 16, 8, true, 0>(tmem + kAE, go_at, P::pair, base + P::e, P::error, steps, true);
+            } else {
+                tc::issue_tiles<FEW, 3, 3, 64, 16, 8, true, 0>(tmem + kAE, go_at, P::pair, base + P::e, P::error, steps, n);
             }
-#pragma unroll
-            for (int p = 0; p < N8 / 2; ++p) {
-                if ((wh * N8 + 2 * p) * 8 >= a.Dk) break;
-                uint32_t f[3][4], f2[FEW][4];
-#pragma unroll
-                for (int m = 0; m < 3; ++m) right_columns(f[m], base + P::ts + m * P::state, W, 2 * ks, wh * N8 + 2 * p);
-                products<NT, 3, 3>(goS[2 * p], goS[2 * p + 1], ago, f);
-                products<FEW, 3, FEW>(yS[2 * p], yS[2 * p + 1], ay, f);
-#pragma unroll
-                for (int m = 0; m < FEW; ++m) right_columns(f2[m], base + P::td + m * P::state, W, 2 * ks, wh * N8 + 2 * p);
-                products<FEW, FEW, FEW>(eD[2 * p], eD[2 * p + 1], ae, f2);
-            }
-#pragma unroll
-            for (int p = 0; p < 2; ++p) {
-                if (2 * wh + p > wr) break;
-                uint32_t f[3][4];
-#pragma unroll
-                for (int m = 0; m < 3; ++m) right_columns(f[m], base + P::te + m * P::values, 8, 2 * ks, 4 * wh + 2 * p);
-                products<NT, 3, 3>(A[2 * p], A[2 * p + 1], ago, f);
-                products<FEW, 3, FEW>(E[2 * p], E[2 * p + 1], ay, f);
-            }
+            tc::commit_one(done);
         }
-        __syncthreads();
-        if (threadIdx.x == 0 && ok && n + 2 < rounds) load(n + 2);
+        __syncwarp();
     }
-    if (NT > 1 && threadIdx.x == 0 && ok) load_keys();
+    // e . y and v . y: over the columns, which are the lanes
 #pragma unroll
-    for (int o = 4; o < 32; o <<= 1)
+    for (int o = 16; o; o >>= 1)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < 8; ++i) {
             ey[i] += __shfl_xor_sync(0xffffffffu, ey[i], o);
             vy[i] += __shfl_xor_sync(0xffffffffu, vy[i], o);
         }
-    if (g == 0) {
-        edot[warp * 8 + 2 * t] = ey[0], edot[warp * 8 + 2 * t + 1] = ey[1];
-        vdot[warp * 8 + 2 * t] = mybeta.x * vy[0], vdot[warp * 8 + 2 * t + 1] = mybeta.y * vy[1];
-    }
-    // the square matrices, as terms
-    const uint32_t At = base + P::square_at, Ct = At + kSquare;
+    if (lane == 0)
 #pragma unroll
-    for (int n = 0; n < 4; ++n)
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int i = wr * 16 + half * 8 + g, j = wh * 32 + n * 8 + 2 * t;
-            float x[2], c[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const float w = j + e <= i ? between(gates, i, j + e) * gates[kBeta + j + e] : 0.f;
-                x[e] = j + e <= i ? a.scale * w * A[n][2 * half + e] : 0.f;
-                c[e] = j + e < i ? -gates[kBeta + i] * w * E[n][2 * half + e] : 0.f;
-            }
-            uint32_t xs[3], cs[3];
-            split<3>(xs, x[0], x[1]);
-            split<3>(cs, c[0], c[1]);
-            uint8_t *to = smem + P::square_at + ((wr * 2 + half) * 8 + wh * 4 + n) * kCell + lane * 4;
-#pragma unroll
-            for (int m = 0; m < 3; ++m) {
-                *reinterpret_cast<uint32_t *>(to + m * SQ) = xs[m];
-                *reinterpret_cast<uint32_t *>(to + kSquare + m * SQ) = cs[m];
-            }
-        }
-    __syncthreads();
-    ok = ok && tc::bar_wait(bar + 16, 0);
-    const uint8_t *qm = smem + P::key_at + P::keys;
-    const uint32_t kt = base + P::key_at, qt = kt + P::keys;
-#pragma unroll
-    for (int n = 0; n < N8; ++n)
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int i = wr * 16 + half * 8 + g;
-            const float f = gates[kFirst + i], bt = gates[kBeta + i], re = gates[kRest + i];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                float &x = goS[n][2 * half + e], &y = yS[n][2 * half + e];
-                x *= a.scale * f;
-                y = bt * fmaf(-f, y, re * eD[n][2 * half + e]);
-            }
-        }
-#pragma unroll
-    for (int ks = 0; ks < 4; ++ks) {
-        if (ks <= wr) {        // A k and C k
-            uint32_t la[3][4], lc[FEW][4];
-#pragma unroll
-            for (int m = 0; m < 3; ++m) left_rows(la[m], At + m * SQ, 8, 2 * wr, 2 * ks);
-#pragma unroll
-            for (int m = 0; m < FEW; ++m) left_rows(lc[m], Ct + m * SQ, 8, 2 * wr, 2 * ks);
-#pragma unroll
-            for (int p = 0; p < N8 / 2; ++p) {
-                if ((wh * N8 + 2 * p) * 8 >= a.Dk) break;
-                uint32_t f[NT][4];
-#pragma unroll
-                for (int m = 0; m < NT; ++m) right_columns(f[m], kt + m * TILE, W, 2 * ks, wh * N8 + 2 * p);
-                products<3, NT, 3>(goS[2 * p], goS[2 * p + 1], la, f);
-                products<FEW, NT, FEW>(yS[2 * p], yS[2 * p + 1], lc, f);
-            }
-        }
-        if (ks >= wr) {        // A^T q and C^T k
-            uint32_t la[FEW][4], lc[FEW][4];
-#pragma unroll
-            for (int m = 0; m < FEW; ++m) {
-                left_columns(la[m], At + m * SQ, 8, 2 * ks, 2 * wr);
-                left_columns(lc[m], Ct + m * SQ, 8, 2 * ks, 2 * wr);
-            }
-#pragma unroll
-            for (int p = 0; p < N8 / 2; ++p) {
-                if ((wh * N8 + 2 * p) * 8 >= a.Dk) break;
-                uint32_t f[NT][4];
-#pragma unroll
-                for (int m = 0; m < NT; ++m) right_columns(f[m], qt + m * TILE, W, 2 * ks, wh * N8 + 2 * p);
-                products<FEW, NT, FEW>(yS[2 * p], yS[2 * p + 1], la, f);
-#pragma unroll
-                for (int m = 0; m < NT; ++m) right_columns(f[m], kt + m * TILE, W, 2 * ks, wh * N8 + 2 * p);
-                products<FEW, NT, FEW>(yS[2 * p], yS[2 * p + 1], lc, f);
-            }
-        }
-    }
-    if (!ok)
-#pragma unroll
-        for (int n = 0; n < N8; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) goS[n][e] = yS[n][e] = tail = __int_as_float(0x7fffffff);
-    float *parts = reinterpret_cast<float *>(scratch + a.p.parts);
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        const int i = wr * 16 + half * 8 + g;
-        const int64_t tok = row + i * s.step;
-        float dot = 0.f;
-#pragma unroll
-        for (int n = 0; n < N8; ++n) {
-            const float2 q = pair_of<NT>(qm, TILE, (wr * 2 + half) * W + wh * N8 + n);
-            dot = fmaf(q.x, goS[n][2 * half], fmaf(q.y, goS[n][2 * half + 1], dot));
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int d = (wh * N8 + n) * 8 + 2 * t + e;
-                if (i >= left || d >= a.Dk) continue;
-                if (group == 1) {
-                    put(gq + (tok * a.Hk + h) * a.Dk + d, goS[n][2 * half + e]);
-                    put(gk + (tok * a.Hk + h) * a.Dk + d, yS[n][2 * half + e]);
-                } else {
-                    parts[(tok * a.Hv + h) * a.Dk + d] = goS[n][2 * half + e];
-                    parts[((a.p.tokens + tok) * a.Hv + h) * a.Dk + d] = yS[n][2 * half + e];
-                }
-            }
-        }
-        dot += __shfl_xor_sync(0xffffffffu, dot, 1);
-        dot += __shfl_xor_sync(0xffffffffu, dot, 2);
-        if (t == 0) qdot[wh][i] = dot;
-    }
+        for (int i = 0; i < 8; ++i) edot[warp * 8 + i] = ey[i], vdot[warp * 8 + i] = gates[kBeta + warp * 8 + i] * vy[i];
 #pragma unroll
     for (int o = 16; o; o >>= 1) tail += __shfl_xor_sync(0xffffffffu, tail, o);
     if (lane == 0) sums[warp] = tail;
+
+    ok = ok && tc::bar_wait(done, (rounds - 1) & 1);
+    tc::fence_after_sync();
+    const int quarter = warp & 3, half = warp >> 2;
+    const uint32_t mine = tmem + ((uint32_t)quarter << 21);
+    // the square matrices as terms: rows 0 to 63 of the sums are A's, the others C's
+    const int i = (quarter & 1) * 32 + lane;
+    const bool isc = quarter >= 2;
+#pragma unroll
+    for (int part = 0; part < 2; ++part) {
+        const int j0 = half * 32 + part * 16;
+        float x[16];
+        tc::tmem_load(x, mine + kAE + j0);
+        const float scale = isc ? -gates[kBeta + i] : a.scale;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            const bool in = j0 + j < i + (isc ? 0 : 1);
+            x[j] = in ? scale * between(gates, i, j0 + j) * gates[kBeta + j0 + j] * x[j] : 0.f;
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            uint8_t *to = smem + (isc ? P::c : P::a) + (i / 8 * 8 + j0 / 8 + c) * kCell + (i & 7) * 16;
+            const float z[8] = {x[8 * c], x[8 * c + 1], x[8 * c + 2], x[8 * c + 3], x[8 * c + 4], x[8 * c + 5], x[8 * c + 6], x[8 * c + 7]};
+            if (isc) put_terms<FEW>(to, SQ, z);
+            else put_terms<3>(to, SQ, z);
+        }
+    }
+    // what has come through the states, scaled, in place
+#pragma unroll
+    for (int part = 0; part < 2; ++part) {
+        const int j0 = half * 32 + part * 16;
+        float x[16], z[16];
+        tc::tmem_load(x, mine + kGoS + j0);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) x[j] *= a.scale * gates[kFirst + j0 + j];
+        tc::tmem_put(mine + kGoS + j0, x);
+        tc::tmem_load(x, mine + kYS + j0);
+        tc::tmem_load(z, mine + kED + j0);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) x[j] = gates[kBeta + j0 + j] * fmaf(-gates[kFirst + j0 + j], x[j], gates[kRest + j0 + j] * z[j]);
+        tc::tmem_put(mine + kYS + j0, x);
+    }
+    tc::tmem_stored();
+    tc::fence_tiles();
+    tc::fence_before_sync();
     __syncthreads();
+    ok = ok && tc::bar_wait(keys_at, 0);
+    if (warp == 0 && ok && tc::elected()) {
+        tc::fence_after_sync();
+        const uint32_t k = base + P::key, q = k + P::keys;
+        tc::issue_tiles<NT, 3, 3, 64, W, 8, false, 1>(tmem + kGoS, k, TILE, base + P::a, SQ, 4, true);
+        tc::issue_tiles<NT, FEW, FEW, 64, W, 8, true, 2>(tmem + kYS, q, TILE, base + P::a, SQ, 4, true);
+        tc::issue_tiles<NT, FEW, FEW, 64, W, 8, false, 1>(tmem + kYS, k, TILE, base + P::c, SQ, 4, true);
+        tc::issue_tiles<NT, FEW, FEW, 64, W, 8, true, 2>(tmem + kYS, k, TILE, base + P::c, SQ, 4, true);
+        tc::commit_one(done);
+    }
+    __syncwarp();
+    ok = ok && tc::bar_wait(done, rounds & 1);
+    tc::fence_after_sync();
+    const int d = quarter * 32 + lane;
+    const uint8_t *qm = smem + P::key + P::keys + d / 8 * kCell + (d & 7) * 2;
+    float *parts = reinterpret_cast<float *>(scratch + a.p.parts);
+    if (quarter * 32 < DKP)
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+            const int j0 = half * 32 + part * 16;
+            const int64_t tok = row + j0 * s.step;
+            float x[16], z[16];
+            tc::tmem_load(x, mine + kGoS + j0);
+            tc::tmem_load(z, mine + kYS + j0);
+            if (!ok)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) x[j] = z[j] = __int_as_float(0x7fffffff);
+            if (d < a.Dk) {
+                if (group == 1) {
+                    T *tq = gq + (tok * a.Hk + h) * a.Dk + d, *tk = gk + (tok * a.Hk + h) * a.Dk + d;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j, tq += s.step * a.Hk * a.Dk, tk += s.step * a.Hk * a.Dk)
+                        if (j0 + j < left) put(tq, x[j]), put(tk, z[j]);
+                } else {
+                    float *tq = parts + (tok * a.Hv + h) * a.Dk + d, *tk = tq + a.p.tokens * a.Hv * a.Dk;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j, tq += s.step * a.Hv * a.Dk, tk += s.step * a.Hv * a.Dk)
+                        if (j0 + j < left) *tq = x[j], *tk = z[j];
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                float v = 0.f;
+#pragma unroll
+                for (int m = NT - 1; m >= 0; --m)
+                    v += value(reinterpret_cast<const __nv_bfloat16 *>(qm + m * TILE + ((j0 + j) / 8 * W) * kCell + ((j0 + j) & 7) * 16));
+                x[j] *= v;
+            }
+            const float dot = sums_of(x);
+            if (!(lane & 1)) qdot[quarter][j0 + lane / 2] = dot;
+        }
+    else
+        qdot[quarter][half * 32 + lane] = 0.f;
     if (!ok) let_land();
+    tc::fence_before_sync();
+    __syncthreads();
+    if (warp == 0) tc::tmem_free_one(tmem, kGradColumns);
     if (warp) return;
     // the gates: sums from each token to the chunk's end, and what comes back through the state
-    double behind_all = 0.0, mine[2];
-    for (int i = 0; i < kWarps; ++i) behind_all += (double)sums[i];
+    double behind_all = 0.0, at[2];
+    for (int w = 0; w < 8; ++w) behind_all += (double)sums[w];
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-        const int i = 2 * lane + e;
-        mine[e] = (double)qdot[0][i] + (double)qdot[1][i] - (double)vdot[i];
+        const int j = 2 * lane + e;
+        at[e] = ((double)qdot[0][j] + (double)qdot[1][j]) + ((double)qdot[2][j] + (double)qdot[3][j]) - (double)vdot[j];
     }
-    double behind = mine[0] + mine[1];
+    double behind = at[0] + at[1];
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const double down = __shfl_down_sync(0xffffffffu, behind, o);
@@ -537,13 +540,13 @@ __global__ void __launch_bounds__(kWarps * 32, 1) delta_gradients_kernel(const _
     }
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-        const int i = 2 * lane + e;
-        if (i >= left) continue;
-        const int64_t at = (row + i * s.step) * a.Hv + h;
+        const int j = 2 * lane + e;
+        if (j >= left) continue;
+        const int64_t to = (row + j * s.step) * a.Hv + h;
         // a decay that is 0 in float32 (exp(-104)) has no gradient
-        const float gate = gates[kHigh + i] - (i ? gates[kHigh + i - 1] : 0.f) + (gates[kLow + i] - (i ? gates[kLow + i - 1] : 0.f));
-        ggate[at] = gate < -104.f ? 0.f : (float)(behind_all + behind - (e ? mine[0] : 0.0));
-        gbeta[at] = edot[i];
+        const float gate = gates[kHigh + j] - (j ? gates[kHigh + j - 1] : 0.f) + (gates[kLow + j] - (j ? gates[kLow + j - 1] : 0.f));
+        ggate[to] = gate < -104.f ? 0.f : (float)(behind_all + behind - (e ? at[0] : 0.0));
+        gbeta[to] = edot[j];
     }
 }
 
@@ -762,7 +765,7 @@ cudaError_t run_backward(const Args &a, const void *go, const float *glast, cons
     constexpr size_t smem = Parts<NT, DKP>::end;
     e = room(delta_gradients_kernel<T, DKP>, smem);
     if (e == cudaSuccess)
-        e = seq_launch(delta_gradients_kernel<T, DKP>, chunks, kWarps * 32, smem, s, 1, a, kept, scratch, (T *)gq, (T *)gk, (T *)gv, ggate, gbeta);
+        e = seq_launch(delta_gradients_kernel<T, DKP>, chunks, 256, smem, s, 1, a, kept, scratch, (T *)gq, (T *)gk, (T *)gv, ggate, gbeta);
     ++*launches;
     if (a.Hv > a.Hk && e == cudaSuccess) {
         const int vec = a.Dk % 4 == 0 ? 4 : 1;

@@ -158,31 +158,6 @@ __device__ __forceinline__ void keep_values(uint8_t *to, uint32_t term, int row,
     }
 }
 
-// Products of NA terms in tensor memory (STEPS blocks of 16 summed places, 8 columns each) and NB terms in shared
-// memory, those whose terms' numbers add up to less than KEEP, the smallest first. TURNED: the right factor's rows
-// run along the summed index, else along the other one. WIDTH: blocks of a row. TRI: of a lower triangle's rows only
-// those from the step on (1), of its columns only those up to the step (2).
-template <int NA, int NB, int KEEP, int STEPS, int N, int WIDTH, bool TURNED, int TRI>
-__device__ __forceinline__ void issue(uint32_t d, uint32_t a, uint32_t aterm, uint32_t b, uint32_t bterm) {
-    const tc::Blocks tile = TURNED ? tc::Blocks(b, WIDTH * kCell, kCell) : tc::Blocks(b, kCell, WIDTH * kCell);
-    bool add = false;
-#pragma unroll
-    for (int sum = KEEP - 1; sum >= 0; --sum)
-#pragma unroll
-        for (int i = 0; i < NA; ++i) {
-            const int j = sum - i;
-            if (j < 0 || j >= NB) continue;
-#pragma unroll
-            for (int n = 0; n < STEPS; ++n) {
-                const int s = TRI == 2 ? STEPS - 1 - n : n;
-                const int from = TRI == 1 ? 16 * s : 0, count = TRI == 1 ? N - 16 * s : TRI == 2 ? 16 * (s + 1) : N;
-                tc::mma_lanes(d + from, a + i * aterm + 8 * s, tile.at(j * bterm + (TURNED ? 2 * s * WIDTH : from / 8 * WIDTH + 2 * s) * kCell),
-                              tc::product_of(128, count, false, TURNED), add);
-                add = true;
-            }
-        }
-}
-
 struct Bars {
     uint64_t tiles[2];                     // a stage's tiles have come
     uint64_t first, second, third;         // all warps have written a round's left factors
@@ -201,13 +176,6 @@ struct Waits {
 // 96 registers a thread at the launch (the compiler's choice for 640 threads), 104 and 64 after: as many in all.
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 104;"); }
 __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 64;"); }
-// One lane of a whole warp, in a way that leaves the compiler's uniform registers usable.
-__device__ __forceinline__ bool elected() {
-    uint32_t yes;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
-    return yes != 0;
-}
-
 // What both walks begin and end with.
 __device__ __forceinline__ uint32_t begin(Bars &bars, uint32_t &where) {
     if (threadIdx.x == 0) {
@@ -257,7 +225,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_forward_kernel(const __grid
     Waits wait{true};
     if (warp >= kWarps) {
         fewer_registers();
-        if (warp == kWarps && elected()) {
+        if (warp == kWarps && tc::elected()) {
             const uint32_t bar = tc::smem_addr(bars.tiles);
             for (int n = 0; n < min(stages, chunks); ++n) load_stage(a, st, base + n * st.bytes, bar + 8 * n, kept, a.p.xe, s.slot + n, h);
             // the stage of chunk n is free when all that reads it is done
@@ -271,19 +239,19 @@ __global__ void __launch_bounds__(kThreads, 1) delta_forward_kernel(const __grid
                 wait(bars.tiles[n % stages], n / stages);
                 wait.done(bars.first, n);
                 if (!wait.ok) break;
-                issue<3, NT, 3, DKP / 16, 64, W, false, 0>(tmem + kSeen, tmem + kState, DKP / 2, k, TILE);
+                tc::issue<3, NT, 3, DKP / 16, 64, W, false, 0>(tmem + kSeen, tmem + kState, DKP / 2, k, TILE);
                 tc::commit_one(tc::smem_addr(&bars.one));
-                issue<3, NT, FEW, DKP / 16, 64, W, false, 0>(tmem + kSeen + 64, tmem + kState, DKP / 2, q, TILE);
+                tc::issue<3, NT, FEW, DKP / 16, 64, W, false, 0>(tmem + kSeen + 64, tmem + kState, DKP / 2, q, TILE);
                 if (n && stages > 1) refill(n - 1);
                 wait.done(bars.second, n);
                 if (!wait.ok) break;
-                issue<3, 3, 3, 4, 64, 8, false, 1>(tmem + kOut, tmem + kError, 32, x, SQ);
+                tc::issue<3, 3, 3, 4, 64, 8, false, 1>(tmem + kOut, tmem + kError, 32, x, SQ);
                 tc::commit_one(tc::smem_addr(&bars.two));
                 wait.done(bars.third, n);
                 if (!wait.ok) break;
-                issue<3, NT, 3, 4, DKP, W, true, 0>(tmem + kSeen, tmem + kState, 32, k, TILE);
+                tc::issue<3, NT, 3, 4, DKP, W, true, 0>(tmem + kSeen, tmem + kState, 32, k, TILE);
                 tc::commit_one(tc::smem_addr(&bars.three));
-                issue<3, FEW, FEW, 4, 64, 8, false, 1>(tmem + kOut, tmem + kError, 32, p, SQ);
+                tc::issue<3, FEW, FEW, 4, 64, 8, false, 1>(tmem + kOut, tmem + kError, 32, p, SQ);
                 tc::commit_one(tc::smem_addr(&bars.four));
                 if (stages == 1) refill(n);
             }
@@ -401,7 +369,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_backward_kernel(const __gri
     Waits wait{true};
     if (warp >= kWarps) {
         fewer_registers();
-        if (warp == kWarps && elected()) {
+        if (warp == kWarps && tc::elected()) {
             const uint32_t bar = tc::smem_addr(bars.tiles);
             for (int n = 0; n < min(stages, chunks); ++n) load_stage(a, st, base + n * st.bytes, bar + 8 * n, kept, a.p.xu, s.slot + chunks - 1 - n, h);
             for (int n = 0; n < chunks; ++n) {
@@ -409,17 +377,17 @@ __global__ void __launch_bounds__(kThreads, 1) delta_backward_kernel(const __gri
                 wait(bars.tiles[n % stages], n / stages);
                 wait.done(bars.first, n);
                 if (!wait.ok) break;
-                issue<3, NT, 3, DKP / 16, 64, W, false, 0>(tmem + kY, tmem + kGrad, DKP / 2, k, TILE);
-                issue<NT, 3, 3, 4, 64, 8, true, 2>(tmem + kPg, tmem + kGo, 32, p, SQ);
+                tc::issue<3, NT, 3, DKP / 16, 64, W, false, 0>(tmem + kY, tmem + kGrad, DKP / 2, k, TILE);
+                tc::issue<NT, 3, 3, 4, 64, 8, true, 2>(tmem + kPg, tmem + kGo, 32, p, SQ);
                 tc::commit_one(tc::smem_addr(&bars.one));
                 wait.done(bars.second, n);
                 if (!wait.ok) break;
-                issue<3, 3, 3, 4, 64, 8, true, 2>(tmem + kY, tmem + kD, 32, x, SQ);
+                tc::issue<3, 3, 3, 4, 64, 8, true, 2>(tmem + kY, tmem + kD, 32, x, SQ);
                 tc::commit_one(tc::smem_addr(&bars.two));
-                issue<3, NT, 3, 4, DKP, W, true, 0>(tmem + kChange, tmem + kGrad, 32, q, TILE);
+                tc::issue<3, NT, 3, 4, DKP, W, true, 0>(tmem + kChange, tmem + kGrad, 32, q, TILE);
                 wait.done(bars.third, n);
                 if (!wait.ok) break;
-                issue<3, NT, 3, 4, DKP, W, true, 0>(tmem + kY, tmem + kD, 32, k, TILE);
+                tc::issue<3, NT, 3, 4, DKP, W, true, 0>(tmem + kY, tmem + kD, 32, k, TILE);
                 tc::commit_one(tc::smem_addr(&bars.three));
                 if (n + stages >= chunks) continue;
                 wait(bars.three, n);

@@ -46,6 +46,13 @@ __device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&v)[8]
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                  ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
+__device__ __forceinline__ void tmem_put(uint32_t addr, const float (&v)[16]) {
+    uint32_t q[2][8];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) q[i / 8][i % 8] = __float_as_uint(v[i]);
+    tmem_store(addr, q[0]);
+    tmem_store(addr + 8, q[1]);
+}
 __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // 16 columns; one statement loads and waits.
 __device__ __forceinline__ void tmem_load(float (&v)[16], uint32_t addr) {
@@ -56,6 +63,63 @@ __device__ __forceinline__ void tmem_load(float (&v)[16], uint32_t addr) {
                    "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
                  : "r"(addr) : "memory");
 }
+
+// One lane of a whole warp, in a way that leaves the compiler's uniform registers usable.
+__device__ __forceinline__ bool elected() {
+    uint32_t yes;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+    return yes != 0;
+}
+
+// Products of NA terms in tensor memory (STEPS blocks of 16 summed places, 8 columns each) and NB terms in shared
+// memory, those whose terms' numbers add up to less than KEEP, the smallest first. TURNED: the right factor's rows
+// run along the summed index, else along the other one. WIDTH: blocks of a row. TRI: of a lower triangle's rows only
+// those from the step on (1), of its columns only those up to the step (2).
+template <int NA, int NB, int KEEP, int STEPS, int N, int WIDTH, bool TURNED, int TRI>
+__device__ __forceinline__ void issue(uint32_t d, uint32_t a, uint32_t aterm, uint32_t b, uint32_t bterm) {
+    const Blocks tile = TURNED ? Blocks(b, WIDTH * kCell, kCell) : Blocks(b, kCell, WIDTH * kCell);
+    bool add = false;
+#pragma unroll
+    for (int sum = KEEP - 1; sum >= 0; --sum)
+#pragma unroll
+        for (int i = 0; i < NA; ++i) {
+            const int j = sum - i;
+            if (j < 0 || j >= NB) continue;
+#pragma unroll
+            for (int n = 0; n < STEPS; ++n) {
+                const int s = TRI == 2 ? STEPS - 1 - n : n;
+                const int from = TRI == 1 ? 16 * s : 0, count = TRI == 1 ? N - 16 * s : TRI == 2 ? 16 * (s + 1) : N;
+                mma_lanes(d + from, a + i * aterm + 8 * s, tile.at(j * bterm + (TURNED ? 2 * s * WIDTH : from / 8 * WIDTH + 2 * s) * kCell),
+                          product_of(128, count, false, TURNED), add);
+                add = true;
+            }
+        }
+}
+// The same of a left factor in shared memory whose rows run along the summed index (AW blocks a row), for `steps` blocks
+// of 16 summed places. add: onto what is there.
+template <int NA, int NB, int KEEP, int N, int AW, int WIDTH, bool TURNED, int TRI>
+__device__ __forceinline__ void issue_tiles(uint32_t d, uint32_t a, uint32_t aterm, uint32_t b, uint32_t bterm, int steps, bool add) {
+    const Blocks left(a, AW * kCell, kCell), right = TURNED ? Blocks(b, WIDTH * kCell, kCell) : Blocks(b, kCell, WIDTH * kCell);
+#pragma unroll
+    for (int sum = KEEP - 1; sum >= 0; --sum)
+#pragma unroll
+        for (int i = 0; i < NA; ++i) {
+            const int j = sum - i;
+            if (j < 0 || j >= NB) continue;
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                const int s = TRI == 2 ? 3 - n : n;
+                if (!TRI && s >= steps) continue;
+                const int from = TRI == 1 ? 16 * s : 0, count = TRI == 1 ? N - 16 * s : TRI == 2 ? 16 * (s + 1) : N;
+                mma_tiles(d + from, left.at(i * aterm + 2 * s * AW * kCell), right.at(j * bterm + (TURNED ? 2 * s * WIDTH : from / 8 * WIDTH + 2 * s) * kCell),
+                          product_of(128, count, true, TURNED), add);
+                add = true;
+            }
+        }
+}
+
+// What threads wrote to shared memory, before products read it.
+__device__ __forceinline__ void fence_tiles() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 }  // namespace tc
 }  // namespace dendsn
