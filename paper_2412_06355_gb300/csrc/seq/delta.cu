@@ -29,34 +29,53 @@
 #include <cmath>
 
 #include "delta_common.cuh"
+#include "pairs.cuh"
 #include "tc_one.cuh"
 
 namespace dendsn {
 using namespace delta;
 namespace {
 
-// 8 neighbours of a row from `at` on, zeros behind its end.
+// 8 neighbours of a row from `at` on as they lie, zeros behind its end.
 template <typename T>
-__device__ __forceinline__ void eight(float (&v)[8], const T *row, int at, int end, bool wide) {
+struct Raw {
+    uint4 r[sizeof(T) / 2];
+};
+template <typename T>
+__device__ __forceinline__ Raw<T> raw_of(const T *row, int at, int end, bool wide) {
+    Raw<T> x;
     if (wide && at + 8 <= end) {
-        if constexpr (sizeof(T) == 2) {
-            const auto q = *reinterpret_cast<const Lot<T, 8> *>(row + at);
-            q.get(v);
-        } else {
-            const float4 x = *reinterpret_cast<const float4 *>(row + at), y = *reinterpret_cast<const float4 *>(row + at + 4);
-            v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w, v[4] = y.x, v[5] = y.y, v[6] = y.z, v[7] = y.w;
-        }
-    } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = at + e < end ? value(row + at + e) : 0.f;
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) x.r[i] = reinterpret_cast<const uint4 *>(row + at)[i];
+    } else {
+        uint32_t w[2 * sizeof(T)] = {};
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (at + e < end) {
+                if constexpr (sizeof(T) == 2) w[e / 2] |= (uint32_t)reinterpret_cast<const uint16_t *>(row)[at + e] << e % 2 * 16;
+                else w[e] = reinterpret_cast<const uint32_t *>(row)[at + e];
+            }
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) x.r[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
     }
+    return x;
+}
+// Their terms: themselves, or three.
+__device__ __forceinline__ void terms_of(uint4 (&t)[1], const Raw<__nv_bfloat16> &x) { t[0] = x.r[0]; }
+__device__ __forceinline__ void terms_of(uint4 (&t)[3], const Raw<float> &x) {
+    uint32_t q[4][3];
+    const uint32_t w[8] = {x.r[0].x, x.r[0].y, x.r[0].z, x.r[0].w, x.r[1].x, x.r[1].y, x.r[1].z, x.r[1].w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) split<3>(q[i], __uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+#pragma unroll
+    for (int n = 0; n < 3; ++n) t[n] = make_uint4(q[0][n], q[1][n], q[2][n], q[3][n]);
 }
 
 // ------------------------------------------------------------------ square matrices of a chunk
-// exp(G_i - G_j): the sums as two floats each, so that far below zero no bits of a difference are lost.
-__device__ __forceinline__ float between(const float *gates, int i, int j) {
-    return expf((gates[kHigh + i] - gates[kHigh + j]) + (gates[kLow + i] - gates[kLow + j]));
-}
+// exp(G_i - G_j) from the sums in units of log(2), as two floats each, so that far below zero no bits of a difference
+// are lost. The hardware's power of two is within 2^-22 of itself.
+__device__ __forceinline__ float between(float2 i, float2 j) { return exp2_fast((i.x - j.x) + (i.y - j.y)); }
+__device__ __forceinline__ float2 sum_at(const float *gates, int i) { return make_float2(gates[kHigh + i], gates[kLow + i]); }
 
 // Float32 matrices of the chunk in shared memory: rows of 68 floats, so that the pairs a product's registers hold
 // are read without bank conflicts.
@@ -110,19 +129,31 @@ __global__ void __launch_bounds__(128) delta_prepare_kernel(const __grid_constan
     const int h = blockIdx.y, group = a.Hv / a.Hk, hk = h / group, left = min(C, s.length - chunk * C);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane / 4, t = lane % 4;
     const int64_t first = s.row + (int64_t)chunk * C * s.step, head = (int64_t)blockIdx.x * a.Hv + h;
-    for (int i = threadIdx.x; i < 2 * C * W; i += 128) {
-        const bool isq = i >= C * W;
-        const int j = i % (C * W), tok = j / W, cell = j % W;
-        float v[8] = {};
-        if (tok < left) eight(v, (isq ? q : k) + ((first + tok * s.step) * a.Hk + hk) * a.Dk, cell * 8, a.Dk, wide);
-        uint32_t x[4][NT];
+    // 8 places a thread at a time, a tile's loads on their way at once; to the images by the key head's first value head
+    const bool leads = h % group == 0;
+    auto tile = [&](const T *from, uint8_t *to, uint8_t *image) {
+        constexpr int LOTS = C * W / 128;
+        Raw<T> r[LOTS];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) split<NT>(x[e], v[2 * e], v[2 * e + 1]);
+        for (int i = 0; i < LOTS; ++i) {
+            const int j = threadIdx.x + i * 128, tok = (j >> 3) / W * 8 + (j & 7);
+            r[i] = raw_of(from + ((first + tok * s.step) * a.Hk + hk) * a.Dk, (j >> 3) % W * 8, tok < left ? a.Dk : 0, wide);
+        }
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-            *reinterpret_cast<uint4 *>((isq ? qtile : ktile) + n * TILE + ((tok / 8) * W + cell) * kCell + (tok & 7) * 16) =
-                make_uint4(x[0][n], x[1][n], x[2][n], x[3][n]);
-    }
+        for (int i = 0; i < LOTS; ++i) {
+            const int at = (threadIdx.x + i * 128) * 16;
+            uint4 x[NT];
+            terms_of(x, r[i]);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                *reinterpret_cast<uint4 *>(to + n * TILE + at) = x[n];
+                if (leads) *reinterpret_cast<uint4 *>(image + n * TILE + at) = x[n];
+            }
+        }
+    };
+    const int64_t image = ((int64_t)blockIdx.x * a.Hk + hk) * a.p.key_bytes;
+    tile(k, ktile, kept + a.p.k + image);
+    tile(q, qtile, kept + a.p.q + image);
     if (warp == 0) {           // sums of the gates, in float64: lane l has tokens 2l and 2l + 1
         float r[2], bt[2];
         double sum[2];
@@ -143,30 +174,20 @@ __global__ void __launch_bounds__(128) delta_prepare_kernel(const __grid_constan
             if (lane >= o) before += up;
         }
         before -= sum[1];
+        const double all = __shfl_sync(0xffffffffu, before + sum[1], 31);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const double G = before + sum[e];
+            const double G = before + sum[e], units = G * 1.4426950408889634;
             const int i = 2 * lane + e;
-            gates[kHigh + i] = (float)G;
-            gates[kLow + i] = (float)(G - (double)gates[kHigh + i]);
+            gates[kHigh + i] = (float)units;
+            gates[kLow + i] = (float)(units - (double)(float)units);
             gates[kBeta + i] = bt[e];
-        }
-        __syncwarp();
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int i = 2 * lane + e;
-            gates[kFirst + i] = expf(gates[kHigh + i] + gates[kLow + i]);
-            gates[kRest + i] = between(gates, C - 1, i);
-            gates[kKeep + i] = expf(gates[kHigh + C - 1] + gates[kLow + C - 1]);
+            gates[kFirst + i] = expf((float)G);
+            gates[kRest + i] = expf((float)(all - G));
+            gates[kKeep + i] = expf((float)all);
         }
     }
     __syncthreads();
-    uint8_t *kimage = kept + a.p.k + ((int64_t)blockIdx.x * a.Hk + hk) * a.p.key_bytes, *qimage = kept + a.p.q + ((int64_t)blockIdx.x * a.Hk + hk) * a.p.key_bytes;
-    if (h % group == 0)
-        for (int i = threadIdx.x; i < NT * TILE / 16; i += 128) {
-            reinterpret_cast<uint4 *>(kimage)[i] = reinterpret_cast<const uint4 *>(ktile)[i];
-            reinterpret_cast<uint4 *>(qimage)[i] = reinterpret_cast<const uint4 *>(qtile)[i];
-        }
     float *gout = reinterpret_cast<float *>(kept + a.p.gates) + head * kGateFloats;
     for (int i = threadIdx.x; i < kGateFloats; i += 128) gout[i] = gates[i];
     // k k^T and q k^T, 16 rows a warp
@@ -190,17 +211,23 @@ __global__ void __launch_bounds__(128) delta_prepare_kernel(const __grid_constan
         }
     }
     uint32_t *pout = reinterpret_cast<uint32_t *>(kept + a.p.p + head * kSquare);
+    const float2 Gi[2] = {sum_at(gates, warp * 16 + g), sum_at(gates, warp * 16 + 8 + g)};
 #pragma unroll
-    for (int n = 0; n < 8; ++n)
+    for (int n = 0; n < 8; ++n) {
+        const int j = n * 8 + 2 * t;
+        const float2 high = *reinterpret_cast<const float2 *>(gates + kHigh + j), low = *reinterpret_cast<const float2 *>(gates + kLow + j);
+        const float2 Gj[2] = {make_float2(high.x, low.x), make_float2(high.y, low.y)};
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            const int i = warp * 16 + half * 8 + g, j = n * 8 + 2 * t;
-            float w[2], lo[2];
+            const int i = warp * 16 + half * 8 + g;
+            float w[2] = {}, lo[2] = {};
+            if (n < 2 * warp + 2) {        // blocks above the diagonal are zeros
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const float x = j + e <= i ? between(gates, i, j + e) : 0.f;
-                w[e] = j + e <= i ? x * qk[n][2 * half + e] : 0.f;
-                lo[e] = j + e < i ? x * kk[n][2 * half + e] : 0.f;
+                for (int e = 0; e < 2; ++e) {
+                    const float x = between(Gi[half], Gj[e]);
+                    w[e] = j + e <= i ? x * qk[n][2 * half + e] : 0.f;
+                    lo[e] = j + e < i ? x * kk[n][2 * half + e] : 0.f;
+                }
             }
             uint32_t x[3];
             split<3>(x, w[0], w[1]);
@@ -208,6 +235,7 @@ __global__ void __launch_bounds__(128) delta_prepare_kernel(const __grid_constan
             for (int m = 0; m < 3; ++m) pout[m * 2048 + ((warp * 2 + half) * 8 + n) * 32 + lane] = x[m];
             *reinterpret_cast<float2 *>(L + i * kPitch + j) = make_float2(lo[0], lo[1]);
         }
+    }
     __syncthreads();
     const bool back = warp >= 2, mine = KEEP || !back;         // two warps an inverse
     float *x = X + (back ? 64 * kPitch : 0);
@@ -395,7 +423,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) delta_gradients_k
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
-    const uint32_t tmem = where;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, where, 0);
     const int left = min(C, s.length - chunk * C);
     const int64_t row = s.row + (int64_t)chunk * C * s.step;
 
@@ -482,17 +510,13 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) delta_gradients_k
         }
         __syncwarp();
     }
-    // e . y and v . y: over the columns, which are the lanes
+    {      // e . y and v . y: over the columns, which are the lanes
+        float x[16];
 #pragma unroll
-    for (int o = 16; o; o >>= 1)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            ey[i] += __shfl_xor_sync(0xffffffffu, ey[i], o);
-            vy[i] += __shfl_xor_sync(0xffffffffu, vy[i], o);
-        }
-    if (lane == 0)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) edot[warp * 8 + i] = ey[i], vdot[warp * 8 + i] = gates[kBeta + warp * 8 + i] * vy[i];
+        for (int i = 0; i < 8; ++i) x[i] = ey[i], x[8 + i] = vy[i] * gates[kBeta + warp * 8 + i];
+        const float dot = sums_of(x);
+        if (!(lane & 1)) (lane < 16 ? edot : vdot)[warp * 8 + (lane / 2 & 7)] = dot;
+    }
 #pragma unroll
     for (int o = 16; o; o >>= 1) tail += __shfl_xor_sync(0xffffffffu, tail, o);
     if (lane == 0) sums[warp] = tail;
@@ -504,16 +528,22 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) delta_gradients_k
     // the square matrices as terms: rows 0 to 63 of the sums are A's, the others C's
     const int i = (quarter & 1) * 32 + lane;
     const bool isc = quarter >= 2;
+    const float2 Gi = sum_at(gates, i);
+    const float mul = isc ? -gates[kBeta + i] : a.scale;
 #pragma unroll
     for (int part = 0; part < 2; ++part) {
         const int j0 = half * 32 + part * 16;
         float x[16];
         tc::tmem_load(x, mine + kAE + j0);
-        const float scale = isc ? -gates[kBeta + i] : a.scale;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            const bool in = j0 + j < i + (isc ? 0 : 1);
-            x[j] = in ? scale * between(gates, i, j0 + j) * gates[kBeta + j0 + j] * x[j] : 0.f;
+        for (int j = 0; j < 16; j += 4) {
+            const float4 high = *reinterpret_cast<const float4 *>(gates + kHigh + j0 + j), low = *reinterpret_cast<const float4 *>(gates + kLow + j0 + j),
+                         bt = *reinterpret_cast<const float4 *>(gates + kBeta + j0 + j);
+            const float2 Gj[4] = {make_float2(high.x, low.x), make_float2(high.y, low.y), make_float2(high.z, low.z), make_float2(high.w, low.w)};
+            const float bj[4] = {bt.x, bt.y, bt.z, bt.w};
+            const int end = i - j0 - j + (isc ? 0 : 1);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[j + e] = e < end ? between(Gi, Gj[e]) * (mul * bj[e]) * x[j + e] : 0.f;
         }
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
@@ -524,20 +554,31 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) delta_gradients_k
         }
     }
     // what has come through the states, scaled, in place
+    if (quarter * 32 < DKP)
 #pragma unroll
-    for (int part = 0; part < 2; ++part) {
-        const int j0 = half * 32 + part * 16;
-        float x[16], z[16];
-        tc::tmem_load(x, mine + kGoS + j0);
+        for (int part = 0; part < 2; ++part) {
+            const int j0 = half * 32 + part * 16;
+            float x[16], z[16];
+            tc::tmem_load(x, mine + kGoS + j0);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) x[j] *= a.scale * gates[kFirst + j0 + j];
-        tc::tmem_put(mine + kGoS + j0, x);
-        tc::tmem_load(x, mine + kYS + j0);
-        tc::tmem_load(z, mine + kED + j0);
+            for (int j = 0; j < 16; j += 4) {
+                const float4 f = *reinterpret_cast<const float4 *>(gates + kFirst + j0 + j);
+                x[j] *= a.scale * f.x, x[j + 1] *= a.scale * f.y, x[j + 2] *= a.scale * f.z, x[j + 3] *= a.scale * f.w;
+            }
+            tc::tmem_put(mine + kGoS + j0, x);
+            tc::tmem_load(x, mine + kYS + j0);
+            tc::tmem_load(z, mine + kED + j0);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) x[j] = gates[kBeta + j0 + j] * fmaf(-gates[kFirst + j0 + j], x[j], gates[kRest + j0 + j] * z[j]);
-        tc::tmem_put(mine + kYS + j0, x);
-    }
+            for (int j = 0; j < 16; j += 4) {
+                const float4 f = *reinterpret_cast<const float4 *>(gates + kFirst + j0 + j), r = *reinterpret_cast<const float4 *>(gates + kRest + j0 + j),
+                             bt = *reinterpret_cast<const float4 *>(gates + kBeta + j0 + j);
+                x[j] = bt.x * fmaf(-f.x, x[j], r.x * z[j]);
+                x[j + 1] = bt.y * fmaf(-f.y, x[j + 1], r.y * z[j + 1]);
+                x[j + 2] = bt.z * fmaf(-f.z, x[j + 2], r.z * z[j + 2]);
+                x[j + 3] = bt.w * fmaf(-f.w, x[j + 3], r.w * z[j + 3]);
+            }
+            tc::tmem_put(mine + kYS + j0, x);
+        }
     tc::tmem_stored();
     tc::fence_tiles();
     tc::fence_before_sync();
@@ -569,18 +610,19 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) delta_gradients_k
             if (!ok)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) x[j] = z[j] = __int_as_float(0x7fffffff);
-            if (d < a.Dk) {
-                if (group == 1) {
-                    T *tq = gq + (tok * a.Hk + h) * a.Dk + d, *tk = gk + (tok * a.Hk + h) * a.Dk + d;
+            auto out = [&](auto *tq, auto *tk, int64_t stride) {
+                if (j0 + 16 <= left) {
 #pragma unroll
-                    for (int j = 0; j < 16; ++j, tq += s.step * a.Hk * a.Dk, tk += s.step * a.Hk * a.Dk)
-                        if (j0 + j < left) put(tq, x[j]), put(tk, z[j]);
+                    for (int j = 0; j < 16; ++j, tq += stride, tk += stride) put(tq, x[j]), put(tk, z[j]);
                 } else {
-                    float *tq = parts + (tok * a.Hv + h) * a.Dk + d, *tk = tq + a.p.tokens * a.Hv * a.Dk;
 #pragma unroll
-                    for (int j = 0; j < 16; ++j, tq += s.step * a.Hv * a.Dk, tk += s.step * a.Hv * a.Dk)
-                        if (j0 + j < left) *tq = x[j], *tk = z[j];
+                    for (int j = 0; j < 16; ++j, tq += stride, tk += stride)
+                        if (j0 + j < left) put(tq, x[j]), put(tk, z[j]);
                 }
+            };
+            if (d < a.Dk) {
+                if (group == 1) out(gq + (tok * a.Hk + h) * a.Dk + d, gk + (tok * a.Hk + h) * a.Dk + d, s.step * a.Hk * a.Dk);
+                else out(parts + (tok * a.Hv + h) * a.Dk + d, parts + ((a.p.tokens + tok) * a.Hv + h) * a.Dk + d, s.step * a.Hv * a.Dk);
             }
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
@@ -619,9 +661,9 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) delta_gradients_k
         const int j = 2 * lane + e;
         if (j >= left) continue;
         const int64_t to = (row + j * s.step) * a.Hv + h;
-        // a decay that is 0 in float32 (exp(-104)) has no gradient
+        // a decay that is 0 in float32 (2^-150) has no gradient
         const float gate = gates[kHigh + j] - (j ? gates[kHigh + j - 1] : 0.f) + (gates[kLow + j] - (j ? gates[kLow + j - 1] : 0.f));
-        ggate[to] = gate < -104.f ? 0.f : (float)(behind_all + behind - (e ? at[0] : 0.0));
+        ggate[to] = gate < -150.f ? 0.f : (float)(behind_all + behind - (e ? at[0] : 0.0));
         gbeta[to] = edot[j];
     }
 }

@@ -190,7 +190,7 @@ __device__ __forceinline__ uint32_t begin(Bars &bars, uint32_t &where) {
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
-    return where;
+    return __shfl_sync(0xffffffffu, where, 0);
 }
 __device__ __forceinline__ void finish(bool ok, uint32_t tmem) {
     if (!ok) let_land();
