@@ -17,6 +17,7 @@
 #include <algorithm>
 #include <cmath>
 
+#include "pairs.cuh"
 #include "pieces.cuh"
 #include "seq_common.h"
 #include "tc.cuh"
@@ -29,7 +30,10 @@ constexpr int kChunk = 4096;           // elements of a block's turn
 constexpr int kThreads = 256;
 constexpr int kGrads = 500;            // tensors of a launch: their gradients' addresses are its arguments
 constexpr int kMostBlocks = 152 * 4;   // sums of squares a step can have; blocks of the norm's launch
-constexpr int kResident = 3;           // blocks of the update on an SM: 24 warps with up to 80 registers
+// Blocks of the update on an SM. Float32 states are bound by memory: 24 warps of 80 registers (16 of 128: 730 us
+// against 660 at 2^27 elements). With states in 8 bits 16 warps without a spill are faster (2^29 elements: 1420 us
+// against 1630).
+constexpr int resident(bool eight) { return eight ? 2 : 3; }
 constexpr uint32_t kStride = 0x9E3779B1u;
 
 enum : int32_t { kParamBf16 = 1, kWide = 2 };
@@ -68,13 +72,18 @@ struct Step {
     int32_t sums;              // sums of squares in the table (0: no clipping)
     bool last;                 // launch of the step
     float lr, eps, max_norm, rest1, rest2;
+    float keep1, keep2, root2;     // beta1, and the roots of beta2 and of 1 - beta2
     float log1_hi, log1_lo, log2_hi, log2_lo;     // logarithms of the betas
     uint32_t seed;
 };
 
 __device__ __forceinline__ uint32_t mix(uint32_t h) {
     h = (h ^ (h >> 16)) * 0x6A09E667u;
-    h = (h ^ (h >> 15)) * 0xADF85459u;
+    return (h ^ (h >> 15)) * 0xADF85459u;
+}
+// ... with the upper half mixed into the lower.
+__device__ __forceinline__ uint32_t mixed(uint32_t h) {
+    h = mix(h);
     return h ^ (h >> 16);
 }
 
@@ -156,42 +165,32 @@ __device__ __forceinline__ void store_codes(const uint32_t (&q)[2], uint8_t *p, 
             if (j * 32 + lane < left) p[j * 32 + lane] = (uint8_t)(q[j >> 2] >> (j & 3) * 8);
     }
 }
-__device__ __forceinline__ void decode(float (&v)[8], const uint32_t (&q)[2], float scale) {
+__device__ __forceinline__ void decode(float (&v)[8], const uint32_t (&q)[2]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         uint32_t h;
         asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)(q[i >> 1] >> (i & 1) * 16)));
         const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h));
-        v[2 * i] = f.x * scale, v[2 * i + 1] = f.y * scale;
+        v[2 * i] = f.x, v[2 * i + 1] = f.y;
     }
 }
 
-// e4m3 code of value (0 to 448) from one of its neighbours. Above 2^-6 a code is the float's leading
-// bits; below, adding 2^-6 gives the codes' even steps to a float's mantissa.
-struct Code {
-    uint32_t bits;             // of the float
-    uint32_t base;             // what its leading bits are above the code
-};
-__device__ __forceinline__ Code code_of(float value) {
-    const bool small = value < 0x1p-6f;
-    return {__float_as_uint(small ? value + 0x1p-6f : value), small ? 121u << 3 : 120u << 3};
+// A code is what a float's leading bits are when its value is brought down by 2^-120: e4m3's exponents then are
+// float32's lowest, and the codes below 2^-6 its denormal numbers.
+constexpr float kDown = 0x1p-120f, kUp = 0x1p120f;
+// The low bytes of four words, and their high bytes.
+__device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
 }
-// The upper neighbour where 16 random bits, as a number in (0, 1), are below the value's share of the way.
-__device__ __forceinline__ uint32_t round_code(float value, uint32_t random) {
-    const Code c = code_of(value);
-    return min(((c.bits + (0xfffffu - 8u - 16u * random)) >> 20) - c.base, 0x7eu);
+__device__ __forceinline__ uint32_t high_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
 }
-// The same for the square: its share of the way between the neighbours' squares. u in (0, 1).
-__device__ __forceinline__ uint32_t round_square(float value, float u) {
-    const Code c = code_of(value);
-    const float twice = c.base == 121u << 3 ? -0x1p-5f : 0.f;           // what was added, off two of them
-    const uint32_t low_bits = c.bits & 0xfff00000u;
-    const float at = __uint_as_float(c.bits), low = __uint_as_float(low_bits), high = __uint_as_float(low_bits + 0x100000u);
-    const bool up = u * ((high - low) * (high + low + twice)) < (at - low) * (at + low + twice);
-    return min((low_bits >> 20) - c.base + (up ? 1u : 0u), 0x7eu);
+// The largest size of three, a NaN above them all.
+__device__ __forceinline__ float top_of(float a, float b, float c) {
+    float d;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
 }
-// 16 bits as a number in (0, 1): (h / 65536) + 2^-17 of a word's upper half.
-__device__ __forceinline__ float upper_half(uint32_t h) { return __uint_as_float(0x3f800000u | (h >> 9 & 0x7fff80u)) - (1.f - 0x1p-17f); }
 __device__ __forceinline__ uint32_t warp_top(uint32_t t) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) t = max(t, __shfl_xor_sync(0xffffffffu, t, o));
@@ -203,11 +202,6 @@ __device__ __forceinline__ uint32_t warp_top(uint32_t t) {
 __device__ __forceinline__ float sqrt_fast(float v) {
     float r;
     asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-    return r;
-}
-__device__ __forceinline__ float rcp_fast(float v) {
-    float r;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
 
@@ -249,60 +243,92 @@ __device__ __forceinline__ void load(Share<EIGHT> &r, const Tensor &x, uint64_t 
     }
 }
 
-template <bool EIGHT, bool WIDE>
-__device__ __forceinline__ void update(Share<EIGHT> &r, const Tensor &x, int64_t at, int lane, const Scalars &c, const Step &s, uint32_t start) {
+template <bool WIDE>
+__device__ __forceinline__ void update(Share<false> &r, const Tensor &x, int64_t at, int lane, const Scalars &c, const Step &s, uint32_t) {
     const int left = r.left;
     const float kept = fmaf(-c.lr, x.decay, 1.f);
-    float m[8], v[8], root[8];
-    if constexpr (EIGHT) {
-        decode(m, r.qm, r.scale.x);
-        decode(v, r.qv, r.scale.y);
-    }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        if constexpr (EIGHT) v[j] *= v[j];
-        else m[j] = r.m[j], v[j] = r.v[j];
         const float g = r.g[j] * c.factor;
-        m[j] = fmaf(s.rest1, g - m[j], m[j]);
-        v[j] = fmaf(s.rest2, fmaf(g, g, -v[j]), v[j]);
-        root[j] = EIGHT ? sqrt_fast(v[j]) : sqrtf(v[j]);
-        const float below = fmaf(root[j], c.inverse_root, s.eps), above = c.rate * m[j];
-        r.p[j] = fmaf(r.p[j], kept, -(EIGHT ? above * rcp_fast(below) : __fdiv_rn(above, below)));
+        r.m[j] = fmaf(s.rest1, g - r.m[j], r.m[j]);
+        r.v[j] = fmaf(s.rest2, fmaf(g, g, -r.v[j]), r.v[j]);
+        r.p[j] = fmaf(r.p[j], kept, -__fdiv_rn(c.rate * r.m[j], fmaf(sqrtf(r.v[j]), c.inverse_root, s.eps)));
     }
     if (x.flags & kParamBf16) store8<WIDE>(r.p, static_cast<__nv_bfloat16 *>(x.param) + at, lane, left);
     else store8<WIDE>(r.p, static_cast<float *>(x.param) + at, lane, left);
     if (x.copy) store8<WIDE>(r.p, x.copy + at, lane, left);
-    if constexpr (!EIGHT) {
-        store8<WIDE>(m, static_cast<float *>(x.m) + at, lane, left);
-        store8<WIDE>(v, static_cast<float *>(x.v) + at, lane, left);
-    } else {
-        // sizes as unsigned integers order as the sizes do, with a NaN above them all (elements behind the
-        // tensor's end are zeros)
-        uint32_t top_m = 0, top_v = 0;
+    store8<WIDE>(r.m, static_cast<float *>(x.m) + at, lane, left);
+    store8<WIDE>(r.v, static_cast<float *>(x.v) + at, lane, left);
+}
+// With states in 8 bits it is instructions that bound the step, so they work on pairs, and factors are taken together:
+// m = beta1 m + (1 - beta1) g and v = (sqrt(beta2) sqrt(v))^2 + (sqrt(1 - beta2) g)^2. (2^29 elements: one by one and
+// with each code's exponent looked at, 100 instructions an element, 2090 us.)
+template <bool WIDE>
+__device__ __forceinline__ void update(Share<true> &r, const Tensor &x, int64_t at, int lane, const Scalars &c, const Step &s, uint32_t start) {
+    const int left = r.left;
+    const F2 kept = both(fmaf(-c.lr, x.decay, 1.f)), rate = both(-c.rate), inverse_root = both(c.inverse_root), eps = both(s.eps);
+    const F2 new1 = both(s.rest1 * c.factor), new2 = both(s.root2 * c.factor), old1 = both(s.keep1 * r.scale.x), old2 = both(s.keep2 * r.scale.y);
+    float mc[8], vc[8];
+    decode(mc, r.qm);
+    decode(vc, r.qv);
+    F2 m[4], root[4];
+    float top_m = 0.f, top_v = 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            top_m = max(top_m, __float_as_uint(m[j]) & 0x7fffffffu);
-            top_v = max(top_v, __float_as_uint(root[j]));
-        }
-        const float tm = __uint_as_float(warp_top(top_m)), tv = __uint_as_float(warp_top(top_v));
-        // below 2^-110 a block's states are zeros: 448 / top would leave float32
-        const float im = tm < 0x1p-110f ? 0.f : 448.f * rcp_fast(tm), iv = tv < 0x1p-110f ? 0.f : 448.f * rcp_fast(tv);
-        if (lane == 0)
-            *reinterpret_cast<float2 *>(x.scales + at / kBlock * 2) =
-                make_float2(tm < 0x1p-110f ? 0.f : tm * (1.f / 448.f), tv < 0x1p-110f ? 0.f : tv * (1.f / 448.f));
-        uint32_t qm[2] = {}, qv[2] = {};
-        const uint32_t first = ((uint32_t)at + (WIDE ? lane * 8 : lane)) * kStride + start;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const uint32_t h = mix(first + (uint32_t)(WIDE ? j : j * 32) * kStride);
-            const uint32_t cm = round_code(fabsf(m[j]) * im, h & 0xffffu) | (__float_as_uint(m[j]) >> 24 & 0x80u);
-            const uint32_t cv = round_square(root[j] * iv, upper_half(h));
-            qm[j >> 2] |= cm << (j & 3) * 8;
-            qv[j >> 2] |= cv << (j & 3) * 8;
-        }
-        store_codes<WIDE>(qm, static_cast<uint8_t *>(x.m) + at, lane, left);
-        store_codes<WIDE>(qv, static_cast<uint8_t *>(x.v) + at, lane, left);
+    for (int j = 0; j < 4; ++j) {
+        const F2 g(r.g[2 * j], r.g[2 * j + 1]), w = mul(F2(vc[2 * j], vc[2 * j + 1]), old2), h = mul(g, new2);
+        m[j] = fma(g, new1, mul(F2(mc[2 * j], mc[2 * j + 1]), old1));
+        const F2 v = fma(h, h, mul(w, w));
+        root[j] = F2(sqrt_fast(v.x()), sqrt_fast(v.y()));
+        const F2 below = fma(root[j], inverse_root, eps);
+        const F2 p = fma(mul(m[j], F2(rcp_fast(below.x()), rcp_fast(below.y()))), rate, mul(F2(r.p[2 * j], r.p[2 * j + 1]), kept));
+        r.p[2 * j] = p.x(), r.p[2 * j + 1] = p.y();
+        // (elements behind the tensor's end are zeros)
+        top_m = top_of(m[j].x(), m[j].y(), top_m);
+        top_v = top_of(root[j].x(), root[j].y(), top_v);
     }
+    if (x.flags & kParamBf16) store8<WIDE>(r.p, static_cast<__nv_bfloat16 *>(x.param) + at, lane, left);
+    else store8<WIDE>(r.p, static_cast<float *>(x.param) + at, lane, left);
+    if (x.copy) store8<WIDE>(r.p, x.copy + at, lane, left);
+    // sizes as unsigned integers order as the sizes do, with a NaN above them all
+    const float tm = __uint_as_float(warp_top(__float_as_uint(top_m))), tv = __uint_as_float(warp_top(__float_as_uint(top_v)));
+    // Below 2^-110 a block's states are zeros: 448 / top would leave float32. Three roundings of at most 2^-22 together
+    // stay below 448 with 2^-22 taken off before, and above what the largest random number leaves at 416.
+    constexpr float kMost = 448.f * (1.f - 0x1p-22f);
+    const F2 im = both(tm < 0x1p-110f ? 0.f : kMost * rcp_fast(tm)), iv = both(tv < 0x1p-110f ? 0.f : kMost * rcp_fast(tv));
+    if (lane == 0)
+        *reinterpret_cast<float2 *>(x.scales + at / kBlock * 2) =
+            make_float2(tm < 0x1p-110f ? 0.f : tm * (1.f / 448.f), tv < 0x1p-110f ? 0.f : tv * (1.f / 448.f));
+    const uint32_t first = ((uint32_t)at + (WIDE ? lane * 8 : lane)) * kStride + start;
+    uint32_t cm[8], cv[8], sign[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const F2 down = mul(mul(m[j], im), both(kDown)), value = mul(root[j], iv), square = mul(value, value), bits = mul(value, both(kDown));
+        const uint32_t h[2] = {mix(first + (uint32_t)(WIDE ? 2 * j : j * 64) * kStride), mix(first + (uint32_t)(WIDE ? 2 * j + 1 : j * 64 + 32) * kStride)};
+        const uint32_t low[2] = {__float_as_uint(bits.x()) & 0xfff00000u, __float_as_uint(bits.y()) & 0xfff00000u};
+        // v: its share of the way between the neighbours' squares against the word's upper half
+        const F2 l = mul(F2(__uint_as_float(low[0]), __uint_as_float(low[1])), both(kUp)),
+                 u = mul(F2(__uint_as_float(low[0] + 0x100000u), __uint_as_float(low[1] + 0x100000u)), both(kUp));
+        const F2 l2 = mul(l, l), step = fma(u, u, F2(-l2.x(), -l2.y()));
+        const F2 random = add(F2(__uint_as_float(0x3f800000u | (h[0] >> 9 & 0x7fff80u)), __uint_as_float(0x3f800000u | (h[1] >> 9 & 0x7fff80u))), both(-(1.f - 0x1p-17f)));
+        const F2 border = fma(random, step, l2);
+        const float b[2] = {border.x(), border.y()}, q[2] = {square.x(), square.y()}, d[2] = {down.x(), down.y()};
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            cv[2 * j + e] = (b[e] < q[e] ? low[e] + 0x100000u : low[e]) >> 20;
+            // m: the upper neighbour where the word's mixed lower half, as a number in (0, 1), is below its share
+            sign[2 * j + e] = __float_as_uint(d[e]);
+            cm[2 * j + e] = (sign[2 * j + e] + 7u + 16u * (~(h[e] ^ h[e] >> 16) & 0xffffu)) >> 20;
+        }
+    }
+    uint32_t qm[2], qv[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        qm[i] = low_bytes(cm[4 * i], cm[4 * i + 1], cm[4 * i + 2], cm[4 * i + 3]) |
+                (high_bytes(sign[4 * i], sign[4 * i + 1], sign[4 * i + 2], sign[4 * i + 3]) & 0x80808080u);
+        qv[i] = low_bytes(cv[4 * i], cv[4 * i + 1], cv[4 * i + 2], cv[4 * i + 3]);
+    }
+    store_codes<WIDE>(qm, static_cast<uint8_t *>(x.m) + at, lane, left);
+    store_codes<WIDE>(qv, static_cast<uint8_t *>(x.v) + at, lane, left);
 }
 
 // A block's run of chunks, and the tensor it is in.
@@ -327,6 +353,75 @@ struct Run {
         if (++chunk >= next && chunk < end) {
             do enter(i + 1);
             while (chunk >= next);     // tensors without elements have no chunk
+        }
+    }
+};
+
+// Pieces of 256 elements with states in 8 bits on their way through shared memory: every lane fetches, and reads,
+// its own 8 elements, so that nothing but its own copies is waited for, and no registers are held meanwhile.
+constexpr int kPieces = 4;             // of a warp: one worked on, three on their way
+constexpr int kPieceBytes = kThreads * 80;
+struct Pieces {
+    uint32_t at;                       // this thread's place in the first piece
+    __device__ __forceinline__ explicit Pieces(const uint8_t *smem) : at(tc::smem_addr(smem)) {}
+    // g, p: 32 bytes a thread (16 used of bfloat16), in two halves; m, v: 8
+    __device__ __forceinline__ uint32_t place(int piece, int kind) const {
+        return at + piece * kPieceBytes + (kind < 4 ? (kind * kThreads + threadIdx.x) * 16 : kThreads * 64 + ((kind - 4) * kThreads + threadIdx.x) * 8);
+    }
+    __device__ __forceinline__ void copy16(int piece, int kind, const void *from) {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(place(piece, kind)), "l"(from) : "memory");
+    }
+    __device__ __forceinline__ void copy8(int piece, int kind, const void *from) {
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(place(piece, kind)), "l"(from) : "memory");
+    }
+    __device__ __forceinline__ void fetch(int piece, const Tensor &x, uint64_t grad, int64_t first, int64_t stop) {
+        const int64_t e = first + (threadIdx.x & 31) * 8;
+        if (first < stop && e < x.n) {
+            if (grad & 1) {
+                copy16(piece, 0, reinterpret_cast<const uint16_t *>(grad - 1) + e);
+            } else {
+                copy16(piece, 0, reinterpret_cast<const float *>(grad) + e);
+                copy16(piece, 1, reinterpret_cast<const float *>(grad) + e + 4);
+            }
+            if (x.flags & kParamBf16) {
+                copy16(piece, 2, static_cast<const uint16_t *>(x.param) + e);
+            } else {
+                copy16(piece, 2, static_cast<const float *>(x.param) + e);
+                copy16(piece, 3, static_cast<const float *>(x.param) + e + 4);
+            }
+            copy8(piece, 4, static_cast<const uint8_t *>(x.m) + e);
+            copy8(piece, 5, static_cast<const uint8_t *>(x.v) + e);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    __device__ __forceinline__ uint4 read16(int piece, int kind) const {
+        uint4 r;
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(place(piece, kind)) : "memory");
+        return r;
+    }
+    __device__ __forceinline__ void eight(float (&v)[8], int piece, int kind, bool bf) const {
+        const uint4 r = read16(piece, kind);
+        if (bf) {
+            Lot<__nv_bfloat16, 8> q;
+            q.r = r;
+            q.get(v);
+        } else {
+            const uint4 t = read16(piece, kind + 1);
+            v[0] = __uint_as_float(r.x), v[1] = __uint_as_float(r.y), v[2] = __uint_as_float(r.z), v[3] = __uint_as_float(r.w);
+            v[4] = __uint_as_float(t.x), v[5] = __uint_as_float(t.y), v[6] = __uint_as_float(t.z), v[7] = __uint_as_float(t.w);
+        }
+    }
+    __device__ __forceinline__ void take(Share<true> &r, int piece, const Tensor &x, uint64_t grad, int64_t first) const {
+        r.left = (int)min((int64_t)kBlock, x.n - first);
+        if ((threadIdx.x & 31) * 8 < r.left) {
+            eight(r.g, piece, 0, grad & 1);
+            eight(r.p, piece, 2, x.flags & kParamBf16);
+            asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(r.qm[0]), "=r"(r.qm[1]) : "r"(place(piece, 4)) : "memory");
+            asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(r.qv[0]), "=r"(r.qv[1]) : "r"(place(piece, 5)) : "memory");
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) r.g[j] = r.p[j] = 0.f;
+            r.qm[0] = r.qm[1] = r.qv[0] = r.qv[1] = 0;
         }
     }
 };
@@ -357,7 +452,7 @@ __device__ void scalars(Scalars &shared, const Step &s, double *part) {
         c.lr = s.lr_at ? *s.lr_at : s.lr;
         c.rate = __fdiv_rn(c.lr, rest_of_power((float)t, s.log1_hi, s.log1_lo));
         c.inverse_root = __fdiv_rn(1.f, sqrtf(rest_of_power((float)t, s.log2_hi, s.log2_lo)));
-        c.start = mix((uint32_t)t * kStride + s.seed);
+        c.start = mixed((uint32_t)t * kStride + s.seed);
         shared = c;
         if (s.last) {        // the block that reads the step last moves it on
             Header *h = reinterpret_cast<Header *>(s.plan);
@@ -372,31 +467,64 @@ __device__ void scalars(Scalars &shared, const Step &s, double *part) {
 }
 
 template <bool EIGHT>
-__global__ void __launch_bounds__(kThreads, kResident) adamw_kernel(const __grid_constant__ Step s, const __grid_constant__ Grads grads) {
+__global__ void __launch_bounds__(kThreads, resident(EIGHT)) adamw_kernel(const __grid_constant__ Step s, const __grid_constant__ Grads grads) {
+    extern __shared__ __align__(16) uint8_t queue[];
     __shared__ Scalars shared;
     __shared__ double part[kThreads / 32];
     pdl_begin();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    constexpr int64_t kTurn = kThreads / 32 * kBlock;      // elements a block takes at once
     Scalars c;
     bool known = false;
+    auto know = [&] {              // while the first elements are on their way
+        if (known) return;
+        scalars(shared, s, part);
+        c = shared;
+        known = true;
+    };
     for (Run r(s); r.chunk < r.end; r.advance()) {
+        const int32_t behind = min(r.end, r.next);         // of this tensor's chunks that are the block's
+        int64_t at = (int64_t)(r.chunk - r.x.first) * kChunk + warp * kBlock;
+        const int64_t stop = min(r.x.n, (int64_t)(behind - r.x.first) * kChunk);
+        r.chunk = behind - 1;
         const uint64_t grad = grads.at[r.i - s.first];
         if (!grad) continue;
         const bool wide = (r.x.flags & kWide) && (grad & 1 ? grad % 16 == 1 : grad % 32 == 0);
-        uint32_t start = 0;
-#pragma unroll 1
-        for (int turn = 0; turn < kChunk / kThreads / 8; ++turn) {
-            const int64_t at = (int64_t)(r.chunk - r.x.first) * kChunk + (turn * (kThreads / 32) + warp) * kBlock;
-            const bool here = at < r.x.n;
+        if constexpr (EIGHT) {
+            if (wide) {
+                Pieces pieces(queue);
+                for (int k = 0; k < kPieces - 1; ++k) pieces.fetch(k, r.x, grad, at + k * kTurn, stop);
+                know();
+                const uint32_t start = mixed(c.start + (uint32_t)r.i);
+                auto scale_at = [&](int64_t to) {
+                    return to < stop ? *reinterpret_cast<const float2 *>(r.x.scales + to / kBlock * 2) : make_float2(0.f, 0.f);
+                };
+                float2 scale = scale_at(at);
+                int piece = 0, last = kPieces - 1;
+                for (; at < stop; at += kTurn) {
+                    pieces.fetch(last, r.x, grad, at + (kPieces - 1) * kTurn, stop);
+                    const float2 next = scale_at(at + kTurn);
+                    asm volatile("cp.async.wait_group %0;" ::"n"(kPieces - 1) : "memory");
+                    Share<true> e;
+                    e.scale = scale;
+                    pieces.take(e, piece, r.x, grad, at);
+                    update<true>(e, r.x, at, lane, c, s, start);
+                    scale = next;
+                    last = piece;
+                    piece = piece + 1 == kPieces ? 0 : piece + 1;
+                }
+                asm volatile("cp.async.wait_group 0;" ::: "memory");
+                continue;
+            }
+        }
+        // every warp comes here equally often: the first time, all of them for the step's values
+        for (bool first = true; first || at < stop; first = false, at += kTurn) {
+            const bool here = at < stop;
             Share<EIGHT> e;
             if (here) wide ? load<EIGHT, true>(e, r.x, grad, at, lane) : load<EIGHT, false>(e, r.x, grad, at, lane);
-            if (!known) {          // while the first elements are on their way
-                scalars(shared, s, part);
-                c = shared;
-                known = true;
-            }
-            if (!turn) start = mix(c.start + (uint32_t)r.i);
-            if (here) wide ? update<EIGHT, true>(e, r.x, at, lane, c, s, start) : update<EIGHT, false>(e, r.x, at, lane, c, s, start);
+            know();
+            const uint32_t start = mixed(c.start + (uint32_t)r.i);
+            if (here) wide ? update<true>(e, r.x, at, lane, c, s, start) : update<false>(e, r.x, at, lane, c, s, start);
         }
     }
     if (!known) scalars(shared, s, part);
@@ -527,6 +655,7 @@ dendsn_status dendsn_adamw_step(const dendsn_adamw_config *cfg, void *plan, cons
     a.max_norm = (float)cfg->max_norm;
     a.rest1 = (float)(1.0 - cfg->beta1);
     a.rest2 = (float)(1.0 - cfg->beta2);
+    a.keep1 = (float)cfg->beta1, a.keep2 = (float)std::sqrt(cfg->beta2), a.root2 = (float)std::sqrt(1.0 - cfg->beta2);
     // the logarithm of a beta of 0 as one whose power is 0 from the first step on
     const double l1 = cfg->beta1 > 0 ? std::log(cfg->beta1) : -1e4, l2 = cfg->beta2 > 0 ? std::log(cfg->beta2) : -1e4;
     a.log1_hi = (float)l1, a.log1_lo = (float)(l1 - (double)a.log1_hi);
@@ -552,13 +681,18 @@ dendsn_status dendsn_adamw_step(const dendsn_adamw_config *cfg, void *plan, cons
             }
             a.chunks = chunk;
             a.last = r == rounds - 1;
-            const int blocks = std::max(1, std::min(a.chunks - a.chunk, pass ? 152 * kResident : most));
+            const int blocks = std::max(1, std::min(a.chunks - a.chunk, pass ? 152 * resident(cfg->state == DENDSN_STATE_E4M3) : most));
             if (pass == 0) {
                 e = seq_launch(adamw_norm_kernel, dim3((unsigned)blocks), kThreads, 0, s, 1, a, g, sums);
                 sums += blocks;
             } else {
-                e = cfg->state == DENDSN_STATE_E4M3 ? seq_launch(adamw_kernel<true>, dim3((unsigned)blocks), kThreads, 0, s, 1, a, g)
-                                                     : seq_launch(adamw_kernel<false>, dim3((unsigned)blocks), kThreads, 0, s, 1, a, g);
+                if (cfg->state == DENDSN_STATE_E4M3) {
+                    constexpr int kBytes = kPieces * kPieceBytes;
+                    e = cudaFuncSetAttribute(adamw_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+                    if (e == cudaSuccess) e = seq_launch(adamw_kernel<true>, dim3((unsigned)blocks), kThreads, kBytes, s, 1, a, g);
+                } else {
+                    e = seq_launch(adamw_kernel<false>, dim3((unsigned)blocks), kThreads, 0, s, 1, a, g);
+                }
             }
             ++launches;
         }
