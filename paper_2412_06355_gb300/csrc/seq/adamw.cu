@@ -291,10 +291,9 @@ __device__ __forceinline__ void update(Share<true> &r, const Tensor &x, int64_t 
     if (x.copy) store8<WIDE>(r.p, x.copy + at, lane, left);
     // sizes as unsigned integers order as the sizes do, with a NaN above them all
     const float tm = __uint_as_float(warp_top(__float_as_uint(top_m))), tv = __uint_as_float(warp_top(__float_as_uint(top_v)));
-    // Below 2^-110 a block's states are zeros: 448 / top would leave float32. Three roundings of at most 2^-22 together
-    // stay below 448 with 2^-22 taken off before, and above what the largest random number leaves at 416.
-    constexpr float kMost = 448.f * (1.f - 0x1p-22f);
-    const F2 im = both(tm < 0x1p-110f ? 0.f : kMost * rcp_fast(tm)), iv = both(tv < 0x1p-110f ? 0.f : kMost * rcp_fast(tv));
+    // Below 2^-110 a block's states are zeros: 448 / top would leave float32. (A value that rounding brings above 448 stays
+    // below what the largest random number lifts to the next code, and its square's share below the smallest's.)
+    const F2 im = both(tm < 0x1p-110f ? 0.f : __fdiv_rn(448.f, tm)), iv = both(tv < 0x1p-110f ? 0.f : __fdiv_rn(448.f, tv));
     if (lane == 0)
         *reinterpret_cast<float2 *>(x.scales + at / kBlock * 2) =
             make_float2(tm < 0x1p-110f ? 0.f : tm * (1.f / 448.f), tv < 0x1p-110f ? 0.f : tv * (1.f / 448.f));

@@ -386,14 +386,19 @@ __device__ __forceinline__ float sums_of(float (&v)[16]) {
 // y); then those within the chunk. A warp has 8 tokens of a round's go, v, y and e, a lane one column of v. Two blocks
 // share an SM (bfloat16), so that one's loads go on beside the other's products. Gradients of shared heads go out in
 // float32 for each value head and are added up by delta_join_kernel.
-// Columns of tensor memory:
-constexpr uint32_t kGoS = 0, kYS = 64, kED = 128, kAE = 192, kGradColumns = 256;
+// The matrix instruction cuts its sums off where it should round: every addition onto a large sum costs up to 2^-23 of
+// it. So the small products come first, in sums of their own where all of tensor memory is one block's (float32), and
+// what is added within the chunk is summed by itself.
+// Columns of tensor memory, of the sums through the states and of A and C; those of D e and of A and C are the sums'
+// within the chunk afterwards.
+constexpr uint32_t kGoS = 0, kYS = 64, kED = 128, kAE = 192, kSums = 256;
 template <typename T, int DKP>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) delta_gradients_kernel(const __grid_constant__ Args a, const uint8_t *kept, uint8_t *scratch,
                                                                                        T *gq, T *gk, T *gv, float *ggate, float *gbeta) {
     constexpr int NT = sizeof(T) == 2 ? 1 : 3, W = DKP / 8, TILE = C * DKP * 2, SQ = kSquare / 3;
     using P = Parts<NT, DKP>;
     constexpr int FEW = P::FEW;
+    constexpr uint32_t LOW = NT == 1 ? 0 : kSums, kGradColumns = kSums + LOW;      // where the small products' sums are
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ uint64_t keys_bar, done_bar;
     __shared__ uint32_t where;
@@ -497,15 +502,15 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) delta_gradients_k
             tc::fence_after_sync();
             const int steps = count / 16;
             const uint32_t go_at = base + P::t, y_at = go_at + 8 * kCell;
-            tc::issue_tiles<3, NT, 3, 64, W, 16, true, 0>(tmem + kGoS, base + P::s, P::state, go_at, P::pair, steps, n);
-            tc::issue_tiles<3, FEW, FEW, 64, W, 16, true, 0>(tmem + kYS, base + P::s, P::state, y_at, P::pair, steps, n);
-            tc::issue_tiles<FEW, 3, FEW, 64, W, 8, true, 0>(tmem + kED, base + P::d, P::state, base + P::e, P::error, steps, n);
-            if (NT == 1) {
-                tc::issue_tiles<1, 1, 1, 64, 16, 8, true, 0>(tmem + kAE, go_at + P::pair, P::pair, base + P::e, P::error, steps, n);
-                tc::issue_tiles<1, 3, 3, 64, 16, 8, true, 0>(tmem + kAE, go_at, P::pair, base + P::e, P::error, steps, true);
-            } else {
-                tc::issue_tiles<FEW, 3, 3, 64, 16, 8, true, 0>(tmem + kAE, go_at, P::pair, base + P::e, P::error, steps, n);
-            }
+            const bool more = n, after = LOW ? more : true;
+            tc::issue_tiles<3, NT, 1, 3, W, 16, true, 0>(tmem + LOW + kGoS, base + P::s, P::state, go_at, P::pair, steps, more);
+            tc::issue_tiles<3, NT, 0, 1, W, 16, true, 0>(tmem + kGoS, base + P::s, P::state, go_at, P::pair, steps, after);
+            tc::issue_tiles<3, FEW, 1, FEW, W, 16, true, 0>(tmem + LOW + kYS, base + P::s, P::state, y_at, P::pair, steps, more);
+            tc::issue_tiles<3, FEW, 0, 1, W, 16, true, 0>(tmem + kYS, base + P::s, P::state, y_at, P::pair, steps, after);
+            tc::issue_tiles<FEW, 3, 1, FEW, W, 8, true, 0>(tmem + LOW + kED, base + P::d, P::state, base + P::e, P::error, steps, more);
+            tc::issue_tiles<FEW, 3, 0, 1, W, 8, true, 0>(tmem + kED, base + P::d, P::state, base + P::e, P::error, steps, after);
+            tc::issue_tiles<FEW, 3, 1, 3, 16, 8, true, 0>(tmem + LOW + kAE, go_at, P::pair, base + P::e, P::error, steps, more);
+            tc::issue_tiles<FEW, 3, 0, 1, 16, 8, true, 0>(tmem + kAE, go_at, P::pair, base + P::e, P::error, steps, after);
             tc::commit_one(done);
         }
         __syncwarp();
@@ -525,6 +530,15 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) delta_gradients_k
     tc::fence_after_sync();
     const int quarter = warp & 3, half = warp >> 2;
     const uint32_t mine = tmem + ((uint32_t)quarter << 21);
+    auto sum_load = [&](float (&x)[16], uint32_t from) {
+        tc::tmem_load(x, from);
+        if (LOW) {
+            float low[16];
+            tc::tmem_load(low, from + LOW);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) x[j] += low[j];
+        }
+    };
     // the square matrices as terms: rows 0 to 63 of the sums are A's, the others C's
     const int i = (quarter & 1) * 32 + lane;
     const bool isc = quarter >= 2;
@@ -534,7 +548,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) delta_gradients_k
     for (int part = 0; part < 2; ++part) {
         const int j0 = half * 32 + part * 16;
         float x[16];
-        tc::tmem_load(x, mine + kAE + j0);
+        sum_load(x, mine + kAE + j0);
 #pragma unroll
         for (int j = 0; j < 16; j += 4) {
             const float4 high = *reinterpret_cast<const float4 *>(gates + kHigh + j0 + j), low = *reinterpret_cast<const float4 *>(gates + kLow + j0 + j),
@@ -559,15 +573,15 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) delta_gradients_k
         for (int part = 0; part < 2; ++part) {
             const int j0 = half * 32 + part * 16;
             float x[16], z[16];
-            tc::tmem_load(x, mine + kGoS + j0);
+            sum_load(x, mine + kGoS + j0);
 #pragma unroll
             for (int j = 0; j < 16; j += 4) {
                 const float4 f = *reinterpret_cast<const float4 *>(gates + kFirst + j0 + j);
                 x[j] *= a.scale * f.x, x[j + 1] *= a.scale * f.y, x[j + 2] *= a.scale * f.z, x[j + 3] *= a.scale * f.w;
             }
             tc::tmem_put(mine + kGoS + j0, x);
-            tc::tmem_load(x, mine + kYS + j0);
-            tc::tmem_load(z, mine + kED + j0);
+            sum_load(x, mine + kYS + j0);
+            sum_load(z, mine + kED + j0);
 #pragma unroll
             for (int j = 0; j < 16; j += 4) {
                 const float4 f = *reinterpret_cast<const float4 *>(gates + kFirst + j0 + j), r = *reinterpret_cast<const float4 *>(gates + kRest + j0 + j),
@@ -587,10 +601,15 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) delta_gradients_k
     if (warp == 0 && ok && tc::elected()) {
         tc::fence_after_sync();
         const uint32_t k = base + P::key, q = k + P::keys;
-        tc::issue_tiles<NT, 3, 3, 64, W, 8, false, 1>(tmem + kGoS, k, TILE, base + P::a, SQ, 4, true);
-        tc::issue_tiles<NT, FEW, FEW, 64, W, 8, true, 2>(tmem + kYS, q, TILE, base + P::a, SQ, 4, true);
-        tc::issue_tiles<NT, FEW, FEW, 64, W, 8, false, 1>(tmem + kYS, k, TILE, base + P::c, SQ, 4, true);
-        tc::issue_tiles<NT, FEW, FEW, 64, W, 8, true, 2>(tmem + kYS, k, TILE, base + P::c, SQ, 4, true);
+        const bool after = !LOW;
+        tc::issue_tiles<NT, 3, 1, 3, W, 8, false, 1>(tmem + LOW + kAE, k, TILE, base + P::a, SQ, 4, false);
+        tc::issue_tiles<NT, 3, 0, 1, W, 8, false, 1>(tmem + kAE, k, TILE, base + P::a, SQ, 4, after);
+        tc::issue_tiles<NT, FEW, 1, FEW, W, 8, true, 2>(tmem + LOW + kED, q, TILE, base + P::a, SQ, 4, false);
+        tc::issue_tiles<NT, FEW, 1, FEW, W, 8, false, 1>(tmem + LOW + kED, k, TILE, base + P::c, SQ, 4, true);
+        tc::issue_tiles<NT, FEW, 1, FEW, W, 8, true, 2>(tmem + LOW + kED, k, TILE, base + P::c, SQ, 4, true);
+        tc::issue_tiles<NT, FEW, 0, 1, W, 8, true, 2>(tmem + kED, q, TILE, base + P::a, SQ, 4, after);
+        tc::issue_tiles<NT, FEW, 0, 1, W, 8, false, 1>(tmem + kED, k, TILE, base + P::c, SQ, 4, true);
+        tc::issue_tiles<NT, FEW, 0, 1, W, 8, true, 2>(tmem + kED, k, TILE, base + P::c, SQ, 4, true);
         tc::commit_one(done);
     }
     __syncwarp();
@@ -605,8 +624,17 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) delta_gradients_k
             const int j0 = half * 32 + part * 16;
             const int64_t tok = row + j0 * s.step;
             float x[16], z[16];
-            tc::tmem_load(x, mine + kGoS + j0);
-            tc::tmem_load(z, mine + kYS + j0);
+            {
+                float add[16];
+                tc::tmem_load(x, mine + kGoS + j0);
+                sum_load(add, mine + kAE + j0);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) x[j] += add[j];
+                tc::tmem_load(z, mine + kYS + j0);
+                sum_load(add, mine + kED + j0);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) z[j] += add[j];
+            }
             if (!ok)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) x[j] = z[j] = __int_as_float(0x7fffffff);

@@ -96,12 +96,12 @@ __device__ __forceinline__ void issue(uint32_t d, uint32_t a, uint32_t aterm, ui
         }
 }
 // The same of a left factor in shared memory whose rows run along the summed index (AW blocks a row), for `steps` blocks
-// of 16 summed places. add: onto what is there.
-template <int NA, int NB, int KEEP, int N, int AW, int WIDTH, bool TURNED, int TRI>
+// of 16 summed places, of the products whose terms' numbers add up to FROM and less than KEEP. add: onto what is there.
+template <int NA, int NB, int FROM, int KEEP, int AW, int WIDTH, bool TURNED, int TRI>
 __device__ __forceinline__ void issue_tiles(uint32_t d, uint32_t a, uint32_t aterm, uint32_t b, uint32_t bterm, int steps, bool add) {
     const Blocks left(a, AW * kCell, kCell), right = TURNED ? Blocks(b, WIDTH * kCell, kCell) : Blocks(b, kCell, WIDTH * kCell);
 #pragma unroll
-    for (int sum = KEEP - 1; sum >= 0; --sum)
+    for (int sum = KEEP - 1; sum >= FROM; --sum)
 #pragma unroll
         for (int i = 0; i < NA; ++i) {
             const int j = sum - i;
@@ -110,7 +110,7 @@ __device__ __forceinline__ void issue_tiles(uint32_t d, uint32_t a, uint32_t ate
             for (int n = 0; n < 4; ++n) {
                 const int s = TRI == 2 ? 3 - n : n;
                 if (!TRI && s >= steps) continue;
-                const int from = TRI == 1 ? 16 * s : 0, count = TRI == 1 ? N - 16 * s : TRI == 2 ? 16 * (s + 1) : N;
+                const int from = TRI == 1 ? 16 * s : 0, count = TRI == 1 ? 64 - 16 * s : TRI == 2 ? 16 * (s + 1) : 64;
                 mma_tiles(d + from, left.at(i * aterm + 2 * s * AW * kCell), right.at(j * bterm + (TURNED ? 2 * s * WIDTH : from / 8 * WIDTH + 2 * s) * kCell),
                           product_of(128, count, true, TURNED), add);
                 add = true;
