@@ -442,6 +442,12 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) delta_gradients_k
     const int rounds = (a.p.DVP + kRound - 1) / kRound, own = lane / 8 * 8 + warp;     // own: the lane's block of 8 columns and 8 tokens
     float ey[8] = {}, vy[8] = {}, tail = 0.f;
     bool ok = true;
+    if (threadIdx.x < 7) {     // all of it is asked for at once, so that the later rounds find it in L2
+        const uint8_t *from[] = {sat, dat, next, yat, eat, goat, vat};
+        const size_t state = a.p.state_bytes, row_bytes = a.p.kept_bytes, tile = a.p.value_bytes;
+        const size_t bytes[] = {state, state, state, row_bytes, row_bytes, tile, tile};
+        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(from[threadIdx.x]), "r"((uint32_t)bytes[threadIdx.x]) : "memory");
+    }
     for (int n = 0; n < rounds; ++n) {
         const int count = min(kRound, a.p.DVP - n * kRound);
         const bool here = lane < count;
@@ -498,7 +504,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) delta_gradients_k
         }
         tc::fence_tiles();
         __syncthreads();
-        if (warp == 0 && ok && tc::elected()) {
+        if (warp == (n & 7) && ok && tc::elected()) {      // in turn: issuing takes a warp's time
             tc::fence_after_sync();
             const int steps = count / 16;
             const uint32_t go_at = base + P::t, y_at = go_at + 8 * kCell;
