@@ -8,7 +8,7 @@
 // distance of two codes, and would be lost in rounding to the nearest.
 //
 // Bound by memory: every state is read and written once, in one launch for all tensors. Tensors are
-// cut into chunks of 4096 elements; a table in device memory says which tensor a chunk belongs to, and
+// cut into chunks of 2048 elements; a table in device memory says which tensor a chunk belongs to, and
 // the gradients' addresses, which change from step to step, come as the launch's arguments. A warp
 // takes 256 elements at a time, 8 neighbours a lane, so that a scale's elements are one warp's.
 // Clipping reads the gradients once more before (a launch that leaves one float64 sum a block).
@@ -26,12 +26,13 @@ namespace dendsn {
 namespace {
 
 constexpr int kBlock = 256;            // elements of a warp's turn, and of a scale
-constexpr int kChunk = 4096;           // elements of a block's turn
+constexpr int kChunk = 2048;           // elements of a block's turn
 constexpr int kThreads = 256;
 constexpr int kGrads = 500;            // tensors of a launch: their gradients' addresses are its arguments
 constexpr int kMostBlocks = 152 * 4;   // sums of squares a step can have; blocks of the norm's launch
 // Blocks of the update on an SM. Float32 states are bound by memory: 24 warps of 80 registers (16 of 128: 730 us
-// against 660 at 2^27 elements). With states in 8 bits 16 warps without a spill are faster (2^29 elements: 1420 us
+// against 660 at 2^27 elements). With states in 8 bits 16 warps without a spill are faster (2^29 elements, before codes
+// were drawn as the formulas round: 1420 us
 // against 1630).
 constexpr int resident(bool eight) { return eight ? 2 : 3; }
 constexpr uint32_t kStride = 0x9E3779B1u;
@@ -72,7 +73,6 @@ struct Step {
     int32_t sums;              // sums of squares in the table (0: no clipping)
     bool last;                 // launch of the step
     float lr, eps, max_norm, rest1, rest2;
-    float keep1, keep2, root2;     // beta1, and the roots of beta2 and of 1 - beta2
     float log1_hi, log1_lo, log2_hi, log2_lo;     // logarithms of the betas
     uint32_t seed;
 };
@@ -196,12 +196,11 @@ __device__ __forceinline__ uint32_t warp_top(uint32_t t) {
     for (int o = 16; o; o >>= 1) t = max(t, __shfl_xor_sync(0xffffffffu, t, o));
     return t;
 }
-// The hardware's square root and reciprocal are within 2^-22 of themselves: roundings of the update, which is
-// a thousandth of p, and of what an 8-bit code of v's root is drawn from. The exact ones cost some twenty
-// instructions more an element, of the sixty that memory leaves time for.
-__device__ __forceinline__ float sqrt_fast(float v) {
+// The hardware's reciprocal root, of numbers from float32's smallest normal one on (of what is below, as of that one,
+// so that the root of zero is zero).
+__device__ __forceinline__ float rsqrt_fast(float v) {
     float r;
-    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(fmaxf(v, 0x1p-126f)));
     return r;
 }
 
@@ -260,14 +259,15 @@ __device__ __forceinline__ void update(Share<false> &r, const Tensor &x, int64_t
     store8<WIDE>(r.m, static_cast<float *>(x.m) + at, lane, left);
     store8<WIDE>(r.v, static_cast<float *>(x.v) + at, lane, left);
 }
-// With states in 8 bits it is instructions that bound the step, so they work on pairs, and factors are taken together:
-// m = beta1 m + (1 - beta1) g and v = (sqrt(beta2) sqrt(v))^2 + (sqrt(1 - beta2) g)^2. (2^29 elements: one by one and
-// with each code's exponent looked at, 100 instructions an element, 2090 us.)
+// With states in 8 bits it is instructions that bound the step, so they work on pairs. What a code is drawn from is
+// rounded as the formulas' own operations are, one by one: a last bit that differs decides one code in a million
+// otherwise. (2^29 elements: 1600 us; one by one and
+// with each code's exponent looked at, 100 instructions an element, 2090.)
 template <bool WIDE>
 __device__ __forceinline__ void update(Share<true> &r, const Tensor &x, int64_t at, int lane, const Scalars &c, const Step &s, uint32_t start) {
     const int left = r.left;
     const F2 kept = both(fmaf(-c.lr, x.decay, 1.f)), rate = both(-c.rate), inverse_root = both(c.inverse_root), eps = both(s.eps);
-    const F2 new1 = both(s.rest1 * c.factor), new2 = both(s.root2 * c.factor), old1 = both(s.keep1 * r.scale.x), old2 = both(s.keep2 * r.scale.y);
+    const F2 scale_m = both(r.scale.x), scale_v = both(r.scale.y), factor = both(c.factor), rest1 = both(s.rest1), rest2 = both(s.rest2), minus = both(-1.f);
     float mc[8], vc[8];
     decode(mc, r.qm);
     decode(vc, r.qv);
@@ -275,10 +275,13 @@ __device__ __forceinline__ void update(Share<true> &r, const Tensor &x, int64_t 
     float top_m = 0.f, top_v = 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const F2 g(r.g[2 * j], r.g[2 * j + 1]), w = mul(F2(vc[2 * j], vc[2 * j + 1]), old2), h = mul(g, new2);
-        m[j] = fma(g, new1, mul(F2(mc[2 * j], mc[2 * j + 1]), old1));
-        const F2 v = fma(h, h, mul(w, w));
-        root[j] = F2(sqrt_fast(v.x()), sqrt_fast(v.y()));
+        const F2 g = mul(F2(r.g[2 * j], r.g[2 * j + 1]), factor), old = mul(F2(mc[2 * j], mc[2 * j + 1]), scale_m);
+        m[j] = add(mul(fma(old, minus, g), rest1), old);
+        const F2 w = mul(F2(vc[2 * j], vc[2 * j + 1]), scale_v), w2 = mul(w, w);
+        const F2 v = add(mul(fma(w2, minus, mul(g, g)), rest2), w2);
+        // the root from the hardware's reciprocal root and one step of Newton's
+        const F2 y(rsqrt_fast(v.x()), rsqrt_fast(v.y())), near = mul(v, y);
+        root[j] = fma(fma(mul(near, minus), near, v), mul(y, both(0.5f)), near);
         const F2 below = fma(root[j], inverse_root, eps);
         const F2 p = fma(mul(m[j], F2(rcp_fast(below.x()), rcp_fast(below.y()))), rate, mul(F2(r.p[2 * j], r.p[2 * j + 1]), kept));
         r.p[2 * j] = p.x(), r.p[2 * j + 1] = p.y();
@@ -293,7 +296,7 @@ __device__ __forceinline__ void update(Share<true> &r, const Tensor &x, int64_t 
     const float tm = __uint_as_float(warp_top(__float_as_uint(top_m))), tv = __uint_as_float(warp_top(__float_as_uint(top_v)));
     // Below 2^-110 a block's states are zeros: 448 / top would leave float32. (A value that rounding brings above 448 stays
     // below what the largest random number lifts to the next code, and its square's share below the smallest's.)
-    const F2 im = both(tm < 0x1p-110f ? 0.f : __fdiv_rn(448.f, tm)), iv = both(tv < 0x1p-110f ? 0.f : __fdiv_rn(448.f, tv));
+    const F2 im = both(tm < 0x1p-110f ? 0.f : __frcp_rn(tm) * 448.f), iv = both(tv < 0x1p-110f ? 0.f : __frcp_rn(tv) * 448.f);
     if (lane == 0)
         *reinterpret_cast<float2 *>(x.scales + at / kBlock * 2) =
             make_float2(tm < 0x1p-110f ? 0.f : tm * (1.f / 448.f), tv < 0x1p-110f ? 0.f : tv * (1.f / 448.f));
@@ -301,16 +304,16 @@ __device__ __forceinline__ void update(Share<true> &r, const Tensor &x, int64_t 
     uint32_t cm[8], cv[8], sign[8];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const F2 down = mul(mul(m[j], im), both(kDown)), value = mul(root[j], iv), square = mul(value, value), bits = mul(value, both(kDown));
+        const F2 down = mul(mul(m[j], im), both(kDown)), value = mul(root[j], iv), bits = mul(value, both(kDown));
         const uint32_t h[2] = {mix(first + (uint32_t)(WIDE ? 2 * j : j * 64) * kStride), mix(first + (uint32_t)(WIDE ? 2 * j + 1 : j * 64 + 32) * kStride)};
         const uint32_t low[2] = {__float_as_uint(bits.x()) & 0xfff00000u, __float_as_uint(bits.y()) & 0xfff00000u};
         // v: its share of the way between the neighbours' squares against the word's upper half
         const F2 l = mul(F2(__uint_as_float(low[0]), __uint_as_float(low[1])), both(kUp)),
                  u = mul(F2(__uint_as_float(low[0] + 0x100000u), __uint_as_float(low[1] + 0x100000u)), both(kUp));
-        const F2 l2 = mul(l, l), step = fma(u, u, F2(-l2.x(), -l2.y()));
+        const F2 above = mul(fma(l, minus, value), add(value, l)), step = mul(fma(l, minus, u), add(u, l));
         const F2 random = add(F2(__uint_as_float(0x3f800000u | (h[0] >> 9 & 0x7fff80u)), __uint_as_float(0x3f800000u | (h[1] >> 9 & 0x7fff80u))), both(-(1.f - 0x1p-17f)));
-        const F2 border = fma(random, step, l2);
-        const float b[2] = {border.x(), border.y()}, q[2] = {square.x(), square.y()}, d[2] = {down.x(), down.y()};
+        const F2 border = mul(random, step);
+        const float b[2] = {border.x(), border.y()}, q[2] = {above.x(), above.y()}, d[2] = {down.x(), down.y()};
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             cv[2 * j + e] = (b[e] < q[e] ? low[e] + 0x100000u : low[e]) >> 20;
@@ -472,7 +475,8 @@ __global__ void __launch_bounds__(kThreads, resident(EIGHT)) adamw_kernel(const 
     __shared__ double part[kThreads / 32];
     pdl_begin();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    constexpr int64_t kTurn = kThreads / 32 * kBlock;      // elements a block takes at once
+    constexpr int64_t kTurn = kChunk;
+    static_assert(kChunk == kThreads / 32 * kBlock, "a warp's turn is 256 elements");
     Scalars c;
     bool known = false;
     auto know = [&] {              // while the first elements are on their way
@@ -536,29 +540,34 @@ __global__ void __launch_bounds__(kThreads) adamw_norm_kernel(const __grid_const
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     double sum = 0.0;
     for (Run r(s); r.chunk < r.end; r.advance()) {
+        const int32_t behind = min(r.end, r.next);         // of this tensor's chunks that are the block's
+        int64_t at = (int64_t)(r.chunk - r.x.first) * kChunk + warp * kBlock;
+        const int64_t stop = min(r.x.n, (int64_t)(behind - r.x.first) * kChunk);
+        r.chunk = behind - 1;
         const uint64_t grad = grads.at[r.i - s.first];
         if (!grad) continue;
-        const int64_t n = r.x.n, first = (int64_t)(r.chunk - r.x.first) * kChunk;
-        const bool bf = grad & 1, wide = n % 8 == 0 && (bf ? grad % 16 == 1 : grad % 32 == 0);
-        float g[kChunk / kThreads / 8][8];
+        const bool bf = grad & 1, wide = r.x.n % 8 == 0 && (bf ? grad % 16 == 1 : grad % 32 == 0);
+        constexpr int kAtOnce = 4;
+        for (; at < stop; at += kAtOnce * kChunk) {
+            float g[kAtOnce][8];
 #pragma unroll
-        for (int k = 0; k < kChunk / kThreads / 8; ++k) {
-            const int64_t at = first + (k * (kThreads / 32) + warp) * kBlock;
-            const int left = (int)max((int64_t)0, min((int64_t)kBlock, n - at));
-            if (bf) {
-                const __nv_bfloat16 *q = reinterpret_cast<const __nv_bfloat16 *>(grad - 1) + at;
-                wide ? load8<true>(g[k], q, lane, left) : load8<false>(g[k], q, lane, left);
-            } else {
-                const float *q = reinterpret_cast<const float *>(grad) + at;
-                wide ? load8<true>(g[k], q, lane, left) : load8<false>(g[k], q, lane, left);
+            for (int k = 0; k < kAtOnce; ++k) {
+                const int left = (int)max((int64_t)0, min((int64_t)kBlock, stop - (at + k * kChunk)));
+                if (bf) {
+                    const __nv_bfloat16 *q = reinterpret_cast<const __nv_bfloat16 *>(grad - 1) + at + k * kChunk;
+                    wide ? load8<true>(g[k], q, lane, left) : load8<false>(g[k], q, lane, left);
+                } else {
+                    const float *q = reinterpret_cast<const float *>(grad) + at + k * kChunk;
+                    wide ? load8<true>(g[k], q, lane, left) : load8<false>(g[k], q, lane, left);
+                }
             }
+            float squares = 0.f;
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) squares = fmaf(g[k][j], g[k][j], squares);
+            sum += (double)squares;
         }
-        float squares = 0.f;
-#pragma unroll
-        for (int k = 0; k < kChunk / kThreads / 8; ++k)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) squares = fmaf(g[k][j], g[k][j], squares);
-        sum += (double)squares;
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -654,7 +663,6 @@ dendsn_status dendsn_adamw_step(const dendsn_adamw_config *cfg, void *plan, cons
     a.max_norm = (float)cfg->max_norm;
     a.rest1 = (float)(1.0 - cfg->beta1);
     a.rest2 = (float)(1.0 - cfg->beta2);
-    a.keep1 = (float)cfg->beta1, a.keep2 = (float)std::sqrt(cfg->beta2), a.root2 = (float)std::sqrt(1.0 - cfg->beta2);
     // the logarithm of a beta of 0 as one whose power is 0 from the first step on
     const double l1 = cfg->beta1 > 0 ? std::log(cfg->beta1) : -1e4, l2 = cfg->beta2 > 0 ? std::log(cfg->beta2) : -1e4;
     a.log1_hi = (float)l1, a.log1_lo = (float)(l1 - (double)a.log1_hi);
