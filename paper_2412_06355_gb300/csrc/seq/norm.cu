@@ -71,12 +71,18 @@ __device__ __forceinline__ void weights(float (&w)[VEC], const float *weight, in
 
 // Sizes as unsigned integers order as the sizes do, and a NaN is above them all.
 __device__ __forceinline__ uint32_t size_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
-// The scale that makes the largest of a group 448, and what the group is multiplied by. A group whose
+// The scale that makes the largest of a group 448, and its reciprocal. A group whose
 // largest is below 2^-100 (none of a model's) keeps scale 1, where its codes are zeros.
 __device__ __forceinline__ float2 scale_of(uint32_t top) {
     const float t = __uint_as_float(top);
     if (t < 0x1p-100f) return make_float2(1.f, 1.f);
-    return make_float2(__fdiv_rn(t, 448.f), __fdiv_rn(448.f, t));
+    const float s = t * (1.f / 448.f);
+    return make_float2(s, __frcp_rn(s));
+}
+// v / scale as the division rounds it: a code is decided by the quotient's last bits only.
+__device__ __forceinline__ float scaled(float v, float2 s) {
+    const float q = v * s.y;
+    return fmaf(fmaf(-q, s.x, v), s.y, q);
 }
 
 struct Rows {
@@ -139,7 +145,7 @@ __global__ void __launch_bounds__(512) norm_forward_kernel(const T *x, const T *
         ss = row_sums(ss, 0.f, p.threads, red[turn]).x;
         const float r = __fdiv_rn(1.f, sqrtf(ss / (float)p.D + p.eps));
         uint32_t top = 0;
-        float inverse[OUT == 2 && VEC == 1 ? (NV + 3) / 4 : 1];
+        float2 scale[OUT == 2 && VEC == 1 ? (NV + 3) / 4 : 1];
         if (OUT == 1) {
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
@@ -160,7 +166,7 @@ __global__ void __launch_bounds__(512) norm_forward_kernel(const T *x, const T *
                 for (int w = 0; w < p.threads >> 5; ++w) top = max(top, tops[w]);
             }
             const float2 s = scale_of(top);
-            inverse[0] = s.y;
+            scale[0] = s;
             if (thread == 0) scales[row] = s.x;
         }
         if (OUT == 2 && VEC == 1) {
@@ -173,7 +179,7 @@ __global__ void __launch_bounds__(512) norm_forward_kernel(const T *x, const T *
                 if (k < p.nv) top = max(top, size_bits(v[0] * r * __ldg(weight + k)));
                 if (j % 4 == 3) {
                     const float2 s = scale_of(warp_max(top, 16));
-                    inverse[j / 4] = s.y;
+                    scale[j / 4] = s;
                     const int first = k - (k & 127);
                     if ((thread & 31) == 0 && first < p.D) scales[row * groups + first / kGroup] = s.x;
                 }
@@ -196,26 +202,26 @@ __global__ void __launch_bounds__(512) norm_forward_kernel(const T *x, const T *
                 if (k < p.nv) reinterpret_cast<L *>(y)[row * p.nv + k] = o;
                 continue;
             }
-            float inv = OUT == 2 && VEC == 1 ? inverse[j / 4] : inverse[0];
+            float2 by = OUT == 2 && VEC == 1 ? scale[j / 4] : scale[0];
             if (OUT == 2 && VEC > 1) {       // 128 columns are 128 / VEC neighbouring lanes' vector
                 top = 0;
                 if (k < p.nv)
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) top = max(top, size_bits(v[e]));
                 const float2 s = scale_of(warp_max(top, 64 / VEC));
-                inv = s.y;
+                by = s;
                 if ((k * VEC) % kGroup == 0 && k < p.nv) scales[row * groups + k * VEC / kGroup] = s.x;
             }
             if (k < p.nv) {
                 uint8_t *to = reinterpret_cast<uint8_t *>(y) + row * p.D + k * VEC;
                 if (VEC == 1) {
-                    *to = (uint8_t)e4m3_pair(v[0] * inv, 0.f);
+                    *to = (uint8_t)e4m3_pair(scaled(v[0], by), 0.f);
                 } else {
                     uint32_t q[VEC / 4 ? VEC / 4 : 1];
 #pragma unroll
                     for (int e = 0; e < VEC / 4; ++e)
-                        q[e] = (uint32_t)e4m3_pair(v[4 * e] * inv, v[4 * e + 1] * inv) |
-                               (uint32_t)e4m3_pair(v[4 * e + 2] * inv, v[4 * e + 3] * inv) << 16;
+                        q[e] = (uint32_t)e4m3_pair(scaled(v[4 * e], by), scaled(v[4 * e + 1], by)) |
+                               (uint32_t)e4m3_pair(scaled(v[4 * e + 2], by), scaled(v[4 * e + 3], by)) << 16;
                     if (VEC == 8) *reinterpret_cast<uint2 *>(to) = make_uint2(q[0], q[VEC / 4 - 1]);
                     else *reinterpret_cast<uint32_t *>(to) = q[0];
                 }
