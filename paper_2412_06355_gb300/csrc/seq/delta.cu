@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(128) delta_prepare_kernel(const __grid_constan
         for (int half = 0; half < 2; ++half) {
             const int i = warp * 16 + half * 8 + g;
             float w[2] = {}, lo[2] = {};
-            if (n < 2 * warp + 2) {        // blocks above the diagonal are zeros
+            if (n < 2 * warp + 2) {        // above the diagonal's blocks there is nothing, and nobody reads
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const float x = between(Gi[half], Gj[e]);
@@ -229,10 +229,12 @@ __global__ void __launch_bounds__(128) delta_prepare_kernel(const __grid_constan
                     lo[e] = j + e < i ? x * kk[n][2 * half + e] : 0.f;
                 }
             }
-            uint32_t x[3];
-            split<3>(x, w[0], w[1]);
+            if (n < 2 * warp + 2) {
+                uint32_t x[3];
+                split<3>(x, w[0], w[1]);
 #pragma unroll
-            for (int m = 0; m < 3; ++m) pout[m * 2048 + ((warp * 2 + half) * 8 + n) * 32 + lane] = x[m];
+                for (int m = 0; m < 3; ++m) pout[m * 2048 + ((warp * 2 + half) * 8 + n) * 32 + lane] = x[m];
+            }
             *reinterpret_cast<float2 *>(L + i * kPitch + j) = make_float2(lo[0], lo[1]);
         }
     }
@@ -309,7 +311,8 @@ __global__ void __launch_bounds__(128) delta_prepare_kernel(const __grid_constan
 #pragma unroll 4
         for (int i = threadIdx.x; i < 2048; i += 128) {
             const int cell = i / 32, row = cell / 8 * 8 + g, col = cell % 8 * 8 + 2 * t;
-            const float2 y = row / 16 < col / 16 ? make_float2(0.f, 0.f) : *reinterpret_cast<const float2 *>(x + row * kPitch + col);
+            if (row / 16 < col / 16) continue;
+            const float2 y = *reinterpret_cast<const float2 *>(x + row * kPitch + col);
             uint32_t w[3];
             split<3>(w, y.x, y.y);
 #pragma unroll

@@ -21,7 +21,7 @@ namespace delta {
 namespace {
 
 constexpr int kWarps = 16;                 // that compute
-constexpr int kThreads = (kWarps + 4) * 32;            // one more issues; three only share its registers out
+constexpr int kThreads = (kWarps + 4) * 32;            // one more issues, one fetches; two only share its registers out
 constexpr int kParts = kWarps / 4;         // threads of a column of v
 constexpr int kTokens = C / kParts;        // tokens of a thread
 constexpr uint32_t kColumns = 512;         // of tensor memory: all there are
@@ -40,15 +40,26 @@ __host__ __device__ inline Stage stage_of(const DeltaPlan &p) {
     s.bytes = s.gates + kGateFloats * 4;
     return s;
 }
-// One thread: the chunk's tiles into a stage.
+// One warp: the chunk's tiles into a stage. Of the square matrices only the blocks on and below the diagonal of 16 x 16
+// are written, and fetched: a row of blocks a lane.
+constexpr uint32_t kTriangle = 3 * 5120;   // bytes of what is fetched of one
 __device__ __forceinline__ void load_stage(const Args &a, const Stage &st, uint32_t smem, uint32_t bar, const uint8_t *kept, size_t x, int64_t slot, int h) {
     const int64_t hk = slot * a.Hk + h / (a.Hv / a.Hk), hv = slot * a.Hv + h;
-    tc::bar_expect(bar, st.bytes);
-    load_bytes(smem + st.k, kept + a.p.k + hk * a.p.key_bytes, (uint32_t)a.p.key_bytes, bar);
-    load_bytes(smem + st.q, kept + a.p.q + hk * a.p.key_bytes, (uint32_t)a.p.key_bytes, bar);
-    load_bytes(smem + st.x, kept + x + hv * kSquare, kSquare, bar);
-    load_bytes(smem + st.p, kept + a.p.p + hv * kSquare, kSquare, bar);
-    load_bytes(smem + st.gates, kept + a.p.gates + hv * kGateFloats * 4, kGateFloats * 4, bar);
+    const int lane = threadIdx.x & 31;
+    if (lane == 0) tc::bar_expect(bar, 2 * (uint32_t)a.p.key_bytes + 2 * kTriangle + kGateFloats * 4);
+    __syncwarp();
+    if (lane < 24) {
+        const uint32_t at = lane * 8 * kCell, bytes = (lane % 8 / 2 + 1) * 2 * kCell;      // term lane / 8, row of blocks lane % 8
+        load_bytes(smem + st.x + at, kept + x + hv * kSquare + at, bytes, bar);
+        load_bytes(smem + st.p + at, kept + a.p.p + hv * kSquare + at, bytes, bar);
+    } else if (lane == 24) {
+        load_bytes(smem + st.k, kept + a.p.k + hk * a.p.key_bytes, (uint32_t)a.p.key_bytes, bar);
+    } else if (lane == 25) {
+        load_bytes(smem + st.q, kept + a.p.q + hk * a.p.key_bytes, (uint32_t)a.p.key_bytes, bar);
+    } else if (lane == 26) {
+        load_bytes(smem + st.gates, kept + a.p.gates + hv * kGateFloats * 4, kGateFloats * 4, bar);
+    }
+    __syncwarp();
 }
 
 // A thread's tokens of one column of v or go, fetched ahead of their use.
@@ -166,6 +177,7 @@ struct Bars {
 struct Waits {
     bool ok;
     __device__ __forceinline__ void operator()(uint64_t &bar, uint32_t phase) { ok = ok && tc::bar_wait(tc::smem_addr(&bar), phase & 1); }
+    __device__ __forceinline__ bool all() { return ok = __all_sync(0xffffffffu, ok); }     // of a warp's lanes
     // of products: what they wrote may be read then
     __device__ __forceinline__ void done(uint64_t &bar, uint32_t phase) {
         operator()(bar, phase);
@@ -225,15 +237,13 @@ __global__ void __launch_bounds__(kThreads, 1) delta_forward_kernel(const __grid
     Waits wait{true};
     if (warp >= kWarps) {
         fewer_registers();
+        if (warp == kWarps + 1)
+            for (int n = 0; n < chunks; ++n) {
+                if (n >= stages) wait(bars.four, n - stages);      // the stage is free when all that reads it is done
+                if (!wait.all()) break;
+                load_stage(a, st, base + n % stages * st.bytes, tc::smem_addr(&bars.tiles[n % stages]), kept, a.p.xe, s.slot + n, h);
+            }
         if (warp == kWarps && tc::elected()) {
-            const uint32_t bar = tc::smem_addr(bars.tiles);
-            for (int n = 0; n < min(stages, chunks); ++n) load_stage(a, st, base + n * st.bytes, bar + 8 * n, kept, a.p.xe, s.slot + n, h);
-            // the stage of chunk n is free when all that reads it is done
-            auto refill = [&](int n) {
-                wait(bars.four, n);
-                if (wait.ok && n + stages < chunks)
-                    load_stage(a, st, base + n % stages * st.bytes, bar + 8 * (n % stages), kept, a.p.xe, s.slot + n + stages, h);
-            };
             for (int n = 0; n < chunks && wait.ok; ++n) {
                 const uint32_t tiles = base + n % stages * st.bytes, k = tiles + st.k, q = tiles + st.q, x = tiles + st.x, p = tiles + st.p;
                 wait(bars.tiles[n % stages], n / stages);
@@ -242,7 +252,6 @@ __global__ void __launch_bounds__(kThreads, 1) delta_forward_kernel(const __grid
                 tc::issue<3, NT, 3, DKP / 16, 64, W, false, 0>(tmem + kSeen, tmem + kState, DKP / 2, k, TILE);
                 tc::commit_one(tc::smem_addr(&bars.one));
                 tc::issue<3, NT, FEW, DKP / 16, 64, W, false, 0>(tmem + kSeen + 64, tmem + kState, DKP / 2, q, TILE);
-                if (n && stages > 1) refill(n - 1);
                 wait.done(bars.second, n);
                 if (!wait.ok) break;
                 tc::issue<3, 3, 3, 4, 64, 8, false, 1>(tmem + kOut, tmem + kError, 32, x, SQ);
@@ -253,7 +262,6 @@ __global__ void __launch_bounds__(kThreads, 1) delta_forward_kernel(const __grid
                 tc::commit_one(tc::smem_addr(&bars.three));
                 tc::issue<3, FEW, FEW, 4, 64, 8, false, 1>(tmem + kOut, tmem + kError, 32, p, SQ);
                 tc::commit_one(tc::smem_addr(&bars.four));
-                if (stages == 1) refill(n);
             }
         }
         __syncwarp();
@@ -373,9 +381,13 @@ __global__ void __launch_bounds__(kThreads, 1) delta_backward_kernel(const __gri
     Waits wait{true};
     if (warp >= kWarps) {
         fewer_registers();
+        if (warp == kWarps + 1)
+            for (int n = 0; n < chunks; ++n) {
+                if (n >= stages) wait(bars.three, n - stages);
+                if (!wait.all()) break;
+                load_stage(a, st, base + n % stages * st.bytes, tc::smem_addr(&bars.tiles[n % stages]), kept, a.p.xu, s.slot + chunks - 1 - n, h);
+            }
         if (warp == kWarps && tc::elected()) {
-            const uint32_t bar = tc::smem_addr(bars.tiles);
-            for (int n = 0; n < min(stages, chunks); ++n) load_stage(a, st, base + n * st.bytes, bar + 8 * n, kept, a.p.xu, s.slot + chunks - 1 - n, h);
             for (int n = 0; n < chunks; ++n) {
                 const uint32_t tiles = base + n % stages * st.bytes, k = tiles + st.k, q = tiles + st.q, x = tiles + st.x, p = tiles + st.p;
                 wait(bars.tiles[n % stages], n / stages);
@@ -393,10 +405,6 @@ __global__ void __launch_bounds__(kThreads, 1) delta_backward_kernel(const __gri
                 if (!wait.ok) break;
                 tc::issue<3, NT, 3, 4, DKP, W, true, 0>(tmem + kY, tmem + kD, 32, k, TILE);
                 tc::commit_one(tc::smem_addr(&bars.three));
-                if (n + stages >= chunks) continue;
-                wait(bars.three, n);
-                if (!wait.ok) break;
-                load_stage(a, st, tiles, bar + 8 * (n % stages), kept, a.p.xu, s.slot + chunks - 1 - n - stages, h);
             }
         }
         __syncwarp();
