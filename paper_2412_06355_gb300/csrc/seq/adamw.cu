@@ -8,7 +8,7 @@
 // distance of two codes, and would be lost in rounding to the nearest.
 //
 // Bound by memory: every state is read and written once, in one launch for all tensors. Tensors are
-// cut into chunks of 2048 elements; a table in device memory says which tensor a chunk belongs to, and
+// cut into chunks of 4096 elements; a table in device memory says which tensor a chunk belongs to, and
 // the gradients' addresses, which change from step to step, come as the launch's arguments. A warp
 // takes 256 elements at a time, 8 neighbours a lane, so that a scale's elements are one warp's.
 // Clipping reads the gradients once more before (a launch that leaves one float64 sum a block).
@@ -26,7 +26,8 @@ namespace dendsn {
 namespace {
 
 constexpr int kBlock = 256;            // elements of a warp's turn, and of a scale
-constexpr int kChunk = 2048;           // elements of a block's turn
+constexpr int kChunk = 4096;           // elements of a place in the table
+constexpr int kTurn = 2048;            // elements of a block's turn, half of that: what blocks are dealt
 constexpr int kThreads = 256;
 constexpr int kGrads = 500;            // tensors of a launch: their gradients' addresses are its arguments
 constexpr int kMostBlocks = 152 * 4;   // sums of squares a step can have; blocks of the norm's launch
@@ -68,7 +69,7 @@ struct Step {
     const float *lr_at;        // or NULL: lr
     float *norm;               // or NULL
     int32_t tensors, first;    // of the plan; the first of this launch
-    int32_t chunk, chunks;     // of this launch: the first, and the one behind the last
+    int32_t turn, turns;       // of this launch: the first, and the one behind the last
     int32_t sums;              // sums of squares in the table (0: no clipping)
     bool last;                 // launch of the step
     float lr, eps, max_norm, rest1, rest2;
@@ -332,28 +333,33 @@ __device__ __forceinline__ void update(Share<true> &r, const Tensor &x, int64_t 
     store_codes<WIDE>(qv, static_cast<uint8_t *>(x.v) + at, lane, left);
 }
 
-// A block's run of chunks, and the tensor it is in.
+// A block's run of turns, and the tensor it is in.
 struct Run {
     const Tensor *tensors;
-    int32_t chunk, end, i, next;       // this chunk, behind the last; its tensor, the next tensor's first chunk
+    int32_t turn, end, i, next;        // this turn, behind the last; its tensor, the next tensor's first turn
     Tensor x;
     __device__ __forceinline__ explicit Run(const Step &s) {
         tensors = reinterpret_cast<const Tensor *>(s.plan + kTensorsAt);
-        const int64_t n = s.chunks - s.chunk;
-        chunk = s.chunk + (int32_t)(n * blockIdx.x / gridDim.x);
-        end = s.chunk + (int32_t)(n * (blockIdx.x + 1) / gridDim.x);
-        next = chunk;
-        if (chunk < end) enter(reinterpret_cast<const int32_t *>(tensors + s.tensors)[chunk]);
+        const int64_t n = s.turns - s.turn;
+        turn = s.turn + (int32_t)(n * blockIdx.x / gridDim.x);
+        end = s.turn + (int32_t)(n * (blockIdx.x + 1) / gridDim.x);
+        next = turn;
+        if (turn < end) enter(reinterpret_cast<const int32_t *>(tensors + s.tensors)[turn / 2]);
     }
     __device__ __forceinline__ void enter(int32_t to) {
         i = to;
         x = tensors[i];
-        next = x.first + (int32_t)((x.n + kChunk - 1) / kChunk);
+        next = 2 * (x.first + (int32_t)((x.n + kChunk - 1) / kChunk));
     }
+    // Where the block's part of this tensor starts and ends (a last half chunk may be empty).
+    __device__ __forceinline__ int64_t first() const { return (int64_t)(turn - 2 * x.first) * kTurn; }
+    __device__ __forceinline__ int64_t stop() const { return min(x.n, (int64_t)(min(end, next) - 2 * x.first) * kTurn); }
+    // To the next tensor.
     __device__ __forceinline__ void advance() {
-        if (++chunk >= next && chunk < end) {
+        turn = min(end, next);
+        if (turn < end) {
             do enter(i + 1);
-            while (chunk >= next);     // tensors without elements have no chunk
+            while (turn >= next);      // tensors without elements have no chunk
         }
     }
 };
@@ -474,8 +480,7 @@ __global__ void __launch_bounds__(kThreads, resident(EIGHT)) adamw_kernel(const 
     __shared__ double part[kThreads / 32];
     pdl_begin();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    constexpr int64_t kTurn = kChunk;
-    static_assert(kChunk == kThreads / 32 * kBlock, "a warp's turn is 256 elements");
+    static_assert(2 * kTurn == kChunk && kTurn == kThreads / 32 * kBlock, "a warp's turn is 256 elements");
     Scalars c;
     bool known = false;
     auto know = [&] {              // while the first elements are on their way
@@ -484,11 +489,9 @@ __global__ void __launch_bounds__(kThreads, resident(EIGHT)) adamw_kernel(const 
         c = shared;
         known = true;
     };
-    for (Run r(s); r.chunk < r.end; r.advance()) {
-        const int32_t behind = min(r.end, r.next);         // of this tensor's chunks that are the block's
-        int64_t at = (int64_t)(r.chunk - r.x.first) * kChunk + warp * kBlock;
-        const int64_t stop = min(r.x.n, (int64_t)(behind - r.x.first) * kChunk);
-        r.chunk = behind - 1;
+    for (Run r(s); r.turn < r.end; r.advance()) {
+        int64_t at = r.first() + warp * kBlock;
+        const int64_t stop = r.stop();
         const uint64_t grad = grads.at[r.i - s.first];
         if (!grad) continue;
         const bool wide = (r.x.flags & kWide) && (grad & 1 ? grad % 16 == 1 : grad % 32 == 0);
@@ -538,25 +541,23 @@ __global__ void __launch_bounds__(kThreads) adamw_norm_kernel(const __grid_const
     pdl_begin();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     double sum = 0.0;
-    for (Run r(s); r.chunk < r.end; r.advance()) {
-        const int32_t behind = min(r.end, r.next);         // of this tensor's chunks that are the block's
-        int64_t at = (int64_t)(r.chunk - r.x.first) * kChunk + warp * kBlock;
-        const int64_t stop = min(r.x.n, (int64_t)(behind - r.x.first) * kChunk);
-        r.chunk = behind - 1;
+    for (Run r(s); r.turn < r.end; r.advance()) {
+        int64_t at = r.first() + warp * kBlock;
+        const int64_t stop = r.stop();
         const uint64_t grad = grads.at[r.i - s.first];
         if (!grad) continue;
         const bool bf = grad & 1, wide = r.x.n % 8 == 0 && (bf ? grad % 16 == 1 : grad % 32 == 0);
         constexpr int kAtOnce = 4;
-        for (; at < stop; at += kAtOnce * kChunk) {
+        for (; at < stop; at += kAtOnce * kTurn) {
             float g[kAtOnce][8];
 #pragma unroll
             for (int k = 0; k < kAtOnce; ++k) {
-                const int left = (int)max((int64_t)0, min((int64_t)kBlock, stop - (at + k * kChunk)));
+                const int left = (int)max((int64_t)0, min((int64_t)kBlock, stop - (at + k * kTurn)));
                 if (bf) {
-                    const __nv_bfloat16 *q = reinterpret_cast<const __nv_bfloat16 *>(grad - 1) + at + k * kChunk;
+                    const __nv_bfloat16 *q = reinterpret_cast<const __nv_bfloat16 *>(grad - 1) + at + k * kTurn;
                     wide ? load8<true>(g[k], q, lane, left) : load8<false>(g[k], q, lane, left);
                 } else {
-                    const float *q = reinterpret_cast<const float *>(grad) + at + k * kChunk;
+                    const float *q = reinterpret_cast<const float *>(grad) + at + k * kTurn;
                     wide ? load8<true>(g[k], q, lane, left) : load8<false>(g[k], q, lane, left);
                 }
             }
@@ -614,7 +615,7 @@ dendsn_status dendsn_adamw_plan(const dendsn_adamw_config *cfg, const dendsn_ada
             return seq_fail(DENDSN_ERR_MISALIGNED, "tensor %d: param, m, v, scales (8 bytes) or copy misaligned", i);
         chunks += chunks_of(t.n);
     }
-    if (chunks > INT32_MAX) return seq_fail(DENDSN_ERR_UNSUPPORTED, "more than 2^31 chunks of %d elements", kChunk);
+    if (chunks > INT32_MAX / 2) return seq_fail(DENDSN_ERR_UNSUPPORTED, "more than 2^30 chunks of %d elements", kChunk);
     if (table_bytes) *table_bytes = kTensorsAt + (size_t)count * sizeof(Tensor) + (size_t)chunks * 4;
     if (!table) return DENDSN_OK;
     if (!seq_aligned(table, 8)) return seq_fail(DENDSN_ERR_MISALIGNED, "table must be 8-byte aligned");
@@ -679,15 +680,15 @@ dendsn_status dendsn_adamw_step(const dendsn_adamw_config *cfg, void *plan, cons
         int sums = 0;
         for (int r = 0; r < rounds && e == cudaSuccess; ++r) {
             a.first = r * kGrads;
-            a.chunk = chunk;
+            a.turn = 2 * chunk;
             const int32_t end = std::min(count, a.first + kGrads);
             for (int32_t i = a.first; i < end; ++i) {
                 g.at[i - a.first] = grads[i] ? reinterpret_cast<uint64_t>(grads[i]) + (grad_dtypes[i] == DENDSN_BF16 ? 1 : 0) : 0;
                 chunk += (int32_t)chunks_of(sizes[i]);
             }
-            a.chunks = chunk;
+            a.turns = 2 * chunk;
             a.last = r == rounds - 1;
-            const int blocks = std::max(1, std::min(a.chunks - a.chunk, pass ? 152 * resident(cfg->state == DENDSN_STATE_E4M3) : most));
+            const int blocks = std::max(1, std::min(a.turns - a.turn, pass ? 152 * resident(cfg->state == DENDSN_STATE_E4M3) : most));
             if (pass == 0) {
                 e = seq_launch(adamw_norm_kernel, dim3((unsigned)blocks), kThreads, 0, s, 1, a, g, sums);
                 sums += blocks;
