@@ -277,6 +277,22 @@ def test_offsets_out_of_order_stay_within_the_buffers():
         assert bool((pad[0] == 7).all()) and bool((pad[2] == 7).all())
 
 
+def test_values_beyond_32_bits():
+    """v and o have more than 2^31 elements; the last sequence gives the bits it gives alone."""
+    T, B, H, Dk, Dv = 8192, 130, 16, 32, 128
+    assert T * B * H * Dv > 2 ** 31
+    one = Case("batch", T, 1, H, H, Dk, Dv, "bf16")
+    o, last = one.forward()
+    z = lambda t: torch.zeros(B, *t.shape[1:], dtype=t.dtype, device="cuda")
+    many = [z(t) for t in (*one.inputs(), one.s0)]
+    for t, x in zip(many, (*one.inputs(), one.s0)):
+        t[-1:] = x
+    cfg = binding.make_delta_config(T, B, H, H, Dk, Dv, "bf16", "batch", one.scale)
+    all_o, all_last = binding.delta_forward(cfg, *many[:5], None, many[5], want_last=True)
+    assert torch.equal(all_o[-1:], o) and torch.equal(all_last[-1:], last)
+    assert not all_o[:2].any() and not all_last[:-1].any()
+
+
 def test_empty():
     for T, B in ((0, 2), (5, 0)):
         cfg = binding.make_delta_config(T, B, 1, 2, 8, 4)
