@@ -445,7 +445,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) delta_gradients_k
     const size_t term = (size_t)a.p.DVP * C * 2;
     const int rounds = (a.p.DVP + kRound - 1) / kRound, own = lane / 8 * 8 + warp;     // own: the lane's block of 8 columns and 8 tokens
     float ey[8] = {}, vy[8] = {}, tail = 0.f;
-    bool ok = true;
+    bool ok = true;            // one value for a warp
     if (threadIdx.x < 7) {     // all of it is asked for at once, so that the later rounds find it in L2
         const uint8_t *from[] = {sat, dat, next, yat, eat, goat, vat};
         const size_t state = a.p.state_bytes, row_bytes = a.p.kept_bytes, tile = a.p.value_bytes;
@@ -476,9 +476,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) delta_gradients_k
                 floats(behind[i], next + at);
             }
         }
-        if (n) {       // the last round's products have read their tiles
-            ok = ok && tc::bar_wait(done, (n - 1) & 1);
-        }
+        if (n) ok = tc::warp_wait(ok, done, (n - 1) & 1);     // the last round's products have read their tiles
         if (here) {
             uint8_t *to = smem + P::t + (lane / 8 * 16 + warp) * kCell + (lane & 7) * 16;
 #pragma unroll
@@ -536,7 +534,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) delta_gradients_k
     for (int o = 16; o; o >>= 1) tail += __shfl_xor_sync(0xffffffffu, tail, o);
     if (lane == 0) sums[warp] = tail;
 
-    ok = ok && tc::bar_wait(done, (rounds - 1) & 1);
+    ok = tc::warp_wait(ok, done, (rounds - 1) & 1);
     tc::fence_after_sync();
     const int quarter = warp & 3, half = warp >> 2;
     const uint32_t mine = tmem + ((uint32_t)quarter << 21);
@@ -607,7 +605,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) delta_gradients_k
     tc::fence_tiles();
     tc::fence_before_sync();
     __syncthreads();
-    ok = ok && tc::bar_wait(keys_at, 0);
+    ok = tc::warp_wait(ok, keys_at, 0);
     if (warp == 0 && ok && tc::elected()) {
         tc::fence_after_sync();
         const uint32_t k = base + P::key, q = k + P::keys;
@@ -623,7 +621,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) delta_gradients_k
         tc::commit_one(done);
     }
     __syncwarp();
-    ok = ok && tc::bar_wait(done, rounds & 1);
+    ok = tc::warp_wait(ok, done, rounds & 1);
     tc::fence_after_sync();
     const int d = quarter * 32 + lane;
     const uint8_t *qm = smem + P::key + P::keys + d / 8 * kCell + (d & 7) * 2;

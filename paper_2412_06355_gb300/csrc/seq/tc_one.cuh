@@ -64,6 +64,13 @@ __device__ __forceinline__ void tmem_load(float (&v)[16], uint32_t addr) {
                  : "r"(addr) : "memory");
 }
 
+// A wait of a whole warp, in turn with those before it (`ok`): true for all its lanes or for none. Each lane looks at
+// the clock by itself, so where a wait runs out lanes may disagree; what all of them have to execute together
+// (elected below names all 32) stands behind a value that is one for the warp.
+__device__ __forceinline__ bool warp_wait(bool ok, uint32_t bar, uint32_t parity) {
+    ok = ok && bar_wait(bar, parity);
+    return __all_sync(0xffffffffu, ok);
+}
 // One lane of a whole warp, in a way that leaves the compiler's uniform registers usable.
 __device__ __forceinline__ bool elected() {
     uint32_t yes;
