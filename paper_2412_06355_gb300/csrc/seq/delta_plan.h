@@ -11,6 +11,14 @@ constexpr int kDeltaMost = 128;            // largest Dk and Dv
 constexpr int kSquare = 3 * 64 * 64 * 2;   // bytes of a chunk's square matrix in three terms
 constexpr int kGateFloats = 6 * 64;        // of a chunk and value head: see the kernels
 
+// A stage of shared memory holds chunk n's tiles, then chunk n + stages'. Each stage has a barrier of its own that says
+// it is free again, when the last product of the chunk that had it is done: its phase by phase, so that it cannot come
+// round a second time while the next tiles are waited for (they are not fetched yet). One barrier for all stages could:
+// the other stage's chunk completes it once more, and a wait for a parity then looks like one for what is to come.
+constexpr int32_t stage_at(int32_t n, int32_t stages) { return n % stages; }
+// What the fetch of chunk n (n >= stages) waits for, of that stage's barrier.
+constexpr uint32_t free_phase(int32_t n, int32_t stages) { return (uint32_t)(n / stages - 1); }
+
 // Places in bytes; sizes of one chunk (and head).
 struct DeltaPlan {
     int32_t terms;                         // bfloat16 terms of an input

@@ -170,7 +170,7 @@ __device__ __forceinline__ void keep_values(uint8_t *to, uint32_t term, int row,
 }
 
 struct Bars {
-    uint64_t tiles[2];                     // a stage's tiles have come
+    uint64_t tiles[2], free[2];            // a stage's tiles have come; all that reads them is done
     uint64_t first, second, third;         // all warps have written a round's left factors
     uint64_t one, two, three, four;        // products are done
 };
@@ -191,7 +191,7 @@ __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec
 // What both walks begin and end with.
 __device__ __forceinline__ uint32_t begin(Bars &bars, uint32_t &where, int warps) {
     if (threadIdx.x == 0) {
-        uint64_t *all[] = {&bars.tiles[0], &bars.tiles[1], &bars.one, &bars.two, &bars.three, &bars.four};
+        uint64_t *all[] = {&bars.tiles[0], &bars.tiles[1], &bars.free[0], &bars.free[1], &bars.one, &bars.two, &bars.three, &bars.four};
         for (uint64_t *b : all) tc::bar_init(tc::smem_addr(b), 1);
         tc::bar_init(tc::smem_addr(&bars.first), warps);
         tc::bar_init(tc::smem_addr(&bars.second), warps);
@@ -239,14 +239,16 @@ __global__ void __launch_bounds__(kThreads, 1) delta_forward_kernel(const __grid
         fewer_registers();
         if (warp == kWarps + 1)
             for (int n = 0; n < chunks; ++n) {
-                if (n >= stages) wait(bars.four, n - stages);      // the stage is free when all that reads it is done
+                const int at = stage_at(n, stages);
+                if (n >= stages) wait(bars.free[at], free_phase(n, stages));
                 if (!wait.all()) break;
-                load_stage(a, st, base + n % stages * st.bytes, tc::smem_addr(&bars.tiles[n % stages]), kept, a.p.xe, s.slot + n, h);
+                load_stage(a, st, base + at * st.bytes, tc::smem_addr(&bars.tiles[at]), kept, a.p.xe, s.slot + n, h);
             }
         if (warp == kWarps && tc::elected()) {
             for (int n = 0; n < chunks && wait.ok; ++n) {
-                const uint32_t tiles = base + n % stages * st.bytes, k = tiles + st.k, q = tiles + st.q, x = tiles + st.x, p = tiles + st.p;
-                wait(bars.tiles[n % stages], n / stages);
+                const int at = stage_at(n, stages);
+                const uint32_t tiles = base + at * st.bytes, k = tiles + st.k, q = tiles + st.q, x = tiles + st.x, p = tiles + st.p;
+                wait(bars.tiles[at], n / stages);
                 wait.done(bars.first, n);
                 if (!wait.ok) break;
                 tc::issue<3, NT, 3, DKP / 16, 64, W, false, 0>(tmem + kSeen, tmem + kState, DKP / 2, k, TILE);
@@ -262,6 +264,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_forward_kernel(const __grid
                 tc::commit_one(tc::smem_addr(&bars.three));
                 tc::issue<3, FEW, FEW, 4, 64, 8, false, 1>(tmem + kOut, tmem + kError, 32, p, SQ);
                 tc::commit_one(tc::smem_addr(&bars.four));
+                tc::commit_one(tc::smem_addr(&bars.free[at]));
             }
         }
         __syncwarp();
@@ -303,7 +306,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_forward_kernel(const __grid
         }
     };
     for (int n = 0; n < chunks; ++n) {
-        const int at = n % stages;
+        const int at = stage_at(n, stages);
         const int64_t hv = (s.slot + n) * a.Hv + h;
         to_lanes<3>(mine + kState + part * (OWN / 2), DKP / 2, S);
         ready(bars.first);
@@ -383,14 +386,16 @@ __global__ void __launch_bounds__(kThreads, 1) delta_backward_kernel(const __gri
         fewer_registers();
         if (warp == kWarps + 1)
             for (int n = 0; n < chunks; ++n) {
-                if (n >= stages) wait(bars.three, n - stages);
+                const int at = stage_at(n, stages);
+                if (n >= stages) wait(bars.free[at], free_phase(n, stages));
                 if (!wait.all()) break;
-                load_stage(a, st, base + n % stages * st.bytes, tc::smem_addr(&bars.tiles[n % stages]), kept, a.p.xu, s.slot + chunks - 1 - n, h);
+                load_stage(a, st, base + at * st.bytes, tc::smem_addr(&bars.tiles[at]), kept, a.p.xu, s.slot + chunks - 1 - n, h);
             }
         if (warp == kWarps && tc::elected()) {
             for (int n = 0; n < chunks; ++n) {
-                const uint32_t tiles = base + n % stages * st.bytes, k = tiles + st.k, q = tiles + st.q, x = tiles + st.x, p = tiles + st.p;
-                wait(bars.tiles[n % stages], n / stages);
+                const int at = stage_at(n, stages);
+                const uint32_t tiles = base + at * st.bytes, k = tiles + st.k, q = tiles + st.q, x = tiles + st.x, p = tiles + st.p;
+                wait(bars.tiles[at], n / stages);
                 wait.done(bars.first, n);
                 if (!wait.ok) break;
                 tc::issue<3, NT, 3, DKP / 16, 64, W, false, 0>(tmem + kY, tmem + kGrad, DKP / 2, k, TILE);
@@ -405,6 +410,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_backward_kernel(const __gri
                 if (!wait.ok) break;
                 tc::issue<3, NT, 3, 4, DKP, W, true, 0>(tmem + kY, tmem + kD, 32, k, TILE);
                 tc::commit_one(tc::smem_addr(&bars.three));
+                tc::commit_one(tc::smem_addr(&bars.free[at]));
             }
         }
         __syncwarp();
@@ -425,7 +431,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_backward_kernel(const __gri
     Ahead<T> ahead;
     fetch(ahead, go + first + (int64_t)(chunks - 1) * C * stride, stride, here && chunks ? s.length - (chunks - 1) * C - tok0 : 0);
     for (int n = 0; n < chunks; ++n) {
-        const int chunk = chunks - 1 - n, at = n % stages;
+        const int chunk = chunks - 1 - n, at = stage_at(n, stages);
         const int64_t hv = (s.slot + chunk) * a.Hv + h;
         to_lanes<3>(mine + kGrad + part * (OWN / 2), DKP / 2, D);
         to_lanes<NT>(mine + kGo + part * (kTokens / 2), 32, ahead);
