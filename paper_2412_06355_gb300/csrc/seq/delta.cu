@@ -22,7 +22,7 @@
 // All sums are float32. Products run on the matrix instruction for 16-bit operands: bfloat16 inputs are
 // exact, everything else (float32 inputs, states, results on their way to the next product) is split into
 // three bfloat16 terms, whose leading products (three with an exact factor, six without) leave 2^-24.
-// Where only a bfloat16 gradient of k (or o) comes of it, two terms (2^-17 of each factor).
+// Where only a bfloat16 gradient of k comes of it, two terms (2^-17 of each factor).
 #include <cuda_bf16.h>
 
 #include <algorithm>

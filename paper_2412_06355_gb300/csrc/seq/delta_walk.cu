@@ -219,7 +219,6 @@ template <typename T, int DKP, bool KEEP>
 __global__ void __launch_bounds__(kThreads, 1) delta_forward_kernel(const __grid_constant__ Args a, const T *v, const float *s0, T *o, float *last,
                                                                     uint8_t *kept, int stages, int columns) {
     constexpr int NT = sizeof(T) == 2 ? 1 : 3, W = DKP / 8, TILE = 64 * DKP * 2, SQ = kSquare / 3, OWN = DKP / kParts;
-    constexpr int FEW = sizeof(T) == 2 ? 2 : 3;        // terms where only a bfloat16 output comes of it
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ Bars bars;
     __shared__ uint32_t where;
@@ -253,7 +252,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_forward_kernel(const __grid
                 if (!wait.ok) break;
                 tc::issue<3, NT, 3, DKP / 16, 64, W, false, 0>(tmem + kSeen, tmem + kState, DKP / 2, k, TILE);
                 tc::commit_one(tc::smem_addr(&bars.one));
-                tc::issue<3, NT, FEW, DKP / 16, 64, W, false, 0>(tmem + kSeen + 64, tmem + kState, DKP / 2, q, TILE);
+                tc::issue<3, NT, 3, DKP / 16, 64, W, false, 0>(tmem + kSeen + 64, tmem + kState, DKP / 2, q, TILE);
                 wait.done(bars.second, n);
                 if (!wait.ok) break;
                 tc::issue<3, 3, 3, 4, 64, 8, false, 1>(tmem + kOut, tmem + kError, 32, x, SQ);
@@ -262,7 +261,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_forward_kernel(const __grid
                 if (!wait.ok) break;
                 tc::issue<3, NT, 3, 4, DKP, W, true, 0>(tmem + kSeen, tmem + kState, 32, k, TILE);
                 tc::commit_one(tc::smem_addr(&bars.three));
-                tc::issue<3, FEW, FEW, 4, 64, 8, false, 1>(tmem + kOut, tmem + kError, 32, p, SQ);
+                tc::issue<3, 3, 3, 4, 64, 8, false, 1>(tmem + kOut, tmem + kError, 32, p, SQ);
                 tc::commit_one(tc::smem_addr(&bars.four));
                 tc::commit_one(tc::smem_addr(&bars.free[at]));
             }
