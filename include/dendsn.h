@@ -422,8 +422,8 @@ dendsn_status dendsn_norm_backward(const dendsn_norm_config *cfg, const void *su
  * multiplied by zero (it has to be finite) and the gate's gradient is 0. NaN and infinities in a sequence
  * reach the tokens behind them and all of their own chunk of 64 tokens, no other sequence.
  * bfloat16 inputs enter the products exactly, float32 inputs as three bfloat16 terms (2^-24); states and
- * everything between the products are float32, in three terms as well where they are factors. grad_k of
- * bfloat16 inputs comes of states, e and y in two terms (2^-17).
+ * everything between the products are float32, in three terms as well where they are factors, whatever the
+ * inputs' type. Exponentials of differences of the gates' sums are the hardware's powers of two (2^-22).
  * last may be s0 itself. saved: written by the forward where not NULL and read by the backward, which
  * needs the same config and offsets, and neither the inputs nor s0. scratch: forward_bytes where saved is
  * NULL, else none; backward_bytes. Both 256-byte aligned. 1 <= Dk, Dv <= 128.

@@ -22,7 +22,6 @@
 // All sums are float32. Products run on the matrix instruction for 16-bit operands: bfloat16 inputs are
 // exact, everything else (float32 inputs, states, results on their way to the next product) is split into
 // three bfloat16 terms, whose leading products (three with an exact factor, six without) leave 2^-24.
-// Where only a bfloat16 gradient of k comes of it, two terms (2^-17 of each factor).
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -327,13 +326,15 @@ __global__ void __launch_bounds__(128) delta_prepare_kernel(const __grid_constan
 constexpr int kRound = 32;
 template <int NT, int DKP>
 struct Parts {
-    static constexpr int FEW = NT == 1 ? 2 : 3;           // terms where a bfloat16 comes of it
     static constexpr uint32_t pair = kRound / 8 * 16 * kCell, error = kRound / 8 * 8 * kCell, state = kRound * DKP * 2;     // bytes of a term
-    static constexpr uint32_t t = 0, e = t + FEW * pair, s = e + 3 * error, d = s + 3 * state, key = d + FEW * state;
-    static constexpr uint32_t keys = NT * C * DKP * 2, end = key + 2 * keys + kCell * 8;    // (64 places: left factors read past their rows)
-    // the square matrices of the chunk, where the rounds' tiles were
-    static constexpr uint32_t a = 0, c = kSquare;
-    static_assert(c + FEW * (kSquare / 3) <= key, "what is laid over fits");
+    static constexpr uint32_t t = 0, e = t + 3 * pair, s = e + 3 * error, d = s + 3 * state, rounds = d + 3 * state;
+    // where the rounds' tiles were: the square matrices of the chunk, and behind them, of one term, k and q, which come
+    // then, so that two blocks share an SM (three terms: beside the tiles, from the start)
+    static constexpr bool LATE = NT == 1;
+    static constexpr uint32_t a = 0, c = kSquare, key = LATE ? c + kSquare : rounds, keys = NT * C * DKP * 2;
+    static_assert(c + kSquare <= key, "what is laid over fits");
+    // (64 places: left factors read past their rows)
+    static constexpr uint32_t end = (rounds > key + 2 * keys ? rounds : key + 2 * keys) + kCell * 8;
 };
 // 8 values as bfloat16 terms, 16 bytes each.
 template <int N>
@@ -401,7 +402,6 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) delta_gradients_k
                                                                                        T *gq, T *gk, T *gv, float *ggate, float *gbeta) {
     constexpr int NT = sizeof(T) == 2 ? 1 : 3, W = DKP / 8, TILE = C * DKP * 2, SQ = kSquare / 3;
     using P = Parts<NT, DKP>;
-    constexpr int FEW = P::FEW;
     constexpr uint32_t LOW = NT == 1 ? 0 : kSums, kGradColumns = kSums + LOW;      // where the small products' sums are
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ uint64_t keys_bar, done_bar;
@@ -419,16 +419,21 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) delta_gradients_k
         tc::bar_init(keys_at, 1);
         tc::bar_init(done, 1);
         tc::bar_init_fence();
-        tc::bar_expect(keys_at, 2 * P::keys);
-        load_bytes(base + P::key, kept + a.p.k + hk * a.p.key_bytes, P::keys, keys_at);
-        load_bytes(base + P::key + P::keys, kept + a.p.q + hk * a.p.key_bytes, P::keys, keys_at);
     }
+    const uint8_t *kat = kept + a.p.k + hk * a.p.key_bytes, *qat = kept + a.p.q + hk * a.p.key_bytes;
+    auto load_keys = [&] {
+        if (threadIdx.x) return;
+        tc::bar_expect(keys_at, 2 * P::keys);
+        load_bytes(base + P::key, kat, P::keys, keys_at);
+        load_bytes(base + P::key + P::keys, qat, P::keys, keys_at);
+    };
+    if (!P::LATE) load_keys();
     if (warp == 0) tc::tmem_alloc_one(tc::smem_addr(&where), kGradColumns);
     const float *gin = reinterpret_cast<const float *>(kept + a.p.gates) + hv * kGateFloats;
     for (int i = threadIdx.x; i < kGateFloats; i += 256) gates[i] = gin[i];
-    if (NT == 1)       // go has no second term
-        for (int i = threadIdx.x; i < kRound / 8 * 64; i += 256)
-            *reinterpret_cast<uint4 *>(smem + P::t + P::pair + (i / 64 * 16 * kCell) + i % 64 * 16) = make_uint4(0, 0, 0, 0);
+    if (NT == 1)       // go has no second and third term
+        for (int i = threadIdx.x; i < 2 * kRound / 8 * 64; i += 256)
+            *reinterpret_cast<uint4 *>(smem + P::t + (1 + i / (kRound / 8 * 64)) * P::pair + (i / 64 % (kRound / 8) * 16 * kCell) + i % 64 * 16) = make_uint4(0, 0, 0, 0);
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
@@ -446,10 +451,10 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) delta_gradients_k
     const int rounds = (a.p.DVP + kRound - 1) / kRound, own = lane / 8 * 8 + warp;     // own: the lane's block of 8 columns and 8 tokens
     float ey[8] = {}, vy[8] = {}, tail = 0.f;
     bool ok = true;            // one value for a warp
-    if (threadIdx.x < 7) {     // all of it is asked for at once, so that the later rounds find it in L2
-        const uint8_t *from[] = {sat, dat, next, yat, eat, goat, vat};
+    if (threadIdx.x < (P::LATE ? 9 : 7)) {     // all of it is asked for at once, so that the later rounds find it in L2
+        const uint8_t *from[] = {sat, dat, next, yat, eat, goat, vat, kat, qat};
         const size_t state = a.p.state_bytes, row_bytes = a.p.kept_bytes, tile = a.p.value_bytes;
-        const size_t bytes[] = {state, state, state, row_bytes, row_bytes, tile, tile};
+        const size_t bytes[] = {state, state, state, row_bytes, row_bytes, tile, tile, P::keys, P::keys};
         asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(from[threadIdx.x]), "r"((uint32_t)bytes[threadIdx.x]) : "memory");
     }
     for (int n = 0; n < rounds; ++n) {
@@ -481,7 +486,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) delta_gradients_k
             uint8_t *to = smem + P::t + (lane / 8 * 16 + warp) * kCell + (lane & 7) * 16;
 #pragma unroll
             for (int m = 0; m < NT; ++m) *reinterpret_cast<uint4 *>(to + m * P::pair) = go.r[m];
-            put_terms<FEW>(to + 8 * kCell, P::pair, y);
+            put_terms<3>(to + 8 * kCell, P::pair, y);
             put_terms<3>(smem + P::e + own * kCell + (lane & 7) * 16, P::error, e);
             float x[8];
             v.get(x);
@@ -499,7 +504,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) delta_gradients_k
             const int lot = threadIdx.x + i * 256;
             if (lot < count * W) {
                 put_terms<3>(smem + P::s + lot * 16, P::state, S[i]);
-                put_terms<FEW>(smem + P::d + lot * 16, P::state, D[i]);
+                put_terms<3>(smem + P::d + lot * 16, P::state, D[i]);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) tail = fmaf(behind[i][j], D[i][j], tail);
             }
@@ -513,12 +518,12 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) delta_gradients_k
             const bool more = n, after = LOW ? more : true;
             tc::issue_tiles<3, NT, 1, 3, W, 16, true, 0>(tmem + LOW + kGoS, base + P::s, P::state, go_at, P::pair, steps, more);
             tc::issue_tiles<3, NT, 0, 1, W, 16, true, 0>(tmem + kGoS, base + P::s, P::state, go_at, P::pair, steps, after);
-            tc::issue_tiles<3, FEW, 1, FEW, W, 16, true, 0>(tmem + LOW + kYS, base + P::s, P::state, y_at, P::pair, steps, more);
-            tc::issue_tiles<3, FEW, 0, 1, W, 16, true, 0>(tmem + kYS, base + P::s, P::state, y_at, P::pair, steps, after);
-            tc::issue_tiles<FEW, 3, 1, FEW, W, 8, true, 0>(tmem + LOW + kED, base + P::d, P::state, base + P::e, P::error, steps, more);
-            tc::issue_tiles<FEW, 3, 0, 1, W, 8, true, 0>(tmem + kED, base + P::d, P::state, base + P::e, P::error, steps, after);
-            tc::issue_tiles<FEW, 3, 1, 3, 16, 8, true, 0>(tmem + LOW + kAE, go_at, P::pair, base + P::e, P::error, steps, more);
-            tc::issue_tiles<FEW, 3, 0, 1, 16, 8, true, 0>(tmem + kAE, go_at, P::pair, base + P::e, P::error, steps, after);
+            tc::issue_tiles<3, 3, 1, 3, W, 16, true, 0>(tmem + LOW + kYS, base + P::s, P::state, y_at, P::pair, steps, more);
+            tc::issue_tiles<3, 3, 0, 1, W, 16, true, 0>(tmem + kYS, base + P::s, P::state, y_at, P::pair, steps, after);
+            tc::issue_tiles<3, 3, 1, 3, W, 8, true, 0>(tmem + LOW + kED, base + P::d, P::state, base + P::e, P::error, steps, more);
+            tc::issue_tiles<3, 3, 0, 1, W, 8, true, 0>(tmem + kED, base + P::d, P::state, base + P::e, P::error, steps, after);
+            tc::issue_tiles<3, 3, 1, 3, 16, 8, true, 0>(tmem + LOW + kAE, go_at, P::pair, base + P::e, P::error, steps, more);
+            tc::issue_tiles<3, 3, 0, 1, 16, 8, true, 0>(tmem + kAE, go_at, P::pair, base + P::e, P::error, steps, after);
             tc::commit_one(done);
         }
         __syncwarp();
@@ -536,6 +541,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) delta_gradients_k
 
     ok = tc::warp_wait(ok, done, (rounds - 1) & 1);
     tc::fence_after_sync();
+    if (P::LATE && ok) load_keys();
     const int quarter = warp & 3, half = warp >> 2;
     const uint32_t mine = tmem + ((uint32_t)quarter << 21);
     auto sum_load = [&](float (&x)[16], uint32_t from) {
@@ -571,8 +577,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) delta_gradients_k
         for (int c = 0; c < 2; ++c) {
             uint8_t *to = smem + (isc ? P::c : P::a) + (i / 8 * 8 + j0 / 8 + c) * kCell + (i & 7) * 16;
             const float z[8] = {x[8 * c], x[8 * c + 1], x[8 * c + 2], x[8 * c + 3], x[8 * c + 4], x[8 * c + 5], x[8 * c + 6], x[8 * c + 7]};
-            if (isc) put_terms<FEW>(to, SQ, z);
-            else put_terms<3>(to, SQ, z);
+            put_terms<3>(to, SQ, z);
         }
     }
     // what has come through the states, scaled, in place
@@ -612,12 +617,12 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) delta_gradients_k
         const bool after = !LOW;
         tc::issue_tiles<NT, 3, 1, 3, W, 8, false, 1>(tmem + LOW + kAE, k, TILE, base + P::a, SQ, 4, false);
         tc::issue_tiles<NT, 3, 0, 1, W, 8, false, 1>(tmem + kAE, k, TILE, base + P::a, SQ, 4, after);
-        tc::issue_tiles<NT, FEW, 1, FEW, W, 8, true, 2>(tmem + LOW + kED, q, TILE, base + P::a, SQ, 4, false);
-        tc::issue_tiles<NT, FEW, 1, FEW, W, 8, false, 1>(tmem + LOW + kED, k, TILE, base + P::c, SQ, 4, true);
-        tc::issue_tiles<NT, FEW, 1, FEW, W, 8, true, 2>(tmem + LOW + kED, k, TILE, base + P::c, SQ, 4, true);
-        tc::issue_tiles<NT, FEW, 0, 1, W, 8, true, 2>(tmem + kED, q, TILE, base + P::a, SQ, 4, after);
-        tc::issue_tiles<NT, FEW, 0, 1, W, 8, false, 1>(tmem + kED, k, TILE, base + P::c, SQ, 4, true);
-        tc::issue_tiles<NT, FEW, 0, 1, W, 8, true, 2>(tmem + kED, k, TILE, base + P::c, SQ, 4, true);
+        tc::issue_tiles<NT, 3, 1, 3, W, 8, true, 2>(tmem + LOW + kED, q, TILE, base + P::a, SQ, 4, false);
+        tc::issue_tiles<NT, 3, 1, 3, W, 8, false, 1>(tmem + LOW + kED, k, TILE, base + P::c, SQ, 4, true);
+        tc::issue_tiles<NT, 3, 1, 3, W, 8, true, 2>(tmem + LOW + kED, k, TILE, base + P::c, SQ, 4, true);
+        tc::issue_tiles<NT, 3, 0, 1, W, 8, true, 2>(tmem + kED, q, TILE, base + P::a, SQ, 4, after);
+        tc::issue_tiles<NT, 3, 0, 1, W, 8, false, 1>(tmem + kED, k, TILE, base + P::c, SQ, 4, true);
+        tc::issue_tiles<NT, 3, 0, 1, W, 8, true, 2>(tmem + kED, k, TILE, base + P::c, SQ, 4, true);
         tc::commit_one(done);
     }
     __syncwarp();

@@ -90,3 +90,55 @@ def test_outputs_read_the_writes_in_three_terms(dtype, gates):
     M = (2 * v * beta[:, :1, :, None]).double()[:, 2:] * torch.exp(gate.double().cumsum(1))[:, 2:, :, None]
     small("o", got["o"][:, 2:], want["o"][:, 2:], M)
     small("o", served[:, 2:], want["o"][:, 2:], M)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gk_reads_the_states_gradient_in_three_terms(dtype):
+    a, v = rand(5, B, H, 64), torch.zeros(B, 2, H, 2, device="cuda")
+    v[..., 0], v[..., 1] = 1, -1
+    got, want, _ = run(dtype, 2, 64, 2, v=v, glast=torch.stack([a, a * (1 + EPS)], 3))
+    small("gk", got["gk"], want["gk"], 2 * a.double()[:, None])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("which", ["e", "y"])
+def test_gk_reads_e_and_y_in_three_terms(dtype, which):
+    """gk = D e - S y of one token with k along the first place, whose row one of the two matrices has."""
+    Dk = 64
+    a = rand(6, B, H)
+    first, other = torch.zeros(B, H, Dk, 2, device="cuda"), torch.zeros(B, H, Dk, 2, device="cuda")
+    first[:, :, 0, 0], first[:, :, 0, 1] = a, a * (1 + EPS)
+    other[:, :, 1:, 0], other[:, :, 1:, 1] = 1, -1
+    k = torch.zeros(B, 1, H, Dk, device="cuda")
+    k[..., 0] = 1
+    got, want, _ = run(dtype, 1, Dk, 2, k=k, **(dict(s0=first, glast=other) if which == "e" else dict(s0=other, glast=first)))
+    M = (2 * a.double())[:, None, :, None]
+    small("gk", got["gk"][..., 1:], want["gk"][..., 1:], M.expand(B, 1, H, Dk - 1))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gk_reads_the_chunks_matrices_in_three_terms(dtype):
+    """go_i . u_j along tokens whose queries cancel, and y_i . u_j, b_i near 1, against what comes through the state."""
+    T, Dk = 40, 8
+    q = torch.zeros(B, T, H, Dk, device="cuda")
+    q[:, 20], q[:, 21] = 1, -1
+    beta, go = rand(7, B, T, H) / 2, torch.zeros(B, T, H, DV, device="cuda")
+    gate = torch.zeros(B, T, H, device="cuda")
+    gate[:, 21] = -EPS
+    go[:, 20] = go[:, 21] = rand(8, B, H, DV)
+    v = rand(9, B, T, H, DV)
+    got, want, _ = run(dtype, T, Dk, q=q, beta=beta, gate=gate, go=go, v=v)
+    dot = (go[:, 20:21].to(DT[dtype]).double() * v.to(DT[dtype]).double()).sum(-1) * beta.double()
+    small("gk", got["gk"][:, :20], want["gk"][:, :20], 2 * dot[:, :20, :, None].expand(B, 20, H, Dk))
+
+    k = torch.zeros(B, T, H, Dk, device="cuda")
+    k[:, 20:, :, 0] = 1
+    beta = torch.ones(B, T, H, device="cuda")
+    beta[:, :20] = rand(10, B, 20, H) / 2
+    beta[:, 20] = 1 - 2.0 ** -9 * rand(11, B, H)
+    beta[:, 21:] = 0
+    glast = torch.zeros(B, H, Dk, DV, device="cuda")
+    glast[:, :, 0] = rand(12, B, H, DV)
+    got, want, _ = run(dtype, T, Dk, k=k, beta=beta, v=v, glast=glast)
+    dot = (glast[:, None, :, 0].double() * v.to(DT[dtype]).double()).sum(-1) * beta.double()
+    small("gk", got["gk"][:, :20, :, 0], want["gk"][:, :20, :, 0], 2 * dot[:, :20])
