@@ -990,9 +990,9 @@ dendsn_status dendsn_delta_forward(const dendsn_delta_config *cfg, const void *q
             e = bf ? (a.p.DKP == 64 ? go(run_forward<__nv_bfloat16, 64>) : go(run_forward<__nv_bfloat16, 128>))
                    : (a.p.DKP == 64 ? go(run_forward<float, 64>) : go(run_forward<float, 128>));
         }
-        if (e == cudaSuccess && packed && cfg->rest == DENDSN_REST_ZERO && tokens)
-            e = fill_rest(a, {{static_cast<uint8_t *>(o)}, {(int64_t)sx * cfg->Hv * cfg->Dv}}, s, &launches);
     }
+    if (e == cudaSuccess && packed && cfg->rest == DENDSN_REST_ZERO && tokens)     // (all of them where there is no sequence)
+        e = fill_rest(a, {{static_cast<uint8_t *>(o)}, {(int64_t)sx * cfg->Hv * cfg->Dv}}, s, &launches);
     if (e != cudaSuccess) return seq_fail(DENDSN_ERR_CUDA, "delta forward launch failed: %s", cudaGetErrorString(e));
     seq_count_launches(launches);
     return DENDSN_OK;
@@ -1025,11 +1025,11 @@ dendsn_status dendsn_delta_backward(const dendsn_delta_config *cfg, const void *
         };
         e = bf ? (a.p.DKP == 64 ? go(run_backward<__nv_bfloat16, 64>) : go(run_backward<__nv_bfloat16, 128>))
                : (a.p.DKP == 64 ? go(run_backward<float, 64>) : go(run_backward<float, 128>));
-        if (e == cudaSuccess && packed && cfg->rest == DENDSN_REST_ZERO && tokens) {
-            const int64_t nk = (int64_t)sx * cfg->Hk * cfg->Dk, nv = (int64_t)sx * cfg->Hv * cfg->Dv, ng = 4 * (int64_t)cfg->Hv;
-            e = fill_rest(a, {{static_cast<uint8_t *>(grad_q), static_cast<uint8_t *>(grad_k), static_cast<uint8_t *>(grad_v),
-                               reinterpret_cast<uint8_t *>(grad_gate), reinterpret_cast<uint8_t *>(grad_beta)}, {nk, nk, nv, ng, ng}}, s, &launches);
-        }
+    }
+    if (e == cudaSuccess && packed && cfg->rest == DENDSN_REST_ZERO && tokens) {
+        const int64_t nk = (int64_t)sx * cfg->Hk * cfg->Dk, nv = (int64_t)sx * cfg->Hv * cfg->Dv, ng = 4 * (int64_t)cfg->Hv;
+        e = fill_rest(a, {{static_cast<uint8_t *>(grad_q), static_cast<uint8_t *>(grad_k), static_cast<uint8_t *>(grad_v),
+                           reinterpret_cast<uint8_t *>(grad_gate), reinterpret_cast<uint8_t *>(grad_beta)}, {nk, nk, nv, ng, ng}}, s, &launches);
     }
     if (e != cudaSuccess) return seq_fail(DENDSN_ERR_CUDA, "delta backward launch failed: %s", cudaGetErrorString(e));
     seq_count_launches(launches);
