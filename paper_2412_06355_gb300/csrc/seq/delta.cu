@@ -920,7 +920,7 @@ cudaError_t run_backward(const Args &a, const void *go, const float *glast, cons
     const dim3 chunks((unsigned)a.p.slots, (unsigned)a.Hv);
     cudaError_t e = delta_walk_backward(a, NT == 1, go, glast, kept, scratch, gs0, s);
     ++*launches;
-    if (!a.p.slots || e != cudaSuccess) return e;
+    if (!a.p.tokens || e != cudaSuccess) return e;     // (packed sequences have slots without tokens too)
     constexpr size_t smem = Parts<NT, DKP>::end;
     e = room(delta_gradients_kernel<T, DKP>, smem);
     if (e == cudaSuccess)

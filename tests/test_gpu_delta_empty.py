@@ -65,3 +65,24 @@ def test_no_sequence_through_autograd():
     o, _ = DeltaFunction.apply(*leaves, None, torch.zeros(1, dtype=torch.int32, device="cuda"), 1.0, "packed")
     assert not o.any()
     assert not any(g.any() for g in torch.autograd.grad((o * go).sum(), leaves))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B", [1, 2, 70])
+def test_sequences_without_a_token(dtype, B):
+    """Two value heads share a key head, and there is no token whose gradients could be added up."""
+    ins, go = tensors(0, dtype)
+    offsets = torch.zeros(B + 1, dtype=torch.int32, device="cuda")
+    s0, glast = (torch.randn(B, HV, DK, DV, device="cuda") for _ in range(2))
+    cfg = binding.make_delta_config(0, B, HK, HV, DK, DV, "f32" if dtype is torch.float32 else "bf16", "packed")
+    _, last = binding.delta_forward(cfg, *ins, offsets, s0, want_last=True)
+    assert torch.equal(last, s0)
+    saved = binding.delta_workspace(cfg)
+    o, last = binding.delta_forward(cfg, *ins, offsets, s0, saved=saved, want_last=True)
+    assert o.shape == (0, HV, DV) and torch.equal(last, s0)
+    g = binding.delta_backward(cfg, *ins, go, offsets, s0, glast, saved)
+    assert torch.equal(g["gs0"], glast) and g["gk"].shape == (0, HK, DK)
+    leaves = [t.requires_grad_() for t in ins] + [s0.requires_grad_()]
+    _, last = DeltaFunction.apply(*leaves, offsets, 1.0, "packed")
+    grads = torch.autograd.grad((last * glast).sum(), leaves)
+    assert torch.equal(grads[5], glast)
