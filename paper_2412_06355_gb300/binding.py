@@ -1266,21 +1266,30 @@ class DeltaFunction(torch.autograd.Function):
             T, B = q.shape[:2] if layout == "time" else (q.shape[1], q.shape[0])
         ctx.cfg = make_delta_config(T, B, q.shape[-2], v.shape[-2], q.shape[-1], v.shape[-1],
                                     _dtype_name(q), layout, scale)
-        ctx.saved = delta_workspace(ctx.cfg, q.device) if any(ctx.needs_input_grad) else None
-        o, last = delta_forward(ctx.cfg, q, k, v, gate, beta, offsets, s0, saved=ctx.saved,
-                                want_last=True)
-        ctx.save_for_backward(q, k, v, gate, beta, s0, offsets)
+        saved = delta_workspace(ctx.cfg, q.device) if any(ctx.needs_input_grad) else None
+        o, last = delta_forward(ctx.cfg, q, k, v, gate, beta, offsets, s0, saved=saved, want_last=True)
+        # the workspace holds all that the backward reads, and goes when the graph's buffers go
+        ctx.save_for_backward(saved, offsets)
+        ctx.device, ctx.state = q.device, s0 is not None
         ctx.set_materialize_grads(False)
         return o, last
 
     @staticmethod
     @once_differentiable
     def backward(ctx, go, glast):
-        q, k, v, gate, beta, s0, offsets = ctx.saved_tensors
-        go = torch.zeros_like(v) if go is None else go.contiguous()
-        g = delta_backward(ctx.cfg, q, k, v, gate, beta, go, offsets, s0,
-                           None if glast is None else glast.contiguous(), ctx.saved)
-        return g["gq"], g["gk"], g["gv"], g["ggate"], g["gbeta"], g.get("gs0"), None, None, None
+        saved, offsets = ctx.saved_tensors
+        cfg, lead, dt = ctx.cfg, _delta_lead(ctx.cfg), _xdtype(ctx.cfg)
+
+        def new(dtype, *shape):
+            return torch.empty(shape, dtype=dtype, device=ctx.device)
+
+        go = new(dt, *lead, cfg.Hv, cfg.Dv).zero_() if go is None else go.contiguous()
+        grads = [new(dt, *lead, cfg.Hk, cfg.Dk), new(dt, *lead, cfg.Hk, cfg.Dk), new(dt, *lead, cfg.Hv, cfg.Dv),
+                 new(torch.float32, *lead, cfg.Hv), new(torch.float32, *lead, cfg.Hv),
+                 new(torch.float32, cfg.B, cfg.Hv, cfg.Dk, cfg.Dv) if ctx.state else None]
+        dendsn_delta_backward(_no_rest(cfg), go, offsets, None if glast is None else glast.contiguous(), saved, *grads,
+                              _scratch(dendsn_delta_workspace_size(cfg)[2], ctx.device))
+        return (*grads, None, None, None)
 
 
 class XentFunction(torch.autograd.Function):
