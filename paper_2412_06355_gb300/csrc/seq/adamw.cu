@@ -296,10 +296,10 @@ __device__ __forceinline__ void update(Share<true> &r, const Tensor &x, int64_t 
     const float tm = __uint_as_float(warp_top(__float_as_uint(top_m))), tv = __uint_as_float(warp_top(__float_as_uint(top_v)));
     // Below 2^-110 a block's states are zeros: 448 / top would leave float32. (A value that rounding brings above 448 stays
     // below what the largest random number lifts to the next code, and its square's share below the smallest's.)
-    const F2 im = both(tm < 0x1p-110f ? 0.f : __frcp_rn(tm) * 448.f), iv = both(tv < 0x1p-110f ? 0.f : __frcp_rn(tv) * 448.f);
+    const F2 im = both(tm < 0x1p-110f ? 0.f : from_top(tm)), iv = both(tv < 0x1p-110f ? 0.f : from_top(tv));
     if (lane == 0)
         *reinterpret_cast<float2 *>(x.scales + at / kBlock * 2) =
-            make_float2(tm < 0x1p-110f ? 0.f : tm * (1.f / 448.f), tv < 0x1p-110f ? 0.f : tv * (1.f / 448.f));
+            make_float2(tm < 0x1p-110f ? 0.f : to_top(tm), tv < 0x1p-110f ? 0.f : to_top(tv));
     const uint32_t first = ((uint32_t)at + (WIDE ? lane * 8 : lane)) * kStride + start;
     uint32_t cm[8], cv[8], sign[8];
 #pragma unroll

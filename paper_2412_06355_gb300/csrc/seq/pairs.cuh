@@ -40,6 +40,17 @@ __device__ __forceinline__ float rcp_fast(float v) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
+// The largest value of an e4m3 code is 448: 448 / top and top / 448 as divisions round them, for top from 2^-110 on.
+// Approximate quotients corrected by what they leave (Markstein's division step). A division each, of which every
+// lane of a warp has two for its 8 elements, cost the optimizer's step with 8-bit states 5%.
+__device__ __forceinline__ float from_top(float top) {
+    const float t = top * 0x1p-9f, r = rcp_fast(t), q = r * 0.875f;      // (1 / top itself would leave float32's normal numbers)
+    return fmaf(fmaf(-q, t, 0.875f), r, q);
+}
+__device__ __forceinline__ float to_top(float top) {
+    const float q = top * (1.f / 448.f);
+    return fmaf(fmaf(-q, 448.f, top), 1.f / 448.f, q);
+}
 // The larger of three (of NaN and a number, the number).
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
