@@ -196,14 +196,6 @@ __device__ __forceinline__ uint32_t warp_top(uint32_t t) {
     for (int o = 16; o; o >>= 1) t = max(t, __shfl_xor_sync(0xffffffffu, t, o));
     return t;
 }
-// The hardware's reciprocal root, of numbers from float32's smallest normal one on (of what is below, as of that one,
-// so that the root of zero is zero).
-__device__ __forceinline__ float rsqrt_fast(float v) {
-    float r;
-    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(fmaxf(v, 0x1p-126f)));
-    return r;
-}
-
 struct Scalars {
     float factor, rate, inverse_root, lr;
     uint32_t start;
@@ -279,9 +271,7 @@ __device__ __forceinline__ void update(Share<true> &r, const Tensor &x, int64_t 
         m[j] = add(mul(fma(old, minus, g), rest1), old);
         const F2 w = mul(F2(vc[2 * j], vc[2 * j + 1]), scale_v), w2 = mul(w, w);
         const F2 v = add(mul(fma(w2, minus, mul(g, g)), rest2), w2);
-        // the root from the hardware's reciprocal root and one step of Newton's
-        const F2 y(rsqrt_fast(v.x()), rsqrt_fast(v.y())), near = mul(v, y);
-        root[j] = fma(fma(mul(near, minus), near, v), mul(y, both(0.5f)), near);
+        root[j] = root_of(v);
         const F2 below = fma(root[j], inverse_root, eps);
         const F2 p = fma(mul(m[j], F2(rcp_fast(below.x()), rcp_fast(below.y()))), rate, mul(F2(r.p[2 * j], r.p[2 * j + 1]), kept));
         r.p[2 * j] = p.x(), r.p[2 * j + 1] = p.y();

@@ -51,6 +51,18 @@ __device__ __forceinline__ float to_top(float top) {
     const float q = top * (1.f / 448.f);
     return fmaf(fmaf(-q, 448.f, top), 1.f / 448.f, q);
 }
+// Roots from the hardware's reciprocal root (of denormal numbers too) and one step of Newton's: the square root's own
+// bits for every number from 2^-102 on; below that what the step corrects by is a denormal number itself, and the root
+// within some 2^-20. The root of zero is zero.
+__device__ __forceinline__ float rsqrt_fast(float v) {
+    float r;
+    asm("rsqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(fmaxf(v, 0x1p-149f)));
+    return r;
+}
+__device__ __forceinline__ F2 root_of(F2 v) {
+    const F2 y(rsqrt_fast(v.x()), rsqrt_fast(v.y())), near = mul(v, y);
+    return fma(fma(mul(near, both(-1.f)), near, v), mul(y, both(0.5f)), near);
+}
 // The larger of three (of NaN and a number, the number).
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;

@@ -28,7 +28,7 @@ def probe(tmp_path_factory):
     subprocess.run([lib_build.nvcc(), *lib_build.ARCH, *lib_build.NVCC_FLAGS, "-shared", "-o", so,
                     os.path.join(HERE, "adamw_probe.cu")], check=True)
     lib = ctypes.CDLL(so)
-    lib.run_quotients.argtypes = [ctypes.c_uint32, ctypes.c_uint32, ctypes.c_void_p]
+    lib.run_quotients.argtypes = lib.run_roots.argtypes = [ctypes.c_uint32, ctypes.c_uint32, ctypes.c_void_p]
     return lib
 
 
@@ -42,6 +42,36 @@ def test_quotients_with_448_are_the_divisions(probe, exponent):
     wrong = torch.zeros(2, dtype=torch.int32, device="cuda")
     assert probe.run_quotients(bits(exponent), 1 << 23, wrong.data_ptr()) == 0
     assert wrong.tolist() == [0, 0]
+
+
+@pytest.mark.parametrize("exponent", [-102, -30, 0, 1, 126, 127])
+def test_roots_are_the_square_roots(probe, exponent):
+    """All mantissas of numbers whose root's correction is no denormal number; even and odd exponents."""
+    wrong = torch.zeros(2, dtype=torch.int32, device="cuda")
+    assert probe.run_roots(bits(exponent), 1 << 23, wrong.data_ptr()) == 0
+    assert wrong.tolist() == [0, 0]
+
+
+@pytest.mark.parametrize("exponent", [-126, -125, -104, -103])
+def test_roots_of_small_numbers(probe, exponent):
+    wrong = torch.zeros(2, dtype=torch.int32, device="cuda")
+    assert probe.run_roots(bits(exponent), 1 << 23, wrong.data_ptr()) == 0
+    assert wrong[1] == 0
+
+
+def test_tiny_gradients_have_roots():
+    """Squares that are denormal numbers: v = g^2 rounded to float32, then its root. With a first step of betas 0 and no
+    eps the parameter moves by g / root, which the square's own rounding (half of 2^-149) takes from 1 by less than
+    2^-150 / g^2; a root without the numbers below 2^-126 was off by half and more."""
+    n = 1 << 16
+    g = gradients(n, 4).sign() * torch.exp2(-65.0 - 4.0 * torch.rand(n, device="cuda", generator=torch.Generator(device="cuda").manual_seed(5)))
+    s = Eight(n).run(g, lr=1.0, betas=(0.0, 0.0), eps=0.0)
+    # the root of denormal numbers is within 2^-19 of theirs where v has 8 bits and more (g above 2^-71); one of few
+    # bits is corrected by whole steps of 2^-149 at most: off by 2^-150 / v in half
+    off = (-s.p.double() * g.sign() - 1.0).abs()
+    assert bool((off <= 2.0 ** -19 + 2.0 ** -149 / g.double().square()).all())
+    top = g.double().abs().view(-1, 256).amax(1)
+    assert bool(((s.scales[:, 1].double() * 448 - top).abs() <= top * (2.0 ** -18 + 2.0 ** -149 / top.square())).all())
 
 
 class Eight:
