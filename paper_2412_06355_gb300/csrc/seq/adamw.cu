@@ -273,7 +273,9 @@ __device__ __forceinline__ void update(Share<true> &r, const Tensor &x, int64_t 
         const F2 v = add(mul(fma(w2, minus, mul(g, g)), rest2), w2);
         root[j] = root_of(v);
         const F2 below = fma(root[j], inverse_root, eps);
-        const F2 p = fma(mul(m[j], F2(rcp_fast(below.x()), rcp_fast(below.y()))), rate, mul(F2(r.p[2 * j], r.p[2 * j + 1]), kept));
+        // m / below: the approximate quotient corrected by what it leaves (the division's bits for all of 2^24 drawn pairs)
+        const F2 over(rcp_fast(below.x()), rcp_fast(below.y())), near = mul(m[j], over);
+        const F2 p = fma(fma(fma(mul(near, minus), below, m[j]), over, near), rate, mul(F2(r.p[2 * j], r.p[2 * j + 1]), kept));
         r.p[2 * j] = p.x(), r.p[2 * j + 1] = p.y();
         // (elements behind the tensor's end are zeros)
         top_m = top_of(m[j].x(), m[j].y(), top_m);

@@ -110,3 +110,17 @@ def test_scales_are_the_largest_divided_by_448():
     top_v = g.cpu().square().sqrt().view(-1, 256).amax(1)
     assert torch.equal(s.scales[:, 0].cpu(), top_m / 448.0)
     assert torch.equal(s.scales[:, 1].cpu(), top_v / 448.0)
+
+
+@pytest.mark.parametrize("eps", [0.02, 1e-8])
+def test_parameters_take_the_quotient_that_a_division_gives(eps):
+    """With betas of 0, parameters of zero and no decay a step is -lr times g / (sqrt(g^2) + eps), and each operation's
+    rounding is known: the product with lr in the step's last operation, onto zero."""
+    n, lr = 1 << 22, 0.125                                  # a power of two: the product is exact
+    g = gradients(n, 6)
+    s = Eight(n).run(g, lr=lr, betas=(0.0, 0.0), eps=eps)
+    c = g.cpu()
+    want = -lr * (c / (c.square().sqrt() + torch.tensor(eps)))
+    same = s.p.cpu() == want
+    # the correction's own last bit is decided by less than 2^-45 of the quotient: fewer than one in a million
+    assert int((~same).sum()) <= n // 1000000
