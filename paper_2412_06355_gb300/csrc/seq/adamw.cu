@@ -251,10 +251,10 @@ __device__ __forceinline__ void update(Share<false> &r, const Tensor &x, int64_t
     store8<WIDE>(r.m, static_cast<float *>(x.m) + at, lane, left);
     store8<WIDE>(r.v, static_cast<float *>(x.v) + at, lane, left);
 }
-// With states in 8 bits it is instructions that bound the step, so they work on pairs. What a code is drawn from is
-// rounded as the formulas' own operations are, one by one: a last bit that differs decides one code in a million
-// otherwise. (2^29 elements: 1600 us; one by one and
-// with each code's exponent looked at, 100 instructions an element, 2090.)
+// With states in 8 bits it is instructions that bound the step, so they work on pairs. m, v and the root are within an
+// ulp or two of the formulas' operations rounded one by one (the assembler joins products with sums), which decides one
+// code in a million. (2^29 elements: 1657 us; one by one and with each code's exponent looked at, 100 instructions an
+// element, 2090.)
 template <bool WIDE>
 __device__ __forceinline__ void update(Share<true> &r, const Tensor &x, int64_t at, int lane, const Scalars &c, const Step &s, uint32_t start) {
     const int left = r.left;

@@ -124,3 +124,95 @@ def test_parameters_take_the_quotient_that_a_division_gives(eps):
     same = s.p.cpu() == want
     # the correction's own last bit is decided by less than 2^-45 of the quotient: fewer than one in a million
     assert int((~same).sum()) <= n // 1000000
+
+
+# ------------------------------------------------------------------ the draw, as the formulas have it
+def mixed(h):
+    """32-bit integers held in 64 bits, scrambled."""
+    h = ((h ^ (h >> 16)) * 0x6A09E667) & 0xFFFFFFFF
+    h = ((h ^ (h >> 15)) * 0xADF85459) & 0xFFFFFFFF
+    return h ^ (h >> 16)
+
+
+def random_numbers(seed, step, index, n):
+    """Two numbers in (0, 1) for each element, of 16 bits each: from seed, step, the tensor's and the element's place."""
+    t = lambda v: torch.tensor(v, dtype=torch.int64, device="cuda")
+    start = mixed((mixed(t((step * 0x9E3779B1 + seed) & 0xFFFFFFFF)) + index) & 0xFFFFFFFF)
+    h = mixed((torch.arange(n, device="cuda") * 0x9E3779B1 + start) & 0xFFFFFFFF)
+    return ((h & 0xFFFF).float() + 0.5) / 65536.0, ((h >> 16).float() + 0.5) / 65536.0
+
+
+def drawn(x, u, squared):
+    """(values of the codes, scales): the largest of 256 becomes 448, the upper neighbour where u is below the share that
+    makes the expectation of the value, or of its square, right."""
+    blocks = x.view(-1, 256)
+    top = blocks.abs().amax(1, keepdim=True)
+    value = (blocks * (torch.full_like(top, 448.0) / top)).abs().view(-1)
+    step = torch.exp2((torch.frexp(value.clamp_min(2.0 ** -6)).exponent - 4).float())
+    low = torch.floor(value / step) * step
+    share = (value - low) * (value + low) / (step * (2.0 * low + step)) if squared else (value - low) / step
+    return torch.copysign(torch.where(u < share, low + step, low).clamp_max(448.0), x), (top / torch.full_like(top, 448.0))[:, 0]
+
+
+def decoded(codes, scale):
+    return codes.float() * scale.repeat_interleave(256)
+
+
+@pytest.mark.parametrize("seed,first", [(0, 0), (77, 3), (2 ** 32 - 1, 1)])
+def test_codes_are_drawn_as_the_formulas_say(seed, first):
+    """Five steps, each from the library's own states before. The library may join a product with the sum behind it, so
+    its m and v are within two last bits (2^-22) of those rounded one by one here. That moves a scale by as much, and a
+    value by as much of itself, which is 16 steps of a code at most: 2^-18 of a step, for the value and for the block's
+    largest each, so that a draw may fall on the other side in 2^-17 of the elements at most (8 in a million)."""
+    n = 1 << 20
+    s, rest = Eight(n, seed, first=first), [torch.tensor(v, device="cuda") for v in (1.0 - 0.9, 1.0 - 0.999)]
+    for step in range(1, 6):
+        g = gradients(n, 20 + step)
+        m, v = decoded(s.m, s.scales[:, 0]), decoded(s.v, s.scales[:, 1]).square()
+        s.run(g)
+        um, uv = random_numbers(seed, step, first, n)
+        for got, scale, x, u, squared in ((s.m, s.scales[:, 0], m + rest[0] * (g - m), um, False),
+                                          (s.v, s.scales[:, 1], (v + rest[1] * (g.square() - v)).sqrt(), uv, True)):
+            want, want_scale = drawn(x, u, squared)
+            assert bool(((scale - want_scale).abs() <= want_scale * 2.0 ** -22).all())
+            assert int((got.float() != want).sum()) <= n * 2.0 ** -17, (step, squared)
+
+
+def test_codes_depend_on_seed_step_and_place():
+    """Equal states and gradients: a third of the codes differ with the seed, the step, the tensor's place in the list,
+    and from one half of a tensor to the other (a share s gives 2 s (1 - s); its mean over even shares is 1/3)."""
+    n = 1 << 16
+    g = gradients(n // 2, 9).repeat(2)
+    base = Eight(n).run(g)
+    late = Eight(n)
+    late.step.fill_(5)                                      # scales and shares are the same: the states start as zeros
+    others = [Eight(n, seed=1).run(g), Eight(n, first=1).run(g), late.run(g)]
+    half = Eight(n)
+    half.m, half.v = (torch.cat([t[n // 2:], t[:n // 2]]) for t in (base.m, base.v))
+    for o in (*others, half):
+        for a, b in ((base.m, o.m), (base.v, o.v)):
+            assert 0.25 < float((a.float() != b.float()).double().mean()) < 0.42
+    again = Eight(n).run(g)
+    assert torch.equal(base.m.float(), again.m.float()) and torch.equal(base.v.float(), again.v.float())
+
+
+def test_expectations_hold_over_hundreds_of_steps():
+    """m and v are linear in what they were, so codes drawn with the right expectations keep them: the mean over many
+    elements of state / float32 state is 1 within five standard errors, after 300 steps as after one."""
+    n = 1 << 19
+    scale = torch.exp2(-3.0 * torch.rand(n, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)))
+    eight = Eight(n, seed=5)
+    cfg = binding.make_adamw_config(state="f32")
+    z = [torch.zeros(n, device="cuda") for _ in range(3)]
+    step = torch.zeros(1, dtype=torch.int64, device="cuda")
+    plan = binding.adamw_plan(cfg, [z[0]], [z[1]], [z[2]])
+    for i in range(300):
+        g = gradients(n, 100 + i) * scale + scale * 0.005
+        eight.run(g)
+        binding.adamw_step(cfg, plan, [g], step)
+    v = decoded(eight.v, eight.scales[:, 1]).double().square() / z[2].double()
+    m = (decoded(eight.m, eight.scales[:, 0]).double() - z[1].double()) / z[2].double().sqrt()
+    for name, x, mean in (("v", v, 1.0), ("m", m, 0.0)):
+        error = float(x.std()) / n ** 0.5
+        # 16 random bits at their middle: no bias of their own; 300 steps of float32 roundings, 2^-24 each
+        assert abs(float(x.mean()) - mean) < 5 * error + 300 * 2.0 ** -24, (name, float(x.mean()), error)
