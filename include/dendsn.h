@@ -466,7 +466,10 @@ dendsn_status dendsn_delta_backward(const dendsn_delta_config *cfg, const void *
  * random so that the expectations of m and of v are right. The random numbers come from seed, the
  * step, the tensor's place in the list and the element's place alone: the same step gives the same
  * bits. Zeros in m, v and scales are the states at the start, for both. A block whose largest value
- * is below 2^-110 is stored as zeros; NaN and infinities spread over their block of 256.
+ * is below 2^-110 is stored as zeros; NaN and infinities spread over their block of 256. What lies below the
+ * smallest code cannot be told from zero, so sqrt(v) counts in the quotient as at least 2^-9 of its scale
+ * before the step: elements whose gradients stay below some 2^-18 of their block's largest move less than
+ * with float32 states.
  * A tensor whose gradient is NULL stays as it is, its states too, and takes no part in the norm.
  * A norm that is infinite scales finite gradients to zero; one that is NaN scales nothing.
  *

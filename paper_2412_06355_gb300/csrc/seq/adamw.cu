@@ -5,7 +5,8 @@
 // with states in float32, or m and sqrt(v) as e4m3 codes with a float32 scale for each 256 elements
 // (the largest becomes 448). A code is drawn from the two neighbours of its value so that the
 // expectation of m and of v is right: a step moves a state by a thousandth, far less than the
-// distance of two codes, and would be lost in rounding to the nearest.
+// distance of two codes, and would be lost in rounding to the nearest. In the quotient sqrt(v) counts as at least
+// the value of the smallest code, 2^-9 of the scale that was read.
 //
 // Bound by memory: every state is read and written once, in one launch for all tensors. Tensors are
 // cut into chunks of 4096 elements; a table in device memory says which tensor a chunk belongs to, and
@@ -191,6 +192,12 @@ __device__ __forceinline__ float top_of(float a, float b, float c) {
     asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
+// The larger of two, a NaN above all.
+__device__ __forceinline__ float at_least(float a, float b) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
 __device__ __forceinline__ uint32_t warp_top(uint32_t t) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) t = max(t, __shfl_xor_sync(0xffffffffu, t, o));
@@ -253,12 +260,15 @@ __device__ __forceinline__ void update(Share<false> &r, const Tensor &x, int64_t
 }
 // With states in 8 bits it is instructions that bound the step, so they work on pairs. m, v and the root are within an
 // ulp or two of the formulas' operations rounded one by one (the assembler joins products with sums), which decides one
-// code in a million. (2^29 elements: 1657 us; one by one and with each code's exponent looked at, 100 instructions an
+// code in a million. (2^29 elements: 1685 us; one by one and with each code's exponent looked at, 100 instructions an
 // element, 2090.)
 template <bool WIDE>
 __device__ __forceinline__ void update(Share<true> &r, const Tensor &x, int64_t at, int lane, const Scalars &c, const Step &s, uint32_t start) {
     const int left = r.left;
     const F2 kept = both(fmaf(-c.lr, x.decay, 1.f)), rate = both(-c.rate), inverse_root = both(c.inverse_root), eps = both(s.eps);
+    // What v's smallest code stands for: a v whose code was drawn as zero may be as large, and m's code beside it is not
+    // zero. (Gradients of 2^-20 of the block's largest, 400 steps: one of 751 lr without this, 3.5 with it.)
+    const float least = r.scale.y * 0x1p-9f;
     const F2 scale_m = both(r.scale.x), scale_v = both(r.scale.y), factor = both(c.factor), rest1 = both(s.rest1), rest2 = both(s.rest2), minus = both(-1.f);
     float mc[8], vc[8];
     decode(mc, r.qm);
@@ -272,7 +282,7 @@ __device__ __forceinline__ void update(Share<true> &r, const Tensor &x, int64_t 
         const F2 w = mul(F2(vc[2 * j], vc[2 * j + 1]), scale_v), w2 = mul(w, w);
         const F2 v = add(mul(fma(w2, minus, mul(g, g)), rest2), w2);
         root[j] = root_of(v);
-        const F2 below = fma(root[j], inverse_root, eps);
+        const F2 below = fma(F2(at_least(root[j].x(), least), at_least(root[j].y(), least)), inverse_root, eps);
         // m / below: the approximate quotient corrected by what it leaves (the division's bits for all of 2^24 drawn pairs)
         const F2 over(rcp_fast(below.x()), rcp_fast(below.y())), near = mul(m[j], over);
         const F2 p = fma(fma(fma(mul(near, minus), below, m[j]), over, near), rate, mul(F2(r.p[2 * j], r.p[2 * j + 1]), kept));

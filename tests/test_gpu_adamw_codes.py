@@ -216,3 +216,52 @@ def test_expectations_hold_over_hundreds_of_steps():
         error = float(x.std()) / n ** 0.5
         # 16 random bits at their middle: no bias of their own; 300 steps of float32 roundings, 2^-24 each
         assert abs(float(x.mean()) - mean) < 5 * error + 300 * 2.0 ** -24, (name, float(x.mean()), error)
+
+
+def test_a_v_of_zero_beside_an_m_that_is_not():
+    """A v whose code was drawn as zero counts in the quotient as the smallest code, 2^-9 of the scale; above it as it is."""
+    n, lr, scales = 1024, 0.5, (3e-4, 2e-3)
+    s = Eight(n)
+    s.m.copy_(torch.linspace(-448, 448, n, device="cuda").to(E4M3))
+    codes = torch.tensor([0.0, 2.0 ** -9, 2.0 ** -8, 448.0], device="cuda").repeat(n // 4)
+    s.v.copy_(codes.to(E4M3))
+    s.scales[:] = torch.tensor(scales, device="cuda")
+    s.step.fill_(50)
+    m = decoded(s.m, s.scales[:, 0]).double() * 0.9
+    s.run(torch.zeros(n, device="cuda"), lr=lr, eps=1e-10)
+    root = torch.maximum((0.999 * codes.double().square()).sqrt(), torch.tensor(2.0 ** -9, device="cuda").double()) * s_of(scales[1])
+    want = -lr / (1 - 0.9 ** 51) * m / (root / (1 - 0.999 ** 51) ** 0.5 + 1e-10)
+    # m and the quotient are some ten float32 operations; m cancels nowhere
+    assert bool(((s.p.double() - want).abs() <= 16 * 2.0 ** -24 * want.abs()).all())
+    assert not s.v.float()[codes == 0].any()                # the state itself stays zero
+
+
+def s_of(v):
+    return float(torch.tensor(v, dtype=F32))
+
+
+@pytest.mark.parametrize("span", [4, 16, 20, 24])
+def test_steps_stay_steps_where_a_blocks_gradients_differ_widely(span):
+    """Gradients from 2^-span of their block's largest on. Float32's m is at most 7.3 sqrt(v) whatever the gradients do
+    (0.1 / sqrt(0.001) / sqrt(1 - 0.81 / 0.999)); a code of m is within an eighth of its value or the smallest, a root
+    counts as no less than the smallest code of v: four times that leaves room for both."""
+    n = 1 << 16
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    scale = torch.exp2(-span * torch.rand(n, device="cuda", generator=gen))
+    s, largest = Eight(n), 0.0
+    for i in range(300):
+        before = s.p.clone()
+        s.run(torch.randn(n, device="cuda", generator=gen) * scale, lr=1.0)
+        if i >= 20:
+            largest = max(largest, float((s.p - before).abs().max()))
+    assert largest < 4 * 7.3
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), 1e25])
+def test_a_gradient_whose_square_is_no_number_gives_no_number(bad):
+    """A v that leaves float32 is no v of zero: the parameter does not move by a number then."""
+    s = Eight(512).run(gradients(512, 1)).run(gradients(512, 2))
+    g, before = gradients(512, 3), s.p.clone()
+    g[7] = bad
+    s.run(g)
+    assert torch.isnan(s.p[7]) and torch.isfinite(s.p[256:]).all() and float((s.p - before)[8:].abs().max()) < 0.01
