@@ -1036,8 +1036,8 @@ def _new_norm(like, stream=None):
 def adamw_step(cfg, plan, grads, step, lr=None, norm=None, stream=None):
     """One step in place. grads: a tensor or None (left as it is) for each of the plan's params, float32
     or bfloat16; step: int64 tensor [1] on the device, counted up; lr: float32 tensor [1] on the device
-    that stands in for cfg's. Returns the gradients' norm (float32 [1]; `norm` itself where given) where
-    the config clips, else None."""
+    that stands in for cfg's. A graph that captures the call needs the plan for as long as it is replayed.
+    Returns the gradients' norm (float32 [1]; `norm` itself where given) where the config clips, else None."""
     n = plan.count
     if cfg.state != plan.state:
         raise ValueError("the config's state is not the plan's")

@@ -7,13 +7,15 @@ from . import binding
 
 
 class AdamW(torch.optim.Optimizer):
-    """AdamW whose step is one launch over all tensors (two where it clips).
+    """AdamW whose step is one launch over all tensors (two where it clips; for each 500 tensors).
 
     params: float32 or bfloat16 parameters on one CUDA device, or groups of them; groups may differ in
     weight_decay, the other options are one for all (a scheduler may change lr). state: m and v as "f32"
     or as "e4m3" codes with scales of 256 elements. max_norm: gradients are scaled down to this norm over
     all parameters (0: not); the last step's norm is in `grad_norm`, a tensor on the device. seed: of the
-    random rounding of e4m3 states. A parameter without a gradient stays as it is.
+    random rounding of e4m3 states. A parameter without a gradient stays as it is. A step in a CUDA graph goes on
+    with the lr, the weight decays and the gradients' memory that it was captured with; one step has to be made
+    before, outside the graph.
     """
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, state="f32",
@@ -30,6 +32,7 @@ class AdamW(torch.optim.Optimizer):
         self._scales = [like(p, ((p.numel() + 255) // 256, 2), torch.float32) for p in ps] if self._eight else None
         self._step = torch.zeros(1, dtype=torch.int64, device=ps[0].device)
         self._plan, self._of = None, None
+        self._captured = []          # plans whose tables CUDA graphs go on using
         self.grad_norm = None
 
     def _params(self):
@@ -59,6 +62,8 @@ class AdamW(torch.optim.Optimizer):
                                             weight_decay=decays)
             self._of = of
         grads = [p.grad if p.grad is None or p.grad.is_contiguous() else p.grad.contiguous() for p in ps]
+        if torch.cuda.is_current_stream_capturing() and self._plan not in self._captured:
+            self._captured.append(self._plan)
         self.grad_norm = binding.adamw_step(cfg, self._plan, grads, self._step)
         return loss
 
