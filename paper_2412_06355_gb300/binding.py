@@ -937,6 +937,14 @@ def delta_backward(cfg, q, k, v, gate, beta, grad_o, offsets=None, s0=None, grad
     return out
 
 
+def _refuse_overlaps(parts):
+    """parts: (address, bytes, name) of what a step writes."""
+    parts = sorted(p for p in parts if p[1])
+    for (at, size, name), (after, _, other) in zip(parts, parts[1:]):
+        if after < at + size:
+            raise ValueError(f"{other} lies in the memory of {name}: the step would update it twice")
+
+
 class AdamwPlan:
     """Tensors of an AdamW step and their table in device memory. Holds the tensors alive."""
 
@@ -952,7 +960,7 @@ class AdamwPlan:
         for name, x in lists:
             if len(x) != n:
                 raise ValueError(f"{name}: {len(x)} entries for {n} params")
-        entries = (dendsn_adamw_tensor * n)()
+        entries, written = (dendsn_adamw_tensor * n)(), []
         for i, p in enumerate(params):
             _dtype_name(p)
             state = E4M3 if eight else torch.float32
@@ -969,8 +977,11 @@ class AdamwPlan:
                 ptrs = [None] * 5
             else:
                 ptrs = _pointers(p, ms[i], vs[i], scale, copy)
+            written += [(at, t.numel() * t.element_size(), f"{name} of tensor {i}") for at, t, name in
+                        zip(ptrs, (p, ms[i], vs[i], scale, copy), ("param", "m", "v", "scales", "copy")) if at]
             entries[i] = dendsn_adamw_tensor(*ptrs, p.numel(), decays[i],
                                              BF16 if p.dtype is torch.bfloat16 else F32, 0)
+        _refuse_overlaps(written)
         need = ctypes.c_size_t(0)
         _check("dendsn_adamw_plan",
                load().dendsn_adamw_plan(ctypes.byref(cfg), entries, n, None, ctypes.byref(need)))
@@ -993,7 +1004,8 @@ class AdamwPlan:
 def adamw_plan(cfg, params, ms, vs, scales=None, copies=None, weight_decay=0.0) -> AdamwPlan:
     """The plan of a step over `params` (float32 or bfloat16) with their states m and v (float32, or
     e4m3 with scales [ceil(n / 256), 2]); copies: bfloat16 tensors that receive the new parameters too
-    (entries may be None); weight_decay: one for all or one each. All states start as zeros."""
+    (entries may be None); weight_decay: one for all or one each. All states start as zeros. Tensors that share
+    memory are refused."""
     return AdamwPlan(cfg, list(params), list(ms), list(vs), None if scales is None else list(scales),
                      None if copies is None else list(copies), weight_decay)
 
