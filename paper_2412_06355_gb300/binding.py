@@ -1247,7 +1247,7 @@ class NormFunction(torch.autograd.Function):
         D = x.shape[-1]
         ctx.cfg = make_norm_config(x.numel() // D if D else 0, D, _dtype_name(x), eps)
         y, total, _ = norm_forward(ctx.cfg, x, weight, None if residual is None else residual.contiguous())
-        ctx.added = residual is not None
+        ctx.residual_shape = None if residual is None else residual.shape     # rows of D, however they are laid out
         ctx.save_for_backward(total, weight)
         ctx.set_materialize_grads(False)
         return y, total
@@ -1260,7 +1260,8 @@ class NormFunction(torch.autograd.Function):
             return None, None, None, None
         gy = torch.zeros_like(total) if gy is None else gy.contiguous()
         g = norm_backward(ctx.cfg, total, weight, gy, None if gsum is None else gsum.contiguous())
-        return g["gx"], g["gx"] if ctx.added else None, g["gweight"], None
+        gx = g["gx"]
+        return gx, None if ctx.residual_shape is None else gx.view(ctx.residual_shape), g["gweight"], None
 
 
 class DeltaFunction(torch.autograd.Function):
