@@ -51,30 +51,16 @@ __device__ __forceinline__ void fetch4(uint32_t (&r)[4], uint32_t addr) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
-__device__ __forceinline__ void fetch4_turned(uint32_t (&r)[4], uint32_t addr) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
-}
 // Right factor, 16 summed places from block `k` and 16 columns from block `n`, of a tile whose rows are
-// the columns (`width` blocks a row), or whose rows are the summed places. r[0], r[1] are the first 8
-// columns', r[2], r[3] the others'.
+// the columns (`width` blocks a row). r[0], r[1] are the first 8 columns', r[2], r[3] the others'.
 __device__ __forceinline__ void right_rows(uint32_t (&r)[4], uint32_t tile, int width, int n, int k) {
     const int lane = threadIdx.x & 31, m = lane >> 3;
     fetch4(r, tile + ((n + (m >> 1)) * width + k + (m & 1)) * kCell + (lane & 7) * 16);
 }
-__device__ __forceinline__ void right_columns(uint32_t (&r)[4], uint32_t tile, int width, int k, int n) {
-    const int lane = threadIdx.x & 31, m = lane >> 3;
-    fetch4_turned(r, tile + ((k + (m & 1)) * width + n + (m >> 1)) * kCell + (lane & 7) * 16);
-}
-// Left factor, 16 rows from block `i` and 16 summed places from block `k`, of a tile whose rows are the
-// rows, or whose rows are the summed places.
+// Left factor, 16 rows from block `i` and 16 summed places from block `k`, of a tile whose rows are the rows.
 __device__ __forceinline__ void left_rows(uint32_t (&a)[4], uint32_t tile, int width, int i, int k) {
     const int lane = threadIdx.x & 31, m = lane >> 3;
     fetch4(a, tile + ((i + (m & 1)) * width + k + (m >> 1)) * kCell + (lane & 7) * 16);
-}
-__device__ __forceinline__ void left_columns(uint32_t (&a)[4], uint32_t tile, int width, int k, int i) {
-    const int lane = threadIdx.x & 31, m = lane >> 3;
-    fetch4_turned(a, tile + ((k + (m >> 1)) * width + i + (m & 1)) * kCell + (lane & 7) * 16);
 }
 
 // Adds to the 16 x 16 results c0, c1 the product of a left factor in NA terms and a right one in NB: the

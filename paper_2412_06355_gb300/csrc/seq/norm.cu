@@ -79,7 +79,8 @@ __device__ __forceinline__ float2 scale_of(uint32_t top) {
     const float s = t * (1.f / 448.f);
     return make_float2(s, __frcp_rn(s));
 }
-// v / scale as the division rounds it: a code is decided by the quotient's last bits only.
+// v / scale as the division rounds it (the approximate quotient corrected by what it leaves, Markstein's division step): a
+// code is decided by the quotient's last bits only.
 __device__ __forceinline__ float scaled(float v, float2 s) {
     const float q = v * s.y;
     return fmaf(fmaf(-q, s.x, v), s.y, q);

@@ -48,10 +48,6 @@ template <> struct Lot<__nv_bfloat16, 1> {
     }
     __device__ __forceinline__ void zero() { r = 0; }
 };
-// Elements as they are between two steps of one kernel: a value rounded to T and taken up again.
-template <typename T> __device__ __forceinline__ float rounded(float v);
-template <> __device__ __forceinline__ float rounded<float>(float v) { return v; }
-template <> __device__ __forceinline__ float rounded<__nv_bfloat16>(float v) { return __bfloat162float(__float2bfloat16_rn(v)); }
 
 // Two values as e4m3 codes, rounded to nearest even, at most 448 in size.
 __device__ __forceinline__ uint16_t e4m3_pair(float lo, float hi) {
