@@ -142,3 +142,28 @@ def test_gk_reads_the_chunks_matrices_in_three_terms(dtype):
     got, want, _ = run(dtype, T, Dk, k=k, beta=beta, v=v, glast=glast)
     dot = (glast[:, None, :, 0].double() * v.to(DT[dtype]).double()).sum(-1) * beta.double()
     small("gk", got["gk"][:, :20, :, 0], want["gk"][:, :20, :, 0], 2 * dot[:, :20])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gq_reads_the_state_in_three_terms(dtype):
+    a, go = rand(13, B, H, 64), torch.zeros(B, 9, H, 2, device="cuda")
+    go[..., 0], go[..., 1] = 1, -1
+    got, want, _ = run(dtype, 9, 64, 2, go=go, s0=torch.stack([a, a * (1 + EPS)], 3))
+    small("gq", got["gq"], want["gq"], 2 * a.double()[:, None])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gq_reads_the_chunks_matrix_in_three_terms(dtype):
+    """Two tokens write along keys that cancel each other for every later token's gradient: A_i0 k_0 + A_i1 k_1."""
+    T, Dk = 40, 8
+    k, v, beta = torch.zeros(B, T, H, Dk, device="cuda"), torch.zeros(B, T, H, DV, device="cuda"), rand(14, B, T, H) / 2
+    half = torch.tensor([1.0, -1.0] * (Dk // 2), device="cuda") / 256        # so short that token 1 reads 2^-13 of what token 0 wrote
+    k[:, 0], k[:, 1] = half, -half
+    v[:, 0] = v[:, 1] = rand(15, B, H, DV)
+    beta[:, 1] = beta[:, 0] * (1 + EPS)
+    go = rand(16, B, T, H, DV)
+    gate = torch.zeros(B, T, H, device="cuda")
+    gate[:, 1] = -EPS / 2
+    got, want, _ = run(dtype, T, Dk, k=k, v=v, beta=beta, gate=gate, go=go)
+    dot = (go.to(DT[dtype]).double() * v[:, :1].to(DT[dtype]).double()).sum(-1) * beta[:, :1].double()
+    small("gq", got["gq"][:, 2:], want["gq"][:, 2:], (2 * dot[:, 2:, :, None] / 256).expand(B, T - 2, H, Dk))
