@@ -938,11 +938,12 @@ def delta_backward(cfg, q, k, v, gate, beta, grad_o, offsets=None, s0=None, grad
 
 
 def _refuse_overlaps(parts):
-    """parts: (address, bytes, name) of what a step writes."""
+    """parts: (address, bytes, what, tensor) of what a step writes."""
     parts = sorted(p for p in parts if p[1])
-    for (at, size, name), (after, _, other) in zip(parts, parts[1:]):
+    for (at, size, *one), (after, _, *other) in zip(parts, parts[1:]):
         if after < at + size:
-            raise ValueError(f"{other} lies in the memory of {name}: the step would update it twice")
+            raise ValueError("{} of tensor {} lies in the memory of {} of tensor {}: the step would update it twice"
+                             .format(*other, *one))
 
 
 class AdamwPlan:
@@ -977,8 +978,9 @@ class AdamwPlan:
                 ptrs = [None] * 5
             else:
                 ptrs = _pointers(p, ms[i], vs[i], scale, copy)
-            written += [(at, t.numel() * t.element_size(), f"{name} of tensor {i}") for at, t, name in
-                        zip(ptrs, (p, ms[i], vs[i], scale, copy), ("param", "m", "v", "scales", "copy")) if at]
+            sizes = p.numel() * p.element_size(), p.numel() * (1 if eight else 4), (p.numel() + 255) // 256 * 8, p.numel() * 2
+            written += [(at, size, what, i) for at, size, what in
+                        zip(ptrs, (sizes[0], sizes[1], *sizes[1:]), ("param", "m", "v", "scales", "copy")) if at]
             entries[i] = dendsn_adamw_tensor(*ptrs, p.numel(), decays[i],
                                              BF16 if p.dtype is torch.bfloat16 else F32, 0)
         _refuse_overlaps(written)

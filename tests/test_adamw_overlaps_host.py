@@ -5,11 +5,14 @@ from paper_2412_06355_gb300 import binding
 
 
 def test_parts_that_meet_are_no_overlap():
-    binding._refuse_overlaps([(64, 32, "b"), (0, 64, "a"), (96, 0, "empty"), (96, 4, "c"), (80, 0, "empty too")])
+    binding._refuse_overlaps([(64, 32, "m", 1), (0, 64, "param", 0), (96, 0, "v", 2), (96, 4, "copy", 3), (80, 0, "m", 4)])
 
 
-@pytest.mark.parametrize("parts", [[(64, 32, "b"), (0, 65, "a")], [(8, 8, "a"), (8, 8, "b")], [(0, 100, "a"), (10, 1, "b")],
-                                   [(300, 4, "z"), (200, 101, "y"), (0, 4, "x")]])
-def test_overlaps_are_refused_by_name(parts):
-    with pytest.raises(ValueError, match="lies in the memory of"):
+@pytest.mark.parametrize("parts,message", [
+    ([(64, 32, "m", 1), (0, 65, "param", 0)], "m of tensor 1 lies in the memory of param of tensor 0"),
+    ([(8, 8, "m", 0), (8, 8, "v", 0)], "v of tensor 0 lies in the memory of m of tensor 0"),
+    ([(0, 100, "param", 0), (10, 1, "copy", 5)], "copy of tensor 5"),
+    ([(300, 4, "scales", 2), (200, 101, "v", 1), (0, 4, "m", 0)], "scales of tensor 2 lies in the memory of v of tensor 1")])
+def test_overlaps_are_refused_by_name(parts, message):
+    with pytest.raises(ValueError, match=message):
         binding._refuse_overlaps(parts)
