@@ -377,7 +377,8 @@ dendsn_status dendsn_xent_backward(const dendsn_xent_config *cfg, const void *hi
  * out SAME: y [M, D] in x_dtype. out E4M3: y [M, D] one-byte e4m3 codes with scales [M, groups]
  * float32, value = code * scale: one scale for a row (group 0) or for each 128 columns (group 128; the
  * last one may have fewer). The largest of a group becomes 448; a group whose values are all below
- * 2^-100 has scale 1. NaN and infinities stay within their row (its sum's mean takes them in).
+ * 2^-100 has scale 1. NaN and infinities stay within their row (its sum's mean takes them in). The mean is
+ * formed in float32: rows whose squares' sum leaves it (values of some 2^60) give y = 0.
  * Backward, from sum: grad_x (the gradient of x and of residual alike), grad_sum added where it is
  * not NULL (what reached sum by another way), and grad_weight summed over the rows.
  *   x, residual, sum, grad_y, grad_sum, grad_x  [M, D] x_dtype;  weight, grad_weight [D] float32
@@ -458,7 +459,7 @@ dendsn_status dendsn_delta_backward(const dendsn_delta_config *cfg, const void *
  *   g = grad * min(1, max_norm / |grads|)     |grads|: over all tensors; max_norm 0: no clipping
  *   m += (1 - beta1) (g - m);  v += (1 - beta2) (g^2 - v);  t = step + 1
  *   param = param (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + eps)
- * all in float32, rounded once where param or copy is bfloat16 (copy: bfloat16 copy of param for the
+ * all in float32 (a product and the sum behind it may be joined), rounded once where param or copy is bfloat16 (copy: bfloat16 copy of param for the
  * next forward, or NULL).
  * state F32: m and v float32 [n]. state E4M3: m and sqrt(v) as one-byte e4m3 codes [n], scales
  * float32 [ceil(n / 256), 2] (of m, of sqrt(v)) of 256 elements each, value = code * scale; the

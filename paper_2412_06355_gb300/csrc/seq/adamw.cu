@@ -33,8 +33,8 @@ constexpr int kThreads = 256;
 constexpr int kGrads = 500;            // tensors of a launch: their gradients' addresses are its arguments
 constexpr int kMostBlocks = 152 * 4;   // sums of squares a step can have; blocks of the norm's launch
 // Blocks of the update on an SM. Float32 states are bound by memory: 24 warps of 80 registers (16 of 128: 730 us
-// against 660 at 2^27 elements). With states in 8 bits 16 warps without a spill are faster (2^29 elements, in an
-// earlier form: 1420 us against 1630).
+// against 660 at 2^27 elements). With states in 8 bits 16 warps of 128 registers with three pieces on their way are
+// faster than 24 of 80 with two (2^29 elements: 1680 us against 1910).
 constexpr int resident(bool eight) { return eight ? 2 : 3; }
 constexpr uint32_t kStride = 0x9E3779B1u;
 

@@ -110,7 +110,7 @@ __device__ __forceinline__ void put_minus(float *x, const float (&r)[2][4]) {
 // One block of 128 threads for a chunk and value head: tiles of k and q (by the first value head of a
 // key head), the gates' sums and exponentials, P, and the inverses (1 + L diag(b))^-1 and, for the
 // backward, (1 + diag(b) L)^-1: diagonal blocks of 16 by substitution, a thread a column; then twice the corner of
-// [[A, 0], [B, D]]^-1 = [[A^-1, 0], [-D^-1 B A^-1, D^-1]], on the matrix instruction. (4096 chunks of 128 places: 138 us,
+// [[A, 0], [B, D]]^-1 = [[A^-1, 0], [-D^-1 B A^-1, D^-1]], on the matrix instruction. (4096 chunks of 128 places: 136 us,
 // 0.4 GB moved; with substitution over all 64 rows 230.)
 template <typename T, int DKP, bool KEEP>
 __global__ void __launch_bounds__(128) delta_prepare_kernel(const __grid_constant__ Args a, const T *q, const T *k, const float *gate,
@@ -389,8 +389,9 @@ __device__ __forceinline__ float sums_of(float (&v)[16]) {
 // columns: S go, S y and D e, over rounds of 32 columns of v, with A and C's sums beside them (rows: tokens of go, of
 // y); then those within the chunk. A warp has 8 tokens of a round's go, v, y and e, a lane one column of v. Two blocks
 // share an SM (bfloat16), so that one's loads go on beside the other's products. Gradients of shared heads go out in
-// float32 for each value head and are added up by delta_join_kernel. (4096 chunks of 128 x 128, bfloat16: 366 us,
-// 1.3 GB moved; bound by instructions and latency. With mma.sync, eight warps an SM: 760.)
+// float32 for each value head and are added up by delta_join_kernel. (4096 chunks of 128 x 128, bfloat16: 386 us,
+// 1.3 GB moved; bound by instructions and latency. In two terms where only gk comes of them 366; with mma.sync, eight warps
+// an SM, 760.)
 // The matrix instruction cuts its sums off where it should round: every addition onto a large sum costs up to 2^-23 of
 // it. So the small products come first, in sums of their own where all of tensor memory is one block's (float32), and
 // what is added within the chunk is summed by itself.
