@@ -459,8 +459,8 @@ dendsn_status dendsn_delta_backward(const dendsn_delta_config *cfg, const void *
  *   g = grad * min(1, max_norm / |grads|)     |grads|: over all tensors; max_norm 0: no clipping
  *   m += (1 - beta1) (g - m);  v += (1 - beta2) (g^2 - v);  t = step + 1
  *   param = param (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + eps)
- * all in float32 (a product and the sum behind it may be joined), rounded once where param or copy is bfloat16 (copy: bfloat16 copy of param for the
- * next forward, or NULL).
+ * all in float32 (a product and the sum behind it may be joined), rounded once where param or copy is
+ * bfloat16 (copy: bfloat16 copy of param for the next forward, or NULL).
  * state F32: m and v float32 [n]. state E4M3: m and sqrt(v) as one-byte e4m3 codes [n], scales
  * float32 [ceil(n / 256), 2] (of m, of sqrt(v)) of 256 elements each, value = code * scale; the
  * largest of a block becomes 448, and the others are rounded to one of their two neighbours at
